@@ -106,7 +106,9 @@ typedef enum {
     MEMOROID_OP_RETURN = 6,            /* memoroid_discounted_return[_prepared]: (B, T) */
     MEMOROID_OP_GAE = 7,               /* memoroid_gae[_prepared]:            (B, T) */
     MEMOROID_OP_TBB_BEGIN_INDICES = 8, /* memoroid_tbb_begin_indices[_prepared]: (T = n) */
-    MEMOROID_OP_TBB_SAMPLE = 9         /* memoroid_tbb_sample[_prepared]:     (B = n_draws, T = batch) */
+    MEMOROID_OP_TBB_SAMPLE = 9,        /* memoroid_tbb_sample[_prepared]:     (B = n_draws, T = batch) */
+    MEMOROID_OP_RETENTION = 10,        /* memoroid_scan_retention:      (B, T, d_or_H = H, dk, dv) */
+    MEMOROID_OP_RETENTION_BWD = 11     /* memoroid_scan_retention_bwd:  (B, T, d_or_H = H, dk, dv), any Hk */
 } memoroid_op;
 
 /* Version of this header the library was built from (MEMOROID_ABI_VERSION). */
@@ -361,6 +363,91 @@ int memoroid_scan_linattn_bwd(const float* q, const float* k, const float* v,
                               float* grad_q, float* grad_k, float* grad_v,
                               int64_t T, int64_t H, int64_t dk, int64_t dv, int64_t chunk,
                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Retention: linear attention whose state decays, at a rate of its own in each
+ * head.  The linear-transformer memoroid (App. G.1) without phi and normaliser
+ * and with a decaying transition, over B tapes of T steps with H heads.  Per
+ * head, with gamma = exp(-|alpha|) as in FFM (App. G.4):
+ *     S_t = k_t^T v_t                      if step t begins an episode,
+ *     S_t = gamma S_{t-1} + k_t^T v_t      otherwise,
+ *     out_t = scale q_t S_t.
+ *
+ *   q          [B][T][H][dk];  k: [B][T][Hk][dk];  v: [B][T][Hk][dv], of
+ *              `dtype` (MEMOROID_F32 or MEMOROID_BF16).  Query head h reads key
+ *              head h / (H / Hk); H must be a multiple of Hk (MEMOROID_EINVAL).
+ *              The state is one per query head.
+ *   alpha      [H] fp32; its sign means nothing, 0 is no decay.
+ *   start      [B][T] begin flags.  Unlike in the other scans step 0 is a begin
+ *              step only if its flag says so: a tape may go on from state_in.
+ *   state_in   optional [B][H][dk][dv] fp32, the state before step 0 (NULL: 0).
+ *   out        out [B][T][H][dv] of dtype.
+ *   state_out  optional out [B][H][dk][dv] fp32, the state after step T - 1;
+ *              not written when T is 0.
+ *   scale      finite (MEMOROID_EINVAL otherwise).
+ *   dk, dv     multiples of 8 up to 128 (MEMOROID_EUNSUPPORTED otherwise);
+ *              B, H <= 65535.  Arrays 16-byte aligned.
+ *   bf16: products of bf16 inputs, fp32 states and sums; the weights of pairs and
+ *   the state as a row reads it are rounded to bf16 once each.  The states out
+ *   are fp32 results.  fp32: fp32 precision throughout.
+ *   A NaN or Inf stays in its episode and in the steps from its own on; there
+ *   an Inf may come out as NaN.
+ *   Workspace (self-initialising): memoroid_scan_retention_workspace_bytes.
+ * ------------------------------------------------------------------------ */
+size_t memoroid_scan_retention_workspace_bytes(int64_t B, int64_t T, int64_t H,
+                                               int64_t dk, int64_t dv, int dtype);
+
+int memoroid_scan_retention(const void* q, const void* k, const void* v, const float* alpha,
+                            const uint8_t* start, const float* state_in,
+                            void* out, float* state_out, float scale,
+                            int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t dk, int64_t dv, int dtype,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Gradient of retention.  With g = dL/dout and G = dL/dS_{T-1}, dS the gradient
+ * with respect to the state,
+ *     dS_t = scale q_t^T g_t + [t+1 < T and step t+1 is not a begin] gamma dS_{t+1}
+ *            + [t == T-1] G,
+ *     dq_t = scale g_t S_t^T,  dk_t = v_t dS_t^T,  dv_t = k_t dS_t  (summed over
+ *     the query heads that share a key head),
+ *     dalpha = -sign(alpha) sum over tapes and non-begin steps of gamma S_{t-1} . dS_t
+ *     (sign(0) = 0),  dstate_in = [step 0 is not a begin] gamma dS_0.
+ * States are recomputed: the forward output is not needed.
+ *
+ *   q, k, v, alpha, start, state_in, scale  as for memoroid_scan_retention.
+ *   grad_out   [B][T][H][dv] of dtype.
+ *   grad_state_out  optional [B][H][dk][dv] fp32: G (NULL: 0).
+ *   grad_q, grad_k, grad_v  out, like q, k, v.
+ *   grad_alpha optional out [H] fp32;  grad_state_in: optional out [B][H][dk][dv]
+ *              fp32.  Both are fp32 results with bf16 inputs too.
+ *   Outputs must not alias any input or each other.
+ *   Workspace (self-initialising): memoroid_scan_retention_bwd_workspace_bytes.
+ * ------------------------------------------------------------------------ */
+size_t memoroid_scan_retention_bwd_workspace_bytes(int64_t B, int64_t T, int64_t H, int64_t Hk,
+                                                   int64_t dk, int64_t dv, int dtype, int want_grad_alpha);
+
+int memoroid_scan_retention_bwd(const void* q, const void* k, const void* v, const float* alpha,
+                                const uint8_t* start, const float* state_in,
+                                const void* grad_out, const float* grad_state_out,
+                                void* grad_q, void* grad_k, void* grad_v,
+                                float* grad_alpha, float* grad_state_in, float scale,
+                                int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t dk, int64_t dv, int dtype,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * One step of retention for B rows (environments, sequences), the state updated
+ * in place:  S <- gamma S + k^T v (k^T v where the row begins an episode),
+ * out = scale q S.
+ *
+ *   q [B][H][dk], k [B][Hk][dk], v [B][Hk][dv], out [B][H][dv] of dtype;
+ *   alpha [H], state [B][H][dk][dv] fp32;  start: optional [B] begin flags (NULL:
+ *   no row begins).  Limits as for memoroid_scan_retention; B may exceed 65535
+ *   as long as B * H * ceil(dv / 32) is below 2^31.
+ * ------------------------------------------------------------------------ */
+int memoroid_retention_step(const void* q, const void* k, const void* v, const float* alpha,
+                            const uint8_t* start, float* state, void* out, float scale,
+                            int64_t B, int64_t H, int64_t Hk, int64_t dk, int64_t dv, int dtype,
+                            void* stream);
 
 /* ------------------------------------------------------------------------
  * Discounted return over a tape (App. D, the discounted-return memoroid

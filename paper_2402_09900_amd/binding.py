@@ -33,7 +33,7 @@ LIB_PATH = os.path.join(HERE, "libmemoroid.so")
 OK, EINVAL, EUNSUPPORTED, EWORKSPACE, EHIP, ETIMEOUT, EMISMATCH = 0, -1, -2, -3, -4, -5, -6
 F32, BF16, C64 = 0, 1, 2
 (OP_DIAG, OP_DIAG_BWD, OP_LINATTN, OP_LINATTN_BWD, OP_FFM, OP_FFM_BWD, OP_RETURN, OP_GAE,
- OP_TBB_BEGIN_INDICES, OP_TBB_SAMPLE) = range(10)
+ OP_TBB_BEGIN_INDICES, OP_TBB_SAMPLE, OP_RETENTION, OP_RETENTION_BWD) = range(12)
 
 _lib = None
 
@@ -109,6 +109,17 @@ def lib() -> ctypes.CDLL:
         L.memoroid_scan_diag_noalloc.argtypes = [P, I64, P, P, P, P, I64, I64, I64, I32, I32, P]
         L.memoroid_workspace_bytes.restype = SZ
         L.memoroid_workspace_bytes.argtypes = [I32, I64, I64, I64, I64, I64, I64]
+        F = ctypes.c_float
+        L.memoroid_scan_retention_workspace_bytes.restype = SZ
+        L.memoroid_scan_retention_workspace_bytes.argtypes = [I64] * 5 + [I32]
+        L.memoroid_scan_retention.restype = I32
+        L.memoroid_scan_retention.argtypes = [P] * 8 + [F] + [I64] * 6 + [I32, P, SZ, P]
+        L.memoroid_scan_retention_bwd_workspace_bytes.restype = SZ
+        L.memoroid_scan_retention_bwd_workspace_bytes.argtypes = [I64] * 6 + [I32, I32]
+        L.memoroid_scan_retention_bwd.restype = I32
+        L.memoroid_scan_retention_bwd.argtypes = [P] * 13 + [F] + [I64] * 6 + [I32, P, SZ, P]
+        L.memoroid_retention_step.restype = I32
+        L.memoroid_retention_step.argtypes = [P] * 7 + [F] + [I64] * 5 + [I32, P]
         L.memoroid_testing_set_fallback_polls.restype = I64
         L.memoroid_testing_set_fallback_polls.argtypes = [I64]
         L.memoroid_testing_tile_steps.restype = I64
@@ -291,6 +302,32 @@ def memoroid_gae_prepared(r, value, value_next, done, start, gamma, lam, adv, ta
                           workspace, workspace_bytes, stream) -> int:
     return lib().memoroid_gae_prepared(r, value, value_next, done, start, gamma, lam, adv, target, B, T,
                                        workspace, workspace_bytes, stream)
+
+
+def memoroid_scan_retention_workspace_bytes(B, T, H, dk, dv, dtype) -> int:
+    return lib().memoroid_scan_retention_workspace_bytes(B, T, H, dk, dv, dtype)
+
+
+def memoroid_scan_retention(q, k, v, alpha, start, state_in, out, state_out, scale, B, T, H, Hk, dk, dv, dtype,
+                            workspace, workspace_bytes, stream) -> int:
+    return lib().memoroid_scan_retention(q, k, v, alpha, start, state_in, out, state_out, scale, B, T, H, Hk, dk, dv,
+                                         dtype, workspace, workspace_bytes, stream)
+
+
+def memoroid_scan_retention_bwd_workspace_bytes(B, T, H, Hk, dk, dv, dtype, want_grad_alpha) -> int:
+    return lib().memoroid_scan_retention_bwd_workspace_bytes(B, T, H, Hk, dk, dv, dtype, want_grad_alpha)
+
+
+def memoroid_scan_retention_bwd(q, k, v, alpha, start, state_in, grad_out, grad_state_out, grad_q, grad_k, grad_v,
+                                grad_alpha, grad_state_in, scale, B, T, H, Hk, dk, dv, dtype, workspace,
+                                workspace_bytes, stream) -> int:
+    return lib().memoroid_scan_retention_bwd(q, k, v, alpha, start, state_in, grad_out, grad_state_out, grad_q, grad_k,
+                                             grad_v, grad_alpha, grad_state_in, scale, B, T, H, Hk, dk, dv, dtype,
+                                             workspace, workspace_bytes, stream)
+
+
+def memoroid_retention_step(q, k, v, alpha, start, state, out, scale, B, H, Hk, dk, dv, dtype, stream) -> int:
+    return lib().memoroid_retention_step(q, k, v, alpha, start, state, out, scale, B, H, Hk, dk, dv, dtype, stream)
 
 
 def memoroid_workspace_status(workspace, workspace_bytes, stream) -> int:
@@ -717,6 +754,120 @@ def scan_linattn_bwd(q, k, v, start, out, grad_out, chunk: int = 64, workspace=N
     return gq, gk, gv
 
 
+def _retention_args(q, k, v, alpha, start, scale, steps):
+    """Checked sizes of a retention call: [B,T,...] tensors (steps) or [B,...]."""
+    torch = _torch()
+    lead = 2 if steps else 1
+    if q.dim() != lead + 2 or k.dim() != lead + 2 or v.dim() != lead + 2:
+        raise ValueError("q, k, v must be %s" % ("[B,T,H,d]" if steps else "[B,H,d]"))
+    B, T = q.shape[0], (q.shape[1] if steps else 1)
+    H, dk = q.shape[lead:]
+    Hk, dv = k.shape[lead], v.shape[lead + 1]
+    if k.shape[:lead] != q.shape[:lead] or v.shape[:lead] != q.shape[:lead] or k.shape[lead + 1] != dk or \
+            v.shape[lead] != Hk:
+        raise ValueError("q must be [...,H,dk], k [...,Hk,dk] and v [...,Hk,dv]")
+    if Hk == 0 or H % Hk:
+        raise ValueError("the query heads must be a multiple of the key heads")
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise TypeError("q, k and v must share a dtype")
+    dt = _code_of(q.dtype)
+    if dt == C64:
+        raise TypeError("retention takes float32 or bfloat16")
+    if alpha.dtype != torch.float32 or alpha.shape != (H,):
+        raise TypeError("alpha must be float32 [H]")
+    if start is not None and (start.dtype != torch.uint8 or start.shape != q.shape[:lead]):
+        raise TypeError("start must be uint8 %s" % ("[B,T]" if steps else "[B]"))
+    return B, T, H, Hk, dk, dv, dt, float(dk ** -0.5 if scale is None else scale)
+
+
+def _state_like(state, name, B, H, dk, dv):
+    if state is not None and (state.dtype != _torch().float32 or state.shape != (B, H, dk, dv)):
+        raise TypeError("%s must be float32 [B,H,dk,dv]" % name)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def scan_retention(q, k, v, alpha, start, scale: Optional[float] = None, state=None, final_state: bool = False,
+                   workspace=None):
+    """Retention (linear attention with a decay per head) over B tapes:
+    S_t = exp(-|alpha|) S_{t-1} + k_t^T v_t, without the first term at a begin
+    step, and out_t = scale q_t S_t (scale: dk^-0.5 by default).
+
+    q: [B,T,H,dk]; k: [B,T,Hk,dk]; v: [B,T,Hk,dv], float32 or bfloat16, query
+    head h on key head h // (H // Hk); alpha: float32 [H]; start: uint8 [B,T];
+    state: optional float32 [B,H,dk,dv], the state before step 0 (which begins
+    an episode only if its flag says so).  Returns out [B,T,H,dv], plus the
+    float32 state after the last step when final_state is true."""
+    torch = _torch()
+    B, T, H, Hk, dk, dv, dt, scale = _retention_args(q, k, v, alpha, start, scale, True)
+    _state_like(state, "state", B, H, dk, dv)
+    dev = _check_cuda(q, k, v, alpha, start, state)
+    out = torch.empty((B, T, H, dv), dtype=q.dtype, device=dev)
+    last = torch.empty((B, H, dk, dv), dtype=torch.float32, device=dev) if final_state else None
+    if T == 0 and final_state:                  # no step: the state stays
+        last.zero_() if state is None else last.copy_(state)
+    ws = _workspace(lib().memoroid_scan_retention_workspace_bytes(B, T, H, dk, dv, dt), dev, workspace)
+    with torch.cuda.device(dev):
+        st = lib().memoroid_scan_retention(q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(),
+                                           start.data_ptr(), _ptr(state), out.data_ptr(), _ptr(last), scale, B, T, H,
+                                           Hk, dk, dv, dt, ws.data_ptr(), ws.numel(), _stream_ptr(dev))
+    _raise(st, "memoroid_scan_retention")
+    return (out, last) if final_state else out
+
+
+def scan_retention_bwd(q, k, v, alpha, start, grad_out, scale: Optional[float] = None, state=None, grad_state=None,
+                       need_grad_alpha: bool = True, workspace=None):
+    """Gradient of scan_retention: (dq, dk, dv, dalpha, dstate).  grad_state is
+    the gradient of the state after the last step (None: zero); dalpha is None
+    if not needed, dstate None if there is no state."""
+    torch = _torch()
+    B, T, H, Hk, dk, dv, dt, scale = _retention_args(q, k, v, alpha, start, scale, True)
+    _state_like(state, "state", B, H, dk, dv)
+    _state_like(grad_state, "grad_state", B, H, dk, dv)
+    if grad_out.dtype != q.dtype or grad_out.shape != (B, T, H, dv):
+        raise TypeError("grad_out must be [B,T,H,dv] of q's dtype")
+    dev = _check_cuda(q, k, v, alpha, start, grad_out, state, grad_state)
+    gq, gk, gv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    ga = torch.empty_like(alpha) if need_grad_alpha else None
+    gs = torch.empty_like(state) if state is not None else None
+    if B == 0 or T == 0:                        # no step: the state stays, nothing decays
+        if ga is not None:
+            ga.zero_()
+        if gs is not None:
+            gs.zero_() if grad_state is None else gs.copy_(grad_state)
+        return gq, gk, gv, ga, gs
+    ws = _workspace(lib().memoroid_scan_retention_bwd_workspace_bytes(B, T, H, Hk, dk, dv, dt, need_grad_alpha), dev,
+                    workspace)
+    with torch.cuda.device(dev):
+        st = lib().memoroid_scan_retention_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(),
+                                               start.data_ptr(), _ptr(state), grad_out.data_ptr(), _ptr(grad_state),
+                                               gq.data_ptr(), gk.data_ptr(), gv.data_ptr(), _ptr(ga), _ptr(gs), scale,
+                                               B, T, H, Hk, dk, dv, dt, ws.data_ptr(), ws.numel(), _stream_ptr(dev))
+    _raise(st, "memoroid_scan_retention_bwd")
+    return gq, gk, gv, ga, gs
+
+
+def retention_step(q, k, v, alpha, state, start=None, scale: Optional[float] = None):
+    """One step of retention for B rows, `state` (float32 [B,H,dk,dv]) updated in
+    place.  q: [B,H,dk]; k: [B,Hk,dk]; v: [B,Hk,dv]; start: optional uint8 [B],
+    the rows that begin an episode with this step.  Returns out [B,H,dv]."""
+    torch = _torch()
+    B, _, H, Hk, dk, dv, dt, scale = _retention_args(q, k, v, alpha, start, scale, False)
+    if state is None:
+        raise TypeError("state must be float32 [B,H,dk,dv]")
+    _state_like(state, "state", B, H, dk, dv)
+    dev = _check_cuda(q, k, v, alpha, start, state)
+    out = torch.empty((B, H, dv), dtype=q.dtype, device=dev)
+    with torch.cuda.device(dev):
+        st = lib().memoroid_retention_step(q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(), _ptr(start),
+                                           state.data_ptr(), out.data_ptr(), scale, B, H, Hk, dk, dv, dt,
+                                           _stream_ptr(dev))
+    _raise(st, "memoroid_retention_step")
+    return out
+
+
 def workspace_status(workspace) -> int:
     """Synchronise and report OK, ETIMEOUT (a cross-tile wait gave up) or
     EMISMATCH (a prepared workspace was bound to another call) for the calls
@@ -791,3 +942,41 @@ def linattn(q, k, v, start):
     if _LinAttn is None:
         _LinAttn = _make_linattn_autograd()
     return _LinAttn.apply(q, k, v, start)
+
+
+def _make_retention_autograd():
+    torch = _torch()
+
+    class Retention(torch.autograd.Function):
+        """Differentiable retention over tapes with resets and a carried state."""
+
+        @staticmethod
+        def forward(ctx, q, k, v, alpha, start, scale, state, final_state):
+            got = scan_retention(q, k, v, alpha, start, scale, state, final_state)
+            ctx.save_for_backward(q, k, v, alpha, start, state)
+            ctx.scale = scale
+            ctx.set_materialize_grads(False)
+            return got
+
+        @staticmethod
+        def backward(ctx, grad_out, grad_state=None):
+            q, k, v, alpha, start, state = ctx.saved_tensors
+            if grad_out is None:
+                grad_out = torch.zeros(q.shape[:3] + v.shape[3:], dtype=q.dtype, device=q.device)
+            gq, gk, gv, ga, gs = scan_retention_bwd(q, k, v, alpha, start, grad_out.contiguous(), ctx.scale, state,
+                                                    None if grad_state is None else grad_state.contiguous(),
+                                                    need_grad_alpha=ctx.needs_input_grad[3])
+            return gq, gk, gv, ga, None, None, gs, None
+
+    return Retention
+
+
+_Retention = None
+
+
+def retention(q, k, v, alpha, start, scale: Optional[float] = None, state=None, final_state: bool = False):
+    """Autograd-aware scan_retention: gradients of q, k, v, alpha and state."""
+    global _Retention
+    if _Retention is None:
+        _Retention = _make_retention_autograd()
+    return _Retention.apply(q, k, v, alpha, start, scale, state, final_state)

@@ -70,7 +70,7 @@ uint64_t layout_sig(std::initializer_list<int64_t> vals) {
 
 // entry points in a signature
 enum SigKind : int64_t { kSigDiag = 1, kSigDiagBwd, kSigFfm, kSigFfmBwd, kSigDiscount, kSigTbbBegins,
-                         kSigLinattn, kSigLinattnBwd, kSigTbbSample };
+                         kSigLinattn, kSigLinattnBwd, kSigTbbSample, kSigRetention, kSigRetentionBwd };
 
 // Tiling and workspace layout of a diagonal scan.  `vec` selects the
 // vectorised lane width; `state_complex` picks the descriptor size.
@@ -898,6 +898,376 @@ int memoroid_scan_linattn_bwd(const float* q, const float* k, const float* v, co
     return check_hip(linattn_dkv_launch(ba, s));
 }
 
+// --------------------------------------------------------------- retention
+// Linear attention with a decay rate per head.  Segments of chunks per
+// (tape, head): what each adds to the state -> scan of the segment states ->
+// walks from them.
+
+namespace {
+
+struct RetPlan {
+    int planes = 1;
+    int32_t chunks = 1, nseg = 1;
+    int64_t rows = 0;               // steps of a segment
+    size_t off_states = 0, off_R = 0, total = 0;
+};
+
+// Enough segments for two workgroups on each of the 256 CUs, none shorter than
+// four chunks.
+void ret_segments(int64_t B, int64_t T, int64_t H, int planes, RetPlan* p) {
+    const int64_t C = ret_chunk(planes), n = (T + C - 1) / C;
+    int64_t nseg = (512 + B * H - 1) / (B * H);
+    if (nseg > (n + 3) / 4) nseg = (n + 3) / 4;
+    p->planes = planes;
+    p->chunks = (int32_t)((n + nseg - 1) / nseg);
+    p->nseg = (int32_t)((n + p->chunks - 1) / p->chunks);
+    p->rows = (int64_t)p->chunks * C;
+}
+
+bool ret_dims_ok(int64_t dk, int64_t dv) {
+    return dk % 8 == 0 && dv % 8 == 0 && dk <= kRetMaxDim && dv <= kRetMaxDim && dk > 0 && dv > 0;
+}
+// grid extents; a chunk's rows are addressed with 32-bit offsets below 2^31
+// (64 rows of 65535 heads of 128 floats are 2147450880 bytes)
+bool ret_extents_ok(int64_t B, int64_t T, int64_t H) { return B <= 65535 && H <= 65535 && T <= (int64_t)INT32_MAX / 2; }
+int ret_planes(int dtype) { return dtype == MEMOROID_BF16 ? 1 : dtype == MEMOROID_F32 ? 3 : 0; }
+
+// The segment states of one direction: [B][H][nseg - 1][dk][dv] floats, flags.
+size_t ret_states_bytes(const RetPlan& p, int64_t B, int64_t H, int64_t dk, int64_t dv) {
+    return align_up((size_t)B * (size_t)H * (size_t)(p.nseg - 1) * (size_t)(dk * dv) * 4);
+}
+
+bool plan_retention(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv, int planes, RetPlan* p) {
+    ret_segments(B, T, H, planes, p);
+    size_t off = kAlign;                                   // header
+    p->off_states = off;
+    off += ret_states_bytes(*p, B, H, dk, dv);
+    p->off_R = off;
+    off = align_up(off + (size_t)B * (size_t)(p->nseg - 1));
+    p->total = off;
+    return true;
+}
+
+struct RetBwdPlan {
+    RetPlan fwd;
+    size_t off_dstates = 0, off_rstates = 0, off_rR = 0, off_part = 0, off_gk = 0, off_gv = 0, total = 0;
+};
+
+bool plan_retention_bwd(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t dk, int64_t dv, int planes, bool want_alpha,
+                        RetBwdPlan* p) {
+    if (!plan_retention(B, T, H, dk, dv, planes, &p->fwd)) return false;
+    const size_t states = ret_states_bytes(p->fwd, B, H, dk, dv);
+    size_t off = p->fwd.total;
+    p->off_rstates = off;
+    off += states;
+    p->off_rR = off;
+    off = align_up(off + (size_t)B * (size_t)(p->fwd.nseg - 1));
+    p->off_dstates = off;
+    if (want_alpha) off += states;
+    p->off_part = off;
+    if (want_alpha) off = align_up(off + (size_t)B * (size_t)H * (size_t)p->fwd.nseg * 8);
+    p->off_gk = off;                                       // shared heads: gradients per query head
+    if (Hk != H) off = align_up(off + (size_t)B * (size_t)T * (size_t)H * (size_t)dk * 4);
+    p->off_gv = off;
+    if (Hk != H) off = align_up(off + (size_t)B * (size_t)T * (size_t)H * (size_t)dv * 4);
+    p->total = off;
+    return true;
+}
+
+RetRole ret_role(const void* p, int64_t heads, int64_t d, int64_t share) {
+    return RetRole{p, (int32_t)heads, (int32_t)d, (int32_t)share};
+}
+
+// Segment states of one direction, scanned.
+int ret_states(const RetPlan& p, RetRole y, RetRole z, const uint8_t* start, const float* alpha, const float* seed,
+               float* states, float* dstates, uint8_t* R, float z_scale, int64_t B, int64_t T, int64_t H, bool rev,
+               WsHeader* hdr, uint64_t sig, hipStream_t s) {
+    RetSummaryArgs a{};
+    a.y = y;
+    a.z = z;
+    a.start = start;
+    a.alpha = alpha;
+    a.states = states;
+    a.dstates = dstates;
+    a.R = R;
+    a.z_scale = z_scale;
+    a.T = T;
+    a.H = (int32_t)H;
+    a.nseg = p.nseg;
+    a.chunks = p.chunks;
+    a.rev = rev;
+    a.hdr = hdr;
+    a.sig = sig;
+    if (ret_summary_launch(p.planes, a, B, s) != hipSuccess) return MEMOROID_EHIP;
+    RetStateScanArgs c{};
+    c.alpha = alpha;
+    c.seed = seed;
+    c.states = states;
+    c.dstates = dstates;
+    c.R = R;
+    c.rows = p.rows;
+    c.words = y.d * z.d;
+    c.H = (int32_t)H;
+    c.n = p.nseg - 1;
+    c.rev = rev;
+    return check_hip(ret_state_scan_launch(c, B, s));
+}
+
+// Argument checks that the retention entry points share; MEMOROID_OK and *empty
+// when there is nothing to do.
+int ret_check(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t dk, int64_t dv, float scale, int dtype, bool* empty) {
+    *empty = false;
+    if (B < 0 || T < 0 || H < 0 || Hk < 0 || dk < 0 || dv < 0 || !std::isfinite(scale)) return MEMOROID_EINVAL;
+    if (!ret_planes(dtype)) return MEMOROID_EUNSUPPORTED;
+    if (B == 0 || T == 0 || H == 0) {
+        *empty = true;
+        return MEMOROID_OK;
+    }
+    if (Hk == 0 || H % Hk != 0) return MEMOROID_EINVAL;
+    if (!ret_dims_ok(dk, dv) || !ret_extents_ok(B, T, H)) return MEMOROID_EUNSUPPORTED;
+    return MEMOROID_OK;
+}
+// every pointer of `must` is there, every one of both is 16-byte aligned and no
+// output is an input or another output
+bool ret_pointers_ok(std::initializer_list<const void*> ins, std::initializer_list<const void*> opt_ins,
+                     std::initializer_list<const void*> outs, std::initializer_list<const void*> opt_outs) {
+    for (const void* x : ins)
+        if (!x || !aligned(x, 16)) return false;
+    for (const void* x : outs)
+        if (!x || !aligned(x, 16)) return false;
+    for (const void* x : opt_ins)
+        if (x && !aligned(x, 16)) return false;
+    for (const void* x : opt_outs)
+        if (x && !aligned(x, 16)) return false;
+    const void* o[8];
+    int n = 0;
+    for (const auto& list : {outs, opt_outs})
+        for (const void* x : list)
+            if (x) o[n++] = x;
+    for (int i = 0; i < n; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (o[i] == o[j]) return false;
+        for (const auto& list : {ins, opt_ins})
+            for (const void* x : list)
+                if (x == o[i]) return false;
+    }
+    return true;
+}
+
+}  // namespace
+
+size_t memoroid_scan_retention_workspace_bytes(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv, int dtype) {
+    bool empty;
+    if (ret_check(B, T, H, H, dk, dv, 1.0f, dtype, &empty) != MEMOROID_OK || empty) return 0;
+    RetPlan p;
+    return plan_retention(B, T, H, dk, dv, ret_planes(dtype), &p) ? p.total : 0;
+}
+
+int memoroid_scan_retention(const void* q, const void* k, const void* v, const float* alpha, const uint8_t* start,
+                            const float* state_in, void* out, float* state_out, float scale, int64_t B, int64_t T,
+                            int64_t H, int64_t Hk, int64_t dk, int64_t dv, int dtype, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+    bool empty;
+    const int ok = ret_check(B, T, H, Hk, dk, dv, scale, dtype, &empty);
+    if (ok != MEMOROID_OK || empty) return ok;
+    if (!start || !alpha || !aligned(alpha, 4)) return MEMOROID_EINVAL;
+    if (!ret_pointers_ok({q, k, v}, {state_in}, {out}, {state_out})) return MEMOROID_EINVAL;
+    if (out == alpha || state_out == alpha || out == start || (const void*)state_out == start) return MEMOROID_EINVAL;
+    RetPlan p;
+    if (!plan_retention(B, T, H, dk, dv, ret_planes(dtype), &p)) return MEMOROID_EUNSUPPORTED;
+    if (!workspace || workspace_bytes < p.total) return MEMOROID_EWORKSPACE;
+    if (!aligned(workspace, 256)) return MEMOROID_EINVAL;
+    hipStream_t s = (hipStream_t)stream;
+    char* ws = (char*)workspace;
+    const uint64_t sig = layout_sig({kSigRetention, B, T, H, dk, dv, dtype});
+    const int64_t G = H / Hk;
+    const RetRole rk = ret_role(k, Hk, dk, G), rv = ret_role(v, Hk, dv, G);
+    float* const states = (float*)(ws + p.off_states);
+    if (p.nseg > 1) {
+        const int st = ret_states(p, rk, rv, start, alpha, state_in, states, nullptr, (uint8_t*)(ws + p.off_R), 1.0f, B,
+                                  T, H, false, (WsHeader*)ws, sig, s);
+        if (st != MEMOROID_OK) return st;
+    }
+    RetWalkArgs a{};
+    a.x = ret_role(q, H, dk, 1);
+    a.y = rk;
+    a.z = rv;
+    a.start = start;
+    a.alpha = alpha;
+    a.out = out;
+    a.seed = state_in;
+    a.states = states;
+    a.fin = state_out;
+    a.sk = (int32_t)dv;
+    a.sv = 1;
+    a.p_scale = a.inter_scale = scale;
+    a.z_scale = 1.0f;
+    a.T = T;
+    a.H = (int32_t)H;
+    a.nseg = p.nseg;
+    a.chunks = p.chunks;
+    if (p.nseg == 1) {
+        a.hdr = (WsHeader*)ws;
+        a.sig = sig;
+    }
+    return check_hip(ret_walk_launch(p.planes, a, B, s));
+}
+
+size_t memoroid_scan_retention_bwd_workspace_bytes(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t dk, int64_t dv,
+                                                   int dtype, int want_grad_alpha) {
+    bool empty;
+    if (ret_check(B, T, H, Hk, dk, dv, 1.0f, dtype, &empty) != MEMOROID_OK || empty) return 0;
+    RetBwdPlan p;
+    return plan_retention_bwd(B, T, H, Hk, dk, dv, ret_planes(dtype), want_grad_alpha != 0, &p) ? p.total : 0;
+}
+
+int memoroid_scan_retention_bwd(const void* q, const void* k, const void* v, const float* alpha, const uint8_t* start,
+                                const float* state_in, const void* grad_out, const float* grad_state_out, void* grad_q,
+                                void* grad_k, void* grad_v, float* grad_alpha, float* grad_state_in, float scale,
+                                int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t dk, int64_t dv, int dtype,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+    bool empty;
+    const int ok = ret_check(B, T, H, Hk, dk, dv, scale, dtype, &empty);
+    if (ok != MEMOROID_OK || empty) return ok;
+    if (!start || !alpha || !aligned(alpha, 4) || (grad_alpha && !aligned(grad_alpha, 4))) return MEMOROID_EINVAL;
+    if (!ret_pointers_ok({q, k, v, grad_out}, {state_in, grad_state_out}, {grad_q, grad_k, grad_v}, {grad_state_in}))
+        return MEMOROID_EINVAL;
+    for (const void* o : {(const void*)grad_q, (const void*)grad_k, (const void*)grad_v, (const void*)grad_state_in}) {
+        if (!o) continue;
+        if (o == alpha || o == start || o == grad_alpha) return MEMOROID_EINVAL;
+    }
+    for (const void* i : {q, k, v, (const void*)alpha, (const void*)start, (const void*)state_in, grad_out,
+                          (const void*)grad_state_out})
+        if (grad_alpha && i == grad_alpha) return MEMOROID_EINVAL;
+    RetBwdPlan bp;
+    if (!plan_retention_bwd(B, T, H, Hk, dk, dv, ret_planes(dtype), grad_alpha != nullptr, &bp))
+        return MEMOROID_EUNSUPPORTED;
+    if (!workspace || workspace_bytes < bp.total) return MEMOROID_EWORKSPACE;
+    if (!aligned(workspace, 256)) return MEMOROID_EINVAL;
+    hipStream_t s = (hipStream_t)stream;
+    char* ws = (char*)workspace;
+    const RetPlan& p = bp.fwd;
+    const uint64_t sig = layout_sig({kSigRetentionBwd, B, T, H, Hk, dk, dv, dtype, grad_alpha != nullptr});
+    const int64_t G = H / Hk;
+    const RetRole rq = ret_role(q, H, dk, 1), rk = ret_role(k, Hk, dk, G), rv = ret_role(v, Hk, dv, G),
+                  rg = ret_role(grad_out, H, dv, 1);
+    float* const states = (float*)(ws + p.off_states);
+    float* const dstates = (float*)(ws + bp.off_dstates);
+    float* const rstates = (float*)(ws + bp.off_rstates);
+    if (p.nseg > 1) {
+        int st = ret_states(p, rk, rv, start, alpha, state_in, states, grad_alpha ? dstates : nullptr,
+                            (uint8_t*)(ws + p.off_R), 1.0f, B, T, H, false, (WsHeader*)ws, sig, s);
+        if (st != MEMOROID_OK) return st;
+        st = ret_states(p, rq, rg, start, alpha, grad_state_out, rstates, nullptr, (uint8_t*)(ws + bp.off_rR), scale, B,
+                        T, H, true, nullptr, 0, s);
+        if (st != MEMOROID_OK) return st;
+    }
+    if (grad_alpha) {
+        RetSensArgs a{};
+        a.q = rq;
+        a.k = rk;
+        a.v = rv;
+        a.g = rg;
+        a.start = start;
+        a.alpha = alpha;
+        a.seed = state_in;
+        a.grad_state = grad_state_out;
+        a.states = states;
+        a.dstates = dstates;
+        a.part = (double*)(ws + bp.off_part);
+        a.scale = scale;
+        a.T = T;
+        a.H = (int32_t)H;
+        a.nseg = p.nseg;
+        a.chunks = p.chunks;
+        if (ret_sens_launch(p.planes, a, B, s) != hipSuccess) return MEMOROID_EHIP;
+        if (ret_alpha_launch(a.part, alpha, grad_alpha, B, (int32_t)H, p.nseg, s) != hipSuccess) return MEMOROID_EHIP;
+    }
+    RetWalkArgs a{};
+    a.start = start;
+    a.alpha = alpha;
+    a.p_scale = scale;
+    a.T = T;
+    a.H = (int32_t)H;
+    a.nseg = p.nseg;
+    a.chunks = p.chunks;
+    // dq = W(dout, v, k) from the carried state, whose rows are v's columns here
+    a.x = rg;
+    a.y = rv;
+    a.z = rk;
+    a.out = grad_q;
+    a.seed = state_in;
+    a.states = states;
+    a.sk = 1;
+    a.sv = (int32_t)dv;
+    a.inter_scale = scale;
+    a.z_scale = 1.0f;
+    if (p.nseg == 1) {
+        a.hdr = (WsHeader*)ws;
+        a.sig = sig;
+    }
+    if (ret_walk_launch(p.planes, a, B, s) != hipSuccess) return MEMOROID_EHIP;
+    a.hdr = nullptr;
+    // dk = W(v, dout, q) and dv = W(k, q, dout), backwards; the state takes the
+    // scale, since the gradient of the state after the tape has none
+    a.rev = 1;
+    a.out_f32 = G > 1;
+    a.seed = grad_state_out;
+    a.states = rstates;
+    a.inter_scale = 1.0f;
+    a.z_scale = scale;
+    a.x = rv;
+    a.y = rg;
+    a.z = rq;
+    a.out = G > 1 ? (void*)(ws + bp.off_gk) : grad_k;
+    if (ret_walk_launch(p.planes, a, B, s) != hipSuccess) return MEMOROID_EHIP;
+    a.x = rk;
+    a.y = rq;
+    a.z = rg;
+    a.out = G > 1 ? (void*)(ws + bp.off_gv) : grad_v;
+    a.sk = (int32_t)dv;
+    a.sv = 1;
+    a.fin = grad_state_in;
+    if (ret_walk_launch(p.planes, a, B, s) != hipSuccess) return MEMOROID_EHIP;
+    if (G > 1) {
+        if (ret_share_launch(p.planes, (const float*)(ws + bp.off_gk), grad_k, B * T, (int32_t)Hk, (int32_t)G,
+                             (int32_t)dk, s) != hipSuccess)
+            return MEMOROID_EHIP;
+        if (ret_share_launch(p.planes, (const float*)(ws + bp.off_gv), grad_v, B * T, (int32_t)Hk, (int32_t)G,
+                             (int32_t)dv, s) != hipSuccess)
+            return MEMOROID_EHIP;
+    }
+    return MEMOROID_OK;
+}
+
+int memoroid_retention_step(const void* q, const void* k, const void* v, const float* alpha, const uint8_t* start,
+                            float* state, void* out, float scale, int64_t B, int64_t H, int64_t Hk, int64_t dk,
+                            int64_t dv, int dtype, void* stream) {
+    bool empty;
+    const int ok = ret_check(B < 65536 ? B : 65535, 1, H, Hk, dk, dv, scale, dtype, &empty);
+    if (ok != MEMOROID_OK || empty) return ok;
+    int64_t groups;
+    if (!mul_ok(B, H * ((dv + 31) / 32), &groups) || groups > (int64_t)INT32_MAX) return MEMOROID_EUNSUPPORTED;
+    if (!alpha || !aligned(alpha, 4)) return MEMOROID_EINVAL;
+    if (!ret_pointers_ok({q, k, v}, {}, {out, state}, {})) return MEMOROID_EINVAL;
+    if (out == alpha || state == alpha || out == start || (const void*)state == start) return MEMOROID_EINVAL;
+    RetStepArgs a{};
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.alpha = alpha;
+    a.start = start;
+    a.state = state;
+    a.out = out;
+    a.scale = scale;
+    a.B = B;
+    a.H = (int32_t)H;
+    a.Hk = (int32_t)Hk;
+    a.dk = (int32_t)dk;
+    a.dv = (int32_t)dv;
+    return check_hip(ret_step_launch(ret_planes(dtype), a, (hipStream_t)stream));
+}
+
 // ------------------------------------------------------------------ status
 
 // ------------------------------------------- discounted return and GAE
@@ -1284,6 +1654,14 @@ size_t memoroid_workspace_bytes(memoroid_op op_in, int64_t B, int64_t T, int64_t
             return memoroid_tbb_begin_indices_workspace_bytes(T);
         case MEMOROID_OP_TBB_SAMPLE:
             return memoroid_tbb_sample_workspace_bytes(B, T);
+        case MEMOROID_OP_RETENTION:
+            for (int dt : {MEMOROID_F32, MEMOROID_BF16})
+                take(memoroid_scan_retention_workspace_bytes(B, T, d_or_H, dk, dv, dt));
+            return best;
+        case MEMOROID_OP_RETENTION_BWD:
+            for (int dt : {MEMOROID_F32, MEMOROID_BF16})
+                take(memoroid_scan_retention_bwd_workspace_bytes(B, T, d_or_H, 1, dk, dv, dt, 1));
+            return best;
     }
     return 0;
 }

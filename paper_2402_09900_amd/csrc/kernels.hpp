@@ -289,6 +289,99 @@ struct LinBwdArgs {
 hipError_t linattn_dq_launch(const LinBwdArgs& a, hipStream_t s);
 hipError_t linattn_dkv_launch(const LinBwdArgs& a, hipStream_t s);
 
+// ------------------------------------------------------------- retention
+// Linear attention with a decay rate per head (retention_common.hpp).  Rows per
+// chunk: 64 of bf16 (planes == 1), 32 of float (planes == 3).
+constexpr int ret_chunk(int planes) { return planes == 1 ? 64 : 32; }
+constexpr int kRetMaxDim = 128;      // widest head
+
+// A tensor in one of the walk's roles: [B][T][heads][d], read by query head h as
+// head h / share.
+struct RetRole {
+    const void* p;
+    int32_t heads, d, share;
+};
+
+// W(x, y, z) over B tapes and H heads, in segments of `chunks` chunks (segment
+// states by RetSummaryArgs and RetStateScanArgs; one segment needs none).
+struct RetWalkArgs {
+    RetRole x, y, z;            // z.d columns of output, x.d == y.d rows of state
+    const uint8_t* start;       // [B][T]
+    const float* alpha;         // [H]
+    void* out;                  // [B][T][H][z.d]
+    int32_t out_f32;            // floats out although the inputs are bf16
+    const float* seed;          // state before the walk [B][H][dk][dv], or NULL
+    const float* states;        // [B][H][nseg - 1][dk][dv]: state after each segment but the last
+    float* fin;                 // state after the walk out, or NULL
+    int32_t sk, sv;             // strides of a state's rows and columns (x.d x z.d) in those arrays
+    float p_scale, inter_scale, z_scale;   // of pairs, of the carried state, into the state
+    int64_t T;
+    int32_t H, nseg, chunks;
+    int32_t rev;                // backwards: see retention.hip on `seed` and `fin`
+    WsHeader* hdr;              // header to prepare with sig, or NULL
+    uint64_t sig;
+};
+struct RetSummaryArgs {
+    RetRole y, z;
+    const uint8_t* start;
+    const float* alpha;
+    float* states;              // [B][H][nseg - 1][y.d][z.d]
+    float* dstates;             // their derivatives by log gamma, or NULL
+    uint8_t* R;                 // [B][nseg - 1] segment holds a begin step
+    float z_scale;
+    int64_t T;
+    int32_t H, nseg, chunks, rev;
+    WsHeader* hdr;
+    uint64_t sig;
+};
+struct RetStateScanArgs {
+    const float* alpha;
+    const float* seed;          // as in RetWalkArgs
+    float* states;              // scanned in place
+    float* dstates;             // likewise, or NULL
+    const uint8_t* R;
+    int64_t rows;               // steps of a segment
+    int32_t words, H, n, rev;   // floats of a state; n = nseg - 1 segments
+};
+// dL/dlog gamma: the derivative state against q dout^T
+struct RetSensArgs {
+    RetRole q, k, v, g;
+    const uint8_t* start;
+    const float* alpha;
+    const float* seed;          // carried state, or NULL
+    const float* grad_state;    // gradient of the state after the tape, or NULL
+    const float* states;        // scanned, as in RetWalkArgs
+    const float* dstates;
+    double* part;               // [B][H][nseg]
+    float scale;
+    int64_t T;
+    int32_t H, nseg, chunks;
+};
+hipError_t ret_walk_launch(int planes, const RetWalkArgs& a, int64_t B, hipStream_t s);
+hipError_t ret_summary_launch(int planes, const RetSummaryArgs& a, int64_t B, hipStream_t s);
+hipError_t ret_state_scan_launch(const RetStateScanArgs& a, int64_t B, hipStream_t s);
+hipError_t ret_sens_launch(int planes, const RetSensArgs& a, int64_t B, hipStream_t s);
+// grad_alpha[h] = -sign(alpha_h) sum of part over tapes and segments
+hipError_t ret_alpha_launch(const double* part, const float* alpha, float* out, int64_t B, int32_t H, int32_t nseg,
+                            hipStream_t s);
+// out[row][kh][.] = sum of part[row][kh G + 0 .. G - 1][.], rounded to bf16 if planes == 1
+hipError_t ret_share_launch(int planes, const float* part, void* out, int64_t rows, int32_t heads, int32_t G, int32_t d,
+                            hipStream_t s);
+
+struct RetStepArgs {
+    const void* q;              // [B][H][dk]
+    const void* k;              // [B][Hk][dk]
+    const void* v;              // [B][Hk][dv]
+    const float* alpha;         // [H]
+    const uint8_t* start;       // [B], or NULL
+    float* state;               // [B][H][dk][dv], updated in place
+    void* out;                  // [B][H][dv]
+    float scale;
+    int64_t B;
+    int32_t H, Hk, dk, dv;
+};
+hipError_t ret_step_launch(int planes, const RetStepArgs& a, hipStream_t s);
+
 // ------------------------------------------- discounted return and GAE
 // Steps per lane: 32 for the return (two streams in registers), 16 for the
 // advantage (four); a tile is 4 wavefronts of 64 lanes.

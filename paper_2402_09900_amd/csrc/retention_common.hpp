@@ -1,0 +1,305 @@
+// retention_common.hpp -- shared pieces of the retention kernels (linear
+// attention whose state decays at a rate of its own in each head): operands of
+// the bf16 matrix cores, LDS tiles of a chunk, register layouts, decay powers.
+//
+// One walk serves the operator and its whole gradient.  With rows i of a tape in
+// walking order, W(x, y, z) is
+//     state_i = gamma state_{i-1} + y_i^T z_i   (the carried part dropped at a begin)
+//     W_i     = x_i state_i
+// and   out = W(q, k, v),  dq = W(dout, v, k)  forwards,
+//       dv  = W(k, q, dout),  dk = W(v, dout, q)  backwards in time,
+// where a step "begins" backwards when the step after it begins an episode.
+//
+// A workgroup of four wavefronts walks a run of chunks of C rows of one head with
+// the state (KD x 64 NT) in registers, a quarter of its columns per wavefront.
+//
+// Every product runs on v_mfma_f32_16x16x32_bf16.  bf16 inputs go in as they
+// are.  A float goes in as three bf16 planes, x = h + m + l with h and m its
+// leading bits cut off: exact, 8 bits each.  Two such numbers take the six
+// products of planes whose indices add to at most 2; what is left out is below
+// 2^-21 of the product, so a product of floats keeps a float's precision at six
+// bf16 instructions, 16 / 6 of the rate of the fp32 matrix cores.
+//
+// With lane = 16 g + c the instruction takes A[i = c][k = 8 g + e] and
+// B[k = 8 g + e][j = c] and returns D[i = 4 g + r][j = c] in register r.  The
+// order of the k slots is free as long as A and B share it, and so is which
+// column stands in which row of A; the layouts use both so that results are
+// operands of the next product where they are:
+//   * rows of a chunk as k: slot (g, e) is row 32 tb + 16 (e / 4) + 4 g + e % 4.
+//     The masked products P^T, two 16-row tiles, come out in that order; columns
+//     of a row-major LDS tile are read in it by ds_read_b64_tr_b16;
+//   * state rows kd as k: slot (g, e) is kd = 32 s + 8 g + e, as 16 bytes of a row
+//     of x are.  The state tile (s, u) holds kd = 32 s + 8 (i / 4) + 4 u + i % 4 in
+//     its row i, so registers of tiles (s, 0) and (s, 1) are those eight slots;
+//   * state columns: tile nt holds column 4 NT (c / 4) + 4 nt + c % 4 of the
+//     wavefront's 16 NT, and a row of the result has 4 NT consecutive columns in
+//     each lane: one store of 16 bytes or more (bf16, NT = 1: 8).
+#pragma once
+
+#include "scan_common.hpp"
+#include "kernels.hpp"
+
+namespace memoroid {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// NP planes per input element: 1 = bf16, 3 = float.  Chunks of float are half as
+// long: the planes of three 64-row chunks of 128 columns do not fit in LDS.
+template <int NP_, int KD_, int NT_>
+struct RetCfg {
+    static constexpr int NP = NP_, KD = KD_, NT = NT_;
+    static constexpr int C = ret_chunk(NP);
+    static constexpr int VD = 64 * NT;
+    static constexpr int ES = NP == 1 ? 2 : 4;        // bytes of an element in memory
+    static constexpr int EPU = 16 / ES;               // elements of a 16-byte unit
+    static constexpr int LDK = KD + 8, LDV = VD + 8;  // LDS row strides in elements
+    static constexpr int NB = C / 16;                 // 16-row blocks
+    static constexpr int NTILE = NB * (NB + 1) / 2;   // tiles of P on and below the diagonal
+};
+
+struct RetLane {
+    int tid, lane, w, g, c;
+    __device__ RetLane() {
+        tid = threadIdx.x;
+        lane = tid & 63;
+        w = __builtin_amdgcn_readfirstlane(tid >> 6);
+        g = lane >> 4;
+        c = lane & 15;
+    }
+};
+
+// ------------------------------------------------------------------ planes
+// the upper halves of a and b in one word, a's in the low half
+__device__ __forceinline__ uint32_t pack_hi(float a, float b) {
+    return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+__device__ __forceinline__ float cut(float x) { return __uint_as_float(__float_as_uint(x) & 0xFFFF0000u); }
+// Two floats as NPL planes of packed bf16 words.  One plane: rounded to nearest.
+// Three: cut, exact (an infinity leaves NaN in its lower planes: the products
+// are then NaN, not infinite).
+template <int NPL>
+__device__ __forceinline__ void planes2(float a, float b, uint32_t (&w)[NPL]) {
+    if constexpr (NPL == 1) {
+        w[0] = f32x2_to_bf16x2(a, b);
+    } else {
+        static_assert(NPL == 3, "one or three planes");
+        w[0] = pack_hi(a, b);
+        a -= cut(a);
+        b -= cut(b);
+        w[1] = pack_hi(a, b);
+        a -= cut(a);
+        b -= cut(b);
+        w[2] = pack_hi(a, b);
+    }
+}
+// eight floats as operands
+template <int NPL>
+__device__ __forceinline__ void planes8(f32x4 lo, f32x4 hi, bf16x8 (&f)[NPL]) {
+    u32x4 w[NPL];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        uint32_t x[NPL];
+        if (p < 2) planes2<NPL>(lo[2 * p], lo[2 * p + 1], x);
+        else planes2<NPL>(hi[2 * p - 4], hi[2 * p - 3], x);
+#pragma unroll
+        for (int i = 0; i < NPL; ++i) w[i][p] = x[i];
+    }
+#pragma unroll
+    for (int i = 0; i < NPL; ++i) f[i] = __builtin_bit_cast(bf16x8, w[i]);
+}
+// the float that NP planes of element e stand for
+template <int NP>
+__device__ __forceinline__ float plane_value(const bf16x8 (&f)[NP], int e) {
+    auto one = [&](int i) {
+        const u32x4 w = __builtin_bit_cast(u32x4, f[i]);
+        return e & 1 ? __uint_as_float(w[e >> 1] & 0xFFFF0000u) : __uint_as_float(w[e >> 1] << 16);
+    };
+    if constexpr (NP == 1) return one(0);
+    else return one(0) + (one(1) + one(2));
+}
+
+template <int NA, int NB>
+__device__ __forceinline__ void mma(f32x4& acc, const bf16x8 (&a)[NA], const bf16x8 (&b)[NB]) {
+#pragma unroll
+    for (int i = NA - 1; i >= 0; --i)
+#pragma unroll
+        for (int j = NB - 1; j >= 0; --j)
+            if (i + j < 3) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], acc, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 zero4() { return f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }
+
+// --------------------------------------------------------- chunks in memory
+// n rows of one head of a [T][heads][d] tensor, from the row at the lowest
+// address; walking backwards row i is the (n - 1 - i)-th of them.  Rows at or
+// past n and columns at or past d read as zeros and drop their stores.
+struct RetRows {
+    Rsrc r;
+    uint32_t row_bytes;
+    int n, d;
+    bool rev;
+    __device__ __forceinline__ uint32_t offset(int row, int col, int es) const {
+        const uint32_t at = (uint32_t)(rev ? n - 1 - row : row) * row_bytes + (uint32_t)(col * es);
+        return row < n && col < d ? at : kOob;
+    }
+};
+template <int ES>
+__device__ __forceinline__ RetRows ret_rows(const void* head0, int64_t row, int d, int64_t w0, int n, int64_t T,
+                                            bool rev) {
+    const int64_t t = rev ? T - w0 - n : w0;
+    return RetRows{make_rsrc((const char*)head0 + t * row * ES, n > 0 ? ((int64_t)(n - 1) * row + d) * ES : 0),
+                   (uint32_t)(row * ES), n, d, rev};
+}
+
+// A chunk's tile of D columns held by the workgroup, 16 bytes a unit
+template <class Cfg, int D>
+struct RetTile {
+    static constexpr int UPR = D / Cfg::EPU, UN = Cfg::C * UPR / 256;
+    static_assert(UN >= 1, "every thread holds a unit");
+    u32x4 u[UN];
+
+    __device__ __forceinline__ void fetch(const RetRows& x, const RetLane& L) {
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+            const int at = i * 256 + L.tid, row = at / UPR, col = at % UPR * Cfg::EPU;
+            u[i] = __builtin_amdgcn_raw_buffer_load_b128(x.r, (int)x.offset(row, col, Cfg::ES), 0, 0);
+        }
+    }
+    // whether some element is not finite
+    __device__ __forceinline__ bool bad() const {
+        constexpr uint32_t kExp = Cfg::NP == 1 ? 0x7F807F80u : 0x7F800000u, kOne = Cfg::NP == 1 ? 0x00800080u : 0x00800000u;
+        uint32_t any = 0;
+#pragma unroll
+        for (int i = 0; i < UN; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) any |= (u[i][e] & kExp) + kOne;
+        return (any & (Cfg::NP == 1 ? 0x80008000u : 0x80000000u)) != 0u;
+    }
+    // rows a .. b - 1 into an LDS tile of NP planes, the others as zeros
+    template <int LD>
+    __device__ __forceinline__ void stage(uint16_t* s, int a, int b, const RetLane& L) const {
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+            const int at = i * 256 + L.tid, row = at / UPR, col = at % UPR * Cfg::EPU;
+            const bool in = row >= a && row < b;
+            u32x4 x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = in ? u[i][e] : 0u;
+            uint16_t* const p = s + row * LD + col;
+            if constexpr (Cfg::NP == 1) {
+                *(u32x4*)p = x;
+            } else {
+                uint32_t lo[3], hi[3];
+                planes2<3>(__uint_as_float(x[0]), __uint_as_float(x[1]), lo);
+                planes2<3>(__uint_as_float(x[2]), __uint_as_float(x[3]), hi);
+#pragma unroll
+                for (int q = 0; q < 3; ++q) *(u32x2*)(p + q * Cfg::C * LD) = u32x2{lo[q], hi[q]};
+            }
+        }
+    }
+};
+
+// ------------------------------------------------------------ LDS operands
+// 16 rows from row0, columns 32 s + 8 g ..: a row operand
+template <class Cfg, int LD>
+__device__ __forceinline__ void row_frag(bf16x8 (&f)[Cfg::NP], const uint16_t* s, int row0, int col0, const RetLane& L) {
+#pragma unroll
+    for (int p = 0; p < Cfg::NP; ++p)
+        f[p] = *(const bf16x8*)(s + p * Cfg::C * LD + (row0 + L.c) * LD + col0 + 8 * L.g);
+}
+// rows 32 tb .. + 31 as k, the column of `col` (of this lane's address: four
+// consecutive columns from there): a column operand
+template <class Cfg, int LD>
+__device__ __forceinline__ void col_frag(bf16x8 (&f)[Cfg::NP], const uint16_t* s, int tb, int col, const RetLane& L) {
+    typedef __attribute__((address_space(3))) s16x4* LdsPtr;
+#pragma unroll
+    for (int p = 0; p < Cfg::NP; ++p) {
+        const uint16_t* const at = s + p * Cfg::C * LD + (32 * tb + 4 * L.g + (L.c >> 2)) * LD + col;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(at + 16 * LD));
+        f[p] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+}
+
+// ---------------------------------------------------------------- the state
+// S[s][u][nt], rows and columns as above; column of this lane (and of this
+// lane's address in col_frag)
+template <class Cfg>
+__device__ __forceinline__ int state_col(int nt, const RetLane& L) {
+    return 16 * Cfg::NT * L.w + 4 * Cfg::NT * (L.c >> 2) + 4 * nt + (L.c & 3);
+}
+template <class Cfg>
+__device__ __forceinline__ int state_col_addr(int nt, const RetLane& L) {
+    return 16 * Cfg::NT * L.w + 4 * Cfg::NT * (L.c & 3) + 4 * nt;
+}
+template <class Cfg>
+__device__ __forceinline__ int state_row_addr(int s, int u, const RetLane& L) { return 32 * s + 8 * (L.c & 3) + 4 * u; }
+__device__ __forceinline__ int state_row(int s, int u, int r, const RetLane& L) { return 32 * s + 8 * L.g + 4 * u + r; }
+
+// An array of dk x dv floats with strides sk, sv: zeros where there is none
+template <class Cfg>
+__device__ __forceinline__ void load_state(f32x4 (&S)[Cfg::KD / 32][2][Cfg::NT], const float* p, int sk, int sv, int kd,
+                                           int vd, const RetLane& L) {
+    const Rsrc r = make_rsrc(p, p ? (int64_t)kd * vd * 4 : 0);
+#pragma unroll
+    for (int s = 0; s < Cfg::KD / 32; ++s)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int nt = 0; nt < Cfg::NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int k = state_row(s, u, e, L), v = state_col<Cfg>(nt, L);
+                    const uint32_t off = k < kd && v < vd ? (uint32_t)(k * sk + v * sv) * 4u : kOob;
+                    S[s][u][nt][e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (int)off, 0, 0));
+                }
+}
+template <class Cfg>
+__device__ __forceinline__ void store_state(const f32x4 (&S)[Cfg::KD / 32][2][Cfg::NT], float* p, int sk, int sv, int kd,
+                                            int vd, float mul, bool drop, const RetLane& L) {
+    const Rsrc r = make_rsrc(p, (int64_t)kd * vd * 4);
+#pragma unroll
+    for (int s = 0; s < Cfg::KD / 32; ++s)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int nt = 0; nt < Cfg::NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int k = state_row(s, u, e, L), v = state_col<Cfg>(nt, L);
+                    const uint32_t off = k < kd && v < vd ? (uint32_t)(k * sk + v * sv) * 4u : kOob;
+                    const float x = drop ? 0.0f : S[s][u][nt][e] * mul;
+                    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), r, (int)off, 0, 0);
+                }
+}
+
+// ------------------------------------------------------------------- decays
+// gamma^n = exp(-rate n), formed in 64 bits: a slow rate compounds over 1e5
+// steps, where the rounding of a 32-bit gamma^C would show.
+__device__ __forceinline__ float decay_pow(double rate, double n) { return n == 0.0 ? 1.0f : (float)exp(-rate * n); }
+// x -> gamma^n x without rounding gamma^n near 1: x + (gamma^n - 1) x there
+struct Carry {
+    float m;
+    bool near1;
+    __device__ __forceinline__ float operator()(float x) const { return near1 ? __builtin_fmaf(x, m, x) : x * m; }
+};
+__device__ __forceinline__ Carry carry_of(double rate, double n) {
+    if (n == 0.0) return Carry{0.0f, true};
+    const double p = exp(-rate * n);
+    return p > 0.5 ? Carry{(float)expm1(-rate * n), true} : Carry{(float)p, false};
+}
+
+// ----------------------------------------------------------------- begins
+// begin bits of the C <= 64 rows of a chunk in walking order
+__device__ __forceinline__ uint64_t ret_begins(const uint8_t* start, int64_t w0, int n, int64_t T, bool rev, int lane) {
+    // backwards, row i is step t = T - 1 - w0 - i and begins if step t + 1 does
+    const int64_t t = rev ? T - w0 - lane : w0 + lane;
+    const bool in = lane < n && t < T;
+    return __ballot(in && start[in ? t : 0] != 0);
+}
+__device__ __forceinline__ uint64_t upto(int i) { return (2ull << i) - 1ull; }          // bits 0 .. i
+__device__ __forceinline__ int last_begin(uint64_t m) { return 63 - __builtin_clzll(m); }   // m != 0
+
+}  // namespace memoroid

@@ -1,0 +1,150 @@
+"""Retention on the CPU: the 64-bit reference against differences, the C entry
+points' refusals (before any HIP call, on pointers that are never followed) and
+the torch layer's."""
+import numpy as np
+import pytest
+
+import retention_ref as ref
+from paper_2402_09900_amd import binding as mb
+
+torch = pytest.importorskip("torch")
+
+P = [0x10000 * (i + 1) for i in range(16)]      # distinct, aligned, never followed
+
+
+@pytest.mark.parametrize("carry", [False, True])
+def test_reference_gradient_against_differences(carry):
+    rng = np.random.default_rng(0)
+    B, T, H, Hk, dk, dv = 2, 9, 4, 2, 3, 5
+    x = dict(q=rng.standard_normal((B, T, H, dk)), k=rng.standard_normal((B, T, Hk, dk)),
+             v=rng.standard_normal((B, T, Hk, dv)), alpha=rng.uniform(-0.5, 0.5, H),
+             state=rng.standard_normal((B, H, dk, dv)) if carry else None)
+    start = (rng.random((B, T)) < 0.2).astype(np.uint8)
+    g = rng.standard_normal((B, T, H, dv))
+    G = rng.standard_normal((B, H, dk, dv)) if carry else np.zeros((B, H, dk, dv))
+
+    def loss(x):
+        out, S, _ = ref.forward(x["q"], x["k"], x["v"], x["alpha"], start, 0.7, x["state"])
+        return (out * g).sum() + (S * G).sum()
+
+    b = ref.backward(x["q"], x["k"], x["v"], x["alpha"], start, 0.7, g, x["state"], G)
+    for n in x:
+        if x[n] is None:
+            continue
+        d, h = rng.standard_normal(x[n].shape), 1e-5
+        num = (loss({**x, n: x[n] + h * d}) - loss({**x, n: x[n] - h * d})) / (2 * h)
+        assert abs(num - (b["d" + n] * d).sum()) <= 1e-6 * (1 + abs(num)), n
+
+
+def scan(q=P[0], k=P[1], v=P[2], alpha=P[3], start=P[4], state_in=P[5], out=P[6], state_out=P[7], scale=1.0, B=2, T=100,
+         H=4, Hk=2, dk=64, dv=64, dtype=mb.F32, ws=P[8], nbytes=1 << 40):
+    return mb.memoroid_scan_retention(q, k, v, alpha, start, state_in, out, state_out, scale, B, T, H, Hk, dk, dv, dtype,
+                                      ws, nbytes, None)
+
+
+def bwd(q=P[0], k=P[1], v=P[2], alpha=P[3], start=P[4], state_in=P[5], g=P[6], G=P[7], dq=P[8], dk_=P[9], dv_=P[10],
+        da=P[11], ds=P[12], scale=1.0, B=2, T=100, H=4, Hk=2, dk=64, dv=64, dtype=mb.F32, ws=P[13], nbytes=1 << 40):
+    return mb.memoroid_scan_retention_bwd(q, k, v, alpha, start, state_in, g, G, dq, dk_, dv_, da, ds, scale, B, T, H, Hk,
+                                          dk, dv, dtype, ws, nbytes, None)
+
+
+def step(q=P[0], k=P[1], v=P[2], alpha=P[3], start=P[4], state=P[5], out=P[6], scale=1.0, B=2, H=4, Hk=2, dk=64, dv=64,
+         dtype=mb.F32):
+    return mb.memoroid_retention_step(q, k, v, alpha, start, state, out, scale, B, H, Hk, dk, dv, dtype, None)
+
+
+SIZES = [(dict(B=-1), mb.EINVAL), (dict(H=-4), mb.EINVAL), (dict(Hk=-1), mb.EINVAL), (dict(dk=-64), mb.EINVAL),
+         (dict(Hk=0), mb.EINVAL), (dict(Hk=3), mb.EINVAL), (dict(H=2, Hk=4), mb.EINVAL),
+         (dict(scale=float("nan")), mb.EINVAL), (dict(scale=float("inf")), mb.EINVAL),
+         (dict(dk=60), mb.EUNSUPPORTED), (dict(dv=136), mb.EUNSUPPORTED), (dict(dk=0), mb.EUNSUPPORTED),
+         (dict(dtype=mb.C64), mb.EUNSUPPORTED), (dict(dtype=7), mb.EUNSUPPORTED),
+         (dict(H=65536, Hk=65536), mb.EUNSUPPORTED), (dict(B=0), mb.OK), (dict(H=0, Hk=0), mb.OK)]
+
+
+@pytest.mark.parametrize("call", [scan, bwd, step])
+@pytest.mark.parametrize("change,status", SIZES)
+def test_sizes(call, change, status):
+    assert call(**change) == status
+
+
+@pytest.mark.parametrize("call", [scan, bwd])
+def test_long_and_empty_tapes(call):
+    assert call(T=0) == mb.OK
+    assert call(T=-1) == mb.EINVAL
+    assert call(T=1 << 31) == mb.EUNSUPPORTED
+    assert call(B=65536) == mb.EUNSUPPORTED
+
+
+def test_step_batch_limit():
+    assert step(B=1 << 40) == mb.EUNSUPPORTED
+    assert step(B=1 << 62) == mb.EUNSUPPORTED
+
+
+def test_missing_pointers():
+    for call, names in ((scan, "q k v alpha start out"), (bwd, "q k v alpha start g dq dk_ dv_"),
+                        (step, "q k v alpha state out")):
+        for n in names.split():
+            assert call(**{n: None}) == mb.EINVAL, (call.__name__, n)
+
+
+def test_alignment():
+    for call, names in ((scan, "q k v state_in out state_out ws"), (bwd, "q k v state_in g G dq dk_ dv_ ds ws"),
+                        (step, "q k v state out")):
+        for n in names.split():
+            assert call(**{n: 0x900008}) == mb.EINVAL, (call.__name__, n)
+    for call in (scan, bwd, step):
+        assert call(alpha=0x900002) == mb.EINVAL
+    assert bwd(da=0x900002) == mb.EINVAL
+
+
+def test_aliasing():
+    for call, ins, outs in ((scan, "q k v alpha start state_in", "out state_out"),
+                            (bwd, "q k v alpha start state_in g G", "dq dk_ dv_ da ds"),
+                            (step, "q k v alpha start", "out state")):
+        for o in outs.split():
+            for i in ins.split():
+                assert call(**{o: 0x900000, i: 0x900000}) == mb.EINVAL, (call.__name__, i, o)
+            for o2 in outs.split():
+                if o2 != o:
+                    assert call(**{o: 0x900000, o2: 0x900000}) == mb.EINVAL, (call.__name__, o, o2)
+
+
+def test_workspace_sizes():
+    for dt in (mb.F32, mb.BF16):
+        n = mb.memoroid_scan_retention_workspace_bytes(2, 5000, 4, 64, 96, dt)
+        assert n >= 256
+        assert scan(T=5000, dv=96, dtype=dt, nbytes=n - 1) == mb.EWORKSPACE
+        assert scan(T=5000, dv=96, dtype=dt, ws=None) == mb.EWORKSPACE
+        assert n <= mb.memoroid_workspace_bytes(mb.OP_RETENTION, 2, 5000, 4, 64, 96, 0)
+        for alpha in (0, 1):
+            n = mb.memoroid_scan_retention_bwd_workspace_bytes(2, 5000, 4, 2, 64, 96, dt, alpha)
+            assert bwd(T=5000, dv=96, dtype=dt, da=P[11] if alpha else None, nbytes=n - 1) == mb.EWORKSPACE
+            assert n <= mb.memoroid_workspace_bytes(mb.OP_RETENTION_BWD, 2, 5000, 4, 64, 96, 0)
+    assert mb.memoroid_scan_retention_workspace_bytes(2, 0, 4, 64, 64, mb.F32) == 0
+    assert mb.memoroid_scan_retention_workspace_bytes(2, 10, 4, 60, 64, mb.F32) == 0
+    assert mb.memoroid_scan_retention_bwd_workspace_bytes(2, 10, 4, 3, 64, 64, mb.F32, 1) == 0
+    assert mb.memoroid_workspace_bytes(mb.OP_RETENTION, -1, 10, 4, 64, 64, 0) == 0
+
+
+def test_torch_layer_refuses():
+    q = torch.zeros(2, 5, 4, 64)
+    k = torch.zeros(2, 5, 2, 64)
+    a, s = torch.zeros(4), torch.zeros(2, 5, dtype=torch.uint8)
+    S = torch.zeros(2, 4, 64, 64)
+    bad = [(ValueError, (q[0], k, k, a, s), {}), (ValueError, (q, k[:, :4], k, a, s), {}),
+           (ValueError, (q, torch.zeros(2, 5, 3, 64), torch.zeros(2, 5, 3, 64), a, s), {}),
+           (ValueError, (q, k[..., :32], k, a, s), {}), (TypeError, (q, k.bfloat16(), k, a, s), {}),
+           (TypeError, (q.half(), k.half(), k.half(), a, s), {}), (TypeError, (q, k, k, a[:3], s), {}),
+           (TypeError, (q, k, k, a.double(), s), {}), (TypeError, (q, k, k, a, s.bool()), {}),
+           (TypeError, (q, k, k, a, s[:, :4]), {}), (TypeError, (q, k, k, a, s), dict(state=S[:1])),
+           (TypeError, (q, k, k, a, s), dict(state=S.bfloat16())),
+           (ValueError, (q, k, k, a, s), {})]                # the CPU's tensors
+    for err, args, kw in bad:
+        with pytest.raises(err):
+            mb.scan_retention(*args, **kw)
+    with pytest.raises(TypeError):
+        mb.scan_retention_bwd(q, k, k, a, s, q[:, :4])
+    with pytest.raises(TypeError):
+        mb.retention_step(q[:, 0], k[:, 0], k[:, 0], a, None)
+    with pytest.raises(TypeError):
+        mb.retention_step(q[:, 0], k[:, 0], k[:, 0], a, S, s[0])
