@@ -108,7 +108,8 @@ typedef enum {
     MEMOROID_OP_TBB_BEGIN_INDICES = 8, /* memoroid_tbb_begin_indices[_prepared]: (T = n) */
     MEMOROID_OP_TBB_SAMPLE = 9,        /* memoroid_tbb_sample[_prepared]:     (B = n_draws, T = batch) */
     MEMOROID_OP_RETENTION = 10,        /* memoroid_scan_retention:      (B, T, d_or_H = H, dk, dv) */
-    MEMOROID_OP_RETENTION_BWD = 11     /* memoroid_scan_retention_bwd:  (B, T, d_or_H = H, dk, dv), any Hk */
+    MEMOROID_OP_RETENTION_BWD = 11,    /* memoroid_scan_retention_bwd:  (B, T, d_or_H = H, dk, dv), any Hk */
+    MEMOROID_OP_ROTATE_QK_BWD = 12     /* memoroid_rotate_qk_bwd:       (T = n, d_or_H = H, dk = Hk, dv = d) */
 } memoroid_op;
 
 /* Version of this header the library was built from (MEMOROID_ABI_VERSION). */
@@ -448,6 +449,57 @@ int memoroid_retention_step(const void* q, const void* k, const void* v, const f
                             const uint8_t* start, float* state, void* out, float scale,
                             int64_t B, int64_t H, int64_t Hk, int64_t dk, int64_t dv, int dtype,
                             void* stream);
+
+/* ------------------------------------------------------------------------
+ * Queries and keys of a layer, for retention or any attention: RMS norm of each
+ * head and the rotation by position, in one pass.  Per head row x of q (of k
+ * likewise, with wk):
+ *     y = x wq / sqrt(mean(x^2) + eps)          (y = x when wq is NULL)
+ *     (y_a, y_b) -> amplitude (y_a cos - y_b sin, y_b cos + y_a sin)  for the pairs
+ * p < rot / 2, angle = positions[i] * freq[p]; elements rot .. d - 1 stay.  A pair
+ * is (p, p + rot / 2), or (2 p, 2 p + 1) when interleaved is nonzero.
+ * Angles are reduced in 64 bits: far positions keep fp32's precision.
+ *
+ *   q          [n][H][d];  k: [n][Hk][d], n steps (B * T of them), of `dtype`
+ *              (MEMOROID_F32 or MEMOROID_BF16).  H or Hk may be 0: that tensor and
+ *              its output are then not touched and may be NULL.
+ *   positions  [n] int32, e.g. the step's place in its episode;  freq: [rot / 2]
+ *              fp32, radians per position, which is where contexts longer than
+ *              the trained ones are scaled.  Both may be NULL when rot is 0.
+ *   wq, wk     optional [d] fp32.
+ *   q_out, k_out  like q and k.
+ *   eps >= 0 and amplitude finite; rot even, 0 <= rot <= d (MEMOROID_EINVAL
+ *   otherwise).  d a multiple of 8 up to 128 (MEMOROID_EUNSUPPORTED otherwise).
+ *   q, k and outputs 16-byte aligned.  No workspace.
+ * ------------------------------------------------------------------------ */
+int memoroid_rotate_qk(const void* q, const void* k, const int32_t* positions, const float* freq,
+                       const float* wq, const float* wk, void* q_out, void* k_out,
+                       float eps, float amplitude, int interleaved,
+                       int64_t n, int64_t H, int64_t Hk, int64_t d, int64_t rot, int dtype, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Its gradient.  With g the upstream gradient turned back (and times the
+ * amplitude) and r = 1 / sqrt(mean(x^2) + eps):
+ *     dwq = sum over rows of g x r,   dq = r g wq - x r^3 mean(g wq x)
+ * (dq = g without a norm).
+ *
+ *   q, k       as in the forward call; read only where wq (wk) is given, may be
+ *              NULL otherwise.
+ *   grad_q_out, grad_k_out  upstream gradients, like q and k.
+ *   grad_q, grad_k  out, like q and k.
+ *   grad_wq, grad_wk  optional out [d] fp32; only with wq (wk).
+ *   Workspace (self-initialising), needed only for grad_wq or grad_wk:
+ *   memoroid_rotate_qk_bwd_workspace_bytes.
+ * ------------------------------------------------------------------------ */
+size_t memoroid_rotate_qk_bwd_workspace_bytes(int64_t n, int64_t H, int64_t Hk, int64_t d, int64_t rot,
+                                              int interleaved, int dtype);
+
+int memoroid_rotate_qk_bwd(const void* q, const void* k, const int32_t* positions, const float* freq,
+                           const float* wq, const float* wk,
+                           const void* grad_q_out, const void* grad_k_out, void* grad_q, void* grad_k,
+                           float* grad_wq, float* grad_wk, float eps, float amplitude, int interleaved,
+                           int64_t n, int64_t H, int64_t Hk, int64_t d, int64_t rot, int dtype,
+                           void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * Discounted return over a tape (App. D, the discounted-return memoroid

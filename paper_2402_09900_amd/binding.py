@@ -23,6 +23,7 @@ from __future__ import annotations
 
 import collections
 import ctypes
+import math
 import os
 import threading
 from typing import Optional, Tuple
@@ -33,7 +34,7 @@ LIB_PATH = os.path.join(HERE, "libmemoroid.so")
 OK, EINVAL, EUNSUPPORTED, EWORKSPACE, EHIP, ETIMEOUT, EMISMATCH = 0, -1, -2, -3, -4, -5, -6
 F32, BF16, C64 = 0, 1, 2
 (OP_DIAG, OP_DIAG_BWD, OP_LINATTN, OP_LINATTN_BWD, OP_FFM, OP_FFM_BWD, OP_RETURN, OP_GAE,
- OP_TBB_BEGIN_INDICES, OP_TBB_SAMPLE, OP_RETENTION, OP_RETENTION_BWD) = range(12)
+ OP_TBB_BEGIN_INDICES, OP_TBB_SAMPLE, OP_RETENTION, OP_RETENTION_BWD, OP_ROTATE_QK_BWD) = range(13)
 
 _lib = None
 
@@ -120,6 +121,12 @@ def lib() -> ctypes.CDLL:
         L.memoroid_scan_retention_bwd.argtypes = [P] * 13 + [F] + [I64] * 6 + [I32, P, SZ, P]
         L.memoroid_retention_step.restype = I32
         L.memoroid_retention_step.argtypes = [P] * 7 + [F] + [I64] * 5 + [I32, P]
+        L.memoroid_rotate_qk.restype = I32
+        L.memoroid_rotate_qk.argtypes = [P] * 8 + [F, F, I32] + [I64] * 5 + [I32, P]
+        L.memoroid_rotate_qk_bwd_workspace_bytes.restype = SZ
+        L.memoroid_rotate_qk_bwd_workspace_bytes.argtypes = [I64] * 5 + [I32, I32]
+        L.memoroid_rotate_qk_bwd.restype = I32
+        L.memoroid_rotate_qk_bwd.argtypes = [P] * 12 + [F, F, I32] + [I64] * 5 + [I32, P, SZ, P]
         L.memoroid_testing_set_fallback_polls.restype = I64
         L.memoroid_testing_set_fallback_polls.argtypes = [I64]
         L.memoroid_testing_tile_steps.restype = I64
@@ -328,6 +335,23 @@ def memoroid_scan_retention_bwd(q, k, v, alpha, start, state_in, grad_out, grad_
 
 def memoroid_retention_step(q, k, v, alpha, start, state, out, scale, B, H, Hk, dk, dv, dtype, stream) -> int:
     return lib().memoroid_retention_step(q, k, v, alpha, start, state, out, scale, B, H, Hk, dk, dv, dtype, stream)
+
+
+def memoroid_rotate_qk(q, k, positions, freq, wq, wk, q_out, k_out, eps, amplitude, interleaved, n, H, Hk, d, rot, dtype,
+                       stream) -> int:
+    return lib().memoroid_rotate_qk(q, k, positions, freq, wq, wk, q_out, k_out, eps, amplitude, interleaved, n, H, Hk, d,
+                                    rot, dtype, stream)
+
+
+def memoroid_rotate_qk_bwd_workspace_bytes(n, H, Hk, d, rot, interleaved, dtype) -> int:
+    return lib().memoroid_rotate_qk_bwd_workspace_bytes(n, H, Hk, d, rot, interleaved, dtype)
+
+
+def memoroid_rotate_qk_bwd(q, k, positions, freq, wq, wk, grad_q_out, grad_k_out, grad_q, grad_k, grad_wq, grad_wk, eps,
+                           amplitude, interleaved, n, H, Hk, d, rot, dtype, workspace, workspace_bytes, stream) -> int:
+    return lib().memoroid_rotate_qk_bwd(q, k, positions, freq, wq, wk, grad_q_out, grad_k_out, grad_q, grad_k, grad_wq,
+                                        grad_wk, eps, amplitude, interleaved, n, H, Hk, d, rot, dtype, workspace,
+                                        workspace_bytes, stream)
 
 
 def memoroid_workspace_status(workspace, workspace_bytes, stream) -> int:
@@ -868,6 +892,101 @@ def retention_step(q, k, v, alpha, state, start=None, scale: Optional[float] = N
     return out
 
 
+def rotary_frequencies(rot: int, base: float = 10000.0, factor: float = 1.0, original_length: Optional[int] = None,
+                       fast: float = 32.0, slow: float = 1.0, device=None):
+    """Radians per position of the rot / 2 pairs, float32: base^(-2 p / rot).
+
+    factor > 1 scales them for contexts that many times longer than the trained
+    ones: all by 1 / factor, or, with original_length (the trained length), only
+    the pairs that turn less than `slow` times over it, not those that turn more
+    than `fast` times, the ones between in part."""
+    torch = _torch()
+    if rot < 0 or rot % 2 or base <= 0 or factor <= 0 or not slow < fast:
+        raise ValueError("rot must be even, base and factor positive, slow below fast")
+    f = base ** (-torch.arange(0, rot, 2, dtype=torch.float64) / max(rot, 1))
+    if original_length is None:
+        f = f / factor
+    else:
+        turns = original_length * f / (2 * math.pi)
+        keep = ((turns - slow) / (fast - slow)).clamp(0, 1)
+        f = f * keep + f / factor * (1 - keep)
+    return f.float().to(device) if device is not None else f.float()
+
+
+def _rotate_args(q, k, positions, freq, wq, wk, name="q and k"):
+    torch = _torch()
+    if q.dim() < 3 or (k is not None and (k.dim() != q.dim() or k.shape[:-2] != q.shape[:-2] or
+                                          k.shape[-1] != q.shape[-1])):
+        raise ValueError("q must be [...,H,d] and k [...,Hk,d]")
+    if k is not None and k.dtype != q.dtype:
+        raise TypeError("%s must share a dtype" % name)
+    dt = _code_of(q.dtype)
+    if dt == C64:
+        raise TypeError("rotation takes float32 or bfloat16")
+    H, d = q.shape[-2:]
+    rot = 0 if freq is None else 2 * freq.numel()
+    if freq is not None and (freq.dtype != torch.float32 or freq.dim() != 1 or rot > d):
+        raise TypeError("freq must be float32 [rot / 2], rot at most d")
+    if rot and (positions is None or positions.dtype != torch.int32 or positions.shape != q.shape[:-2]):
+        raise TypeError("positions must be int32 of q's leading shape")
+    for w in (wq, wk):
+        if w is not None and (w.dtype != torch.float32 or w.shape != (d,)):
+            raise TypeError("wq and wk must be float32 [d]")
+    if k is None and wk is not None:
+        raise ValueError("wk without k")
+    n = 1
+    for x in q.shape[:-2]:
+        n *= x
+    return n, H, (0 if k is None else k.shape[-2]), d, rot, dt
+
+
+def rotate_qk(q, k, positions, freq, wq=None, wk=None, eps: float = 1e-6, interleaved: bool = False,
+              amplitude: float = 1.0):
+    """RMS norm of every head of q and k (by wq, wk; none where they are None) and
+    the rotation of its first 2 * len(freq) elements by positions * freq, in one
+    pass.  q: [...,H,d], k: [...,Hk,d] or None, float32 or bfloat16; positions:
+    int32 [...]; freq: float32 [rot / 2] (rotary_frequencies), None for norms
+    alone; wq, wk: float32 [d].  Pairs are (p, p + rot / 2), or neighbours when
+    interleaved.  Returns (q, k) so treated."""
+    torch = _torch()
+    n, H, Hk, d, rot, dt = _rotate_args(q, k, positions, freq, wq, wk)
+    dev = _check_cuda(q, k, positions, freq, wq, wk)
+    qo = torch.empty_like(q)
+    ko = None if k is None else torch.empty_like(k)
+    with torch.cuda.device(dev):
+        st = lib().memoroid_rotate_qk(q.data_ptr(), _ptr(k), _ptr(positions), _ptr(freq), _ptr(wq), _ptr(wk),
+                                      qo.data_ptr(), _ptr(ko), eps, amplitude, interleaved, n, H, Hk, d, rot, dt,
+                                      _stream_ptr(dev))
+    _raise(st, "memoroid_rotate_qk")
+    return qo, ko
+
+
+def rotate_qk_bwd(q, k, positions, freq, grad_q, grad_k, wq=None, wk=None, eps: float = 1e-6, interleaved: bool = False,
+                  amplitude: float = 1.0, need_grad_weights: bool = True, workspace=None):
+    """Gradient of rotate_qk: (dq, dk, dwq, dwk), None for what there is not."""
+    torch = _torch()
+    n, H, Hk, d, rot, dt = _rotate_args(q, k, positions, freq, wq, wk)
+    if grad_q.shape != q.shape or grad_q.dtype != q.dtype or (k is None) != (grad_k is None) or \
+            (k is not None and (grad_k.shape != k.shape or grad_k.dtype != k.dtype)):
+        raise TypeError("grad_q and grad_k must be like q and k")
+    dev = _check_cuda(q, k, positions, freq, wq, wk, grad_q, grad_k)
+    gq = torch.empty_like(q)
+    gk = None if k is None else torch.empty_like(k)
+    # (no rows: sums of nothing)
+    gwq, gwk = ((torch.empty_like(w) if n and x is not None and x.numel() else torch.zeros_like(w))
+                if need_grad_weights and w is not None else None for w, x in ((wq, q), (wk, k)))
+    ws = None
+    if gwq is not None or gwk is not None:
+        ws = _workspace(lib().memoroid_rotate_qk_bwd_workspace_bytes(n, H, Hk, d, rot, interleaved, dt), dev, workspace)
+    with torch.cuda.device(dev):
+        st = lib().memoroid_rotate_qk_bwd(q.data_ptr(), _ptr(k), _ptr(positions), _ptr(freq), _ptr(wq), _ptr(wk),
+                                          grad_q.data_ptr(), _ptr(grad_k), gq.data_ptr(), _ptr(gk), _ptr(gwq), _ptr(gwk),
+                                          eps, amplitude, interleaved, n, H, Hk, d, rot, dt, _ptr(ws),
+                                          0 if ws is None else ws.numel(), _stream_ptr(dev))
+    _raise(st, "memoroid_rotate_qk_bwd")
+    return gq, gk, gwq, gwk
+
+
 def workspace_status(workspace) -> int:
     """Synchronise and report OK, ETIMEOUT (a cross-tile wait gave up) or
     EMISMATCH (a prepared workspace was bound to another call) for the calls
@@ -980,3 +1099,39 @@ def retention(q, k, v, alpha, start, scale: Optional[float] = None, state=None, 
     if _Retention is None:
         _Retention = _make_retention_autograd()
     return _Retention.apply(q, k, v, alpha, start, scale, state, final_state)
+
+
+def _make_rotate_autograd():
+    torch = _torch()
+
+    class RotateQK(torch.autograd.Function):
+        """Differentiable norms and rotation of queries and keys."""
+
+        @staticmethod
+        def forward(ctx, q, k, positions, freq, wq, wk, eps, interleaved, amplitude):
+            got = rotate_qk(q, k, positions, freq, wq, wk, eps, interleaved, amplitude)
+            ctx.save_for_backward(q, k, positions, freq, wq, wk)
+            ctx.more = (eps, interleaved, amplitude)
+            return got
+
+        @staticmethod
+        def backward(ctx, grad_q, grad_k):
+            q, k, positions, freq, wq, wk = ctx.saved_tensors
+            gq, gk, gwq, gwk = rotate_qk_bwd(q, k, positions, freq, grad_q.contiguous(),
+                                             None if k is None else grad_k.contiguous(), wq, wk, *ctx.more,
+                                             need_grad_weights=ctx.needs_input_grad[4] or ctx.needs_input_grad[5])
+            return gq, gk, None, None, gwq, gwk, None, None, None
+
+    return RotateQK
+
+
+_RotateQK = None
+
+
+def qk_rotate(q, k, positions, freq, wq=None, wk=None, eps: float = 1e-6, interleaved: bool = False,
+              amplitude: float = 1.0):
+    """Autograd-aware rotate_qk: gradients of q, k, wq and wk."""
+    global _RotateQK
+    if _RotateQK is None:
+        _RotateQK = _make_rotate_autograd()
+    return _RotateQK.apply(q, k, positions, freq, wq, wk, eps, interleaved, amplitude)

@@ -70,7 +70,7 @@ uint64_t layout_sig(std::initializer_list<int64_t> vals) {
 
 // entry points in a signature
 enum SigKind : int64_t { kSigDiag = 1, kSigDiagBwd, kSigFfm, kSigFfmBwd, kSigDiscount, kSigTbbBegins,
-                         kSigLinattn, kSigLinattnBwd, kSigTbbSample, kSigRetention, kSigRetentionBwd };
+                         kSigLinattn, kSigLinattnBwd, kSigTbbSample, kSigRetention, kSigRetentionBwd, kSigRotateBwd };
 
 // Tiling and workspace layout of a diagonal scan.  `vec` selects the
 // vectorised lane width; `state_complex` picks the descriptor size.
@@ -1268,6 +1268,176 @@ int memoroid_retention_step(const void* q, const void* k, const void* v, const f
     return check_hip(ret_step_launch(ret_planes(dtype), a, (hipStream_t)stream));
 }
 
+// ----------------------------------------- norms and rotation of queries, keys
+
+namespace {
+
+struct RotPlan {
+    int ch = 1, lpr = 1, parts = 1;
+    int64_t groups = 0;
+    size_t off_part = 0, total = 0;
+};
+
+// Runs of ch elements per lane, as long as 16 bytes and the layout allow: a
+// row is a whole number of pairs of runs, and in the half layout so are its
+// turned part and its rest.  Short batches share a step among wavefronts.
+void plan_rotate(int64_t n, int64_t H, int64_t Hk, int64_t d, int64_t rot, bool inter, int dtype, bool grad, RotPlan* p) {
+    int ch = dtype == MEMOROID_BF16 ? 8 : 4;
+    while (ch > 1 && (d % (2 * ch) != 0 || (!inter && rot % (2 * ch) != 0))) ch /= 2;
+    p->ch = ch;
+    p->lpr = (int)next_pow2(d / (2 * ch));
+    const int64_t rows = H + Hk, at_once = 64 / p->lpr;
+    const int64_t most = (rows + at_once - 1) / at_once;
+    int64_t parts = n >= 8192 ? 1 : (8192 + n - 1) / n;
+    if (parts > most) parts = most;
+    p->parts = (int)parts;
+    const int64_t per = n > INT64_MAX / parts ? INT64_MAX / 4 : n * parts;
+    const int64_t cap = grad ? 1024 : 2048;
+    p->groups = (per + 3) / 4 < cap ? (per + 3) / 4 : cap;
+    p->off_part = kAlign;
+    p->total = align_up(kAlign + (size_t)p->groups * 2 * (size_t)d * 4);
+}
+
+int rot_check(int64_t n, int64_t H, int64_t Hk, int64_t d, int64_t rot, float eps, float amplitude, int dtype, bool* empty) {
+    *empty = false;
+    if (n < 0 || H < 0 || Hk < 0 || d < 0 || rot < 0 || rot > d || rot % 2 != 0 || !(eps >= 0.0f) || !std::isfinite(eps) ||
+        !std::isfinite(amplitude))
+        return MEMOROID_EINVAL;
+    if (dtype != MEMOROID_F32 && dtype != MEMOROID_BF16) return MEMOROID_EUNSUPPORTED;
+    if (n == 0 || (H == 0 && Hk == 0)) {
+        *empty = true;
+        return MEMOROID_OK;
+    }
+    if (d == 0 || d % 8 != 0 || d > kRotMaxDim || H > 65535 || Hk > 65535 || n > ((int64_t)1 << 40))
+        return MEMOROID_EUNSUPPORTED;
+    return MEMOROID_OK;
+}
+// the shared operands: positions and frequencies where something turns
+bool rot_tables_ok(const int32_t* positions, const float* freq, const float* wq, const float* wk, int64_t rot) {
+    if (rot > 0 && (!positions || !freq)) return false;
+    return aligned(positions, 4) && aligned(freq, 4) && aligned(wq, 4) && aligned(wk, 4);
+}
+bool rot_distinct(std::initializer_list<const void*> ins, std::initializer_list<const void*> outs) {
+    const void* seen[4];
+    int n = 0;
+    for (const void* o : outs) {
+        if (!o) continue;
+        for (const void* i : ins)
+            if (i == o) return false;
+        for (int j = 0; j < n; ++j)
+            if (seen[j] == o) return false;
+        seen[n++] = o;
+    }
+    return true;
+}
+
+}  // namespace
+
+int memoroid_rotate_qk(const void* q, const void* k, const int32_t* positions, const float* freq, const float* wq,
+                       const float* wk, void* q_out, void* k_out, float eps, float amplitude, int interleaved, int64_t n,
+                       int64_t H, int64_t Hk, int64_t d, int64_t rot, int dtype, void* stream) {
+    bool empty;
+    const int ok = rot_check(n, H, Hk, d, rot, eps, amplitude, dtype, &empty);
+    if (ok != MEMOROID_OK || empty) return ok;
+    if (H == 0) q = q_out = nullptr;
+    if (Hk == 0) k = k_out = nullptr;
+    if ((H > 0 && (!q || !q_out)) || (Hk > 0 && (!k || !k_out))) return MEMOROID_EINVAL;
+    if (!rot_tables_ok(positions, freq, wq, wk, rot)) return MEMOROID_EINVAL;
+    for (const void* x : {q, k, (const void*)q_out, (const void*)k_out})
+        if (!aligned(x, 16)) return MEMOROID_EINVAL;
+    if (!rot_distinct({q, k, positions, freq, wq, wk}, {q_out, k_out})) return MEMOROID_EINVAL;
+    RotPlan p;
+    plan_rotate(n, H, Hk, d, rot, interleaved != 0, dtype, false, &p);
+    RotateArgs a{};
+    a.q = q;
+    a.k = k;
+    a.positions = positions;
+    a.freq = freq;
+    a.wq = wq;
+    a.wk = wk;
+    a.q_out = q_out;
+    a.k_out = k_out;
+    a.eps = eps;
+    a.amplitude = amplitude;
+    a.inter = interleaved != 0;
+    a.H = (int32_t)H;
+    a.Hk = (int32_t)Hk;
+    a.d = (int32_t)d;
+    a.rot = (int32_t)rot;
+    a.lpr = p.lpr;
+    a.parts = p.parts;
+    a.n = n;
+    return check_hip(rotate_launch(dtype == MEMOROID_BF16, false, p.ch, p.groups, a, (hipStream_t)stream));
+}
+
+size_t memoroid_rotate_qk_bwd_workspace_bytes(int64_t n, int64_t H, int64_t Hk, int64_t d, int64_t rot, int interleaved,
+                                              int dtype) {
+    bool empty;
+    if (rot_check(n, H, Hk, d, rot, 0.0f, 1.0f, dtype, &empty) != MEMOROID_OK || empty) return 0;
+    RotPlan p;
+    plan_rotate(n, H, Hk, d, rot, interleaved != 0, dtype, true, &p);
+    return p.total;
+}
+
+int memoroid_rotate_qk_bwd(const void* q, const void* k, const int32_t* positions, const float* freq, const float* wq,
+                           const float* wk, const void* grad_q_out, const void* grad_k_out, void* grad_q, void* grad_k,
+                           float* grad_wq, float* grad_wk, float eps, float amplitude, int interleaved, int64_t n,
+                           int64_t H, int64_t Hk, int64_t d, int64_t rot, int dtype, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+    bool empty;
+    const int ok = rot_check(n, H, Hk, d, rot, eps, amplitude, dtype, &empty);
+    if (ok != MEMOROID_OK || empty) return ok;
+    if (H == 0) grad_q_out = grad_q = nullptr;
+    if (Hk == 0) grad_k_out = grad_k = nullptr;
+    if (H == 0 || !wq) q = nullptr;                        // not read
+    if (Hk == 0 || !wk) k = nullptr;
+    if ((H > 0 && (!grad_q_out || !grad_q || (wq && !q))) || (Hk > 0 && (!grad_k_out || !grad_k || (wk && !k))))
+        return MEMOROID_EINVAL;
+    if ((grad_wq && !wq) || (grad_wk && !wk)) return MEMOROID_EINVAL;
+    if (!rot_tables_ok(positions, freq, wq, wk, rot) || !aligned(grad_wq, 4) || !aligned(grad_wk, 4)) return MEMOROID_EINVAL;
+    for (const void* x : {q, k, grad_q_out, grad_k_out, (const void*)grad_q, (const void*)grad_k})
+        if (!aligned(x, 16)) return MEMOROID_EINVAL;
+    if (!rot_distinct({q, k, positions, freq, wq, wk, grad_q_out, grad_k_out}, {grad_q, grad_k, grad_wq, grad_wk}))
+        return MEMOROID_EINVAL;
+    RotPlan p;
+    plan_rotate(n, H, Hk, d, rot, interleaved != 0, dtype, true, &p);
+    const bool weights = grad_wq || grad_wk;
+    if (weights) {
+        if (!workspace || workspace_bytes < p.total) return MEMOROID_EWORKSPACE;
+        if (!aligned(workspace, 16)) return MEMOROID_EINVAL;
+    }
+    RotateArgs a{};
+    a.q = q;
+    a.k = k;
+    a.gq = grad_q_out;
+    a.gk = grad_k_out;
+    a.positions = positions;
+    a.freq = freq;
+    a.wq = wq;
+    a.wk = wk;
+    a.q_out = grad_q;
+    a.k_out = grad_k;
+    a.part = weights ? (float*)((char*)workspace + p.off_part) : nullptr;
+    a.eps = eps;
+    a.amplitude = amplitude;
+    a.inter = interleaved != 0;
+    a.H = (int32_t)H;
+    a.Hk = (int32_t)Hk;
+    a.d = (int32_t)d;
+    a.rot = (int32_t)rot;
+    a.lpr = p.lpr;
+    a.parts = p.parts;
+    a.n = n;
+    if (weights) {
+        a.hdr = (WsHeader*)workspace;
+        a.sig = layout_sig({kSigRotateBwd, n, H, Hk, d, rot, interleaved != 0, dtype});
+    }
+    hipStream_t s = (hipStream_t)stream;
+    if (rotate_launch(dtype == MEMOROID_BF16, true, p.ch, p.groups, a, s) != hipSuccess) return MEMOROID_EHIP;
+    if (!weights) return MEMOROID_OK;
+    return check_hip(rotate_weights_launch(a.part, grad_wq, grad_wk, p.groups, (int)d, s));
+}
+
 // ------------------------------------------------------------------ status
 
 // ------------------------------------------- discounted return and GAE
@@ -1661,6 +1831,12 @@ size_t memoroid_workspace_bytes(memoroid_op op_in, int64_t B, int64_t T, int64_t
         case MEMOROID_OP_RETENTION_BWD:
             for (int dt : {MEMOROID_F32, MEMOROID_BF16})
                 take(memoroid_scan_retention_bwd_workspace_bytes(B, T, d_or_H, 1, dk, dv, dt, 1));
+            return best;
+        case MEMOROID_OP_ROTATE_QK_BWD:
+            // any rotated width and layout: the narrowest runs take the most groups
+            for (int dt : {MEMOROID_F32, MEMOROID_BF16})
+                for (int64_t rot : {(int64_t)0, (int64_t)2})
+                    take(memoroid_rotate_qk_bwd_workspace_bytes(T, d_or_H, dk, dv, rot, 0, dt));
             return best;
     }
     return 0;

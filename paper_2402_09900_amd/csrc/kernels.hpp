@@ -382,6 +382,29 @@ struct RetStepArgs {
 };
 hipError_t ret_step_launch(int planes, const RetStepArgs& a, hipStream_t s);
 
+// Norms and rotation of queries and keys (rotate.hip)
+constexpr int kRotMaxDim = 128;
+struct RotateArgs {
+    const void* q;              // [n][H][d]; k: [n][Hk][d]
+    const void* k;
+    const void* gq;             // gradient: upstream gradients, like q and k
+    const void* gk;
+    const int32_t* positions;   // [n]
+    const float* freq;          // [rot / 2]
+    const float* wq;            // [d], or NULL: no norm
+    const float* wk;
+    void* q_out;                // results, or the gradients of q and k
+    void* k_out;
+    float* part;                // gradient: [groups][2 d] sums for wq and wk, or NULL
+    float eps, amplitude;
+    int32_t inter, H, Hk, d, rot, lpr, parts;   // lanes per row; wavefronts that share a step
+    int64_t n;
+    WsHeader* hdr;              // header to prepare with sig, or NULL
+    uint64_t sig;
+};
+hipError_t rotate_launch(bool bf16, bool grad, int ch, int64_t groups, const RotateArgs& a, hipStream_t s);
+hipError_t rotate_weights_launch(const float* part, float* dwq, float* dwk, int64_t groups, int d, hipStream_t s);
+
 // ------------------------------------------- discounted return and GAE
 // Steps per lane: 32 for the return (two streams in registers), 16 for the
 // advantage (four); a tile is 4 wavefronts of 64 lanes.

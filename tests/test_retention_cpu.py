@@ -148,3 +148,86 @@ def test_torch_layer_refuses():
         mb.retention_step(q[:, 0], k[:, 0], k[:, 0], a, None)
     with pytest.raises(TypeError):
         mb.retention_step(q[:, 0], k[:, 0], k[:, 0], a, S, s[0])
+
+
+def rot(q=P[0], k=P[1], pos=P[2], freq=P[3], wq=P[4], wk=P[5], qo=P[6], ko=P[7], eps=1e-6, amp=1.0, inter=0, n=10, H=4, Hk=2,
+        d=64, rot=64, dtype=mb.F32):
+    return mb.memoroid_rotate_qk(q, k, pos, freq, wq, wk, qo, ko, eps, amp, inter, n, H, Hk, d, rot, dtype, None)
+
+
+def rotb(q=P[0], k=P[1], pos=P[2], freq=P[3], wq=P[4], wk=P[5], gq=P[6], gk=P[7], dq=P[8], dk_=P[9], dwq=P[10], dwk=P[11],
+         eps=1e-6, amp=1.0, inter=0, n=10, H=4, Hk=2, d=64, rot=64, dtype=mb.F32, ws=P[12], nbytes=1 << 40):
+    return mb.memoroid_rotate_qk_bwd(q, k, pos, freq, wq, wk, gq, gk, dq, dk_, dwq, dwk, eps, amp, inter, n, H, Hk, d, rot,
+                                     dtype, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("call", [rot, rotb])
+def test_rotation_refusals(call):
+    nan, inf = float("nan"), float("inf")
+    for change in (dict(n=-1), dict(H=-1), dict(Hk=-1), dict(d=-8), dict(rot=-2), dict(rot=3), dict(rot=66), dict(eps=-1.0),
+                   dict(eps=nan), dict(eps=inf), dict(amp=nan), dict(amp=inf), dict(pos=None), dict(freq=None),
+                   dict(pos=0x900002), dict(freq=0x900002), dict(wq=0x900002), dict(wk=0x900001), dict(q=0x900008),
+                   dict(k=0x900008)):
+        assert call(**change) == mb.EINVAL, change
+    for change in (dict(d=136, rot=0), dict(d=60, rot=0), dict(dtype=mb.C64), dict(dtype=9), dict(H=65536), dict(Hk=65536),
+                   dict(n=1 << 50)):
+        assert call(**change) == mb.EUNSUPPORTED, change
+    for change in (dict(n=0), dict(H=0, Hk=0)):
+        assert call(**change) == mb.OK, change
+    outs = ("qo", "ko") if call is rot else ("dq", "dk_", "dwq", "dwk")
+    ins = ("q", "k", "pos", "freq", "wq", "wk") + (() if call is rot else ("gq", "gk"))
+    for o in outs:
+        for i in ins + tuple(x for x in outs if x != o):
+            assert call(**{o: 0x900000, i: 0x900000}) == mb.EINVAL, (o, i)
+    for n in outs[:2] + (("q", "k") if call is rot else ("q", "k", "gq", "gk")):
+        assert call(**{n: None}) == mb.EINVAL, n
+
+
+def test_rotation_gradient_weights_and_workspace():
+    assert rotb(wq=None) == mb.EINVAL                       # dwq without wq
+    assert rotb(wk=None) == mb.EINVAL
+    assert rotb(ws=None) == mb.EWORKSPACE
+    need = mb.memoroid_rotate_qk_bwd_workspace_bytes(10, 4, 2, 64, 64, 0, mb.F32)
+    assert rotb(nbytes=need - 1) == mb.EWORKSPACE
+    assert rotb(ws=0x900008) == mb.EINVAL
+    for dt in (mb.F32, mb.BF16):
+        for n in (1, 100, 5000, 100000):
+            for r in (0, 2, 20, 64):
+                for inter in (0, 1):
+                    assert mb.memoroid_rotate_qk_bwd_workspace_bytes(n, 4, 2, 64, r, inter, dt) <= \
+                        mb.memoroid_workspace_bytes(mb.OP_ROTATE_QK_BWD, 0, n, 4, 2, 64, 0)
+    assert mb.memoroid_rotate_qk_bwd_workspace_bytes(10, 4, 2, 60, 20, 0, mb.F32) == 0
+
+
+def test_rotation_torch_layer_refuses():
+    q, k = torch.zeros(2, 5, 4, 64), torch.zeros(2, 5, 2, 64)
+    pos, f, w = torch.zeros(2, 5, dtype=torch.int32), torch.ones(32), torch.ones(64)
+    for err, args, kw in ((ValueError, (q[0, 0], None, pos, f), {}), (ValueError, (q, k[:1], pos, f), {}),
+                          (ValueError, (q, k[..., :32], pos, f), {}), (TypeError, (q, k.bfloat16(), pos, f), {}),
+                          (TypeError, (q.half(), k.half(), pos, f), {}), (TypeError, (q, k, pos.long(), f), {}),
+                          (TypeError, (q, k, None, f), {}), (TypeError, (q, k, pos[:1], f), {}),
+                          (TypeError, (q, k, pos, f.double()), {}), (TypeError, (q, k, pos, torch.ones(33)), {}),
+                          (TypeError, (q, k, pos, f), dict(wq=w[:32])), (TypeError, (q, k, pos, f), dict(wk=w.bfloat16())),
+                          (ValueError, (q, None, pos, f), dict(wk=w)), (ValueError, (q, k, pos, f), {})):
+        with pytest.raises(err):
+            mb.rotate_qk(*args, **kw)
+    with pytest.raises(TypeError):
+        mb.rotate_qk_bwd(q, k, pos, f, q, None)
+    for bad in (dict(rot=3), dict(rot=-2), dict(rot=4, base=0.0), dict(rot=4, factor=0.0), dict(rot=4, fast=1.0, slow=2.0)):
+        with pytest.raises(ValueError):
+            mb.rotary_frequencies(**bad)
+
+
+def test_rotation_reference_against_differences():
+    import rotate_ref
+    rng = np.random.default_rng(1)
+    for inter in (False, True):
+        x, w, g = rng.standard_normal((2, 3, 2, 12)), rng.standard_normal(12), rng.standard_normal((2, 3, 2, 12))
+        pos, f = rng.integers(0, 50, (2, 3)), rng.uniform(0, 1, 4)
+        args = (pos, f, 1e-3, 1.2, inter)
+        _, (dx, _), (dw, _) = rotate_ref.rotate(x, w, *args, grad=g)
+        u, uw, h = rng.standard_normal(x.shape), rng.standard_normal(12), 1e-6
+        num = ((rotate_ref.rotate(x + h * u, w, *args)[0][0] - rotate_ref.rotate(x - h * u, w, *args)[0][0]) * g).sum() / (2 * h)
+        assert abs(num - (dx * u).sum()) <= 1e-6 * (1 + abs(num))
+        num = ((rotate_ref.rotate(x, w + h * uw, *args)[0][0] - rotate_ref.rotate(x, w - h * uw, *args)[0][0]) * g).sum() / (2 * h)
+        assert abs(num - (dw * uw).sum()) <= 1e-6 * (1 + abs(num))
