@@ -32,34 +32,34 @@ __device__ __forceinline__ void ret_header(WsHeader* hdr, uint64_t sig) {
     }
 }
 
-template <int ES>
-__device__ __forceinline__ const void* role_head(const RetRole& x, int64_t b, int64_t h, int64_t T) {
-    return (const char*)x.p + (b * T * x.heads + h / x.share) * x.d * ES;
+// a role as head h of tape b sees it
+struct Head {
+    const void* p;
+    int64_t row_bytes;
+    int d;
+};
+template <class Cfg>
+__device__ __forceinline__ Head head_of(const RetRole& x, int64_t b, int64_t h, int64_t T) {
+    return Head{(const char*)x.p + (b * T * x.heads + h / x.share) * x.d * Cfg::ES, (int64_t)x.heads * x.d * Cfg::ES, x.d};
+}
+template <class Cfg>
+__device__ __forceinline__ RetRows rows_of(const Head& x, int64_t w0, int n, int64_t T, bool rev) {
+    return ret_rows(x.p, x.row_bytes, x.d, Cfg::ES, w0, n, T, rev);
 }
 
+// gamma^n and its carry for n = 0 .. C
 template <class Cfg>
-using State = f32x4[Cfg::KD / 32][2][Cfg::NT];
+struct Decays {
+    float pw[Cfg::C + 1];
+    Carry carry[Cfg::C + 1];
+    __device__ __forceinline__ void fill(double rate, int tid) {
+        if (tid <= Cfg::C) {
+            pw[tid] = decay_pow(rate, tid);
+            carry[tid] = carry_of(rate, tid);
+        }
+    }
+};
 
-template <class Cfg>
-__device__ __forceinline__ void zero_state(State<Cfg>& S) {
-#pragma unroll
-    for (int s = 0; s < Cfg::KD / 32; ++s)
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int nt = 0; nt < Cfg::NT; ++nt) S[s][u][nt] = zero4();
-}
-template <class Cfg>
-__device__ __forceinline__ void carry_state(State<Cfg>& S, const Carry& cy, bool drop) {
-#pragma unroll
-    for (int s = 0; s < Cfg::KD / 32; ++s)
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int nt = 0; nt < Cfg::NT; ++nt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) S[s][u][nt][e] = drop ? 0.0f : cy(S[s][u][nt][e]);
-}
 // the value operand times a weight per row, in planes
 template <class Cfg>
 __device__ __forceinline__ void weigh(bf16x8 (&out)[3], const bf16x8 (&z)[Cfg::NP], const float* w, int tb,
@@ -71,20 +71,6 @@ __device__ __forceinline__ void weigh(bf16x8 (&out)[3], const bf16x8 (&z)[Cfg::N
         hi[e] *= plane_value<Cfg::NP>(z, e + 4);
     }
     planes8<3>(lo, hi, out);
-}
-// S += y^T (weighted z) over rows 32 tb .. + 31
-template <class Cfg>
-__device__ __forceinline__ void state_add(State<Cfg>& S, const uint16_t* sY, const bf16x8 (&zw)[Cfg::NT][3], int tb,
-                                          const RetLane& L) {
-#pragma unroll
-    for (int s = 0; s < Cfg::KD / 32; ++s)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            bf16x8 y[Cfg::NP];
-            col_frag<Cfg, Cfg::LDK>(y, sY, tb, state_row_addr<Cfg>(s, u, L), L);
-#pragma unroll
-            for (int nt = 0; nt < Cfg::NT; ++nt) mma<Cfg::NP, 3>(S[s][u][nt], y, zw[nt]);
-        }
 }
 // tile `idx` of the triangle: rows 16 jb.. of y against rows 16 ib.. of x
 __device__ __forceinline__ void tile_of(int idx, int& jb, int& ib) {
@@ -108,20 +94,17 @@ __device__ __forceinline__ f32x4 pair_products(const uint16_t* sY, const uint16_
 // What a segment adds to the state after it: the sum over its rows from the last
 // begin on.  DOT: also its derivative by log gamma, sum (n-1-j) gamma^(n-1-j) y^T z.
 template <class Cfg, bool DOT>
-__global__ __launch_bounds__(256, 2) void ret_summary_kernel(RetSummaryArgs p) {
+__global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummaryArgs p) {
     __shared__ __attribute__((aligned(16))) uint16_t sY[Cfg::NP * Cfg::C * Cfg::LDK];
     __shared__ __attribute__((aligned(16))) uint16_t sZ[Cfg::NP * Cfg::C * Cfg::LDV];
-    __shared__ float sPw[Cfg::C + 1];
+    __shared__ Decays<Cfg> sD;
     __shared__ __attribute__((aligned(16))) float sW[DOT ? 2 : 1][Cfg::C];
-    const RetLane L;
+    RetLane L;
     const int64_t seg = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
     ret_header(p.hdr, p.sig);
     const double rate = fabs((double)p.alpha[h]);
-    if (L.tid <= Cfg::C) sPw[L.tid] = decay_pow(rate, L.tid);
-    const Carry full = carry_of(rate, Cfg::C);
-    const void* const y0 = role_head<Cfg::ES>(p.y, b, h, p.T);
-    const void* const z0 = role_head<Cfg::ES>(p.z, b, h, p.T);
-    const int64_t yrow = (int64_t)p.y.heads * p.y.d, zrow = (int64_t)p.z.heads * p.z.d;
+    sD.fill(rate, L.tid);
+    const Head hy = head_of<Cfg>(p.y, b, h, p.T), hz = head_of<Cfg>(p.z, b, h, p.T);
     const uint8_t* const start = p.start + b * p.T;
     State<Cfg> S, D;
     zero_state<Cfg>(S);
@@ -129,55 +112,64 @@ __global__ __launch_bounds__(256, 2) void ret_summary_kernel(RetSummaryArgs p) {
     bool any = false;
     RetTile<Cfg, Cfg::KD> ty;
     RetTile<Cfg, Cfg::VD> tz;
+    uint32_t flag;
+    // every segment here is a whole one: C rows per chunk (the last fetch, of a
+    // chunk that is not there, reads nothing)
+    auto fetch = [&](int ch) {
+        const bool have = ch < p.chunks;
+        const int64_t w0 = have ? (seg * p.chunks + ch) * Cfg::C : 0;
+        const int n = have ? Cfg::C : 0;
+        flag = ret_flag(start, w0, n, p.T, p.rev, L.lane);
+        ty.fetch(rows_of<Cfg>(hy, w0, n, p.T, p.rev), L);
+        tz.fetch(rows_of<Cfg>(hz, w0, n, p.T, p.rev), L);
+    };
+    fetch(0);
 #pragma unroll 1
     for (int ch = 0; ch < p.chunks; ++ch) {
-        // every segment here is a whole one: C rows per chunk
-        const int64_t w0 = (seg * p.chunks + ch) * Cfg::C;
-        ty.fetch(ret_rows<Cfg::ES>(y0, yrow, p.y.d, w0, Cfg::C, p.T, p.rev), L);
-        tz.fetch(ret_rows<Cfg::ES>(z0, zrow, p.z.d, w0, Cfg::C, p.T, p.rev), L);
-        const uint64_t m = ret_begins(start, w0, Cfg::C, p.T, p.rev, L.lane);
+        L.again();
+        const uint64_t m = __ballot(flag != 0u);
         const int from = m ? last_begin(m) : 0;
         any = any || m != 0;
-        __syncthreads();                                   // the last chunk's operands have been read
-        ty.template stage<Cfg::LDK>(sY, from, Cfg::C, L);
-        tz.template stage<Cfg::LDV>(sZ, from, Cfg::C, L);
+        barrier_lds();                                     // the last chunk's operands have been read
+        if (m) {
+            ty.template stage<Cfg::LDK, true>(sY, from, Cfg::C, L);
+            tz.template stage<Cfg::LDV, true>(sZ, from, Cfg::C, L);
+        } else {
+            ty.template stage<Cfg::LDK, false>(sY, 0, 0, L);
+            tz.template stage<Cfg::LDV, false>(sZ, 0, 0, L);
+        }
         if (L.tid < Cfg::C) {
             const int age = Cfg::C - 1 - L.tid;
-            const float w = L.tid >= from ? sPw[age] * p.z_scale : 0.0f;
+            const float w = L.tid >= from ? sD.pw[age] * p.z_scale : 0.0f;
             sW[0][L.tid] = w;
             if (DOT) sW[DOT ? 1 : 0][L.tid] = w * (float)age;
         }
-        __syncthreads();
+        fetch(ch + 1);
+        barrier_lds();
         if (DOT) {
             // d(gamma^C S)/dlog gamma = gamma^C (D + C S)
-#pragma unroll
-            for (int s = 0; s < Cfg::KD / 32; ++s)
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int nt = 0; nt < Cfg::NT; ++nt)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            D[s][u][nt][e] = __builtin_fmaf((float)Cfg::C, S[s][u][nt][e], D[s][u][nt][e]);
-            carry_state<Cfg>(D, full, m != 0);
+            each<Cfg>(D, [&](float x, int s, int u, int e) { return __builtin_fmaf((float)Cfg::C, S[s][u][e], x); });
+            carry_state<Cfg>(D, sD.carry[Cfg::C], m != 0);
         }
-        carry_state<Cfg>(S, full, m != 0);
+        carry_state<Cfg>(S, sD.carry[Cfg::C], m != 0);
 #pragma unroll
         for (int tb = 0; tb < Cfg::C / 32; ++tb) {
-            bf16x8 z[Cfg::NT][Cfg::NP], zw[Cfg::NT][3];
+            bf16x8 z[Cfg::NP], zw[3], zd[3];
+            col_frag<Cfg, Cfg::LDV>(z, sZ, tb, state_col_addr(L), L);
+            weigh<Cfg>(zw, z, sW[0], tb, L);
+            if (DOT) weigh<Cfg>(zd, z, sW[DOT ? 1 : 0], tb, L);
 #pragma unroll
-            for (int nt = 0; nt < Cfg::NT; ++nt) {
-                col_frag<Cfg, Cfg::LDV>(z[nt], sZ, tb, state_col_addr<Cfg>(nt, L), L);
-                weigh<Cfg>(zw[nt], z[nt], sW[0], tb, L);
-            }
-            state_add<Cfg>(S, sY, zw, tb, L);
-            if (DOT) {
+            for (int s = 0; s < Cfg::KS; ++s)
 #pragma unroll
-                for (int nt = 0; nt < Cfg::NT; ++nt) weigh<Cfg>(zw[nt], z[nt], sW[DOT ? 1 : 0], tb, L);
-                state_add<Cfg>(D, sY, zw, tb, L);
-            }
+                for (int u = 0; u < 2; ++u) {
+                    bf16x8 y[Cfg::NP];
+                    col_frag<Cfg, Cfg::LDK>(y, sY, tb, state_row_addr(s, u, L), L);
+                    mma<Cfg::NP, 3>(S[s][u], y, zw);
+                    if (DOT) mma<Cfg::NP, 3>(D[s][u], y, zd);
+                }
         }
     }
+    L.again();
     const int64_t words = (int64_t)p.y.d * p.z.d, n = p.nseg - 1;
     const int64_t at = ((b * p.H + h) * n + seg) * words;
     store_state<Cfg>(S, p.states + at, p.z.d, 1, p.y.d, p.z.d, 1.0f, false, L);
@@ -212,86 +204,86 @@ __global__ __launch_bounds__(256) void ret_state_scan_kernel(RetStateScanArgs p)
 
 // ---------------------------------------------------------------------- walk
 template <class Cfg>
-__global__ __launch_bounds__(256, Cfg::NP == 1 ? 2 : 1) void ret_walk_kernel(RetWalkArgs p) {
+__global__ __launch_bounds__(Cfg::THREADS, Cfg::NP == 1 ? 4 : 2) void ret_walk_kernel(RetWalkArgs p) {
     __shared__ __attribute__((aligned(16))) uint16_t sX[Cfg::NP * Cfg::C * Cfg::LDK];
     __shared__ __attribute__((aligned(16))) uint16_t sY[Cfg::NP * Cfg::C * Cfg::LDK];
     __shared__ __attribute__((aligned(16))) uint16_t sZ[Cfg::NP * Cfg::C * Cfg::LDV];
     __shared__ u32x2 sP[Cfg::NTILE][Cfg::NP][64];
-    __shared__ float sPw[Cfg::C + 1];
+    __shared__ Decays<Cfg> sD;
     __shared__ __attribute__((aligned(16))) float sW[Cfg::C];
-    __shared__ uint32_t sBad[4];
-    const RetLane L;
+    __shared__ uint32_t sBad[Cfg::W];
+    RetLane L;
     const int64_t seg = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
     ret_header(p.hdr, p.sig);
     const double rate = fabs((double)p.alpha[h]);
-    if (L.tid <= Cfg::C) sPw[L.tid] = decay_pow(rate, L.tid);
-    const Carry full = carry_of(rate, Cfg::C);
-    const void* const x0 = role_head<Cfg::ES>(p.x, b, h, p.T);
-    const void* const y0 = role_head<Cfg::ES>(p.y, b, h, p.T);
-    const void* const z0 = role_head<Cfg::ES>(p.z, b, h, p.T);
-    const int64_t xrow = (int64_t)p.x.heads * p.x.d, yrow = (int64_t)p.y.heads * p.y.d;
-    const int64_t zrow = (int64_t)p.z.heads * p.z.d, orow = (int64_t)p.H * p.z.d;
+    sD.fill(rate, L.tid);
+    const Head hx = head_of<Cfg>(p.x, b, h, p.T), hy = head_of<Cfg>(p.y, b, h, p.T), hz = head_of<Cfg>(p.z, b, h, p.T);
     const uint8_t* const start = p.start + b * p.T;
     const int64_t words = (int64_t)p.x.d * p.z.d, bh = b * p.H + h;
     const int64_t seg0 = seg * p.chunks * Cfg::C;
     const int64_t left = (p.T - seg0 + Cfg::C - 1) / Cfg::C;
     const int nch = (int)(left < p.chunks ? left : p.chunks);
 
-    State<Cfg> S;
-    const float* const before = seg == 0 ? (p.seed ? p.seed + bh * words : nullptr)
-                                         : p.states + (bh * (p.nseg - 1) + seg - 1) * words;
-    load_state<Cfg>(S, before, p.sk, p.sv, p.x.d, p.z.d, L);
-
     RetTile<Cfg, Cfg::KD> tx, ty;
     RetTile<Cfg, Cfg::VD> tz;
+    uint32_t flag;
     auto fetch = [&](int ch) {
-        const int64_t w0 = seg0 + (int64_t)ch * Cfg::C;
-        const int64_t rest = ch < nch ? p.T - w0 : 0;
+        const bool have = ch < nch;
+        const int64_t w0 = have ? seg0 + (int64_t)ch * Cfg::C : 0;
+        const int64_t rest = have ? p.T - w0 : 0;
         const int n = (int)(rest < Cfg::C ? rest : Cfg::C);
-        const int64_t w = ch < nch ? w0 : 0;
-        tx.fetch(ret_rows<Cfg::ES>(x0, xrow, p.x.d, w, n, p.T, p.rev), L);
-        ty.fetch(ret_rows<Cfg::ES>(y0, yrow, p.y.d, w, n, p.T, p.rev), L);
-        tz.fetch(ret_rows<Cfg::ES>(z0, zrow, p.z.d, w, n, p.T, p.rev), L);
+        flag = ret_flag(start, w0, n, p.T, p.rev, L.lane);
+        tx.fetch(rows_of<Cfg>(hx, w0, n, p.T, p.rev), L);
+        ty.fetch(rows_of<Cfg>(hy, w0, n, p.T, p.rev), L);
+        tz.fetch(rows_of<Cfg>(hz, w0, n, p.T, p.rev), L);
     };
     fetch(0);
+    State<Cfg> S;
+    load_state<Cfg>(S, seg == 0 ? (p.seed ? p.seed + bh * words : nullptr) : p.states + (bh * (p.nseg - 1) + seg - 1) * words,
+                    p.sk, p.sv, p.x.d, p.z.d, L);
 #pragma unroll 1
     for (int ch = 0; ch < nch; ++ch) {
+        L.again();
         const int64_t w0 = seg0 + (int64_t)ch * Cfg::C;
         const int n = (int)(p.T - w0 < Cfg::C ? p.T - w0 : Cfg::C);
-        const uint64_t m = ret_begins(start, w0, n, p.T, p.rev, L.lane);
-        const uint64_t not_finite = __ballot(tx.bad() || ty.bad() || tz.bad());
-        __syncthreads();                                   // the last chunk's operands have been read
+        const uint64_t m = __ballot(flag != 0u);
+        const uint64_t not_finite = __ballot((tx.bad() | ty.bad() | tz.bad()) != 0u);
+        barrier_lds();                                     // the last chunk's operands have been read
         if (L.lane == 0) sBad[L.w] = not_finite != 0;
-        tx.template stage<Cfg::LDK>(sX, 0, n, L);
-        ty.template stage<Cfg::LDK>(sY, 0, n, L);
-        tz.template stage<Cfg::LDV>(sZ, 0, n, L);
+        tx.template stage<Cfg::LDK, false>(sX, 0, 0, L);
+        ty.template stage<Cfg::LDK, false>(sY, 0, 0, L);
+        tz.template stage<Cfg::LDV, false>(sZ, 0, 0, L);
         // weights of the rows into the state: no begin step after them
         if (L.tid < Cfg::C) {
             const int from = m ? last_begin(m) : 0;
-            sW[L.tid] = L.tid >= from && L.tid < n ? sPw[n - 1 - L.tid] * p.z_scale : 0.0f;
+            sW[L.tid] = L.tid >= from && L.tid < n ? sD.pw[L.tid < n ? n - 1 - L.tid : 0] * p.z_scale : 0.0f;
         }
-        __syncthreads();
-        const bool by_row = (sBad[0] | sBad[1] | sBad[2] | sBad[3]) != 0;
+        barrier_lds();
+        uint32_t any_bad = 0;
+#pragma unroll
+        for (int i = 0; i < Cfg::W; ++i) any_bad |= sBad[i];
+        const bool by_row = __builtin_amdgcn_readfirstlane((int)any_bad) != 0;
         int a = 0;
 #pragma unroll 1
         do {
+            L.again();
             const int to = by_row ? a + 1 : n;             // rows a .. to - 1
             if (by_row) {
-                __syncthreads();
-                tx.template stage<Cfg::LDK>(sX, a, to, L);
-                ty.template stage<Cfg::LDK>(sY, a, to, L);
-                tz.template stage<Cfg::LDV>(sZ, a, to, L);
+                barrier_lds();
+                tx.template stage<Cfg::LDK, true>(sX, a, to, L);
+                ty.template stage<Cfg::LDK, true>(sY, a, to, L);
+                tz.template stage<Cfg::LDV, true>(sZ, a, to, L);
                 if (L.tid < Cfg::C) sW[L.tid] = L.tid == a ? p.z_scale : 0.0f;
-                __syncthreads();
+                barrier_lds();
             }
             if (to == n) fetch(ch + 1);
             const uint64_t mw = m & (upto(to - 1) & ~((1ull << a) - 1ull));
             const int e = p.rev && w0 + a == 0 ? 0 : 1;
 
-            // ---- the pairs' products, a few tiles per wavefront
+            // ---- the pairs' products, a tile or two per wavefront
 #pragma unroll
-            for (int i = 0; i < (Cfg::NTILE + 3) / 4; ++i) {
-                const int idx = 4 * i + L.w;
+            for (int i = 0; i < (Cfg::NTILE + Cfg::W - 1) / Cfg::W; ++i) {
+                const int idx = Cfg::W * i + L.w;
                 if (idx >= Cfg::NTILE) break;
                 int jb, ib;
                 tile_of(idx, jb, ib);
@@ -302,7 +294,7 @@ __global__ __launch_bounds__(256, Cfg::NP == 1 ? 2 : 1) void ret_walk_kernel(Ret
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int j = 16 * jb + 4 * L.g + r;
-                    d[r] = j <= row && j >= first ? d[r] * (sPw[j <= row ? row - j : 0] * p.p_scale) : 0.0f;
+                    d[r] = j <= row && j >= first ? d[r] * (sD.pw[j <= row ? row - j : 0] * p.p_scale) : 0.0f;
                 }
                 uint32_t lo[Cfg::NP], hi[Cfg::NP];
                 planes2<Cfg::NP>(d[0], d[1], lo);
@@ -310,46 +302,38 @@ __global__ __launch_bounds__(256, Cfg::NP == 1 ? 2 : 1) void ret_walk_kernel(Ret
 #pragma unroll
                 for (int q = 0; q < Cfg::NP; ++q) sP[idx][q][L.lane] = u32x2{lo[q], hi[q]};
             }
-            __syncthreads();
+            barrier_lds();
 
             // ---- the rows against the state before the chunk
-            f32x4 acc[Cfg::NB][Cfg::NT];
+            f32x4 acc[Cfg::NB];
 #pragma unroll
-            for (int ib = 0; ib < Cfg::NB; ++ib)
+            for (int ib = 0; ib < Cfg::NB; ++ib) acc[ib] = zero4();
 #pragma unroll
-                for (int nt = 0; nt < Cfg::NT; ++nt) acc[ib][nt] = zero4();
-#pragma unroll
-            for (int s = 0; s < Cfg::KD / 32; ++s) {
-                bf16x8 st[Cfg::NT][Cfg::NP];
-#pragma unroll
-                for (int nt = 0; nt < Cfg::NT; ++nt) planes8<Cfg::NP>(S[s][0][nt], S[s][1][nt], st[nt]);
+            for (int s = 0; s < Cfg::KS; ++s) {
+                bf16x8 st[Cfg::NP];
+                planes8<Cfg::NP>(S[s][0], S[s][1], st);
 #pragma unroll
                 for (int ib = 0; ib < Cfg::NB; ++ib) {
                     bf16x8 x[Cfg::NP];
                     row_frag<Cfg, Cfg::LDK>(x, sX, 16 * ib, 32 * s, L);
-#pragma unroll
-                    for (int nt = 0; nt < Cfg::NT; ++nt) mma<Cfg::NP, Cfg::NP>(acc[ib][nt], st[nt], x);
+                    mma<Cfg::NP, Cfg::NP>(acc[ib], st, x);
                 }
             }
 #pragma unroll
             for (int ib = 0; ib < Cfg::NB; ++ib) {
                 const int row = 16 * ib + L.c;
                 const bool goes_on = (mw & upto(row)) == 0 && row >= a && row < to;
-                const float f = goes_on ? sPw[row - a + e] * p.inter_scale : 0.0f;
+                const float f = goes_on ? sD.pw[row - a + e] * p.inter_scale : 0.0f;
 #pragma unroll
-                for (int nt = 0; nt < Cfg::NT; ++nt)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[ib][nt][r] = goes_on ? acc[ib][nt][r] * f : 0.0f;
+                for (int r = 0; r < 4; ++r) acc[ib][r] = goes_on ? acc[ib][r] * f : 0.0f;
             }
 
             // ---- the rows against each other, and the state after the chunk
-            carry_state<Cfg>(S, to - a - 1 + e == Cfg::C ? full : carry_of(rate, (double)(to - a - 1 + e)), mw != 0);
+            carry_state<Cfg>(S, sD.carry[to - a - 1 + e], mw != 0);
 #pragma unroll
             for (int tb = 0; tb < Cfg::C / 32; ++tb) {
-                bf16x8 z[Cfg::NT][Cfg::NP], zw[Cfg::NT][3];
-#pragma unroll
-                for (int nt = 0; nt < Cfg::NT; ++nt)
-                    col_frag<Cfg, Cfg::LDV>(z[nt], sZ, tb, state_col_addr<Cfg>(nt, L), L);
+                bf16x8 z[Cfg::NP], zw[3];
+                col_frag<Cfg, Cfg::LDV>(z, sZ, tb, state_col_addr(L), L);
 #pragma unroll
                 for (int ib = 2 * tb; ib < Cfg::NB; ++ib) {
                     const int t0 = ib * (ib + 1) / 2 + 2 * tb;
@@ -360,44 +344,34 @@ __global__ __launch_bounds__(256, Cfg::NP == 1 ? 2 : 1) void ret_walk_kernel(Ret
                         const u32x2 hi = ib > 2 * tb ? sP[t0 + (ib > 2 * tb ? 1 : 0)][q][L.lane] : u32x2{0u, 0u};
                         pr[q] = __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
                     }
-#pragma unroll
-                    for (int nt = 0; nt < Cfg::NT; ++nt) mma<Cfg::NP, Cfg::NP>(acc[ib][nt], z[nt], pr);
+                    mma<Cfg::NP, Cfg::NP>(acc[ib], z, pr);
                 }
+                weigh<Cfg>(zw, z, sW, tb, L);
 #pragma unroll
-                for (int nt = 0; nt < Cfg::NT; ++nt) weigh<Cfg>(zw[nt], z[nt], sW, tb, L);
-                state_add<Cfg>(S, sY, zw, tb, L);
+                for (int s = 0; s < Cfg::KS; ++s)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        bf16x8 y[Cfg::NP];
+                        col_frag<Cfg, Cfg::LDK>(y, sY, tb, state_row_addr(s, u, L), L);
+                        mma<Cfg::NP, 3>(S[s][u], y, zw);
+                    }
             }
 
-            // ---- out: 4 NT consecutive columns of a row per lane
+            // ---- out: four consecutive columns of a row per lane
             {
                 const int os = Cfg::NP == 1 && !p.out_f32 ? 2 : 4;
-                const int64_t t = p.rev ? p.T - w0 - n : w0;
-                const RetRows o{make_rsrc((char*)p.out + (((b * p.T + t) * p.H + h) * p.z.d) * os,
-                                          ((int64_t)(n - 1) * orow + p.z.d) * os),
-                                (uint32_t)(orow * os), n, p.z.d, (bool)p.rev};
+                const int64_t orow = (int64_t)p.H * p.z.d * os;
+                const RetRows o = ret_rows((char*)p.out + (b * p.T * p.H + h) * p.z.d * os, orow, p.z.d, os, w0, n, p.T, p.rev);
 #pragma unroll
                 for (int ib = 0; ib < Cfg::NB; ++ib) {
                     const int row = 16 * ib + L.c;
-                    const int col = 16 * Cfg::NT * L.w + 4 * Cfg::NT * L.g;
-                    const bool in = row >= a && row < to;
-                    const uint32_t off = in ? o.offset(row, col, os) : kOob;
-                    if (os == 2) {
-                        uint32_t wd[2 * Cfg::NT];
-#pragma unroll
-                        for (int nt = 0; nt < Cfg::NT; ++nt) {
-                            wd[2 * nt] = f32x2_to_bf16x2(acc[ib][nt][0], acc[ib][nt][1]);
-                            wd[2 * nt + 1] = f32x2_to_bf16x2(acc[ib][nt][2], acc[ib][nt][3]);
-                        }
-                        if constexpr (Cfg::NT == 2)
-                            __builtin_amdgcn_raw_buffer_store_b128(u32x4{wd[0], wd[1], wd[2], wd[3]}, o.r, (int)off, 0, 0);
-                        else
-                            __builtin_amdgcn_raw_buffer_store_b64(u32x2{wd[0], wd[1]}, o.r, (int)off, 0, 0);
-                    } else {
-#pragma unroll
-                        for (int nt = 0; nt < Cfg::NT; ++nt)
-                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[ib][nt]), o.r,
-                                                                   (int)(off + 16u * nt), 0, 0);
-                    }
+                    const uint32_t off = row >= a && row < to ? o.offset(row, 16 * L.w + 4 * L.g, os) : kOob;
+                    if (os == 2)
+                        __builtin_amdgcn_raw_buffer_store_b64(
+                            u32x2{f32x2_to_bf16x2(acc[ib][0], acc[ib][1]), f32x2_to_bf16x2(acc[ib][2], acc[ib][3])}, o.r,
+                            (int)off, 0, 0);
+                    else
+                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[ib]), o.r, (int)off, 0, 0);
                 }
             }
             a = to;
@@ -407,7 +381,7 @@ __global__ __launch_bounds__(256, Cfg::NP == 1 ? 2 : 1) void ret_walk_kernel(Ret
         // backwards: the gradient of the state before the tape, one step further
         // back, and none if step 0 begins an episode
         const bool drop = p.rev && start[0] != 0;
-        store_state<Cfg>(S, p.fin + bh * words, p.sk, p.sv, p.x.d, p.z.d, p.rev ? decay_pow(rate, 1.0) : 1.0f, drop, L);
+        store_state<Cfg>(S, p.fin + bh * words, p.sk, p.sv, p.x.d, p.z.d, p.rev ? sD.pw[1] : 1.0f, drop, L);
     }
 }
 
@@ -420,79 +394,96 @@ __global__ __launch_bounds__(256, Cfg::NP == 1 ? 2 : 1) void ret_walk_kernel(Ret
 // The two outer products arrive in the state's own layout, so they meet S and D
 // as floats in registers: nothing here is rounded to bf16.
 template <class Cfg>
-__global__ __launch_bounds__(256, 1) void ret_sens_kernel(RetSensArgs p) {
+__global__ __launch_bounds__(Cfg::THREADS, 2) void ret_sens_kernel(RetSensArgs p) {
     __shared__ __attribute__((aligned(16))) uint16_t sQ[Cfg::NP * Cfg::C * Cfg::LDK];
     __shared__ __attribute__((aligned(16))) uint16_t sK[Cfg::NP * Cfg::C * Cfg::LDK];
     __shared__ __attribute__((aligned(16))) uint16_t sV[Cfg::NP * Cfg::C * Cfg::LDV];
     __shared__ __attribute__((aligned(16))) uint16_t sG[Cfg::NP * Cfg::C * Cfg::LDV];
-    __shared__ float sPw[Cfg::C + 1];
+    __shared__ Decays<Cfg> sD;
     __shared__ __attribute__((aligned(16))) float sW[4][Cfg::C];
-    __shared__ uint32_t sBad[4];
-    __shared__ double sSum[4];
-    const RetLane L;
+    __shared__ uint32_t sBad[Cfg::W];
+    __shared__ double sSum[Cfg::W];
+    RetLane L;
     const int64_t seg = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
     const double rate = fabs((double)p.alpha[h]);
-    if (L.tid <= Cfg::C) sPw[L.tid] = decay_pow(rate, L.tid);
-    const Carry full = carry_of(rate, Cfg::C);
+    sD.fill(rate, L.tid);
     const int kd = p.q.d, vd = p.v.d;
-    const void* const q0 = role_head<Cfg::ES>(p.q, b, h, p.T);
-    const void* const k0 = role_head<Cfg::ES>(p.k, b, h, p.T);
-    const void* const v0 = role_head<Cfg::ES>(p.v, b, h, p.T);
-    const void* const g0 = role_head<Cfg::ES>(p.g, b, h, p.T);
-    const int64_t qrow = (int64_t)p.q.heads * kd, krow = (int64_t)p.k.heads * kd;
-    const int64_t vrow = (int64_t)p.v.heads * vd, grow = (int64_t)p.g.heads * vd;
+    const Head hq = head_of<Cfg>(p.q, b, h, p.T), hk = head_of<Cfg>(p.k, b, h, p.T), hv = head_of<Cfg>(p.v, b, h, p.T),
+               hg = head_of<Cfg>(p.g, b, h, p.T);
     const uint8_t* const start = p.start + b * p.T;
     const int64_t words = (int64_t)kd * vd, bh = b * p.H + h;
     const int64_t seg0 = seg * p.chunks * Cfg::C;
     const int64_t left = (p.T - seg0 + Cfg::C - 1) / Cfg::C;
     const int nch = (int)(left < p.chunks ? left : p.chunks);
 
+    RetTile<Cfg, Cfg::KD> tq, tk;
+    RetTile<Cfg, Cfg::VD> tv, tg;
+    uint32_t flag;
+    auto fetch = [&](int ch) {
+        const bool have = ch < nch;
+        const int64_t w0 = have ? seg0 + (int64_t)ch * Cfg::C : 0;
+        const int64_t rest = have ? p.T - w0 : 0;
+        const int n = (int)(rest < Cfg::C ? rest : Cfg::C);
+        flag = ret_flag(start, w0, n, p.T, false, L.lane);
+        tq.fetch(rows_of<Cfg>(hq, w0, n, p.T, false), L);
+        tk.fetch(rows_of<Cfg>(hk, w0, n, p.T, false), L);
+        tv.fetch(rows_of<Cfg>(hv, w0, n, p.T, false), L);
+        tg.fetch(rows_of<Cfg>(hg, w0, n, p.T, false), L);
+    };
+    fetch(0);
     State<Cfg> S, D;
     const int64_t at = (bh * (p.nseg - 1) + seg - 1) * words;
     load_state<Cfg>(S, seg == 0 ? (p.seed ? p.seed + bh * words : nullptr) : p.states + at, vd, 1, kd, vd, L);
     load_state<Cfg>(D, seg == 0 ? nullptr : p.dstates + at, vd, 1, kd, vd, L);
     double sum = 0.0;
-    RetTile<Cfg, Cfg::KD> tq, tk;
-    RetTile<Cfg, Cfg::VD> tv, tg;
 #pragma unroll 1
     for (int ch = 0; ch < nch; ++ch) {
+        L.again();
         const int64_t w0 = seg0 + (int64_t)ch * Cfg::C;
         const int n = (int)(p.T - w0 < Cfg::C ? p.T - w0 : Cfg::C);
-        tq.fetch(ret_rows<Cfg::ES>(q0, qrow, kd, w0, n, p.T, false), L);
-        tk.fetch(ret_rows<Cfg::ES>(k0, krow, kd, w0, n, p.T, false), L);
-        tv.fetch(ret_rows<Cfg::ES>(v0, vrow, vd, w0, n, p.T, false), L);
-        tg.fetch(ret_rows<Cfg::ES>(g0, grow, vd, w0, n, p.T, false), L);
-        const uint64_t m = ret_begins(start, w0, n, p.T, false, L.lane);
-        const uint64_t not_finite = __ballot(tq.bad() || tk.bad() || tv.bad() || tg.bad());
+        const uint64_t m = __ballot(flag != 0u);
+        const uint64_t not_finite = __ballot((tq.bad() | tk.bad() | tv.bad() | tg.bad()) != 0u);
         if (L.lane == 0) sBad[L.w] = not_finite != 0;
-        __syncthreads();
-        const bool by_row = (sBad[0] | sBad[1] | sBad[2] | sBad[3]) != 0;
+        barrier_lds();
+        uint32_t any_bad = 0;
+#pragma unroll
+        for (int i = 0; i < Cfg::W; ++i) any_bad |= sBad[i];
+        const bool by_row = __builtin_amdgcn_readfirstlane((int)any_bad) != 0;
         int a = 0;
 #pragma unroll 1
         do {
+            L.again();
             const int to = by_row ? a + 1 : n;
             const uint64_t mw = m & (upto(to - 1) & ~((1ull << a) - 1ull));
-            __syncthreads();                               // the last operands have been read
-            tq.template stage<Cfg::LDK>(sQ, a, to, L);
-            tk.template stage<Cfg::LDK>(sK, a, to, L);
-            tv.template stage<Cfg::LDV>(sV, a, to, L);
-            tg.template stage<Cfg::LDV>(sG, a, to, L);
+            barrier_lds();                                 // the last operands have been read
+            if (by_row) {
+                tq.template stage<Cfg::LDK, true>(sQ, a, to, L);
+                tk.template stage<Cfg::LDK, true>(sK, a, to, L);
+                tv.template stage<Cfg::LDV, true>(sV, a, to, L);
+                tg.template stage<Cfg::LDV, true>(sG, a, to, L);
+            } else {
+                tq.template stage<Cfg::LDK, false>(sQ, 0, 0, L);
+                tk.template stage<Cfg::LDK, false>(sK, 0, 0, L);
+                tv.template stage<Cfg::LDV, false>(sV, 0, 0, L);
+                tg.template stage<Cfg::LDV, false>(sG, 0, 0, L);
+            }
             if (L.tid < Cfg::C) {
                 const int i = L.tid;
                 const bool in = i >= a && i < to;
                 const int from = mw ? last_begin(mw) : a;
-                const float w = in && i >= from ? sPw[to - 1 - i] : 0.0f;
+                const float w = in && i >= from ? sD.pw[in ? to - 1 - i : 0] : 0.0f;
                 sW[0][i] = w;
                 sW[1][i] = w * (float)(to - 1 - i);
-                const float f = in && (mw & upto(i)) == 0 ? sPw[i - a + 1] * p.scale : 0.0f;
+                const float f = in && (mw & upto(i)) == 0 ? sD.pw[in ? i - a + 1 : 0] * p.scale : 0.0f;
                 sW[2][i] = f;
                 sW[3][i] = f * (float)(i - a + 1);
             }
-            __syncthreads();
+            if (to == n) fetch(ch + 1);
+            barrier_lds();
             float part = 0.0f;
 #pragma unroll
-            for (int i = 0; i < (Cfg::NTILE + 3) / 4; ++i) {
-                const int idx = 4 * i + L.w;
+            for (int i = 0; i < (Cfg::NTILE + Cfg::W - 1) / Cfg::W; ++i) {
+                const int idx = Cfg::W * i + L.w;
                 if (idx >= Cfg::NTILE) break;
                 int jb, ib;
                 tile_of(idx, jb, ib);
@@ -505,96 +496,82 @@ __global__ __launch_bounds__(256, 1) void ret_sens_kernel(RetSensArgs p) {
                 for (int r = 0; r < 4; ++r) {
                     const int j = 16 * jb + 4 * L.g + r;
                     const bool in = j < row && j >= first;
-                    const float w = sPw[in ? row - j : 0] * (float)(row - j) * p.scale;
+                    const float w = sD.pw[in ? row - j : 0] * (float)(row - j) * p.scale;
                     part += in ? x[r] * y[r] * w : 0.0f;
                 }
             }
             // rows against (S, D): skipped where the first row begins an episode,
             // so that values of S that are not finite stay out
             if (!(mw >> a & 1ull)) {
-                // two running sums per wavefront column and state row block, in
-                // float within the chunk
-#pragma unroll 1
-                for (int s = 0; s < Cfg::KD / 32; ++s) {
+                bf16x8 g1[Cfg::C / 32][3], g2[Cfg::C / 32][3];
+#pragma unroll
+                for (int tb = 0; tb < Cfg::C / 32; ++tb) {
+                    bf16x8 g[Cfg::NP];
+                    col_frag<Cfg, Cfg::LDV>(g, sG, tb, state_col_addr(L), L);
+                    weigh<Cfg>(g1[tb], g, sW[2], tb, L);
+                    weigh<Cfg>(g2[tb], g, sW[3], tb, L);
+                }
+#pragma unroll
+                for (int s = 0; s < Cfg::KS; ++s)
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
-                        f32x4 o1[Cfg::NT], o2[Cfg::NT];
-#pragma unroll
-                        for (int nt = 0; nt < Cfg::NT; ++nt) o1[nt] = o2[nt] = zero4();
+                        f32x4 o1 = zero4(), o2 = zero4();
 #pragma unroll
                         for (int tb = 0; tb < Cfg::C / 32; ++tb) {
                             bf16x8 q[Cfg::NP];
-                            col_frag<Cfg, Cfg::LDK>(q, sQ, tb, state_row_addr<Cfg>(s, u, L), L);
-#pragma unroll
-                            for (int nt = 0; nt < Cfg::NT; ++nt) {
-                                bf16x8 g[Cfg::NP], gw[3];
-                                col_frag<Cfg, Cfg::LDV>(g, sG, tb, state_col_addr<Cfg>(nt, L), L);
-                                weigh<Cfg>(gw, g, sW[2], tb, L);
-                                mma<Cfg::NP, 3>(o1[nt], q, gw);
-                                weigh<Cfg>(gw, g, sW[3], tb, L);
-                                mma<Cfg::NP, 3>(o2[nt], q, gw);
-                            }
+                            col_frag<Cfg, Cfg::LDK>(q, sQ, tb, state_row_addr(s, u, L), L);
+                            mma<Cfg::NP, 3>(o1, q, g1[tb]);
+                            mma<Cfg::NP, 3>(o2, q, g2[tb]);
                         }
 #pragma unroll
-                        for (int ss = 0; ss < Cfg::KD / 32; ++ss)
-                            if (ss == s)
-#pragma unroll
-                                for (int nt = 0; nt < Cfg::NT; ++nt)
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e)
-                                        part = __builtin_fmaf(S[ss][u][nt][e], o2[nt][e],
-                                                              __builtin_fmaf(D[ss][u][nt][e], o1[nt][e], part));
+                        for (int e = 0; e < 4; ++e)
+                            part = __builtin_fmaf(S[s][u][e], o2[e], __builtin_fmaf(D[s][u][e], o1[e], part));
                     }
-                }
             }
             sum += (double)part;
             // (S, D) after these rows
             const int len = to - a;
-            const Carry cy = len == Cfg::C ? full : carry_of(rate, (double)len);
-#pragma unroll
-            for (int s = 0; s < Cfg::KD / 32; ++s)
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int nt = 0; nt < Cfg::NT; ++nt)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            D[s][u][nt][e] = __builtin_fmaf((float)len, S[s][u][nt][e], D[s][u][nt][e]);
-            carry_state<Cfg>(D, cy, mw != 0);
-            carry_state<Cfg>(S, cy, mw != 0);
+            each<Cfg>(D, [&](float x, int s, int u, int e) { return __builtin_fmaf((float)len, S[s][u][e], x); });
+            carry_state<Cfg>(D, sD.carry[len], mw != 0);
+            carry_state<Cfg>(S, sD.carry[len], mw != 0);
 #pragma unroll
             for (int tb = 0; tb < Cfg::C / 32; ++tb) {
-                bf16x8 z[Cfg::NT][Cfg::NP], zw[Cfg::NT][3];
+                bf16x8 z[Cfg::NP], zw[3], zd[3];
+                col_frag<Cfg, Cfg::LDV>(z, sV, tb, state_col_addr(L), L);
+                weigh<Cfg>(zw, z, sW[0], tb, L);
+                weigh<Cfg>(zd, z, sW[1], tb, L);
 #pragma unroll
-                for (int nt = 0; nt < Cfg::NT; ++nt) {
-                    col_frag<Cfg, Cfg::LDV>(z[nt], sV, tb, state_col_addr<Cfg>(nt, L), L);
-                    weigh<Cfg>(zw[nt], z[nt], sW[0], tb, L);
-                }
-                state_add<Cfg>(S, sK, zw, tb, L);
+                for (int s = 0; s < Cfg::KS; ++s)
 #pragma unroll
-                for (int nt = 0; nt < Cfg::NT; ++nt) weigh<Cfg>(zw[nt], z[nt], sW[1], tb, L);
-                state_add<Cfg>(D, sK, zw, tb, L);
+                    for (int u = 0; u < 2; ++u) {
+                        bf16x8 y[Cfg::NP];
+                        col_frag<Cfg, Cfg::LDK>(y, sK, tb, state_row_addr(s, u, L), L);
+                        mma<Cfg::NP, 3>(S[s][u], y, zw);
+                        mma<Cfg::NP, 3>(D[s][u], y, zd);
+                    }
             }
             a = to;
         } while (a < n);
     }
+    L.again();
     if (p.grad_state && seg == p.nseg - 1) {
         State<Cfg> G;
         load_state<Cfg>(G, p.grad_state + bh * words, vd, 1, kd, vd, L);
-#pragma unroll
-        for (int s = 0; s < Cfg::KD / 32; ++s)
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int nt = 0; nt < Cfg::NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) sum += (double)D[s][u][nt][e] * (double)G[s][u][nt][e];
+        each<Cfg>(G, [&](float x, int s, int u, int e) {
+            sum += (double)D[s][u][e] * (double)x;
+            return x;
+        });
     }
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x, 64);
     if (L.lane == 0) sSum[L.w] = sum;
     __syncthreads();
-    if (L.tid == 0) p.part[bh * p.nseg + seg] = (sSum[0] + sSum[1]) + (sSum[2] + sSum[3]);
+    if (L.tid == 0) {
+        double s = 0.0;
+#pragma unroll
+        for (int i = 0; i < Cfg::W; ++i) s += sSum[i];
+        p.part[bh * p.nseg + seg] = s;
+    }
 }
 
 __global__ __launch_bounds__(256) void ret_alpha_kernel(const double* part, const float* alpha, float* out, int64_t B,
@@ -634,11 +611,11 @@ namespace {
 template <int NP, class F>
 void with_tiles(int kd, int vd, F&& f) {
     if (kd <= 64) {
-        if (vd <= 64) f(RetCfg<NP, 64, 1>{});
-        else f(RetCfg<NP, 64, 2>{});
+        if (vd <= 64) f(RetCfg<NP, 64, 64>{});
+        else f(RetCfg<NP, 64, 128>{});
     } else {
-        if (vd <= 64) f(RetCfg<NP, 128, 1>{});
-        else f(RetCfg<NP, 128, 2>{});
+        if (vd <= 64) f(RetCfg<NP, 128, 64>{});
+        else f(RetCfg<NP, 128, 128>{});
     }
 }
 template <class F>
@@ -649,17 +626,19 @@ void with_cfg(int planes, int kd, int vd, F&& f) {
 }  // namespace
 
 hipError_t ret_walk_launch(int planes, const RetWalkArgs& a, int64_t B, hipStream_t s) {
-    const dim3 grid((unsigned)a.nseg, (unsigned)a.H, (unsigned)B), block(256);
+    const dim3 grid((unsigned)a.nseg, (unsigned)a.H, (unsigned)B);
     with_cfg(planes, a.x.d, a.z.d, [&](auto cfg) {
-        hipLaunchKernelGGL((ret_walk_kernel<decltype(cfg)>), grid, block, 0, s, a);
+        using Cfg = decltype(cfg);
+        hipLaunchKernelGGL((ret_walk_kernel<Cfg>), grid, dim3(Cfg::THREADS), 0, s, a);
     });
     return hipGetLastError();
 }
 
 hipError_t ret_summary_launch(int planes, const RetSummaryArgs& a, int64_t B, hipStream_t s) {
-    const dim3 grid((unsigned)(a.nseg - 1), (unsigned)a.H, (unsigned)B), block(256);
+    const dim3 grid((unsigned)(a.nseg - 1), (unsigned)a.H, (unsigned)B);
     with_cfg(planes, a.y.d, a.z.d, [&](auto cfg) {
         using Cfg = decltype(cfg);
+        const dim3 block(Cfg::THREADS);
         if (a.dstates) hipLaunchKernelGGL((ret_summary_kernel<Cfg, true>), grid, block, 0, s, a);
         else hipLaunchKernelGGL((ret_summary_kernel<Cfg, false>), grid, block, 0, s, a);
     });
@@ -674,9 +653,10 @@ hipError_t ret_state_scan_launch(const RetStateScanArgs& a, int64_t B, hipStream
 }
 
 hipError_t ret_sens_launch(int planes, const RetSensArgs& a, int64_t B, hipStream_t s) {
-    const dim3 grid((unsigned)a.nseg, (unsigned)a.H, (unsigned)B), block(256);
+    const dim3 grid((unsigned)a.nseg, (unsigned)a.H, (unsigned)B);
     with_cfg(planes, a.q.d, a.v.d, [&](auto cfg) {
-        hipLaunchKernelGGL((ret_sens_kernel<decltype(cfg)>), grid, block, 0, s, a);
+        using Cfg = decltype(cfg);
+        hipLaunchKernelGGL((ret_sens_kernel<Cfg>), grid, dim3(Cfg::THREADS), 0, s, a);
     });
     return hipGetLastError();
 }

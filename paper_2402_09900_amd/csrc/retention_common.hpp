@@ -10,8 +10,8 @@
 //       dv  = W(k, q, dout),  dk = W(v, dout, q)  backwards in time,
 // where a step "begins" backwards when the step after it begins an episode.
 //
-// A workgroup of four wavefronts walks a run of chunks of C rows of one head with
-// the state (KD x 64 NT) in registers, a quarter of its columns per wavefront.
+// A workgroup of VD / 16 wavefronts walks a run of chunks of C rows of one head
+// with the state (KD x VD) in registers, 16 of its columns per wavefront.
 //
 // Every product runs on v_mfma_f32_16x16x32_bf16.  bf16 inputs go in as they
 // are.  A float goes in as three bf16 planes, x = h + m + l with h and m its
@@ -31,9 +31,8 @@
 //   * state rows kd as k: slot (g, e) is kd = 32 s + 8 g + e, as 16 bytes of a row
 //     of x are.  The state tile (s, u) holds kd = 32 s + 8 (i / 4) + 4 u + i % 4 in
 //     its row i, so registers of tiles (s, 0) and (s, 1) are those eight slots;
-//   * state columns: tile nt holds column 4 NT (c / 4) + 4 nt + c % 4 of the
-//     wavefront's 16 NT, and a row of the result has 4 NT consecutive columns in
-//     each lane: one store of 16 bytes or more (bf16, NT = 1: 8).
+//   * a wavefront has 16 of the state's columns, and a row of the result has four
+//     consecutive ones in each lane.
 #pragma once
 
 #include "scan_common.hpp"
@@ -48,24 +47,32 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // NP planes per input element: 1 = bf16, 3 = float.  Chunks of float are half as
 // long: the planes of three 64-row chunks of 128 columns do not fit in LDS.
-template <int NP_, int KD_, int NT_>
+template <int NP_, int KD_, int VD_>
 struct RetCfg {
-    static constexpr int NP = NP_, KD = KD_, NT = NT_;
+    static constexpr int NP = NP_, KD = KD_, VD = VD_;
     static constexpr int C = ret_chunk(NP);
-    static constexpr int VD = 64 * NT;
+    static constexpr int W = VD / 16, THREADS = 64 * W;
     static constexpr int ES = NP == 1 ? 2 : 4;        // bytes of an element in memory
     static constexpr int EPU = 16 / ES;               // elements of a 16-byte unit
     static constexpr int LDK = KD + 8, LDV = VD + 8;  // LDS row strides in elements
     static constexpr int NB = C / 16;                 // 16-row blocks
     static constexpr int NTILE = NB * (NB + 1) / 2;   // tiles of P on and below the diagonal
+    static constexpr int KS = KD / 32;                // steps of a product over kd
 };
 
 struct RetLane {
     int tid, lane, w, g, c;
     __device__ RetLane() {
         tid = threadIdx.x;
-        lane = tid & 63;
         w = __builtin_amdgcn_readfirstlane(tid >> 6);
+        again();
+    }
+    // The same again, opaque to the compiler: what it derives from these is
+    // recomputed in each chunk instead of being kept over the loop (a hundred
+    // addresses and masks, which took the registers that the state needs).
+    __device__ __forceinline__ void again() {
+        asm volatile("" : "+v"(tid));
+        lane = tid & 63;
         g = lane >> 4;
         c = lane & 15;
     }
@@ -132,9 +139,11 @@ __device__ __forceinline__ void mma(f32x4& acc, const bf16x8 (&a)[NA], const bf1
 __device__ __forceinline__ f32x4 zero4() { return f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }
 
 // --------------------------------------------------------- chunks in memory
-// n rows of one head of a [T][heads][d] tensor, from the row at the lowest
-// address; walking backwards row i is the (n - 1 - i)-th of them.  Rows at or
-// past n and columns at or past d read as zeros and drop their stores.
+// n rows of one head of a [T][heads][d] tensor as a buffer, from the row at the
+// lowest address on; walking backwards row i is the (n - 1 - i)-th of them.  Rows
+// at or past n lie outside the buffer (backwards: below offset 0, which wraps
+// past its end), columns at or past d are sent there: they read as zeros and drop
+// their stores.
 struct RetRows {
     Rsrc r;
     uint32_t row_bytes;
@@ -142,52 +151,56 @@ struct RetRows {
     bool rev;
     __device__ __forceinline__ uint32_t offset(int row, int col, int es) const {
         const uint32_t at = (uint32_t)(rev ? n - 1 - row : row) * row_bytes + (uint32_t)(col * es);
-        return row < n && col < d ? at : kOob;
+        return col < d ? at : kOob;
     }
 };
-template <int ES>
-__device__ __forceinline__ RetRows ret_rows(const void* head0, int64_t row, int d, int64_t w0, int n, int64_t T,
-                                            bool rev) {
+__device__ __forceinline__ RetRows ret_rows(const void* head0, int64_t row_bytes, int d, int es, int64_t w0, int n,
+                                            int64_t T, bool rev) {
     const int64_t t = rev ? T - w0 - n : w0;
-    return RetRows{make_rsrc((const char*)head0 + t * row * ES, n > 0 ? ((int64_t)(n - 1) * row + d) * ES : 0),
-                   (uint32_t)(row * ES), n, d, rev};
+    return RetRows{make_rsrc((const char*)head0 + t * row_bytes, n > 0 ? (n - 1) * row_bytes + d * es : 0),
+                   (uint32_t)row_bytes, n, d, rev};
 }
 
-// A chunk's tile of D columns held by the workgroup, 16 bytes a unit
+// A chunk's tile of D columns held by the workgroup, 16 bytes a unit: thread
+// `tid` has the same columns of rows tid / UPR + i RS
 template <class Cfg, int D>
 struct RetTile {
-    static constexpr int UPR = D / Cfg::EPU, UN = Cfg::C * UPR / 256;
-    static_assert(UN >= 1, "every thread holds a unit");
+    static constexpr int UPR = D / Cfg::EPU, RS = Cfg::THREADS / UPR, UN = Cfg::C / RS;
+    static_assert(UN >= 1 && UN * RS == Cfg::C, "every thread holds a unit");
     u32x4 u[UN];
 
     __device__ __forceinline__ void fetch(const RetRows& x, const RetLane& L) {
+        const int col = L.tid % UPR * Cfg::EPU;
+        uint32_t off = x.offset(L.tid / UPR, col, Cfg::ES);
+        const uint32_t step = col < x.d ? (uint32_t)RS * x.row_bytes : 0u;
 #pragma unroll
         for (int i = 0; i < UN; ++i) {
-            const int at = i * 256 + L.tid, row = at / UPR, col = at % UPR * Cfg::EPU;
-            u[i] = __builtin_amdgcn_raw_buffer_load_b128(x.r, (int)x.offset(row, col, Cfg::ES), 0, 0);
+            u[i] = __builtin_amdgcn_raw_buffer_load_b128(x.r, (int)off, 0, 0);
+            off = x.rev ? off - step : off + step;
         }
     }
-    // whether some element is not finite
-    __device__ __forceinline__ bool bad() const {
+    // nonzero if some element is not finite
+    __device__ __forceinline__ uint32_t bad() const {
         constexpr uint32_t kExp = Cfg::NP == 1 ? 0x7F807F80u : 0x7F800000u, kOne = Cfg::NP == 1 ? 0x00800080u : 0x00800000u;
         uint32_t any = 0;
 #pragma unroll
         for (int i = 0; i < UN; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) any |= (u[i][e] & kExp) + kOne;
-        return (any & (Cfg::NP == 1 ? 0x80008000u : 0x80000000u)) != 0u;
+        return any & (Cfg::NP == 1 ? 0x80008000u : 0x80000000u);
     }
-    // rows a .. b - 1 into an LDS tile of NP planes, the others as zeros
-    template <int LD>
+    // into an LDS tile of NP planes; WINDOW: rows a .. b - 1, the others as zeros
+    template <int LD, bool WINDOW>
     __device__ __forceinline__ void stage(uint16_t* s, int a, int b, const RetLane& L) const {
+        uint16_t* const p0 = s + L.tid / UPR * LD + L.tid % UPR * Cfg::EPU;
 #pragma unroll
         for (int i = 0; i < UN; ++i) {
-            const int at = i * 256 + L.tid, row = at / UPR, col = at % UPR * Cfg::EPU;
-            const bool in = row >= a && row < b;
+            const int row = L.tid / UPR + i * RS;
+            const bool in = !WINDOW || (row >= a && row < b);
             u32x4 x;
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = in ? u[i][e] : 0u;
-            uint16_t* const p = s + row * LD + col;
+            uint16_t* const p = p0 + i * RS * LD;
             if constexpr (Cfg::NP == 1) {
                 *(u32x4*)p = x;
             } else {
@@ -224,55 +237,52 @@ __device__ __forceinline__ void col_frag(bf16x8 (&f)[Cfg::NP], const uint16_t* s
 }
 
 // ---------------------------------------------------------------- the state
-// S[s][u][nt], rows and columns as above; column of this lane (and of this
-// lane's address in col_frag)
+// S[s][u], rows as above.  The column and the rows of this lane, and those of its
+// address in col_frag (four columns from there)
 template <class Cfg>
-__device__ __forceinline__ int state_col(int nt, const RetLane& L) {
-    return 16 * Cfg::NT * L.w + 4 * Cfg::NT * (L.c >> 2) + 4 * nt + (L.c & 3);
-}
-template <class Cfg>
-__device__ __forceinline__ int state_col_addr(int nt, const RetLane& L) {
-    return 16 * Cfg::NT * L.w + 4 * Cfg::NT * (L.c & 3) + 4 * nt;
-}
-template <class Cfg>
-__device__ __forceinline__ int state_row_addr(int s, int u, const RetLane& L) { return 32 * s + 8 * (L.c & 3) + 4 * u; }
-__device__ __forceinline__ int state_row(int s, int u, int r, const RetLane& L) { return 32 * s + 8 * L.g + 4 * u + r; }
+using State = f32x4[Cfg::KS][2];
 
-// An array of dk x dv floats with strides sk, sv: zeros where there is none
-template <class Cfg>
-__device__ __forceinline__ void load_state(f32x4 (&S)[Cfg::KD / 32][2][Cfg::NT], const float* p, int sk, int sv, int kd,
-                                           int vd, const RetLane& L) {
-    const Rsrc r = make_rsrc(p, p ? (int64_t)kd * vd * 4 : 0);
+__device__ __forceinline__ int state_col(const RetLane& L) { return 16 * L.w + L.c; }
+__device__ __forceinline__ int state_col_addr(const RetLane& L) { return 16 * L.w + 4 * (L.c & 3); }
+__device__ __forceinline__ int state_row(int s, int u, int r, const RetLane& L) { return 32 * s + 8 * L.g + 4 * u + r; }
+__device__ __forceinline__ int state_row_addr(int s, int u, const RetLane& L) { return 32 * s + 8 * (L.c & 3) + 4 * u; }
+
+template <class Cfg, class F>
+__device__ __forceinline__ void each(State<Cfg>& S, F&& f) {
 #pragma unroll
-    for (int s = 0; s < Cfg::KD / 32; ++s)
+    for (int s = 0; s < Cfg::KS; ++s)
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int nt = 0; nt < Cfg::NT; ++nt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int k = state_row(s, u, e, L), v = state_col<Cfg>(nt, L);
-                    const uint32_t off = k < kd && v < vd ? (uint32_t)(k * sk + v * sv) * 4u : kOob;
-                    S[s][u][nt][e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (int)off, 0, 0));
-                }
+            for (int e = 0; e < 4; ++e) S[s][u][e] = f(S[s][u][e], s, u, e);
 }
 template <class Cfg>
-__device__ __forceinline__ void store_state(const f32x4 (&S)[Cfg::KD / 32][2][Cfg::NT], float* p, int sk, int sv, int kd,
-                                            int vd, float mul, bool drop, const RetLane& L) {
+__device__ __forceinline__ void zero_state(State<Cfg>& S) {
+    each<Cfg>(S, [](float, int, int, int) { return 0.0f; });
+}
+// An array of kd x vd floats with strides sk, sv: zeros where there is none
+template <class Cfg>
+__device__ __forceinline__ void load_state(State<Cfg>& S, const float* p, int sk, int sv, int kd, int vd,
+                                           const RetLane& L) {
+    const Rsrc r = make_rsrc(p, p ? (int64_t)kd * vd * 4 : 0);
+    const int v = state_col(L);
+    each<Cfg>(S, [&](float, int s, int u, int e) {
+        const int k = state_row(s, u, e, L);
+        const uint32_t off = k < kd && v < vd ? (uint32_t)(k * sk + v * sv) * 4u : kOob;
+        return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (int)off, 0, 0));
+    });
+}
+template <class Cfg>
+__device__ __forceinline__ void store_state(State<Cfg>& S, float* p, int sk, int sv, int kd, int vd, float mul, bool drop,
+                                            const RetLane& L) {
     const Rsrc r = make_rsrc(p, (int64_t)kd * vd * 4);
-#pragma unroll
-    for (int s = 0; s < Cfg::KD / 32; ++s)
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int nt = 0; nt < Cfg::NT; ++nt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int k = state_row(s, u, e, L), v = state_col<Cfg>(nt, L);
-                    const uint32_t off = k < kd && v < vd ? (uint32_t)(k * sk + v * sv) * 4u : kOob;
-                    const float x = drop ? 0.0f : S[s][u][nt][e] * mul;
-                    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), r, (int)off, 0, 0);
-                }
+    const int v = state_col(L);
+    each<Cfg>(S, [&](float x, int s, int u, int e) {
+        const int k = state_row(s, u, e, L);
+        const uint32_t off = k < kd && v < vd ? (uint32_t)(k * sk + v * sv) * 4u : kOob;
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(drop ? 0.0f : x * mul), r, (int)off, 0, 0);
+        return x;
+    });
 }
 
 // ------------------------------------------------------------------- decays
@@ -280,24 +290,32 @@ __device__ __forceinline__ void store_state(const f32x4 (&S)[Cfg::KD / 32][2][Cf
 // steps, where the rounding of a 32-bit gamma^C would show.
 __device__ __forceinline__ float decay_pow(double rate, double n) { return n == 0.0 ? 1.0f : (float)exp(-rate * n); }
 // x -> gamma^n x without rounding gamma^n near 1: x + (gamma^n - 1) x there
+// m = gamma^n - 1 and keep = 1 there, m = gamma^n and keep = 0 elsewhere
 struct Carry {
-    float m;
-    bool near1;
-    __device__ __forceinline__ float operator()(float x) const { return near1 ? __builtin_fmaf(x, m, x) : x * m; }
+    float m, keep;
+    __device__ __forceinline__ float operator()(float x) const { return __builtin_fmaf(x, m, keep != 0.0f ? x : 0.0f); }
 };
 __device__ __forceinline__ Carry carry_of(double rate, double n) {
-    if (n == 0.0) return Carry{0.0f, true};
+    if (n == 0.0) return Carry{0.0f, 1.0f};
     const double p = exp(-rate * n);
-    return p > 0.5 ? Carry{(float)expm1(-rate * n), true} : Carry{(float)p, false};
+    return p > 0.5 ? Carry{(float)expm1(-rate * n), 1.0f} : Carry{(float)p, 0.0f};
+}
+template <class Cfg>
+__device__ __forceinline__ void carry_state(State<Cfg>& S, Carry cy, bool drop) {
+    if (drop) zero_state<Cfg>(S);
+    else if (cy.keep != 0.0f) each<Cfg>(S, [&](float x, int, int, int) { return __builtin_fmaf(x, cy.m, x); });
+    else each<Cfg>(S, [&](float x, int, int, int) { return x * cy.m; });
 }
 
 // ----------------------------------------------------------------- begins
-// begin bits of the C <= 64 rows of a chunk in walking order
-__device__ __forceinline__ uint64_t ret_begins(const uint8_t* start, int64_t w0, int n, int64_t T, bool rev, int lane) {
-    // backwards, row i is step t = T - 1 - w0 - i and begins if step t + 1 does
-    const int64_t t = rev ? T - w0 - lane : w0 + lane;
-    const bool in = lane < n && t < T;
-    return __ballot(in && start[in ? t : 0] != 0);
+// The begin flag of row `lane` of a chunk in walking order, 0 past its n rows:
+// backwards row i is step t = T - 1 - w0 - i and begins if step t + 1 does (the last
+// step goes on from what follows the tape).
+__device__ __forceinline__ uint32_t ret_flag(const uint8_t* start, int64_t w0, int n, int64_t T, bool rev, int lane) {
+    const int64_t t0 = rev ? T - w0 - (n - 1) : w0;        // the lowest step looked at
+    const int64_t left = T - t0;
+    const Rsrc r = make_rsrc(start + t0, n <= 0 ? 0 : left < n ? left : n);
+    return bload_u8(r, (uint32_t)(rev ? n - 1 - lane : lane));
 }
 __device__ __forceinline__ uint64_t upto(int i) { return (2ull << i) - 1ull; }          // bits 0 .. i
 __device__ __forceinline__ int last_begin(uint64_t m) { return 63 - __builtin_clzll(m); }   // m != 0
