@@ -19,7 +19,7 @@
 //
 // A value that is not finite must not reach other episodes, nor earlier rows of
 // its own, through a zero of P or of the decays (0 * NaN): a chunk that holds one
-// is walked row by row, each a chunk of its own with the other rows as zeros.
+// is walked row by row, by the recurrence itself in floats.
 #include "retention_common.hpp"
 
 namespace memoroid {
@@ -77,14 +77,14 @@ __device__ __forceinline__ void tile_of(int idx, int& jb, int& ib) {
     ib = idx >= 6 ? 3 : idx >= 3 ? 2 : idx >= 1 ? 1 : 0;
     jb = idx - ib * (ib + 1) / 2;
 }
-template <class Cfg, int LD, int D>
+template <class Cfg, int D>
 __device__ __forceinline__ f32x4 pair_products(const uint16_t* sY, const uint16_t* sX, int jb, int ib, const RetLane& L) {
     f32x4 d = zero4();
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) {
         bf16x8 y[Cfg::NP], x[Cfg::NP];
-        row_frag<Cfg, LD>(y, sY, 16 * jb, 32 * s, L);
-        row_frag<Cfg, LD>(x, sX, 16 * ib, 32 * s, L);
+        row_frag<Cfg, D>(y, sY, 16 * jb, s, L);
+        row_frag<Cfg, D>(x, sX, 16 * ib, s, L);
         mma<Cfg::NP, Cfg::NP>(d, y, x);
     }
     return d;
@@ -95,8 +95,8 @@ __device__ __forceinline__ f32x4 pair_products(const uint16_t* sY, const uint16_
 // begin on.  DOT: also its derivative by log gamma, sum (n-1-j) gamma^(n-1-j) y^T z.
 template <class Cfg, bool DOT>
 __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummaryArgs p) {
-    __shared__ __attribute__((aligned(16))) uint16_t sY[Cfg::NP * Cfg::C * Cfg::LDK];
-    __shared__ __attribute__((aligned(16))) uint16_t sZ[Cfg::NP * Cfg::C * Cfg::LDV];
+    __shared__ __attribute__((aligned(16))) uint16_t sY[Cfg::NP * Cfg::C * Cfg::KD];
+    __shared__ __attribute__((aligned(16))) uint16_t sZ[Cfg::NP * Cfg::C * Cfg::VD];
     __shared__ Decays<Cfg> sD;
     __shared__ __attribute__((aligned(16))) float sW[DOT ? 2 : 1][Cfg::C];
     RetLane L;
@@ -131,13 +131,8 @@ __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummary
         const int from = m ? last_begin(m) : 0;
         any = any || m != 0;
         barrier_lds();                                     // the last chunk's operands have been read
-        if (m) {
-            ty.template stage<Cfg::LDK, true>(sY, from, Cfg::C, L);
-            tz.template stage<Cfg::LDV, true>(sZ, from, Cfg::C, L);
-        } else {
-            ty.template stage<Cfg::LDK, false>(sY, 0, 0, L);
-            tz.template stage<Cfg::LDV, false>(sZ, 0, 0, L);
-        }
+        ty.stage(sY, from, L);
+        tz.stage(sZ, from, L);
         if (L.tid < Cfg::C) {
             const int age = Cfg::C - 1 - L.tid;
             const float w = L.tid >= from ? sD.pw[age] * p.z_scale : 0.0f;
@@ -155,7 +150,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummary
 #pragma unroll
         for (int tb = 0; tb < Cfg::C / 32; ++tb) {
             bf16x8 z[Cfg::NP], zw[3], zd[3];
-            col_frag<Cfg, Cfg::LDV>(z, sZ, tb, state_col_addr(L), L);
+            col_frag<Cfg, Cfg::VD>(z, sZ, tb, state_col_addr(L), L);
             weigh<Cfg>(zw, z, sW[0], tb, L);
             if (DOT) weigh<Cfg>(zd, z, sW[DOT ? 1 : 0], tb, L);
 #pragma unroll
@@ -163,7 +158,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummary
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     bf16x8 y[Cfg::NP];
-                    col_frag<Cfg, Cfg::LDK>(y, sY, tb, state_row_addr(s, u, L), L);
+                    col_frag<Cfg, Cfg::KD>(y, sY, tb, state_row_addr(s, u, L), L);
                     mma<Cfg::NP, 3>(S[s][u], y, zw);
                     if (DOT) mma<Cfg::NP, 3>(D[s][u], y, zd);
                 }
@@ -203,13 +198,54 @@ __global__ __launch_bounds__(256) void ret_state_scan_kernel(RetStateScanArgs p)
 }
 
 // ---------------------------------------------------------------------- walk
+// The masked, decayed products of a chunk's rows in tiles as operands of the next
+// product, a tile or two per wavefront.  by_age[16 + n]: the weight of a partner n
+// steps back, 0 for n < 0;  m: begin bits.  Returns whether a row's
+// product with itself came out not finite: every x and y that is not finite shows
+// there (and so does one that overflows).
 template <class Cfg>
-__global__ __launch_bounds__(Cfg::THREADS, Cfg::NP == 1 ? 4 : 2) void ret_walk_kernel(RetWalkArgs p) {
-    __shared__ __attribute__((aligned(16))) uint16_t sX[Cfg::NP * Cfg::C * Cfg::LDK];
-    __shared__ __attribute__((aligned(16))) uint16_t sY[Cfg::NP * Cfg::C * Cfg::LDK];
-    __shared__ __attribute__((aligned(16))) uint16_t sZ[Cfg::NP * Cfg::C * Cfg::LDV];
+__device__ __forceinline__ bool pairs(u32x2 (&sP)[Cfg::NTILE][Cfg::NP][64], const uint16_t* sX, const uint16_t* sY,
+                                      const float* by_age, uint64_t m, const RetLane& L) {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < (Cfg::NTILE + Cfg::W - 1) / Cfg::W; ++i) {
+        const int idx = Cfg::W * i + L.w;
+        if (idx >= Cfg::NTILE) break;
+        int jb, ib;
+        tile_of(idx, jb, ib);
+        f32x4 d = pair_products<Cfg, Cfg::KD>(sY, sX, jb, ib, L);
+        const int row = 16 * ib + L.c, age = row - 16 * jb - 4 * L.g;      // of register 0
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if (ib == jb) bad |= age == r && !(fabsf(d[r]) < __builtin_inff());
+            d[r] *= by_age[age - r + 16];
+        }
+        if (m) {                                                           // age of the row's first partner
+            const uint64_t mr = m & upto(row);
+            const int oldest = mr ? row - last_begin(mr) : row;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) d[r] = age - r <= oldest ? d[r] : 0.0f;
+        }
+        uint32_t lo[Cfg::NP], hi[Cfg::NP];
+        planes2<Cfg::NP>(d[0], d[1], lo);
+        planes2<Cfg::NP>(d[2], d[3], hi);
+#pragma unroll
+        for (int q = 0; q < Cfg::NP; ++q) sP[idx][q][L.lane] = u32x2{lo[q], hi[q]};
+    }
+    return bad;
+}
+
+template <class Cfg>
+__global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 : 3) void ret_walk_kernel(RetWalkArgs p) {
+    __shared__ __attribute__((aligned(16))) uint16_t sX[Cfg::NP * Cfg::C * Cfg::KD];
+    __shared__ __attribute__((aligned(16))) uint16_t sY[Cfg::NP * Cfg::C * Cfg::KD];
+    __shared__ __attribute__((aligned(16))) uint16_t sZ[Cfg::NP * Cfg::C * Cfg::VD];
+    // bf16 out: rows gathered here, so that they leave 16 bytes a lane, a row at a
+    // time (a wavefront's own 32 bytes of a row doubled the bytes written)
+    __shared__ __attribute__((aligned(16))) uint16_t sO[Cfg::NP == 1 ? Cfg::C * Cfg::VD : 8];
     __shared__ u32x2 sP[Cfg::NTILE][Cfg::NP][64];
     __shared__ Decays<Cfg> sD;
+    __shared__ float sAge[Cfg::C + 16];
     __shared__ __attribute__((aligned(16))) float sW[Cfg::C];
     __shared__ uint32_t sBad[Cfg::W];
     RetLane L;
@@ -217,25 +253,45 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::NP == 1 ? 4 : 2) void ret_walk_k
     ret_header(p.hdr, p.sig);
     const double rate = fabs((double)p.alpha[h]);
     sD.fill(rate, L.tid);
+    if (L.tid < Cfg::C + 16) sAge[L.tid] = L.tid < 16 ? 0.0f : decay_pow(rate, L.tid - 16) * p.p_scale;
     const Head hx = head_of<Cfg>(p.x, b, h, p.T), hy = head_of<Cfg>(p.y, b, h, p.T), hz = head_of<Cfg>(p.z, b, h, p.T);
     const uint8_t* const start = p.start + b * p.T;
     const int64_t words = (int64_t)p.x.d * p.z.d, bh = b * p.H + h;
     const int64_t seg0 = seg * p.chunks * Cfg::C;
     const int64_t left = (p.T - seg0 + Cfg::C - 1) / Cfg::C;
     const int nch = (int)(left < p.chunks ? left : p.chunks);
+    const int os = Cfg::NP == 1 && !p.out_f32 ? 2 : 4;
+    auto rows_in = [&](int ch) {                           // rows of chunk ch, none past the segment
+        const int64_t rest = ch < nch ? p.T - (seg0 + (int64_t)ch * Cfg::C) : 0;
+        return (int)(rest < Cfg::C ? rest : Cfg::C);
+    };
+    auto first_of = [&](int ch) { return ch < nch ? seg0 + (int64_t)ch * Cfg::C : 0; };
+    auto rows_out = [&](int ch) {
+        return ret_rows((char*)p.out + (b * p.T * p.H + h) * p.z.d * os, (int64_t)p.H * p.z.d * os, p.z.d, os, first_of(ch),
+                        rows_in(ch), p.T, p.rev);
+    };
 
     RetTile<Cfg, Cfg::KD> tx, ty;
     RetTile<Cfg, Cfg::VD> tz;
     uint32_t flag;
     auto fetch = [&](int ch) {
-        const bool have = ch < nch;
-        const int64_t w0 = have ? seg0 + (int64_t)ch * Cfg::C : 0;
-        const int64_t rest = have ? p.T - w0 : 0;
-        const int n = (int)(rest < Cfg::C ? rest : Cfg::C);
+        const int64_t w0 = first_of(ch);
+        const int n = rows_in(ch);
         flag = ret_flag(start, w0, n, p.T, p.rev, L.lane);
         tx.fetch(rows_of<Cfg>(hx, w0, n, p.T, p.rev), L);
         ty.fetch(rows_of<Cfg>(hy, w0, n, p.T, p.rev), L);
         tz.fetch(rows_of<Cfg>(hz, w0, n, p.T, p.rev), L);
+    };
+    bool held = false;                                     // the last chunk's rows wait in sO
+    auto put_rows = [&](int ch) {
+        const RetRows o = rows_out(ch);
+        constexpr int UPR = Cfg::VD / 8, RS = Cfg::THREADS / UPR;
+#pragma unroll
+        for (int i = 0; i < Cfg::C / RS; ++i) {
+            const int row = L.tid / UPR + i * RS, unit = L.tid % UPR;
+            const u32x4 x = *(const u32x4*)(sO + row * Cfg::VD + swizzled<Cfg::VD>(unit, row) * 8);
+            __builtin_amdgcn_raw_buffer_store_b128(x, o.r, (int)o.offset(row, 8 * unit, 2), 0, 0);
+        }
     };
     fetch(0);
     State<Cfg> S;
@@ -244,66 +300,34 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::NP == 1 ? 4 : 2) void ret_walk_k
 #pragma unroll 1
     for (int ch = 0; ch < nch; ++ch) {
         L.again();
-        const int64_t w0 = seg0 + (int64_t)ch * Cfg::C;
-        const int n = (int)(p.T - w0 < Cfg::C ? p.T - w0 : Cfg::C);
+        const int n = rows_in(ch);
         const uint64_t m = __ballot(flag != 0u);
-        const uint64_t not_finite = __ballot((tx.bad() | ty.bad() | tz.bad()) != 0u);
+        const bool bad_z = tz.bad() != 0u;
         barrier_lds();                                     // the last chunk's operands have been read
-        if (L.lane == 0) sBad[L.w] = not_finite != 0;
-        tx.template stage<Cfg::LDK, false>(sX, 0, 0, L);
-        ty.template stage<Cfg::LDK, false>(sY, 0, 0, L);
-        tz.template stage<Cfg::LDV, false>(sZ, 0, 0, L);
+        tx.stage(sX, 0, L);
+        ty.stage(sY, 0, L);
+        tz.stage(sZ, 0, L);
         // weights of the rows into the state: no begin step after them
         if (L.tid < Cfg::C) {
             const int from = m ? last_begin(m) : 0;
             sW[L.tid] = L.tid >= from && L.tid < n ? sD.pw[L.tid < n ? n - 1 - L.tid : 0] * p.z_scale : 0.0f;
         }
+        fetch(ch + 1);
+        if (Cfg::NP == 1 && held) put_rows(ch - 1);
         barrier_lds();
+        const bool bad = bad_z | pairs<Cfg>(sP, sX, sY, sAge, m, L);
+        const uint64_t bads = __ballot(bad);
+        if (L.lane == 0) sBad[L.w] = bads != 0;
+        barrier_lds();
+        L.again();
         uint32_t any_bad = 0;
 #pragma unroll
         for (int i = 0; i < Cfg::W; ++i) any_bad |= sBad[i];
-        const bool by_row = __builtin_amdgcn_readfirstlane((int)any_bad) != 0;
-        int a = 0;
-#pragma unroll 1
-        do {
-            L.again();
-            const int to = by_row ? a + 1 : n;             // rows a .. to - 1
-            if (by_row) {
-                barrier_lds();
-                tx.template stage<Cfg::LDK, true>(sX, a, to, L);
-                ty.template stage<Cfg::LDK, true>(sY, a, to, L);
-                tz.template stage<Cfg::LDV, true>(sZ, a, to, L);
-                if (L.tid < Cfg::C) sW[L.tid] = L.tid == a ? p.z_scale : 0.0f;
-                barrier_lds();
-            }
-            if (to == n) fetch(ch + 1);
-            const uint64_t mw = m & (upto(to - 1) & ~((1ull << a) - 1ull));
-            const int e = p.rev && w0 + a == 0 ? 0 : 1;
+        // the gradient of the state after the tape belongs to the last step
+        const int e = p.rev && seg == 0 && ch == 0 ? 0 : 1;
+        held = Cfg::NP == 1 && os == 2 && any_bad == 0;
 
-            // ---- the pairs' products, a tile or two per wavefront
-#pragma unroll
-            for (int i = 0; i < (Cfg::NTILE + Cfg::W - 1) / Cfg::W; ++i) {
-                const int idx = Cfg::W * i + L.w;
-                if (idx >= Cfg::NTILE) break;
-                int jb, ib;
-                tile_of(idx, jb, ib);
-                f32x4 d = pair_products<Cfg, Cfg::LDK, Cfg::KD>(sY, sX, jb, ib, L);
-                const int row = 16 * ib + L.c;
-                const uint64_t mr = mw & upto(row);
-                const int first = mr ? last_begin(mr) : a;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int j = 16 * jb + 4 * L.g + r;
-                    d[r] = j <= row && j >= first ? d[r] * (sD.pw[j <= row ? row - j : 0] * p.p_scale) : 0.0f;
-                }
-                uint32_t lo[Cfg::NP], hi[Cfg::NP];
-                planes2<Cfg::NP>(d[0], d[1], lo);
-                planes2<Cfg::NP>(d[2], d[3], hi);
-#pragma unroll
-                for (int q = 0; q < Cfg::NP; ++q) sP[idx][q][L.lane] = u32x2{lo[q], hi[q]};
-            }
-            barrier_lds();
-
+        if (__builtin_amdgcn_readfirstlane((int)any_bad) == 0) {
             // ---- the rows against the state before the chunk
             f32x4 acc[Cfg::NB];
 #pragma unroll
@@ -315,25 +339,28 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::NP == 1 ? 4 : 2) void ret_walk_k
 #pragma unroll
                 for (int ib = 0; ib < Cfg::NB; ++ib) {
                     bf16x8 x[Cfg::NP];
-                    row_frag<Cfg, Cfg::LDK>(x, sX, 16 * ib, 32 * s, L);
+                    row_frag<Cfg, Cfg::KD>(x, sX, 16 * ib, s, L);
                     mma<Cfg::NP, Cfg::NP>(acc[ib], st, x);
                 }
+                // without a limit the scheduler reads all of x ahead, and the
+                // registers of the next chunk's rows are spilled, which waits for them
+                if (s % 2 == 1) __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
             for (int ib = 0; ib < Cfg::NB; ++ib) {
                 const int row = 16 * ib + L.c;
-                const bool goes_on = (mw & upto(row)) == 0 && row >= a && row < to;
-                const float f = goes_on ? sD.pw[row - a + e] * p.inter_scale : 0.0f;
+                const bool goes_on = (m & upto(row)) == 0;
+                const float f = sD.pw[row + e] * p.inter_scale;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) acc[ib][r] = goes_on ? acc[ib][r] * f : 0.0f;
             }
 
             // ---- the rows against each other, and the state after the chunk
-            carry_state<Cfg>(S, sD.carry[to - a - 1 + e], mw != 0);
+            carry_state<Cfg>(S, sD.carry[n - 1 + e], m != 0);
 #pragma unroll
             for (int tb = 0; tb < Cfg::C / 32; ++tb) {
                 bf16x8 z[Cfg::NP], zw[3];
-                col_frag<Cfg, Cfg::LDV>(z, sZ, tb, state_col_addr(L), L);
+                col_frag<Cfg, Cfg::VD>(z, sZ, tb, state_col_addr(L), L);
 #pragma unroll
                 for (int ib = 2 * tb; ib < Cfg::NB; ++ib) {
                     const int t0 = ib * (ib + 1) / 2 + 2 * tb;
@@ -352,30 +379,57 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::NP == 1 ? 4 : 2) void ret_walk_k
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         bf16x8 y[Cfg::NP];
-                        col_frag<Cfg, Cfg::LDK>(y, sY, tb, state_row_addr(s, u, L), L);
+                        col_frag<Cfg, Cfg::KD>(y, sY, tb, state_row_addr(s, u, L), L);
                         mma<Cfg::NP, 3>(S[s][u], y, zw);
                     }
             }
 
             // ---- out: four consecutive columns of a row per lane
-            {
-                const int os = Cfg::NP == 1 && !p.out_f32 ? 2 : 4;
-                const int64_t orow = (int64_t)p.H * p.z.d * os;
-                const RetRows o = ret_rows((char*)p.out + (b * p.T * p.H + h) * p.z.d * os, orow, p.z.d, os, w0, n, p.T, p.rev);
+            if (Cfg::NP == 1 && os == 2) {
 #pragma unroll
                 for (int ib = 0; ib < Cfg::NB; ++ib) {
-                    const int row = 16 * ib + L.c;
-                    const uint32_t off = row >= a && row < to ? o.offset(row, 16 * L.w + 4 * L.g, os) : kOob;
-                    if (os == 2)
-                        __builtin_amdgcn_raw_buffer_store_b64(
-                            u32x2{f32x2_to_bf16x2(acc[ib][0], acc[ib][1]), f32x2_to_bf16x2(acc[ib][2], acc[ib][3])}, o.r,
-                            (int)off, 0, 0);
-                    else
-                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[ib]), o.r, (int)off, 0, 0);
+                    const int row = 16 * ib + L.c, unit = 2 * L.w + (L.g >> 1);
+                    *(u32x2*)(sO + row * Cfg::VD + swizzled<Cfg::VD>(unit, row) * 8 + 4 * (L.g & 1)) =
+                        u32x2{f32x2_to_bf16x2(acc[ib][0], acc[ib][1]), f32x2_to_bf16x2(acc[ib][2], acc[ib][3])};
                 }
+            } else {
+                const RetRows o = rows_out(ch);
+#pragma unroll
+                for (int ib = 0; ib < Cfg::NB; ++ib)
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[ib]), o.r,
+                                                           (int)o.offset(16 * ib + L.c, 16 * L.w + 4 * L.g, 4), 0, 0);
             }
-            a = to;
-        } while (a < n);
+        } else {
+            // ---- row by row
+            const RetRows o = rows_out(ch);
+#pragma unroll 1
+            for (int i = 0; i < n; ++i) {
+                carry_state<Cfg>(S, sD.carry[i == 0 ? e : 1], (m >> i) & 1ull);
+                const float z = tile_value<Cfg, Cfg::VD>(sZ, i, state_col(L)) * p.z_scale;
+                float sum = 0.0f;
+#pragma unroll
+                for (int s = 0; s < Cfg::KS; ++s) {
+                    float x[8], y[8];
+                    row_values<Cfg, Cfg::KD>(x, sX, i, s, L);
+                    row_values<Cfg, Cfg::KD>(y, sY, i, s, L);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        S[s][k >> 2][k & 3] = __builtin_fmaf(y[k], z, S[s][k >> 2][k & 3]);
+                        sum = __builtin_fmaf(x[k], S[s][k >> 2][k & 3], sum);
+                    }
+                }
+                sum += lanes_xor(sum, 16);
+                sum += lanes_xor(sum, 32);
+                sum *= p.inter_scale;
+                const uint32_t off = L.g == 0 ? o.offset(i, state_col(L), os) : kOob;
+                if (os == 2) __builtin_amdgcn_raw_buffer_store_b16((uint16_t)f32_to_bf16(sum), o.r, (int)off, 0, 0);
+                else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(sum), o.r, (int)off, 0, 0);
+            }
+        }
+    }
+    if (Cfg::NP == 1 && held) {
+        barrier_lds();
+        put_rows(nch - 1);
     }
     if (p.fin && seg == p.nseg - 1) {
         // backwards: the gradient of the state before the tape, one step further
@@ -395,11 +449,12 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::NP == 1 ? 4 : 2) void ret_walk_k
 // as floats in registers: nothing here is rounded to bf16.
 template <class Cfg>
 __global__ __launch_bounds__(Cfg::THREADS, 2) void ret_sens_kernel(RetSensArgs p) {
-    __shared__ __attribute__((aligned(16))) uint16_t sQ[Cfg::NP * Cfg::C * Cfg::LDK];
-    __shared__ __attribute__((aligned(16))) uint16_t sK[Cfg::NP * Cfg::C * Cfg::LDK];
-    __shared__ __attribute__((aligned(16))) uint16_t sV[Cfg::NP * Cfg::C * Cfg::LDV];
-    __shared__ __attribute__((aligned(16))) uint16_t sG[Cfg::NP * Cfg::C * Cfg::LDV];
+    __shared__ __attribute__((aligned(16))) uint16_t sQ[Cfg::NP * Cfg::C * Cfg::KD];
+    __shared__ __attribute__((aligned(16))) uint16_t sK[Cfg::NP * Cfg::C * Cfg::KD];
+    __shared__ __attribute__((aligned(16))) uint16_t sV[Cfg::NP * Cfg::C * Cfg::VD];
+    __shared__ __attribute__((aligned(16))) uint16_t sG[Cfg::NP * Cfg::C * Cfg::VD];
     __shared__ Decays<Cfg> sD;
+    __shared__ float sAge[Cfg::C + 16];                    // [16 + n]: n gamma^n scale, 0 for n < 0
     __shared__ __attribute__((aligned(16))) float sW[4][Cfg::C];
     __shared__ uint32_t sBad[Cfg::W];
     __shared__ double sSum[Cfg::W];
@@ -407,6 +462,10 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void ret_sens_kernel(RetSensArgs p
     const int64_t seg = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
     const double rate = fabs((double)p.alpha[h]);
     sD.fill(rate, L.tid);
+    if (L.tid < Cfg::C + 16) {
+        const int age = L.tid - 16;
+        sAge[L.tid] = age < 0 ? 0.0f : decay_pow(rate, age) * (float)age * p.scale;
+    }
     const int kd = p.q.d, vd = p.v.d;
     const Head hq = head_of<Cfg>(p.q, b, h, p.T), hk = head_of<Cfg>(p.k, b, h, p.T), hv = head_of<Cfg>(p.v, b, h, p.T),
                hg = head_of<Cfg>(p.g, b, h, p.T);
@@ -443,71 +502,51 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void ret_sens_kernel(RetSensArgs p
         const int n = (int)(p.T - w0 < Cfg::C ? p.T - w0 : Cfg::C);
         const uint64_t m = __ballot(flag != 0u);
         const uint64_t not_finite = __ballot((tq.bad() | tk.bad() | tv.bad() | tg.bad()) != 0u);
+        barrier_lds();                                     // the last operands have been read
         if (L.lane == 0) sBad[L.w] = not_finite != 0;
+        tq.stage(sQ, 0, L);
+        tk.stage(sK, 0, L);
+        tv.stage(sV, 0, L);
+        tg.stage(sG, 0, L);
+        if (L.tid < Cfg::C) {
+            const int i = L.tid;
+            const int from = m ? last_begin(m) : 0;
+            const float w = i < n && i >= from ? sD.pw[i < n ? n - 1 - i : 0] : 0.0f;
+            sW[0][i] = w;
+            sW[1][i] = w * (float)(n - 1 - i);
+            const float f = i < n && (m & upto(i)) == 0 ? sD.pw[i + 1] * p.scale : 0.0f;
+            sW[2][i] = f;
+            sW[3][i] = f * (float)(i + 1);
+        }
+        fetch(ch + 1);
         barrier_lds();
         uint32_t any_bad = 0;
 #pragma unroll
         for (int i = 0; i < Cfg::W; ++i) any_bad |= sBad[i];
-        const bool by_row = __builtin_amdgcn_readfirstlane((int)any_bad) != 0;
-        int a = 0;
-#pragma unroll 1
-        do {
-            L.again();
-            const int to = by_row ? a + 1 : n;
-            const uint64_t mw = m & (upto(to - 1) & ~((1ull << a) - 1ull));
-            barrier_lds();                                 // the last operands have been read
-            if (by_row) {
-                tq.template stage<Cfg::LDK, true>(sQ, a, to, L);
-                tk.template stage<Cfg::LDK, true>(sK, a, to, L);
-                tv.template stage<Cfg::LDV, true>(sV, a, to, L);
-                tg.template stage<Cfg::LDV, true>(sG, a, to, L);
-            } else {
-                tq.template stage<Cfg::LDK, false>(sQ, 0, 0, L);
-                tk.template stage<Cfg::LDK, false>(sK, 0, 0, L);
-                tv.template stage<Cfg::LDV, false>(sV, 0, 0, L);
-                tg.template stage<Cfg::LDV, false>(sG, 0, 0, L);
-            }
-            if (L.tid < Cfg::C) {
-                const int i = L.tid;
-                const bool in = i >= a && i < to;
-                const int from = mw ? last_begin(mw) : a;
-                const float w = in && i >= from ? sD.pw[in ? to - 1 - i : 0] : 0.0f;
-                sW[0][i] = w;
-                sW[1][i] = w * (float)(to - 1 - i);
-                const float f = in && (mw & upto(i)) == 0 ? sD.pw[in ? i - a + 1 : 0] * p.scale : 0.0f;
-                sW[2][i] = f;
-                sW[3][i] = f * (float)(i - a + 1);
-            }
-            if (to == n) fetch(ch + 1);
-            barrier_lds();
-            float part = 0.0f;
+        float part = 0.0f;
+        if (__builtin_amdgcn_readfirstlane((int)any_bad) == 0) {
 #pragma unroll
             for (int i = 0; i < (Cfg::NTILE + Cfg::W - 1) / Cfg::W; ++i) {
                 const int idx = Cfg::W * i + L.w;
                 if (idx >= Cfg::NTILE) break;
                 int jb, ib;
                 tile_of(idx, jb, ib);
-                const f32x4 x = pair_products<Cfg, Cfg::LDK, Cfg::KD>(sK, sQ, jb, ib, L);
-                const f32x4 y = pair_products<Cfg, Cfg::LDV, Cfg::VD>(sV, sG, jb, ib, L);
-                const int row = 16 * ib + L.c;
-                const uint64_t mr = mw & upto(row);
-                const int first = mr ? last_begin(mr) : a;
+                const f32x4 x = pair_products<Cfg, Cfg::KD>(sK, sQ, jb, ib, L);
+                const f32x4 y = pair_products<Cfg, Cfg::VD>(sV, sG, jb, ib, L);
+                const int row = 16 * ib + L.c, age = row - 16 * jb - 4 * L.g;
+                const uint64_t mr = m & upto(row);
+                const int oldest = mr ? row - last_begin(mr) : row;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int j = 16 * jb + 4 * L.g + r;
-                    const bool in = j < row && j >= first;
-                    const float w = sD.pw[in ? row - j : 0] * (float)(row - j) * p.scale;
-                    part += in ? x[r] * y[r] * w : 0.0f;
-                }
+                for (int r = 0; r < 4; ++r) part += age - r <= oldest ? x[r] * y[r] * sAge[age - r + 16] : 0.0f;
             }
             // rows against (S, D): skipped where the first row begins an episode,
             // so that values of S that are not finite stay out
-            if (!(mw >> a & 1ull)) {
+            if (!(m & 1ull)) {
                 bf16x8 g1[Cfg::C / 32][3], g2[Cfg::C / 32][3];
 #pragma unroll
                 for (int tb = 0; tb < Cfg::C / 32; ++tb) {
                     bf16x8 g[Cfg::NP];
-                    col_frag<Cfg, Cfg::LDV>(g, sG, tb, state_col_addr(L), L);
+                    col_frag<Cfg, Cfg::VD>(g, sG, tb, state_col_addr(L), L);
                     weigh<Cfg>(g1[tb], g, sW[2], tb, L);
                     weigh<Cfg>(g2[tb], g, sW[3], tb, L);
                 }
@@ -519,7 +558,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void ret_sens_kernel(RetSensArgs p
 #pragma unroll
                         for (int tb = 0; tb < Cfg::C / 32; ++tb) {
                             bf16x8 q[Cfg::NP];
-                            col_frag<Cfg, Cfg::LDK>(q, sQ, tb, state_row_addr(s, u, L), L);
+                            col_frag<Cfg, Cfg::KD>(q, sQ, tb, state_row_addr(s, u, L), L);
                             mma<Cfg::NP, 3>(o1, q, g1[tb]);
                             mma<Cfg::NP, 3>(o2, q, g2[tb]);
                         }
@@ -528,16 +567,14 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void ret_sens_kernel(RetSensArgs p
                             part = __builtin_fmaf(S[s][u][e], o2[e], __builtin_fmaf(D[s][u][e], o1[e], part));
                     }
             }
-            sum += (double)part;
-            // (S, D) after these rows
-            const int len = to - a;
-            each<Cfg>(D, [&](float x, int s, int u, int e) { return __builtin_fmaf((float)len, S[s][u][e], x); });
-            carry_state<Cfg>(D, sD.carry[len], mw != 0);
-            carry_state<Cfg>(S, sD.carry[len], mw != 0);
+            // (S, D) after the chunk
+            each<Cfg>(D, [&](float x, int s, int u, int e) { return __builtin_fmaf((float)n, S[s][u][e], x); });
+            carry_state<Cfg>(D, sD.carry[n], m != 0);
+            carry_state<Cfg>(S, sD.carry[n], m != 0);
 #pragma unroll
             for (int tb = 0; tb < Cfg::C / 32; ++tb) {
                 bf16x8 z[Cfg::NP], zw[3], zd[3];
-                col_frag<Cfg, Cfg::LDV>(z, sV, tb, state_col_addr(L), L);
+                col_frag<Cfg, Cfg::VD>(z, sV, tb, state_col_addr(L), L);
                 weigh<Cfg>(zw, z, sW[0], tb, L);
                 weigh<Cfg>(zd, z, sW[1], tb, L);
 #pragma unroll
@@ -545,13 +582,37 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void ret_sens_kernel(RetSensArgs p
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         bf16x8 y[Cfg::NP];
-                        col_frag<Cfg, Cfg::LDK>(y, sK, tb, state_row_addr(s, u, L), L);
+                        col_frag<Cfg, Cfg::KD>(y, sK, tb, state_row_addr(s, u, L), L);
                         mma<Cfg::NP, 3>(S[s][u], y, zw);
                         mma<Cfg::NP, 3>(D[s][u], y, zd);
                     }
             }
-            a = to;
-        } while (a < n);
+        } else {
+            // ---- row by row
+#pragma unroll 1
+            for (int i = 0; i < n; ++i) {
+                const bool begin = (m >> i) & 1ull;
+                each<Cfg>(D, [&](float x, int s, int u, int e) { return x + S[s][u][e]; });
+                carry_state<Cfg>(D, sD.carry[1], begin);
+                carry_state<Cfg>(S, sD.carry[1], begin);
+                const float v = tile_value<Cfg, Cfg::VD>(sV, i, state_col(L));
+                float dot = 0.0f;
+#pragma unroll
+                for (int s = 0; s < Cfg::KS; ++s) {
+                    float q[8], k[8];
+                    row_values<Cfg, Cfg::KD>(q, sQ, i, s, L);
+                    row_values<Cfg, Cfg::KD>(k, sK, i, s, L);
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) {
+                        S[s][x >> 2][x & 3] = __builtin_fmaf(k[x], v, S[s][x >> 2][x & 3]);
+                        dot = __builtin_fmaf(q[x], D[s][x >> 2][x & 3], dot);
+                    }
+                }
+                // (nothing where the row begins: 0 times what is not finite stays out)
+                if (!begin) part = __builtin_fmaf(dot * p.scale, tile_value<Cfg, Cfg::VD>(sG, i, state_col(L)), part);
+            }
+        }
+        sum += (double)part;
     }
     L.again();
     if (p.grad_state && seg == p.nseg - 1) {

@@ -54,7 +54,6 @@ struct RetCfg {
     static constexpr int W = VD / 16, THREADS = 64 * W;
     static constexpr int ES = NP == 1 ? 2 : 4;        // bytes of an element in memory
     static constexpr int EPU = 16 / ES;               // elements of a 16-byte unit
-    static constexpr int LDK = KD + 8, LDV = VD + 8;  // LDS row strides in elements
     static constexpr int NB = C / 16;                 // 16-row blocks
     static constexpr int NTILE = NB * (NB + 1) / 2;   // tiles of P on and below the diagonal
     static constexpr int KS = KD / 32;                // steps of a product over kd
@@ -146,19 +145,31 @@ __device__ __forceinline__ f32x4 zero4() { return f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 // their stores.
 struct RetRows {
     Rsrc r;
-    uint32_t row_bytes;
-    int n, d;
-    bool rev;
+    int first, step, d;         // byte offsets of row 0 and from row to row
     __device__ __forceinline__ uint32_t offset(int row, int col, int es) const {
-        const uint32_t at = (uint32_t)(rev ? n - 1 - row : row) * row_bytes + (uint32_t)(col * es);
-        return col < d ? at : kOob;
+        return col < d ? (uint32_t)(first + row * step + col * es) : kOob;
     }
 };
 __device__ __forceinline__ RetRows ret_rows(const void* head0, int64_t row_bytes, int d, int es, int64_t w0, int n,
                                             int64_t T, bool rev) {
     const int64_t t = rev ? T - w0 - n : w0;
-    return RetRows{make_rsrc((const char*)head0 + t * row_bytes, n > 0 ? (n - 1) * row_bytes + d * es : 0),
-                   (uint32_t)row_bytes, n, d, rev};
+    const int rb = (int)row_bytes, end = (n - 1) * rb;
+    return RetRows{make_rsrc((const char*)head0 + t * row_bytes, n > 0 ? (int64_t)end + d * es : 0), rev ? end : 0,
+                   rev ? -rb : rb, d};
+}
+
+// Where the 16-byte unit `unit` of row `row` of an LDS tile of D columns lies: the
+// units of a row are exchanged by its number, so that no operand meets a bank
+// conflict and rows need no padding.  A row operand reads one unit of 16 rows,
+// which lie in different banks (28 cycles more without the exchange); a column
+// operand reads half a unit each of four units, a quarter of the row, in four
+// neighbouring rows, so it is those rows' numbers that tell the quarters apart
+// (with the quarters told apart by row / 4 they were 5.5 cycles more a read).
+template <int D>
+__device__ __forceinline__ int swizzled(int unit, int row) {
+    static_assert(D == 64 || D == 128, "8 or 16 units a row");
+    const int q = (row >> 2) & 3;
+    return D == 128 ? unit ^ (((row & 3) << 2) | q) : unit ^ (((row & 2) << 1) | q);
 }
 
 // A chunk's tile of D columns held by the workgroup, 16 bytes a unit: thread
@@ -172,11 +183,11 @@ struct RetTile {
     __device__ __forceinline__ void fetch(const RetRows& x, const RetLane& L) {
         const int col = L.tid % UPR * Cfg::EPU;
         uint32_t off = x.offset(L.tid / UPR, col, Cfg::ES);
-        const uint32_t step = col < x.d ? (uint32_t)RS * x.row_bytes : 0u;
+        const uint32_t step = col < x.d ? (uint32_t)(RS * x.step) : 0u;
 #pragma unroll
         for (int i = 0; i < UN; ++i) {
             u[i] = __builtin_amdgcn_raw_buffer_load_b128(x.r, (int)off, 0, 0);
-            off = x.rev ? off - step : off + step;
+            off += step;
         }
     }
     // nonzero if some element is not finite
@@ -189,18 +200,17 @@ struct RetTile {
             for (int e = 0; e < 4; ++e) any |= (u[i][e] & kExp) + kOne;
         return any & (Cfg::NP == 1 ? 0x80008000u : 0x80000000u);
     }
-    // into an LDS tile of NP planes; WINDOW: rows a .. b - 1, the others as zeros
-    template <int LD, bool WINDOW>
-    __device__ __forceinline__ void stage(uint16_t* s, int a, int b, const RetLane& L) const {
-        uint16_t* const p0 = s + L.tid / UPR * LD + L.tid % UPR * Cfg::EPU;
+    // into an LDS tile of NP planes, rows before `from` as zeros
+    __device__ __forceinline__ void stage(uint16_t* s, int from, const RetLane& L) {
+        if (from > 0)
+#pragma unroll
+            for (int i = 0; i < UN; ++i)
+                if (L.tid / UPR + i * RS < from) u[i] = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
         for (int i = 0; i < UN; ++i) {
-            const int row = L.tid / UPR + i * RS;
-            const bool in = !WINDOW || (row >= a && row < b);
-            u32x4 x;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = in ? u[i][e] : 0u;
-            uint16_t* const p = p0 + i * RS * LD;
+            const int row = L.tid / UPR + i * RS, col = L.tid % UPR * Cfg::EPU;
+            const u32x4 x = u[i];
+            uint16_t* const p = s + row * D + swizzled<D>(col / 8, row) * 8 + col % 8;
             if constexpr (Cfg::NP == 1) {
                 *(u32x4*)p = x;
             } else {
@@ -208,30 +218,49 @@ struct RetTile {
                 planes2<3>(__uint_as_float(x[0]), __uint_as_float(x[1]), lo);
                 planes2<3>(__uint_as_float(x[2]), __uint_as_float(x[3]), hi);
 #pragma unroll
-                for (int q = 0; q < 3; ++q) *(u32x2*)(p + q * Cfg::C * LD) = u32x2{lo[q], hi[q]};
+                for (int q = 0; q < 3; ++q) *(u32x2*)(p + q * Cfg::C * D) = u32x2{lo[q], hi[q]};
             }
         }
     }
 };
 
 // ------------------------------------------------------------ LDS operands
-// 16 rows from row0, columns 32 s + 8 g ..: a row operand
-template <class Cfg, int LD>
-__device__ __forceinline__ void row_frag(bf16x8 (&f)[Cfg::NP], const uint16_t* s, int row0, int col0, const RetLane& L) {
+// columns 32 s + 8 g .. + 7 of one row as floats, the same in the 16 lanes of g
+template <class Cfg, int D>
+__device__ __forceinline__ void row_values(float (&v)[8], const uint16_t* t, int row, int s, const RetLane& L) {
+    bf16x8 f[Cfg::NP];
 #pragma unroll
     for (int p = 0; p < Cfg::NP; ++p)
-        f[p] = *(const bf16x8*)(s + p * Cfg::C * LD + (row0 + L.c) * LD + col0 + 8 * L.g);
+        f[p] = *(const bf16x8*)(t + p * Cfg::C * D + row * D + swizzled<D>(4 * s + L.g, row) * 8);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = plane_value<Cfg::NP>(f, e);
+}
+// one element
+template <class Cfg, int D>
+__device__ __forceinline__ float tile_value(const uint16_t* t, int row, int col) {
+    const uint16_t* const at = t + row * D + swizzled<D>(col >> 3, row) * 8 + (col & 7);
+    const float h = __uint_as_float((uint32_t)at[0] << 16);
+    if constexpr (Cfg::NP == 1) return h;
+    else return h + (__uint_as_float((uint32_t)at[Cfg::C * D] << 16) + __uint_as_float((uint32_t)at[2 * Cfg::C * D] << 16));
+}
+// 16 rows from row0 (a multiple of 16), columns 32 s + 8 g ..: a row operand
+template <class Cfg, int D>
+__device__ __forceinline__ void row_frag(bf16x8 (&f)[Cfg::NP], const uint16_t* t, int row0, int s, const RetLane& L) {
+#pragma unroll
+    for (int p = 0; p < Cfg::NP; ++p)
+        f[p] = *(const bf16x8*)(t + p * Cfg::C * D + (row0 + L.c) * D + swizzled<D>(4 * s + L.g, L.c) * 8);
 }
 // rows 32 tb .. + 31 as k, the column of `col` (of this lane's address: four
 // consecutive columns from there): a column operand
-template <class Cfg, int LD>
-__device__ __forceinline__ void col_frag(bf16x8 (&f)[Cfg::NP], const uint16_t* s, int tb, int col, const RetLane& L) {
+template <class Cfg, int D>
+__device__ __forceinline__ void col_frag(bf16x8 (&f)[Cfg::NP], const uint16_t* t, int tb, int col, const RetLane& L) {
     typedef __attribute__((address_space(3))) s16x4* LdsPtr;
+    const int row = 4 * L.g + (L.c >> 2);                  // of 16
+    const uint16_t* const t0 = t + (32 * tb + row) * D + swizzled<D>(col >> 3, row) * 8 + (col & 7);
 #pragma unroll
     for (int p = 0; p < Cfg::NP; ++p) {
-        const uint16_t* const at = s + p * Cfg::C * LD + (32 * tb + 4 * L.g + (L.c >> 2)) * LD + col;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(at + 16 * LD));
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(t0 + p * Cfg::C * D));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(t0 + p * Cfg::C * D + 16 * D));
         f[p] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 }
@@ -289,22 +318,24 @@ __device__ __forceinline__ void store_state(State<Cfg>& S, float* p, int sk, int
 // gamma^n = exp(-rate n), formed in 64 bits: a slow rate compounds over 1e5
 // steps, where the rounding of a 32-bit gamma^C would show.
 __device__ __forceinline__ float decay_pow(double rate, double n) { return n == 0.0 ? 1.0f : (float)exp(-rate * n); }
-// x -> gamma^n x without rounding gamma^n near 1: x + (gamma^n - 1) x there
-// m = gamma^n - 1 and keep = 1 there, m = gamma^n and keep = 0 elsewhere
+// x -> gamma^n x with gamma^n = hi + lo to 48 bits: a rounded factor near 1 would
+// be off the same way at every chunk
 struct Carry {
-    float m, keep;
-    __device__ __forceinline__ float operator()(float x) const { return __builtin_fmaf(x, m, keep != 0.0f ? x : 0.0f); }
+    float hi, lo;
+    __device__ __forceinline__ float operator()(float x) const { return __builtin_fmaf(x, lo, x * hi); }
 };
 __device__ __forceinline__ Carry carry_of(double rate, double n) {
-    if (n == 0.0) return Carry{0.0f, 1.0f};
-    const double p = exp(-rate * n);
-    return p > 0.5 ? Carry{(float)expm1(-rate * n), 1.0f} : Carry{(float)p, 0.0f};
+    const double p = n == 0.0 ? 1.0 : exp(-rate * n);
+    return Carry{(float)p, (float)(p - (double)(float)p)};
 }
 template <class Cfg>
 __device__ __forceinline__ void carry_state(State<Cfg>& S, Carry cy, bool drop) {
     if (drop) zero_state<Cfg>(S);
-    else if (cy.keep != 0.0f) each<Cfg>(S, [&](float x, int, int, int) { return __builtin_fmaf(x, cy.m, x); });
-    else each<Cfg>(S, [&](float x, int, int, int) { return x * cy.m; });
+    // one set of registers: without this both ways' results are kept apart
+    each<Cfg>(S, [&](float x, int, int, int) {
+        asm volatile("" : "+v"(x));
+        return cy(x);
+    });
 }
 
 // ----------------------------------------------------------------- begins
