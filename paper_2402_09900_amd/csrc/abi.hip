@@ -981,7 +981,7 @@ RetRole ret_role(const void* p, int64_t heads, int64_t d, int64_t share) {
 // Segment states of one direction, scanned.
 int ret_states(const RetPlan& p, RetRole y, RetRole z, const uint8_t* start, const float* alpha, const float* seed,
                float* states, float* dstates, uint8_t* R, float z_scale, int64_t B, int64_t T, int64_t H, bool rev,
-               WsHeader* hdr, uint64_t sig, hipStream_t s) {
+               bool exact, WsHeader* hdr, uint64_t sig, hipStream_t s) {
     RetSummaryArgs a{};
     a.y = y;
     a.z = z;
@@ -996,6 +996,7 @@ int ret_states(const RetPlan& p, RetRole y, RetRole z, const uint8_t* start, con
     a.nseg = p.nseg;
     a.chunks = p.chunks;
     a.rev = rev;
+    a.exact = exact;
     a.hdr = hdr;
     a.sig = sig;
     if (ret_summary_launch(p.planes, a, B, s) != hipSuccess) return MEMOROID_EHIP;
@@ -1085,7 +1086,7 @@ int memoroid_scan_retention(const void* q, const void* k, const void* v, const f
     float* const states = (float*)(ws + p.off_states);
     if (p.nseg > 1) {
         const int st = ret_states(p, rk, rv, start, alpha, state_in, states, nullptr, (uint8_t*)(ws + p.off_R), 1.0f, B,
-                                  T, H, false, (WsHeader*)ws, sig, s);
+                                  T, H, false, state_out != nullptr, (WsHeader*)ws, sig, s);
         if (st != MEMOROID_OK) return st;
     }
     RetWalkArgs a{};
@@ -1098,6 +1099,7 @@ int memoroid_scan_retention(const void* q, const void* k, const void* v, const f
     a.seed = state_in;
     a.states = states;
     a.fin = state_out;
+    a.exact = state_out != nullptr;
     a.sk = (int32_t)dv;
     a.sv = 1;
     a.p_scale = a.inter_scale = scale;
@@ -1156,10 +1158,10 @@ int memoroid_scan_retention_bwd(const void* q, const void* k, const void* v, con
     float* const rstates = (float*)(ws + bp.off_rstates);
     if (p.nseg > 1) {
         int st = ret_states(p, rk, rv, start, alpha, state_in, states, grad_alpha ? dstates : nullptr,
-                            (uint8_t*)(ws + p.off_R), 1.0f, B, T, H, false, (WsHeader*)ws, sig, s);
+                            (uint8_t*)(ws + p.off_R), 1.0f, B, T, H, false, grad_alpha != nullptr, (WsHeader*)ws, sig, s);
         if (st != MEMOROID_OK) return st;
         st = ret_states(p, rq, rg, start, alpha, grad_state_out, rstates, nullptr, (uint8_t*)(ws + bp.off_rR), scale, B,
-                        T, H, true, nullptr, 0, s);
+                        T, H, true, grad_state_in != nullptr, nullptr, 0, s);
         if (st != MEMOROID_OK) return st;
     }
     if (grad_alpha) {
@@ -1228,6 +1230,7 @@ int memoroid_scan_retention_bwd(const void* q, const void* k, const void* v, con
     a.sk = (int32_t)dv;
     a.sv = 1;
     a.fin = grad_state_in;
+    a.exact = grad_state_in != nullptr;
     if (ret_walk_launch(p.planes, a, B, s) != hipSuccess) return MEMOROID_EHIP;
     if (G > 1) {
         if (ret_share_launch(p.planes, (const float*)(ws + bp.off_gk), grad_k, B * T, (int32_t)Hk, (int32_t)G,

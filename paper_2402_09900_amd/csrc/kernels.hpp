@@ -318,6 +318,7 @@ struct RetWalkArgs {
     int64_t T;
     int32_t H, nseg, chunks;
     int32_t rev;                // backwards: see retention.hip on `seed` and `fin`
+    int32_t exact;              // bf16: the state is an fp32 result (always so with fin)
     WsHeader* hdr;              // header to prepare with sig, or NULL
     uint64_t sig;
 };
@@ -331,6 +332,7 @@ struct RetSummaryArgs {
     float z_scale;
     int64_t T;
     int32_t H, nseg, chunks, rev;
+    int32_t exact;              // as in RetWalkArgs (always so with dstates)
     WsHeader* hdr;
     uint64_t sig;
 };

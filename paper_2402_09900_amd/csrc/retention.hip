@@ -12,7 +12,8 @@
 // belongs to the last step itself: e = 0 in their first chunk.
 //
 // Precision.  States, decays and all sums are floats; z is multiplied by its
-// decay in float and goes into the state as three planes, exactly.  With bf16
+// decay in float and goes into the state as three planes, exactly (two, right to
+// 2^-18, where no state of bf16 inputs comes out).  With bf16
 // inputs P and the S that a row is multiplied with are rounded to bf16 once
 // each, as operands: together they add to the output's own rounding what one
 // more rounding would (1.4 times its error), and the state itself takes neither.
@@ -21,6 +22,8 @@
 // its own, through a zero of P or of the decays (0 * NaN): a chunk that holds one
 // is walked row by row, by the recurrence itself in floats.
 #include "retention_common.hpp"
+
+#include <type_traits>
 
 namespace memoroid {
 
@@ -47,22 +50,9 @@ __device__ __forceinline__ RetRows rows_of(const Head& x, int64_t w0, int n, int
     return ret_rows(x.p, x.row_bytes, x.d, Cfg::ES, w0, n, T, rev);
 }
 
-// gamma^n and its carry for n = 0 .. C
-template <class Cfg>
-struct Decays {
-    float pw[Cfg::C + 1];
-    Carry carry[Cfg::C + 1];
-    __device__ __forceinline__ void fill(double rate, int tid) {
-        if (tid <= Cfg::C) {
-            pw[tid] = decay_pow(rate, tid);
-            carry[tid] = carry_of(rate, tid);
-        }
-    }
-};
-
 // the value operand times a weight per row, in planes
-template <class Cfg>
-__device__ __forceinline__ void weigh(bf16x8 (&out)[3], const bf16x8 (&z)[Cfg::NP], const float* w, int tb,
+template <class Cfg, int ZP>
+__device__ __forceinline__ void weigh(bf16x8 (&out)[ZP], const bf16x8 (&z)[Cfg::NP], const float* w, int tb,
                                       const RetLane& L) {
     f32x4 lo = *(const f32x4*)(w + 32 * tb + 4 * L.g), hi = *(const f32x4*)(w + 32 * tb + 16 + 4 * L.g);
 #pragma unroll
@@ -70,7 +60,7 @@ __device__ __forceinline__ void weigh(bf16x8 (&out)[3], const bf16x8 (&z)[Cfg::N
         lo[e] *= plane_value<Cfg::NP>(z, e);
         hi[e] *= plane_value<Cfg::NP>(z, e + 4);
     }
-    planes8<3>(lo, hi, out);
+    planes8<ZP>(lo, hi, out);
 }
 // tile `idx` of the triangle: rows 16 jb.. of y against rows 16 ib.. of x
 __device__ __forceinline__ void tile_of(int idx, int& jb, int& ib) {
@@ -93,22 +83,24 @@ __device__ __forceinline__ f32x4 pair_products(const uint16_t* sY, const uint16_
 // ---------------------------------------------------------------- summaries
 // What a segment adds to the state after it: the sum over its rows from the last
 // begin on.  DOT: also its derivative by log gamma, sum (n-1-j) gamma^(n-1-j) y^T z.
-template <class Cfg, bool DOT>
+template <class Cfg, int ZP, bool DOT>
 __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummaryArgs p) {
     __shared__ __attribute__((aligned(16))) uint16_t sY[Cfg::NP * Cfg::C * Cfg::KD];
     __shared__ __attribute__((aligned(16))) uint16_t sZ[Cfg::NP * Cfg::C * Cfg::VD];
-    __shared__ Decays<Cfg> sD;
+    __shared__ Powers<Cfg::C + 1> sPw;
     __shared__ __attribute__((aligned(16))) float sW[DOT ? 2 : 1][Cfg::C];
     RetLane L;
     const int64_t seg = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
     ret_header(p.hdr, p.sig);
     const double rate = fabs((double)p.alpha[h]);
-    sD.fill(rate, L.tid);
+    sPw.fill(rate, L.tid);
     const Head hy = head_of<Cfg>(p.y, b, h, p.T), hz = head_of<Cfg>(p.z, b, h, p.T);
     const uint8_t* const start = p.start + b * p.T;
     State<Cfg> S, D;
     zero_state<Cfg>(S);
     if (DOT) zero_state<Cfg>(D);
+    Owed owed;
+    __syncthreads();                                       // the powers are there
     bool any = false;
     RetTile<Cfg, Cfg::KD> ty;
     RetTile<Cfg, Cfg::VD> tz;
@@ -117,8 +109,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummary
     // chunk that is not there, reads nothing)
     auto fetch = [&](int ch) {
         const bool have = ch < p.chunks;
-        const int64_t w0 = have ? (seg * p.chunks + ch) * Cfg::C : 0;
-        const int n = have ? Cfg::C : 0;
+        const int w0 = have ? ((int)seg * p.chunks + ch) * Cfg::C : 0, n = have ? Cfg::C : 0;
         flag = ret_flag(start, w0, n, p.T, p.rev, L.lane);
         ty.fetch(rows_of<Cfg>(hy, w0, n, p.T, p.rev), L);
         tz.fetch(rows_of<Cfg>(hz, w0, n, p.T, p.rev), L);
@@ -130,45 +121,50 @@ __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummary
         const uint64_t m = __ballot(flag != 0u);
         const int from = m ? last_begin(m) : 0;
         any = any || m != 0;
+        bool take = false;
+        if (m) owed.none();
+        else take = owed.add(sPw, Cfg::C);
+        const Carry cy = carry_by(owed.now);
+        if (take) owed.none();
         barrier_lds();                                     // the last chunk's operands have been read
         ty.stage(sY, from, L);
         tz.stage(sZ, from, L);
         if (L.tid < Cfg::C) {
             const int age = Cfg::C - 1 - L.tid;
-            const float w = L.tid >= from ? sD.pw[age] * p.z_scale : 0.0f;
+            const float w = L.tid >= from ? sPw.f(age) * p.z_scale * (float)owed.inverse : 0.0f;
             sW[0][L.tid] = w;
             if (DOT) sW[DOT ? 1 : 0][L.tid] = w * (float)age;
         }
         fetch(ch + 1);
         barrier_lds();
+        // d(gamma^C S)/dlog gamma = gamma^C (D + C S)
         if (DOT) {
-            // d(gamma^C S)/dlog gamma = gamma^C (D + C S)
             each<Cfg>(D, [&](float x, int s, int u, int e) { return __builtin_fmaf((float)Cfg::C, S[s][u][e], x); });
-            carry_state<Cfg>(D, sD.carry[Cfg::C], m != 0);
+            settle<Cfg>(D, m != 0, take, cy);
         }
-        carry_state<Cfg>(S, sD.carry[Cfg::C], m != 0);
+        settle<Cfg>(S, m != 0, take, cy);
 #pragma unroll
         for (int tb = 0; tb < Cfg::C / 32; ++tb) {
-            bf16x8 z[Cfg::NP], zw[3], zd[3];
+            bf16x8 z[Cfg::NP], zw[ZP], zd[ZP];
             col_frag<Cfg, Cfg::VD>(z, sZ, tb, state_col_addr(L), L);
-            weigh<Cfg>(zw, z, sW[0], tb, L);
-            if (DOT) weigh<Cfg>(zd, z, sW[DOT ? 1 : 0], tb, L);
+            weigh<Cfg, ZP>(zw, z, sW[0], tb, L);
+            if (DOT) weigh<Cfg, ZP>(zd, z, sW[DOT ? 1 : 0], tb, L);
 #pragma unroll
             for (int s = 0; s < Cfg::KS; ++s)
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     bf16x8 y[Cfg::NP];
                     col_frag<Cfg, Cfg::KD>(y, sY, tb, state_row_addr(s, u, L), L);
-                    mma<Cfg::NP, 3>(S[s][u], y, zw);
-                    if (DOT) mma<Cfg::NP, 3>(D[s][u], y, zd);
+                    mma<Cfg::NP, ZP>(S[s][u], y, zw);
+                    if (DOT) mma<Cfg::NP, ZP>(D[s][u], y, zd);
                 }
         }
     }
     L.again();
     const int64_t words = (int64_t)p.y.d * p.z.d, n = p.nseg - 1;
     const int64_t at = ((b * p.H + h) * n + seg) * words;
-    store_state<Cfg>(S, p.states + at, p.z.d, 1, p.y.d, p.z.d, 1.0f, false, L);
-    if (DOT) store_state<Cfg>(D, p.dstates + at, p.z.d, 1, p.y.d, p.z.d, 1.0f, false, L);
+    store_state<Cfg>(S, p.states + at, p.z.d, 1, p.y.d, p.z.d, (float)owed.now, false, L);
+    if (DOT) store_state<Cfg>(D, p.dstates + at, p.z.d, 1, p.y.d, p.z.d, (float)owed.now, false, L);
     if (h == 0 && L.tid == 0) p.R[b * n + seg] = any ? 1 : 0;
 }
 
@@ -235,7 +231,7 @@ __device__ __forceinline__ bool pairs(u32x2 (&sP)[Cfg::NTILE][Cfg::NP][64], cons
     return bad;
 }
 
-template <class Cfg>
+template <class Cfg, int ZP>
 __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 : 3) void ret_walk_kernel(RetWalkArgs p) {
     __shared__ __attribute__((aligned(16))) uint16_t sX[Cfg::NP * Cfg::C * Cfg::KD];
     __shared__ __attribute__((aligned(16))) uint16_t sY[Cfg::NP * Cfg::C * Cfg::KD];
@@ -244,7 +240,7 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 :
     // time (a wavefront's own 32 bytes of a row doubled the bytes written)
     __shared__ __attribute__((aligned(16))) uint16_t sO[Cfg::NP == 1 ? Cfg::C * Cfg::VD : 8];
     __shared__ u32x2 sP[Cfg::NTILE][Cfg::NP][64];
-    __shared__ Decays<Cfg> sD;
+    __shared__ Powers<Cfg::C + 1> sPw;
     __shared__ float sAge[Cfg::C + 16];
     __shared__ __attribute__((aligned(16))) float sW[Cfg::C];
     __shared__ uint32_t sBad[Cfg::W];
@@ -252,20 +248,19 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 :
     const int64_t seg = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
     ret_header(p.hdr, p.sig);
     const double rate = fabs((double)p.alpha[h]);
-    sD.fill(rate, L.tid);
+    sPw.fill(rate, L.tid);
     if (L.tid < Cfg::C + 16) sAge[L.tid] = L.tid < 16 ? 0.0f : decay_pow(rate, L.tid - 16) * p.p_scale;
     const Head hx = head_of<Cfg>(p.x, b, h, p.T), hy = head_of<Cfg>(p.y, b, h, p.T), hz = head_of<Cfg>(p.z, b, h, p.T);
     const uint8_t* const start = p.start + b * p.T;
     const int64_t words = (int64_t)p.x.d * p.z.d, bh = b * p.H + h;
-    const int64_t seg0 = seg * p.chunks * Cfg::C;
-    const int64_t left = (p.T - seg0 + Cfg::C - 1) / Cfg::C;
-    const int nch = (int)(left < p.chunks ? left : p.chunks);
+    const int T = (int)p.T, seg0 = (int)seg * p.chunks * Cfg::C;
+    const int left = (T - seg0 + Cfg::C - 1) / Cfg::C, nch = left < p.chunks ? left : p.chunks;
     const int os = Cfg::NP == 1 && !p.out_f32 ? 2 : 4;
     auto rows_in = [&](int ch) {                           // rows of chunk ch, none past the segment
-        const int64_t rest = ch < nch ? p.T - (seg0 + (int64_t)ch * Cfg::C) : 0;
-        return (int)(rest < Cfg::C ? rest : Cfg::C);
+        const int rest = ch < nch ? T - (seg0 + ch * Cfg::C) : 0;
+        return rest < Cfg::C ? rest : Cfg::C;
     };
-    auto first_of = [&](int ch) { return ch < nch ? seg0 + (int64_t)ch * Cfg::C : 0; };
+    auto first_of = [&](int ch) { return ch < nch ? seg0 + ch * Cfg::C : 0; };
     auto rows_out = [&](int ch) {
         return ret_rows((char*)p.out + (b * p.T * p.H + h) * p.z.d * os, (int64_t)p.H * p.z.d * os, p.z.d, os, first_of(ch),
                         rows_in(ch), p.T, p.rev);
@@ -275,13 +270,14 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 :
     RetTile<Cfg, Cfg::VD> tz;
     uint32_t flag;
     auto fetch = [&](int ch) {
-        const int64_t w0 = first_of(ch);
-        const int n = rows_in(ch);
+        const int w0 = first_of(ch), n = rows_in(ch);
         flag = ret_flag(start, w0, n, p.T, p.rev, L.lane);
         tx.fetch(rows_of<Cfg>(hx, w0, n, p.T, p.rev), L);
         ty.fetch(rows_of<Cfg>(hy, w0, n, p.T, p.rev), L);
-        tz.fetch(rows_of<Cfg>(hz, w0, n, p.T, p.rev), L);
     };
+    auto fetch_z = [&](int ch) { tz.fetch(rows_of<Cfg>(hz, first_of(ch), rows_in(ch), p.T, p.rev), L); };
+    Owed owed;
+    __syncthreads();                                       // the powers are there
     bool held = false;                                     // the last chunk's rows wait in sO
     auto put_rows = [&](int ch) {
         const RetRows o = rows_out(ch);
@@ -294,6 +290,7 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 :
         }
     };
     fetch(0);
+    fetch_z(0);
     State<Cfg> S;
     load_state<Cfg>(S, seg == 0 ? (p.seed ? p.seed + bh * words : nullptr) : p.states + (bh * (p.nseg - 1) + seg - 1) * words,
                     p.sk, p.sv, p.x.d, p.z.d, L);
@@ -303,6 +300,14 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 :
         const int n = rows_in(ch);
         const uint64_t m = __ballot(flag != 0u);
         const bool bad_z = tz.bad() != 0u;
+        // the gradient of the state after the tape belongs to the last step
+        const int e = p.rev && seg == 0 && ch == 0 ? 0 : 1;
+        const float was = uniform((float)owed.now), before = was * p.inter_scale;
+        bool take = false;
+        if (m) owed.none();
+        else take = owed.add(sPw, n - 1 + e);
+        const Carry cy = carry_by(owed.now);
+        if (take) owed.none();
         barrier_lds();                                     // the last chunk's operands have been read
         tx.stage(sX, 0, L);
         ty.stage(sY, 0, L);
@@ -310,7 +315,7 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 :
         // weights of the rows into the state: no begin step after them
         if (L.tid < Cfg::C) {
             const int from = m ? last_begin(m) : 0;
-            sW[L.tid] = L.tid >= from && L.tid < n ? sD.pw[L.tid < n ? n - 1 - L.tid : 0] * p.z_scale : 0.0f;
+            sW[L.tid] = L.tid >= from && L.tid < n ? sPw.f(L.tid < n ? n - 1 - L.tid : 0) * p.z_scale * (float)owed.inverse : 0.0f;
         }
         fetch(ch + 1);
         if (Cfg::NP == 1 && held) put_rows(ch - 1);
@@ -323,8 +328,6 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 :
         uint32_t any_bad = 0;
 #pragma unroll
         for (int i = 0; i < Cfg::W; ++i) any_bad |= sBad[i];
-        // the gradient of the state after the tape belongs to the last step
-        const int e = p.rev && seg == 0 && ch == 0 ? 0 : 1;
         held = Cfg::NP == 1 && os == 2 && any_bad == 0;
 
         if (__builtin_amdgcn_readfirstlane((int)any_bad) == 0) {
@@ -347,19 +350,22 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 :
                 if (s % 2 == 1) __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
-            for (int ib = 0; ib < Cfg::NB; ++ib) {
-                const int row = 16 * ib + L.c;
-                const bool goes_on = (m & upto(row)) == 0;
-                const float f = sD.pw[row + e] * p.inter_scale;
+            for (int ib = 0; ib < Cfg::NB; ++ib) acc[ib] *= sPw.f(16 * ib + L.c + e) * before;
+            if (m) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) acc[ib][r] = goes_on ? acc[ib][r] * f : 0.0f;
+                for (int ib = 0; ib < Cfg::NB; ++ib) {
+                    const bool goes_on = (m & upto(16 * ib + L.c)) == 0;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[ib][r] = goes_on ? acc[ib][r] : 0.0f;
+                }
             }
+            settle<Cfg>(S, m != 0, take, cy);
+            fetch_z(ch + 1);                               // here, for the registers
 
             // ---- the rows against each other, and the state after the chunk
-            carry_state<Cfg>(S, sD.carry[n - 1 + e], m != 0);
 #pragma unroll
             for (int tb = 0; tb < Cfg::C / 32; ++tb) {
-                bf16x8 z[Cfg::NP], zw[3];
+                bf16x8 z[Cfg::NP], zw[ZP];
                 col_frag<Cfg, Cfg::VD>(z, sZ, tb, state_col_addr(L), L);
 #pragma unroll
                 for (int ib = 2 * tb; ib < Cfg::NB; ++ib) {
@@ -373,14 +379,14 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 :
                     }
                     mma<Cfg::NP, Cfg::NP>(acc[ib], z, pr);
                 }
-                weigh<Cfg>(zw, z, sW, tb, L);
+                weigh<Cfg, ZP>(zw, z, sW, tb, L);
 #pragma unroll
                 for (int s = 0; s < Cfg::KS; ++s)
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         bf16x8 y[Cfg::NP];
                         col_frag<Cfg, Cfg::KD>(y, sY, tb, state_row_addr(s, u, L), L);
-                        mma<Cfg::NP, 3>(S[s][u], y, zw);
+                        mma<Cfg::NP, ZP>(S[s][u], y, zw);
                     }
             }
 
@@ -402,9 +408,15 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 :
         } else {
             // ---- row by row
             const RetRows o = rows_out(ch);
+            fetch_z(ch + 1);
+            carry_state<Cfg>(S, Carry{was, 0.0f});
+            owed.none();
+            const Carry one = carry_by(sPw.of[1]);
 #pragma unroll 1
             for (int i = 0; i < n; ++i) {
-                carry_state<Cfg>(S, sD.carry[i == 0 ? e : 1], (m >> i) & 1ull);
+                const bool begin = (m >> i) & 1ull;
+                const Carry by = i == 0 && e == 0 ? Carry{1.0f, 0.0f} : one;
+                each<Cfg>(S, [&](float x, int, int, int) { return begin ? 0.0f : by(x); });
                 const float z = tile_value<Cfg, Cfg::VD>(sZ, i, state_col(L)) * p.z_scale;
                 float sum = 0.0f;
 #pragma unroll
@@ -417,6 +429,7 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 :
                         S[s][k >> 2][k & 3] = __builtin_fmaf(y[k], z, S[s][k >> 2][k & 3]);
                         sum = __builtin_fmaf(x[k], S[s][k >> 2][k & 3], sum);
                     }
+                    __builtin_amdgcn_sched_barrier(0);     // few registers: the next chunk's rows hold theirs
                 }
                 sum += lanes_xor(sum, 16);
                 sum += lanes_xor(sum, 32);
@@ -435,7 +448,7 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 :
         // backwards: the gradient of the state before the tape, one step further
         // back, and none if step 0 begins an episode
         const bool drop = p.rev && start[0] != 0;
-        store_state<Cfg>(S, p.fin + bh * words, p.sk, p.sv, p.x.d, p.z.d, p.rev ? sD.pw[1] : 1.0f, drop, L);
+        store_state<Cfg>(S, p.fin + bh * words, p.sk, p.sv, p.x.d, p.z.d, (p.rev ? sPw.f(1) : 1.0f) * (float)owed.now, drop, L);
     }
 }
 
@@ -453,7 +466,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void ret_sens_kernel(RetSensArgs p
     __shared__ __attribute__((aligned(16))) uint16_t sK[Cfg::NP * Cfg::C * Cfg::KD];
     __shared__ __attribute__((aligned(16))) uint16_t sV[Cfg::NP * Cfg::C * Cfg::VD];
     __shared__ __attribute__((aligned(16))) uint16_t sG[Cfg::NP * Cfg::C * Cfg::VD];
-    __shared__ Decays<Cfg> sD;
+    __shared__ Powers<Cfg::C + 1> sPw;
     __shared__ float sAge[Cfg::C + 16];                    // [16 + n]: n gamma^n scale, 0 for n < 0
     __shared__ __attribute__((aligned(16))) float sW[4][Cfg::C];
     __shared__ uint32_t sBad[Cfg::W];
@@ -461,7 +474,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void ret_sens_kernel(RetSensArgs p
     RetLane L;
     const int64_t seg = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
     const double rate = fabs((double)p.alpha[h]);
-    sD.fill(rate, L.tid);
+    sPw.fill(rate, L.tid);
     if (L.tid < Cfg::C + 16) {
         const int age = L.tid - 16;
         sAge[L.tid] = age < 0 ? 0.0f : decay_pow(rate, age) * (float)age * p.scale;
@@ -471,18 +484,15 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void ret_sens_kernel(RetSensArgs p
                hg = head_of<Cfg>(p.g, b, h, p.T);
     const uint8_t* const start = p.start + b * p.T;
     const int64_t words = (int64_t)kd * vd, bh = b * p.H + h;
-    const int64_t seg0 = seg * p.chunks * Cfg::C;
-    const int64_t left = (p.T - seg0 + Cfg::C - 1) / Cfg::C;
-    const int nch = (int)(left < p.chunks ? left : p.chunks);
+    const int T = (int)p.T, seg0 = (int)seg * p.chunks * Cfg::C;
+    const int left = (T - seg0 + Cfg::C - 1) / Cfg::C, nch = left < p.chunks ? left : p.chunks;
 
     RetTile<Cfg, Cfg::KD> tq, tk;
     RetTile<Cfg, Cfg::VD> tv, tg;
     uint32_t flag;
     auto fetch = [&](int ch) {
         const bool have = ch < nch;
-        const int64_t w0 = have ? seg0 + (int64_t)ch * Cfg::C : 0;
-        const int64_t rest = have ? p.T - w0 : 0;
-        const int n = (int)(rest < Cfg::C ? rest : Cfg::C);
+        const int w0 = have ? seg0 + ch * Cfg::C : 0, rest = have ? T - w0 : 0, n = rest < Cfg::C ? rest : Cfg::C;
         flag = ret_flag(start, w0, n, p.T, false, L.lane);
         tq.fetch(rows_of<Cfg>(hq, w0, n, p.T, false), L);
         tk.fetch(rows_of<Cfg>(hk, w0, n, p.T, false), L);
@@ -494,13 +504,20 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void ret_sens_kernel(RetSensArgs p
     const int64_t at = (bh * (p.nseg - 1) + seg - 1) * words;
     load_state<Cfg>(S, seg == 0 ? (p.seed ? p.seed + bh * words : nullptr) : p.states + at, vd, 1, kd, vd, L);
     load_state<Cfg>(D, seg == 0 ? nullptr : p.dstates + at, vd, 1, kd, vd, L);
+    Owed owed;
+    __syncthreads();                                       // the powers are there
     double sum = 0.0;
 #pragma unroll 1
     for (int ch = 0; ch < nch; ++ch) {
         L.again();
-        const int64_t w0 = seg0 + (int64_t)ch * Cfg::C;
-        const int n = (int)(p.T - w0 < Cfg::C ? p.T - w0 : Cfg::C);
+        const int rest = T - (seg0 + ch * Cfg::C), n = rest < Cfg::C ? rest : Cfg::C;
         const uint64_t m = __ballot(flag != 0u);
+        const float before = uniform((float)owed.now);
+        bool take = false;
+        if (m) owed.none();
+        else take = owed.add(sPw, n);
+        const Carry cy = carry_by(owed.now);
+        if (take) owed.none();
         const uint64_t not_finite = __ballot((tq.bad() | tk.bad() | tv.bad() | tg.bad()) != 0u);
         barrier_lds();                                     // the last operands have been read
         if (L.lane == 0) sBad[L.w] = not_finite != 0;
@@ -511,10 +528,10 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void ret_sens_kernel(RetSensArgs p
         if (L.tid < Cfg::C) {
             const int i = L.tid;
             const int from = m ? last_begin(m) : 0;
-            const float w = i < n && i >= from ? sD.pw[i < n ? n - 1 - i : 0] : 0.0f;
+            const float w = i < n && i >= from ? sPw.f(i < n ? n - 1 - i : 0) * (float)owed.inverse : 0.0f;
             sW[0][i] = w;
             sW[1][i] = w * (float)(n - 1 - i);
-            const float f = i < n && (m & upto(i)) == 0 ? sD.pw[i + 1] * p.scale : 0.0f;
+            const float f = i < n && (m & upto(i)) == 0 ? sPw.f(i + 1) * p.scale * before : 0.0f;
             sW[2][i] = f;
             sW[3][i] = f * (float)(i + 1);
         }
@@ -547,8 +564,8 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void ret_sens_kernel(RetSensArgs p
                 for (int tb = 0; tb < Cfg::C / 32; ++tb) {
                     bf16x8 g[Cfg::NP];
                     col_frag<Cfg, Cfg::VD>(g, sG, tb, state_col_addr(L), L);
-                    weigh<Cfg>(g1[tb], g, sW[2], tb, L);
-                    weigh<Cfg>(g2[tb], g, sW[3], tb, L);
+                    weigh<Cfg, 3>(g1[tb], g, sW[2], tb, L);
+                    weigh<Cfg, 3>(g2[tb], g, sW[3], tb, L);
                 }
 #pragma unroll
                 for (int s = 0; s < Cfg::KS; ++s)
@@ -569,14 +586,14 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void ret_sens_kernel(RetSensArgs p
             }
             // (S, D) after the chunk
             each<Cfg>(D, [&](float x, int s, int u, int e) { return __builtin_fmaf((float)n, S[s][u][e], x); });
-            carry_state<Cfg>(D, sD.carry[n], m != 0);
-            carry_state<Cfg>(S, sD.carry[n], m != 0);
+            settle<Cfg>(D, m != 0, take, cy);
+            settle<Cfg>(S, m != 0, take, cy);
 #pragma unroll
             for (int tb = 0; tb < Cfg::C / 32; ++tb) {
                 bf16x8 z[Cfg::NP], zw[3], zd[3];
                 col_frag<Cfg, Cfg::VD>(z, sV, tb, state_col_addr(L), L);
-                weigh<Cfg>(zw, z, sW[0], tb, L);
-                weigh<Cfg>(zd, z, sW[1], tb, L);
+                weigh<Cfg, 3>(zw, z, sW[0], tb, L);
+                weigh<Cfg, 3>(zd, z, sW[1], tb, L);
 #pragma unroll
                 for (int s = 0; s < Cfg::KS; ++s)
 #pragma unroll
@@ -589,12 +606,15 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void ret_sens_kernel(RetSensArgs p
             }
         } else {
             // ---- row by row
+            carry_state<Cfg>(S, Carry{before, 0.0f});
+            carry_state<Cfg>(D, Carry{before, 0.0f});
+            owed.none();
+            const Carry one = carry_by(sPw.of[1]);
 #pragma unroll 1
             for (int i = 0; i < n; ++i) {
                 const bool begin = (m >> i) & 1ull;
-                each<Cfg>(D, [&](float x, int s, int u, int e) { return x + S[s][u][e]; });
-                carry_state<Cfg>(D, sD.carry[1], begin);
-                carry_state<Cfg>(S, sD.carry[1], begin);
+                each<Cfg>(D, [&](float x, int s, int u, int e) { return begin ? 0.0f : one(x + S[s][u][e]); });
+                each<Cfg>(S, [&](float x, int, int, int) { return begin ? 0.0f : one(x); });
                 const float v = tile_value<Cfg, Cfg::VD>(sV, i, state_col(L));
                 float dot = 0.0f;
 #pragma unroll
@@ -607,6 +627,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void ret_sens_kernel(RetSensArgs p
                         S[s][x >> 2][x & 3] = __builtin_fmaf(k[x], v, S[s][x >> 2][x & 3]);
                         dot = __builtin_fmaf(q[x], D[s][x >> 2][x & 3], dot);
                     }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
                 // (nothing where the row begins: 0 times what is not finite stays out)
                 if (!begin) part = __builtin_fmaf(dot * p.scale, tile_value<Cfg, Cfg::VD>(sG, i, state_col(L)), part);
@@ -619,7 +640,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void ret_sens_kernel(RetSensArgs p
         State<Cfg> G;
         load_state<Cfg>(G, p.grad_state + bh * words, vd, 1, kd, vd, L);
         each<Cfg>(G, [&](float x, int s, int u, int e) {
-            sum += (double)D[s][u][e] * (double)x;
+            sum += (double)D[s][u][e] * (double)x * owed.now;
             return x;
         });
     }
@@ -684,13 +705,26 @@ void with_cfg(int planes, int kd, int vd, F&& f) {
     if (planes == 1) with_tiles<1>(kd, vd, f);
     else with_tiles<3>(kd, vd, f);
 }
+// the planes of z: three, or two where bf16's state stays inside (kernels.hpp)
+template <class Cfg, class F>
+void with_planes(bool exact, F&& f) {
+    if constexpr (Cfg::NP == 1) {
+        if (!exact) {
+            f(std::integral_constant<int, 2>{});
+            return;
+        }
+    }
+    f(std::integral_constant<int, 3>{});
+}
 }  // namespace
 
 hipError_t ret_walk_launch(int planes, const RetWalkArgs& a, int64_t B, hipStream_t s) {
     const dim3 grid((unsigned)a.nseg, (unsigned)a.H, (unsigned)B);
     with_cfg(planes, a.x.d, a.z.d, [&](auto cfg) {
         using Cfg = decltype(cfg);
-        hipLaunchKernelGGL((ret_walk_kernel<Cfg>), grid, dim3(Cfg::THREADS), 0, s, a);
+        with_planes<Cfg>(a.exact, [&](auto zp) {
+            hipLaunchKernelGGL((ret_walk_kernel<Cfg, decltype(zp)::value>), grid, dim3(Cfg::THREADS), 0, s, a);
+        });
     });
     return hipGetLastError();
 }
@@ -700,8 +734,12 @@ hipError_t ret_summary_launch(int planes, const RetSummaryArgs& a, int64_t B, hi
     with_cfg(planes, a.y.d, a.z.d, [&](auto cfg) {
         using Cfg = decltype(cfg);
         const dim3 block(Cfg::THREADS);
-        if (a.dstates) hipLaunchKernelGGL((ret_summary_kernel<Cfg, true>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL((ret_summary_kernel<Cfg, false>), grid, block, 0, s, a);
+        if (a.dstates)
+            hipLaunchKernelGGL((ret_summary_kernel<Cfg, 3, true>), grid, block, 0, s, a);
+        else
+            with_planes<Cfg>(a.exact, [&](auto zp) {
+                hipLaunchKernelGGL((ret_summary_kernel<Cfg, decltype(zp)::value, false>), grid, block, 0, s, a);
+            });
     });
     return hipGetLastError();
 }

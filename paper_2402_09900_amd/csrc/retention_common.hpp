@@ -84,14 +84,14 @@ __device__ __forceinline__ uint32_t pack_hi(float a, float b) {
 }
 __device__ __forceinline__ float cut(float x) { return __uint_as_float(__float_as_uint(x) & 0xFFFF0000u); }
 // Two floats as NPL planes of packed bf16 words.  One plane: rounded to nearest.
-// Three: cut, exact (an infinity leaves NaN in its lower planes: the products
-// are then NaN, not infinite).
+// Two: the rounding error rounded once more, right to 2^-18.  Three: cut, exact (an
+// infinity leaves NaN in its lower planes: the products are then NaN, not infinite).
 template <int NPL>
 __device__ __forceinline__ void planes2(float a, float b, uint32_t (&w)[NPL]) {
-    if constexpr (NPL == 1) {
+    if constexpr (NPL < 3) {
         w[0] = f32x2_to_bf16x2(a, b);
+        if constexpr (NPL == 2) w[1] = f32x2_to_bf16x2(a - __uint_as_float(w[0] << 16), b - cut(__uint_as_float(w[0])));
     } else {
-        static_assert(NPL == 3, "one or three planes");
         w[0] = pack_hi(a, b);
         a -= cut(a);
         b -= cut(b);
@@ -318,23 +318,72 @@ __device__ __forceinline__ void store_state(State<Cfg>& S, float* p, int sk, int
 // gamma^n = exp(-rate n), formed in 64 bits: a slow rate compounds over 1e5
 // steps, where the rounding of a 32-bit gamma^C would show.
 __device__ __forceinline__ float decay_pow(double rate, double n) { return n == 0.0 ? 1.0f : (float)exp(-rate * n); }
+// a value that is the same in all lanes, kept once
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ float uniform(float x) { return __uint_as_float((uint32_t)uniform((int)__float_as_uint(x))); }
+__device__ __forceinline__ double uniform(double x) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(double, (uint64_t)(uint32_t)uniform((int)(uint32_t)b) |
+                                          (uint64_t)(uint32_t)uniform((int)(uint32_t)(b >> 32)) << 32);
+}
 // x -> gamma^n x with gamma^n = hi + lo to 48 bits: a rounded factor near 1 would
-// be off the same way at every chunk
+// be off the same way every time
 struct Carry {
     float hi, lo;
     __device__ __forceinline__ float operator()(float x) const { return __builtin_fmaf(x, lo, x * hi); }
 };
-__device__ __forceinline__ Carry carry_of(double rate, double n) {
-    const double p = n == 0.0 ? 1.0 : exp(-rate * n);
-    return Carry{(float)p, (float)(p - (double)(float)p)};
+__device__ __forceinline__ Carry carry_by(double p) {
+    return Carry{uniform((float)p), uniform((float)(p - (double)(float)p))};
 }
+__device__ __forceinline__ Carry carry_of(double rate, double n) { return carry_by(n == 0.0 ? 1.0 : exp(-rate * n)); }
 template <class Cfg>
-__device__ __forceinline__ void carry_state(State<Cfg>& S, Carry cy, bool drop) {
-    if (drop) zero_state<Cfg>(S);
-    // one set of registers: without this both ways' results are kept apart
+__device__ __forceinline__ void carry_state(State<Cfg>& S, Carry cy) {
+    each<Cfg>(S, [&](float x, int, int, int) { return cy(x); });
+}
+
+// The decay of a walk's state that its registers have not taken yet: state =
+// now S, with what is added divided by `now`.  They take it when it passes 2^-20,
+// which keeps the quotients far from float's range; a slow head almost never
+// does, and none pays 64 instructions a chunk for it.  All in 64 bits.  (A rate
+// that is NaN makes them take it too.)
+struct Owed {
+    double now = 1.0, inverse = 1.0;
+    __device__ __forceinline__ void none() { now = inverse = 1.0; }
+    // n steps of decay more; whether the registers have to take `now`
+    template <class Powers>
+    __device__ __forceinline__ bool add(const Powers& p, int n) {
+        now = uniform(now * p.of[n]);
+        inverse = uniform(inverse * p.inverse[n]);
+        return !(now >= 0x1p-20);
+    }
+};
+// gamma^n and its inverse for n = 0 .. N - 1, in LDS
+template <int N>
+struct Powers {
+    double of[N], inverse[N];
+    __device__ __forceinline__ void fill(double rate, int tid) {
+        if (tid < N) {
+            of[tid] = tid == 0 ? 1.0 : exp(-rate * tid);
+            inverse[tid] = tid == 0 ? 1.0 : exp(rate * tid);
+        }
+    }
+    __device__ __forceinline__ float f(int n) const { return (float)of[n]; }
+};
+
+// What a chunk makes of the state before it: nothing is left where a step begins,
+// else it takes the decay it owes if it has to.  The asm keeps the state in one
+// set of registers; the ways through the branches got one each, and spilled.
+template <class Cfg>
+__device__ __forceinline__ void settle(State<Cfg>& S, bool begins, bool take, Carry cy) {
+    if (begins) zero_state<Cfg>(S);
     each<Cfg>(S, [&](float x, int, int, int) {
         asm volatile("" : "+v"(x));
-        return cy(x);
+        return x;
+    });
+    if (take) carry_state<Cfg>(S, cy);
+    each<Cfg>(S, [&](float x, int, int, int) {
+        asm volatile("" : "+v"(x));
+        return x;
     });
 }
 
