@@ -375,15 +375,17 @@ def memoroid_workspace_prepare(workspace, workspace_bytes, stream) -> int:
 _T = None                   # the torch module, imported on first use
 _CODES = {}                 # torch dtype -> memoroid_dtype
 _raw_stream = None          # device index -> the current stream's hipStream_t
+_current_device = None      # () -> index of the current device
 
 
 def _torch():
-    global _T, _raw_stream
+    global _T, _raw_stream, _current_device
     if _T is None:
         import torch
         _CODES.update({torch.float32: F32, torch.bfloat16: BF16, torch.complex64: C64})
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda index: torch.cuda.current_stream(index).cuda_stream)
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         _T = torch
     return _T
 
@@ -416,6 +418,20 @@ def _check_cuda(*ts):
         elif t.get_device() != index:
             raise ValueError("tensors must live on one device")
     return None if first is None else first.device
+
+
+def _launch(name, dev, *args):
+    """The library's `name` on the device of its tensors and that device's
+    current stream."""
+    fn = getattr(_lib or lib(), name)
+    stream = _raw_stream(dev.index)
+    if _current_device() == dev.index:
+        st = fn(*args, stream)
+    else:
+        with _T.cuda.device(dev):
+            st = fn(*args, stream)
+    if st:
+        _raise(st, name)
 
 
 def _raise(status: int, where: str):
@@ -833,11 +849,9 @@ def scan_retention(q, k, v, alpha, start, scale: Optional[float] = None, state=N
     if T == 0 and final_state:                  # no step: the state stays
         last.zero_() if state is None else last.copy_(state)
     ws = _workspace(lib().memoroid_scan_retention_workspace_bytes(B, T, H, dk, dv, dt), dev, workspace)
-    with torch.cuda.device(dev):
-        st = lib().memoroid_scan_retention(q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(),
-                                           start.data_ptr(), _ptr(state), out.data_ptr(), _ptr(last), scale, B, T, H,
-                                           Hk, dk, dv, dt, ws.data_ptr(), ws.numel(), _stream_ptr(dev))
-    _raise(st, "memoroid_scan_retention")
+    _launch("memoroid_scan_retention", dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(),
+            start.data_ptr(), _ptr(state), out.data_ptr(), _ptr(last), scale, B, T, H, Hk, dk, dv, dt, ws.data_ptr(),
+            ws.numel())
     return (out, last) if final_state else out
 
 
@@ -864,12 +878,9 @@ def scan_retention_bwd(q, k, v, alpha, start, grad_out, scale: Optional[float] =
         return gq, gk, gv, ga, gs
     ws = _workspace(lib().memoroid_scan_retention_bwd_workspace_bytes(B, T, H, Hk, dk, dv, dt, need_grad_alpha), dev,
                     workspace)
-    with torch.cuda.device(dev):
-        st = lib().memoroid_scan_retention_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(),
-                                               start.data_ptr(), _ptr(state), grad_out.data_ptr(), _ptr(grad_state),
-                                               gq.data_ptr(), gk.data_ptr(), gv.data_ptr(), _ptr(ga), _ptr(gs), scale,
-                                               B, T, H, Hk, dk, dv, dt, ws.data_ptr(), ws.numel(), _stream_ptr(dev))
-    _raise(st, "memoroid_scan_retention_bwd")
+    _launch("memoroid_scan_retention_bwd", dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(),
+            start.data_ptr(), _ptr(state), grad_out.data_ptr(), _ptr(grad_state), gq.data_ptr(), gk.data_ptr(),
+            gv.data_ptr(), _ptr(ga), _ptr(gs), scale, B, T, H, Hk, dk, dv, dt, ws.data_ptr(), ws.numel())
     return gq, gk, gv, ga, gs
 
 
@@ -884,11 +895,8 @@ def retention_step(q, k, v, alpha, state, start=None, scale: Optional[float] = N
     _state_like(state, "state", B, H, dk, dv)
     dev = _check_cuda(q, k, v, alpha, start, state)
     out = torch.empty((B, H, dv), dtype=q.dtype, device=dev)
-    with torch.cuda.device(dev):
-        st = lib().memoroid_retention_step(q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(), _ptr(start),
-                                           state.data_ptr(), out.data_ptr(), scale, B, H, Hk, dk, dv, dt,
-                                           _stream_ptr(dev))
-    _raise(st, "memoroid_retention_step")
+    _launch("memoroid_retention_step", dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(), _ptr(start),
+            state.data_ptr(), out.data_ptr(), scale, B, H, Hk, dk, dv, dt)
     return out
 
 
@@ -953,11 +961,8 @@ def rotate_qk(q, k, positions, freq, wq=None, wk=None, eps: float = 1e-6, interl
     dev = _check_cuda(q, k, positions, freq, wq, wk)
     qo = torch.empty_like(q)
     ko = None if k is None else torch.empty_like(k)
-    with torch.cuda.device(dev):
-        st = lib().memoroid_rotate_qk(q.data_ptr(), _ptr(k), _ptr(positions), _ptr(freq), _ptr(wq), _ptr(wk),
-                                      qo.data_ptr(), _ptr(ko), eps, amplitude, interleaved, n, H, Hk, d, rot, dt,
-                                      _stream_ptr(dev))
-    _raise(st, "memoroid_rotate_qk")
+    _launch("memoroid_rotate_qk", dev, q.data_ptr(), _ptr(k), _ptr(positions), _ptr(freq), _ptr(wq), _ptr(wk),
+            qo.data_ptr(), _ptr(ko), eps, amplitude, interleaved, n, H, Hk, d, rot, dt)
     return qo, ko
 
 
@@ -978,12 +983,9 @@ def rotate_qk_bwd(q, k, positions, freq, grad_q, grad_k, wq=None, wk=None, eps: 
     ws = None
     if gwq is not None or gwk is not None:
         ws = _workspace(lib().memoroid_rotate_qk_bwd_workspace_bytes(n, H, Hk, d, rot, interleaved, dt), dev, workspace)
-    with torch.cuda.device(dev):
-        st = lib().memoroid_rotate_qk_bwd(q.data_ptr(), _ptr(k), _ptr(positions), _ptr(freq), _ptr(wq), _ptr(wk),
-                                          grad_q.data_ptr(), _ptr(grad_k), gq.data_ptr(), _ptr(gk), _ptr(gwq), _ptr(gwk),
-                                          eps, amplitude, interleaved, n, H, Hk, d, rot, dt, _ptr(ws),
-                                          0 if ws is None else ws.numel(), _stream_ptr(dev))
-    _raise(st, "memoroid_rotate_qk_bwd")
+    _launch("memoroid_rotate_qk_bwd", dev, q.data_ptr(), _ptr(k), _ptr(positions), _ptr(freq), _ptr(wq), _ptr(wk),
+            grad_q.data_ptr(), _ptr(grad_k), gq.data_ptr(), _ptr(gk), _ptr(gwq), _ptr(gwk), eps, amplitude,
+            interleaved, n, H, Hk, d, rot, dt, _ptr(ws), 0 if ws is None else ws.numel())
     return gq, gk, gwq, gwk
 
 

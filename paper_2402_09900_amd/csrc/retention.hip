@@ -171,14 +171,13 @@ __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummary
 // ---------------------------------------------------------------- state scan
 // states[i] becomes the state after segment i: its summary, plus gamma^rows times
 // the state before it where it holds no begin step; with DOT the derivative
-// likewise, d' = own + gamma^rows (d + rows s).  A workgroup takes one 128-byte
-// line of the states (8 16-byte columns) and all segments, 32 RPT of them at a
-// time: thread (grp, col) holds RPT consecutive segments of a column in registers,
-// the 32 groups combine through LDS.  One read and one write of the states, all
-// loads in flight at once (one segment after the other took 39 us for 128 segments
-// of 4 heads of 64 x 64).
-constexpr int kRetScanCols = 8, kRetScanGroups = 32;
-
+// likewise, d' = own + gamma^rows (d + rows s).  GROUPS threads share a 16-byte
+// column of the states, each with RPT consecutive segments of it in registers, all
+// loads in flight at once; the groups combine through LDS.  One read and one write
+// of the states.  One group where there are few segments or many columns (3
+// segments of 128 heads of 128 x 128: 10 us, 294 us in 32 groups; 31 segments of 16
+// such heads: 16 and 53 us), else 32 (128 segments of 4 heads of 64 x 64: 8 us, 39 us
+// one segment after the other).
 template <bool DOT>
 struct SegState {
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f}, d = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -192,14 +191,14 @@ struct SegState {
     }
 };
 
-template <int RPT, bool DOT>
+template <int GROUPS, int RPT, bool DOT>
 __global__ __launch_bounds__(256) void ret_state_scan_kernel(RetStateScanArgs p) {
-    __shared__ f32x4 sTot[DOT ? 2 : 1][kRetScanGroups][kRetScanCols];
-    __shared__ uint32_t sFlag[kRetScanGroups];
-    constexpr int kTile = kRetScanGroups * RPT;
-    const int col = threadIdx.x % kRetScanCols, grp = threadIdx.x / kRetScanCols;
+    constexpr int kCols = 256 / GROUPS, kTile = GROUPS * RPT;
+    __shared__ f32x4 sTot[GROUPS > 1 && DOT ? 2 : 1][GROUPS][GROUPS > 1 ? kCols : 1];
+    __shared__ uint32_t sFlag[GROUPS];
+    const int col = threadIdx.x % kCols, grp = threadIdx.x / kCols;
     const int64_t h = blockIdx.y, b = blockIdx.z, bh = b * p.H + h;
-    const int c4 = (int)blockIdx.x * kRetScanCols + col, w4 = p.words / 4;   // words is a multiple of 64
+    const int c4 = (int)blockIdx.x * kCols + col, w4 = p.words / 4;   // words is a multiple of 64
     const bool in = c4 < w4;
     const double rate = fabs((double)p.alpha[h]), rows = (double)p.rows;
     const Carry one = carry_of(rate, rows), many = carry_of(rate, rows * RPT);
@@ -222,24 +221,26 @@ __global__ __launch_bounds__(256) void ret_state_scan_kernel(RetStateScanArgs p)
             if (DOT) y[DOT ? i : 0] = have ? D[(int64_t)l * w4] : zero;
             fl[i] = l < p.n && R[l < p.n ? l : 0] != 0;
         }
-        SegState<DOT> tot;
-        bool any = false;
-#pragma unroll
-        for (int i = 0; i < RPT; ++i) {
-            tot.then(x[i], y[DOT ? i : 0], fl[i], one, (float)p.rows);
-            any |= fl[i];
-        }
-        __syncthreads();                                   // the last tile's totals have been read
-        sTot[0][grp][col] = tot.s;
-        if (DOT) sTot[DOT ? 1 : 0][grp][col] = tot.d;
-        if (col == 0) sFlag[grp] = any;
-        __syncthreads();
         SegState<DOT> mine = before;                       // the state before this thread's run
+        if constexpr (GROUPS > 1) {
+            SegState<DOT> tot;
+            bool any = false;
+#pragma unroll
+            for (int i = 0; i < RPT; ++i) {
+                tot.then(x[i], y[DOT ? i : 0], fl[i], one, (float)p.rows);
+                any |= fl[i];
+            }
+            __syncthreads();                               // the last tile's totals have been read
+            sTot[0][grp][col] = tot.s;
+            if (DOT) sTot[DOT ? 1 : 0][grp][col] = tot.d;
+            if (col == 0) sFlag[grp] = any;
+            __syncthreads();
 #pragma unroll 4
-        for (int k = 0; k < kRetScanGroups; ++k) {
-            if (k == grp) mine = before;
-            before.then(sTot[0][k][col], sTot[DOT ? 1 : 0][k][col], sFlag[k] != 0u, base == 0 && k == 0 ? many0 : many,
-                        (float)p.rows * RPT);
+            for (int k = 0; k < GROUPS; ++k) {
+                if (k == grp) mine = before;
+                before.then(sTot[0][k][col], sTot[DOT ? 1 : 0][k][col], sFlag[k] != 0u, base == 0 && k == 0 ? many0 : many,
+                            (float)p.rows * RPT);
+            }
         }
 #pragma unroll
         for (int i = 0; i < RPT; ++i) {
@@ -250,6 +251,7 @@ __global__ __launch_bounds__(256) void ret_state_scan_kernel(RetStateScanArgs p)
                 if (DOT) D[(int64_t)l * w4] = mine.d;
             }
         }
+        if constexpr (GROUPS == 1) before = mine;
     }
 }
 
@@ -805,20 +807,25 @@ hipError_t ret_summary_launch(int planes, const RetSummaryArgs& a, int64_t B, hi
 }
 
 namespace {
+template <int GROUPS, int RPT, bool DOT>
+void state_scan(const RetStateScanArgs& a, int64_t B, hipStream_t s) {
+    constexpr int kCols = 256 / GROUPS;
+    const dim3 grid((unsigned)((a.words / 4 + kCols - 1) / kCols), (unsigned)a.H, (unsigned)B);
+    hipLaunchKernelGGL((ret_state_scan_kernel<GROUPS, RPT, DOT>), grid, dim3(256), 0, s, a);
+}
 template <bool DOT>
-void state_scan(const RetStateScanArgs& a, dim3 grid, hipStream_t s) {
-    const dim3 block(256);
-    // the fewest segments per thread that take all at once
-    if (a.n <= kRetScanGroups) hipLaunchKernelGGL((ret_state_scan_kernel<1, DOT>), grid, block, 0, s, a);
-    else if (a.n <= 2 * kRetScanGroups) hipLaunchKernelGGL((ret_state_scan_kernel<2, DOT>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((ret_state_scan_kernel<4, DOT>), grid, block, 0, s, a);
+void state_scan_for(const RetStateScanArgs& a, int64_t B, hipStream_t s) {
+    const int64_t columns = B * a.H * (a.words / 4);
+    if (a.n <= 4) state_scan<1, 4, DOT>(a, B, s);
+    else if (a.n <= 16 || columns >= 16384) state_scan<1, 16, DOT>(a, B, s);
+    else if (a.n <= 64) state_scan<32, 2, DOT>(a, B, s);
+    else state_scan<32, 4, DOT>(a, B, s);
 }
 }  // namespace
 
 hipError_t ret_state_scan_launch(const RetStateScanArgs& a, int64_t B, hipStream_t s) {
-    const dim3 grid((unsigned)((a.words / 4 + kRetScanCols - 1) / kRetScanCols), (unsigned)a.H, (unsigned)B);
-    if (a.dstates) state_scan<true>(a, grid, s);
-    else state_scan<false>(a, grid, s);
+    if (a.dstates) state_scan_for<true>(a, B, s);
+    else state_scan_for<false>(a, B, s);
     return hipGetLastError();
 }
 
