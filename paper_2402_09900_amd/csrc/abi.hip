@@ -934,40 +934,51 @@ bool ret_dims_ok(int64_t dk, int64_t dv) {
 bool ret_extents_ok(int64_t B, int64_t T, int64_t H) { return B <= 65535 && H <= 65535 && T <= (int64_t)INT32_MAX / 2; }
 int ret_planes(int dtype) { return dtype == MEMOROID_BF16 ? 1 : dtype == MEMOROID_F32 ? 3 : 0; }
 
-// The segment states of one direction: [B][H][nseg - 1][dk][dv] floats, flags.
+// One array of segment states: [B][H][nseg][dk][dv] floats
 size_t ret_states_bytes(const RetPlan& p, int64_t B, int64_t H, int64_t dk, int64_t dv) {
-    return align_up((size_t)B * (size_t)H * (size_t)(p.nseg - 1) * (size_t)(dk * dv) * 4);
+    return align_up((size_t)B * (size_t)H * (size_t)p.nseg * (size_t)(dk * dv) * 4);
 }
 
 bool plan_retention(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv, int planes, RetPlan* p) {
     ret_segments(B, T, H, planes, p);
     size_t off = kAlign;                                   // header
     p->off_states = off;
-    off += ret_states_bytes(*p, B, H, dk, dv);
+    if (p->nseg > 1) off += ret_states_bytes(*p, B, H, dk, dv);
     p->off_R = off;
-    off = align_up(off + (size_t)B * (size_t)(p->nseg - 1));
+    off = align_up(off + (size_t)B * (size_t)p->nseg);
     p->total = off;
     return true;
 }
 
 struct RetBwdPlan {
     RetPlan fwd;
-    size_t off_dstates = 0, off_rstates = 0, off_rR = 0, off_part = 0, off_gk = 0, off_gv = 0, total = 0;
+    int64_t nparts = 0;
+    bool prep = false;           // a pass for the segments' states or the rates' gradient
+    size_t off_states = 0, off_rstates = 0, off_dstates = 0, off_estates = 0, off_R = 0, off_bad = 0, off_part = 0,
+           off_gk = 0, off_gv = 0, total = 0;
 };
 
 bool plan_retention_bwd(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t dk, int64_t dv, int planes, bool want_alpha,
                         RetBwdPlan* p) {
-    if (!plan_retention(B, T, H, dk, dv, planes, &p->fwd)) return false;
+    ret_segments(B, T, H, planes, &p->fwd);
     const size_t states = ret_states_bytes(p->fwd, B, H, dk, dv);
-    size_t off = p->fwd.total;
+    p->nparts = p->fwd.nseg + ret_scan_parts(dk * dv, B * H, p->fwd.nseg);
+    p->prep = want_alpha || p->fwd.nseg > 1;
+    size_t off = kAlign;                                   // header
+    p->off_states = off;
+    if (p->prep) off += states;
     p->off_rstates = off;
-    off += states;
-    p->off_rR = off;
-    off = align_up(off + (size_t)B * (size_t)(p->fwd.nseg - 1));
+    if (p->prep) off += states;
     p->off_dstates = off;
     if (want_alpha) off += states;
+    p->off_estates = off;
+    if (want_alpha) off += states;
+    p->off_R = off;
+    off = align_up(off + (size_t)B * (size_t)p->fwd.nseg);
+    p->off_bad = off;
+    if (want_alpha) off = align_up(off + (size_t)B * (size_t)H * (size_t)p->fwd.nseg);
     p->off_part = off;
-    if (want_alpha) off = align_up(off + (size_t)B * (size_t)H * (size_t)p->fwd.nseg * 8);
+    if (want_alpha) off = align_up(off + (size_t)B * (size_t)H * (size_t)p->nparts * 8);
     p->off_gk = off;                                       // shared heads: gradients per query head
     if (Hk != H) off = align_up(off + (size_t)B * (size_t)T * (size_t)H * (size_t)dk * 4);
     p->off_gv = off;
@@ -978,42 +989,6 @@ bool plan_retention_bwd(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t dk,
 
 RetRole ret_role(const void* p, int64_t heads, int64_t d, int64_t share) {
     return RetRole{p, (int32_t)heads, (int32_t)d, (int32_t)share};
-}
-
-// Segment states of one direction, scanned.
-int ret_states(const RetPlan& p, RetRole y, RetRole z, const uint8_t* start, const float* alpha, const float* seed,
-               float* states, float* dstates, uint8_t* R, float z_scale, int64_t B, int64_t T, int64_t H, bool rev,
-               bool exact, WsHeader* hdr, uint64_t sig, hipStream_t s) {
-    RetSummaryArgs a{};
-    a.y = y;
-    a.z = z;
-    a.start = start;
-    a.alpha = alpha;
-    a.states = states;
-    a.dstates = dstates;
-    a.R = R;
-    a.z_scale = z_scale;
-    a.T = T;
-    a.H = (int32_t)H;
-    a.nseg = p.nseg;
-    a.chunks = p.chunks;
-    a.rev = rev;
-    a.exact = exact;
-    a.hdr = hdr;
-    a.sig = sig;
-    if (ret_summary_launch(p.planes, a, B, s) != hipSuccess) return MEMOROID_EHIP;
-    RetStateScanArgs c{};
-    c.alpha = alpha;
-    c.seed = seed;
-    c.states = states;
-    c.dstates = dstates;
-    c.R = R;
-    c.rows = p.rows;
-    c.words = y.d * z.d;
-    c.H = (int32_t)H;
-    c.n = p.nseg - 1;
-    c.rev = rev;
-    return check_hip(ret_state_scan_launch(c, B, s));
 }
 
 // Argument checks that the retention entry points share; MEMOROID_OK and *empty
@@ -1087,9 +1062,32 @@ int memoroid_scan_retention(const void* q, const void* k, const void* v, const f
     const RetRole rk = ret_role(k, Hk, dk, G), rv = ret_role(v, Hk, dv, G);
     float* const states = (float*)(ws + p.off_states);
     if (p.nseg > 1) {
-        const int st = ret_states(p, rk, rv, start, alpha, state_in, states, nullptr, (uint8_t*)(ws + p.off_R), 1.0f, B,
-                                  T, H, false, state_out != nullptr, (WsHeader*)ws, sig, s);
-        if (st != MEMOROID_OK) return st;
+        RetSummaryArgs m{};
+        m.y = rk;
+        m.z = rv;
+        m.start = start;
+        m.alpha = alpha;
+        m.states = states;
+        m.R = (uint8_t*)(ws + p.off_R);
+        m.T = T;
+        m.H = (int32_t)H;
+        m.nseg = p.nseg;
+        m.chunks = p.chunks;
+        m.exact = state_out != nullptr;
+        m.hdr = (WsHeader*)ws;
+        m.sig = sig;
+        if (ret_summary_launch(p.planes, m, B, s) != hipSuccess) return MEMOROID_EHIP;
+        RetStateScanArgs c{};
+        c.alpha = alpha;
+        c.seed = state_in;
+        c.states = states;
+        c.R = m.R;
+        c.rows = p.rows;
+        c.last_rows = T - (int64_t)(p.nseg - 1) * p.rows;
+        c.words = (int32_t)(dk * dv);
+        c.H = (int32_t)H;
+        c.nseg = p.nseg;
+        if (ret_state_scan_launch(c, B, s) != hipSuccess) return MEMOROID_EHIP;
     }
     RetWalkArgs a{};
     a.x = ret_role(q, H, dk, 1);
@@ -1155,37 +1153,61 @@ int memoroid_scan_retention_bwd(const void* q, const void* k, const void* v, con
     const int64_t G = H / Hk;
     const RetRole rq = ret_role(q, H, dk, 1), rk = ret_role(k, Hk, dk, G), rv = ret_role(v, Hk, dv, G),
                   rg = ret_role(grad_out, H, dv, 1);
-    float* const states = (float*)(ws + p.off_states);
-    float* const dstates = (float*)(ws + bp.off_dstates);
+    float* const states = (float*)(ws + bp.off_states);
     float* const rstates = (float*)(ws + bp.off_rstates);
-    if (p.nseg > 1) {
-        int st = ret_states(p, rk, rv, start, alpha, state_in, states, grad_alpha ? dstates : nullptr,
-                            (uint8_t*)(ws + p.off_R), 1.0f, B, T, H, false, grad_alpha != nullptr, (WsHeader*)ws, sig, s);
-        if (st != MEMOROID_OK) return st;
-        st = ret_states(p, rq, rg, start, alpha, grad_state_out, rstates, nullptr, (uint8_t*)(ws + bp.off_rR), scale, B,
-                        T, H, true, grad_state_in != nullptr, nullptr, 0, s);
-        if (st != MEMOROID_OK) return st;
-    }
-    if (grad_alpha) {
-        RetSensArgs a{};
-        a.q = rq;
-        a.k = rk;
-        a.v = rv;
-        a.g = rg;
-        a.start = start;
-        a.alpha = alpha;
-        a.seed = state_in;
-        a.grad_state = grad_state_out;
-        a.states = states;
-        a.dstates = dstates;
-        a.part = (double*)(ws + bp.off_part);
-        a.scale = scale;
-        a.T = T;
-        a.H = (int32_t)H;
-        a.nseg = p.nseg;
-        a.chunks = p.chunks;
-        if (ret_sens_launch(p.planes, a, B, s) != hipSuccess) return MEMOROID_EHIP;
-        if (ret_alpha_launch(a.part, alpha, grad_alpha, B, (int32_t)H, p.nseg, s) != hipSuccess) return MEMOROID_EHIP;
+    if (bp.prep) {
+        RetPrepArgs m{};
+        m.q = rq;
+        m.k = rk;
+        m.v = rv;
+        m.g = rg;
+        m.start = start;
+        m.alpha = alpha;
+        m.states = states;
+        m.rstates = rstates;
+        m.dstates = grad_alpha ? (float*)(ws + bp.off_dstates) : nullptr;
+        m.estates = (float*)(ws + bp.off_estates);
+        m.part = (double*)(ws + bp.off_part);
+        m.R = (uint8_t*)(ws + bp.off_R);
+        m.bad = (uint8_t*)(ws + bp.off_bad);
+        m.scale = scale;
+        m.T = T;
+        m.H = (int32_t)H;
+        m.nseg = p.nseg;
+        m.chunks = p.chunks;
+        m.nparts = (int32_t)bp.nparts;
+        m.exact = grad_state_in != nullptr;
+        m.hdr = (WsHeader*)ws;
+        m.sig = sig;
+        if (ret_prep_launch(p.planes, m, B, s) != hipSuccess) return MEMOROID_EHIP;
+        RetStateScanArgs c{};
+        c.alpha = alpha;
+        c.R = m.R;
+        c.rows = p.rows;
+        c.last_rows = T - (int64_t)(p.nseg - 1) * p.rows;
+        c.words = (int32_t)(dk * dv);
+        c.H = (int32_t)H;
+        c.nseg = p.nseg;
+        // forwards first: it reads U before the scan backwards replaces it
+        c.seed = state_in;
+        c.states = states;
+        c.dstates = m.dstates;
+        c.rstates = rstates;
+        c.estates = m.estates;
+        c.grad_state = grad_state_out;
+        c.part = m.part;
+        c.nparts = m.nparts;
+        if (ret_state_scan_launch(c, B, s) != hipSuccess) return MEMOROID_EHIP;
+        if (grad_alpha &&
+            ret_alpha_launch(m.part, alpha, grad_alpha, B, (int32_t)H, m.nparts, s) != hipSuccess)
+            return MEMOROID_EHIP;
+        if (p.nseg > 1) {
+            c.rev = 1;
+            c.seed = grad_state_out;
+            c.states = rstates;
+            c.dstates = nullptr;
+            if (ret_state_scan_launch(c, B, s) != hipSuccess) return MEMOROID_EHIP;
+        }
     }
     RetWalkArgs a{};
     a.start = start;
@@ -1206,7 +1228,7 @@ int memoroid_scan_retention_bwd(const void* q, const void* k, const void* v, con
     a.sv = (int32_t)dv;
     a.inter_scale = scale;
     a.z_scale = 1.0f;
-    if (p.nseg == 1) {
+    if (!bp.prep) {
         a.hdr = (WsHeader*)ws;
         a.sig = sig;
     }

@@ -302,8 +302,12 @@ struct RetRole {
     int32_t heads, d, share;
 };
 
-// W(x, y, z) over B tapes and H heads, in segments of `chunks` chunks (segment
-// states by RetSummaryArgs and RetStateScanArgs; one segment needs none).
+// Begin steps of a segment: any; any after its first step, or at the step that
+// follows it (backwards); its first step
+constexpr uint32_t kSegBegins = 1, kSegBeginsBack = 2, kSegBeginsFirst = 4;
+
+// W(x, y, z) over B tapes and H heads, in segments of `chunks` chunks.  States of
+// segments are [B][H][nseg][rows][columns]; one segment needs none.
 struct RetWalkArgs {
     RetRole x, y, z;            // z.d columns of output, x.d == y.d rows of state
     const uint8_t* start;       // [B][T]
@@ -311,7 +315,7 @@ struct RetWalkArgs {
     void* out;                  // [B][T][H][z.d]
     int32_t out_f32;            // floats out although the inputs are bf16
     const float* seed;          // state before the walk [B][H][dk][dv], or NULL
-    const float* states;        // [B][H][nseg - 1][dk][dv]: state after each segment but the last
+    const float* states;        // scanned: the state after each segment (in walking order)
     float* fin;                 // state after the walk out, or NULL
     int32_t sk, sv;             // strides of a state's rows and columns (x.d x z.d) in those arrays
     float p_scale, inter_scale, z_scale;   // of pairs, of the carried state, into the state
@@ -322,17 +326,35 @@ struct RetWalkArgs {
     WsHeader* hdr;              // header to prepare with sig, or NULL
     uint64_t sig;
 };
+// what the segments but the last add to the state
 struct RetSummaryArgs {
     RetRole y, z;
     const uint8_t* start;
     const float* alpha;
-    float* states;              // [B][H][nseg - 1][y.d][z.d]
-    float* dstates;             // their derivatives by log gamma, or NULL
-    uint8_t* R;                 // [B][nseg - 1] segment holds a begin step
-    float z_scale;
+    float* states;
+    uint8_t* R;                 // [B][nseg] begin steps
     int64_t T;
-    int32_t H, nseg, chunks, rev;
-    int32_t exact;              // as in RetWalkArgs (always so with dstates)
+    int32_t H, nseg, chunks;
+    int32_t exact;              // as in RetWalkArgs
+    WsHeader* hdr;
+    uint64_t sig;
+};
+// what the gradient needs of every segment (retention.hip)
+struct RetPrepArgs {
+    RetRole q, k, v, g;
+    const uint8_t* start;
+    const float* alpha;
+    float* states;              // S
+    float* rstates;             // U
+    float* dstates;             // D and E: NULL where the rates' gradient is not asked for
+    float* estates;
+    double* part;               // [B][H][nparts], a segment's own share first
+    uint8_t* R;
+    uint8_t* bad;               // [B][H][nseg] a segment holds a value that is not finite
+    float scale;
+    int64_t T;
+    int32_t H, nseg, chunks, nparts;
+    int32_t exact;
     WsHeader* hdr;
     uint64_t sig;
 };
@@ -341,30 +363,22 @@ struct RetStateScanArgs {
     const float* seed;          // as in RetWalkArgs
     float* states;              // scanned in place
     float* dstates;             // likewise, or NULL
+    const float* rstates;       // with dstates: U and E, for
+    const float* estates;
+    const float* grad_state;    // (optional)
+    double* part;               // the states' shares of the rates' gradient, from nseg on
     const uint8_t* R;
-    int64_t rows;               // steps of a segment
-    int32_t words, H, n, rev;   // floats of a state; n = nseg - 1 segments
-};
-// dL/dlog gamma: the derivative state against q dout^T
-struct RetSensArgs {
-    RetRole q, k, v, g;
-    const uint8_t* start;
-    const float* alpha;
-    const float* seed;          // carried state, or NULL
-    const float* grad_state;    // gradient of the state after the tape, or NULL
-    const float* states;        // scanned, as in RetWalkArgs
-    const float* dstates;
-    double* part;               // [B][H][nseg]
-    float scale;
-    int64_t T;
-    int32_t H, nseg, chunks;
+    int64_t rows, last_rows;    // steps of a segment, of the last one
+    int32_t words, H, nseg, nparts, rev;   // floats of a state
 };
 hipError_t ret_walk_launch(int planes, const RetWalkArgs& a, int64_t B, hipStream_t s);
 hipError_t ret_summary_launch(int planes, const RetSummaryArgs& a, int64_t B, hipStream_t s);
 hipError_t ret_state_scan_launch(const RetStateScanArgs& a, int64_t B, hipStream_t s);
-hipError_t ret_sens_launch(int planes, const RetSensArgs& a, int64_t B, hipStream_t s);
-// grad_alpha[h] = -sign(alpha_h) sum of part over tapes and segments
-hipError_t ret_alpha_launch(const double* part, const float* alpha, float* out, int64_t B, int32_t H, int32_t nseg,
+hipError_t ret_prep_launch(int planes, const RetPrepArgs& a, int64_t B, hipStream_t s);
+// workgroups of a state scan per head
+int64_t ret_scan_parts(int64_t words, int64_t heads, int64_t nseg);
+// grad_alpha[h] = -sign(alpha_h) sum of part over tapes
+hipError_t ret_alpha_launch(const double* part, const float* alpha, float* out, int64_t B, int32_t H, int32_t nparts,
                             hipStream_t s);
 // out[row][kh][.] = sum of part[row][kh G + 0 .. G - 1][.], rounded to bf16 if planes == 1
 hipError_t ret_share_launch(int planes, const float* part, void* out, int64_t rows, int32_t heads, int32_t G, int32_t d,

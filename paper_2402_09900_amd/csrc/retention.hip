@@ -46,9 +46,27 @@ __device__ __forceinline__ Head head_of(const RetRole& x, int64_t b, int64_t h, 
     return Head{(const char*)x.p + (b * T * x.heads + h / x.share) * x.d * Cfg::ES, (int64_t)x.heads * x.d * Cfg::ES, x.d};
 }
 template <class Cfg>
-__device__ __forceinline__ RetRows rows_of(const Head& x, int64_t w0, int n, int64_t T, bool rev) {
-    return ret_rows(x.p, x.row_bytes, x.d, Cfg::ES, w0, n, T, rev);
+__device__ __forceinline__ RetRows rows_of(const Head& x, int t0, int n, bool rev = false) {
+    return ret_rows(x.p, x.row_bytes, x.d, Cfg::ES, t0, n, rev);
 }
+// A workgroup's run of chunks: steps r0 .. r1 - 1, in chunks of C from r0 on or,
+// backwards, from r1 - 1 on; the last of them may be short.
+template <class Cfg>
+struct Run {
+    int r0, r1, nch, rev;
+    __device__ Run(int seg, int chunks, int T, int rev_) : r0(seg * chunks * Cfg::C), rev(rev_) {
+        const int all = chunks * Cfg::C;
+        r1 = T - r0 < all ? T : r0 + all;
+        nch = (r1 - r0 + Cfg::C - 1) / Cfg::C;
+    }
+    __device__ __forceinline__ int rows(int ch) const {    // none past the run
+        const int left = ch < nch ? r1 - r0 - ch * Cfg::C : 0;
+        return left < Cfg::C ? left : Cfg::C;
+    }
+    __device__ __forceinline__ int first(int ch) const {   // the chunk's first step
+        return ch >= nch ? r0 : rev ? r1 - ch * Cfg::C - rows(ch) : r0 + ch * Cfg::C;
+    }
+};
 
 // the value operand times a weight per row, in planes
 template <class Cfg, int ZP>
@@ -82,13 +100,13 @@ __device__ __forceinline__ f32x4 pair_products(const uint16_t* sY, const uint16_
 
 // ---------------------------------------------------------------- summaries
 // What a segment adds to the state after it: the sum over its rows from the last
-// begin on.  DOT: also its derivative by log gamma, sum (n-1-j) gamma^(n-1-j) y^T z.
-template <class Cfg, int ZP, bool DOT>
+// begin on.
+template <class Cfg, int ZP>
 __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummaryArgs p) {
     __shared__ __attribute__((aligned(16))) uint16_t sY[Cfg::NP * Cfg::C * Cfg::KD];
     __shared__ __attribute__((aligned(16))) uint16_t sZ[Cfg::NP * Cfg::C * Cfg::VD];
     __shared__ Powers<Cfg::C + 1> sPw;
-    __shared__ __attribute__((aligned(16))) float sW[DOT ? 2 : 1][Cfg::C];
+    __shared__ __attribute__((aligned(16))) float sW[Cfg::C];
     RetLane L;
     const int64_t seg = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
     ret_header(p.hdr, p.sig);
@@ -96,27 +114,24 @@ __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummary
     sPw.fill(rate, L.tid);
     const Head hy = head_of<Cfg>(p.y, b, h, p.T), hz = head_of<Cfg>(p.z, b, h, p.T);
     const uint8_t* const start = p.start + b * p.T;
-    State<Cfg> S, D;
+    const Run<Cfg> run((int)seg, p.chunks, (int)p.T, 0);  // a whole segment: the last has no summary
+    State<Cfg> S;
     zero_state<Cfg>(S);
-    if (DOT) zero_state<Cfg>(D);
     Owed owed;
     __syncthreads();                                       // the powers are there
     bool any = false;
     RetTile<Cfg, Cfg::KD> ty;
     RetTile<Cfg, Cfg::VD> tz;
     uint32_t flag;
-    // every segment here is a whole one: C rows per chunk (the last fetch, of a
-    // chunk that is not there, reads nothing)
     auto fetch = [&](int ch) {
-        const bool have = ch < p.chunks;
-        const int w0 = have ? ((int)seg * p.chunks + ch) * Cfg::C : 0, n = have ? Cfg::C : 0;
-        flag = ret_flag(start, w0, n, p.T, p.rev, L.lane);
-        ty.fetch(rows_of<Cfg>(hy, w0, n, p.T, p.rev), L);
-        tz.fetch(rows_of<Cfg>(hz, w0, n, p.T, p.rev), L);
+        const int t0 = run.first(ch), n = run.rows(ch);
+        flag = ret_flag(start, t0, n, (int)p.T, false, L.lane);
+        ty.fetch(rows_of<Cfg>(hy, t0, n), L);
+        tz.fetch(rows_of<Cfg>(hz, t0, n), L);
     };
     fetch(0);
 #pragma unroll 1
-    for (int ch = 0; ch < p.chunks; ++ch) {
+    for (int ch = 0; ch < run.nch; ++ch) {
         L.again();
         const uint64_t m = __ballot(flag != 0u);
         const int from = m ? last_begin(m) : 0;
@@ -126,29 +141,23 @@ __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummary
         else take = owed.add(sPw, Cfg::C);
         const Carry cy = carry_by(owed.now);
         if (take) owed.none();
-        barrier_lds();                                     // the last chunk's operands have been read
-        ty.stage(sY, from, L);
-        tz.stage(sZ, from, L);
-        if (L.tid < Cfg::C) {
-            const int age = Cfg::C - 1 - L.tid;
-            const float w = L.tid >= from ? sPw.f(age) * p.z_scale * (float)owed.inverse : 0.0f;
-            sW[0][L.tid] = w;
-            if (DOT) sW[DOT ? 1 : 0][L.tid] = w * (float)age;
+        if (m) {
+            ty.keep(from, Cfg::C, L);
+            tz.keep(from, Cfg::C, L);
         }
+        barrier_lds();                                     // the last chunk's operands have been read
+        ty.stage(sY, L);
+        tz.stage(sZ, L);
+        if (L.tid < Cfg::C)
+            sW[L.tid] = L.tid >= from ? sPw.f(Cfg::C - 1 - L.tid) * (float)owed.inverse : 0.0f;
         fetch(ch + 1);
         barrier_lds();
-        // d(gamma^C S)/dlog gamma = gamma^C (D + C S)
-        if (DOT) {
-            each<Cfg>(D, [&](float x, int s, int u, int e) { return __builtin_fmaf((float)Cfg::C, S[s][u][e], x); });
-            settle<Cfg>(D, m != 0, take, cy);
-        }
         settle<Cfg>(S, m != 0, take, cy);
 #pragma unroll
         for (int tb = 0; tb < Cfg::C / 32; ++tb) {
-            bf16x8 z[Cfg::NP], zw[ZP], zd[ZP];
+            bf16x8 z[Cfg::NP], zw[ZP];
             col_frag<Cfg, Cfg::VD>(z, sZ, tb, state_col_addr(L), L);
-            weigh<Cfg, ZP>(zw, z, sW[0], tb, L);
-            if (DOT) weigh<Cfg, ZP>(zd, z, sW[DOT ? 1 : 0], tb, L);
+            weigh<Cfg, ZP>(zw, z, sW, tb, L);
 #pragma unroll
             for (int s = 0; s < Cfg::KS; ++s)
 #pragma unroll
@@ -156,16 +165,341 @@ __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummary
                     bf16x8 y[Cfg::NP];
                     col_frag<Cfg, Cfg::KD>(y, sY, tb, state_row_addr(s, u, L), L);
                     mma<Cfg::NP, ZP>(S[s][u], y, zw);
-                    if (DOT) mma<Cfg::NP, ZP>(D[s][u], y, zd);
                 }
         }
     }
     L.again();
-    const int64_t words = (int64_t)p.y.d * p.z.d, n = p.nseg - 1;
-    const int64_t at = ((b * p.H + h) * n + seg) * words;
-    store_state<Cfg>(S, p.states + at, p.z.d, 1, p.y.d, p.z.d, (float)owed.now, false, L);
-    if (DOT) store_state<Cfg>(D, p.dstates + at, p.z.d, 1, p.y.d, p.z.d, (float)owed.now, false, L);
-    if (h == 0 && L.tid == 0) p.R[b * n + seg] = any ? 1 : 0;
+    const int64_t words = (int64_t)p.y.d * p.z.d;
+    store_state<Cfg>(S, p.states + ((b * p.H + h) * p.nseg + seg) * words, p.z.d, 1, p.y.d, p.z.d, (float)owed.now, false, L);
+    if (h == 0 && L.tid == 0) p.R[b * p.nseg + seg] = any ? kSegBegins : 0;
+}
+
+// ------------------------------------------- what the gradient needs of a segment
+// With f_t = scale gamma^(t - r0) for the steps t of a segment that no begin
+// separates from its first step r0,
+//     S  = what the segment adds to the state after it,
+//     U  = sum f_t q_t^T g_t, what it adds to the gradient of the state at r0,
+// and for the gradient of the rates (ALPHA)
+//     D  = dS / dlog gamma,   E = sum (t - r0) f_t q_t^T g_t,
+//     part = the segment's own share of dL/dlog gamma, as if the state before it
+//            were zero.
+// With D_t = dS_t / dlog gamma = gamma (D_{t-1} + S_{t-1}) + 0 inside an episode,
+//     dL/dlog gamma = scale sum_t q_t D_t g_t^T   (+ D_{T-1} . grad_state),
+// which per chunk, (S, D) before it, o1 = sum gamma^i q_i^T g_i and o2 = sum i gamma^i
+// q_i^T g_i over its rows whose episode began earlier, is
+//     sum_ij (i-j) gamma^(i-j) (q_i . k_j)(g_i . v_j)  +  gamma (S . (o1 + o2) + D . o1).
+// The outer products arrive in the state's own layout, so they meet S and D as
+// floats in registers, and the pairs' products are not rounded either: nothing of
+// dL/dlog gamma is rounded to bf16.  What a state before the segment adds to it,
+// gamma (S . (U + E) + D . U), follows in the state scan.
+//
+// FWD: S, D and part; BACK: U and E.  One pass for both reads q, k, v and g once,
+// with the states in registers, 64 rows of each per wavefront (RetCfg64).  Four
+// states of 128 x 128 do not fit: there ALPHA takes two passes.
+//
+// A value that is not finite would reach other episodes and earlier rows through
+// zero weights.  Without ALPHA the rows that take no part become zeros.  With
+// ALPHA, where every row takes part in something, the segment is marked and done
+// again row by row by ret_prep_rows_kernel.
+template <class Cfg, int ZP, bool ALPHA, bool FWD, bool BACK>
+__global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void ret_prep_kernel(RetPrepArgs p) {
+    __shared__ __attribute__((aligned(16))) uint16_t sQ[Cfg::NP * Cfg::C * Cfg::KD];
+    __shared__ __attribute__((aligned(16))) uint16_t sK[FWD ? Cfg::NP * Cfg::C * Cfg::KD : 8];
+    __shared__ __attribute__((aligned(16))) uint16_t sV[FWD ? Cfg::NP * Cfg::C * Cfg::VD : 8];
+    __shared__ __attribute__((aligned(16))) uint16_t sG[Cfg::NP * Cfg::C * Cfg::VD];
+    __shared__ Powers<Cfg::C + 1> sPw;
+    __shared__ float sAge[Cfg::C + 16];                    // [16 + n]: n gamma^n scale, 0 for n < 0
+    __shared__ __attribute__((aligned(16))) float sW[4][Cfg::C];
+    __shared__ double sSum[Cfg::W];
+    RetLane L;
+    const int wave = L.w;
+    L.k0 = wave / Cfg::CW * 64;
+    L.w = wave % Cfg::CW;
+    const int64_t seg = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+    ret_header(p.hdr, p.sig);
+    const double rate = fabs((double)p.alpha[h]);
+    sPw.fill(rate, L.tid);
+    if (ALPHA && FWD && L.tid < Cfg::C + 16) {
+        const int age = L.tid - 16;
+        sAge[L.tid] = age < 0 ? 0.0f : decay_pow(rate, age) * (float)age * p.scale;
+    }
+    const int kd = p.q.d, vd = p.v.d;
+    const Head hq = head_of<Cfg>(p.q, b, h, p.T), hk = head_of<Cfg>(p.k, b, h, p.T), hv = head_of<Cfg>(p.v, b, h, p.T),
+               hg = head_of<Cfg>(p.g, b, h, p.T);
+    const uint8_t* const start = p.start + b * p.T;
+    const Run<Cfg> run((int)seg, p.chunks, (int)p.T, 0);
+
+    RetTile<Cfg, Cfg::KD> tq, tk;
+    RetTile<Cfg, Cfg::VD> tv, tg;
+    uint32_t flag;
+    auto fetch = [&](int ch) {
+        const int t0 = run.first(ch), n = run.rows(ch);
+        flag = ret_flag(start, t0, n, (int)p.T, false, L.lane);
+        tq.fetch(rows_of<Cfg>(hq, t0, n), L);
+        if (FWD) tk.fetch(rows_of<Cfg>(hk, t0, n), L);
+        if (FWD) tv.fetch(rows_of<Cfg>(hv, t0, n), L);
+        tg.fetch(rows_of<Cfg>(hg, t0, n), L);
+    };
+    fetch(0);
+    State<Cfg> S, D, U, E;
+    zero_state<Cfg>(S);
+    zero_state<Cfg>(U);
+    if (ALPHA) {
+        zero_state<Cfg>(D);
+        zero_state<Cfg>(E);
+    }
+    Owed owed;
+    __syncthreads();                                       // the powers are there
+    const float gamma = uniform(sPw.f(1));
+    double sum = 0.0, reach = 1.0;                         // gamma^(steps before the rows at hand)
+    bool open = true;                                      // no begin since r0
+    uint32_t begins = 0, bad = 0;
+#pragma unroll 1
+    for (int ch = 0; ch < run.nch; ++ch) {
+        L.again();
+        const int n = run.rows(ch);
+        const uint64_t m = __ballot(flag != 0u);
+        if (ch == 0 && (m & 1ull)) begins |= kSegBeginsFirst;
+        if (ALPHA && FWD) bad |= tq.bad() | tk.bad() | tv.bad() | tg.bad();
+        const uint64_t mo = ch == 0 ? m & ~1ull : m;   // a begin at r0 separates nothing from it
+        if (m) begins |= kSegBegins;
+        if (mo) begins |= kSegBeginsBack;
+        // rows from `from` on enter S, rows before `to` go on from before the chunk
+        const int from = m ? last_begin(m) : 0, to = mo ? __builtin_ctzll(mo) : n;
+        const float was = uniform((float)owed.now);
+        bool take = false;
+        if (m) owed.none();
+        else take = owed.add(sPw, n);
+        const Carry cy = carry_by(owed.now);
+        if (take) owed.none();
+        const float far = uniform((float)reach), off = (float)(ch * Cfg::C);
+        if (!ALPHA && m) {
+            tk.keep(from, Cfg::C, L);
+            tv.keep(from, Cfg::C, L);
+            tq.keep(0, open ? to : 0, L);
+            tg.keep(0, open ? to : 0, L);
+        }
+        barrier_lds();                                 // the last operands have been read
+        tq.stage(sQ, L);
+        if (FWD) tk.stage(sK, L);
+        if (FWD) tv.stage(sV, L);
+        tg.stage(sG, L);
+        if (L.tid < Cfg::C) {
+            const int i = L.tid;
+            const float w = i >= from && i < n ? sPw.f(i < n ? n - 1 - i : 0) * (float)owed.inverse : 0.0f;
+            sW[0][i] = w;
+            const float f = i < to ? sPw.f(i) * p.scale : 0.0f;
+            sW[2][i] = f;
+            if (ALPHA) {
+                sW[1][i] = w * (float)(n - 1 - i);
+                sW[3][i] = f * (float)i;
+            }
+        }
+        fetch(ch + 1);
+        barrier_lds();
+        if constexpr (ALPHA && FWD) {
+            float part = 0.0f;
+#pragma unroll
+            for (int i = 0; i < (Cfg::NTILE + Cfg::W - 1) / Cfg::W; ++i) {
+                const int idx = Cfg::W * i + wave;
+                if (idx >= Cfg::NTILE) break;
+                int jb, ib;
+                tile_of(idx, jb, ib);
+                const f32x4 x = pair_products<Cfg, Cfg::KD>(sK, sQ, jb, ib, L);
+                const f32x4 y = pair_products<Cfg, Cfg::VD>(sV, sG, jb, ib, L);
+                const int row = 16 * ib + L.c, age = row - 16 * jb - 4 * L.g;
+                const uint64_t mr = m & upto(row);
+                const int oldest = mr ? row - last_begin(mr) : row;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    part += age - r > 0 && age - r <= oldest ? x[r] * y[r] * sAge[age - r + 16] : 0.0f;
+            }
+            sum += (double)part;
+        }
+        // ---- rows of the first episode: outer products of q and g.  Without any
+        // such row nothing is touched, so that values of S that are not finite
+        // stay out
+        if (to > 0 && ((ALPHA && FWD) || open)) {
+            const float use = open ? far : 0.0f;
+            float part = 0.0f;
+            // o1, then o2: one set of weighted g at a time, for the registers
+#pragma unroll
+            for (int k = 0; k < (ALPHA ? 2 : 1); ++k) {
+                bf16x8 gw[Cfg::C / 32][ZP];
+#pragma unroll
+                for (int tb = 0; tb < Cfg::C / 32; ++tb) {
+                    bf16x8 g[Cfg::NP];
+                    col_frag<Cfg, Cfg::VD>(g, sG, tb, state_col_addr(L), L);
+                    weigh<Cfg, ZP>(gw[tb], g, sW[2 + k], tb, L);
+                }
+#pragma unroll
+                for (int s = 0; s < Cfg::KS; ++s)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        f32x4 o = zero4();
+#pragma unroll
+                        for (int tb = 0; tb < Cfg::C / 32; ++tb) {
+                            bf16x8 q[Cfg::NP];
+                            col_frag<Cfg, Cfg::KD>(q, sQ, tb, state_row_addr(s, u, L), L);
+                            mma<Cfg::NP, ZP>(o, q, gw[tb]);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if (BACK && k == 0) U[s][u][e] = __builtin_fmaf(use, o[e], U[s][u][e]);
+                            if (BACK && ALPHA) E[s][u][e] = __builtin_fmaf(k == 0 ? use * off : use, o[e], E[s][u][e]);
+                            if (FWD && ALPHA)
+                                part = __builtin_fmaf(k == 0 ? S[s][u][e] + D[s][u][e] : S[s][u][e], o[e], part);
+                        }
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            // (before the first step there is no state, and no state is NaN)
+            if (ALPHA && FWD && ch > 0) sum += (double)(part * (was * gamma));
+        }
+        // ---- (S, D) after the rows
+        if constexpr (FWD && ALPHA) {
+            const float steps = (float)n;
+            each<Cfg>(D, [&](float x, int s, int u, int e) { return __builtin_fmaf(steps, S[s][u][e], x); });
+            settle<Cfg>(D, m != 0, take, cy);
+        }
+        if constexpr (FWD) settle<Cfg>(S, m != 0, take, cy);
+#pragma unroll
+        for (int tb = 0; tb < (FWD ? Cfg::C / 32 : 0); ++tb) {
+            bf16x8 z[Cfg::NP];
+            col_frag<Cfg, Cfg::VD>(z, sV, tb, state_col_addr(L), L);
+#pragma unroll
+            for (int k = 0; k < (ALPHA ? 2 : 1); ++k) {
+                bf16x8 zw[ZP];
+                weigh<Cfg, ZP>(zw, z, sW[k], tb, L);
+#pragma unroll
+                for (int s = 0; s < Cfg::KS; ++s)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        bf16x8 y[Cfg::NP];
+                        col_frag<Cfg, Cfg::KD>(y, sK, tb, state_row_addr(s, u, L), L);
+                        mma<Cfg::NP, ZP>(k ? D[s][u] : S[s][u], y, zw);
+                    }
+            }
+        }
+        open = open && mo == 0;
+        reach = uniform(reach * sPw.of[n]);
+    }
+    L.again();
+    const int64_t words = (int64_t)kd * vd, bh = b * p.H + h, at = (bh * p.nseg + seg) * words;
+    if (FWD) store_state<Cfg>(S, p.states + at, vd, 1, kd, vd, (float)owed.now, false, L);
+    if (BACK) store_state<Cfg>(U, p.rstates + at, vd, 1, kd, vd, 1.0f, false, L);
+    if (FWD && ALPHA) store_state<Cfg>(D, p.dstates + at, vd, 1, kd, vd, (float)owed.now, false, L);
+    if (BACK && ALPHA) store_state<Cfg>(E, p.estates + at, vd, 1, kd, vd, 1.0f, false, L);
+    if (FWD && ALPHA) {
+#pragma unroll
+        for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x, 64);
+        if (L.lane == 0) sSum[wave] = sum;
+        __syncthreads();
+        if (L.tid == 0) {
+            double s = 0.0;
+#pragma unroll
+            for (int i = 0; i < Cfg::W; ++i) s += sSum[i];
+            p.part[bh * p.nparts + seg] = s;
+        }
+        // a value that is not finite, in the inputs or by overflow: the segment is done
+        // again by ret_prep_rows_kernel
+        const bool any_bad = __syncthreads_or(bad != 0u || !(fabs(sum) < (double)__builtin_inff())) != 0;
+        if (L.tid == 0) p.bad[bh * p.nseg + seg] = any_bad;
+    }
+    if (FWD && h == 0 && L.tid == 0) {
+        if (run.r1 < p.T && start[run.r1] != 0) begins |= kSegBeginsBack;
+        p.R[b * p.nseg + seg] = (uint8_t)begins;
+    }
+}
+
+// The same, with ALPHA, of the segments that hold a value that is not finite, by the
+// recurrences themselves in floats.
+template <class Cfg>
+__global__ __launch_bounds__(Cfg::THREADS) void ret_prep_rows_kernel(RetPrepArgs p) {
+    const int64_t seg = blockIdx.x, h = blockIdx.y, b = blockIdx.z, bh = b * p.H + h;
+    if (!p.bad[bh * p.nseg + seg]) return;
+    __shared__ __attribute__((aligned(16))) uint16_t sQ[Cfg::NP * Cfg::C * Cfg::KD];
+    __shared__ __attribute__((aligned(16))) uint16_t sK[Cfg::NP * Cfg::C * Cfg::KD];
+    __shared__ __attribute__((aligned(16))) uint16_t sV[Cfg::NP * Cfg::C * Cfg::VD];
+    __shared__ __attribute__((aligned(16))) uint16_t sG[Cfg::NP * Cfg::C * Cfg::VD];
+    __shared__ double sSum[Cfg::W];
+    RetLane L;
+    const int wave = L.w;
+    L.k0 = wave / Cfg::CW * 64;
+    L.w = wave % Cfg::CW;
+    const double rate = fabs((double)p.alpha[h]);
+    const Carry one = carry_of(rate, 1.0);
+    const int kd = p.q.d, vd = p.v.d;
+    const Head hq = head_of<Cfg>(p.q, b, h, p.T), hk = head_of<Cfg>(p.k, b, h, p.T), hv = head_of<Cfg>(p.v, b, h, p.T),
+               hg = head_of<Cfg>(p.g, b, h, p.T);
+    const uint8_t* const start = p.start + b * p.T;
+    const Run<Cfg> run((int)seg, p.chunks, (int)p.T, 0);
+    State<Cfg> S, D, U, E;
+    zero_state<Cfg>(S);
+    zero_state<Cfg>(D);
+    zero_state<Cfg>(U);
+    zero_state<Cfg>(E);
+    bool open = true;
+    double sum = 0.0;
+#pragma unroll 1
+    for (int ch = 0; ch < run.nch; ++ch) {
+        RetTile<Cfg, Cfg::KD> tq, tk;
+        RetTile<Cfg, Cfg::VD> tv, tg;
+        const int t0 = run.first(ch), n = run.rows(ch);
+        const uint64_t m = __ballot(ret_flag(start, t0, n, (int)p.T, false, L.lane) != 0u);
+        tq.fetch(rows_of<Cfg>(hq, t0, n), L);
+        tk.fetch(rows_of<Cfg>(hk, t0, n), L);
+        tv.fetch(rows_of<Cfg>(hv, t0, n), L);
+        tg.fetch(rows_of<Cfg>(hg, t0, n), L);
+        __syncthreads();
+        tq.stage(sQ, L);
+        tk.stage(sK, L);
+        tv.stage(sV, L);
+        tg.stage(sG, L);
+        __syncthreads();
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
+            const int t = ch * Cfg::C + i;                 // steps since r0
+            const bool begin = (m >> i) & 1ull;
+            open = open && !(begin && t > 0);
+            const float f = decay_pow(rate, (double)t) * p.scale;
+            const float v = tile_value<Cfg, Cfg::VD>(sV, i, state_col(L)), g = tile_value<Cfg, Cfg::VD>(sG, i, state_col(L));
+            float dot = 0.0f;
+#pragma unroll
+            for (int s = 0; s < Cfg::KS; ++s) {
+                float q[8], k[8];
+                row_values<Cfg, Cfg::KD>(q, sQ, i, s, L);
+                row_values<Cfg, Cfg::KD>(k, sK, i, s, L);
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    const int u = x >> 2, e = x & 3;
+                    const float d = begin ? 0.0f : one(D[s][u][e] + S[s][u][e]);
+                    D[s][u][e] = d;
+                    S[s][u][e] = __builtin_fmaf(k[x], v, begin ? 0.0f : one(S[s][u][e]));
+                    dot = __builtin_fmaf(q[x], d, dot);
+                    const float o = q[x] * (f * g);
+                    U[s][u][e] = open ? U[s][u][e] + o : U[s][u][e];
+                    E[s][u][e] = open && t > 0 ? __builtin_fmaf((float)t, o, E[s][u][e]) : E[s][u][e];
+                }
+            }
+            if (!begin && t > 0) sum += (double)(dot * p.scale * g);
+        }
+    }
+    const int64_t words = (int64_t)kd * vd, at = (bh * p.nseg + seg) * words;
+    store_state<Cfg>(S, p.states + at, vd, 1, kd, vd, 1.0f, false, L);
+    store_state<Cfg>(D, p.dstates + at, vd, 1, kd, vd, 1.0f, false, L);
+    store_state<Cfg>(U, p.rstates + at, vd, 1, kd, vd, 1.0f, false, L);
+    store_state<Cfg>(E, p.estates + at, vd, 1, kd, vd, 1.0f, false, L);
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x, 64);
+    if (L.lane == 0) sSum[wave] = sum;
+    __syncthreads();
+    if (L.tid == 0) {
+        double s = 0.0;
+#pragma unroll
+        for (int i = 0; i < Cfg::W; ++i) s += sSum[i];
+        p.part[bh * p.nparts + seg] = s;
+    }
 }
 
 // ---------------------------------------------------------------- state scan
@@ -196,30 +530,42 @@ __global__ __launch_bounds__(256) void ret_state_scan_kernel(RetStateScanArgs p)
     constexpr int kCols = 256 / GROUPS, kTile = GROUPS * RPT;
     __shared__ f32x4 sTot[GROUPS > 1 && DOT ? 2 : 1][GROUPS][GROUPS > 1 ? kCols : 1];
     __shared__ uint32_t sFlag[GROUPS];
+    __shared__ double sSum[DOT ? 4 : 1];
     const int col = threadIdx.x % kCols, grp = threadIdx.x / kCols;
     const int64_t h = blockIdx.y, b = blockIdx.z, bh = b * p.H + h;
     const int c4 = (int)blockIdx.x * kCols + col, w4 = p.words / 4;   // words is a multiple of 64
     const bool in = c4 < w4;
-    const double rate = fabs((double)p.alpha[h]), rows = (double)p.rows;
+    const double rate = fabs((double)p.alpha[h]), rows = (double)p.rows, last = (double)p.last_rows;
+    // the nseg - 1 segments that have one behind them in scan order; with DOT the
+    // last one too, for what it takes from the state before it
+    const int n = DOT ? p.nseg : p.nseg - 1;
     const Carry one = carry_of(rate, rows), many = carry_of(rate, rows * RPT);
-    // backwards the seed belongs to the last step itself: one decay less
-    const Carry one0 = p.rev ? carry_of(rate, rows - 1.0) : one, many0 = p.rev ? carry_of(rate, rows * RPT - 1.0) : many;
-    f32x4* const S = (f32x4*)p.states + bh * p.n * w4 + c4;
-    f32x4* const D = DOT ? (f32x4*)p.dstates + bh * p.n * w4 + c4 : nullptr;
-    const uint8_t* const R = p.R + b * p.n;
+    // Backwards the last segment, which may be short, comes first, and the seed
+    // belongs to its last step itself: one decay less.
+    const Carry one0 = p.rev ? carry_of(rate, last - 1.0) : one;
+    const Carry many0 = p.rev ? carry_of(rate, last - 1.0 + rows * (RPT - 1)) : many;
+    const Carry one_last = carry_of(rate, last);
+    const uint32_t bit = p.rev ? kSegBeginsBack : kSegBegins;
+    f32x4* const S = (f32x4*)p.states + bh * p.nseg * w4 + c4;
+    f32x4* const D = DOT ? (f32x4*)p.dstates + bh * p.nseg * w4 + c4 : nullptr;
+    const f32x4* const U = DOT ? (const f32x4*)p.rstates + bh * p.nseg * w4 + c4 : nullptr;
+    const f32x4* const E = DOT ? (const f32x4*)p.estates + bh * p.nseg * w4 + c4 : nullptr;
+    const uint8_t* const R = p.R + b * p.nseg;
+    auto seg_of = [&](int l) { return p.rev ? p.nseg - 1 - l : l; };
     const f32x4 zero = zero4();
+    double sum = 0.0;
     SegState<DOT> before;                                  // the state before the tile
     if (p.seed && in) before.s = ((const f32x4*)p.seed)[bh * w4 + c4];
-    for (int base = 0; base < p.n; base += kTile) {
+    for (int base = 0; base < n; base += kTile) {
         f32x4 x[RPT], y[DOT ? RPT : 1];
-        bool fl[RPT];
+        uint32_t fl[RPT];
 #pragma unroll
         for (int i = 0; i < RPT; ++i) {
-            const int l = base + grp * RPT + i;
-            const bool have = in && l < p.n;
-            x[i] = have ? S[(int64_t)l * w4] : zero;
-            if (DOT) y[DOT ? i : 0] = have ? D[(int64_t)l * w4] : zero;
-            fl[i] = l < p.n && R[l < p.n ? l : 0] != 0;
+            const int l = base + grp * RPT + i, sg = seg_of(l);
+            const bool have = in && l < n;
+            x[i] = have ? S[(int64_t)sg * w4] : zero;
+            if (DOT) y[DOT ? i : 0] = have ? D[(int64_t)sg * w4] : zero;
+            fl[i] = l < n ? R[l < n ? sg : 0] : 0u;
         }
         SegState<DOT> mine = before;                       // the state before this thread's run
         if constexpr (GROUPS > 1) {
@@ -227,8 +573,8 @@ __global__ __launch_bounds__(256) void ret_state_scan_kernel(RetStateScanArgs p)
             bool any = false;
 #pragma unroll
             for (int i = 0; i < RPT; ++i) {
-                tot.then(x[i], y[DOT ? i : 0], fl[i], one, (float)p.rows);
-                any |= fl[i];
+                tot.then(x[i], y[DOT ? i : 0], (fl[i] & bit) != 0u, one, (float)p.rows);
+                any |= (fl[i] & bit) != 0u;
             }
             __syncthreads();                               // the last tile's totals have been read
             sTot[0][grp][col] = tot.s;
@@ -245,13 +591,43 @@ __global__ __launch_bounds__(256) void ret_state_scan_kernel(RetStateScanArgs p)
 #pragma unroll
         for (int i = 0; i < RPT; ++i) {
             const int l = base + grp * RPT + i;
-            mine.then(x[i], y[DOT ? i : 0], fl[i], l == 0 ? one0 : one, (float)p.rows);
-            if (in && l < p.n) {
-                S[(int64_t)l * w4] = mine.s;
-                if (DOT) D[(int64_t)l * w4] = mine.d;
+            const bool have = in && l < n;
+            if constexpr (DOT) {
+                // gamma (S . (U + E) + D . U), where the segment's first step goes on
+                if (have && !(fl[i] & kSegBeginsFirst)) {
+                    const f32x4 u = U[(int64_t)l * w4], e = E[(int64_t)l * w4];
+                    float d = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        d = __builtin_fmaf(mine.s[k], u[k] + e[k], __builtin_fmaf(mine.d[k], u[k], d));
+                    sum += (double)(d * decay_pow(rate, 1.0));
+                }
+                const bool at_end = l == p.nseg - 1;
+                mine.then(x[i], y[DOT ? i : 0], (fl[i] & bit) != 0u, at_end ? one_last : one,
+                          (float)(at_end ? p.last_rows : p.rows));
+                if (have && !at_end) {
+                    S[(int64_t)l * w4] = mine.s;
+                    D[(int64_t)l * w4] = mine.d;
+                }
+                if (have && at_end && p.grad_state) {      // D after the tape . grad_state
+                    const f32x4 g = ((const f32x4*)p.grad_state)[bh * w4 + c4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) sum += (double)mine.d[k] * (double)g[k];
+                }
+            } else {
+                mine.then(x[i], zero, (fl[i] & bit) != 0u, l == 0 ? one0 : one, 0.0f);
+                if (have) S[(int64_t)seg_of(l) * w4] = mine.s;
             }
         }
         if constexpr (GROUPS == 1) before = mine;
+    }
+    if constexpr (DOT) {
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m, 64);
+        if ((threadIdx.x & 63) == 0) sSum[threadIdx.x >> 6] = sum;
+        __syncthreads();
+        if (threadIdx.x == 0)
+            p.part[bh * p.nparts + p.nseg + blockIdx.x] = (sSum[0] + sSum[1]) + (sSum[2] + sSum[3]);
     }
 }
 
@@ -315,29 +691,24 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 :
     const Head hx = head_of<Cfg>(p.x, b, h, p.T), hy = head_of<Cfg>(p.y, b, h, p.T), hz = head_of<Cfg>(p.z, b, h, p.T);
     const uint8_t* const start = p.start + b * p.T;
     const int64_t words = (int64_t)p.x.d * p.z.d, bh = b * p.H + h;
-    const int T = (int)p.T, seg0 = (int)seg * p.chunks * Cfg::C;
-    const int left = (T - seg0 + Cfg::C - 1) / Cfg::C, nch = left < p.chunks ? left : p.chunks;
+    const Run<Cfg> run((int)seg, p.chunks, (int)p.T, p.rev);
+    const int64_t at_start = p.rev ? p.nseg - 1 : 0;       // the segment that the walk begins with
     const int os = Cfg::NP == 1 && !p.out_f32 ? 2 : 4;
-    auto rows_in = [&](int ch) {                           // rows of chunk ch, none past the segment
-        const int rest = ch < nch ? T - (seg0 + ch * Cfg::C) : 0;
-        return rest < Cfg::C ? rest : Cfg::C;
-    };
-    auto first_of = [&](int ch) { return ch < nch ? seg0 + ch * Cfg::C : 0; };
     auto rows_out = [&](int ch) {
-        return ret_rows((char*)p.out + (b * p.T * p.H + h) * p.z.d * os, (int64_t)p.H * p.z.d * os, p.z.d, os, first_of(ch),
-                        rows_in(ch), p.T, p.rev);
+        return ret_rows((char*)p.out + (b * p.T * p.H + h) * p.z.d * os, (int64_t)p.H * p.z.d * os, p.z.d, os, run.first(ch),
+                        run.rows(ch), p.rev);
     };
 
     RetTile<Cfg, Cfg::KD> tx, ty;
     RetTile<Cfg, Cfg::VD> tz;
     uint32_t flag;
     auto fetch = [&](int ch) {
-        const int w0 = first_of(ch), n = rows_in(ch);
-        flag = ret_flag(start, w0, n, p.T, p.rev, L.lane);
-        tx.fetch(rows_of<Cfg>(hx, w0, n, p.T, p.rev), L);
-        ty.fetch(rows_of<Cfg>(hy, w0, n, p.T, p.rev), L);
+        const int t0 = run.first(ch), n = run.rows(ch);
+        flag = ret_flag(start, t0, n, (int)p.T, p.rev, L.lane);
+        tx.fetch(rows_of<Cfg>(hx, t0, n, p.rev), L);
+        ty.fetch(rows_of<Cfg>(hy, t0, n, p.rev), L);
     };
-    auto fetch_z = [&](int ch) { tz.fetch(rows_of<Cfg>(hz, first_of(ch), rows_in(ch), p.T, p.rev), L); };
+    auto fetch_z = [&](int ch) { tz.fetch(rows_of<Cfg>(hz, run.first(ch), run.rows(ch), p.rev), L); };
     Owed owed;
     __syncthreads();                                       // the powers are there
     bool held = false;                                     // the last chunk's rows wait in sO
@@ -354,16 +725,17 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 :
     fetch(0);
     fetch_z(0);
     State<Cfg> S;
-    load_state<Cfg>(S, seg == 0 ? (p.seed ? p.seed + bh * words : nullptr) : p.states + (bh * (p.nseg - 1) + seg - 1) * words,
+    load_state<Cfg>(S, seg == at_start ? (p.seed ? p.seed + bh * words : nullptr)
+                                       : p.states + (bh * p.nseg + (p.rev ? seg + 1 : seg - 1)) * words,
                     p.sk, p.sv, p.x.d, p.z.d, L);
 #pragma unroll 1
-    for (int ch = 0; ch < nch; ++ch) {
+    for (int ch = 0; ch < run.nch; ++ch) {
         L.again();
-        const int n = rows_in(ch);
+        const int n = run.rows(ch);
         const uint64_t m = __ballot(flag != 0u);
         const bool bad_z = tz.bad() != 0u;
         // the gradient of the state after the tape belongs to the last step
-        const int e = p.rev && seg == 0 && ch == 0 ? 0 : 1;
+        const int e = p.rev && seg == at_start && ch == 0 ? 0 : 1;
         const float was = uniform((float)owed.now), before = was * p.inter_scale;
         bool take = false;
         if (m) owed.none();
@@ -371,9 +743,9 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 :
         const Carry cy = carry_by(owed.now);
         if (take) owed.none();
         barrier_lds();                                     // the last chunk's operands have been read
-        tx.stage(sX, 0, L);
-        ty.stage(sY, 0, L);
-        tz.stage(sZ, 0, L);
+        tx.stage(sX, L);
+        ty.stage(sY, L);
+        tz.stage(sZ, L);
         // weights of the rows into the state: no begin step after them
         if (L.tid < Cfg::C) {
             const int from = m ? last_begin(m) : 0;
@@ -504,9 +876,9 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 :
     }
     if (Cfg::NP == 1 && held) {
         barrier_lds();
-        put_rows(nch - 1);
+        put_rows(run.nch - 1);
     }
-    if (p.fin && seg == p.nseg - 1) {
+    if (p.fin && seg == (p.rev ? 0 : p.nseg - 1)) {
         // backwards: the gradient of the state before the tape, one step further
         // back, and none if step 0 begins an episode
         const bool drop = p.rev && start[0] != 0;
@@ -514,216 +886,13 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 :
     }
 }
 
-// ------------------------------------------------------- gradient of the rate
-// With D_t = dS_t / dlog gamma, D_t = gamma (D_{t-1} + S_{t-1}) inside an episode,
-//     dL/dlog gamma = scale sum_t q_t D_t dout_t^T  (+ D_T-1 . grad_state),
-// per chunk, (S, D) before it:
-//     sum_ij (i-j) gamma^(i-j) (q_i . k_j)(dout_i . v_j)     both products in float
-//   + S . sum_i (i+1) gamma^(i+1) q_i^T dout_i + D . sum_i gamma^(i+1) q_i^T dout_i
-// The two outer products arrive in the state's own layout, so they meet S and D
-// as floats in registers: nothing here is rounded to bf16.
-template <class Cfg>
-__global__ __launch_bounds__(Cfg::THREADS, 2) void ret_sens_kernel(RetSensArgs p) {
-    __shared__ __attribute__((aligned(16))) uint16_t sQ[Cfg::NP * Cfg::C * Cfg::KD];
-    __shared__ __attribute__((aligned(16))) uint16_t sK[Cfg::NP * Cfg::C * Cfg::KD];
-    __shared__ __attribute__((aligned(16))) uint16_t sV[Cfg::NP * Cfg::C * Cfg::VD];
-    __shared__ __attribute__((aligned(16))) uint16_t sG[Cfg::NP * Cfg::C * Cfg::VD];
-    __shared__ Powers<Cfg::C + 1> sPw;
-    __shared__ float sAge[Cfg::C + 16];                    // [16 + n]: n gamma^n scale, 0 for n < 0
-    __shared__ __attribute__((aligned(16))) float sW[4][Cfg::C];
-    __shared__ uint32_t sBad[Cfg::W];
-    __shared__ double sSum[Cfg::W];
-    RetLane L;
-    const int64_t seg = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
-    const double rate = fabs((double)p.alpha[h]);
-    sPw.fill(rate, L.tid);
-    if (L.tid < Cfg::C + 16) {
-        const int age = L.tid - 16;
-        sAge[L.tid] = age < 0 ? 0.0f : decay_pow(rate, age) * (float)age * p.scale;
-    }
-    const int kd = p.q.d, vd = p.v.d;
-    const Head hq = head_of<Cfg>(p.q, b, h, p.T), hk = head_of<Cfg>(p.k, b, h, p.T), hv = head_of<Cfg>(p.v, b, h, p.T),
-               hg = head_of<Cfg>(p.g, b, h, p.T);
-    const uint8_t* const start = p.start + b * p.T;
-    const int64_t words = (int64_t)kd * vd, bh = b * p.H + h;
-    const int T = (int)p.T, seg0 = (int)seg * p.chunks * Cfg::C;
-    const int left = (T - seg0 + Cfg::C - 1) / Cfg::C, nch = left < p.chunks ? left : p.chunks;
-
-    RetTile<Cfg, Cfg::KD> tq, tk;
-    RetTile<Cfg, Cfg::VD> tv, tg;
-    uint32_t flag;
-    auto fetch = [&](int ch) {
-        const bool have = ch < nch;
-        const int w0 = have ? seg0 + ch * Cfg::C : 0, rest = have ? T - w0 : 0, n = rest < Cfg::C ? rest : Cfg::C;
-        flag = ret_flag(start, w0, n, p.T, false, L.lane);
-        tq.fetch(rows_of<Cfg>(hq, w0, n, p.T, false), L);
-        tk.fetch(rows_of<Cfg>(hk, w0, n, p.T, false), L);
-        tv.fetch(rows_of<Cfg>(hv, w0, n, p.T, false), L);
-        tg.fetch(rows_of<Cfg>(hg, w0, n, p.T, false), L);
-    };
-    fetch(0);
-    State<Cfg> S, D;
-    const int64_t at = (bh * (p.nseg - 1) + seg - 1) * words;
-    load_state<Cfg>(S, seg == 0 ? (p.seed ? p.seed + bh * words : nullptr) : p.states + at, vd, 1, kd, vd, L);
-    load_state<Cfg>(D, seg == 0 ? nullptr : p.dstates + at, vd, 1, kd, vd, L);
-    Owed owed;
-    __syncthreads();                                       // the powers are there
-    double sum = 0.0;
-#pragma unroll 1
-    for (int ch = 0; ch < nch; ++ch) {
-        L.again();
-        const int rest = T - (seg0 + ch * Cfg::C), n = rest < Cfg::C ? rest : Cfg::C;
-        const uint64_t m = __ballot(flag != 0u);
-        const float before = uniform((float)owed.now);
-        bool take = false;
-        if (m) owed.none();
-        else take = owed.add(sPw, n);
-        const Carry cy = carry_by(owed.now);
-        if (take) owed.none();
-        const uint64_t not_finite = __ballot((tq.bad() | tk.bad() | tv.bad() | tg.bad()) != 0u);
-        barrier_lds();                                     // the last operands have been read
-        if (L.lane == 0) sBad[L.w] = not_finite != 0;
-        tq.stage(sQ, 0, L);
-        tk.stage(sK, 0, L);
-        tv.stage(sV, 0, L);
-        tg.stage(sG, 0, L);
-        if (L.tid < Cfg::C) {
-            const int i = L.tid;
-            const int from = m ? last_begin(m) : 0;
-            const float w = i < n && i >= from ? sPw.f(i < n ? n - 1 - i : 0) * (float)owed.inverse : 0.0f;
-            sW[0][i] = w;
-            sW[1][i] = w * (float)(n - 1 - i);
-            const float f = i < n && (m & upto(i)) == 0 ? sPw.f(i + 1) * p.scale * before : 0.0f;
-            sW[2][i] = f;
-            sW[3][i] = f * (float)(i + 1);
-        }
-        fetch(ch + 1);
-        barrier_lds();
-        uint32_t any_bad = 0;
-#pragma unroll
-        for (int i = 0; i < Cfg::W; ++i) any_bad |= sBad[i];
-        float part = 0.0f;
-        if (__builtin_amdgcn_readfirstlane((int)any_bad) == 0) {
-#pragma unroll
-            for (int i = 0; i < (Cfg::NTILE + Cfg::W - 1) / Cfg::W; ++i) {
-                const int idx = Cfg::W * i + L.w;
-                if (idx >= Cfg::NTILE) break;
-                int jb, ib;
-                tile_of(idx, jb, ib);
-                const f32x4 x = pair_products<Cfg, Cfg::KD>(sK, sQ, jb, ib, L);
-                const f32x4 y = pair_products<Cfg, Cfg::VD>(sV, sG, jb, ib, L);
-                const int row = 16 * ib + L.c, age = row - 16 * jb - 4 * L.g;
-                const uint64_t mr = m & upto(row);
-                const int oldest = mr ? row - last_begin(mr) : row;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) part += age - r <= oldest ? x[r] * y[r] * sAge[age - r + 16] : 0.0f;
-            }
-            // rows against (S, D): skipped where the first row begins an episode,
-            // so that values of S that are not finite stay out
-            if (!(m & 1ull)) {
-                bf16x8 g1[Cfg::C / 32][3], g2[Cfg::C / 32][3];
-#pragma unroll
-                for (int tb = 0; tb < Cfg::C / 32; ++tb) {
-                    bf16x8 g[Cfg::NP];
-                    col_frag<Cfg, Cfg::VD>(g, sG, tb, state_col_addr(L), L);
-                    weigh<Cfg, 3>(g1[tb], g, sW[2], tb, L);
-                    weigh<Cfg, 3>(g2[tb], g, sW[3], tb, L);
-                }
-#pragma unroll
-                for (int s = 0; s < Cfg::KS; ++s)
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        f32x4 o1 = zero4(), o2 = zero4();
-#pragma unroll
-                        for (int tb = 0; tb < Cfg::C / 32; ++tb) {
-                            bf16x8 q[Cfg::NP];
-                            col_frag<Cfg, Cfg::KD>(q, sQ, tb, state_row_addr(s, u, L), L);
-                            mma<Cfg::NP, 3>(o1, q, g1[tb]);
-                            mma<Cfg::NP, 3>(o2, q, g2[tb]);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            part = __builtin_fmaf(S[s][u][e], o2[e], __builtin_fmaf(D[s][u][e], o1[e], part));
-                    }
-            }
-            // (S, D) after the chunk
-            each<Cfg>(D, [&](float x, int s, int u, int e) { return __builtin_fmaf((float)n, S[s][u][e], x); });
-            settle<Cfg>(D, m != 0, take, cy);
-            settle<Cfg>(S, m != 0, take, cy);
-#pragma unroll
-            for (int tb = 0; tb < Cfg::C / 32; ++tb) {
-                bf16x8 z[Cfg::NP], zw[3], zd[3];
-                col_frag<Cfg, Cfg::VD>(z, sV, tb, state_col_addr(L), L);
-                weigh<Cfg, 3>(zw, z, sW[0], tb, L);
-                weigh<Cfg, 3>(zd, z, sW[1], tb, L);
-#pragma unroll
-                for (int s = 0; s < Cfg::KS; ++s)
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        bf16x8 y[Cfg::NP];
-                        col_frag<Cfg, Cfg::KD>(y, sK, tb, state_row_addr(s, u, L), L);
-                        mma<Cfg::NP, 3>(S[s][u], y, zw);
-                        mma<Cfg::NP, 3>(D[s][u], y, zd);
-                    }
-            }
-        } else {
-            // ---- row by row
-            carry_state<Cfg>(S, Carry{before, 0.0f});
-            carry_state<Cfg>(D, Carry{before, 0.0f});
-            owed.none();
-            const Carry one = carry_by(sPw.of[1]);
-#pragma unroll 1
-            for (int i = 0; i < n; ++i) {
-                const bool begin = (m >> i) & 1ull;
-                each<Cfg>(D, [&](float x, int s, int u, int e) { return begin ? 0.0f : one(x + S[s][u][e]); });
-                each<Cfg>(S, [&](float x, int, int, int) { return begin ? 0.0f : one(x); });
-                const float v = tile_value<Cfg, Cfg::VD>(sV, i, state_col(L));
-                float dot = 0.0f;
-#pragma unroll
-                for (int s = 0; s < Cfg::KS; ++s) {
-                    float q[8], k[8];
-                    row_values<Cfg, Cfg::KD>(q, sQ, i, s, L);
-                    row_values<Cfg, Cfg::KD>(k, sK, i, s, L);
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) {
-                        S[s][x >> 2][x & 3] = __builtin_fmaf(k[x], v, S[s][x >> 2][x & 3]);
-                        dot = __builtin_fmaf(q[x], D[s][x >> 2][x & 3], dot);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-                // (nothing where the row begins: 0 times what is not finite stays out)
-                if (!begin) part = __builtin_fmaf(dot * p.scale, tile_value<Cfg, Cfg::VD>(sG, i, state_col(L)), part);
-            }
-        }
-        sum += (double)part;
-    }
-    L.again();
-    if (p.grad_state && seg == p.nseg - 1) {
-        State<Cfg> G;
-        load_state<Cfg>(G, p.grad_state + bh * words, vd, 1, kd, vd, L);
-        each<Cfg>(G, [&](float x, int s, int u, int e) {
-            sum += (double)D[s][u][e] * (double)x * owed.now;
-            return x;
-        });
-    }
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x, 64);
-    if (L.lane == 0) sSum[L.w] = sum;
-    __syncthreads();
-    if (L.tid == 0) {
-        double s = 0.0;
-#pragma unroll
-        for (int i = 0; i < Cfg::W; ++i) s += sSum[i];
-        p.part[bh * p.nseg + seg] = s;
-    }
-}
-
+// ------------------------------------------------------- gradient of the rates
 __global__ __launch_bounds__(256) void ret_alpha_kernel(const double* part, const float* alpha, float* out, int64_t B,
-                                                        int32_t H, int32_t nseg) {
+                                                        int32_t H, int32_t nparts) {
     __shared__ double sSum[4];
-    const int64_t h = blockIdx.x, n = B * nseg;
+    const int64_t h = blockIdx.x, n = B * nparts;
     double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += 256) sum += part[((i / nseg) * H + h) * nseg + i % nseg];
+    for (int64_t i = threadIdx.x; i < n; i += 256) sum += part[((i / nparts) * H + h) * nparts + i % nparts];
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x, 64);
     if ((threadIdx.x & 63) == 0) sSum[threadIdx.x >> 6] = sum;
@@ -795,18 +964,39 @@ hipError_t ret_summary_launch(int planes, const RetSummaryArgs& a, int64_t B, hi
     const dim3 grid((unsigned)(a.nseg - 1), (unsigned)a.H, (unsigned)B);
     with_cfg(planes, a.y.d, a.z.d, [&](auto cfg) {
         using Cfg = decltype(cfg);
-        const dim3 block(Cfg::THREADS);
-        if (a.dstates)
-            hipLaunchKernelGGL((ret_summary_kernel<Cfg, 3, true>), grid, block, 0, s, a);
-        else
+        with_planes<Cfg>(a.exact, [&](auto zp) {
+            hipLaunchKernelGGL((ret_summary_kernel<Cfg, decltype(zp)::value>), grid, dim3(Cfg::THREADS), 0, s, a);
+        });
+    });
+    return hipGetLastError();
+}
+
+hipError_t ret_prep_launch(int planes, const RetPrepArgs& a, int64_t B, hipStream_t s) {
+    const dim3 grid((unsigned)a.nseg, (unsigned)a.H, (unsigned)B);
+    with_cfg(planes, a.q.d, a.v.d, [&](auto cfg) {
+        using Cfg = RetCfg64<decltype(cfg)>;
+        using Whole = decltype(cfg);
+        const dim3 block(Cfg::THREADS), whole(Whole::THREADS);
+        if (!a.dstates) {
             with_planes<Cfg>(a.exact, [&](auto zp) {
-                hipLaunchKernelGGL((ret_summary_kernel<Cfg, decltype(zp)::value, false>), grid, block, 0, s, a);
+                hipLaunchKernelGGL((ret_prep_kernel<Cfg, decltype(zp)::value, false, true, true>), grid, block, 0, s, a);
             });
+        } else {
+            if constexpr (Cfg::KD == 128 && Cfg::VD == 128) {
+                hipLaunchKernelGGL((ret_prep_kernel<Whole, 3, true, true, false>), grid, whole, 0, s, a);
+                hipLaunchKernelGGL((ret_prep_kernel<Whole, 3, true, false, true>), grid, whole, 0, s, a);
+            } else {
+                hipLaunchKernelGGL((ret_prep_kernel<Cfg, 3, true, true, true>), grid, block, 0, s, a);
+            }
+            hipLaunchKernelGGL((ret_prep_rows_kernel<Cfg>), grid, block, 0, s, a);
+        }
     });
     return hipGetLastError();
 }
 
 namespace {
+// One group where there are few segments or many columns, else 32
+bool scan_one_group(int64_t words, int64_t heads, int64_t n) { return n <= 16 || heads * (words / 4) >= 16384; }
 template <int GROUPS, int RPT, bool DOT>
 void state_scan(const RetStateScanArgs& a, int64_t B, hipStream_t s) {
     constexpr int kCols = 256 / GROUPS;
@@ -815,13 +1005,22 @@ void state_scan(const RetStateScanArgs& a, int64_t B, hipStream_t s) {
 }
 template <bool DOT>
 void state_scan_for(const RetStateScanArgs& a, int64_t B, hipStream_t s) {
-    const int64_t columns = B * a.H * (a.words / 4);
-    if (a.n <= 4) state_scan<1, 4, DOT>(a, B, s);
-    else if (a.n <= 16 || columns >= 16384) state_scan<1, 16, DOT>(a, B, s);
-    else if (a.n <= 64) state_scan<32, 2, DOT>(a, B, s);
-    else state_scan<32, 4, DOT>(a, B, s);
+    const int n = DOT ? a.nseg : a.nseg - 1;
+    if (!scan_one_group(a.words, B * a.H, n)) {
+        if (n <= 64) state_scan<32, 2, DOT>(a, B, s);
+        else state_scan<32, 4, DOT>(a, B, s);
+    } else if (n <= 4) {
+        state_scan<1, 4, DOT>(a, B, s);
+    } else {
+        state_scan<1, 16, DOT>(a, B, s);
+    }
 }
 }  // namespace
+
+int64_t ret_scan_parts(int64_t words, int64_t heads, int64_t nseg) {
+    const int64_t cols = scan_one_group(words, heads, nseg) ? 256 : 256 / 32;
+    return (words / 4 + cols - 1) / cols;
+}
 
 hipError_t ret_state_scan_launch(const RetStateScanArgs& a, int64_t B, hipStream_t s) {
     if (a.dstates) state_scan_for<true>(a, B, s);
@@ -829,18 +1028,9 @@ hipError_t ret_state_scan_launch(const RetStateScanArgs& a, int64_t B, hipStream
     return hipGetLastError();
 }
 
-hipError_t ret_sens_launch(int planes, const RetSensArgs& a, int64_t B, hipStream_t s) {
-    const dim3 grid((unsigned)a.nseg, (unsigned)a.H, (unsigned)B);
-    with_cfg(planes, a.q.d, a.v.d, [&](auto cfg) {
-        using Cfg = decltype(cfg);
-        hipLaunchKernelGGL((ret_sens_kernel<Cfg>), grid, dim3(Cfg::THREADS), 0, s, a);
-    });
-    return hipGetLastError();
-}
-
-hipError_t ret_alpha_launch(const double* part, const float* alpha, float* out, int64_t B, int32_t H, int32_t nseg,
+hipError_t ret_alpha_launch(const double* part, const float* alpha, float* out, int64_t B, int32_t H, int32_t nparts,
                             hipStream_t s) {
-    hipLaunchKernelGGL(ret_alpha_kernel, dim3((unsigned)H), dim3(256), 0, s, part, alpha, out, B, H, nseg);
+    hipLaunchKernelGGL(ret_alpha_kernel, dim3((unsigned)H), dim3(256), 0, s, part, alpha, out, B, H, nparts);
     return hipGetLastError();
 }
 

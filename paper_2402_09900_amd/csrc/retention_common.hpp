@@ -51,7 +51,7 @@ template <int NP_, int KD_, int VD_>
 struct RetCfg {
     static constexpr int NP = NP_, KD = KD_, VD = VD_;
     static constexpr int C = ret_chunk(NP);
-    static constexpr int W = VD / 16, THREADS = 64 * W;
+    static constexpr int CW = VD / 16, W = CW, THREADS = 64 * W;   // wavefronts per state's columns, in all
     static constexpr int ES = NP == 1 ? 2 : 4;        // bytes of an element in memory
     static constexpr int EPU = 16 / ES;               // elements of a 16-byte unit
     static constexpr int NB = C / 16;                 // 16-row blocks
@@ -59,8 +59,17 @@ struct RetCfg {
     static constexpr int KS = KD / 32;                // steps of a product over kd
 };
 
+// The same for a workgroup that holds several states: 64 of a state's rows per
+// wavefront, (KD / 64) (VD / 16) wavefronts, so that four states fit.  (No product
+// over the state's rows is taken there, so nothing is added up across wavefronts.)
+template <class Cfg>
+struct RetCfg64 : Cfg {
+    static constexpr int W = Cfg::CW * (Cfg::KD / 64), THREADS = 64 * W, KS = 2;
+};
+
 struct RetLane {
     int tid, lane, w, g, c;
+    int k0 = 0;                                       // first state row of the wavefront
     __device__ RetLane() {
         tid = threadIdx.x;
         w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -138,8 +147,7 @@ __device__ __forceinline__ void mma(f32x4& acc, const bf16x8 (&a)[NA], const bf1
 __device__ __forceinline__ f32x4 zero4() { return f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }
 
 // --------------------------------------------------------- chunks in memory
-// n rows of one head of a [T][heads][d] tensor as a buffer, from the row at the
-// lowest address on; walking backwards row i is the (n - 1 - i)-th of them.  Rows
+// n rows of one head of a [T][heads][d] tensor as a buffer, from step t0 on; walking backwards row i is the (n - 1 - i)-th of them.  Rows
 // at or past n lie outside the buffer (backwards: below offset 0, which wraps
 // past its end), columns at or past d are sent there: they read as zeros and drop
 // their stores.
@@ -150,11 +158,9 @@ struct RetRows {
         return col < d ? (uint32_t)(first + row * step + col * es) : kOob;
     }
 };
-__device__ __forceinline__ RetRows ret_rows(const void* head0, int64_t row_bytes, int d, int es, int64_t w0, int n,
-                                            int64_t T, bool rev) {
-    const int64_t t = rev ? T - w0 - n : w0;
+__device__ __forceinline__ RetRows ret_rows(const void* head0, int64_t row_bytes, int d, int es, int t0, int n, bool rev) {
     const int rb = (int)row_bytes, end = (n - 1) * rb;
-    return RetRows{make_rsrc((const char*)head0 + t * row_bytes, n > 0 ? (int64_t)end + d * es : 0), rev ? end : 0,
+    return RetRows{make_rsrc((const char*)head0 + t0 * row_bytes, n > 0 ? (int64_t)end + d * es : 0), rev ? end : 0,
                    rev ? -rb : rb, d};
 }
 
@@ -200,12 +206,16 @@ struct RetTile {
             for (int e = 0; e < 4; ++e) any |= (u[i][e] & kExp) + kOne;
         return any & (Cfg::NP == 1 ? 0x80008000u : 0x80000000u);
     }
-    // into an LDS tile of NP planes, rows before `from` as zeros
-    __device__ __forceinline__ void stage(uint16_t* s, int from, const RetLane& L) {
-        if (from > 0)
+    // rows from .. to - 1 stay, the others become zeros
+    __device__ __forceinline__ void keep(int from, int to, const RetLane& L) {
 #pragma unroll
-            for (int i = 0; i < UN; ++i)
-                if (L.tid / UPR + i * RS < from) u[i] = u32x4{0u, 0u, 0u, 0u};
+        for (int i = 0; i < UN; ++i) {
+            const int row = L.tid / UPR + i * RS;
+            if (row < from || row >= to) u[i] = u32x4{0u, 0u, 0u, 0u};
+        }
+    }
+    // into an LDS tile of NP planes
+    __device__ __forceinline__ void stage(uint16_t* s, const RetLane& L) const {
 #pragma unroll
         for (int i = 0; i < UN; ++i) {
             const int row = L.tid / UPR + i * RS, col = L.tid % UPR * Cfg::EPU;
@@ -225,13 +235,13 @@ struct RetTile {
 };
 
 // ------------------------------------------------------------ LDS operands
-// columns 32 s + 8 g .. + 7 of one row as floats, the same in the 16 lanes of g
+// columns k0 + 32 s + 8 g .. + 7 of one row as floats, the same in the 16 lanes of g
 template <class Cfg, int D>
 __device__ __forceinline__ void row_values(float (&v)[8], const uint16_t* t, int row, int s, const RetLane& L) {
     bf16x8 f[Cfg::NP];
 #pragma unroll
     for (int p = 0; p < Cfg::NP; ++p)
-        f[p] = *(const bf16x8*)(t + p * Cfg::C * D + row * D + swizzled<D>(4 * s + L.g, row) * 8);
+        f[p] = *(const bf16x8*)(t + p * Cfg::C * D + row * D + swizzled<D>(L.k0 / 8 + 4 * s + L.g, row) * 8);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = plane_value<Cfg::NP>(f, e);
 }
@@ -273,8 +283,12 @@ using State = f32x4[Cfg::KS][2];
 
 __device__ __forceinline__ int state_col(const RetLane& L) { return 16 * L.w + L.c; }
 __device__ __forceinline__ int state_col_addr(const RetLane& L) { return 16 * L.w + 4 * (L.c & 3); }
-__device__ __forceinline__ int state_row(int s, int u, int r, const RetLane& L) { return 32 * s + 8 * L.g + 4 * u + r; }
-__device__ __forceinline__ int state_row_addr(int s, int u, const RetLane& L) { return 32 * s + 8 * (L.c & 3) + 4 * u; }
+__device__ __forceinline__ int state_row(int s, int u, int r, const RetLane& L) {
+    return L.k0 + 32 * s + 8 * L.g + 4 * u + r;
+}
+__device__ __forceinline__ int state_row_addr(int s, int u, const RetLane& L) {
+    return L.k0 + 32 * s + 8 * (L.c & 3) + 4 * u;
+}
 
 template <class Cfg, class F>
 __device__ __forceinline__ void each(State<Cfg>& S, F&& f) {
@@ -388,13 +402,12 @@ __device__ __forceinline__ void settle(State<Cfg>& S, bool begins, bool take, Ca
 }
 
 // ----------------------------------------------------------------- begins
-// The begin flag of row `lane` of a chunk in walking order, 0 past its n rows:
-// backwards row i is step t = T - 1 - w0 - i and begins if step t + 1 does (the last
-// step goes on from what follows the tape).
-__device__ __forceinline__ uint32_t ret_flag(const uint8_t* start, int64_t w0, int n, int64_t T, bool rev, int lane) {
-    const int64_t t0 = rev ? T - w0 - (n - 1) : w0;        // the lowest step looked at
-    const int64_t left = T - t0;
-    const Rsrc r = make_rsrc(start + t0, n <= 0 ? 0 : left < n ? left : n);
+// The begin flag of row `lane` of a chunk of n steps from t0 on, 0 past them:
+// backwards row i is step t0 + n - 1 - i and begins if the step after it does (the
+// last step of the tape goes on from what follows it).
+__device__ __forceinline__ uint32_t ret_flag(const uint8_t* start, int t0, int n, int T, bool rev, int lane) {
+    const int low = rev ? t0 + 1 : t0, left = T - low;     // the lowest step looked at
+    const Rsrc r = make_rsrc(start + low, n <= 0 ? 0 : left < n ? left : n);
     return bload_u8(r, (uint32_t)(rev ? n - 1 - lane : lane));
 }
 __device__ __forceinline__ uint64_t upto(int i) { return (2ull << i) - 1ull; }          // bits 0 .. i
