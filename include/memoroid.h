@@ -387,7 +387,7 @@ int memoroid_scan_linattn_bwd(const float* q, const float* k, const float* v,
  *              not written when T is 0.
  *   scale      finite (MEMOROID_EINVAL otherwise).
  *   dk, dv     multiples of 8 up to 128 (MEMOROID_EUNSUPPORTED otherwise);
- *              B, H <= 65535.  Arrays 16-byte aligned.
+ *              B <= 32767, H <= 65535, B H < 2^29.  Arrays 16-byte aligned.
  *   bf16: products of bf16 inputs, fp32 states and sums; the weights of pairs and
  *   the state as a row reads it are rounded to bf16 once each.  The states out
  *   are fp32 results.  fp32: fp32 precision throughout.
@@ -442,7 +442,7 @@ int memoroid_scan_retention_bwd(const void* q, const void* k, const void* v, con
  *
  *   q [B][H][dk], k [B][Hk][dk], v [B][Hk][dv], out [B][H][dv] of dtype;
  *   alpha [H], state [B][H][dk][dv] fp32;  start: optional [B] begin flags (NULL:
- *   no row begins).  Limits as for memoroid_scan_retention; B may exceed 65535
+ *   no row begins).  Limits as for memoroid_scan_retention; B may be larger
  *   as long as B * H * ceil(dv / 32) is below 2^31.
  * ------------------------------------------------------------------------ */
 int memoroid_retention_step(const void* q, const void* k, const void* v, const float* alpha,

@@ -931,7 +931,10 @@ bool ret_dims_ok(int64_t dk, int64_t dv) {
 }
 // grid extents; a chunk's rows are addressed with 32-bit offsets below 2^31
 // (64 rows of 65535 heads of 128 floats are 2147450880 bytes)
-bool ret_extents_ok(int64_t B, int64_t T, int64_t H) { return B <= 65535 && H <= 65535 && T <= (int64_t)INT32_MAX / 2; }
+// and the walks' tasks (at most 512 / (B H) + 1 segments each) are one grid
+bool ret_extents_ok(int64_t B, int64_t T, int64_t H) {
+    return B <= 32767 && H <= 65535 && T <= (int64_t)INT32_MAX / 2 && B * H <= (int64_t)INT32_MAX / 4;
+}
 int ret_planes(int dtype) { return dtype == MEMOROID_BF16 ? 1 : dtype == MEMOROID_F32 ? 3 : 0; }
 
 // One array of segment states: [B][H][nseg][dk][dv] floats
@@ -954,7 +957,7 @@ struct RetBwdPlan {
     RetPlan fwd;
     int64_t nparts = 0;
     bool prep = false;           // a pass for the segments' states or the rates' gradient
-    size_t off_states = 0, off_rstates = 0, off_dstates = 0, off_estates = 0, off_R = 0, off_bad = 0, off_part = 0,
+    size_t off_states = 0, off_rstates = 0, off_rscan = 0, off_dstates = 0, off_estates = 0, off_R = 0, off_part = 0,
            off_gk = 0, off_gv = 0, total = 0;
 };
 
@@ -969,14 +972,14 @@ bool plan_retention_bwd(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t dk,
     if (p->prep) off += states;
     p->off_rstates = off;
     if (p->prep) off += states;
+    p->off_rscan = off;                                    // (without alpha: in place)
+    if (want_alpha) off += states;
     p->off_dstates = off;
     if (want_alpha) off += states;
     p->off_estates = off;
     if (want_alpha) off += states;
     p->off_R = off;
     off = align_up(off + (size_t)B * (size_t)p->fwd.nseg);
-    p->off_bad = off;
-    if (want_alpha) off = align_up(off + (size_t)B * (size_t)H * (size_t)p->fwd.nseg);
     p->off_part = off;
     if (want_alpha) off = align_up(off + (size_t)B * (size_t)H * (size_t)p->nparts * 8);
     p->off_gk = off;                                       // shared heads: gradients per query head
@@ -1080,16 +1083,19 @@ int memoroid_scan_retention(const void* q, const void* k, const void* v, const f
         RetStateScanArgs c{};
         c.alpha = alpha;
         c.seed = state_in;
-        c.states = states;
+        c.states = c.out = states;
         c.R = m.R;
         c.rows = p.rows;
         c.last_rows = T - (int64_t)(p.nseg - 1) * p.rows;
         c.words = (int32_t)(dk * dv);
         c.H = (int32_t)H;
         c.nseg = p.nseg;
-        if (ret_state_scan_launch(c, B, s) != hipSuccess) return MEMOROID_EHIP;
+        if (ret_state_scan_launch(c, nullptr, B, s) != hipSuccess) return MEMOROID_EHIP;
     }
-    RetWalkArgs a{};
+    RetWalkSet set{};
+    set.n = 1;
+    set.H = (int32_t)H;
+    RetWalkArgs& a = set.w[0];
     a.x = ret_role(q, H, dk, 1);
     a.y = rk;
     a.z = rv;
@@ -1112,7 +1118,7 @@ int memoroid_scan_retention(const void* q, const void* k, const void* v, const f
         a.hdr = (WsHeader*)ws;
         a.sig = sig;
     }
-    return check_hip(ret_walk_launch(p.planes, a, B, s));
+    return check_hip(ret_walk_launch(p.planes, set, B, s));
 }
 
 size_t memoroid_scan_retention_bwd_workspace_bytes(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t dk, int64_t dv,
@@ -1155,6 +1161,7 @@ int memoroid_scan_retention_bwd(const void* q, const void* k, const void* v, con
                   rg = ret_role(grad_out, H, dv, 1);
     float* const states = (float*)(ws + bp.off_states);
     float* const rstates = (float*)(ws + bp.off_rstates);
+    float* const rscan = grad_alpha ? (float*)(ws + bp.off_rscan) : rstates;
     if (bp.prep) {
         RetPrepArgs m{};
         m.q = rq;
@@ -1169,7 +1176,6 @@ int memoroid_scan_retention_bwd(const void* q, const void* k, const void* v, con
         m.estates = (float*)(ws + bp.off_estates);
         m.part = (double*)(ws + bp.off_part);
         m.R = (uint8_t*)(ws + bp.off_R);
-        m.bad = (uint8_t*)(ws + bp.off_bad);
         m.scale = scale;
         m.T = T;
         m.H = (int32_t)H;
@@ -1188,26 +1194,20 @@ int memoroid_scan_retention_bwd(const void* q, const void* k, const void* v, con
         c.words = (int32_t)(dk * dv);
         c.H = (int32_t)H;
         c.nseg = p.nseg;
-        // forwards first: it reads U before the scan backwards replaces it
+        RetStateScanArgs back = c;
         c.seed = state_in;
-        c.states = states;
+        c.states = c.out = states;
         c.dstates = m.dstates;
         c.rstates = rstates;
         c.estates = m.estates;
         c.grad_state = grad_state_out;
         c.part = m.part;
         c.nparts = m.nparts;
-        if (ret_state_scan_launch(c, B, s) != hipSuccess) return MEMOROID_EHIP;
-        if (grad_alpha &&
-            ret_alpha_launch(m.part, alpha, grad_alpha, B, (int32_t)H, m.nparts, s) != hipSuccess)
-            return MEMOROID_EHIP;
-        if (p.nseg > 1) {
-            c.rev = 1;
-            c.seed = grad_state_out;
-            c.states = rstates;
-            c.dstates = nullptr;
-            if (ret_state_scan_launch(c, B, s) != hipSuccess) return MEMOROID_EHIP;
-        }
+        back.rev = 1;
+        back.seed = grad_state_out;
+        back.states = rstates;
+        back.out = rscan;
+        if (ret_state_scan_launch(c, p.nseg > 1 ? &back : nullptr, B, s) != hipSuccess) return MEMOROID_EHIP;
     }
     RetWalkArgs a{};
     a.start = start;
@@ -1218,51 +1218,68 @@ int memoroid_scan_retention_bwd(const void* q, const void* k, const void* v, con
     a.nseg = p.nseg;
     a.chunks = p.chunks;
     // dq = W(dout, v, k) from the carried state, whose rows are v's columns here
-    a.x = rg;
-    a.y = rv;
-    a.z = rk;
-    a.out = grad_q;
-    a.seed = state_in;
-    a.states = states;
-    a.sk = 1;
-    a.sv = (int32_t)dv;
-    a.inter_scale = scale;
-    a.z_scale = 1.0f;
-    if (!bp.prep) {
-        a.hdr = (WsHeader*)ws;
-        a.sig = sig;
-    }
-    if (ret_walk_launch(p.planes, a, B, s) != hipSuccess) return MEMOROID_EHIP;
-    a.hdr = nullptr;
+    RetWalkArgs wq = a;
+    wq.x = rg;
+    wq.y = rv;
+    wq.z = rk;
+    wq.out = grad_q;
+    wq.seed = state_in;
+    wq.states = states;
+    wq.sk = 1;
+    wq.sv = (int32_t)dv;
+    wq.inter_scale = scale;
+    wq.z_scale = 1.0f;
     // dk = W(v, dout, q) and dv = W(k, q, dout), backwards; the state takes the
     // scale, since the gradient of the state after the tape has none
-    a.rev = 1;
-    a.out_f32 = G > 1;
-    a.seed = grad_state_out;
-    a.states = rstates;
-    a.inter_scale = 1.0f;
-    a.z_scale = scale;
-    a.x = rv;
-    a.y = rg;
-    a.z = rq;
-    a.out = G > 1 ? (void*)(ws + bp.off_gk) : grad_k;
-    if (ret_walk_launch(p.planes, a, B, s) != hipSuccess) return MEMOROID_EHIP;
-    a.x = rk;
-    a.y = rq;
-    a.z = rg;
-    a.out = G > 1 ? (void*)(ws + bp.off_gv) : grad_v;
-    a.sk = (int32_t)dv;
-    a.sv = 1;
-    a.fin = grad_state_in;
-    a.exact = grad_state_in != nullptr;
-    if (ret_walk_launch(p.planes, a, B, s) != hipSuccess) return MEMOROID_EHIP;
+    RetWalkArgs wk = a;
+    wk.rev = 1;
+    wk.out_f32 = G > 1;
+    wk.seed = grad_state_out;
+    wk.states = rscan;
+    wk.inter_scale = 1.0f;
+    wk.z_scale = scale;
+    RetWalkArgs wv = wk;
+    wk.x = rv;
+    wk.y = rg;
+    wk.z = rq;
+    wk.out = G > 1 ? (void*)(ws + bp.off_gk) : grad_k;
+    wk.sk = 1;
+    wk.sv = (int32_t)dv;
+    wv.x = rk;
+    wv.y = rq;
+    wv.z = rg;
+    wv.out = G > 1 ? (void*)(ws + bp.off_gv) : grad_v;
+    wv.sk = (int32_t)dv;
+    wv.sv = 1;
+    wv.fin = grad_state_in;
+    wv.exact = grad_state_in != nullptr;
+    RetWalkSet set{};
+    set.H = (int32_t)H;
+    set.nparts = (int32_t)bp.nparts;
+    set.part = (const double*)(ws + bp.off_part);
+    set.grad_alpha = grad_alpha;
+    if (!bp.prep) {                                        // the first kernel prepares the header
+        wk.hdr = (WsHeader*)ws;
+        wk.sig = sig;
+    }
+    set.w[0] = wk;
+    set.w[1] = wq;
+    set.w[2] = wv;
+    set.n = ret_same_tiles(dv, dk, dk, dv) ? 3 : 2;
+    if (ret_walk_launch(p.planes, set, B, s) != hipSuccess) return MEMOROID_EHIP;
+    if (set.n == 2) {
+        set.w[0] = wv;
+        set.n = 1;
+        set.grad_alpha = nullptr;
+        if (ret_walk_launch(p.planes, set, B, s) != hipSuccess) return MEMOROID_EHIP;
+    }
     if (G > 1) {
-        if (ret_share_launch(p.planes, (const float*)(ws + bp.off_gk), grad_k, B * T, (int32_t)Hk, (int32_t)G,
-                             (int32_t)dk, s) != hipSuccess)
-            return MEMOROID_EHIP;
-        if (ret_share_launch(p.planes, (const float*)(ws + bp.off_gv), grad_v, B * T, (int32_t)Hk, (int32_t)G,
-                             (int32_t)dv, s) != hipSuccess)
-            return MEMOROID_EHIP;
+        RetShareArgs h{};
+        h.k = {(const float*)(ws + bp.off_gk), grad_k, (int32_t)dk};
+        h.v = {(const float*)(ws + bp.off_gv), grad_v, (int32_t)dv};
+        h.rows = B * T * Hk;
+        h.G = (int32_t)G;
+        if (ret_share_launch(p.planes, h, s) != hipSuccess) return MEMOROID_EHIP;
     }
     return MEMOROID_OK;
 }
@@ -1271,7 +1288,7 @@ int memoroid_retention_step(const void* q, const void* k, const void* v, const f
                             float* state, void* out, float scale, int64_t B, int64_t H, int64_t Hk, int64_t dk,
                             int64_t dv, int dtype, void* stream) {
     bool empty;
-    const int ok = ret_check(B < 65536 ? B : 65535, 1, H, Hk, dk, dv, scale, dtype, &empty);
+    const int ok = ret_check(B > 1 ? 1 : B, 1, H, Hk, dk, dv, scale, dtype, &empty);
     if (ok != MEMOROID_OK || empty) return ok;
     int64_t groups;
     if (!mul_ok(B, H * ((dv + 31) / 32), &groups) || groups > (int64_t)INT32_MAX) return MEMOROID_EUNSUPPORTED;

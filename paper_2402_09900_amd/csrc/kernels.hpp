@@ -326,6 +326,15 @@ struct RetWalkArgs {
     WsHeader* hdr;              // header to prepare with sig, or NULL
     uint64_t sig;
 };
+// Up to three walks over the same tapes and segments with states of the same tiles,
+// in one launch, and the sum of the rates' gradients (grad_alpha or NULL)
+struct RetWalkSet {
+    RetWalkArgs w[3];
+    int32_t n, H, nparts;
+    const double* part;         // [B][H][nparts]
+    float* grad_alpha;
+    int64_t B, tasks, blocks;   // (set by the launch)
+};
 // what the segments but the last add to the state
 struct RetSummaryArgs {
     RetRole y, z;
@@ -350,7 +359,6 @@ struct RetPrepArgs {
     float* estates;
     double* part;               // [B][H][nparts], a segment's own share first
     uint8_t* R;
-    uint8_t* bad;               // [B][H][nseg] a segment holds a value that is not finite
     float scale;
     int64_t T;
     int32_t H, nseg, chunks, nparts;
@@ -361,8 +369,9 @@ struct RetPrepArgs {
 struct RetStateScanArgs {
     const float* alpha;
     const float* seed;          // as in RetWalkArgs
-    float* states;              // scanned in place
-    float* dstates;             // likewise, or NULL
+    const float* states;
+    float* out;                 // the scanned states (may be `states`)
+    float* dstates;             // scanned in place, or NULL
     const float* rstates;       // with dstates: U and E, for
     const float* estates;
     const float* grad_state;    // (optional)
@@ -371,18 +380,27 @@ struct RetStateScanArgs {
     int64_t rows, last_rows;    // steps of a segment, of the last one
     int32_t words, H, nseg, nparts, rev;   // floats of a state
 };
-hipError_t ret_walk_launch(int planes, const RetWalkArgs& a, int64_t B, hipStream_t s);
+// Gradients of shared heads: out[step][kh][.] = sum of part[step][kh G + 0 .. G - 1][.],
+// rounded to bf16 if planes == 1, for k and v
+struct RetShareArgs {
+    struct Part {
+        const float* part;
+        void* out;
+        int32_t d;
+    } k, v;
+    int64_t rows;               // steps times key heads
+    int32_t G;
+};
+hipError_t ret_walk_launch(int planes, RetWalkSet set, int64_t B, hipStream_t s);
+// whether states of kd0 x vd0 and kd1 x vd1 take the same tiles
+bool ret_same_tiles(int64_t kd0, int64_t vd0, int64_t kd1, int64_t vd1);
 hipError_t ret_summary_launch(int planes, const RetSummaryArgs& a, int64_t B, hipStream_t s);
-hipError_t ret_state_scan_launch(const RetStateScanArgs& a, int64_t B, hipStream_t s);
+// with `back`, a scan backwards of as many segments beside it
+hipError_t ret_state_scan_launch(const RetStateScanArgs& a, const RetStateScanArgs* back, int64_t B, hipStream_t s);
 hipError_t ret_prep_launch(int planes, const RetPrepArgs& a, int64_t B, hipStream_t s);
 // workgroups of a state scan per head
 int64_t ret_scan_parts(int64_t words, int64_t heads, int64_t nseg);
-// grad_alpha[h] = -sign(alpha_h) sum of part over tapes
-hipError_t ret_alpha_launch(const double* part, const float* alpha, float* out, int64_t B, int32_t H, int32_t nparts,
-                            hipStream_t s);
-// out[row][kh][.] = sum of part[row][kh G + 0 .. G - 1][.], rounded to bf16 if planes == 1
-hipError_t ret_share_launch(int planes, const float* part, void* out, int64_t rows, int32_t heads, int32_t G, int32_t d,
-                            hipStream_t s);
+hipError_t ret_share_launch(int planes, const RetShareArgs& a, hipStream_t s);
 
 struct RetStepArgs {
     const void* q;              // [B][H][dk]

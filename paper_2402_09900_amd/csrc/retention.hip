@@ -199,8 +199,74 @@ __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummary
 //
 // A value that is not finite would reach other episodes and earlier rows through
 // zero weights.  Without ALPHA the rows that take no part become zeros.  With
-// ALPHA, where every row takes part in something, the segment is marked and done
-// again row by row by ret_prep_rows_kernel.
+// ALPHA, where every row takes part in something, the segment is done again row by
+// row.
+// The sums of ret_prep_kernel, with ALPHA, of a segment that holds a value that is not
+// finite, by the recurrences themselves in floats.  Returns this lane's part.
+template <class Cfg, bool FWD, bool BACK>
+__device__ __forceinline__ double prep_rows(const RetPrepArgs& p, const Run<Cfg>& run, const Head& hq, const Head& hk,
+                                            const Head& hv, const Head& hg, const uint8_t* start, double rate,
+                                            uint16_t* sQ, uint16_t* sK, uint16_t* sV, uint16_t* sG, State<Cfg>& S,
+                                            State<Cfg>& D, State<Cfg>& U, State<Cfg>& E, const RetLane& L) {
+    const Carry one = carry_of(rate, 1.0);
+    zero_state<Cfg>(S);
+    zero_state<Cfg>(D);
+    zero_state<Cfg>(U);
+    zero_state<Cfg>(E);
+    bool open = true;
+    double sum = 0.0;
+#pragma unroll 1
+    for (int ch = 0; ch < run.nch; ++ch) {
+        RetTile<Cfg, Cfg::KD> tq, tk;
+        RetTile<Cfg, Cfg::VD> tv, tg;
+        const int t0 = run.first(ch), n = run.rows(ch);
+        const uint64_t m = __ballot(ret_flag(start, t0, n, (int)p.T, false, L.lane) != 0u);
+        tq.fetch(rows_of<Cfg>(hq, t0, n), L);
+        if (FWD) tk.fetch(rows_of<Cfg>(hk, t0, n), L);
+        if (FWD) tv.fetch(rows_of<Cfg>(hv, t0, n), L);
+        tg.fetch(rows_of<Cfg>(hg, t0, n), L);
+        __syncthreads();
+        tq.stage(sQ, L);
+        if (FWD) tk.stage(sK, L);
+        if (FWD) tv.stage(sV, L);
+        tg.stage(sG, L);
+        __syncthreads();
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
+            const int t = ch * Cfg::C + i;                 // steps since r0
+            const bool begin = (m >> i) & 1ull;
+            open = open && !(begin && t > 0);
+            const float f = decay_pow(rate, (double)t) * p.scale;
+            const float v = FWD ? tile_value<Cfg, Cfg::VD>(sV, i, state_col(L)) : 0.0f;
+            const float g = tile_value<Cfg, Cfg::VD>(sG, i, state_col(L));
+            float dot = 0.0f;
+#pragma unroll
+            for (int s = 0; s < Cfg::KS; ++s) {
+                float q[8], k[8];
+                row_values<Cfg, Cfg::KD>(q, sQ, i, s, L);
+                if (FWD) row_values<Cfg, Cfg::KD>(k, sK, i, s, L);
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    const int u = x >> 2, e = x & 3;
+                    if (FWD) {
+                        const float d = begin ? 0.0f : one(D[s][u][e] + S[s][u][e]);
+                        D[s][u][e] = d;
+                        S[s][u][e] = __builtin_fmaf(k[x], v, begin ? 0.0f : one(S[s][u][e]));
+                        dot = __builtin_fmaf(q[x], d, dot);
+                    }
+                    if (BACK) {
+                        const float o = q[x] * (f * g);
+                        U[s][u][e] = open ? U[s][u][e] + o : U[s][u][e];
+                        E[s][u][e] = open && t > 0 ? __builtin_fmaf((float)t, o, E[s][u][e]) : E[s][u][e];
+                    }
+                }
+            }
+            if (!begin && t > 0) sum += (double)(dot * p.scale * g);
+        }
+    }
+    return sum;
+}
+
 template <class Cfg, int ZP, bool ALPHA, bool FWD, bool BACK>
 __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void ret_prep_kernel(RetPrepArgs p) {
     __shared__ __attribute__((aligned(16))) uint16_t sQ[Cfg::NP * Cfg::C * Cfg::KD];
@@ -260,7 +326,8 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void re
         const int n = run.rows(ch);
         const uint64_t m = __ballot(flag != 0u);
         if (ch == 0 && (m & 1ull)) begins |= kSegBeginsFirst;
-        if (ALPHA && FWD) bad |= tq.bad() | tk.bad() | tv.bad() | tg.bad();
+        if (ALPHA) bad |= tq.bad() | tg.bad();
+        if (ALPHA && FWD) bad |= tk.bad() | tv.bad();
         const uint64_t mo = ch == 0 ? m & ~1ull : m;   // a begin at r0 separates nothing from it
         if (m) begins |= kSegBegins;
         if (mo) begins |= kSegBeginsBack;
@@ -386,9 +453,17 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void re
     }
     L.again();
     const int64_t words = (int64_t)kd * vd, bh = b * p.H + h, at = (bh * p.nseg + seg) * words;
-    if (FWD) store_state<Cfg>(S, p.states + at, vd, 1, kd, vd, (float)owed.now, false, L);
+    float now = (float)owed.now;
+    if constexpr (ALPHA) {
+        // a value that is not finite, in the inputs or by overflow
+        if (__syncthreads_or(bad != 0u || !(fabs(sum) < (double)__builtin_inff()))) {
+            sum = prep_rows<Cfg, FWD, BACK>(p, run, hq, hk, hv, hg, start, rate, sQ, sK, sV, sG, S, D, U, E, L);
+            now = 1.0f;
+        }
+    }
+    if (FWD) store_state<Cfg>(S, p.states + at, vd, 1, kd, vd, now, false, L);
     if (BACK) store_state<Cfg>(U, p.rstates + at, vd, 1, kd, vd, 1.0f, false, L);
-    if (FWD && ALPHA) store_state<Cfg>(D, p.dstates + at, vd, 1, kd, vd, (float)owed.now, false, L);
+    if (FWD && ALPHA) store_state<Cfg>(D, p.dstates + at, vd, 1, kd, vd, now, false, L);
     if (BACK && ALPHA) store_state<Cfg>(E, p.estates + at, vd, 1, kd, vd, 1.0f, false, L);
     if (FWD && ALPHA) {
 #pragma unroll
@@ -401,10 +476,6 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void re
             for (int i = 0; i < Cfg::W; ++i) s += sSum[i];
             p.part[bh * p.nparts + seg] = s;
         }
-        // a value that is not finite, in the inputs or by overflow: the segment is done
-        // again by ret_prep_rows_kernel
-        const bool any_bad = __syncthreads_or(bad != 0u || !(fabs(sum) < (double)__builtin_inff())) != 0;
-        if (L.tid == 0) p.bad[bh * p.nseg + seg] = any_bad;
     }
     if (FWD && h == 0 && L.tid == 0) {
         if (run.r1 < p.T && start[run.r1] != 0) begins |= kSegBeginsBack;
@@ -412,98 +483,8 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void re
     }
 }
 
-// The same, with ALPHA, of the segments that hold a value that is not finite, by the
-// recurrences themselves in floats.
-template <class Cfg>
-__global__ __launch_bounds__(Cfg::THREADS) void ret_prep_rows_kernel(RetPrepArgs p) {
-    const int64_t seg = blockIdx.x, h = blockIdx.y, b = blockIdx.z, bh = b * p.H + h;
-    if (!p.bad[bh * p.nseg + seg]) return;
-    __shared__ __attribute__((aligned(16))) uint16_t sQ[Cfg::NP * Cfg::C * Cfg::KD];
-    __shared__ __attribute__((aligned(16))) uint16_t sK[Cfg::NP * Cfg::C * Cfg::KD];
-    __shared__ __attribute__((aligned(16))) uint16_t sV[Cfg::NP * Cfg::C * Cfg::VD];
-    __shared__ __attribute__((aligned(16))) uint16_t sG[Cfg::NP * Cfg::C * Cfg::VD];
-    __shared__ double sSum[Cfg::W];
-    RetLane L;
-    const int wave = L.w;
-    L.k0 = wave / Cfg::CW * 64;
-    L.w = wave % Cfg::CW;
-    const double rate = fabs((double)p.alpha[h]);
-    const Carry one = carry_of(rate, 1.0);
-    const int kd = p.q.d, vd = p.v.d;
-    const Head hq = head_of<Cfg>(p.q, b, h, p.T), hk = head_of<Cfg>(p.k, b, h, p.T), hv = head_of<Cfg>(p.v, b, h, p.T),
-               hg = head_of<Cfg>(p.g, b, h, p.T);
-    const uint8_t* const start = p.start + b * p.T;
-    const Run<Cfg> run((int)seg, p.chunks, (int)p.T, 0);
-    State<Cfg> S, D, U, E;
-    zero_state<Cfg>(S);
-    zero_state<Cfg>(D);
-    zero_state<Cfg>(U);
-    zero_state<Cfg>(E);
-    bool open = true;
-    double sum = 0.0;
-#pragma unroll 1
-    for (int ch = 0; ch < run.nch; ++ch) {
-        RetTile<Cfg, Cfg::KD> tq, tk;
-        RetTile<Cfg, Cfg::VD> tv, tg;
-        const int t0 = run.first(ch), n = run.rows(ch);
-        const uint64_t m = __ballot(ret_flag(start, t0, n, (int)p.T, false, L.lane) != 0u);
-        tq.fetch(rows_of<Cfg>(hq, t0, n), L);
-        tk.fetch(rows_of<Cfg>(hk, t0, n), L);
-        tv.fetch(rows_of<Cfg>(hv, t0, n), L);
-        tg.fetch(rows_of<Cfg>(hg, t0, n), L);
-        __syncthreads();
-        tq.stage(sQ, L);
-        tk.stage(sK, L);
-        tv.stage(sV, L);
-        tg.stage(sG, L);
-        __syncthreads();
-#pragma unroll 1
-        for (int i = 0; i < n; ++i) {
-            const int t = ch * Cfg::C + i;                 // steps since r0
-            const bool begin = (m >> i) & 1ull;
-            open = open && !(begin && t > 0);
-            const float f = decay_pow(rate, (double)t) * p.scale;
-            const float v = tile_value<Cfg, Cfg::VD>(sV, i, state_col(L)), g = tile_value<Cfg, Cfg::VD>(sG, i, state_col(L));
-            float dot = 0.0f;
-#pragma unroll
-            for (int s = 0; s < Cfg::KS; ++s) {
-                float q[8], k[8];
-                row_values<Cfg, Cfg::KD>(q, sQ, i, s, L);
-                row_values<Cfg, Cfg::KD>(k, sK, i, s, L);
-#pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    const int u = x >> 2, e = x & 3;
-                    const float d = begin ? 0.0f : one(D[s][u][e] + S[s][u][e]);
-                    D[s][u][e] = d;
-                    S[s][u][e] = __builtin_fmaf(k[x], v, begin ? 0.0f : one(S[s][u][e]));
-                    dot = __builtin_fmaf(q[x], d, dot);
-                    const float o = q[x] * (f * g);
-                    U[s][u][e] = open ? U[s][u][e] + o : U[s][u][e];
-                    E[s][u][e] = open && t > 0 ? __builtin_fmaf((float)t, o, E[s][u][e]) : E[s][u][e];
-                }
-            }
-            if (!begin && t > 0) sum += (double)(dot * p.scale * g);
-        }
-    }
-    const int64_t words = (int64_t)kd * vd, at = (bh * p.nseg + seg) * words;
-    store_state<Cfg>(S, p.states + at, vd, 1, kd, vd, 1.0f, false, L);
-    store_state<Cfg>(D, p.dstates + at, vd, 1, kd, vd, 1.0f, false, L);
-    store_state<Cfg>(U, p.rstates + at, vd, 1, kd, vd, 1.0f, false, L);
-    store_state<Cfg>(E, p.estates + at, vd, 1, kd, vd, 1.0f, false, L);
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x, 64);
-    if (L.lane == 0) sSum[wave] = sum;
-    __syncthreads();
-    if (L.tid == 0) {
-        double s = 0.0;
-#pragma unroll
-        for (int i = 0; i < Cfg::W; ++i) s += sSum[i];
-        p.part[bh * p.nparts + seg] = s;
-    }
-}
-
 // ---------------------------------------------------------------- state scan
-// states[i] becomes the state after segment i: its summary, plus gamma^rows times
+// out[i] is the state after segment i: its summary, plus gamma^rows times
 // the state before it where it holds no begin step; with DOT the derivative
 // likewise, d' = own + gamma^rows (d + rows s).  GROUPS threads share a 16-byte
 // column of the states, each with RPT consecutive segments of it in registers, all
@@ -526,13 +507,13 @@ struct SegState {
 };
 
 template <int GROUPS, int RPT, bool DOT>
-__global__ __launch_bounds__(256) void ret_state_scan_kernel(RetStateScanArgs p) {
+__device__ __forceinline__ void state_scan_body(const RetStateScanArgs& p, int64_t b) {
     constexpr int kCols = 256 / GROUPS, kTile = GROUPS * RPT;
     __shared__ f32x4 sTot[GROUPS > 1 && DOT ? 2 : 1][GROUPS][GROUPS > 1 ? kCols : 1];
     __shared__ uint32_t sFlag[GROUPS];
     __shared__ double sSum[DOT ? 4 : 1];
     const int col = threadIdx.x % kCols, grp = threadIdx.x / kCols;
-    const int64_t h = blockIdx.y, b = blockIdx.z, bh = b * p.H + h;
+    const int64_t h = blockIdx.y, bh = b * p.H + h;
     const int c4 = (int)blockIdx.x * kCols + col, w4 = p.words / 4;   // words is a multiple of 64
     const bool in = c4 < w4;
     const double rate = fabs((double)p.alpha[h]), rows = (double)p.rows, last = (double)p.last_rows;
@@ -546,7 +527,8 @@ __global__ __launch_bounds__(256) void ret_state_scan_kernel(RetStateScanArgs p)
     const Carry many0 = p.rev ? carry_of(rate, last - 1.0 + rows * (RPT - 1)) : many;
     const Carry one_last = carry_of(rate, last);
     const uint32_t bit = p.rev ? kSegBeginsBack : kSegBegins;
-    f32x4* const S = (f32x4*)p.states + bh * p.nseg * w4 + c4;
+    const f32x4* const S = (const f32x4*)p.states + bh * p.nseg * w4 + c4;
+    f32x4* const O = (f32x4*)p.out + bh * p.nseg * w4 + c4;
     f32x4* const D = DOT ? (f32x4*)p.dstates + bh * p.nseg * w4 + c4 : nullptr;
     const f32x4* const U = DOT ? (const f32x4*)p.rstates + bh * p.nseg * w4 + c4 : nullptr;
     const f32x4* const E = DOT ? (const f32x4*)p.estates + bh * p.nseg * w4 + c4 : nullptr;
@@ -606,7 +588,7 @@ __global__ __launch_bounds__(256) void ret_state_scan_kernel(RetStateScanArgs p)
                 mine.then(x[i], y[DOT ? i : 0], (fl[i] & bit) != 0u, at_end ? one_last : one,
                           (float)(at_end ? p.last_rows : p.rows));
                 if (have && !at_end) {
-                    S[(int64_t)l * w4] = mine.s;
+                    O[(int64_t)l * w4] = mine.s;
                     D[(int64_t)l * w4] = mine.d;
                 }
                 if (have && at_end && p.grad_state) {      // D after the tape . grad_state
@@ -616,7 +598,7 @@ __global__ __launch_bounds__(256) void ret_state_scan_kernel(RetStateScanArgs p)
                 }
             } else {
                 mine.then(x[i], zero, (fl[i] & bit) != 0u, l == 0 ? one0 : one, 0.0f);
-                if (have) S[(int64_t)seg_of(l) * w4] = mine.s;
+                if (have) O[(int64_t)seg_of(l) * w4] = mine.s;
             }
         }
         if constexpr (GROUPS == 1) before = mine;
@@ -628,6 +610,34 @@ __global__ __launch_bounds__(256) void ret_state_scan_kernel(RetStateScanArgs p)
         __syncthreads();
         if (threadIdx.x == 0)
             p.part[bh * p.nparts + p.nseg + blockIdx.x] = (sSum[0] + sSum[1]) + (sSum[2] + sSum[3]);
+    }
+}
+
+// tapes 0 .. B - 1 forwards, then (with a grid for them) backwards
+template <int GROUPS, int RPT, bool DOT>
+__global__ __launch_bounds__(256) void ret_state_scan_kernel(RetStateScanArgs p, RetStateScanArgs back, int B) {
+    if ((int)blockIdx.z < B) state_scan_body<GROUPS, RPT, DOT>(p, blockIdx.z);
+    else state_scan_body<GROUPS, RPT, false>(back, blockIdx.z - B);
+}
+
+// ------------------------------------------------------- gradient of the rates
+// grad_alpha[h] = -sign(alpha_h) times the sum of the shares over tapes, in a fixed
+// order
+__device__ __forceinline__ void alpha_sum(const RetWalkSet& p, int64_t h) {
+    __shared__ double sSum[16];
+    const int threads = blockDim.x;
+    const int64_t n = p.B * p.nparts;
+    double sum = 0.0;
+    for (int64_t i = threadIdx.x; i < n; i += threads) sum += p.part[((i / p.nparts) * p.H + h) * p.nparts + i % p.nparts];
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x, 64);
+    if ((threadIdx.x & 63) == 0) sSum[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const float a = p.w[0].alpha[h];
+        double s = 0.0;
+        for (int i = 0; i < threads / 64; ++i) s += sSum[i];
+        p.grad_alpha[h] = a > 0.0f ? (float)-s : a < 0.0f ? (float)s : a == 0.0f ? 0.0f : a;   // NaN stays NaN
     }
 }
 
@@ -670,7 +680,18 @@ __device__ __forceinline__ bool pairs(u32x2 (&sP)[Cfg::NTILE][Cfg::NP][64], cons
 }
 
 template <class Cfg, int ZP>
-__global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 : 3) void ret_walk_kernel(RetWalkArgs p) {
+__global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 : 3) void ret_walk_kernel(RetWalkSet set) {
+    // Tasks of the walks in turn, eight at a time: the workgroups of the same task
+    // of two walks run on the same of the eight dies, one behind the other, and what
+    // both read comes from its cache once.  Behind them, the rates' gradients.
+    const int64_t id = blockIdx.x;
+    if (id >= set.blocks) {
+        alpha_sum(set, id - set.blocks);
+        return;
+    }
+    const RetWalkArgs& p = set.w[(id >> 3) % set.n];
+    const int64_t task = (id >> 3) / set.n * 8 + (id & 7);
+    if (task >= set.tasks) return;
     __shared__ __attribute__((aligned(16))) uint16_t sX[Cfg::NP * Cfg::C * Cfg::KD];
     __shared__ __attribute__((aligned(16))) uint16_t sY[Cfg::NP * Cfg::C * Cfg::KD];
     __shared__ __attribute__((aligned(16))) uint16_t sZ[Cfg::NP * Cfg::C * Cfg::VD];
@@ -683,8 +704,8 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 :
     __shared__ __attribute__((aligned(16))) float sW[Cfg::C];
     __shared__ uint32_t sBad[Cfg::W];
     RetLane L;
-    const int64_t seg = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
-    ret_header(p.hdr, p.sig);
+    const int64_t seg = task % p.nseg, h = task / p.nseg % p.H, b = task / p.nseg / p.H;
+    if (id == 0) ret_header(p.hdr, p.sig);
     const double rate = fabs((double)p.alpha[h]);
     sPw.fill(rate, L.tid);
     if (L.tid < Cfg::C + 16) sAge[L.tid] = L.tid < 16 ? 0.0f : decay_pow(rate, L.tid - 16) * p.p_scale;
@@ -886,35 +907,18 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 :
     }
 }
 
-// ------------------------------------------------------- gradient of the rates
-__global__ __launch_bounds__(256) void ret_alpha_kernel(const double* part, const float* alpha, float* out, int64_t B,
-                                                        int32_t H, int32_t nparts) {
-    __shared__ double sSum[4];
-    const int64_t h = blockIdx.x, n = B * nparts;
-    double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += 256) sum += part[((i / nparts) * H + h) * nparts + i % nparts];
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x, 64);
-    if ((threadIdx.x & 63) == 0) sSum[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        const float a = alpha[h];
-        const double s = (sSum[0] + sSum[1]) + (sSum[2] + sSum[3]);
-        out[h] = a > 0.0f ? (float)-s : a < 0.0f ? (float)s : a == 0.0f ? 0.0f : a;     // NaN stays NaN
-    }
-}
-
 // ------------------------------------------------------ gradients of shared heads
 template <int NP>
-__global__ __launch_bounds__(256) void ret_share_kernel(const float* part, void* out, int64_t units, int32_t heads,
-                                                        int32_t G, int32_t d4) {
+__global__ __launch_bounds__(256) void ret_share_kernel(RetShareArgs p) {
+    const RetShareArgs::Part& a = blockIdx.y ? p.v : p.k;
+    const int64_t units = p.rows * (a.d / 4);
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < units; i += (int64_t)gridDim.x * 256) {
-        const int64_t rk = i / d4, c = i % d4;             // (row, key head), four columns
-        const f32x4* const x = (const f32x4*)part + rk * G * d4 + c;
+        const int64_t rk = i / (a.d / 4), c = i % (a.d / 4);   // (step, key head), four columns
+        const f32x4* const x = (const f32x4*)a.part + rk * p.G * (a.d / 4) + c;
         f32x4 s = x[0];
-        for (int g = 1; g < G; ++g) s += x[(int64_t)g * d4];
-        if (NP == 1) ((u32x2*)out)[i] = u32x2{f32x2_to_bf16x2(s[0], s[1]), f32x2_to_bf16x2(s[2], s[3])};
-        else ((f32x4*)out)[i] = s;
+        for (int g = 1; g < p.G; ++g) s += x[(int64_t)g * (a.d / 4)];
+        if (NP == 1) ((u32x2*)a.out)[i] = u32x2{f32x2_to_bf16x2(s[0], s[1]), f32x2_to_bf16x2(s[2], s[3])};
+        else ((f32x4*)a.out)[i] = s;
     }
 }
 
@@ -949,15 +953,24 @@ void with_planes(bool exact, F&& f) {
 }
 }  // namespace
 
-hipError_t ret_walk_launch(int planes, const RetWalkArgs& a, int64_t B, hipStream_t s) {
-    const dim3 grid((unsigned)a.nseg, (unsigned)a.H, (unsigned)B);
+hipError_t ret_walk_launch(int planes, RetWalkSet set, int64_t B, hipStream_t s) {
+    const RetWalkArgs& a = set.w[0];
+    set.B = B;
+    set.tasks = B * a.H * a.nseg;
+    set.blocks = (set.tasks + 7) / 8 * 8 * set.n;
+    const dim3 grid((unsigned)(set.blocks + (set.grad_alpha ? a.H : 0)));
+    bool exact = false;
+    for (int i = 0; i < set.n; ++i) exact = exact || set.w[i].exact;
     with_cfg(planes, a.x.d, a.z.d, [&](auto cfg) {
         using Cfg = decltype(cfg);
-        with_planes<Cfg>(a.exact, [&](auto zp) {
-            hipLaunchKernelGGL((ret_walk_kernel<Cfg, decltype(zp)::value>), grid, dim3(Cfg::THREADS), 0, s, a);
+        with_planes<Cfg>(exact, [&](auto zp) {
+            hipLaunchKernelGGL((ret_walk_kernel<Cfg, decltype(zp)::value>), grid, dim3(Cfg::THREADS), 0, s, set);
         });
     });
     return hipGetLastError();
+}
+bool ret_same_tiles(int64_t kd0, int64_t vd0, int64_t kd1, int64_t vd1) {
+    return (kd0 <= 64) == (kd1 <= 64) && (vd0 <= 64) == (vd1 <= 64);
 }
 
 hipError_t ret_summary_launch(int planes, const RetSummaryArgs& a, int64_t B, hipStream_t s) {
@@ -988,7 +1001,6 @@ hipError_t ret_prep_launch(int planes, const RetPrepArgs& a, int64_t B, hipStrea
             } else {
                 hipLaunchKernelGGL((ret_prep_kernel<Cfg, 3, true, true, true>), grid, block, 0, s, a);
             }
-            hipLaunchKernelGGL((ret_prep_rows_kernel<Cfg>), grid, block, 0, s, a);
         }
     });
     return hipGetLastError();
@@ -998,21 +1010,21 @@ namespace {
 // One group where there are few segments or many columns, else 32
 bool scan_one_group(int64_t words, int64_t heads, int64_t n) { return n <= 16 || heads * (words / 4) >= 16384; }
 template <int GROUPS, int RPT, bool DOT>
-void state_scan(const RetStateScanArgs& a, int64_t B, hipStream_t s) {
+void state_scan(const RetStateScanArgs& a, const RetStateScanArgs* back, int64_t B, hipStream_t s) {
     constexpr int kCols = 256 / GROUPS;
-    const dim3 grid((unsigned)((a.words / 4 + kCols - 1) / kCols), (unsigned)a.H, (unsigned)B);
-    hipLaunchKernelGGL((ret_state_scan_kernel<GROUPS, RPT, DOT>), grid, dim3(256), 0, s, a);
+    const dim3 grid((unsigned)((a.words / 4 + kCols - 1) / kCols), (unsigned)a.H, (unsigned)(back ? 2 * B : B));
+    hipLaunchKernelGGL((ret_state_scan_kernel<GROUPS, RPT, DOT>), grid, dim3(256), 0, s, a, back ? *back : a, (int)B);
 }
 template <bool DOT>
-void state_scan_for(const RetStateScanArgs& a, int64_t B, hipStream_t s) {
+void state_scan_for(const RetStateScanArgs& a, const RetStateScanArgs* back, int64_t B, hipStream_t s) {
     const int n = DOT ? a.nseg : a.nseg - 1;
-    if (!scan_one_group(a.words, B * a.H, n)) {
-        if (n <= 64) state_scan<32, 2, DOT>(a, B, s);
-        else state_scan<32, 4, DOT>(a, B, s);
+    if (!scan_one_group(a.words, B * a.H, a.nseg)) {
+        if (n <= 64) state_scan<32, 2, DOT>(a, back, B, s);
+        else state_scan<32, 4, DOT>(a, back, B, s);
     } else if (n <= 4) {
-        state_scan<1, 4, DOT>(a, B, s);
+        state_scan<1, 4, DOT>(a, back, B, s);
     } else {
-        state_scan<1, 16, DOT>(a, B, s);
+        state_scan<1, 16, DOT>(a, back, B, s);
     }
 }
 }  // namespace
@@ -1022,25 +1034,17 @@ int64_t ret_scan_parts(int64_t words, int64_t heads, int64_t nseg) {
     return (words / 4 + cols - 1) / cols;
 }
 
-hipError_t ret_state_scan_launch(const RetStateScanArgs& a, int64_t B, hipStream_t s) {
-    if (a.dstates) state_scan_for<true>(a, B, s);
-    else state_scan_for<false>(a, B, s);
+hipError_t ret_state_scan_launch(const RetStateScanArgs& a, const RetStateScanArgs* back, int64_t B, hipStream_t s) {
+    if (a.dstates) state_scan_for<true>(a, back, B, s);
+    else state_scan_for<false>(a, back, B, s);
     return hipGetLastError();
 }
 
-hipError_t ret_alpha_launch(const double* part, const float* alpha, float* out, int64_t B, int32_t H, int32_t nparts,
-                            hipStream_t s) {
-    hipLaunchKernelGGL(ret_alpha_kernel, dim3((unsigned)H), dim3(256), 0, s, part, alpha, out, B, H, nparts);
-    return hipGetLastError();
-}
-
-hipError_t ret_share_launch(int planes, const float* part, void* out, int64_t rows, int32_t heads, int32_t G, int32_t d,
-                            hipStream_t s) {
-    const int64_t units = rows * heads * (d / 4);
-    const int64_t blocks = (units + 255) / 256 < 8192 ? (units + 255) / 256 : 8192;
-    const dim3 grid((unsigned)blocks), block(256);
-    if (planes == 1) hipLaunchKernelGGL((ret_share_kernel<1>), grid, block, 0, s, part, out, units, heads, G, d / 4);
-    else hipLaunchKernelGGL((ret_share_kernel<3>), grid, block, 0, s, part, out, units, heads, G, d / 4);
+hipError_t ret_share_launch(int planes, const RetShareArgs& a, hipStream_t s) {
+    const int64_t units = a.rows * ((a.k.d > a.v.d ? a.k.d : a.v.d) / 4), blocks = (units + 255) / 256;
+    const dim3 grid((unsigned)(blocks < 8192 ? blocks : 8192), 2), block(256);
+    if (planes == 1) hipLaunchKernelGGL((ret_share_kernel<1>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((ret_share_kernel<3>), grid, block, 0, s, a);
     return hipGetLastError();
 }
 
