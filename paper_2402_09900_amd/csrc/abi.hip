@@ -912,13 +912,13 @@ struct RetPlan {
     size_t off_states = 0, off_R = 0, total = 0;
 };
 
-// Enough segments for two workgroups on each of the 256 CUs (a walk of T = 32768, 4
-// heads of 64, fp32: 45 us, 62 with half as many and 45 with twice as many, which
-// have twice the states to scan), down to a chunk each (T = 1000: the forward
-// pass 33 -> 20 us against segments of four chunks).
-void ret_segments(int64_t B, int64_t T, int64_t H, int planes, RetPlan* p) {
+// Enough segments for `groups` workgroups, down to a chunk each.  512, two on each of
+// the 256 CUs: a walk of T = 32768, 4 heads of 64, fp32, takes 45 us, 62 with half as
+// many and 45 with twice as many, which have twice the states to scan.  A chunk:
+// T = 1000, the forward pass 33 -> 20 us against segments of four.
+void ret_segments(int64_t B, int64_t T, int64_t H, int planes, int64_t groups, RetPlan* p) {
     const int64_t C = ret_chunk(planes), n = (T + C - 1) / C;
-    int64_t nseg = (512 + B * H - 1) / (B * H);
+    int64_t nseg = (groups + B * H - 1) / (B * H);
     if (nseg > n) nseg = n;
     p->planes = planes;
     p->chunks = (int32_t)((n + nseg - 1) / nseg);
@@ -943,7 +943,7 @@ size_t ret_states_bytes(const RetPlan& p, int64_t B, int64_t H, int64_t dk, int6
 }
 
 bool plan_retention(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv, int planes, RetPlan* p) {
-    ret_segments(B, T, H, planes, p);
+    ret_segments(B, T, H, planes, 512, p);
     size_t off = kAlign;                                   // header
     p->off_states = off;
     if (p->nseg > 1) off += ret_states_bytes(*p, B, H, dk, dv);
@@ -963,7 +963,11 @@ struct RetBwdPlan {
 
 bool plan_retention_bwd(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t dk, int64_t dv, int planes, bool want_alpha,
                         RetBwdPlan* p) {
-    ret_segments(B, T, H, planes, &p->fwd);
+    // The pass that prepares the segments has one workgroup on a CU unless the head is
+    // narrow, and the three walks fill the CUs with half the segments: T = 4096, 8
+    // tapes, 16 heads of 128, bf16, 1193 us with 512 groups, 1155 with 256 (kernels);
+    // T = 32768, 4 heads of 64, fp32, 264 and 287.
+    ret_segments(B, T, H, planes, dk <= 64 && dv <= 64 ? 512 : 256, &p->fwd);
     const size_t states = ret_states_bytes(p->fwd, B, H, dk, dv);
     p->nparts = p->fwd.nseg + ret_scan_parts(dk * dv, B * H, p->fwd.nseg);
     p->prep = want_alpha || p->fwd.nseg > 1;
