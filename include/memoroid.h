@@ -39,7 +39,8 @@
  *    kernel with identical results.
  *  - The workspace is caller-allocated device memory of at least the size the
  *    matching *_workspace_bytes query (or memoroid_workspace_bytes) returns
- *    for the same arguments, 16-byte aligned (256 for linear attention).
+ *    for the same arguments, 16-byte aligned (256 for linear attention and
+ *    retention).
  *    Concurrent calls must use distinct workspaces.  Two kinds of call:
  *      * SELF-INITIALISING -- every entry point without the _prepared
  *        suffix.  The workspace contents are undefined on entry and on exit;
@@ -387,13 +388,16 @@ int memoroid_scan_linattn_bwd(const float* q, const float* k, const float* v,
  *              not written when T is 0.
  *   scale      finite (MEMOROID_EINVAL otherwise).
  *   dk, dv     multiples of 8 up to 128 (MEMOROID_EUNSUPPORTED otherwise);
- *              B <= 32767, H <= 65535, B H < 2^29.  Arrays 16-byte aligned.
+ *              B <= 32767, H <= 65535, B H <= 2^21, T < 2^30 (likewise).  Arrays
+ *              16-byte aligned.
  *   bf16: products of bf16 inputs, fp32 states and sums; the weights of pairs and
  *   the state as a row reads it are rounded to bf16 once each.  The states out
  *   are fp32 results.  fp32: fp32 precision throughout.
  *   A NaN or Inf stays in its episode and in the steps from its own on; there
- *   an Inf may come out as NaN.
- *   Workspace (self-initialising): memoroid_scan_retention_workspace_bytes.
+ *   an Inf may come out as NaN.  So may elements above 2^100, and products of two
+ *   (q_t . k_s among them), which can overflow before they have decayed.
+ *   state_out must not be state_in.  Workspace (self-initialising):
+ *   memoroid_scan_retention_workspace_bytes.
  * ------------------------------------------------------------------------ */
 size_t memoroid_scan_retention_workspace_bytes(int64_t B, int64_t T, int64_t H,
                                                int64_t dk, int64_t dv, int dtype);
@@ -443,7 +447,7 @@ int memoroid_scan_retention_bwd(const void* q, const void* k, const void* v, con
  *   q [B][H][dk], k [B][Hk][dk], v [B][Hk][dv], out [B][H][dv] of dtype;
  *   alpha [H], state [B][H][dk][dv] fp32;  start: optional [B] begin flags (NULL:
  *   no row begins).  Limits as for memoroid_scan_retention; B may be larger
- *   as long as B * H * ceil(dv / 32) is below 2^31.
+ *   as long as B * H * ceil(dv / 32) is below 2^24.
  * ------------------------------------------------------------------------ */
 int memoroid_retention_step(const void* q, const void* k, const void* v, const float* alpha,
                             const uint8_t* start, float* state, void* out, float scale,

@@ -815,7 +815,7 @@ def _retention_args(q, k, v, alpha, start, scale, steps):
         raise TypeError("retention takes float32 or bfloat16")
     if alpha.dtype != torch.float32 or alpha.shape != (H,):
         raise TypeError("alpha must be float32 [H]")
-    if start is not None and (start.dtype != torch.uint8 or start.shape != q.shape[:lead]):
+    if (start is None and steps) or (start is not None and (start.dtype != torch.uint8 or start.shape != q.shape[:lead])):
         raise TypeError("start must be uint8 %s" % ("[B,T]" if steps else "[B]"))
     return B, T, H, Hk, dk, dv, dt, float(dk ** -0.5 if scale is None else scale)
 
@@ -897,6 +897,7 @@ def retention_step(q, k, v, alpha, state, start=None, scale: Optional[float] = N
     out = torch.empty((B, H, dv), dtype=q.dtype, device=dev)
     _launch("memoroid_retention_step", dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(), _ptr(start),
             state.data_ptr(), out.data_ptr(), scale, B, H, Hk, dk, dv, dt)
+    torch.autograd.graph.increment_version(state)      # a graph that has saved it refuses its backward pass
     return out
 
 
@@ -1080,6 +1081,7 @@ def _make_retention_autograd():
             return got
 
         @staticmethod
+        @torch.autograd.function.once_differentiable
         def backward(ctx, grad_out, grad_state=None):
             q, k, v, alpha, start, state = ctx.saved_tensors
             if grad_out is None:
@@ -1117,6 +1119,7 @@ def _make_rotate_autograd():
             return got
 
         @staticmethod
+        @torch.autograd.function.once_differentiable
         def backward(ctx, grad_q, grad_k):
             q, k, positions, freq, wq, wk = ctx.saved_tensors
             gq, gk, gwq, gwk = rotate_qk_bwd(q, k, positions, freq, grad_q.contiguous(),

@@ -929,11 +929,13 @@ void ret_segments(int64_t B, int64_t T, int64_t H, int planes, int64_t groups, R
 bool ret_dims_ok(int64_t dk, int64_t dv) {
     return dk % 8 == 0 && dv % 8 == 0 && dk <= kRetMaxDim && dv <= kRetMaxDim && dk > 0 && dv > 0;
 }
-// grid extents; a chunk's rows are addressed with 32-bit offsets below 2^31
-// (64 rows of 65535 heads of 128 floats are 2147450880 bytes)
-// and the walks' tasks (at most 512 / (B H) + 1 segments each) are one grid
+// Grid extents.  A chunk's rows are addressed with 32-bit offsets below 2^31 (64 rows
+// of 65535 heads of 128 floats are 2147450880 bytes).  Three walks of B H (512 /
+// (B H) + 1) tasks in workgroups of 512 are one grid, of less than 2^32 threads.
 bool ret_extents_ok(int64_t B, int64_t T, int64_t H) {
-    return B <= 32767 && H <= 65535 && T <= (int64_t)INT32_MAX / 2 && B * H <= (int64_t)INT32_MAX / 4;
+    int64_t n;
+    return B <= 32767 && H <= 65535 && T < ((int64_t)1 << 30) && B * H <= ((int64_t)1 << 21) && mul_ok(B * H, T, &n) &&
+           mul_ok(n, kRetMaxDim * 4, &n);
 }
 int ret_planes(int dtype) { return dtype == MEMOROID_BF16 ? 1 : dtype == MEMOROID_F32 ? 3 : 0; }
 
@@ -1295,7 +1297,8 @@ int memoroid_retention_step(const void* q, const void* k, const void* v, const f
     const int ok = ret_check(B > 1 ? 1 : B, 1, H, Hk, dk, dv, scale, dtype, &empty);
     if (ok != MEMOROID_OK || empty) return ok;
     int64_t groups;
-    if (!mul_ok(B, H * ((dv + 31) / 32), &groups) || groups > (int64_t)INT32_MAX) return MEMOROID_EUNSUPPORTED;
+    // one grid, of less than 2^32 threads
+    if (!mul_ok(B, H * ((dv + 31) / 32), &groups) || groups >= ((int64_t)1 << 24)) return MEMOROID_EUNSUPPORTED;
     if (!alpha || !aligned(alpha, 4)) return MEMOROID_EINVAL;
     if (!ret_pointers_ok({q, k, v}, {}, {out, state}, {})) return MEMOROID_EINVAL;
     if (out == alpha || state == alpha || out == start || (const void*)state == start) return MEMOROID_EINVAL;

@@ -13,10 +13,10 @@
 //
 // Precision.  States, decays and all sums are floats; z is multiplied by its
 // decay in float and goes into the state as three planes, exactly (two, right to
-// 2^-18, where no state of bf16 inputs comes out).  With bf16
-// inputs P and the S that a row is multiplied with are rounded to bf16 once
-// each, as operands: together they add to the output's own rounding what one
-// more rounding would (1.4 times its error), and the state itself takes neither.
+// 2^-18, where no state of bf16 inputs comes out).  With bf16 inputs P and the S
+// that a row is multiplied with are rounded to bf16 once each, as operands:
+// together they add to the output's own rounding what one more rounding would
+// (1.4 times its error), and the state itself takes neither.
 //
 // A value that is not finite must not reach other episodes, nor earlier rows of
 // its own, through a zero of P or of the decays (0 * NaN): a chunk that holds one
@@ -201,6 +201,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummary
 // zero weights.  Without ALPHA the rows that take no part become zeros.  With
 // ALPHA, where every row takes part in something, the segment is done again row by
 // row.
+
 // The sums of ret_prep_kernel, with ALPHA, of a segment that holds a value that is not
 // finite, by the recurrences themselves in floats.  Returns this lane's part.
 template <class Cfg, bool FWD, bool BACK>
@@ -659,11 +660,14 @@ __device__ __forceinline__ bool pairs(u32x2 (&sP)[Cfg::NTILE][Cfg::NP][64], cons
         tile_of(idx, jb, ib);
         f32x4 d = pair_products<Cfg, Cfg::KD>(sY, sX, jb, ib, L);
         const int row = 16 * ib + L.c, age = row - 16 * jb - 4 * L.g;      // of register 0
+        if (ib == jb)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            if (ib == jb) bad |= age == r && !(fabsf(d[r]) < __builtin_inff());
-            d[r] *= by_age[age - r + 16];
-        }
+            for (int r = 0; r < 4; ++r) {
+                bad |= age == r && !(fabsf(d[r]) < __builtin_inff());
+                d[r] = age >= r ? d[r] : 0.0f;                             // (its weight is 0, the product may have overflowed)
+            }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) d[r] *= by_age[age - r + 16];
         if (m) {                                                           // age of the row's first partner
             const uint64_t mr = m & upto(row);
             const int oldest = mr ? row - last_begin(mr) : row;

@@ -147,10 +147,10 @@ __device__ __forceinline__ void mma(f32x4& acc, const bf16x8 (&a)[NA], const bf1
 __device__ __forceinline__ f32x4 zero4() { return f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }
 
 // --------------------------------------------------------- chunks in memory
-// n rows of one head of a [T][heads][d] tensor as a buffer, from step t0 on; walking backwards row i is the (n - 1 - i)-th of them.  Rows
-// at or past n lie outside the buffer (backwards: below offset 0, which wraps
-// past its end), columns at or past d are sent there: they read as zeros and drop
-// their stores.
+// n rows of one head of a [T][heads][d] tensor as a buffer, from step t0 on; walking
+// backwards row i is the (n - 1 - i)-th of them.  Rows at or past n lie outside the
+// buffer (backwards: below offset 0, which wraps past its end), columns at or past d
+// are sent there: they read as zeros and drop their stores.
 struct RetRows {
     Rsrc r;
     int first, step, d;         // byte offsets of row 0 and from row to row

@@ -144,7 +144,6 @@ __device__ __forceinline__ void wave_lds_fence() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// LPR: lanes per row, a power of two; IT: units of a row per lane
 template <int BF16, int CH, bool GRAD>
 __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs p) {
     __shared__ float sCs[4][kPairs][2];

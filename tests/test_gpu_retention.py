@@ -380,3 +380,259 @@ def test_graph(dtype):
         want = c.run()
         for n, y in zip(("out", "state", "dq", "dk", "dv", "dalpha", "dstate"), (out, S) + grads):
             assert torch.equal(y, want[n]), (i, n)
+
+
+class LongCase(Case):
+    """More chunks than the bound above counts: 3 roundings for each of them."""
+
+    def tol(self, name):
+        chunks = (self.cpu["q"].shape[1] + 31) // 32
+        f32 = (24 + 6 + 3 * chunks + 8) * 2.0 ** -24 + 2 * 2.0 ** -21
+        return f32 if self.dtype == "f32" or name in ("state", "dalpha", "dstate") else 3 * 2.0 ** -8 + f32
+
+
+@pytest.mark.parametrize("dtype,T", [("f32", 2100), ("f32", 4200), ("bf16", 4200), ("bf16", 8400)])
+@pytest.mark.parametrize("begins", ["none", "some"])
+def test_many_segments(dtype, T, begins):
+    """More segments than the state scan's groups take at once, and than two turns
+    of them: 66 and 132 of a chunk each."""
+    assert segments(1, T, 2, dtype) - 1 in (66, 132)        # (the query counts the flags' bytes as one more)
+    LongCase(dtype, 1, T, 2, 1, 32, 64, begins, True, seed=T, rates=[2e-4, 0.01]).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dk,dv", [(64, 128), (128, 64), (128, 128), (72, 40)])
+def test_segments_of_wide_heads(dtype, dk, dv):
+    """Two classes of tiles in one gradient, shared heads, a state in and out."""
+    LongCase(dtype, 1, 700, 4, 2, dk, dv, "some", True, seed=dk, rates=[1e-3, 0.05]).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,T,H", [(2, 40, 2), (1, 500, 2), (300, 70, 2)])
+def test_single_segment_and_many_tapes(dtype, B, T, H):
+    """One chunk, a few segments, one segment of several chunks (600 heads of
+    tapes: enough workgroups without a second segment)."""
+    LongCase(dtype, B, T, H, 1, 32, 40, "some", True, seed=B, rates=[0.02]).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [30, 700])
+@pytest.mark.parametrize("dk,dv", [(32, 64), (128, 128)])
+@pytest.mark.parametrize("carry", [False, True])
+def test_gradient_without_rates(dtype, T, dk, dv, carry):
+    """need_grad_alpha=False is a pass of its own."""
+    c = LongCase(dtype, 1, T, 2, 1, dk, dv, "some", carry, seed=T)
+    g = c.gpu
+    got = mb.scan_retention_bwd(*c.gpu_args(), g["grad_out"], scale=c.scale, state=g["state"], grad_state=g["grad_state"],
+                                need_grad_alpha=False)
+    assert got[3] is None
+    r, m = c.expected()
+    for name, y in zip(("dq", "dk", "dv", None, "dstate"), got):
+        if y is not None:
+            assert cond_err(y.double().cpu().numpy(), r[name], m[name]) <= c.tol(name), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dk,dv", [(32, 64), (128, 128)])
+@pytest.mark.parametrize("what", ["q", "k", "v", "grad_out"])
+@pytest.mark.parametrize("alpha", [False, True])
+@pytest.mark.parametrize("begins", [False, True])
+def test_nonfinite_values_in_later_segments(dtype, dk, dv, what, alpha, begins):
+    """As above over several segments, the value in the third chunk or later, with
+    and without the rates' gradient.  (dalpha is a sum over everything.)"""
+    T = 400
+    c = LongCase(dtype, 1, T, 2, 1, dk, dv, "none", True, seed=9)
+    f = c.cpu["start"]
+    if begins:
+        f[:, [0, 20, 130, 170, 200, 300]] = 1
+        c.gpu["start"] = torch.from_numpy(f).to(DEV)
+    x = c.gpu[what].clone()
+    x[0, 180, 0, 7] = float("nan")
+    x[0, 199, 0, 3] = float("inf")
+    c.put(what, x.cpu())
+    g = c.gpu
+    out, S = mb.scan_retention(*c.gpu_args(), scale=c.scale, state=g["state"], final_state=True)
+    dq, dk_, dv_, da, ds = mb.scan_retention_bwd(*c.gpu_args(), g["grad_out"], scale=c.scale, state=g["state"],
+                                                 grad_state=g["grad_state"], need_grad_alpha=alpha)
+    torch.cuda.synchronize()
+    with np.errstate(invalid="ignore"):
+        r, _ = c.expected()
+    x = c.cpu[what]
+    x[~np.isfinite(x)] = 1.0
+    m = ref.magnitudes(*c.ref_args(), c.cpu["grad_out"], c.cpu["state"], c.cpu["grad_state"])
+    for name, y in (("out", out), ("state", S), ("dq", dq), ("dk", dk_), ("dv", dv_), ("dalpha", da), ("dstate", ds)):
+        if y is None:
+            continue
+        y = y.double().cpu().numpy()
+        fine = np.isfinite(r[name])
+        assert np.array_equal(np.isfinite(y), fine), name
+        assert cond_err(y[fine], r[name][fine], m[name][fine]) <= c.tol(name), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("same_episode", [True, False])
+def test_products_that_the_mask_leaves_out_may_overflow(dtype, same_episode):
+    """A query of 1e20 before a key of 1e20: their product is no part of anything,
+    and is infinite."""
+    c = Case(dtype, 1, 100, 2, 2, 32, 32, "none", True, seed=13)
+    if not same_episode:
+        c.cpu["start"][0, 41] = 1
+        c.gpu["start"] = torch.from_numpy(c.cpu["start"]).to(DEV)
+    q, k = c.gpu["q"].clone(), c.gpu["k"].clone()
+    q[0, 37, :, 5] = 1e20
+    k[0, 37, :, 5] = 0.5
+    k[0, 45, :, 5] = 1e20
+    q[0, 45, :, 5] = 0.5
+    c.put("q", q.cpu())
+    c.put("k", k.cpu())
+    c.check()
+
+
+def test_dalpha_to_its_own_size():
+    """dalpha's bound above is its terms' sizes, which mostly cancel.  Against the
+    gradient itself: a head's terms add up like a walk of n steps, so that errors of
+    half a step of float each, independent, leave about 2^-24 of it, and a row of
+    sums of 8 roundings one after the other 8 2^-24; with the planes' 2^-21 of a pair
+    of floats, 2^-20 = 1e-6 of the largest |dalpha|.  Five times that."""
+    for dtype in ("f32", "bf16"):
+        c = LongCase(dtype, 2, 600, 4, 2, 64, 64, "some", True, seed=17, rates=[1e-3, 0.01, 0.05, 0.3])
+        da = c.run()["dalpha"].double().cpu().numpy()
+        r, _ = c.expected()
+        e = np.abs(da - r["dalpha"]).max() / np.abs(r["dalpha"]).max()
+        print("  dalpha %.1e" % e, flush=True)
+        assert e <= 5e-6
+
+
+def test_two_threads_on_two_streams():
+    """Calls at once, each on its own stream: the bits of the calls alone."""
+    import threading
+    cases = [Case("bf16", 2, 500, 4, 2, 64, 64, "some", True, seed=40),
+             Case("f32", 1, 900, 2, 2, 32, 64, "some", True, seed=41)]
+    alone = [c.run() for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    got, errors = [None, None], []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(streams[i]):
+                for _ in range(5):
+                    got[i] = cases[i].run()
+        except Exception as e:      # noqa: BLE001 -- handed to the test below
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    for a, b in zip(alone, got):
+        for n in a:
+            assert torch.equal(a[n], b[n]), n
+
+
+def test_two_graphs_of_training_steps():
+    """Forward and backward through autograd captured twice, with inputs of their
+    own, replayed in turn with eager calls between: the eager results each time."""
+    cases = [Case("bf16", 1, 300, 4, 2, 64, 64, "some", False, seed=50 + i) for i in range(2)]
+
+    def step(c):
+        x = [c.gpu[n].detach().requires_grad_(True) for n in ("q", "k", "v", "alpha")]
+        out = mb.retention(*x, c.gpu["start"], scale=c.scale)
+        return (out,) + torch.autograd.grad(out, x, c.gpu["grad_out"])
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for c in cases:
+            step(c)
+    torch.cuda.current_stream().wait_stream(s)
+    graphs, results = [], []
+    for c in cases:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            results.append([y.detach() for y in step(c)])
+    for i in range(4):
+        for c in cases:
+            for n in ("q", "v", "grad_out"):
+                c.gpu[n].copy_(torch.roll(c.gpu[n], 1 + i, 1))
+        for j in (0, 1) if i % 2 else (1, 0):
+            graphs[j].replay()
+        torch.cuda.synchronize()
+        for c, y in zip(cases, results):
+            for a, b in zip(step(c), y):
+                assert torch.equal(a, b)
+
+
+def test_more_than_2_31_elements():
+    """A tape whose last rows lie past 2^31 elements and 2^32 bytes: the rows behind
+    its last begin against the formula, all of them finite."""
+    T, H, d, tail = 560000, 32, 128, 70
+    announce("retention T=%d H=%d d=%d bf16" % (T, H, d))
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    x = [torch.empty(1, T, H, d, dtype=torch.bfloat16, device=DEV).normal_(generator=g) for _ in range(4)]
+    assert x[0].numel() > 1 << 31
+    alpha = torch.linspace(0.001, 0.1, H, device=DEV)
+    start = torch.zeros(1, T, dtype=torch.uint8, device=DEV)
+    start[0, T - tail] = 1
+    out, S = mb.scan_retention(*x[:3], alpha, start, final_state=True)
+    got = mb.scan_retention_bwd(*x[:3], alpha, start, x[3])
+    for y in (out, S) + got[:4]:
+        assert bool(torch.isfinite(y.sum(dtype=torch.float32)))
+    heads = [0, H - 1]
+    cut = [t[:, T - tail:, heads].double().cpu().numpy() for t in x]
+    args = (*cut[:3], alpha[heads].double().cpu().numpy(), start[:, T - tail:].cpu().numpy(), d ** -0.5)
+    r = ref.forward(*args)
+    b = ref.backward(*args, cut[3])
+    m = ref.magnitudes(*args, cut[3])
+    for name, y, want in (("out", out, r[0]), ("dq", got[0], b["dq"]), ("dk", got[1], b["dk"]), ("dv", got[2], b["dv"])):
+        y = y[:, T - tail:, heads].double().cpu().numpy()
+        assert cond_err(y, want, m[name]) <= BF16_TOL, name
+    assert cond_err(S[:, heads].double().cpu().numpy(), r[1], m["state"]) <= F32_TOL
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_step_of_a_large_batch(dtype):
+    """More rows than a grid has in y or z; rows that begin among them."""
+    B, H, d = 70001, 2, 32
+    announce("retention step B=%d" % B)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(5)
+    q, k, v = (torch.randn(B, H, d, generator=g, device=DEV).to(DT[dtype]) for _ in range(3))
+    S = torch.randn(B, H, d, d, generator=g, device=DEV)
+    start = (torch.rand(B, generator=g, device=DEV) < 0.3).to(torch.uint8)
+    alpha = torch.tensor([0.1, -0.5], device=DEV)
+    keep = torch.where(start[:, None].bool(), 0.0, torch.exp(-alpha.double().abs())[None])
+    old = keep[:, :, None, None] * S.double()
+    want = old + k.double()[..., None] * v.double()[:, :, None]
+    m = old.abs() + (k.double()[..., None] * v.double()[:, :, None]).abs()
+    out = mb.retention_step(q, k, v, alpha, S, start)
+    assert float(((S.double() - want).abs() / torch.maximum(want.abs(), m)).max()) <= 3 * 2.0 ** -24 * 1.01
+    o = (q.double()[..., None] * want).sum(2) * d ** -0.5
+    mo = (q.double().abs()[..., None] * m).sum(2) * d ** -0.5
+    e = float(((out.double() - o).abs() / mo).max())
+    assert e <= F32_TOL + (0 if dtype == "f32" else 2.0 ** -8), e
+
+
+def test_step_marks_the_state_as_changed():
+    """A graph that saved the state before the step must not use it after."""
+    c = Case("f32", 1, 20, 2, 2, 32, 32, "none", True, seed=2)
+    g = c.gpu
+    v = g["v"].clone().requires_grad_(True)
+    S = g["state"].clone()
+    out = mb.retention(g["q"], g["k"], v, g["alpha"], g["start"], state=S)
+    mb.retention_step(*(g[n][:, 0].contiguous() for n in "qkv"), g["alpha"], S)
+    with pytest.raises(RuntimeError):
+        out.sum().backward()
+
+
+def test_second_derivative_is_refused():
+    c = Case("f32", 1, 20, 2, 2, 32, 32, "none", False, seed=2)
+    g = c.gpu
+    v = g["v"].clone().requires_grad_(True)
+    out = mb.retention(g["q"], g["k"], v, g["alpha"], g["start"])
+    dv, = torch.autograd.grad(out.square().sum(), v, create_graph=True)
+    with pytest.raises(RuntimeError):
+        dv.sum().backward()

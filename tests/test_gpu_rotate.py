@@ -231,3 +231,92 @@ def test_rotated_retention_trains_as_its_formula():
             a, c = mb.rotate_qk(q[:, t].contiguous(), k[:, t].contiguous(), args[0][:, t].contiguous(), args[1], wd, wd)
             o = mb.retention_step(a, c, v[:, t].contiguous(), al, S, st[:, t].contiguous())
         assert np.abs(o.double().cpu().numpy() - want[:, t]).max() <= 20 * 2.4e-5 * np.abs(want).max()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_keys_alone(dtype):
+    """No query heads: q and its gradients may be missing, and their weight's
+    gradient is zero."""
+    n, Hk, d = 37, 3, 64
+    announce("rotate H=0 %s" % dtype)
+    dt = DT[dtype]
+    code = mb.F32 if dtype == "f32" else mb.BF16
+    g = torch.Generator(device=DEV)
+    g.manual_seed(4)
+    k, gk = (torch.randn(n, Hk, d, generator=g, device=DEV).to(dt) for _ in range(2))
+    pos = torch.arange(n, dtype=torch.int32, device=DEV)
+    freq = mb.rotary_frequencies(d, device=DEV)
+    w = torch.linspace(0.5, 1.5, d, device=DEV)
+    want, _ = mb.rotate_qk(k, None, pos, freq, w)
+    want_k, _, want_w, _ = mb.rotate_qk_bwd(k, None, pos, freq, gk, None, w)
+    out, dk = torch.empty_like(k), torch.empty_like(k)
+    dwq, dwk = torch.full_like(w, 7.0), torch.full_like(w, 7.0)
+    s = torch.cuda.current_stream().cuda_stream
+    assert mb.memoroid_rotate_qk(None, k.data_ptr(), pos.data_ptr(), freq.data_ptr(), w.data_ptr(), w.data_ptr(), None,
+                                 out.data_ptr(), 1e-6, 1.0, 0, n, 0, Hk, d, d, code, s) == mb.OK
+    nb = mb.memoroid_rotate_qk_bwd_workspace_bytes(n, 0, Hk, d, d, 0, code)
+    ws = torch.empty(nb, dtype=torch.uint8, device=DEV)
+    assert mb.memoroid_rotate_qk_bwd(None, k.data_ptr(), pos.data_ptr(), freq.data_ptr(), w.data_ptr(), w.data_ptr(), None,
+                                     gk.data_ptr(), None, dk.data_ptr(), dwq.data_ptr(), dwk.data_ptr(), 1e-6, 1.0, 0, n, 0,
+                                     Hk, d, d, code, ws.data_ptr(), nb, s) == mb.OK
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(dk, want_k) and torch.equal(dwk, want_w)
+    assert not bool(dwq.any())
+
+
+def test_more_than_2_31_elements():
+    """Rows past 2^31 elements are the rows of a call of their own."""
+    n, H, d, tail = 560000, 32, 128, 50
+    announce("rotate n=%d H=%d d=%d bf16" % (n, H, d))
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    q, gq = (torch.empty(n, H, d, dtype=torch.bfloat16, device=DEV).normal_(generator=g) for _ in range(2))
+    assert q.numel() > 1 << 31
+    pos = torch.arange(n, dtype=torch.int32, device=DEV)
+    freq = mb.rotary_frequencies(d, device=DEV)
+    w = torch.linspace(0.5, 1.5, d, device=DEV)
+    out = mb.rotate_qk(q, None, pos, freq, w)[0]
+    dq = mb.rotate_qk_bwd(q, None, pos, freq, gq, None, w)[0]
+    for rows in (slice(0, tail), slice(n - tail, n)):
+        x, gx, p = q[rows].contiguous(), gq[rows].contiguous(), pos[rows].contiguous()
+        assert torch.equal(out[rows], mb.rotate_qk(x, None, p, freq, w)[0])
+        assert torch.equal(dq[rows], mb.rotate_qk_bwd(x, None, p, freq, gx, None, w)[0])
+
+
+def test_two_graphs_of_training_steps():
+    """Forward and backward through autograd captured twice, replayed in turn with
+    eager calls between."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(6)
+    B, T, H, Hk, d = 2, 150, 4, 2, 64
+    freq = mb.rotary_frequencies(d, device=DEV)
+    pos = torch.arange(T, dtype=torch.int32, device=DEV).repeat(B, 1)
+    sets = [[torch.randn(B, T, h, d, generator=g, device=DEV) for h in (H, Hk, H, Hk)] +
+            [1 + 0.2 * torch.randn(d, generator=g, device=DEV) for _ in range(2)] for _ in range(2)]
+
+    def step(q, k, gq, gk, wq, wk):
+        x = [t.detach().requires_grad_(True) for t in (q, k, wq, wk)]
+        out = mb.qk_rotate(x[0], x[1], pos, freq, x[2], x[3])
+        return out + torch.autograd.grad(out, x, (gq, gk))
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for c in sets:
+            step(*c)
+    torch.cuda.current_stream().wait_stream(s)
+    graphs, results = [], []
+    for c in sets:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            results.append([y.detach() for y in step(*c)])
+    for i in range(4):
+        for c in sets:
+            for t in c[:4]:
+                t.copy_(torch.roll(t, 1 + i, 1))
+        for j in (0, 1) if i % 2 else (1, 0):
+            graphs[j].replay()
+        torch.cuda.synchronize()
+        for c, y in zip(sets, results):
+            for a, b in zip(step(*c), y):
+                assert torch.equal(a, b)

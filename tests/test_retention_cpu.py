@@ -231,3 +231,25 @@ def test_rotation_reference_against_differences():
         assert abs(num - (dx * u).sum()) <= 1e-6 * (1 + abs(num))
         num = ((rotate_ref.rotate(x, w + h * uw, *args)[0][0] - rotate_ref.rotate(x, w - h * uw, *args)[0][0]) * g).sum() / (2 * h)
         assert abs(num - (dw * uw).sum()) <= 1e-6 * (1 + abs(num))
+
+
+@pytest.mark.parametrize("call", [scan, bwd])
+def test_limits_of_one_launch(call):
+    """What no grid or address holds is refused before anything is launched; a
+    workspace query of it gives 0."""
+    assert call(B=2048, T=1, H=1025, Hk=1025) == mb.EUNSUPPORTED
+    assert call(T=1 << 30) == mb.EUNSUPPORTED
+    assert call(B=2048, T=1, H=1024, Hk=1024, nbytes=0) == mb.EWORKSPACE
+    assert mb.memoroid_scan_retention_workspace_bytes(2048, 1, 1025, 64, 64, mb.F32) == 0
+    assert mb.memoroid_scan_retention_bwd_workspace_bytes(2048, 1, 1025, 1, 64, 64, mb.F32, 1) == 0
+
+
+def test_step_of_one_launch():
+    assert step(B=1 << 22, H=1, Hk=1, dv=128) == mb.EUNSUPPORTED
+    assert step(B=1 << 24, H=1, Hk=1, dk=8, dv=8) == mb.EUNSUPPORTED
+
+
+def test_retention_needs_flags():
+    x = torch.zeros(1, 3, 2, 8)
+    with pytest.raises(TypeError):
+        mb.scan_retention(x, x, x, torch.zeros(2), None)
