@@ -1324,29 +1324,48 @@ int memoroid_retention_step(const void* q, const void* k, const void* v, const f
 namespace {
 
 struct RotPlan {
-    int ch = 1, lpr = 1, parts = 1;
-    int64_t groups = 0;
+    int ch = 1, lpr = 1;
+    int32_t parts[2] = {1, 1}, groups[2] = {0, 0};   // of q, of k
     size_t off_part = 0, total = 0;
 };
 
 // Runs of ch elements per lane, as long as 16 bytes and the layout allow: a
 // row is a whole number of pairs of runs, and in the half layout so are its
-// turned part and its rest.  Short batches share a step among wavefronts.
+// turned part and its rest.  Short batches share a step among wavefronts.  The
+// workgroups are divided between q and k by their rows; past 512 a wavefront has four
+// steps or more, up to twice (gradient) or four times as many wavefronts as run at
+// once (6 + 2 heads of 80, fp32, 5997 steps: forward 21 us with a step each, 14 with
+// four; 32 + 8 heads of 128, bf16, 32768 steps: gradient 243 us with 1024
+// workgroups, 207 with 2048, 247 with 4096, which leave more sums to add up).
 void plan_rotate(int64_t n, int64_t H, int64_t Hk, int64_t d, int64_t rot, bool inter, int dtype, bool grad, RotPlan* p) {
     int ch = dtype == MEMOROID_BF16 ? 8 : 4;
     while (ch > 1 && (d % (2 * ch) != 0 || (!inter && rot % (2 * ch) != 0))) ch /= 2;
     p->ch = ch;
     p->lpr = (int)next_pow2(d / (2 * ch));
-    const int64_t rows = H + Hk, at_once = 64 / p->lpr;
-    const int64_t most = (rows + at_once - 1) / at_once;
-    int64_t parts = n >= 8192 ? 1 : (8192 + n - 1) / n;
-    if (parts > most) parts = most;
-    p->parts = (int)parts;
-    const int64_t per = n > INT64_MAX / parts ? INT64_MAX / 4 : n * parts;
-    const int64_t cap = grad ? 1024 : 2048;
-    p->groups = (per + 3) / 4 < cap ? (per + 3) / 4 : cap;
+    const int64_t at_once = 64 / p->lpr, cap = grad ? 2048 : 4096, heads[2] = {H, Hk};
+    for (int i = 0; i < 2; ++i) {
+        if (heads[i] == 0) continue;
+        const int64_t most = (heads[i] + at_once - 1) / at_once;
+        int64_t parts = n >= 8192 ? 1 : (8192 + n - 1) / n;
+        if (parts > most) parts = most;
+        int64_t share = cap * heads[i] / (H + Hk);
+        if (share < 1) share = 1;
+        int64_t groups = (n * parts + 3) / 4;
+        if (groups > 512) groups = groups > 2048 ? groups / 4 : 512;
+        p->parts[i] = (int32_t)parts;
+        p->groups[i] = (int32_t)(groups < share ? groups : share);
+    }
     p->off_part = kAlign;
-    p->total = align_up(kAlign + (size_t)p->groups * 2 * (size_t)d * 4);
+    p->total = align_up(kAlign + (size_t)(p->groups[0] + p->groups[1]) * (size_t)d * 4);
+}
+
+RotateArgs rotate_args(const RotPlan& p, const void* q, const void* k, const void* gq, const void* gk, const float* wq,
+                       const float* wk, void* oq, void* ok, int64_t H, int64_t Hk) {
+    RotateArgs a{};
+    a.side[0] = {q, gq, wq, oq, (int32_t)H, p.parts[0], p.groups[0]};
+    a.side[1] = {k, gk, wk, ok, (int32_t)Hk, p.parts[1], p.groups[1]};
+    a.lpr = p.lpr;
+    return a;
 }
 
 int rot_check(int64_t n, int64_t H, int64_t Hk, int64_t d, int64_t rot, float eps, float amplitude, int dtype, bool* empty) {
@@ -1399,26 +1418,16 @@ int memoroid_rotate_qk(const void* q, const void* k, const int32_t* positions, c
     if (!rot_distinct({q, k, positions, freq, wq, wk}, {q_out, k_out})) return MEMOROID_EINVAL;
     RotPlan p;
     plan_rotate(n, H, Hk, d, rot, interleaved != 0, dtype, false, &p);
-    RotateArgs a{};
-    a.q = q;
-    a.k = k;
+    RotateArgs a = rotate_args(p, q, k, nullptr, nullptr, wq, wk, q_out, k_out, H, Hk);
     a.positions = positions;
     a.freq = freq;
-    a.wq = wq;
-    a.wk = wk;
-    a.q_out = q_out;
-    a.k_out = k_out;
     a.eps = eps;
     a.amplitude = amplitude;
     a.inter = interleaved != 0;
-    a.H = (int32_t)H;
-    a.Hk = (int32_t)Hk;
     a.d = (int32_t)d;
     a.rot = (int32_t)rot;
-    a.lpr = p.lpr;
-    a.parts = p.parts;
     a.n = n;
-    return check_hip(rotate_launch(dtype == MEMOROID_BF16, false, p.ch, p.groups, a, (hipStream_t)stream));
+    return check_hip(rotate_launch(dtype == MEMOROID_BF16, false, p.ch, a, (hipStream_t)stream));
 }
 
 size_t memoroid_rotate_qk_bwd_workspace_bytes(int64_t n, int64_t H, int64_t Hk, int64_t d, int64_t rot, int interleaved,
@@ -1457,36 +1466,24 @@ int memoroid_rotate_qk_bwd(const void* q, const void* k, const int32_t* position
         if (!workspace || workspace_bytes < p.total) return MEMOROID_EWORKSPACE;
         if (!aligned(workspace, 16)) return MEMOROID_EINVAL;
     }
-    RotateArgs a{};
-    a.q = q;
-    a.k = k;
-    a.gq = grad_q_out;
-    a.gk = grad_k_out;
+    RotateArgs a = rotate_args(p, q, k, grad_q_out, grad_k_out, wq, wk, grad_q, grad_k, H, Hk);
     a.positions = positions;
     a.freq = freq;
-    a.wq = wq;
-    a.wk = wk;
-    a.q_out = grad_q;
-    a.k_out = grad_k;
     a.part = weights ? (float*)((char*)workspace + p.off_part) : nullptr;
     a.eps = eps;
     a.amplitude = amplitude;
     a.inter = interleaved != 0;
-    a.H = (int32_t)H;
-    a.Hk = (int32_t)Hk;
     a.d = (int32_t)d;
     a.rot = (int32_t)rot;
-    a.lpr = p.lpr;
-    a.parts = p.parts;
     a.n = n;
     if (weights) {
         a.hdr = (WsHeader*)workspace;
         a.sig = layout_sig({kSigRotateBwd, n, H, Hk, d, rot, interleaved != 0, dtype});
     }
     hipStream_t s = (hipStream_t)stream;
-    if (rotate_launch(dtype == MEMOROID_BF16, true, p.ch, p.groups, a, s) != hipSuccess) return MEMOROID_EHIP;
+    if (rotate_launch(dtype == MEMOROID_BF16, true, p.ch, a, s) != hipSuccess) return MEMOROID_EHIP;
     if (!weights) return MEMOROID_OK;
-    return check_hip(rotate_weights_launch(a.part, grad_wq, grad_wk, p.groups, (int)d, s));
+    return check_hip(rotate_weights_launch(a, grad_wq, grad_wk, s));
 }
 
 // ------------------------------------------------------------------ status

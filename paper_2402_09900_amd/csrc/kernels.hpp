@@ -418,26 +418,26 @@ hipError_t ret_step_launch(int planes, const RetStepArgs& a, hipStream_t s);
 
 // Norms and rotation of queries and keys (rotate.hip)
 constexpr int kRotMaxDim = 128;
+struct RotateSide {             // q or k
+    const void* x;              // [n][H][d]
+    const void* g;              // gradient: upstream gradient, like x
+    const float* w;             // [d], or NULL: no norm
+    void* out;                  // result, or the gradient of x
+    int32_t H, parts, groups;   // wavefronts that share a step; workgroups (none: no such rows)
+};
 struct RotateArgs {
-    const void* q;              // [n][H][d]; k: [n][Hk][d]
-    const void* k;
-    const void* gq;             // gradient: upstream gradients, like q and k
-    const void* gk;
+    RotateSide side[2];
     const int32_t* positions;   // [n]
     const float* freq;          // [rot / 2]
-    const float* wq;            // [d], or NULL: no norm
-    const float* wk;
-    void* q_out;                // results, or the gradients of q and k
-    void* k_out;
-    float* part;                // gradient: [groups][2 d] sums for wq and wk, or NULL
+    float* part;                // gradient: [groups of q, then of k][d] sums for the weights, or NULL
     float eps, amplitude;
-    int32_t inter, H, Hk, d, rot, lpr, parts;   // lanes per row; wavefronts that share a step
+    int32_t inter, d, rot, lpr; // lanes per row, a power of two
     int64_t n;
     WsHeader* hdr;              // header to prepare with sig, or NULL
     uint64_t sig;
 };
-hipError_t rotate_launch(bool bf16, bool grad, int ch, int64_t groups, const RotateArgs& a, hipStream_t s);
-hipError_t rotate_weights_launch(const float* part, float* dwq, float* dwk, int64_t groups, int d, hipStream_t s);
+hipError_t rotate_launch(bool bf16, bool grad, int ch, const RotateArgs& a, hipStream_t s);
+hipError_t rotate_weights_launch(const RotateArgs& a, float* dwq, float* dwk, hipStream_t s);
 
 // ------------------------------------------- discounted return and GAE
 // Steps per lane: 32 for the return (two streams in registers), 16 for the

@@ -7,14 +7,21 @@
 // Gradient, with gy the upstream gradient turned back:
 //     dw = sum over rows of gy x r,   dx = r gy w - x r^3 mean(gy w x).
 //
-// Bound by memory: every element read once and written once, 10 (gradient: 30)
-// flops each.  A lane holds two runs of CH elements, A and B, that are the halves
-// of its CH pairs (half layout: elements p and p + rot / 2; interleaved: the even
-// and odd ones of 2 CH in a row), so a pair never crosses lanes; LPR lanes hold a
-// row and a wavefront the rows of one step, several at a time.  The angles of a
-// step are formed once for all its rows, a pair per lane, and handed on through
-// LDS: in 64 bits down to the fraction of a turn (position 1e5 times frequency 1
-// has 7 bits left behind the point in 32), then sine and cosine in 32.
+// Bound by memory: every element read once and written once (gradient: x and the
+// upstream gradient read), 10 (gradient: 30) flops each.  65536 steps of 16 + 16
+// heads of 128, bf16: 190 us, 5.6 TB/s, faster than a copy of 2 GiB (4.9).  32768
+// steps of 32 + 8 heads of 128, bf16: 126 us forward, gradient 207 (4.9 TB/s) and 7
+// for the weights' sums.
+//
+// A lane holds two runs of CH elements, A and B, that are the halves of its CH pairs
+// (half layout: elements p and p + rot / 2; interleaved: the even and odd ones of
+// 2 CH in a row), so a pair never crosses lanes; LPR lanes hold a row and a wavefront
+// the rows of one step of q or of k, several at a time.  Wavefronts with rows of both
+// held two sets of weights and of their sums: two of them on a SIMD instead of three,
+// and 279 us for the gradient above.  The angles of a step are formed once for all
+// its rows, a pair per lane, while the rows are on their way, and handed on through
+// LDS: in 64 bits down to the fraction of a turn (position 1e5 times frequency 1 has
+// 7 bits left behind the point in 32), then sine and cosine in 32.
 #include "scan_common.hpp"
 #include "kernels.hpp"
 
@@ -24,50 +31,52 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kPairs = kRotMaxDim / 2;
+static_assert(kPairs == 64, "a lane per pair");
 
+// CH elements as they lie in memory
 template <int BF16, int CH>
-struct Run {
-    float v[CH];
+struct Raw {
+    static constexpr int WORDS = BF16 ? (CH + 1) / 2 : CH;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int e = 0; e < WORDS; ++e) w[e] = 0u;
+    }
     __device__ __forceinline__ void load(const void* p, int64_t i) {
-        if constexpr (BF16) {
-            const uint16_t* const s = (const uint16_t*)p + i;
-            uint32_t w[(CH + 1) / 2];
-            if constexpr (CH == 8) *(u32x4*)w = *(const u32x4*)s;
-            else if constexpr (CH == 4) *(u32x2*)w = *(const u32x2*)s;
-            else if constexpr (CH == 2) w[0] = *(const uint32_t*)s;
-            else w[0] = *s;
-#pragma unroll
-            for (int e = 0; e < CH; ++e) v[e] = e & 1 ? bf16_hi(w[e / 2]) : __uint_as_float(w[e / 2] << 16);
+        if constexpr (BF16 && CH == 1) {
+            w[0] = ((const uint16_t*)p)[i];
         } else {
-            const float* const s = (const float*)p + i;
-            if constexpr (CH == 4) *(f32x4*)v = *(const f32x4*)s;
-            else
-#pragma unroll
-                for (int e = 0; e < CH; ++e) v[e] = s[e];
+            const uint32_t* const s = (const uint32_t*)((const char*)p + i * (BF16 ? 2 : 4));
+            if constexpr (WORDS == 4) *(u32x4*)w = *(const u32x4*)s;
+            else if constexpr (WORDS == 2) *(u32x2*)w = *(const u32x2*)s;
+            else w[0] = *s;
         }
     }
-    __device__ __forceinline__ void store(void* p, int64_t i) const {
-        if constexpr (BF16) {
-            uint16_t* const s = (uint16_t*)p + i;
-            if constexpr (CH == 1) {
-                *s = (uint16_t)f32_to_bf16(v[0]);
-            } else {
-                uint32_t w[CH / 2];
+    __device__ __forceinline__ void values(float (&v)[CH]) const {
 #pragma unroll
-                for (int e = 0; e < CH / 2; ++e) w[e] = f32x2_to_bf16x2(v[2 * e], v[2 * e + 1]);
-                if constexpr (CH == 8) *(u32x4*)s = *(u32x4*)w;
-                else if constexpr (CH == 4) *(u32x2*)s = *(u32x2*)w;
-                else *(uint32_t*)s = w[0];
-            }
-        } else {
-            float* const s = (float*)p + i;
-            if constexpr (CH == 4) *(f32x4*)s = *(const f32x4*)v;
-            else
-#pragma unroll
-                for (int e = 0; e < CH; ++e) s[e] = v[e];
+        for (int e = 0; e < CH; ++e) {
+            if constexpr (BF16) v[e] = e & 1 ? bf16_hi(w[e / 2]) : __uint_as_float(w[e / 2] << 16);
+            else v[e] = __uint_as_float(w[e]);
         }
     }
 };
+template <int BF16, int CH>
+__device__ __forceinline__ void store_run(const float (&v)[CH], void* p, int64_t i) {
+    if constexpr (BF16 && CH == 1) {
+        ((uint16_t*)p)[i] = (uint16_t)f32_to_bf16(v[0]);
+    } else {
+        uint32_t w[Raw<BF16, CH>::WORDS];
+#pragma unroll
+        for (int e = 0; e < Raw<BF16, CH>::WORDS; ++e) {
+            if constexpr (BF16) w[e] = f32x2_to_bf16x2(v[2 * e], v[2 * e + 1]);
+            else w[e] = __float_as_uint(v[e]);
+        }
+        uint32_t* const s = (uint32_t*)((char*)p + i * (BF16 ? 2 : 4));
+        if constexpr (Raw<BF16, CH>::WORDS == 4) *(u32x4*)s = *(u32x4*)w;
+        else if constexpr (Raw<BF16, CH>::WORDS == 2) *(u32x2*)s = *(u32x2*)w;
+        else *s = w[0];
+    }
+}
 
 // A lane's place in a row: where its runs lie, and its pairs
 template <int CH>
@@ -115,21 +124,14 @@ __device__ __forceinline__ void from_pairs(float (&a)[CH], float (&b)[CH], bool 
     }
 }
 
-// cosine and sine of every pair of a step, times the amplitude; (1, 0) for the
-// pairs that are not turned
-__device__ __forceinline__ void angles(float (*cs)[2], int pairs, const float* freq, int rot, int32_t position,
-                                       float amplitude, int lane) {
-    for (int p = lane; p < pairs; p += 64) {
-        float c = 1.0f, s = 0.0f;
-        if (p < rot / 2) {
-            const double turns = (double)position * (double)freq[p] * 0.15915494309189533577;   // 1 / 2 pi
-            sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
-            c *= amplitude;
-            s *= amplitude;
-        }
-        cs[p][0] = c;
-        cs[p][1] = s;
-    }
+// cosine and sine of this lane's pair of a step, times the amplitude; (1, 0) for a
+// pair that is not turned.  turns: of the pair, per position
+__device__ __forceinline__ void angle(float (&cs)[2], bool turned, double turns, int32_t position, float amplitude) {
+    const double x = (double)position * turns;
+    float s, c;
+    sincospif(2.0f * (float)(x - rint(x)), &s, &c);
+    cs[0] = turned ? c * amplitude : 1.0f;
+    cs[1] = turned ? s * amplitude : 0.0f;
 }
 // sum over the lanes of a row
 __device__ __forceinline__ float row_sum(float v, int lpr) {
@@ -147,37 +149,66 @@ __device__ __forceinline__ void wave_lds_fence() {
 template <int BF16, int CH, bool GRAD>
 __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs p) {
     __shared__ float sCs[4][kPairs][2];
-    __shared__ float sDw[GRAD ? 4 : 1][GRAD ? 2 * kRotMaxDim : 1];
-    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    __shared__ float sDw[GRAD ? 4 : 1][GRAD ? kRotMaxDim : 1];
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (p.hdr && blockIdx.x == 0 && threadIdx.x < 16) {
         const u32x4 ones = {kEmpty32, kEmpty32, kEmpty32, kEmpty32};
         const u32x4 head = {kEmpty32, kEmpty32, (uint32_t)p.sig, (uint32_t)(p.sig >> 32)};
         ((u32x4*)p.hdr)[threadIdx.x] = threadIdx.x == 0 ? head : ones;
     }
+    // a workgroup has rows of q or rows of k: one set of weights and of their sums
+    const bool keys = (int)blockIdx.x >= p.side[0].groups;
+    const RotateSide& S = p.side[keys ? 1 : 0];
+    const int group = (int)blockIdx.x - (keys ? p.side[0].groups : 0);
     const int lpr = p.lpr, rpw = 64 / lpr;
     const int sub = lane / lpr;
     const RotLane<CH> L(lane % lpr, p.d, p.rot, p.inter);
-    const int rows = p.H + p.Hk, per = (rows + p.parts - 1) / p.parts;
+    const int per = (S.H + S.parts - 1) / S.parts;
     const float inv_d = 1.0f / (float)p.d;
+    const bool norm = S.w != nullptr;
     // the lane's weights, in pairs
-    float wa[2][CH], wb[2][CH], da[2][CH], db[2][CH];
+    float wa[CH], wb[CH], da[CH], db[CH];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const float* const wt = i ? p.wk : p.wq;
-#pragma unroll
-        for (int e = 0; e < CH; ++e) {
-            wa[i][e] = wt && L.in ? wt[L.first + e] : 1.0f;
-            wb[i][e] = wt && L.in ? wt[L.second + e] : 1.0f;
-            da[i][e] = db[i][e] = 0.0f;
-        }
-        to_pairs<CH>(wa[i], wb[i], p.inter);
+    for (int e = 0; e < CH; ++e) {
+        wa[e] = norm && L.in ? S.w[L.first + e] : 1.0f;
+        wb[e] = norm && L.in ? S.w[L.second + e] : 1.0f;
+        da[e] = db[e] = 0.0f;
     }
-    const int64_t waves = (int64_t)gridDim.x * 4, tasks = p.n * p.parts;
-    for (int64_t task = (int64_t)blockIdx.x * 4 + w; task < tasks; task += waves) {
-        const int64_t t = task / p.parts;
-        const int r0 = (int)(task % p.parts) * per, r1 = r0 + per < rows ? r0 + per : rows;
+    to_pairs<CH>(wa, wb, p.inter);
+    const bool turned = lane < p.rot / 2;
+    const double turns = turned ? (double)p.freq[lane] * 0.15915494309189533577 : 0.0;   // 1 / 2 pi
+    constexpr int NR = 2;                                  // rows of a lane in flight
+    Raw<BF16, CH> xa[NR], xb[NR], ya[GRAD ? NR : 1], yb[GRAD ? NR : 1];
+    auto fetch = [&](int64_t at0, int row0, int r1) {
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const int row = row0 + i * rpw;
+            const bool in = L.in && row < r1;
+            const int64_t at = at0 + (int64_t)row * p.d;
+            xa[i].zero();
+            xb[i].zero();
+            if (in && (!GRAD || norm)) {                   // (a gradient without a norm does not need x)
+                xa[i].load(S.x, at + L.first);
+                xb[i].load(S.x, at + L.second);
+            }
+            if constexpr (GRAD) {
+                ya[i].zero();
+                yb[i].zero();
+                if (in) {
+                    ya[i].load(S.g, at + L.first);
+                    yb[i].load(S.g, at + L.second);
+                }
+            }
+        }
+    };
+    const int64_t waves = (int64_t)S.groups * 4, tasks = p.n * S.parts;
+    for (int64_t task = (int64_t)group * 4 + w; task < tasks; task += waves) {
+        const int64_t t = task / S.parts, at0 = t * S.H * p.d;
+        const int r0 = (int)(task % S.parts) * per, r1 = r0 + per < S.H ? r0 + per : S.H;
+        const int32_t position = p.rot ? p.positions[t] : 0;
+        fetch(at0, r0 + sub, r1);                          // before the angles
         wave_lds_fence();                                  // the last step's angles have been read
-        angles(sCs[w], p.d / 2, p.freq, p.rot, p.rot ? p.positions[t] : 0, p.amplitude, lane);
+        angle(sCs[w][lane], turned, turns, position, p.amplitude);
         wave_lds_fence();
         float c[CH], s[CH];
 #pragma unroll
@@ -185,85 +216,73 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs p) {
             c[e] = L.in ? sCs[w][L.pair0 + e][0] : 1.0f;
             s[e] = L.in ? sCs[w][L.pair0 + e][1] : 0.0f;
         }
-        constexpr int NR = GRAD ? 2 : 4;                   // rows of a lane in flight
         for (int row0 = r0 + sub; row0 - sub < r1; row0 += NR * rpw) {
-            Run<BF16, CH> a[NR], b[NR], ga[GRAD ? NR : 1], gb[GRAD ? NR : 1];
-            int64_t at[NR];
-            bool in[NR], isk[NR];
+            if (row0 != r0 + sub) fetch(at0, row0, r1);
 #pragma unroll
             for (int i = 0; i < NR; ++i) {
+                if (row0 - sub + i * rpw >= r1) break;     // no lane has a row
                 const int row = row0 + i * rpw;
-                in[i] = L.in && row < r1;
-                isk[i] = row >= p.H;
-                at[i] = isk[i] ? (t * p.Hk + (row - p.H)) * p.d : (t * p.H + row) * p.d;
-#pragma unroll
-                for (int e = 0; e < CH; ++e) a[i].v[e] = b[i].v[e] = 0.0f;
-                // (a gradient without a norm does not need x)
-                if (in[i] && (!GRAD || (isk[i] ? p.wk : p.wq) != nullptr)) {
-                    a[i].load(isk[i] ? p.k : p.q, at[i] + L.first);
-                    b[i].load(isk[i] ? p.k : p.q, at[i] + L.second);
+                const bool in = L.in && row < r1;
+                const int64_t at = at0 + (int64_t)row * p.d;
+                float a[CH], b[CH], r = 1.0f;
+                if (!GRAD || norm) {
+                    xa[i].values(a);
+                    xb[i].values(b);
+                    to_pairs<CH>(a, b, p.inter);
                 }
-                if constexpr (GRAD) {
+                if (norm) {
+                    float sq = 0.0f;
 #pragma unroll
-                    for (int e = 0; e < CH; ++e) ga[i].v[e] = gb[i].v[e] = 0.0f;
-                    if (in[i]) {
-                        ga[i].load(isk[i] ? p.gk : p.gq, at[i] + L.first);
-                        gb[i].load(isk[i] ? p.gk : p.gq, at[i] + L.second);
-                    }
+                    for (int e = 0; e < CH; ++e) sq = __builtin_fmaf(a[e], a[e], __builtin_fmaf(b[e], b[e], sq));
+                    sq = row_sum(sq, lpr);
+                    // past the last row nothing is normed: eps may be 0
+                    if (row < r1) r = rsqrtf(__builtin_fmaf(sq, inv_d, p.eps));
                 }
-            }
-#pragma unroll
-            for (int i = 0; i < NR; ++i) {
-                to_pairs<CH>(a[i].v, b[i].v, p.inter);
-                // past the last row nothing is normed: eps may be 0
-                const bool norm = row0 + i * rpw < r1 && (isk[i] ? p.wk : p.wq) != nullptr;
-                float r = 1.0f;
-                float sq = 0.0f;
-#pragma unroll
-                for (int e = 0; e < CH; ++e) sq = __builtin_fmaf(a[i].v[e], a[i].v[e], __builtin_fmaf(b[i].v[e], b[i].v[e], sq));
-                sq = row_sum(sq, lpr);
-                if (norm) r = rsqrtf(__builtin_fmaf(sq, inv_d, p.eps));
                 if constexpr (!GRAD) {
 #pragma unroll
                     for (int e = 0; e < CH; ++e) {
-                        const float x = a[i].v[e] * (r * (isk[i] ? wa[1][e] : wa[0][e]));
-                        const float y = b[i].v[e] * (r * (isk[i] ? wb[1][e] : wb[0][e]));
-                        a[i].v[e] = x * c[e] - y * s[e];
-                        b[i].v[e] = y * c[e] + x * s[e];
+                        const float x = a[e] * (r * wa[e]), y = b[e] * (r * wb[e]);
+                        a[e] = x * c[e] - y * s[e];
+                        b[e] = y * c[e] + x * s[e];
                     }
-                    from_pairs<CH>(a[i].v, b[i].v, p.inter);
-                    if (in[i]) {
-                        a[i].store(isk[i] ? p.k_out : p.q_out, at[i] + L.first);
-                        b[i].store(isk[i] ? p.k_out : p.q_out, at[i] + L.second);
+                    from_pairs<CH>(a, b, p.inter);
+                    if (in) {
+                        store_run<BF16, CH>(a, S.out, at + L.first);
+                        store_run<BF16, CH>(b, S.out, at + L.second);
                     }
                 } else {
-                    to_pairs<CH>(ga[i].v, gb[i].v, p.inter);
-                    float dot = 0.0f;
+                    float ga[CH], gb[CH];
+                    ya[i].values(ga);
+                    yb[i].values(gb);
+                    to_pairs<CH>(ga, gb, p.inter);
 #pragma unroll
                     for (int e = 0; e < CH; ++e) {
-                        const float x = ga[i].v[e] * c[e] + gb[i].v[e] * s[e];
-                        const float y = gb[i].v[e] * c[e] - ga[i].v[e] * s[e];
-                        // rows of q and of k add to different sums
-                        const float ax = norm ? x * a[i].v[e] * r : 0.0f, by = norm ? y * b[i].v[e] * r : 0.0f;
-                        da[0][e] += isk[i] ? 0.0f : ax;
-                        db[0][e] += isk[i] ? 0.0f : by;
-                        da[1][e] += isk[i] ? ax : 0.0f;
-                        db[1][e] += isk[i] ? by : 0.0f;
-                        ga[i].v[e] = x * (isk[i] ? wa[1][e] : wa[0][e]);
-                        gb[i].v[e] = y * (isk[i] ? wb[1][e] : wb[0][e]);
-                        dot = __builtin_fmaf(ga[i].v[e], a[i].v[e], __builtin_fmaf(gb[i].v[e], b[i].v[e], dot));
+                        const float x = ga[e] * c[e] + gb[e] * s[e];
+                        gb[e] = gb[e] * c[e] - ga[e] * s[e];
+                        ga[e] = x;
                     }
-                    dot = row_sum(dot, lpr);
-                    const float f = norm ? dot * inv_d * r * r * r : 0.0f;
+                    if (norm) {
+                        float dot = 0.0f;
 #pragma unroll
-                    for (int e = 0; e < CH; ++e) {
-                        ga[i].v[e] = norm ? __builtin_fmaf(-f, a[i].v[e], r * ga[i].v[e]) : ga[i].v[e];
-                        gb[i].v[e] = norm ? __builtin_fmaf(-f, b[i].v[e], r * gb[i].v[e]) : gb[i].v[e];
+                        for (int e = 0; e < CH; ++e) {
+                            da[e] = __builtin_fmaf(ga[e] * a[e], r, da[e]);
+                            db[e] = __builtin_fmaf(gb[e] * b[e], r, db[e]);
+                            ga[e] *= wa[e];
+                            gb[e] *= wb[e];
+                            dot = __builtin_fmaf(ga[e], a[e], __builtin_fmaf(gb[e], b[e], dot));
+                        }
+                        dot = row_sum(dot, lpr);
+                        const float f = dot * inv_d * r * r * r;
+#pragma unroll
+                        for (int e = 0; e < CH; ++e) {
+                            ga[e] = __builtin_fmaf(-f, a[e], r * ga[e]);
+                            gb[e] = __builtin_fmaf(-f, b[e], r * gb[e]);
+                        }
                     }
-                    from_pairs<CH>(ga[i].v, gb[i].v, p.inter);
-                    if (in[i]) {
-                        ga[i].store(isk[i] ? p.k_out : p.q_out, at[i] + L.first);
-                        gb[i].store(isk[i] ? p.k_out : p.q_out, at[i] + L.second);
+                    from_pairs<CH>(ga, gb, p.inter);
+                    if (in) {
+                        store_run<BF16, CH>(ga, S.out, at + L.first);
+                        store_run<BF16, CH>(gb, S.out, at + L.second);
                     }
                 }
             }
@@ -273,39 +292,63 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs p) {
         if (!p.part) return;
         // the wavefront's rows of a step, then its four wavefronts, in a fixed order
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int e = 0; e < CH; ++e)
 #pragma unroll
-            for (int e = 0; e < CH; ++e)
-#pragma unroll
-                for (int m = 1; m < 64; m <<= 1)
-                    if (m >= lpr) {
-                        da[i][e] += lanes_xor(da[i][e], m);
-                        db[i][e] += lanes_xor(db[i][e], m);
-                    }
-            from_pairs<CH>(da[i], db[i], p.inter);
-            if (sub == 0 && L.in)
-#pragma unroll
-                for (int e = 0; e < CH; ++e) {
-                    sDw[w][i * p.d + L.first + e] = da[i][e];
-                    sDw[w][i * p.d + L.second + e] = db[i][e];
+            for (int m = 1; m < 64; m <<= 1)
+                if (m >= lpr) {
+                    da[e] += lanes_xor(da[e], m);
+                    db[e] += lanes_xor(db[e], m);
                 }
-        }
+        from_pairs<CH>(da, db, p.inter);
+        if (sub == 0 && L.in)
+#pragma unroll
+            for (int e = 0; e < CH; ++e) {
+                sDw[w][L.first + e] = da[e];
+                sDw[w][L.second + e] = db[e];
+            }
         __syncthreads();
-        for (int i = threadIdx.x; i < 2 * p.d; i += 256)
-            p.part[(int64_t)blockIdx.x * 2 * p.d + i] = (sDw[0][i] + sDw[GRAD ? 1 : 0][i]) + (sDw[GRAD ? 2 : 0][i] + sDw[GRAD ? 3 : 0][i]);
+        for (int i = threadIdx.x; i < p.d; i += 256)
+            p.part[(int64_t)blockIdx.x * p.d + i] =
+                (sDw[0][i] + sDw[GRAD ? 1 : 0][i]) + (sDw[GRAD ? 2 : 0][i] + sDw[GRAD ? 3 : 0][i]);
     }
 }
 
-// the workgroups' sums, in 64 bits: one column of [groups][2 d] per wavefront
-__global__ __launch_bounds__(256) void rotate_weights_kernel(const float* part, float* dwq, float* dwk, int groups, int d) {
-    const int col = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (col >= 2 * d) return;
-    double s = 0.0;
-    for (int i = lane; i < groups; i += 64) s += (double)part[(int64_t)i * 2 * d + col];
+// dwq = sum of part[0 .. qgroups - 1][d], dwk = of the groups behind, in 64 bits: 16
+// columns per workgroup, 256 rows of 4 of them at a time, all in flight (2048 groups of
+// 128: 4 us, 8 with 64 rows at a time)
+__global__ __launch_bounds__(1024) void rotate_weights_kernel(const float* part, float* dwq, float* dwk, int qgroups,
+                                                              int groups, int d) {
+    __shared__ double sSum[16][16];
+    const int unit = threadIdx.x & 3, row = threadIdx.x >> 2, col = (int)blockIdx.x * 16 + unit * 4;
+    float* const out = blockIdx.y ? dwk : dwq;
+    if (!out) return;
+    const int i0 = blockIdx.y ? qgroups : 0, i1 = blockIdx.y ? groups : qgroups;
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
+    for (int base = i0; base < i1; base += 256 * 8) {
+        f32x4 x[8];
 #pragma unroll
-    for (int m = 1; m < 64; m <<= 1) s += __shfl_xor(s, m, 64);
-    float* const out = col < d ? dwq : dwk;
-    if (lane == 0 && out) out[col < d ? col : col - d] = (float)s;
+        for (int k = 0; k < 8; ++k) {
+            const int i = base + 256 * k + row;
+            x[k] = i < i1 && col < d ? *(const f32x4*)(part + (int64_t)i * d + col) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] += (double)x[k][e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+#pragma unroll
+        for (int m = 4; m < 64; m <<= 1) s[e] += __shfl_xor(s[e], m, 64);
+        if ((threadIdx.x & 63) < 4) sSum[threadIdx.x >> 6][unit * 4 + e] = s[e];
+    }
+    __syncthreads();
+    const int i = threadIdx.x, at = (int)blockIdx.x * 16 + i;
+    if (i < 16 && at < d) {
+        double sum = 0.0;
+        for (int k = 0; k < 16; ++k) sum += sSum[k][i];
+        out[at] = (float)sum;
+    }
 }
 
 namespace {
@@ -323,8 +366,8 @@ void rotate_dispatch(int ch, dim3 grid, const RotateArgs& a, hipStream_t s) {
 }
 }  // namespace
 
-hipError_t rotate_launch(bool bf16, bool grad, int ch, int64_t groups, const RotateArgs& a, hipStream_t s) {
-    const dim3 grid((unsigned)groups);
+hipError_t rotate_launch(bool bf16, bool grad, int ch, const RotateArgs& a, hipStream_t s) {
+    const dim3 grid((unsigned)(a.side[0].groups + a.side[1].groups));
     if (bf16) {
         if (grad) rotate_dispatch<1, true>(ch, grid, a, s);
         else rotate_dispatch<1, false>(ch, grid, a, s);
@@ -335,9 +378,9 @@ hipError_t rotate_launch(bool bf16, bool grad, int ch, int64_t groups, const Rot
     return hipGetLastError();
 }
 
-hipError_t rotate_weights_launch(const float* part, float* dwq, float* dwk, int64_t groups, int d, hipStream_t s) {
-    hipLaunchKernelGGL(rotate_weights_kernel, dim3((unsigned)((2 * d + 3) / 4)), dim3(256), 0, s, part, dwq, dwk,
-                       (int)groups, d);
+hipError_t rotate_weights_launch(const RotateArgs& a, float* dwq, float* dwk, hipStream_t s) {
+    hipLaunchKernelGGL(rotate_weights_kernel, dim3((unsigned)((a.d + 15) / 16), 2), dim3(1024), 0, s, a.part, dwq, dwk,
+                       a.side[0].groups, a.side[0].groups + a.side[1].groups, a.d);
     return hipGetLastError();
 }
 
