@@ -796,32 +796,37 @@ def scan_linattn_bwd(q, k, v, start, out, grad_out, chunk: int = 64, workspace=N
 
 def _retention_args(q, k, v, alpha, start, scale, steps):
     """Checked sizes of a retention call: [B,T,...] tensors (steps) or [B,...]."""
-    torch = _torch()
-    lead = 2 if steps else 1
-    if q.dim() != lead + 2 or k.dim() != lead + 2 or v.dim() != lead + 2:
-        raise ValueError("q, k, v must be %s" % ("[B,T,H,d]" if steps else "[B,H,d]"))
-    B, T = q.shape[0], (q.shape[1] if steps else 1)
-    H, dk = q.shape[lead:]
-    Hk, dv = k.shape[lead], v.shape[lead + 1]
-    if k.shape[:lead] != q.shape[:lead] or v.shape[:lead] != q.shape[:lead] or k.shape[lead + 1] != dk or \
-            v.shape[lead] != Hk:
+    try:
+        if steps:
+            (B, T, H, dk), (Bk, Tk, Hk, dkk), (Bv, Tv, Hv, dv) = q.shape, k.shape, v.shape
+        else:
+            T = Tk = Tv = 1
+            (B, H, dk), (Bk, Hk, dkk), (Bv, Hv, dv) = q.shape, k.shape, v.shape
+    except ValueError:
+        raise ValueError("q, k, v must be %s" % ("[B,T,H,d]" if steps else "[B,H,d]")) from None
+    if B != Bk or B != Bv or T != Tk or T != Tv or dk != dkk or Hk != Hv:
         raise ValueError("q must be [...,H,dk], k [...,Hk,dk] and v [...,Hk,dv]")
     if Hk == 0 or H % Hk:
         raise ValueError("the query heads must be a multiple of the key heads")
-    if k.dtype != q.dtype or v.dtype != q.dtype:
+    dtype = q.dtype
+    if k.dtype != dtype or v.dtype != dtype:
         raise TypeError("q, k and v must share a dtype")
-    dt = _code_of(q.dtype)
+    dt = _code_of(dtype)
     if dt == C64:
         raise TypeError("retention takes float32 or bfloat16")
-    if alpha.dtype != torch.float32 or alpha.shape != (H,):
+    if alpha.dtype != _T.float32 or alpha.shape != (H,):
         raise TypeError("alpha must be float32 [H]")
-    if (start is None and steps) or (start is not None and (start.dtype != torch.uint8 or start.shape != q.shape[:lead])):
+    if start is None:
+        wrong = steps
+    else:
+        wrong = start.dtype != _T.uint8 or start.shape != ((B, T) if steps else (B,))
+    if wrong:
         raise TypeError("start must be uint8 %s" % ("[B,T]" if steps else "[B]"))
     return B, T, H, Hk, dk, dv, dt, float(dk ** -0.5 if scale is None else scale)
 
 
 def _state_like(state, name, B, H, dk, dv):
-    if state is not None and (state.dtype != _torch().float32 or state.shape != (B, H, dk, dv)):
+    if state is not None and (state.dtype != _T.float32 or state.shape != (B, H, dk, dv)):
         raise TypeError("%s must be float32 [B,H,dk,dv]" % name)
 
 
@@ -844,8 +849,8 @@ def scan_retention(q, k, v, alpha, start, scale: Optional[float] = None, state=N
     B, T, H, Hk, dk, dv, dt, scale = _retention_args(q, k, v, alpha, start, scale, True)
     _state_like(state, "state", B, H, dk, dv)
     dev = _check_cuda(q, k, v, alpha, start, state)
-    out = torch.empty((B, T, H, dv), dtype=q.dtype, device=dev)
-    last = torch.empty((B, H, dk, dv), dtype=torch.float32, device=dev) if final_state else None
+    out = q.new_empty((B, T, H, dv))
+    last = alpha.new_empty((B, H, dk, dv)) if final_state else None
     if T == 0 and final_state:                  # no step: the state stays
         last.zero_() if state is None else last.copy_(state)
     ws = _workspace(lib().memoroid_scan_retention_workspace_bytes(B, T, H, dk, dv, dt), dev, workspace)
@@ -894,7 +899,7 @@ def retention_step(q, k, v, alpha, state, start=None, scale: Optional[float] = N
         raise TypeError("state must be float32 [B,H,dk,dv]")
     _state_like(state, "state", B, H, dk, dv)
     dev = _check_cuda(q, k, v, alpha, start, state)
-    out = torch.empty((B, H, dv), dtype=q.dtype, device=dev)
+    out = q.new_empty((B, H, dv))
     _launch("memoroid_retention_step", dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(), _ptr(start),
             state.data_ptr(), out.data_ptr(), scale, B, H, Hk, dk, dv, dt)
     torch.autograd.graph.increment_version(state)      # a graph that has saved it refuses its backward pass
@@ -922,31 +927,34 @@ def rotary_frequencies(rot: int, base: float = 10000.0, factor: float = 1.0, ori
     return f.float().to(device) if device is not None else f.float()
 
 
-def _rotate_args(q, k, positions, freq, wq, wk, name="q and k"):
-    torch = _torch()
-    if q.dim() < 3 or (k is not None and (k.dim() != q.dim() or k.shape[:-2] != q.shape[:-2] or
-                                          k.shape[-1] != q.shape[-1])):
+def _rotate_args(q, k, positions, freq, wq, wk):
+    if q.dim() < 3 or (k is not None and k.dim() != q.dim()):
         raise ValueError("q must be [...,H,d] and k [...,Hk,d]")
-    if k is not None and k.dtype != q.dtype:
-        raise TypeError("%s must share a dtype" % name)
+    *lead, H, d = q.shape
+    Hk = 0
+    if k is not None:
+        *leadk, Hk, dk = k.shape
+        if leadk != lead or dk != d:
+            raise ValueError("q must be [...,H,d] and k [...,Hk,d]")
+        if k.dtype != q.dtype:
+            raise TypeError("q and k must share a dtype")
     dt = _code_of(q.dtype)
     if dt == C64:
         raise TypeError("rotation takes float32 or bfloat16")
-    H, d = q.shape[-2:]
     rot = 0 if freq is None else 2 * freq.numel()
-    if freq is not None and (freq.dtype != torch.float32 or freq.dim() != 1 or rot > d):
+    if freq is not None and (freq.dtype != _T.float32 or freq.dim() != 1 or rot > d):
         raise TypeError("freq must be float32 [rot / 2], rot at most d")
-    if rot and (positions is None or positions.dtype != torch.int32 or positions.shape != q.shape[:-2]):
+    if rot and (positions is None or positions.dtype != _T.int32 or list(positions.shape) != lead):
         raise TypeError("positions must be int32 of q's leading shape")
     for w in (wq, wk):
-        if w is not None and (w.dtype != torch.float32 or w.shape != (d,)):
+        if w is not None and (w.dtype != _T.float32 or w.shape != (d,)):
             raise TypeError("wq and wk must be float32 [d]")
     if k is None and wk is not None:
         raise ValueError("wk without k")
     n = 1
-    for x in q.shape[:-2]:
+    for x in lead:
         n *= x
-    return n, H, (0 if k is None else k.shape[-2]), d, rot, dt
+    return n, H, Hk, d, rot, dt
 
 
 def rotate_qk(q, k, positions, freq, wq=None, wk=None, eps: float = 1e-6, interleaved: bool = False,
