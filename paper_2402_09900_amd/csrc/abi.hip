@@ -967,8 +967,8 @@ bool plan_retention_bwd(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t dk,
                         RetBwdPlan* p) {
     // The pass that prepares the segments has one workgroup on a CU unless the head is
     // narrow, and the three walks fill the CUs with half the segments: T = 4096, 8
-    // tapes, 16 heads of 128, bf16, 1193 us with 512 groups, 1155 with 256 (kernels);
-    // T = 32768, 4 heads of 64, fp32, 264 and 287.
+    // tapes, 16 heads of 128, bf16, 1150 us with 512 groups, 1100 with 256 (kernels,
+    // forward pass included); T = 32768, 4 heads of 64, fp32, 267 and 291.
     ret_segments(B, T, H, planes, dk <= 64 && dv <= 64 ? 512 : 256, &p->fwd);
     const size_t states = ret_states_bytes(p->fwd, B, H, dk, dv);
     p->nparts = p->fwd.nseg + ret_scan_parts(dk * dv, B * H, p->fwd.nseg);

@@ -193,9 +193,12 @@ __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummary
 // dL/dlog gamma is rounded to bf16.  What a state before the segment adds to it,
 // gamma (S . (U + E) + D . U), follows in the state scan.
 //
-// FWD: S, D and part; BACK: U and E.  One pass for both reads q, k, v and g once,
-// with the states in registers, 64 rows of each per wavefront (RetCfg64).  Four
-// states of 128 x 128 do not fit: there ALPHA takes two passes.
+// One pass reads q, k, v and g once, with the states in registers, 64 rows of each per
+// wavefront (RetCfg64).  With four states of 128 x 128 a workgroup of 16 wavefronts
+// takes all 128 registers of each; what the next chunk's rows need of them is free
+// only behind the outer products, so they are fetched there (T = 4096, 8 tapes, 16
+// heads, bf16: 390 us, 504 fetched before them, 487 in two passes of eight wavefronts
+// with two states each).
 //
 // A value that is not finite would reach other episodes and earlier rows through
 // zero weights.  Without ALPHA the rows that take no part become zeros.  With
@@ -204,7 +207,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummary
 
 // The sums of ret_prep_kernel, with ALPHA, of a segment that holds a value that is not
 // finite, by the recurrences themselves in floats.  Returns this lane's part.
-template <class Cfg, bool FWD, bool BACK>
+template <class Cfg>
 __device__ __forceinline__ double prep_rows(const RetPrepArgs& p, const Run<Cfg>& run, const Head& hq, const Head& hk,
                                             const Head& hv, const Head& hg, const uint8_t* start, double rate,
                                             uint16_t* sQ, uint16_t* sK, uint16_t* sV, uint16_t* sG, State<Cfg>& S,
@@ -223,13 +226,13 @@ __device__ __forceinline__ double prep_rows(const RetPrepArgs& p, const Run<Cfg>
         const int t0 = run.first(ch), n = run.rows(ch);
         const uint64_t m = __ballot(ret_flag(start, t0, n, (int)p.T, false, L.lane) != 0u);
         tq.fetch(rows_of<Cfg>(hq, t0, n), L);
-        if (FWD) tk.fetch(rows_of<Cfg>(hk, t0, n), L);
-        if (FWD) tv.fetch(rows_of<Cfg>(hv, t0, n), L);
+        tk.fetch(rows_of<Cfg>(hk, t0, n), L);
+        tv.fetch(rows_of<Cfg>(hv, t0, n), L);
         tg.fetch(rows_of<Cfg>(hg, t0, n), L);
         __syncthreads();
         tq.stage(sQ, L);
-        if (FWD) tk.stage(sK, L);
-        if (FWD) tv.stage(sV, L);
+        tk.stage(sK, L);
+        tv.stage(sV, L);
         tg.stage(sG, L);
         __syncthreads();
 #pragma unroll 1
@@ -238,28 +241,24 @@ __device__ __forceinline__ double prep_rows(const RetPrepArgs& p, const Run<Cfg>
             const bool begin = (m >> i) & 1ull;
             open = open && !(begin && t > 0);
             const float f = decay_pow(rate, (double)t) * p.scale;
-            const float v = FWD ? tile_value<Cfg, Cfg::VD>(sV, i, state_col(L)) : 0.0f;
+            const float v = tile_value<Cfg, Cfg::VD>(sV, i, state_col(L));
             const float g = tile_value<Cfg, Cfg::VD>(sG, i, state_col(L));
             float dot = 0.0f;
 #pragma unroll
             for (int s = 0; s < Cfg::KS; ++s) {
                 float q[8], k[8];
                 row_values<Cfg, Cfg::KD>(q, sQ, i, s, L);
-                if (FWD) row_values<Cfg, Cfg::KD>(k, sK, i, s, L);
+                row_values<Cfg, Cfg::KD>(k, sK, i, s, L);
 #pragma unroll
                 for (int x = 0; x < 8; ++x) {
                     const int u = x >> 2, e = x & 3;
-                    if (FWD) {
-                        const float d = begin ? 0.0f : one(D[s][u][e] + S[s][u][e]);
-                        D[s][u][e] = d;
-                        S[s][u][e] = __builtin_fmaf(k[x], v, begin ? 0.0f : one(S[s][u][e]));
-                        dot = __builtin_fmaf(q[x], d, dot);
-                    }
-                    if (BACK) {
-                        const float o = q[x] * (f * g);
-                        U[s][u][e] = open ? U[s][u][e] + o : U[s][u][e];
-                        E[s][u][e] = open && t > 0 ? __builtin_fmaf((float)t, o, E[s][u][e]) : E[s][u][e];
-                    }
+                    const float d = begin ? 0.0f : one(D[s][u][e] + S[s][u][e]);
+                    D[s][u][e] = d;
+                    S[s][u][e] = __builtin_fmaf(k[x], v, begin ? 0.0f : one(S[s][u][e]));
+                    dot = __builtin_fmaf(q[x], d, dot);
+                    const float o = q[x] * (f * g);
+                    U[s][u][e] = open ? U[s][u][e] + o : U[s][u][e];
+                    E[s][u][e] = open && t > 0 ? __builtin_fmaf((float)t, o, E[s][u][e]) : E[s][u][e];
                 }
             }
             if (!begin && t > 0) sum += (double)(dot * p.scale * g);
@@ -268,11 +267,13 @@ __device__ __forceinline__ double prep_rows(const RetPrepArgs& p, const Run<Cfg>
     return sum;
 }
 
-template <class Cfg, int ZP, bool ALPHA, bool FWD, bool BACK>
+template <class Cfg, int ZP, bool ALPHA>
 __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void ret_prep_kernel(RetPrepArgs p) {
+    // four states in 128 registers: nothing is read ahead of its use
+    constexpr bool kFull = Cfg::THREADS == 1024 && ALPHA;
     __shared__ __attribute__((aligned(16))) uint16_t sQ[Cfg::NP * Cfg::C * Cfg::KD];
-    __shared__ __attribute__((aligned(16))) uint16_t sK[FWD ? Cfg::NP * Cfg::C * Cfg::KD : 8];
-    __shared__ __attribute__((aligned(16))) uint16_t sV[FWD ? Cfg::NP * Cfg::C * Cfg::VD : 8];
+    __shared__ __attribute__((aligned(16))) uint16_t sK[Cfg::NP * Cfg::C * Cfg::KD];
+    __shared__ __attribute__((aligned(16))) uint16_t sV[Cfg::NP * Cfg::C * Cfg::VD];
     __shared__ __attribute__((aligned(16))) uint16_t sG[Cfg::NP * Cfg::C * Cfg::VD];
     __shared__ Powers<Cfg::C + 1> sPw;
     __shared__ float sAge[Cfg::C + 16];                    // [16 + n]: n gamma^n scale, 0 for n < 0
@@ -286,7 +287,7 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void re
     ret_header(p.hdr, p.sig);
     const double rate = fabs((double)p.alpha[h]);
     sPw.fill(rate, L.tid);
-    if (ALPHA && FWD && L.tid < Cfg::C + 16) {
+    if (ALPHA && L.tid < Cfg::C + 16) {
         const int age = L.tid - 16;
         sAge[L.tid] = age < 0 ? 0.0f : decay_pow(rate, age) * (float)age * p.scale;
     }
@@ -303,8 +304,8 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void re
         const int t0 = run.first(ch), n = run.rows(ch);
         flag = ret_flag(start, t0, n, (int)p.T, false, L.lane);
         tq.fetch(rows_of<Cfg>(hq, t0, n), L);
-        if (FWD) tk.fetch(rows_of<Cfg>(hk, t0, n), L);
-        if (FWD) tv.fetch(rows_of<Cfg>(hv, t0, n), L);
+        tk.fetch(rows_of<Cfg>(hk, t0, n), L);
+        tv.fetch(rows_of<Cfg>(hv, t0, n), L);
         tg.fetch(rows_of<Cfg>(hg, t0, n), L);
     };
     fetch(0);
@@ -327,8 +328,7 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void re
         const int n = run.rows(ch);
         const uint64_t m = __ballot(flag != 0u);
         if (ch == 0 && (m & 1ull)) begins |= kSegBeginsFirst;
-        if (ALPHA) bad |= tq.bad() | tg.bad();
-        if (ALPHA && FWD) bad |= tk.bad() | tv.bad();
+        if (ALPHA) bad |= tq.bad() | tk.bad() | tv.bad() | tg.bad();
         const uint64_t mo = ch == 0 ? m & ~1ull : m;   // a begin at r0 separates nothing from it
         if (m) begins |= kSegBegins;
         if (mo) begins |= kSegBeginsBack;
@@ -349,8 +349,8 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void re
         }
         barrier_lds();                                 // the last operands have been read
         tq.stage(sQ, L);
-        if (FWD) tk.stage(sK, L);
-        if (FWD) tv.stage(sV, L);
+        tk.stage(sK, L);
+        tv.stage(sV, L);
         tg.stage(sG, L);
         if (L.tid < Cfg::C) {
             const int i = L.tid;
@@ -363,9 +363,8 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void re
                 sW[3][i] = f * (float)i;
             }
         }
-        fetch(ch + 1);
         barrier_lds();
-        if constexpr (ALPHA && FWD) {
+        if constexpr (ALPHA) {
             float part = 0.0f;
 #pragma unroll
             for (int i = 0; i < (Cfg::NTILE + Cfg::W - 1) / Cfg::W; ++i) {
@@ -387,7 +386,7 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void re
         // ---- rows of the first episode: outer products of q and g.  Without any
         // such row nothing is touched, so that values of S that are not finite
         // stay out
-        if (to > 0 && ((ALPHA && FWD) || open)) {
+        if (to > 0 && (ALPHA || open)) {
             const float use = open ? far : 0.0f;
             float part = 0.0f;
             // o1, then o2: one set of weighted g at a time, for the registers
@@ -413,26 +412,28 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void re
                         }
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            if (BACK && k == 0) U[s][u][e] = __builtin_fmaf(use, o[e], U[s][u][e]);
-                            if (BACK && ALPHA) E[s][u][e] = __builtin_fmaf(k == 0 ? use * off : use, o[e], E[s][u][e]);
-                            if (FWD && ALPHA)
+                            if (k == 0) U[s][u][e] = __builtin_fmaf(use, o[e], U[s][u][e]);
+                            if (ALPHA) E[s][u][e] = __builtin_fmaf(k == 0 ? use * off : use, o[e], E[s][u][e]);
+                            if (ALPHA)
                                 part = __builtin_fmaf(k == 0 ? S[s][u][e] + D[s][u][e] : S[s][u][e], o[e], part);
                         }
+                        if constexpr (kFull) __builtin_amdgcn_sched_barrier(0);
                     }
                 __builtin_amdgcn_sched_barrier(0);
             }
             // (before the first step there is no state, and no state is NaN)
-            if (ALPHA && FWD && ch > 0) sum += (double)(part * (was * gamma));
+            if (ALPHA && ch > 0) sum += (double)(part * (was * gamma));
         }
+        fetch(ch + 1);                                 // here, for the registers
         // ---- (S, D) after the rows
-        if constexpr (FWD && ALPHA) {
+        if constexpr (ALPHA) {
             const float steps = (float)n;
             each<Cfg>(D, [&](float x, int s, int u, int e) { return __builtin_fmaf(steps, S[s][u][e], x); });
             settle<Cfg>(D, m != 0, take, cy);
         }
-        if constexpr (FWD) settle<Cfg>(S, m != 0, take, cy);
+        settle<Cfg>(S, m != 0, take, cy);
 #pragma unroll
-        for (int tb = 0; tb < (FWD ? Cfg::C / 32 : 0); ++tb) {
+        for (int tb = 0; tb < Cfg::C / 32; ++tb) {
             bf16x8 z[Cfg::NP];
             col_frag<Cfg, Cfg::VD>(z, sV, tb, state_col_addr(L), L);
 #pragma unroll
@@ -446,6 +447,7 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void re
                         bf16x8 y[Cfg::NP];
                         col_frag<Cfg, Cfg::KD>(y, sK, tb, state_row_addr(s, u, L), L);
                         mma<Cfg::NP, ZP>(k ? D[s][u] : S[s][u], y, zw);
+                        if constexpr (kFull) __builtin_amdgcn_sched_barrier(0);
                     }
             }
         }
@@ -458,15 +460,15 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void re
     if constexpr (ALPHA) {
         // a value that is not finite, in the inputs or by overflow
         if (__syncthreads_or(bad != 0u || !(fabs(sum) < (double)__builtin_inff()))) {
-            sum = prep_rows<Cfg, FWD, BACK>(p, run, hq, hk, hv, hg, start, rate, sQ, sK, sV, sG, S, D, U, E, L);
+            sum = prep_rows<Cfg>(p, run, hq, hk, hv, hg, start, rate, sQ, sK, sV, sG, S, D, U, E, L);
             now = 1.0f;
         }
     }
-    if (FWD) store_state<Cfg>(S, p.states + at, vd, 1, kd, vd, now, false, L);
-    if (BACK) store_state<Cfg>(U, p.rstates + at, vd, 1, kd, vd, 1.0f, false, L);
-    if (FWD && ALPHA) store_state<Cfg>(D, p.dstates + at, vd, 1, kd, vd, now, false, L);
-    if (BACK && ALPHA) store_state<Cfg>(E, p.estates + at, vd, 1, kd, vd, 1.0f, false, L);
-    if (FWD && ALPHA) {
+    store_state<Cfg>(S, p.states + at, vd, 1, kd, vd, now, false, L);
+    store_state<Cfg>(U, p.rstates + at, vd, 1, kd, vd, 1.0f, false, L);
+    if (ALPHA) store_state<Cfg>(D, p.dstates + at, vd, 1, kd, vd, now, false, L);
+    if (ALPHA) store_state<Cfg>(E, p.estates + at, vd, 1, kd, vd, 1.0f, false, L);
+    if (ALPHA) {
 #pragma unroll
         for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x, 64);
         if (L.lane == 0) sSum[wave] = sum;
@@ -478,7 +480,7 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void re
             p.part[bh * p.nparts + seg] = s;
         }
     }
-    if (FWD && h == 0 && L.tid == 0) {
+    if (h == 0 && L.tid == 0) {
         if (run.r1 < p.T && start[run.r1] != 0) begins |= kSegBeginsBack;
         p.R[b * p.nseg + seg] = (uint8_t)begins;
     }
@@ -992,19 +994,12 @@ hipError_t ret_prep_launch(int planes, const RetPrepArgs& a, int64_t B, hipStrea
     const dim3 grid((unsigned)a.nseg, (unsigned)a.H, (unsigned)B);
     with_cfg(planes, a.q.d, a.v.d, [&](auto cfg) {
         using Cfg = RetCfg64<decltype(cfg)>;
-        using Whole = decltype(cfg);
-        const dim3 block(Cfg::THREADS), whole(Whole::THREADS);
-        if (!a.dstates) {
-            with_planes<Cfg>(a.exact, [&](auto zp) {
-                hipLaunchKernelGGL((ret_prep_kernel<Cfg, decltype(zp)::value, false, true, true>), grid, block, 0, s, a);
-            });
+        if (a.dstates) {
+            hipLaunchKernelGGL((ret_prep_kernel<Cfg, 3, true>), grid, dim3(Cfg::THREADS), 0, s, a);
         } else {
-            if constexpr (Cfg::KD == 128 && Cfg::VD == 128) {
-                hipLaunchKernelGGL((ret_prep_kernel<Whole, 3, true, true, false>), grid, whole, 0, s, a);
-                hipLaunchKernelGGL((ret_prep_kernel<Whole, 3, true, false, true>), grid, whole, 0, s, a);
-            } else {
-                hipLaunchKernelGGL((ret_prep_kernel<Cfg, 3, true, true, true>), grid, block, 0, s, a);
-            }
+            with_planes<Cfg>(a.exact, [&](auto zp) {
+                hipLaunchKernelGGL((ret_prep_kernel<Cfg, decltype(zp)::value, false>), grid, dim3(Cfg::THREADS), 0, s, a);
+            });
         }
     });
     return hipGetLastError();
