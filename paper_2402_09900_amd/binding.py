@@ -13,8 +13,9 @@ runs in the library's HIP kernels:
   of prepared workspaces, one per (device, stream, entry point, sizes,
   flags, operand alignment).  A workspace tensor passed in explicitly goes
   to the self-initialising entry point (which fills what it needs on the
-  stream).  ``DiagScan`` wraps the diagonal pair as a
-  ``torch.autograd.Function``.
+  stream), as retention and rotation always do, on a workspace of the call's
+  own where none is passed.  ``diag_scan``, ``retention`` and ``qk_rotate`` are
+  the differentiable forms (``torch.autograd.Function``).
 
 Loading fails loudly (``MemoroidError``) if the shared library is missing:
 there is no fallback implementation.

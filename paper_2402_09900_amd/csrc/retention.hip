@@ -686,7 +686,8 @@ __device__ __forceinline__ bool pairs(u32x2 (&sP)[Cfg::NTILE][Cfg::NP][64], cons
 }
 
 template <class Cfg, int ZP>
-__global__ __launch_bounds__(Cfg::THREADS, Cfg::KD == 64 || Cfg::VD == 128 ? 4 : 3) void ret_walk_kernel(RetWalkSet set) {
+__global__ __launch_bounds__(Cfg::THREADS, Cfg::VD == 128 ? 4 : Cfg::KD == 128 ? 2 : Cfg::NP == 1 ? 4 : 3)
+    void ret_walk_kernel(RetWalkSet set) {
     // Tasks of the walks in turn, eight at a time: the workgroups of the same task
     // of two walks run on the same of the eight dies, one behind the other, and what
     // both read comes from its cache once.  Behind them, the rates' gradients.
