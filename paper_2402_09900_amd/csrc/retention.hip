@@ -100,7 +100,9 @@ __device__ __forceinline__ f32x4 pair_products(const uint16_t* sY, const uint16_
 
 // ---------------------------------------------------------------- summaries
 // What a segment adds to the state after it: the sum over its rows from the last
-// begin on.
+// begin on.  Reads y and z once: T = 65536, 16 heads of 128, bf16, 151 us, 3.5 TB/s
+// (8 tapes of 4096, state not asked for: 64 us, 3.1 TB/s), with waits for memory in
+// 0.44 of its wavefronts' time.
 template <class Cfg, int ZP>
 __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummaryArgs p) {
     __shared__ __attribute__((aligned(16))) uint16_t sY[Cfg::NP * Cfg::C * Cfg::KD];
@@ -197,8 +199,11 @@ __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummary
 // wavefront (RetCfg64).  With four states of 128 x 128 a workgroup of 16 wavefronts
 // takes all 128 registers of each; what the next chunk's rows need of them is free
 // only behind the outer products, so they are fetched there (T = 4096, 8 tapes, 16
-// heads, bf16: 390 us, 504 fetched before them, 487 in two passes of eight wavefronts
-// with two states each).
+// heads, bf16: 380 us, 504 fetched before them, 487 in two passes of eight wavefronts
+// with two states each).  Its VALU instructions take about 210 of those, the matrix
+// cores 86; half of them form the rows' weights in three planes, once for each 64 of
+// the state's rows.  (Once for all of them, the second state's columns in lanes c >= 8
+// of a wavefront with 8 columns: 531 us, since more registers spill.)
 //
 // A value that is not finite would reach other episodes and earlier rows through
 // zero weights.  Without ALPHA the rows that take no part become zeros.  With
@@ -685,6 +690,12 @@ __device__ __forceinline__ bool pairs(u32x2 (&sP)[Cfg::NTILE][Cfg::NP][64], cons
     return bad;
 }
 
+// Two workgroups on a CU, whose phases (staging, pairs, rows against the state, rows
+// into it) cover each other's waits.  T = 65536, 16 heads of 128, bf16, state out: 329
+// us, 3.3 TB/s of x, y, z and out; 8 tapes of 4096 without: 147 us, 3.7 TB/s, and 437
+// for the gradient's three walks.  fp32, T = 32768, 4 heads of 64: 45 us, and 108 for
+// three: 394 TFLOP/s of bf16 products, six for one of floats, a third of what a large
+// bf16 product reaches.
 template <class Cfg, int ZP>
 __global__ __launch_bounds__(Cfg::THREADS, Cfg::VD == 128 ? 4 : Cfg::KD == 128 ? 2 : Cfg::NP == 1 ? 4 : 3)
     void ret_walk_kernel(RetWalkSet set) {
@@ -915,6 +926,7 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::VD == 128 ? 4 : Cfg::KD == 128 ?
 }
 
 // ------------------------------------------------------ gradients of shared heads
+// Bound by memory: T = 32768, 32 query heads on 8 of 128, 240 us, 5.0 TB/s.
 template <int NP>
 __global__ __launch_bounds__(256) void ret_share_kernel(RetShareArgs p) {
     const RetShareArgs::Part& a = blockIdx.y ? p.v : p.k;
