@@ -43,6 +43,29 @@ int main(void) {
                 sink += memoroid_tbb_begin_indices_workspace_bytes(T);
                 sink += memoroid_tbb_sample_workspace_bytes(B, T);
                 for (int op = -1; op <= 10; ++op) sink += memoroid_workspace_bytes((memoroid_op)op, B, T, d, 64, 64, 64);
+                for (int dt = -1; dt < 4; ++dt) {
+                    sink += memoroid_scan_retention_workspace_bytes(B, T, d, 64, 128, dt);
+                    sink += memoroid_scan_retention_workspace_bytes(B, T, 4, d, d, dt);
+                    sink += memoroid_scan_retention_bwd_workspace_bytes(B, T, d, 1, 64, 128, dt, 1);
+                    sink += memoroid_scan_retention_bwd_workspace_bytes(B, T, 4, 4, d, d, dt, 0);
+                    sink += memoroid_rotate_qk_bwd_workspace_bytes(B, T, d, 64, 0, 0, dt);
+                    sink += memoroid_rotate_qk_bwd_workspace_bytes(B, T, 4, d, 2, 1, dt);
+                }
+                for (int op = MEMOROID_OP_RETENTION; op <= MEMOROID_OP_ROTATE_QK_BWD; ++op)
+                    sink += memoroid_workspace_bytes((memoroid_op)op, B, T, d, 64, 64, 64);
+                /* no workspace or no operands: stopped whatever the sizes */
+                CHECK(memoroid_scan_retention(P(0x10000), P(0x20000), P(0x30000), P(0x40000), P(0x50000), NULL, P(0x60000),
+                                              NULL, 1.0f, B, T, d, 1, 64, 64, MEMOROID_BF16, NULL, 0, NULL) !=
+                      MEMOROID_EHIP);
+                CHECK(memoroid_scan_retention_bwd(P(0x10000), P(0x20000), P(0x30000), P(0x40000), P(0x50000), NULL,
+                                                  P(0x60000), NULL, P(0x70000), P(0x80000), P(0x90000), NULL, NULL, 1.0f, B,
+                                                  T, d, 1, 64, 64, MEMOROID_F32, NULL, 0, NULL) != MEMOROID_EHIP);
+                CHECK(memoroid_retention_step(NULL, P(0x20000), P(0x30000), P(0x40000), NULL, P(0x60000), P(0x70000), 1.0f,
+                                              B, T, d, 64, 64, MEMOROID_F32, NULL) != MEMOROID_EHIP);
+                CHECK(memoroid_rotate_qk(NULL, NULL, NULL, NULL, NULL, NULL, NULL, NULL, 1e-6f, 1.0f, 0, B, T, d, 64, 2,
+                                         MEMOROID_BF16, NULL) != MEMOROID_EHIP);
+                CHECK(memoroid_rotate_qk_bwd(NULL, NULL, NULL, NULL, NULL, NULL, NULL, NULL, NULL, NULL, NULL, NULL, 1e-6f,
+                                             1.0f, 0, B, T, d, 64, 2, MEMOROID_F32, NULL, 0, NULL) != MEMOROID_EHIP);
                 for (int rev = 0; rev < 2; ++rev)
                     for (int vec = 0; vec < 2; ++vec)
                         sink += (size_t)memoroid_testing_tile_steps(rev, B, T, d, MEMOROID_F32, 0, vec);
