@@ -448,8 +448,11 @@ def _shaped(t, *shape):
 def _workspace(nbytes: int, device, workspace=None):
     """Workspace of a self-initialising entry point."""
     torch = _torch()
-    if workspace is not None and workspace.numel() >= nbytes:
-        return workspace
+    if workspace is not None:
+        if workspace.device != device:
+            raise ValueError("the workspace must live on the tensors' device")
+        if workspace.numel() >= nbytes:
+            return workspace
     return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
 
 

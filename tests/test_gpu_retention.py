@@ -636,3 +636,11 @@ def test_second_derivative_is_refused():
     dv, = torch.autograd.grad(out.square().sum(), v, create_graph=True)
     with pytest.raises(RuntimeError):
         dv.sum().backward()
+
+
+def test_workspace_elsewhere_is_refused():
+    c = Case("f32", 1, 20, 2, 2, 32, 32, "none", False, seed=2)
+    with pytest.raises(ValueError):
+        mb.scan_retention(*c.gpu_args(), workspace=torch.empty(1 << 20, dtype=torch.uint8))
+    with pytest.raises(ValueError):
+        mb.scan_retention_bwd(*c.gpu_args(), c.gpu["grad_out"], workspace=torch.empty(1 << 24, dtype=torch.uint8))
