@@ -391,8 +391,8 @@ int memoroid_scan_linattn_bwd(const float* q, const float* k, const float* v,
  *              B <= 32767, H <= 65535, B H <= 2^21, T < 2^30 (likewise).  Arrays
  *              16-byte aligned.
  *   bf16: products of bf16 inputs, fp32 states and sums; the weights of pairs and
- *   the state as a row reads it are rounded to bf16 once each.  The states out
- *   are fp32 results.  fp32: fp32 precision throughout.
+ *   the state as a row reads it keep 2^-17, results are rounded to bf16 once.  The
+ *   states out are fp32 results.  fp32: fp32 precision throughout.
  *   A NaN or Inf stays in its episode and in the steps from its own on; there
  *   an Inf may come out as NaN.  So may elements above 2^100, and products of two
  *   (q_t . k_s among them), which can overflow before they have decayed.

@@ -13,10 +13,11 @@
 //
 // Precision.  States, decays and all sums are floats; z is multiplied by its
 // decay in float and goes into the state as three planes, exactly (two, right to
-// 2^-18, where no state of bf16 inputs comes out).  With bf16 inputs P and the S
-// that a row is multiplied with are rounded to bf16 once each, as operands:
-// together they add to the output's own rounding what one more rounding would
-// (1.4 times its error), and the state itself takes neither.
+// 2^-17, where no state of bf16 inputs comes out).  With bf16 inputs P and the S
+// that a row is multiplied with are operands of two planes, 2^-17 of a term: the
+// result is rounded to bf16 once, when it leaves (error against 64 bits 1.66e-3;
+// 2.35e-3 with one plane each, which takes 8 % less time: T = 65536, 16 heads of 128,
+// 423 us and 459).
 //
 // A value that is not finite must not reach other episodes, nor earlier rows of
 // its own, through a zero of P or of the decays (0 * NaN): a chunk that holds one
@@ -656,7 +657,7 @@ __device__ __forceinline__ void alpha_sum(const RetWalkSet& p, int64_t h) {
 // product with itself came out not finite: every x and y that is not finite shows
 // there (and so does one that overflows).
 template <class Cfg>
-__device__ __forceinline__ bool pairs(u32x2 (&sP)[Cfg::NTILE][Cfg::NP][64], const uint16_t* sX, const uint16_t* sY,
+__device__ __forceinline__ bool pairs(u32x2 (&sP)[Cfg::NTILE][Cfg::FP][64], const uint16_t* sX, const uint16_t* sY,
                                       const float* by_age, uint64_t m, const RetLane& L) {
     bool bad = false;
 #pragma unroll
@@ -681,11 +682,11 @@ __device__ __forceinline__ bool pairs(u32x2 (&sP)[Cfg::NTILE][Cfg::NP][64], cons
 #pragma unroll
             for (int r = 0; r < 4; ++r) d[r] = age - r <= oldest ? d[r] : 0.0f;
         }
-        uint32_t lo[Cfg::NP], hi[Cfg::NP];
-        planes2<Cfg::NP>(d[0], d[1], lo);
-        planes2<Cfg::NP>(d[2], d[3], hi);
+        uint32_t lo[Cfg::FP], hi[Cfg::FP];
+        planes2<Cfg::FP>(d[0], d[1], lo);
+        planes2<Cfg::FP>(d[2], d[3], hi);
 #pragma unroll
-        for (int q = 0; q < Cfg::NP; ++q) sP[idx][q][L.lane] = u32x2{lo[q], hi[q]};
+        for (int q = 0; q < Cfg::FP; ++q) sP[idx][q][L.lane] = u32x2{lo[q], hi[q]};
     }
     return bad;
 }
@@ -697,7 +698,7 @@ __device__ __forceinline__ bool pairs(u32x2 (&sP)[Cfg::NTILE][Cfg::NP][64], cons
 // three: 394 TFLOP/s of bf16 products, six for one of floats, a third of what a large
 // bf16 product reaches.
 template <class Cfg, int ZP>
-__global__ __launch_bounds__(Cfg::THREADS, Cfg::VD == 128 ? 4 : Cfg::KD == 128 ? 2 : Cfg::NP == 1 ? 4 : 3)
+__global__ __launch_bounds__(Cfg::THREADS, Cfg::VD == 128 ? 4 : Cfg::KD == 128 ? 2 : 3)
     void ret_walk_kernel(RetWalkSet set) {
     // Tasks of the walks in turn, eight at a time: the workgroups of the same task
     // of two walks run on the same of the eight dies, one behind the other, and what
@@ -716,7 +717,7 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::VD == 128 ? 4 : Cfg::KD == 128 ?
     // bf16 out: rows gathered here, so that they leave 16 bytes a lane, a row at a
     // time (a wavefront's own 32 bytes of a row doubled the bytes written)
     __shared__ __attribute__((aligned(16))) uint16_t sO[Cfg::NP == 1 ? Cfg::C * Cfg::VD : 8];
-    __shared__ u32x2 sP[Cfg::NTILE][Cfg::NP][64];
+    __shared__ u32x2 sP[Cfg::NTILE][Cfg::FP][64];
     __shared__ Powers<Cfg::C + 1> sPw;
     __shared__ float sAge[Cfg::C + 16];
     __shared__ __attribute__((aligned(16))) float sW[Cfg::C];
@@ -810,13 +811,13 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::VD == 128 ? 4 : Cfg::KD == 128 ?
             for (int ib = 0; ib < Cfg::NB; ++ib) acc[ib] = zero4();
 #pragma unroll
             for (int s = 0; s < Cfg::KS; ++s) {
-                bf16x8 st[Cfg::NP];
-                planes8<Cfg::NP>(S[s][0], S[s][1], st);
+                bf16x8 st[Cfg::FP];
+                planes8<Cfg::FP>(S[s][0], S[s][1], st);
 #pragma unroll
                 for (int ib = 0; ib < Cfg::NB; ++ib) {
                     bf16x8 x[Cfg::NP];
                     row_frag<Cfg, Cfg::KD>(x, sX, 16 * ib, s, L);
-                    mma<Cfg::NP, Cfg::NP>(acc[ib], st, x);
+                    mma<Cfg::FP, Cfg::NP>(acc[ib], st, x);
                 }
                 // without a limit the scheduler reads all of x ahead, and the
                 // registers of the next chunk's rows are spilled, which waits for them
@@ -843,14 +844,14 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::VD == 128 ? 4 : Cfg::KD == 128 ?
 #pragma unroll
                 for (int ib = 2 * tb; ib < Cfg::NB; ++ib) {
                     const int t0 = ib * (ib + 1) / 2 + 2 * tb;
-                    bf16x8 pr[Cfg::NP];
+                    bf16x8 pr[Cfg::FP];
 #pragma unroll
-                    for (int q = 0; q < Cfg::NP; ++q) {
+                    for (int q = 0; q < Cfg::FP; ++q) {
                         const u32x2 lo = sP[t0][q][L.lane];
                         const u32x2 hi = ib > 2 * tb ? sP[t0 + (ib > 2 * tb ? 1 : 0)][q][L.lane] : u32x2{0u, 0u};
                         pr[q] = __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
                     }
-                    mma<Cfg::NP, Cfg::NP>(acc[ib], z, pr);
+                    mma<Cfg::NP, Cfg::FP>(acc[ib], z, pr);
                 }
                 weigh<Cfg, ZP>(zw, z, sW, tb, L);
 #pragma unroll

@@ -50,6 +50,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 template <int NP_, int KD_, int VD_>
 struct RetCfg {
     static constexpr int NP = NP_, KD = KD_, VD = VD_;
+    static constexpr int FP = NP == 1 ? 2 : 3;        // planes of a float as an operand (pairs' weights, the state)
     static constexpr int C = ret_chunk(NP);
     static constexpr int CW = VD / 16, W = CW, THREADS = 64 * W;   // wavefronts per state's columns, in all
     static constexpr int ES = NP == 1 ? 2 : 4;        // bytes of an element in memory
@@ -93,7 +94,7 @@ __device__ __forceinline__ uint32_t pack_hi(float a, float b) {
 }
 __device__ __forceinline__ float cut(float x) { return __uint_as_float(__float_as_uint(x) & 0xFFFF0000u); }
 // Two floats as NPL planes of packed bf16 words.  One plane: rounded to nearest.
-// Two: the rounding error rounded once more, right to 2^-18.  Three: cut, exact (an
+// Two: the rounding error rounded once more, right to 2^-17.  Three: cut, exact (an
 // infinity leaves NaN in its lower planes: the products are then NaN, not infinite).
 template <int NPL>
 __device__ __forceinline__ void planes2(float a, float b, uint32_t (&w)[NPL]) {
