@@ -1082,7 +1082,6 @@ int memoroid_scan_retention(const void* q, const void* k, const void* v, const f
         m.H = (int32_t)H;
         m.nseg = p.nseg;
         m.chunks = p.chunks;
-        m.exact = state_out != nullptr;
         m.hdr = (WsHeader*)ws;
         m.sig = sig;
         if (ret_summary_launch(p.planes, m, B, s) != hipSuccess) return MEMOROID_EHIP;
@@ -1111,7 +1110,6 @@ int memoroid_scan_retention(const void* q, const void* k, const void* v, const f
     a.seed = state_in;
     a.states = states;
     a.fin = state_out;
-    a.exact = state_out != nullptr;
     a.sk = (int32_t)dv;
     a.sv = 1;
     a.p_scale = a.inter_scale = scale;
@@ -1188,7 +1186,6 @@ int memoroid_scan_retention_bwd(const void* q, const void* k, const void* v, con
         m.nseg = p.nseg;
         m.chunks = p.chunks;
         m.nparts = (int32_t)bp.nparts;
-        m.exact = grad_state_in != nullptr;
         m.hdr = (WsHeader*)ws;
         m.sig = sig;
         if (ret_prep_launch(p.planes, m, B, s) != hipSuccess) return MEMOROID_EHIP;
@@ -1258,7 +1255,6 @@ int memoroid_scan_retention_bwd(const void* q, const void* k, const void* v, con
     wv.sk = (int32_t)dv;
     wv.sv = 1;
     wv.fin = grad_state_in;
-    wv.exact = grad_state_in != nullptr;
     RetWalkSet set{};
     set.H = (int32_t)H;
     set.nparts = (int32_t)bp.nparts;

@@ -322,7 +322,6 @@ struct RetWalkArgs {
     int64_t T;
     int32_t H, nseg, chunks;
     int32_t rev;                // backwards: see retention.hip on `seed` and `fin`
-    int32_t exact;              // bf16: the state is an fp32 result (always so with fin)
     WsHeader* hdr;              // header to prepare with sig, or NULL
     uint64_t sig;
 };
@@ -344,7 +343,6 @@ struct RetSummaryArgs {
     uint8_t* R;                 // [B][nseg] begin steps
     int64_t T;
     int32_t H, nseg, chunks;
-    int32_t exact;              // as in RetWalkArgs
     WsHeader* hdr;
     uint64_t sig;
 };
@@ -362,7 +360,6 @@ struct RetPrepArgs {
     float scale;
     int64_t T;
     int32_t H, nseg, chunks, nparts;
-    int32_t exact;
     WsHeader* hdr;
     uint64_t sig;
 };

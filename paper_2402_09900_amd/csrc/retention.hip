@@ -12,19 +12,18 @@
 // belongs to the last step itself: e = 0 in their first chunk.
 //
 // Precision.  States, decays and all sums are floats; z is multiplied by its
-// decay in float and goes into the state as three planes, exactly (two, right to
-// 2^-17, where no state of bf16 inputs comes out).  With bf16 inputs P and the S
-// that a row is multiplied with are operands of two planes, 2^-17 of a term: the
-// result is rounded to bf16 once, when it leaves (error against 64 bits 1.66e-3;
-// 2.35e-3 with one plane each, which takes 8 % less time: T = 65536, 16 heads of 128,
-// 423 us and 459).
+// decay in float and goes into the state as three planes, exactly, whether a state
+// comes out or not: results do not depend on what else is asked for (two planes
+// where none does: 975 us instead of 1022, 8 tapes of 4096, 16 heads of 128, forward
+// and gradient).  With bf16 inputs P and the S that a row is multiplied with are
+// operands of two planes, 2^-17 of a term, and the result is rounded to bf16 once,
+// when it leaves: its error against 64 bits is the rounding's, 1.66e-3 (2.35e-3 with
+// one plane each: 423 us instead of 459, T = 65536, 16 heads of 128).
 //
 // A value that is not finite must not reach other episodes, nor earlier rows of
 // its own, through a zero of P or of the decays (0 * NaN): a chunk that holds one
 // is walked row by row, by the recurrence itself in floats.
 #include "retention_common.hpp"
-
-#include <type_traits>
 
 namespace memoroid {
 
@@ -70,8 +69,8 @@ struct Run {
 };
 
 // the value operand times a weight per row, in planes
-template <class Cfg, int ZP>
-__device__ __forceinline__ void weigh(bf16x8 (&out)[ZP], const bf16x8 (&z)[Cfg::NP], const float* w, int tb,
+template <class Cfg>
+__device__ __forceinline__ void weigh(bf16x8 (&out)[3], const bf16x8 (&z)[Cfg::NP], const float* w, int tb,
                                       const RetLane& L) {
     f32x4 lo = *(const f32x4*)(w + 32 * tb + 4 * L.g), hi = *(const f32x4*)(w + 32 * tb + 16 + 4 * L.g);
 #pragma unroll
@@ -79,7 +78,7 @@ __device__ __forceinline__ void weigh(bf16x8 (&out)[ZP], const bf16x8 (&z)[Cfg::
         lo[e] *= plane_value<Cfg::NP>(z, e);
         hi[e] *= plane_value<Cfg::NP>(z, e + 4);
     }
-    planes8<ZP>(lo, hi, out);
+    planes8<3>(lo, hi, out);
 }
 // tile `idx` of the triangle: rows 16 jb.. of y against rows 16 ib.. of x
 __device__ __forceinline__ void tile_of(int idx, int& jb, int& ib) {
@@ -104,7 +103,7 @@ __device__ __forceinline__ f32x4 pair_products(const uint16_t* sY, const uint16_
 // begin on.  Reads y and z once: T = 65536, 16 heads of 128, bf16, 151 us, 3.5 TB/s
 // (8 tapes of 4096, state not asked for: 64 us, 3.1 TB/s), with waits for memory in
 // 0.44 of its wavefronts' time.
-template <class Cfg, int ZP>
+template <class Cfg>
 __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummaryArgs p) {
     __shared__ __attribute__((aligned(16))) uint16_t sY[Cfg::NP * Cfg::C * Cfg::KD];
     __shared__ __attribute__((aligned(16))) uint16_t sZ[Cfg::NP * Cfg::C * Cfg::VD];
@@ -158,16 +157,16 @@ __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummary
         settle<Cfg>(S, m != 0, take, cy);
 #pragma unroll
         for (int tb = 0; tb < Cfg::C / 32; ++tb) {
-            bf16x8 z[Cfg::NP], zw[ZP];
+            bf16x8 z[Cfg::NP], zw[3];
             col_frag<Cfg, Cfg::VD>(z, sZ, tb, state_col_addr(L), L);
-            weigh<Cfg, ZP>(zw, z, sW, tb, L);
+            weigh<Cfg>(zw, z, sW, tb, L);
 #pragma unroll
             for (int s = 0; s < Cfg::KS; ++s)
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     bf16x8 y[Cfg::NP];
                     col_frag<Cfg, Cfg::KD>(y, sY, tb, state_row_addr(s, u, L), L);
-                    mma<Cfg::NP, ZP>(S[s][u], y, zw);
+                    mma<Cfg::NP, 3>(S[s][u], y, zw);
                 }
         }
     }
@@ -273,7 +272,7 @@ __device__ __forceinline__ double prep_rows(const RetPrepArgs& p, const Run<Cfg>
     return sum;
 }
 
-template <class Cfg, int ZP, bool ALPHA>
+template <class Cfg, bool ALPHA>
 __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void ret_prep_kernel(RetPrepArgs p) {
     // four states in 128 registers: nothing is read ahead of its use
     constexpr bool kFull = Cfg::THREADS == 1024 && ALPHA;
@@ -398,12 +397,12 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void re
             // o1, then o2: one set of weighted g at a time, for the registers
 #pragma unroll
             for (int k = 0; k < (ALPHA ? 2 : 1); ++k) {
-                bf16x8 gw[Cfg::C / 32][ZP];
+                bf16x8 gw[Cfg::C / 32][3];
 #pragma unroll
                 for (int tb = 0; tb < Cfg::C / 32; ++tb) {
                     bf16x8 g[Cfg::NP];
                     col_frag<Cfg, Cfg::VD>(g, sG, tb, state_col_addr(L), L);
-                    weigh<Cfg, ZP>(gw[tb], g, sW[2 + k], tb, L);
+                    weigh<Cfg>(gw[tb], g, sW[2 + k], tb, L);
                 }
 #pragma unroll
                 for (int s = 0; s < Cfg::KS; ++s)
@@ -414,7 +413,7 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void re
                         for (int tb = 0; tb < Cfg::C / 32; ++tb) {
                             bf16x8 q[Cfg::NP];
                             col_frag<Cfg, Cfg::KD>(q, sQ, tb, state_row_addr(s, u, L), L);
-                            mma<Cfg::NP, ZP>(o, q, gw[tb]);
+                            mma<Cfg::NP, 3>(o, q, gw[tb]);
                         }
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
@@ -444,15 +443,15 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void re
             col_frag<Cfg, Cfg::VD>(z, sV, tb, state_col_addr(L), L);
 #pragma unroll
             for (int k = 0; k < (ALPHA ? 2 : 1); ++k) {
-                bf16x8 zw[ZP];
-                weigh<Cfg, ZP>(zw, z, sW[k], tb, L);
+                bf16x8 zw[3];
+                weigh<Cfg>(zw, z, sW[k], tb, L);
 #pragma unroll
                 for (int s = 0; s < Cfg::KS; ++s)
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         bf16x8 y[Cfg::NP];
                         col_frag<Cfg, Cfg::KD>(y, sK, tb, state_row_addr(s, u, L), L);
-                        mma<Cfg::NP, ZP>(k ? D[s][u] : S[s][u], y, zw);
+                        mma<Cfg::NP, 3>(k ? D[s][u] : S[s][u], y, zw);
                         if constexpr (kFull) __builtin_amdgcn_sched_barrier(0);
                     }
             }
@@ -697,7 +696,7 @@ __device__ __forceinline__ bool pairs(u32x2 (&sP)[Cfg::NTILE][Cfg::FP][64], cons
 // for the gradient's three walks.  fp32, T = 32768, 4 heads of 64: 45 us, and 108 for
 // three: 394 TFLOP/s of bf16 products, six for one of floats, a third of what a large
 // bf16 product reaches.
-template <class Cfg, int ZP>
+template <class Cfg>
 __global__ __launch_bounds__(Cfg::THREADS, Cfg::VD == 128 ? 4 : Cfg::KD == 128 ? 2 : 3)
     void ret_walk_kernel(RetWalkSet set) {
     // Tasks of the walks in turn, eight at a time: the workgroups of the same task
@@ -839,7 +838,7 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::VD == 128 ? 4 : Cfg::KD == 128 ?
             // ---- the rows against each other, and the state after the chunk
 #pragma unroll
             for (int tb = 0; tb < Cfg::C / 32; ++tb) {
-                bf16x8 z[Cfg::NP], zw[ZP];
+                bf16x8 z[Cfg::NP], zw[3];
                 col_frag<Cfg, Cfg::VD>(z, sZ, tb, state_col_addr(L), L);
 #pragma unroll
                 for (int ib = 2 * tb; ib < Cfg::NB; ++ib) {
@@ -853,14 +852,14 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::VD == 128 ? 4 : Cfg::KD == 128 ?
                     }
                     mma<Cfg::NP, Cfg::FP>(acc[ib], z, pr);
                 }
-                weigh<Cfg, ZP>(zw, z, sW, tb, L);
+                weigh<Cfg>(zw, z, sW, tb, L);
 #pragma unroll
                 for (int s = 0; s < Cfg::KS; ++s)
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         bf16x8 y[Cfg::NP];
                         col_frag<Cfg, Cfg::KD>(y, sY, tb, state_row_addr(s, u, L), L);
-                        mma<Cfg::NP, ZP>(S[s][u], y, zw);
+                        mma<Cfg::NP, 3>(S[s][u], y, zw);
                     }
             }
 
@@ -960,17 +959,6 @@ void with_cfg(int planes, int kd, int vd, F&& f) {
     if (planes == 1) with_tiles<1>(kd, vd, f);
     else with_tiles<3>(kd, vd, f);
 }
-// the planes of z: three, or two where bf16's state stays inside (kernels.hpp)
-template <class Cfg, class F>
-void with_planes(bool exact, F&& f) {
-    if constexpr (Cfg::NP == 1) {
-        if (!exact) {
-            f(std::integral_constant<int, 2>{});
-            return;
-        }
-    }
-    f(std::integral_constant<int, 3>{});
-}
 }  // namespace
 
 hipError_t ret_walk_launch(int planes, RetWalkSet set, int64_t B, hipStream_t s) {
@@ -979,13 +967,9 @@ hipError_t ret_walk_launch(int planes, RetWalkSet set, int64_t B, hipStream_t s)
     set.tasks = B * a.H * a.nseg;
     set.blocks = (set.tasks + 7) / 8 * 8 * set.n;
     const dim3 grid((unsigned)(set.blocks + (set.grad_alpha ? a.H : 0)));
-    bool exact = false;
-    for (int i = 0; i < set.n; ++i) exact = exact || set.w[i].exact;
     with_cfg(planes, a.x.d, a.z.d, [&](auto cfg) {
         using Cfg = decltype(cfg);
-        with_planes<Cfg>(exact, [&](auto zp) {
-            hipLaunchKernelGGL((ret_walk_kernel<Cfg, decltype(zp)::value>), grid, dim3(Cfg::THREADS), 0, s, set);
-        });
+        hipLaunchKernelGGL((ret_walk_kernel<Cfg>), grid, dim3(Cfg::THREADS), 0, s, set);
     });
     return hipGetLastError();
 }
@@ -997,9 +981,7 @@ hipError_t ret_summary_launch(int planes, const RetSummaryArgs& a, int64_t B, hi
     const dim3 grid((unsigned)(a.nseg - 1), (unsigned)a.H, (unsigned)B);
     with_cfg(planes, a.y.d, a.z.d, [&](auto cfg) {
         using Cfg = decltype(cfg);
-        with_planes<Cfg>(a.exact, [&](auto zp) {
-            hipLaunchKernelGGL((ret_summary_kernel<Cfg, decltype(zp)::value>), grid, dim3(Cfg::THREADS), 0, s, a);
-        });
+        hipLaunchKernelGGL((ret_summary_kernel<Cfg>), grid, dim3(Cfg::THREADS), 0, s, a);
     });
     return hipGetLastError();
 }
@@ -1008,13 +990,8 @@ hipError_t ret_prep_launch(int planes, const RetPrepArgs& a, int64_t B, hipStrea
     const dim3 grid((unsigned)a.nseg, (unsigned)a.H, (unsigned)B);
     with_cfg(planes, a.q.d, a.v.d, [&](auto cfg) {
         using Cfg = RetCfg64<decltype(cfg)>;
-        if (a.dstates) {
-            hipLaunchKernelGGL((ret_prep_kernel<Cfg, 3, true>), grid, dim3(Cfg::THREADS), 0, s, a);
-        } else {
-            with_planes<Cfg>(a.exact, [&](auto zp) {
-                hipLaunchKernelGGL((ret_prep_kernel<Cfg, decltype(zp)::value, false>), grid, dim3(Cfg::THREADS), 0, s, a);
-            });
-        }
+        if (a.dstates) hipLaunchKernelGGL((ret_prep_kernel<Cfg, true>), grid, dim3(Cfg::THREADS), 0, s, a);
+        else hipLaunchKernelGGL((ret_prep_kernel<Cfg, false>), grid, dim3(Cfg::THREADS), 0, s, a);
     });
     return hipGetLastError();
 }

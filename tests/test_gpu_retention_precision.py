@@ -6,6 +6,7 @@ import pytest
 from test_gpu_retention import F32_TOL, Case
 
 torch = pytest.importorskip("torch")
+from paper_2402_09900_amd import binding as mb  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +30,22 @@ def test_bf16_results_round_once(dk, dv, T, H, Hk):
         worst[name] = float((err / allowed).max())
     print("  " + " ".join("%s %.2f" % w for w in worst.items()), flush=True)
     assert max(worst.values()) <= 1.0, worst
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dk,dv", [(64, 64), (128, 128), (64, 128)])
+@pytest.mark.parametrize("T", [50, 700])
+def test_same_bits_whatever_else_is_asked_for(dtype, dk, dv, T):
+    """The state after the tape, or a carried state of zeros and its gradient, change
+    no bit of the other results."""
+    c = Case(dtype, 1, T, 2, 1, dk, dv, "some", False, seed=T)
+    args, g = c.gpu_args(), c.gpu["grad_out"]
+    out = mb.scan_retention(*args, scale=c.scale)
+    zeros = torch.zeros(1, 2, dk, dv, device=out.device)
+    assert torch.equal(out, mb.scan_retention(*args, scale=c.scale, final_state=True)[0])
+    assert torch.equal(out, mb.scan_retention(*args, scale=c.scale, state=zeros))
+    for alpha in (False, True):
+        alone = mb.scan_retention_bwd(*args, g, scale=c.scale, need_grad_alpha=alpha)
+        with_state = mb.scan_retention_bwd(*args, g, scale=c.scale, state=zeros, grad_state=zeros, need_grad_alpha=alpha)
+        for name, x, y in zip(("dq", "dk", "dv", "dalpha"), alone, with_state):
+            assert (x is None and y is None) or torch.equal(x, y), (name, alpha)
