@@ -426,6 +426,9 @@ int memoroid_scan_retention(const void* q, const void* k, const void* v, const f
  *   grad_alpha optional out [H] fp32;  grad_state_in: optional out [B][H][dk][dv]
  *              fp32.  Both are fp32 results with bf16 inputs too.
  *   Outputs must not alias any input or each other.
+ *   An empty problem (B, T or H equal to 0) writes no output: with no query
+ *   heads on Hk key heads the gradients grad_k and grad_v are zeros, with no
+ *   steps grad_alpha is zero and grad_state_in is G, all the caller's to set.
  *   Workspace (self-initialising): memoroid_scan_retention_bwd_workspace_bytes.
  * ------------------------------------------------------------------------ */
 size_t memoroid_scan_retention_bwd_workspace_bytes(int64_t B, int64_t T, int64_t H, int64_t Hk,

@@ -879,6 +879,9 @@ def scan_retention_bwd(q, k, v, alpha, start, grad_out, scale: Optional[float] =
     gq, gk, gv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
     ga = torch.empty_like(alpha) if need_grad_alpha else None
     gs = torch.empty_like(state) if state is not None else None
+    if H == 0:                                  # nobody reads the keys: sums of nothing
+        gk.zero_()
+        gv.zero_()
     if B == 0 or T == 0:                        # no step: the state stays, nothing decays
         if ga is not None:
             ga.zero_()

@@ -644,3 +644,22 @@ def test_workspace_elsewhere_is_refused():
         mb.scan_retention(*c.gpu_args(), workspace=torch.empty(1 << 20, dtype=torch.uint8))
     with pytest.raises(ValueError):
         mb.scan_retention_bwd(*c.gpu_args(), c.gpu["grad_out"], workspace=torch.empty(1 << 24, dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [0, 1, 70])
+def test_gradient_without_query_heads(dtype, T):
+    """Key heads that no query head reads have a gradient of zeros.  (The memory that
+    the gradients get held other values before.)"""
+    announce("retention bwd H=0 %s T=%d" % (dtype, T))
+    k, v = (torch.randn(2, T, 3, d, device=DEV).to(DT[dtype]) for d in (64, 32))
+    q, g = (torch.empty(2, T, 0, d, dtype=DT[dtype], device=DEV) for d in (64, 32))
+    alpha, start = torch.empty(0, device=DEV), torch.zeros(2, T, dtype=torch.uint8, device=DEV)
+    old = [torch.full_like(x, 7.0) for x in (k, v)]
+    del old
+    dq, dk, dv, da, ds = mb.scan_retention_bwd(q, k, v, alpha, start, g)
+    assert dq.shape == q.shape and da.shape == (0,) and ds is None
+    assert dk.shape == k.shape and dv.shape == v.shape and not bool(dk.any()) and not bool(dv.any())
+    leaves = [x.clone().requires_grad_(True) for x in (q, k, v)]
+    mb.retention(*leaves, alpha, start).backward(g)
+    assert not bool(leaves[1].grad.any()) and not bool(leaves[2].grad.any())
