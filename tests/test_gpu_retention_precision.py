@@ -3,7 +3,8 @@ against the 64-bit recurrence (retention_ref.py) or a closed form."""
 import numpy as np
 import pytest
 
-from test_gpu_retention import F32_TOL, Case
+from conftest import announce
+from test_gpu_retention import DEV, F32_TOL, Case
 
 torch = pytest.importorskip("torch")
 from paper_2402_09900_amd import binding as mb  # noqa: E402
@@ -49,3 +50,83 @@ def test_same_bits_whatever_else_is_asked_for(dtype, dk, dv, T):
         with_state = mb.scan_retention_bwd(*args, g, scale=c.scale, state=zeros, grad_state=zeros, need_grad_alpha=alpha)
         for name, x, y in zip(("dq", "dk", "dv", "dalpha"), alone, with_state):
             assert (x is None and y is None) or torch.equal(x, y), (name, alpha)
+
+
+def slow_rates(n):
+    return torch.logspace(np.log10(1 / 3000), -5, n, dtype=torch.float64).float()
+
+
+def decayed(rates, T):
+    """gamma^t for t = 1 .. T, and the sum of gamma^0 .. gamma^(t - 1), [T, heads]."""
+    r = rates.double()[None]
+    t = torch.arange(1, T + 1, dtype=torch.float64)[:, None]
+    return torch.exp(-r * t), torch.expm1(-r * t) / torch.expm1(-r)
+
+
+def walk_bound(rates, T, per_step, more):
+    """T steps of `per_step` roundings of at most 2^-24 each, as likely up as down: a
+    variance of 2^-48 / 3 a rounding, which decays by gamma^2 a step where the steps
+    add to the value; five standard deviations, and `more` single roundings."""
+    n = torch.clamp(0.5 / rates.double(), max=float(T))
+    return 5 * 2.0 ** -24 * torch.sqrt(per_step * n / 3) + more * 2.0 ** -24
+
+
+def test_rows_with_bad_values_keep_slow_decays():
+    """Every chunk holds a NaN, in a column of its own: all are walked row by row.  The
+    other columns against the closed form, q = k = v = 1: 8 scale times the sum of
+    gamma^n.  A row rounds twice (its decay, what it adds); the sum of 8
+    products and the decay's own 2^-24: 12."""
+    T, H = 16384, 512
+    announce("retention row by row, T=%d H=%d" % (T, H))
+    rates = slow_rates(H)
+    one = torch.ones(1, T, H, 8, device=DEV)
+    v = one.clone()
+    v[0, 5::32, :, 7] = float("nan")
+    out, S = mb.scan_retention(one, one, v, rates.to(DEV), torch.zeros(1, T, dtype=torch.uint8, device=DEV), scale=1.0,
+                               final_state=True)
+    want = decayed(rates, T)[1].to(DEV)
+    bound = walk_bound(rates, T, 2, 12).to(DEV)
+    e = (out[0, :, :, 3].double() / (8 * want) - 1).abs().amax(0) / bound
+    print("  out %.2f" % float(e.max()), flush=True)
+    assert float(e.max()) <= 1
+    e = (S[0, :, 2, 3].double() / want[-1] - 1).abs() / bound
+    assert float(e.max()) <= 1
+    assert bool(torch.isnan(out[0, 5:, :, 7]).all())
+
+
+def test_gradient_of_rows_with_bad_values_keeps_slow_decays():
+    """k holds a NaN in every chunk, in one column: both halves of the tape go through
+    the segments' states row by row, and the walk as well.  dq's other columns, with
+    ones everywhere else, are those of the scan above."""
+    T, H = 16384, 256
+    announce("retention gradient row by row, T=%d H=%d" % (T, H))
+    rates = slow_rates(H)
+    one = torch.ones(1, T, H, 8, device=DEV)
+    k = one.clone()
+    k[0, 5::32, :, 7] = float("nan")
+    dq = mb.scan_retention_bwd(one, k, one, rates.to(DEV), torch.zeros(1, T, dtype=torch.uint8, device=DEV), one, scale=1.0)[0]
+    want = decayed(rates, T)[1].to(DEV)
+    e = (dq[0, :, :, 3].double() / (8 * want) - 1).abs().amax(0) / walk_bound(rates, T, 2, 12).to(DEV)
+    print("  dq %.2f" % float(e.max()), flush=True)
+    assert float(e.max()) <= 1
+
+
+@pytest.mark.parametrize("H,d", [(1, 8), (4, 128)])
+def test_segment_states_keep_slow_decays(H, d):
+    """A state of ones and nothing added to it: out_t is d gamma^t, through as many
+    segments as there are, each of which rounds once as it takes the state on (both
+    forms of the scan of segments); in its own segment a row rounds the state's decay,
+    the sum of d equal products and the result: 8."""
+    T = 32 * 512 // H
+    announce("retention segments, T=%d H=%d d=%d" % (T, H, d))
+    one, none = torch.ones(1, T, H, d, device=DEV), torch.zeros(1, T, H, d, device=DEV)
+    start = torch.zeros(1, T, dtype=torch.uint8, device=DEV)
+    worst = 0.0
+    for rates in slow_rates(64).reshape(-1, H):
+        out = mb.scan_retention(one, none, none, rates.to(DEV), start, scale=1.0, state=torch.ones(1, H, d, d, device=DEV))
+        want = decayed(rates, T)[0].to(DEV)
+        e = (out[0, :, :, 3].double() / (d * want) - 1).abs().max()
+        worst = max(worst, float(e))
+    bound = 2.0 ** -24 * (5 * (132 / 3) ** 0.5 + 8)        # 128 segments or groups of them, and 4 in a group
+    print("  out %.1e of %.1e" % (worst, bound), flush=True)
+    assert worst <= bound
