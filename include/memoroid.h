@@ -451,6 +451,8 @@ int memoroid_scan_retention_bwd(const void* q, const void* k, const void* v, con
  *   alpha [H], state [B][H][dk][dv] fp32;  start: optional [B] begin flags (NULL:
  *   no row begins).  Limits as for memoroid_scan_retention; B may be larger
  *   as long as B * H * ceil(dv / 32) is below 2^24.
+ *   The state is rounded to fp32 at every step: where a step's decay and k^T v are
+ *   less than half its last place (rates below 2^-24) it stays as it is.
  * ------------------------------------------------------------------------ */
 int memoroid_retention_step(const void* q, const void* k, const void* v, const float* alpha,
                             const uint8_t* start, float* state, void* out, float scale,

@@ -130,3 +130,26 @@ def test_segment_states_keep_slow_decays(H, d):
     bound = 2.0 ** -24 * (5 * (132 / 3) ** 0.5 + 8)        # 128 segments or groups of them, and 4 in a group
     print("  out %.1e of %.1e" % (worst, bound), flush=True)
     assert worst <= bound
+
+
+def test_steps_keep_slow_decays():
+    """16384 steps of q = k = v = 1 against the closed form, 8 scale times the sum of
+    gamma^n, and against the scan of the same steps (whose own bound comes on top).
+    Two roundings a step, the sum of 8 products and the decay's own 2^-24."""
+    T, H = 16384, 64
+    announce("retention %d steps" % T)
+    rates = torch.cat([slow_rates(H - 3), torch.tensor([1 / 3000, 1 / 4096, 1 / 51200])])
+    one, alpha = torch.ones(1, H, 8, device=DEV), rates.to(DEV)
+    S = torch.zeros(1, H, 8, 8, device=DEV)
+    for _ in range(T):
+        out = mb.retention_step(one, one, one, alpha, S, scale=1.0)
+    want, bound = decayed(rates, T)[1][-1], walk_bound(rates, T, 2, 12)
+    e = (out[0, :, 3].double().cpu() / (8 * want) - 1).abs() / bound
+    print("  out %.2f" % float(e.max()), flush=True)
+    assert float(e.max()) <= 1
+    many = torch.ones(1, T, H, 8, device=DEV)
+    scan, last = mb.scan_retention(many, many, many, alpha, torch.zeros(1, T, dtype=torch.uint8, device=DEV), scale=1.0,
+                                   final_state=True)
+    for x, y in ((out, scan[:, -1]), (S, last)):
+        e = (x.double() / y.double() - 1).abs().reshape(H, -1).amax(1).cpu()
+        assert bool((e <= bound + F32_TOL).all())
