@@ -899,12 +899,19 @@ def scan_retention_bwd(q, k, v, alpha, start, grad_out, scale: Optional[float] =
 def retention_step(q, k, v, alpha, state, start=None, scale: Optional[float] = None):
     """One step of retention for B rows, `state` (float32 [B,H,dk,dv]) updated in
     place.  q: [B,H,dk]; k: [B,Hk,dk]; v: [B,Hk,dv]; start: optional uint8 [B],
-    the rows that begin an episode with this step.  Returns out [B,H,dv]."""
+    the rows that begin an episode with this step.  Returns out [B,H,dv].
+
+    The step has no gradient and refuses inputs that want one (outside
+    torch.no_grad()): retention() of tapes of one step with a carried state has."""
     torch = _torch()
     B, _, H, Hk, dk, dv, dt, scale = _retention_args(q, k, v, alpha, start, scale, False)
     if state is None:
         raise TypeError("state must be float32 [B,H,dk,dv]")
     _state_like(state, "state", B, H, dk, dv)
+    if (q.requires_grad or k.requires_grad or v.requires_grad or alpha.requires_grad or state.requires_grad) and \
+            torch.is_grad_enabled():
+        raise RuntimeError("retention_step has no gradient: call it under torch.no_grad(), or retention() on tapes of "
+                           "one step")
     dev = _check_cuda(q, k, v, alpha, start, state)
     out = q.new_empty((B, H, dv))
     _launch("memoroid_retention_step", dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(), _ptr(start),

@@ -253,3 +253,18 @@ def test_retention_needs_flags():
     x = torch.zeros(1, 3, 2, 8)
     with pytest.raises(TypeError):
         mb.scan_retention(x, x, x, torch.zeros(2), None)
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v", "alpha", "state"])
+def test_step_refuses_inputs_that_want_a_gradient(name):
+    """Its result has no graph: a loss on it would miss the step without a word.  Under
+    no_grad the call goes on, here to the refusal of the CPU's tensors."""
+    x = dict(q=torch.zeros(2, 4, 8), k=torch.zeros(2, 2, 8), v=torch.zeros(2, 2, 8), alpha=torch.zeros(4),
+             state=torch.zeros(2, 4, 8, 8))
+    x[name].requires_grad_(True)
+    with pytest.raises(RuntimeError, match="no gradient"):
+        mb.retention_step(**x)
+    with torch.no_grad(), pytest.raises(ValueError):
+        mb.retention_step(**x)
+    with torch.inference_mode(), pytest.raises(ValueError):
+        mb.retention_step(**x)
