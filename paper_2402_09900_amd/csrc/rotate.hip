@@ -149,7 +149,8 @@ __device__ __forceinline__ void wave_lds_fence() {
 template <int BF16, int CH, bool GRAD>
 __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs p) {
     __shared__ float sCs[4][kPairs][2];
-    __shared__ float sDw[GRAD ? 4 : 1][GRAD ? kRotMaxDim : 1];
+    __shared__ double sDw[GRAD ? 4 : 1][GRAD ? kRotMaxDim : 1];
+    __shared__ double sSum[GRAD ? 2 * CH : 1][GRAD ? 256 : 1];   // a lane's sums past 64 rows
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (p.hdr && blockIdx.x == 0 && threadIdx.x < 16) {
         const u32x4 ones = {kEmpty32, kEmpty32, kEmpty32, kEmpty32};
@@ -175,6 +176,23 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs p) {
         da[e] = db[e] = 0.0f;
     }
     to_pairs<CH>(wa, wb, p.inter);
+    // Sums of the weights' gradients are in floats over 64 rows, then in doubles: a
+    // lane's rows grow with the call, and floats would add up their roundings.
+    if constexpr (GRAD) {
+#pragma unroll
+        for (int e = 0; e < 2 * CH; ++e) sSum[e][threadIdx.x] = 0.0;
+    }
+    auto put_by = [&] {
+        if constexpr (GRAD) {
+#pragma unroll
+            for (int e = 0; e < CH; ++e) {
+                sSum[e][threadIdx.x] += (double)da[e];
+                sSum[CH + e][threadIdx.x] += (double)db[e];
+                da[e] = db[e] = 0.0f;
+            }
+        }
+    };
+    int rows = 0;                                          // in da, db
     const bool turned = lane < p.rot / 2;
     const double turns = turned ? (double)p.freq[lane] * 0.15915494309189533577 : 0.0;   // 1 / 2 pi
     constexpr int NR = 2;                                  // rows of a lane in flight
@@ -218,6 +236,11 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs p) {
         }
         for (int row0 = r0 + sub; row0 - sub < r1; row0 += NR * rpw) {
             if (row0 != r0 + sub) fetch(at0, row0, r1);
+            if (GRAD && rows >= 64) {
+                put_by();
+                rows = 0;
+            }
+            rows += NR;
 #pragma unroll
             for (int i = 0; i < NR; ++i) {
                 if (row0 - sub + i * rpw >= r1) break;     // no lane has a row
@@ -290,26 +313,31 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs p) {
     }
     if constexpr (GRAD) {
         if (!p.part) return;
-        // the wavefront's rows of a step, then its four wavefronts, in a fixed order
+        // the lanes of a column, then the four wavefronts, in a fixed order
+        put_by();
+        double a[CH], b[CH];
 #pragma unroll
-        for (int e = 0; e < CH; ++e)
+        for (int e = 0; e < CH; ++e) {
+            a[e] = sSum[e][threadIdx.x];
+            b[e] = sSum[CH + e][threadIdx.x];
 #pragma unroll
             for (int m = 1; m < 64; m <<= 1)
                 if (m >= lpr) {
-                    da[e] += lanes_xor(da[e], m);
-                    db[e] += lanes_xor(db[e], m);
+                    a[e] += __shfl_xor(a[e], m, 64);
+                    b[e] += __shfl_xor(b[e], m, 64);
                 }
-        from_pairs<CH>(da, db, p.inter);
+        }
         if (sub == 0 && L.in)
 #pragma unroll
             for (int e = 0; e < CH; ++e) {
-                sDw[w][L.first + e] = da[e];
-                sDw[w][L.second + e] = db[e];
+                // pairs as they lie in memory: halves, or one behind the other
+                sDw[w][p.inter ? L.first + 2 * e : L.first + e] = a[e];
+                sDw[w][p.inter ? L.first + 2 * e + 1 : L.second + e] = b[e];
             }
         __syncthreads();
         for (int i = threadIdx.x; i < p.d; i += 256)
             p.part[(int64_t)blockIdx.x * p.d + i] =
-                (sDw[0][i] + sDw[GRAD ? 1 : 0][i]) + (sDw[GRAD ? 2 : 0][i] + sDw[GRAD ? 3 : 0][i]);
+                (float)((sDw[0][i] + sDw[GRAD ? 1 : 0][i]) + (sDw[GRAD ? 2 : 0][i] + sDw[GRAD ? 3 : 0][i]));
     }
 }
 

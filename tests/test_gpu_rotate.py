@@ -320,3 +320,45 @@ def test_two_graphs_of_training_steps():
         for c, y in zip(sets, results):
             for a, b in zip(step(*c), y):
                 assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype,value", [("f32", 0.1), ("bf16", 0.7)])
+@pytest.mark.parametrize("rows", [4096, 40960])
+def test_weight_gradient_of_many_rows(dtype, value, rows):
+    """One key head beside 2047 query heads has few lanes, each with `rows` of its rows:
+    sums of equal terms, whose roundings in floats all go one way, against the product.
+    No sum of floats is longer than 64 of them, so the bound above holds: 8e-6."""
+    announce("rotate weights' gradient, %s, %d rows a lane" % (dtype, rows))
+    n, H, d = 4 * rows, 2047, 8                             # four wavefronts for the key head
+    q = torch.ones(n, H, d, dtype=DT[dtype], device=DEV)
+    k = torch.ones(n, 1, d, dtype=DT[dtype], device=DEV)
+    gk = torch.full_like(k, value)
+    w = torch.ones(d, device=DEV)
+    got = mb.rotate_qk_bwd(q, k, None, None, q, gk, w, w)
+    for dw, g, heads in ((got[2], 1.0, H), (got[3], float(gk[0, 0, 0].double()), 1)):
+        want = n * heads * g / np.sqrt(1.0 + float(np.float32(1e-6)))
+        e = float((dw.double() / want - 1).abs().max())
+        print("  %.1e" % e, flush=True)
+        assert e <= 8e-6
+
+
+def test_weight_gradient_past_2_31_elements():
+    """Against blocked 64-bit sums, relative to the sum over absolute values."""
+    n, H, d = 560000, 32, 128
+    announce("rotate weights' gradient n=%d H=%d d=%d bf16" % (n, H, d))
+    g = torch.Generator(device=DEV)
+    g.manual_seed(7)
+    q, gq = (torch.empty(n, H, d, dtype=torch.bfloat16, device=DEV).normal_(generator=g) for _ in range(2))
+    assert q.numel() > 1 << 31
+    gq.abs_()
+    w = torch.linspace(0.5, 1.5, d, device=DEV)
+    dw = mb.rotate_qk_bwd(q, None, None, None, gq, None, w)[2]
+    want, size = (torch.zeros(d, dtype=torch.float64, device=DEV) for _ in range(2))
+    for i in range(0, n, 20000):
+        x = q[i:i + 20000].double()
+        t = gq[i:i + 20000].double() * x / torch.sqrt(x.square().mean(-1, keepdim=True) + 1e-6)
+        want += t.sum((0, 1))
+        size += t.abs().sum((0, 1))
+    e = float(((dw.double() - want).abs() / size).max())
+    print("  %.1e" % e, flush=True)
+    assert e <= 8e-6
