@@ -124,14 +124,14 @@ __device__ __forceinline__ void from_pairs(float (&a)[CH], float (&b)[CH], bool 
     }
 }
 
-// cosine and sine of this lane's pair of a step, times the amplitude; (1, 0) for a
-// pair that is not turned.  turns: of the pair, per position
-__device__ __forceinline__ void angle(float (&cs)[2], bool turned, double turns, int32_t position, float amplitude) {
+// cosine and sine of this lane's pair of a step, times the amplitude (of a pair that
+// is turned).  turns: of the pair, per position
+__device__ __forceinline__ void angle(float (&cs)[2], double turns, int32_t position, float amplitude) {
     const double x = (double)position * turns;
     float s, c;
     sincospif(2.0f * (float)(x - rint(x)), &s, &c);
-    cs[0] = turned ? c * amplitude : 1.0f;
-    cs[1] = turned ? s * amplitude : 0.0f;
+    cs[0] = c * amplitude;
+    cs[1] = s * amplitude;
 }
 // sum over the lanes of a row
 __device__ __forceinline__ float row_sum(float v, int lpr) {
@@ -193,8 +193,11 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs p) {
         }
     };
     int rows = 0;                                          // in da, db
-    const bool turned = lane < p.rot / 2;
-    const double turns = turned ? (double)p.freq[lane] * 0.15915494309189533577 : 0.0;   // 1 / 2 pi
+    // whether the lane's pair e is turned: a selection, since a factor of 0 would make
+    // its neighbour's infinity a NaN
+    const int turned_pairs = p.rot / 2 - L.pair0;
+    auto turned = [&](int e) { return e < turned_pairs; };
+    const double turns = lane < p.rot / 2 ? (double)p.freq[lane] * 0.15915494309189533577 : 0.0;   // 1 / 2 pi
     constexpr int NR = 2;                                  // rows of a lane in flight
     Raw<BF16, CH> xa[NR], xb[NR], ya[GRAD ? NR : 1], yb[GRAD ? NR : 1];
     auto fetch = [&](int64_t at0, int row0, int r1) {
@@ -226,7 +229,7 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs p) {
         const int32_t position = p.rot ? p.positions[t] : 0;
         fetch(at0, r0 + sub, r1);                          // before the angles
         wave_lds_fence();                                  // the last step's angles have been read
-        angle(sCs[w][lane], turned, turns, position, p.amplitude);
+        angle(sCs[w][lane], turns, position, p.amplitude);
         wave_lds_fence();
         float c[CH], s[CH];
 #pragma unroll
@@ -265,8 +268,8 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs p) {
 #pragma unroll
                     for (int e = 0; e < CH; ++e) {
                         const float x = a[e] * (r * wa[e]), y = b[e] * (r * wb[e]);
-                        a[e] = x * c[e] - y * s[e];
-                        b[e] = y * c[e] + x * s[e];
+                        a[e] = turned(e) ? x * c[e] - y * s[e] : x;
+                        b[e] = turned(e) ? y * c[e] + x * s[e] : y;
                     }
                     from_pairs<CH>(a, b, p.inter);
                     if (in) {
@@ -280,9 +283,9 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs p) {
                     to_pairs<CH>(ga, gb, p.inter);
 #pragma unroll
                     for (int e = 0; e < CH; ++e) {
-                        const float x = ga[e] * c[e] + gb[e] * s[e];
-                        gb[e] = gb[e] * c[e] - ga[e] * s[e];
-                        ga[e] = x;
+                        const float x = ga[e], y = gb[e];
+                        ga[e] = turned(e) ? x * c[e] + y * s[e] : x;
+                        gb[e] = turned(e) ? y * c[e] - x * s[e] : y;
                     }
                     if (norm) {
                         float dot = 0.0f;

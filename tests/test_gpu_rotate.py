@@ -362,3 +362,28 @@ def test_weight_gradient_past_2_31_elements():
     e = float(((dw.double() - want).abs() / size).max())
     print("  %.1e" % e, flush=True)
     assert e <= 8e-6
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("d,rot", [(64, 32), (80, 20), (16, 6), (8, 2), (64, 0)])
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+def test_nonfinite_values_behind_the_turned_part(dtype, inter, d, rot, value):
+    """Elements rot .. d - 1 stay as they are, an infinity or NaN among them too, and
+    change no other element: without a norm every row is that of finite values, apart
+    from the element itself; in both directions."""
+    announce("rotate nonfinite %s inter=%d d=%d rot=%d" % (dtype, inter, d, rot))
+    g = torch.Generator(device=DEV)
+    g.manual_seed(8)
+    x = torch.randn(d - rot, 3, d, generator=g, device=DEV).to(DT[dtype])
+    bad = x.clone()
+    i = torch.arange(d - rot, device=DEV)
+    bad[i, 1, rot + i] = value                              # each of them in a step of its own
+    pos = torch.arange(d - rot, dtype=torch.int32, device=DEV)
+    freq = mb.rotary_frequencies(rot, device=DEV) if rot else None
+    for call in (lambda t: mb.rotate_qk(t, None, pos, freq, interleaved=inter, amplitude=1.5)[0],
+                 lambda t: mb.rotate_qk_bwd(t, None, pos, freq, t, None, interleaved=inter, amplitude=1.5)[0]):
+        want = call(x)
+        assert torch.equal(want[..., rot:], x[..., rot:])
+        want[i, 1, rot + i] = value
+        assert torch.equal(torch.nan_to_num(call(bad), nan=-1e6), torch.nan_to_num(want, nan=-1e6))
