@@ -445,14 +445,20 @@ def _shaped(t, *shape):
     return t if t.shape == shape else t.reshape(shape)
 
 
+def _given(workspace, device):
+    """The caller's workspace, if the kernels may write all that it counts."""
+    if workspace.device != device:
+        raise ValueError("the workspace must live on the tensors' device")
+    if not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    return workspace
+
+
 def _workspace(nbytes: int, device, workspace=None):
     """Workspace of a self-initialising entry point."""
     torch = _torch()
-    if workspace is not None:
-        if workspace.device != device:
-            raise ValueError("the workspace must live on the tensors' device")
-        if workspace.numel() >= nbytes:
-            return workspace
+    if workspace is not None and _given(workspace, device).numel() >= nbytes:
+        return workspace
     return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
 
 
@@ -487,9 +493,9 @@ def _prepared(nbytes, device, key, pointers, workspace, entry):
     vectorised kernels) is added here, from the operands' pointers or'ed
     together.  A workspace given by the caller goes to the self-initialising
     `entry` (a smaller one raises EWORKSPACE there)."""
-    stream = _raw_stream(device.index)
     if workspace is not None:
-        return _Workspace(workspace, getattr(lib(), entry), stream)
+        return _Workspace(_given(workspace, device), getattr(lib(), entry), _raw_stream(device.index))
+    stream = _raw_stream(device.index)
     full = (device.index, stream, pointers % 16 == 0, key)
     got = _PREPARED.get(full)
     if got is None:

@@ -268,3 +268,25 @@ def test_step_refuses_inputs_that_want_a_gradient(name):
         mb.retention_step(**x)
     with torch.inference_mode(), pytest.raises(ValueError):
         mb.retention_step(**x)
+
+
+@pytest.mark.parametrize("prepared", [False, True])
+def test_workspaces_that_are_not_what_they_count_are_refused(prepared):
+    """A view that repeats or skips its memory counts bytes that are not its own to
+    write; one on another device is no workspace either.  Refused by both ways that a
+    caller's workspace takes, before the library is called."""
+    def give(workspace, device):
+        if prepared:
+            return mb._prepared(lambda: 1024, device, ("diag",), 0, workspace, "memoroid_scan_diag")
+        return mb._workspace(1024, device, workspace)
+
+    cpu, other = torch.device("cpu"), torch.device("cuda", 0)
+    for bad in (torch.empty(1, dtype=torch.uint8).expand(4096), torch.empty(8192, dtype=torch.uint8)[::2],
+                torch.empty(64, 64, dtype=torch.uint8).T[:32]):
+        with pytest.raises(ValueError, match="contiguous"):
+            give(bad, cpu)
+    with pytest.raises(ValueError, match="device"):
+        give(torch.empty(4096, dtype=torch.uint8), other)
+    if not prepared:
+        whole = torch.empty(4096, dtype=torch.uint8)
+        assert give(whole, cpu) is whole and give(whole[:10], cpu) is not whole
