@@ -832,7 +832,7 @@ def _retention_args(q, k, v, alpha, start, scale, steps):
         wrong = start.dtype != _T.uint8 or start.shape != ((B, T) if steps else (B,))
     if wrong:
         raise TypeError("start must be uint8 %s" % ("[B,T]" if steps else "[B]"))
-    return B, T, H, Hk, dk, dv, dt, float(dk ** -0.5 if scale is None else scale)
+    return B, T, H, Hk, dk, dv, dt, float((dk or 1) ** -0.5 if scale is None else scale)
 
 
 def _state_like(state, name, B, H, dk, dv):

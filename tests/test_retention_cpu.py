@@ -290,3 +290,14 @@ def test_workspaces_that_are_not_what_they_count_are_refused(prepared):
     if not prepared:
         whole = torch.empty(4096, dtype=torch.uint8)
         assert give(whole, cpu) is whole and give(whole[:10], cpu) is not whole
+
+
+def test_heads_without_columns_get_as_far_as_the_others():
+    """dk = 0 has no default scale of its own; the library refuses it (test_sizes), here
+    the layer the CPU's tensors."""
+    x, v = torch.zeros(1, 3, 2, 0), torch.zeros(1, 3, 2, 8)
+    a, s = torch.zeros(2), torch.zeros(1, 3, dtype=torch.uint8)
+    with pytest.raises(ValueError):
+        mb.scan_retention(x, x, v, a, s)
+    with pytest.raises(ValueError):
+        mb.retention_step(x[:, 0], x[:, 0], v[:, 0], a, torch.zeros(1, 2, 0, 8))
