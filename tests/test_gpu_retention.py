@@ -663,3 +663,42 @@ def test_gradient_without_query_heads(dtype, T):
     leaves = [x.clone().requires_grad_(True) for x in (q, k, v)]
     mb.retention(*leaves, alpha, start).backward(g)
     assert not bool(leaves[1].grad.any()) and not bool(leaves[2].grad.any())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Hk", [1, 65535])
+def test_most_heads_of_a_tape(dtype, Hk):
+    """H = 65535 of 128 columns: a chunk's rows span just under 2^31 bytes where the
+    gradients of shared heads are floats.  The first and last query heads' results, and
+    the key heads' gradients as sums over all of them."""
+    T, H, d = 65, 65535, 128
+    announce("retention %s T=%d H=%d/%d d=%d" % (dtype, T, H, Hk, d))
+    g = torch.Generator(device=DEV)
+    g.manual_seed(11)
+    q, k, v, go = (torch.randn(1, T, h, d, generator=g, device=DEV).to(DT[dtype]) for h in (H, Hk, Hk, H))
+    alpha = torch.linspace(0.01, 0.3, H, device=DEV)
+    start = torch.zeros(1, T, dtype=torch.uint8, device=DEV)
+    start[0, [0, 20, 64]] = 1
+    out = mb.scan_retention(q, k, v, alpha, start)
+    dq, dk, dv, da, _ = mb.scan_retention_bwd(q, k, v, alpha, start, go)
+    heads = [0, 1, H - 1]
+    cut = [t[:, :, heads if t.shape[2] == H else [0, 0, 0]].double().cpu().numpy() for t in (q, k, v, go)]
+    args = (*cut[:3], alpha[heads].double().cpu().numpy(), start.cpu().numpy(), d ** -0.5)
+    r, b, m = ref.forward(*args)[0], ref.backward(*args, cut[3]), ref.magnitudes(*args, cut[3])
+    tol = F32_TOL if dtype == "f32" else BF16_TOL
+    for name, y, want in (("out", out, r), ("dq", dq, b["dq"])) + ((("dk", dk, b["dk"]), ("dv", dv, b["dv"])) if Hk == H else ()):
+        assert cond_err(y[:, :, heads].double().cpu().numpy(), want, m[name]) <= tol, name
+    assert cond_err(da[heads].double().cpu().numpy(), b["dalpha"], m["dalpha"]) <= F32_TOL
+    if Hk == 1:                                            # the last step alone: dk = scale v (q . q's head's gradient)
+        p = (go[0, 64].double() @ v[0, 64, 0].double()) * d ** -0.5
+        want = (p[:, None] * q[0, 64].double()).sum(0)
+        size = (p.abs()[:, None] * q[0, 64].double().abs()).sum(0)
+        e = float(((dk[0, 64, 0].double() - want).abs() / torch.maximum(size, want.abs())).max())
+        # a sum of 65535 floats, one after the other: as a walk of as many roundings
+        assert e <= tol + 5 * 2.0 ** -24 * 65535 ** 0.5, e
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_most_tapes(dtype):
+    """B = 32767: the largest grid of a launch for both directions at once."""
+    LongCase(dtype, 32767, 3, 2, 1, 8, 16, "some", True, seed=12).check()

@@ -387,3 +387,8 @@ def test_nonfinite_values_behind_the_turned_part(dtype, inter, d, rot, value):
         assert torch.equal(want[..., rot:], x[..., rot:])
         want[i, 1, rot + i] = value
         assert torch.equal(torch.nan_to_num(call(bad), nan=-1e6), torch.nan_to_num(want, nan=-1e6))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_most_heads(dtype):
+    check(dtype, 1, 3, 65535, 65535, 8, 8, False, seed=1)
