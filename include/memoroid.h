@@ -392,7 +392,8 @@ int memoroid_scan_linattn_bwd(const float* q, const float* k, const float* v,
  *              16-byte aligned.
  *   bf16: products of bf16 inputs, fp32 states and sums; the weights of pairs and
  *   the state as a row reads it keep 2^-17, results are rounded to bf16 once.  The
- *   states out are fp32 results.  fp32: fp32 precision throughout.
+ *   states out are fp32 results.  fp32: fp32 states and sums, products of two
+ *   floats keep 2^-21.
  *   A NaN or Inf stays in its episode and in the steps from its own on; there
  *   an Inf may come out as NaN.  So may elements above 2^100, and products of two
  *   (q_t . k_s among them), which can overflow before they have decayed.
@@ -452,7 +453,8 @@ int memoroid_scan_retention_bwd(const void* q, const void* k, const void* v, con
  *   no row begins).  Limits as for memoroid_scan_retention; B may be larger
  *   as long as B * H * ceil(dv / 32) is below 2^24.
  *   The state is rounded to fp32 at every step: where a step's decay and k^T v are
- *   less than half its last place (rates below 2^-24) it stays as it is.
+ *   less than half its last place (rates below 2^-24) it stays as it is.  An
+ *   infinite element may become NaN.
  * ------------------------------------------------------------------------ */
 int memoroid_retention_step(const void* q, const void* k, const void* v, const float* alpha,
                             const uint8_t* start, float* state, void* out, float scale,
@@ -467,7 +469,9 @@ int memoroid_retention_step(const void* q, const void* k, const void* v, const f
  *     (y_a, y_b) -> amplitude (y_a cos - y_b sin, y_b cos + y_a sin)  for the pairs
  * p < rot / 2, angle = positions[i] * freq[p]; elements rot .. d - 1 stay.  A pair
  * is (p, p + rot / 2), or (2 p, 2 p + 1) when interleaved is nonzero.
- * Angles are reduced in 64 bits: far positions keep fp32's precision.
+ * Angles are reduced in 64 bits: far positions keep fp32's precision.  The mean of
+ * squares is an fp32 number: rows whose squares overflow it (elements above 2^60) may
+ * come out as zeros, and rows below 2^-60 need an eps above 0.
  *
  *   q          [n][H][d];  k: [n][Hk][d], n steps (B * T of them), of `dtype`
  *              (MEMOROID_F32 or MEMOROID_BF16).  H or Hk may be 0: that tensor and

@@ -912,10 +912,11 @@ struct RetPlan {
     size_t off_states = 0, off_R = 0, total = 0;
 };
 
-// Enough segments for `groups` workgroups, down to a chunk each.  512, two on each of
-// the 256 CUs: a walk of T = 32768, 4 heads of 64, fp32, takes 45 us, 62 with half as
-// many and 45 with twice as many, which have twice the states to scan.  A chunk:
-// T = 1000, the forward pass 33 -> 20 us against segments of four.
+// Enough segments for `groups` workgroups, down to a chunk each.  Forward 512, two on
+// each of the 256 CUs (a call with 256 / 512 / 1024: T = 32768, 4 heads of 64, fp32, 88 /
+// 64 / 67 us; 32 + 8 heads of 128, bf16, 492 / 404 / 429; 8 tapes of 4096, 16 heads of
+// 128, bf16, 257 / 220 / 246).  A chunk: T = 1000, the forward pass 33 -> 20 us against
+// segments of four.
 void ret_segments(int64_t B, int64_t T, int64_t H, int planes, int64_t groups, RetPlan* p) {
     const int64_t C = ret_chunk(planes), n = (T + C - 1) / C;
     int64_t nseg = (groups + B * H - 1) / (B * H);
@@ -966,9 +967,10 @@ struct RetBwdPlan {
 bool plan_retention_bwd(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t dk, int64_t dv, int planes, bool want_alpha,
                         RetBwdPlan* p) {
     // The pass that prepares the segments has one workgroup on a CU unless the head is
-    // narrow, and the three walks fill the CUs with half the segments: T = 4096, 8
-    // tapes, 16 heads of 128, bf16, 1150 us with 512 groups, 1100 with 256 (kernels,
-    // forward pass included); T = 32768, 4 heads of 64, fp32, 267 and 291.
+    // narrow, and the three walks fill the CUs with half the segments.  A call with 256 /
+    // 512 groups: T = 4096, 8 tapes, 16 heads of 128, bf16, 797 / 822 us (without the
+    // rates' gradient 592 / 609); T = 32768, 32 + 8 heads of 128, bf16, 1705 / 1718 (1394
+    // / 1378); T = 32768, 4 heads of 64, fp32, 184 / 165 (144 / 143).
     ret_segments(B, T, H, planes, dk <= 64 && dv <= 64 ? 512 : 256, &p->fwd);
     const size_t states = ret_states_bytes(p->fwd, B, H, dk, dv);
     p->nparts = p->fwd.nseg + ret_scan_parts(dk * dv, B * H, p->fwd.nseg);

@@ -100,9 +100,9 @@ __device__ __forceinline__ f32x4 pair_products(const uint16_t* sY, const uint16_
 
 // ---------------------------------------------------------------- summaries
 // What a segment adds to the state after it: the sum over its rows from the last
-// begin on.  Reads y and z once: T = 65536, 16 heads of 128, bf16, 151 us, 3.5 TB/s
-// (8 tapes of 4096, state not asked for: 64 us, 3.1 TB/s), with waits for memory in
-// 0.44 of its wavefronts' time.
+// begin on.  Reads y and z once: T = 65536, 16 heads of 128, bf16, 136 us, 4.1 TB/s
+// with the states written (8 tapes of 4096: 63 us, 3.6 TB/s); its wavefronts wait
+// for 0.35 of their time.
 template <class Cfg>
 __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummaryArgs p) {
     __shared__ __attribute__((aligned(16))) uint16_t sY[Cfg::NP * Cfg::C * Cfg::KD];
@@ -197,13 +197,14 @@ __global__ __launch_bounds__(Cfg::THREADS, 4) void ret_summary_kernel(RetSummary
 //
 // One pass reads q, k, v and g once, with the states in registers, 64 rows of each per
 // wavefront (RetCfg64).  With four states of 128 x 128 a workgroup of 16 wavefronts
-// takes all 128 registers of each; what the next chunk's rows need of them is free
-// only behind the outer products, so they are fetched there (T = 4096, 8 tapes, 16
-// heads, bf16: 380 us, 504 fetched before them, 487 in two passes of eight wavefronts
-// with two states each).  Its VALU instructions take about 210 of those, the matrix
-// cores 86; half of them form the rows' weights in three planes, once for each 64 of
-// the state's rows.  (Once for all of them, the second state's columns in lanes c >= 8
-// of a wavefront with 8 columns: 531 us, since more registers spill.)
+// takes all 128 registers of each and spills 16; what the next chunk's rows need of
+// them is free only behind the outer products, so they are fetched there.  T = 4096, 8
+// tapes, 16 heads, bf16: 326 us.  Its VALU instructions take about 210 of those, the
+// matrix cores 86; half of them form the rows' weights in three planes, once for each
+// 64 of the state's rows.  In short runs, before the clocks have risen, 380 us: 504
+// with the rows fetched before the products, 487 in two passes of eight wavefronts with
+// two states each, 531 with the weights formed once for all rows (the second state's
+// columns in lanes c >= 8 of a wavefront with 8 columns), since more registers spill.
 //
 // A value that is not finite would reach other episodes and earlier rows through
 // zero weights.  Without ALPHA the rows that take no part become zeros.  With
@@ -499,8 +500,8 @@ __global__ __launch_bounds__(Cfg::THREADS, Cfg::THREADS == 1024 ? 4 : 2) void re
 // loads in flight at once; the groups combine through LDS.  One read and one write
 // of the states.  One group where there are few segments or many columns (3
 // segments of 128 heads of 128 x 128: 10 us, 294 us in 32 groups; 31 segments of 16
-// such heads: 16 and 53 us), else 32 (128 segments of 4 heads of 64 x 64: 8 us, 39 us
-// one segment after the other).
+// such heads: 12 us, 53 in 32 groups in a short run, in which one takes 16), else 32
+// (128 segments of 4 heads of 64 x 64: 9 us, 39 us one segment after the other).
 template <bool DOT>
 struct SegState {
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f}, d = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -691,11 +692,12 @@ __device__ __forceinline__ bool pairs(u32x2 (&sP)[Cfg::NTILE][Cfg::FP][64], cons
 }
 
 // Two workgroups on a CU, whose phases (staging, pairs, rows against the state, rows
-// into it) cover each other's waits.  T = 65536, 16 heads of 128, bf16, state out: 329
-// us, 3.3 TB/s of x, y, z and out; 8 tapes of 4096 without: 147 us, 3.7 TB/s, and 437
-// for the gradient's three walks.  fp32, T = 32768, 4 heads of 64: 45 us, and 108 for
-// three: 394 TFLOP/s of bf16 products, six for one of floats, a third of what a large
-// bf16 product reaches.
+// into it) cover each other's waits.  T = 65536, 16 heads of 128, bf16: 303 us, 3.5
+// TB/s of x, y, z and out; 8 tapes of 4096: 149 us, 3.6 TB/s, and 441 for the
+// gradient's three walks, with the matrix cores busy for a quarter of the time and waits
+// in 0.42 of the wavefronts'.  fp32, T = 32768, 4 heads of 64: 41 us, and 97 for three: 440
+// TFLOP/s of bf16 products, six for one of floats, 0.38 of what a large bf16 product
+// reaches.
 template <class Cfg>
 __global__ __launch_bounds__(Cfg::THREADS, Cfg::VD == 128 ? 4 : Cfg::KD == 128 ? 2 : 3)
     void ret_walk_kernel(RetWalkSet set) {

@@ -17,7 +17,7 @@
 // are.  A float goes in as three bf16 planes, x = h + m + l with h and m its
 // leading bits cut off: exact, 8 bits each.  Two such numbers take the six
 // products of planes whose indices add to at most 2; what is left out is below
-// 2^-21 of the product, so a product of floats keeps a float's precision at six
+// 2^-21 of the product, which sums of 64 and more floats do not keep either: six
 // bf16 instructions, 16 / 6 of the rate of the fp32 matrix cores.
 //
 // With lane = 16 g + c the instruction takes A[i = c][k = 8 g + e] and
@@ -166,12 +166,15 @@ __device__ __forceinline__ RetRows ret_rows(const void* head0, int64_t row_bytes
 }
 
 // Where the 16-byte unit `unit` of row `row` of an LDS tile of D columns lies: the
-// units of a row are exchanged by its number, so that no operand meets a bank
-// conflict and rows need no padding.  A row operand reads one unit of 16 rows,
+// units of a row are exchanged by its number, so that operands take the cycles of
+// their bytes and rows need no padding.  A row operand reads one unit of 16 rows,
 // which lie in different banks (28 cycles more without the exchange); a column
 // operand reads half a unit each of four units, a quarter of the row, in four
 // neighbouring rows, so it is those rows' numbers that tell the quarters apart
 // (with the quarters told apart by row / 4 they were 5.5 cycles more a read).
+// Counted (128 x 128, bf16): SQ_LDS_IDX_ACTIVE of a walk is 546 cycles per wavefront
+// and chunk, which moves 71 KB, 554 cycles at 128 bytes each; SQ_LDS_BANK_CONFLICT
+// calls 200 of them conflicts, two of the four of every transposed read among them.
 template <int D>
 __device__ __forceinline__ int swizzled(int unit, int row) {
     static_assert(D == 64 || D == 128, "8 or 16 units a row");

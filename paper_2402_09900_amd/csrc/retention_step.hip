@@ -4,8 +4,8 @@
 //     S <- gamma S + k^T v   (k^T v at a begin),   out = scale q S
 //
 // Bound by the state, read once and written once (2 x 4 dk dv bytes a head; q, k,
-// v and out are a hundredth of it): 256 rows of 16 heads of 128 in 108 us, 5.0 TB/s,
-// what a copy reaches; 16 rows of 4 heads of 64 in 4.  A workgroup takes 32 columns
+// v and out are a hundredth of it): 256 rows of 16 heads of 128 in 106 us, 5.1 TB/s;
+// 16 rows of 4 heads of 64 in 4.  A workgroup takes 32 columns
 // of one head's state, a 128-byte line of each of its rows: eight lanes a row, 32
 // rows at a time, so that a head of 128 x 128 has all its loads in flight at once,
 // and a small batch still spreads over the chip (16 rows of 4 heads of 64: 128

@@ -9,9 +9,9 @@
 //
 // Bound by memory: every element read once and written once (gradient: x and the
 // upstream gradient read), 10 (gradient: 30) flops each.  65536 steps of 16 + 16
-// heads of 128, bf16: 190 us, 5.6 TB/s, faster than a copy of 2 GiB (4.9).  32768
-// steps of 32 + 8 heads of 128, bf16: 126 us forward, gradient 207 (4.9 TB/s) and 7
-// for the weights' sums.
+// heads of 128, bf16: 192 us, 5.6 TB/s.  32768 steps of 32 + 8 heads of 128, bf16: 123
+// us forward, gradient 206 (4.9 TB/s) and 6 for the weights' sums; 32768 steps of 16 +
+// 16 heads of 128, fp32: a call of either 205 and 312 us, 5.2 TB/s.
 //
 // A lane holds two runs of CH elements, A and B, that are the halves of its CH pairs
 // (half layout: elements p and p + rot / 2; interleaved: the even and odd ones of
