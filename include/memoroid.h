@@ -110,7 +110,10 @@ typedef enum {
     MEMOROID_OP_TBB_SAMPLE = 9,        /* memoroid_tbb_sample[_prepared]:     (B = n_draws, T = batch) */
     MEMOROID_OP_RETENTION = 10,        /* memoroid_scan_retention:      (B, T, d_or_H = H, dk, dv) */
     MEMOROID_OP_RETENTION_BWD = 11,    /* memoroid_scan_retention_bwd:  (B, T, d_or_H = H, dk, dv), any Hk */
-    MEMOROID_OP_ROTATE_QK_BWD = 12     /* memoroid_rotate_qk_bwd:       (T = n, d_or_H = H, dk = Hk, dv = d) */
+    MEMOROID_OP_ROTATE_QK_BWD = 12,    /* memoroid_rotate_qk_bwd:       (T = n, d_or_H = H, dk = Hk, dv = d) */
+    MEMOROID_OP_GATED = 13,            /* memoroid_scan_gated:          (B, T, d_or_H = d) */
+    MEMOROID_OP_GATED_BWD = 14,        /* memoroid_scan_gated_bwd:      (B, T, d_or_H = d) */
+    MEMOROID_OP_LAYER_NORM_BWD = 15    /* memoroid_layer_norm_bwd:      (T = n, d_or_H = d) */
 } memoroid_op;
 
 /* Version of this header the library was built from (MEMOROID_ABI_VERSION). */
@@ -513,6 +516,142 @@ int memoroid_rotate_qk_bwd(const void* q, const void* k, const int32_t* position
                            float* grad_wq, float* grad_wk, float eps, float amplitude, int interleaved,
                            int64_t n, int64_t H, int64_t Hk, int64_t d, int64_t rot, int dtype,
                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Gated recurrence: the real diagonal memoroid whose decay and input are gated at
+ * every step, over B tapes of episodes.  Per feature, with (r, i) the step's gates
+ * and sig the sigmoid,
+ *     u_t = |alpha| sig(r_t),   a_t = exp(-u_t),   b_t = sqrt(1 - a_t^2) sig(i_t) x_t,
+ *     h_t = b_t at a begin step,   a_t h_{t-1} + b_t otherwise.
+ *
+ *   x          [B][T][d];  gates: [B][T][2][d], r before i; of `dtype`
+ *              (MEMOROID_F32 or MEMOROID_BF16).
+ *   alpha      [d] fp32, finite; its sign means nothing, 0 is no decay (and lets no
+ *              input in).
+ *   start      [B][T] begin flags.  As for retention, step 0 is a begin step only if its
+ *              flag says so: a tape may go on from state_in.
+ *   state_in   optional [B][d] fp32, the state before step 0 (NULL: 0).
+ *   h          out [B][T][d] of dtype.
+ *   state_out  optional out [B][d] fp32, the state after step T - 1 (not rounded to
+ *              bf16); not written when T is 0.
+ *   states     optional out [B][ceil(T / MEMOROID_GATED_STATE_STEPS)][d] fp32, the states
+ *              before steps 0, 128, 256 ...: what the gradient starts from.
+ *   Gates may be infinite: r = -inf holds the state and lets nothing in (a = 1, b = 0),
+ *   r = inf takes the whole rate.  A NaN (or an infinite x) stays in its feature's episode
+ *   and in the steps from its own on.  States are fp32; b, a and their products are right
+ *   to a few 2^-24; h is rounded to bf16 once.  Results do not depend on timing.
+ *   d <= 2^18, T < 2^30 and B ceil(T / 64) ceil(d / 64) < 2^23 (MEMOROID_EUNSUPPORTED
+ *   otherwise).  fp32 arrays 4-byte aligned.  state_out must
+ *   not be state_in.  Workspace (self-initialising): memoroid_scan_gated_workspace_bytes.
+ * ------------------------------------------------------------------------ */
+#define MEMOROID_GATED_STATE_STEPS 128
+
+size_t memoroid_scan_gated_workspace_bytes(int64_t B, int64_t T, int64_t d, int dtype);
+
+int memoroid_scan_gated(const void* x, const void* gates, const float* alpha, const uint8_t* start,
+                        const float* state_in, void* h, float* state_out, float* states,
+                        int64_t B, int64_t T, int64_t d, int dtype,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Its gradient.  With g = dL/dh and G = dL/dh_{T-1} beside it,
+ *     lam_t = g_t + [t+1 < T and step t+1 is not a begin] a_{t+1} lam_{t+1} + [t == T-1] G,
+ *     hp_t = h_{t-1}, 0 at a begin step,   m_t = sqrt(1 - a_t^2),
+ *     dx_t = lam_t m_t sig(i_t),   di_t = lam_t b_t (1 - sig(i_t)),
+ *     du_t = lam_t a_t (sig(i_t) x_t a_t / m_t - hp_t)   (no first term where m_t is 0),
+ *     dr_t = du_t u_t (1 - sig(r_t)),   dalpha = sign(alpha) sum du_t sig(r_t)  (sign(0) = 0),
+ *     dstate_in = [step 0 is not a begin] a_0 lam_0.
+ *
+ *   x, gates, alpha, start  as in the forward call, states as it wrote them.
+ *   grad_h     [B][T][d] of dtype;  grad_state_out: optional [B][d] fp32: G (NULL: 0).
+ *   grad_x, grad_gates  out, like x and gates.
+ *   grad_alpha optional out [d] fp32;  grad_state_in: optional out [B][d] fp32.
+ *   An empty problem writes no output: with no steps grad_alpha is zero and
+ *   grad_state_in is G, the caller's to set.
+ *   Workspace (self-initialising): memoroid_scan_gated_bwd_workspace_bytes.
+ * ------------------------------------------------------------------------ */
+size_t memoroid_scan_gated_bwd_workspace_bytes(int64_t B, int64_t T, int64_t d, int dtype);
+
+int memoroid_scan_gated_bwd(const void* x, const void* gates, const float* alpha, const uint8_t* start,
+                            const float* states, const void* grad_h, const float* grad_state_out,
+                            void* grad_x, void* grad_gates, float* grad_alpha, float* grad_state_in,
+                            int64_t B, int64_t T, int64_t d, int dtype,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * One step of the gated recurrence for B rows, the state updated in place.
+ *   x [B][d], gates [B][2][d], h out [B][d] of dtype;  alpha [d], state [B][d] fp32;
+ *   start: optional [B] begin flags (NULL: no row begins).  d <= 2^18, B d < 2^31
+ *   (MEMOROID_EUNSUPPORTED otherwise).
+ * ------------------------------------------------------------------------ */
+int memoroid_gated_step(const void* x, const void* gates, const float* alpha, const uint8_t* start,
+                        float* state, void* h, int64_t B, int64_t d, int dtype, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Dropout into a residual: out = residual + mask x / (1 - p) (residual NULL: 0), rows of
+ * d elements.  The mask is a function of (seed, step, site, row, column), never stored;
+ * the gradient of x is the same call on the upstream gradient, without the residual.
+ *
+ * An element stays if its 32-bit number is not below p 2^32 (rounded to the nearest).
+ * Philox4x32-10 (Salmon, Moraes, Dror, Shaw 2011) with key (seed low, seed high) and
+ * counter (column / 8, row, step, site) gives four words, their eight 16-bit halves
+ * (low before high) being the upper halves of the numbers of eight columns; the lower
+ * halves come from the same counter with the top bit of its first word set.
+ *
+ *   x, out     [n][d] of `dtype` (MEMOROID_F32 or MEMOROID_BF16), residual like x.
+ *   rng        [2] int64 in device memory: seed, and step, of which the low 32 bits count.
+ *              Read by the kernels, so a captured call sees what is there at each replay.
+ *              May be NULL when p is 0.
+ *   site       0 <= site < 2^32: which of a model's dropouts this is.
+ *   p          0 <= p <= 1 (MEMOROID_EINVAL otherwise).  A dropped element is 0 (the
+ *              residual), whatever x holds there; p = 1 drops all.
+ *   n < 2^31, d < 2^31, n ceil(d / 8) < 2^31 (MEMOROID_EUNSUPPORTED otherwise).  out may
+ *   not be x or the residual.  No workspace.
+ * ------------------------------------------------------------------------ */
+int memoroid_dropout(const void* x, const void* residual, const int64_t* rng, void* out,
+                     double p, int64_t site, int64_t n, int64_t d, int dtype, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Layer norm of rows, with dropout and the residual in the same pass:
+ *     s = residual + mask x / (1 - p)   (as memoroid_dropout; s = x with neither),
+ *     y = (s - mean) rstd weight + bias,   rstd = 1 / sqrt(mean((s - mean)^2) + eps).
+ * Sums are fp32, the deviation from the mean is taken before it is squared; y is formed
+ * from s before s is rounded.
+ *
+ *   x, residual, rng, p, site  as for memoroid_dropout.
+ *   weight, bias  optional [d] fp32 (NULL: 1, 0).
+ *   y          out [n][d] of dtype;  s_out: optional out, likewise.
+ *   stats      optional out [n][2] fp32: mean and rstd, for the gradient.
+ *   eps >= 0, finite.  1 <= d <= 16384, n < 2^31 (MEMOROID_EUNSUPPORTED otherwise).  A row
+ *   whose values are all equal has no deviation but the rounding of its mean; with eps = 0
+ *   it may come out as NaN.  A NaN or Inf stays in its row.  No workspace.
+ * ------------------------------------------------------------------------ */
+int memoroid_layer_norm(const void* x, const void* residual, const float* weight, const float* bias,
+                        const int64_t* rng, void* y, void* s_out, float* stats,
+                        float eps, double p, int64_t site, int64_t n, int64_t d, int dtype, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Its gradient.  With xh = (s - mean) rstd and gw = grad_y weight,
+ *     ds = grad_s + rstd (gw - mean(gw) - xh mean(gw xh)),
+ *     dresidual = ds,   dx = mask ds / (1 - p),
+ *     dweight = sum over rows of grad_y xh,   dbias = sum of grad_y.
+ *
+ *   x, residual, weight, rng, p, site  as in the forward call, stats as it wrote them.
+ *   grad_y     [n][d] of dtype;  grad_s: optional, likewise (NULL: 0).
+ *   grad_x     out [n][d];  grad_residual: optional out [n][d]; with p = 0 it equals
+ *              grad_x and may be left out.
+ *   grad_weight, grad_bias  optional out [d] fp32 (n = 0 writes nothing: zeros, the
+ *              caller's to set).
+ *   Workspace (self-initialising), needed only for grad_weight or grad_bias:
+ *   memoroid_layer_norm_bwd_workspace_bytes.
+ * ------------------------------------------------------------------------ */
+size_t memoroid_layer_norm_bwd_workspace_bytes(int64_t n, int64_t d);
+
+int memoroid_layer_norm_bwd(const void* x, const void* residual, const float* weight, const int64_t* rng,
+                            const float* stats, const void* grad_y, const void* grad_s,
+                            void* grad_x, void* grad_residual, float* grad_weight, float* grad_bias,
+                            double p, int64_t site, int64_t n, int64_t d, int dtype,
+                            void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * Discounted return over a tape (App. D, the discounted-return memoroid

@@ -13,8 +13,9 @@ runs in the library's HIP kernels:
   of prepared workspaces, one per (device, stream, entry point, sizes,
   flags, operand alignment).  A workspace tensor passed in explicitly goes
   to the self-initialising entry point (which fills what it needs on the
-  stream), as retention and rotation always do, on a workspace of the call's
-  own where none is passed.  ``diag_scan``, ``retention`` and ``qk_rotate`` are
+  stream), as retention, rotation, the gated recurrence and layer norm always
+  do, on a workspace of the call's own where none is passed.  ``diag_scan``,
+  ``retention``, ``qk_rotate``, ``gated_scan``, ``layer_norm`` and ``dropout`` are
   the differentiable forms (``torch.autograd.Function``).
 
 Loading fails loudly (``MemoroidError``) if the shared library is missing:
@@ -35,7 +36,10 @@ LIB_PATH = os.path.join(HERE, "libmemoroid.so")
 OK, EINVAL, EUNSUPPORTED, EWORKSPACE, EHIP, ETIMEOUT, EMISMATCH = 0, -1, -2, -3, -4, -5, -6
 F32, BF16, C64 = 0, 1, 2
 (OP_DIAG, OP_DIAG_BWD, OP_LINATTN, OP_LINATTN_BWD, OP_FFM, OP_FFM_BWD, OP_RETURN, OP_GAE,
- OP_TBB_BEGIN_INDICES, OP_TBB_SAMPLE, OP_RETENTION, OP_RETENTION_BWD, OP_ROTATE_QK_BWD) = range(13)
+ OP_TBB_BEGIN_INDICES, OP_TBB_SAMPLE, OP_RETENTION, OP_RETENTION_BWD, OP_ROTATE_QK_BWD, OP_GATED, OP_GATED_BWD,
+ OP_LAYER_NORM_BWD) = range(16)
+
+GATED_STATE_STEPS = 128             # MEMOROID_GATED_STATE_STEPS
 
 _lib = None
 
@@ -128,6 +132,25 @@ def lib() -> ctypes.CDLL:
         L.memoroid_rotate_qk_bwd_workspace_bytes.argtypes = [I64] * 5 + [I32, I32]
         L.memoroid_rotate_qk_bwd.restype = I32
         L.memoroid_rotate_qk_bwd.argtypes = [P] * 12 + [F, F, I32] + [I64] * 5 + [I32, P, SZ, P]
+        L.memoroid_scan_gated_workspace_bytes.restype = SZ
+        L.memoroid_scan_gated_workspace_bytes.argtypes = [I64] * 3 + [I32]
+        L.memoroid_scan_gated.restype = I32
+        L.memoroid_scan_gated.argtypes = [P] * 8 + [I64] * 3 + [I32, P, SZ, P]
+        L.memoroid_scan_gated_bwd_workspace_bytes.restype = SZ
+        L.memoroid_scan_gated_bwd_workspace_bytes.argtypes = [I64] * 3 + [I32]
+        L.memoroid_scan_gated_bwd.restype = I32
+        L.memoroid_scan_gated_bwd.argtypes = [P] * 11 + [I64] * 3 + [I32, P, SZ, P]
+        L.memoroid_gated_step.restype = I32
+        L.memoroid_gated_step.argtypes = [P] * 6 + [I64] * 2 + [I32, P]
+        D = ctypes.c_double
+        L.memoroid_dropout.restype = I32
+        L.memoroid_dropout.argtypes = [P] * 4 + [D] + [I64] * 3 + [I32, P]
+        L.memoroid_layer_norm.restype = I32
+        L.memoroid_layer_norm.argtypes = [P] * 8 + [F, D] + [I64] * 3 + [I32, P]
+        L.memoroid_layer_norm_bwd_workspace_bytes.restype = SZ
+        L.memoroid_layer_norm_bwd_workspace_bytes.argtypes = [I64] * 2
+        L.memoroid_layer_norm_bwd.restype = I32
+        L.memoroid_layer_norm_bwd.argtypes = [P] * 11 + [D] + [I64] * 3 + [I32, P, SZ, P]
         L.memoroid_testing_set_fallback_polls.restype = I64
         L.memoroid_testing_set_fallback_polls.argtypes = [I64]
         L.memoroid_testing_tile_steps.restype = I64
@@ -353,6 +376,49 @@ def memoroid_rotate_qk_bwd(q, k, positions, freq, wq, wk, grad_q_out, grad_k_out
     return lib().memoroid_rotate_qk_bwd(q, k, positions, freq, wq, wk, grad_q_out, grad_k_out, grad_q, grad_k, grad_wq,
                                         grad_wk, eps, amplitude, interleaved, n, H, Hk, d, rot, dtype, workspace,
                                         workspace_bytes, stream)
+
+
+def memoroid_scan_gated_workspace_bytes(B, T, d, dtype) -> int:
+    return lib().memoroid_scan_gated_workspace_bytes(B, T, d, dtype)
+
+
+def memoroid_scan_gated(x, gates, alpha, start, state_in, h, state_out, states, B, T, d, dtype, workspace,
+                        workspace_bytes, stream) -> int:
+    return lib().memoroid_scan_gated(x, gates, alpha, start, state_in, h, state_out, states, B, T, d, dtype, workspace,
+                                     workspace_bytes, stream)
+
+
+def memoroid_scan_gated_bwd_workspace_bytes(B, T, d, dtype) -> int:
+    return lib().memoroid_scan_gated_bwd_workspace_bytes(B, T, d, dtype)
+
+
+def memoroid_scan_gated_bwd(x, gates, alpha, start, states, grad_h, grad_state_out, grad_x, grad_gates, grad_alpha,
+                            grad_state_in, B, T, d, dtype, workspace, workspace_bytes, stream) -> int:
+    return lib().memoroid_scan_gated_bwd(x, gates, alpha, start, states, grad_h, grad_state_out, grad_x, grad_gates,
+                                         grad_alpha, grad_state_in, B, T, d, dtype, workspace, workspace_bytes, stream)
+
+
+def memoroid_gated_step(x, gates, alpha, start, state, h, B, d, dtype, stream) -> int:
+    return lib().memoroid_gated_step(x, gates, alpha, start, state, h, B, d, dtype, stream)
+
+
+def memoroid_dropout(x, residual, rng, out, p, site, n, d, dtype, stream) -> int:
+    return lib().memoroid_dropout(x, residual, rng, out, p, site, n, d, dtype, stream)
+
+
+def memoroid_layer_norm(x, residual, weight, bias, rng, y, s_out, stats, eps, p, site, n, d, dtype, stream) -> int:
+    return lib().memoroid_layer_norm(x, residual, weight, bias, rng, y, s_out, stats, eps, p, site, n, d, dtype, stream)
+
+
+def memoroid_layer_norm_bwd_workspace_bytes(n, d) -> int:
+    return lib().memoroid_layer_norm_bwd_workspace_bytes(n, d)
+
+
+def memoroid_layer_norm_bwd(x, residual, weight, rng, stats, grad_y, grad_s, grad_x, grad_residual, grad_weight,
+                            grad_bias, p, site, n, d, dtype, workspace, workspace_bytes, stream) -> int:
+    return lib().memoroid_layer_norm_bwd(x, residual, weight, rng, stats, grad_y, grad_s, grad_x, grad_residual,
+                                         grad_weight, grad_bias, p, site, n, d, dtype, workspace, workspace_bytes,
+                                         stream)
 
 
 def memoroid_workspace_status(workspace, workspace_bytes, stream) -> int:
@@ -1018,6 +1084,200 @@ def rotate_qk_bwd(q, k, positions, freq, grad_q, grad_k, wq=None, wk=None, eps: 
     return gq, gk, gwq, gwk
 
 
+def _gated_args(x, gates, alpha, start, steps: bool):
+    """Sizes of a gated call (steps: tapes, else single steps) and its checks."""
+    shape = x.shape
+    if len(shape) != (3 if steps else 2):
+        raise ValueError("x must be %s" % ("[B,T,d]" if steps else "[B,d]"))
+    B, T, d = shape if steps else (shape[0], 1, shape[1])
+    if gates.shape != shape[:-1] + (2, d):
+        raise ValueError("gates must be %s" % ("[B,T,2,d]" if steps else "[B,2,d]"))
+    if gates.dtype != x.dtype:
+        raise TypeError("x and gates must share a dtype")
+    dt = _code_of(x.dtype)
+    if dt == C64:
+        raise TypeError("the gated recurrence takes float32 or bfloat16")
+    if alpha.dtype != _T.float32 or alpha.shape != (d,):
+        raise TypeError("alpha must be float32 [d]")
+    if (start is None and steps) or (start is not None and (start.dtype != _T.uint8 or start.shape != shape[:-1])):
+        raise TypeError("start must be uint8 %s" % ("[B,T]" if steps else "[B]"))
+    return B, T, d, dt
+
+
+def _gated_state(state, name, B, d):
+    if state is not None and (state.dtype != _T.float32 or state.shape != (B, d)):
+        raise TypeError("%s must be float32 [B,d]" % name)
+
+
+def scan_gated(x, gates, alpha, start, state=None, final_state: bool = False, keep_states: bool = False, workspace=None):
+    """Gated recurrence over B tapes: per feature, with (r, i) the step's gates and
+    u = |alpha| sigmoid(r), a = exp(-u),
+
+        h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigmoid(i_t) x_t
+
+    without the first term at a begin step.  x: [B,T,d]; gates: [B,T,2,d] (r, i),
+    float32 or bfloat16; alpha: float32 [d]; start: uint8 [B,T]; state: optional
+    float32 [B,d], the state before step 0 (which begins an episode only if its flag
+    says so).  Returns h [B,T,d], followed by the float32 state after the last step
+    when final_state is true and by the states [B,ceil(T/128),d] that scan_gated_bwd
+    takes when keep_states is true."""
+    torch = _torch()
+    B, T, d, dt = _gated_args(x, gates, alpha, start, True)
+    _gated_state(state, "state", B, d)
+    dev = _check_cuda(x, gates, alpha, start, state)
+    h = torch.empty_like(x)
+    last = alpha.new_empty((B, d)) if final_state else None
+    kept = alpha.new_empty((B, -(-T // GATED_STATE_STEPS), d)) if keep_states else None
+    if T == 0 and final_state:                  # no step: the state stays
+        last.zero_() if state is None else last.copy_(state)
+    ws = _workspace(lib().memoroid_scan_gated_workspace_bytes(B, T, d, dt), dev, workspace)
+    _launch("memoroid_scan_gated", dev, x.data_ptr(), gates.data_ptr(), alpha.data_ptr(), start.data_ptr(), _ptr(state),
+            h.data_ptr(), _ptr(last), _ptr(kept), B, T, d, dt, ws.data_ptr(), ws.numel())
+    got = (h,) + ((last,) if final_state else ()) + ((kept,) if keep_states else ())
+    return got if len(got) > 1 else h
+
+
+def scan_gated_bwd(x, gates, alpha, start, states, grad_h, grad_state=None, need_grad_alpha: bool = True,
+                   need_grad_state: bool = True, workspace=None):
+    """Gradient of scan_gated: (dx, dgates, dalpha, dstate), from the states that
+    scan_gated kept.  grad_state is the gradient of the state after the last step (None:
+    zero); dalpha and dstate are None if not needed."""
+    torch = _torch()
+    B, T, d, dt = _gated_args(x, gates, alpha, start, True)
+    _gated_state(grad_state, "grad_state", B, d)
+    if states.dtype != torch.float32 or states.shape != (B, -(-T // GATED_STATE_STEPS), d):
+        raise TypeError("states must be float32 [B,ceil(T/128),d]")
+    if grad_h.dtype != x.dtype or grad_h.shape != x.shape:
+        raise TypeError("grad_h must be [B,T,d] of x's dtype")
+    dev = _check_cuda(x, gates, alpha, start, states, grad_h, grad_state)
+    gx, gg = torch.empty_like(x), torch.empty_like(gates)
+    ga = torch.empty_like(alpha) if need_grad_alpha else None
+    gs = alpha.new_empty((B, d)) if need_grad_state else None
+    if B == 0 or T == 0:                        # no step: the state stays, nothing decays
+        if ga is not None:
+            ga.zero_()
+        if gs is not None:
+            gs.zero_() if grad_state is None else gs.copy_(grad_state)
+        return gx, gg, ga, gs
+    ws = _workspace(lib().memoroid_scan_gated_bwd_workspace_bytes(B, T, d, dt), dev, workspace)
+    _launch("memoroid_scan_gated_bwd", dev, x.data_ptr(), gates.data_ptr(), alpha.data_ptr(), start.data_ptr(),
+            states.data_ptr(), grad_h.data_ptr(), _ptr(grad_state), gx.data_ptr(), gg.data_ptr(), _ptr(ga), _ptr(gs),
+            B, T, d, dt, ws.data_ptr(), ws.numel())
+    return gx, gg, ga, gs
+
+
+def gated_step(x, gates, alpha, state, start=None):
+    """One step of the gated recurrence for B rows, `state` (float32 [B,d]) updated in
+    place.  x: [B,d]; gates: [B,2,d]; start: optional uint8 [B], the rows that begin an
+    episode with this step.  Returns h [B,d], the state in x's dtype.
+
+    The step has no gradient and refuses inputs that want one (outside
+    torch.no_grad()): gated_scan() of tapes of one step with a carried state has."""
+    torch = _torch()
+    B, _, d, dt = _gated_args(x, gates, alpha, start, False)
+    if state is None:
+        raise TypeError("state must be float32 [B,d]")
+    _gated_state(state, "state", B, d)
+    if (x.requires_grad or gates.requires_grad or alpha.requires_grad or state.requires_grad) and \
+            torch.is_grad_enabled():
+        raise RuntimeError("gated_step has no gradient: call it under torch.no_grad(), or gated_scan() on tapes of one "
+                           "step")
+    dev = _check_cuda(x, gates, alpha, start, state)
+    h = torch.empty_like(x)
+    _launch("memoroid_gated_step", dev, x.data_ptr(), gates.data_ptr(), alpha.data_ptr(), _ptr(start), state.data_ptr(),
+            h.data_ptr(), B, d, dt)
+    torch.autograd.graph.increment_version(state)      # a graph that has saved it refuses its backward pass
+    return h
+
+
+def _rows_args(x, residual, p, rng, site, *grads):
+    """Rows of a norm's or dropout's input and its checks."""
+    if x.dim() < 1:
+        raise ValueError("x must be [...,d]")
+    dt = _code_of(x.dtype)
+    if dt == C64:
+        raise TypeError("x must be float32 or bfloat16")
+    for t in (residual,) + grads:
+        if t is not None and (t.dtype != x.dtype or t.shape != x.shape):
+            raise TypeError("the residual and upstream gradients must be like x")
+    if not 0.0 <= p <= 1.0:
+        raise ValueError("p must be in [0, 1]")
+    if p > 0 and rng is None:
+        raise ValueError("dropout needs rng, int64 [2] on x's device: seed and step")
+    if rng is not None and (rng.dtype != _T.int64 or rng.shape != (2,)):
+        raise TypeError("rng must be int64 [2]")
+    if not 0 <= site < 1 << 32:
+        raise ValueError("site must be in [0, 2^32)")
+    d = x.shape[-1]
+    return (x.numel() // d if d else 0), d, dt
+
+
+def _weights_ok(d, *ws):
+    for w in ws:
+        if w is not None and (w.dtype != _T.float32 or w.shape != (d,)):
+            raise TypeError("weight and bias must be float32 [d]")
+
+
+def drop_rows(x, p: float, rng, site: int = 0, residual=None):
+    """residual + dropout(x): an element of x stays, times 1 / (1 - p), where its 32-bit
+    random number is not below p 2^32.  x, residual: [...,d], float32 or bfloat16; rng:
+    int64 [2] on the device, (seed, step): the numbers are a function of seed, step (its
+    low 32 bits), site and the element's row and column (Philox4x32-10; see
+    include/memoroid.h), so that a program draws anew by raising the step -- in a
+    captured graph too -- and gives each of a model's dropouts a site of its own.  The
+    gradient of x is the same call on the upstream gradient, without the residual."""
+    torch = _torch()
+    n, d, dt = _rows_args(x, residual, p, rng, site)
+    dev = _check_cuda(x, residual, rng)
+    out = torch.empty_like(x)
+    _launch("memoroid_dropout", dev, x.data_ptr(), _ptr(residual), _ptr(rng), out.data_ptr(), p, site, n, d, dt)
+    return out
+
+
+def norm_rows(x, weight=None, bias=None, eps: float = 1e-5, residual=None, p: float = 0.0, rng=None, site: int = 0,
+              keep_stats: bool = False):
+    """Layer norm of the rows of s = residual + dropout(x) (drop_rows; p = 0: none):
+    y = (s - mean) / sqrt(var + eps) weight + bias.  x, residual: [...,d], float32 or
+    bfloat16, d up to 16384; weight, bias: float32 [d] or None.  Returns y, followed by s
+    when there is a residual or dropout and by the rows' (mean, 1 / deviation), float32
+    [...,2], when keep_stats is true."""
+    torch = _torch()
+    n, d, dt = _rows_args(x, residual, p, rng, site)
+    _weights_ok(d, weight, bias)
+    dev = _check_cuda(x, residual, weight, bias, rng)
+    y = torch.empty_like(x)
+    s = torch.empty_like(x) if residual is not None or p > 0 else None
+    stats = torch.empty(x.shape[:-1] + (2,), dtype=torch.float32, device=dev) if keep_stats else None
+    _launch("memoroid_layer_norm", dev, x.data_ptr(), _ptr(residual), _ptr(weight), _ptr(bias), _ptr(rng), y.data_ptr(),
+            _ptr(s), _ptr(stats), eps, p, site, n, d, dt)
+    got = (y,) + ((s,) if s is not None else ()) + ((stats,) if keep_stats else ())
+    return got if len(got) > 1 else y
+
+
+def norm_rows_bwd(x, stats, grad_y, weight=None, residual=None, grad_s=None, p: float = 0.0, rng=None, site: int = 0,
+                  need_grad_weights: bool = True, workspace=None):
+    """Gradient of norm_rows: (dx, dresidual, dweight, dbias), from the stats that it
+    kept.  grad_s is the gradient of s (None: zero).  dresidual is None without a
+    residual, and dx itself with p = 0; dweight and dbias are None if not needed."""
+    torch = _torch()
+    n, d, dt = _rows_args(x, residual, p, rng, site, grad_y, grad_s)
+    _weights_ok(d, weight)
+    if stats.dtype != torch.float32 or stats.shape != x.shape[:-1] + (2,):
+        raise TypeError("stats must be float32 [...,2]")
+    dev = _check_cuda(x, residual, weight, rng, stats, grad_y, grad_s)
+    gx = torch.empty_like(x)
+    gr = None if residual is None else torch.empty_like(x) if p > 0 else gx
+    gw, gb = (torch.empty(d, dtype=torch.float32, device=dev) if need_grad_weights else None for _ in range(2))
+    if n == 0 and need_grad_weights:            # no rows: sums of nothing
+        gw.zero_()
+        gb.zero_()
+    ws = _workspace(lib().memoroid_layer_norm_bwd_workspace_bytes(n, d), dev, workspace) if need_grad_weights else None
+    _launch("memoroid_layer_norm_bwd", dev, x.data_ptr(), _ptr(residual), _ptr(weight), _ptr(rng), stats.data_ptr(),
+            grad_y.data_ptr(), _ptr(grad_s), gx.data_ptr(), gr.data_ptr() if gr is not None and p > 0 else None,
+            _ptr(gw), _ptr(gb), p, site, n, d, dt, _ptr(ws), 0 if ws is None else ws.numel())
+    return gx, gr, gw, gb
+
+
 def workspace_status(workspace) -> int:
     """Synchronise and report OK, ETIMEOUT (a cross-tile wait gave up) or
     EMISMATCH (a prepared workspace was bound to another call) for the calls
@@ -1168,3 +1428,120 @@ def qk_rotate(q, k, positions, freq, wq=None, wk=None, eps: float = 1e-6, interl
     if _RotateQK is None:
         _RotateQK = _make_rotate_autograd()
     return _RotateQK.apply(q, k, positions, freq, wq, wk, eps, interleaved, amplitude)
+
+
+def _make_gated_autograd():
+    torch = _torch()
+
+    class GatedScan(torch.autograd.Function):
+        """Differentiable gated recurrence over tapes with resets and a carried state."""
+
+        @staticmethod
+        def forward(ctx, x, gates, alpha, start, state, final_state):
+            *got, states = scan_gated(x, gates, alpha, start, state, final_state, keep_states=True)
+            ctx.save_for_backward(x, gates, alpha, start, states)
+            ctx.set_materialize_grads(False)
+            return tuple(got) if final_state else got[0]
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, grad_h, grad_state=None):
+            x, gates, alpha, start, states = ctx.saved_tensors
+            grad_h = torch.zeros_like(x) if grad_h is None else grad_h.contiguous()
+            gx, gg, ga, gs = scan_gated_bwd(x, gates, alpha, start, states, grad_h,
+                                            None if grad_state is None else grad_state.contiguous(),
+                                            need_grad_alpha=ctx.needs_input_grad[2],
+                                            need_grad_state=ctx.needs_input_grad[4])
+            return gx, gg, ga, None, gs, None
+
+    return GatedScan
+
+
+_GatedScan = None
+
+
+def gated_scan(x, gates, alpha, start, state=None, final_state: bool = False):
+    """Autograd-aware scan_gated: gradients of x, gates, alpha and state."""
+    global _GatedScan
+    if _GatedScan is None:
+        _GatedScan = _make_gated_autograd()
+    return _GatedScan.apply(x, gates, alpha, start, state, final_state)
+
+
+def _make_norm_autograd():
+    torch = _torch()
+
+    class LayerNorm(torch.autograd.Function):
+        """Differentiable layer norm with dropout and a residual in its pass."""
+
+        @staticmethod
+        def forward(ctx, x, weight, bias, eps, residual, p, rng, site):
+            *got, stats = norm_rows(x, weight, bias, eps, residual, p, rng, site, keep_stats=True)
+            ctx.save_for_backward(x, weight, residual, rng if p > 0 else None, stats)
+            ctx.more = (p, site)
+            ctx.set_materialize_grads(False)
+            return tuple(got) if len(got) > 1 else got[0]
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, grad_y, grad_s=None):
+            x, weight, residual, rng, stats = ctx.saved_tensors
+            p, site = ctx.more
+            need = ctx.needs_input_grad
+            grad_y = torch.zeros_like(x) if grad_y is None else grad_y.contiguous()
+            gx, gr, gw, gb = norm_rows_bwd(x, stats, grad_y, weight, residual,
+                                           None if grad_s is None else grad_s.contiguous(), p, rng, site,
+                                           need_grad_weights=need[1] or need[2])
+            return gx, gw if need[1] else None, gb if need[2] else None, None, gr, None, None, None
+
+    return LayerNorm
+
+
+_LayerNorm = None
+
+
+def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, p: float = 0.0, rng=None, site: int = 0):
+    """Autograd-aware norm_rows: y, or (y, s) with a residual or dropout; gradients of
+    x, weight, bias and the residual."""
+    global _LayerNorm
+    if _LayerNorm is None:
+        _LayerNorm = _make_norm_autograd()
+    return _LayerNorm.apply(x, weight, bias, eps, residual, p, rng, site)
+
+
+def _make_dropout_autograd():
+    torch = _torch()
+
+    class Dropout(torch.autograd.Function):
+        """Differentiable dropout into a residual."""
+
+        @staticmethod
+        def forward(ctx, x, p, rng, site, residual):
+            ctx.save_for_backward(rng if p > 0 else None)
+            ctx.more = (p, site, residual is not None)
+            return drop_rows(x, p, rng, site, residual)
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, grad):
+            rng, = ctx.saved_tensors
+            p, site, added = ctx.more
+            gx = None
+            if ctx.needs_input_grad[0]:
+                gx = drop_rows(grad.contiguous(), p, rng, site) if p > 0 else grad
+            return gx, None, None, None, grad if added else None
+
+    return Dropout
+
+
+_Dropout = None
+
+
+def dropout(x, p: float, rng, site: int = 0, residual=None):
+    """Autograd-aware drop_rows: gradients of x and the residual.  The backward pass
+    forms the mask again from rng, which must not have changed since (it raises if it
+    has): a program raises the step after the backward pass."""
+    global _Dropout
+    if _Dropout is None:
+        _Dropout = _make_dropout_autograd()
+    return _Dropout.apply(x, p, rng, site, residual)

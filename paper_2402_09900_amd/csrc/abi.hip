@@ -70,7 +70,8 @@ uint64_t layout_sig(std::initializer_list<int64_t> vals) {
 
 // entry points in a signature
 enum SigKind : int64_t { kSigDiag = 1, kSigDiagBwd, kSigFfm, kSigFfmBwd, kSigDiscount, kSigTbbBegins,
-                         kSigLinattn, kSigLinattnBwd, kSigTbbSample, kSigRetention, kSigRetentionBwd, kSigRotateBwd };
+                         kSigLinattn, kSigLinattnBwd, kSigTbbSample, kSigRetention, kSigRetentionBwd, kSigRotateBwd,
+                         kSigGated, kSigGatedBwd, kSigNormBwd };
 
 // Tiling and workspace layout of a diagonal scan.  `vec` selects the
 // vectorised lane width; `state_complex` picks the descriptor size.
@@ -1016,18 +1017,19 @@ int ret_check(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t dk, int64_t d
     if (!ret_dims_ok(dk, dv) || !ret_extents_ok(B, T, H)) return MEMOROID_EUNSUPPORTED;
     return MEMOROID_OK;
 }
-// every pointer of `must` is there, every one of both is 16-byte aligned and no
+// every pointer of `must` is there, every one of both is aligned (to 16 bytes) and no
 // output is an input or another output
 bool ret_pointers_ok(std::initializer_list<const void*> ins, std::initializer_list<const void*> opt_ins,
-                     std::initializer_list<const void*> outs, std::initializer_list<const void*> opt_outs) {
+                     std::initializer_list<const void*> outs, std::initializer_list<const void*> opt_outs,
+                     size_t align = 16) {
     for (const void* x : ins)
-        if (!x || !aligned(x, 16)) return false;
+        if (!x || !aligned(x, align)) return false;
     for (const void* x : outs)
-        if (!x || !aligned(x, 16)) return false;
+        if (!x || !aligned(x, align)) return false;
     for (const void* x : opt_ins)
-        if (x && !aligned(x, 16)) return false;
+        if (x && !aligned(x, align)) return false;
     for (const void* x : opt_outs)
-        if (x && !aligned(x, 16)) return false;
+        if (x && !aligned(x, align)) return false;
     const void* o[8];
     int n = 0;
     for (const auto& list : {outs, opt_outs})
@@ -1486,6 +1488,276 @@ int memoroid_rotate_qk_bwd(const void* q, const void* k, const int32_t* position
 
 // ------------------------------------------------------------------ status
 
+// ------------------------------------------------------- gated recurrence
+
+namespace {
+
+static_assert(kGateStateSteps == MEMOROID_GATED_STATE_STEPS, "the header's and the kernels' steps");
+
+bool floats_ok(std::initializer_list<const void*> ps) {
+    for (const void* x : ps)
+        if (x && !aligned(x, 4)) return false;
+    return true;
+}
+
+struct GatedPlan {
+    size_t off_part = 0, total = 0;
+    int64_t part_rows = 0;
+};
+void plan_gated(int64_t B, int64_t T, int64_t d, bool grad, GatedPlan* p) {
+    (void)T;
+    p->total = kAlign;
+    if (!grad) return;
+    p->off_part = kAlign;
+    p->part_rows = B;
+    p->total = align_up(p->off_part + (size_t)p->part_rows * (size_t)d * 4);
+}
+
+// Argument checks that the gated entry points share; MEMOROID_OK and *empty when there
+// is nothing to do.
+int gated_check(int64_t B, int64_t T, int64_t d, int dtype, bool* empty) {
+    *empty = false;
+    if (B < 0 || T < 0 || d < 0) return MEMOROID_EINVAL;
+    if (dtype != MEMOROID_F32 && dtype != MEMOROID_BF16) return MEMOROID_EUNSUPPORTED;
+    if (B == 0 || T == 0 || d == 0) {
+        *empty = true;
+        return MEMOROID_OK;
+    }
+    int64_t tiles;
+    if (d > ((int64_t)1 << 18) || T >= ((int64_t)1 << 30) || !mul_ok(B, (T + 63) / 64 * ((d + 63) / 64), &tiles) ||
+        tiles >= ((int64_t)1 << 23))
+        return MEMOROID_EUNSUPPORTED;
+    return MEMOROID_OK;
+}
+
+}  // namespace
+
+size_t memoroid_scan_gated_workspace_bytes(int64_t B, int64_t T, int64_t d, int dtype) {
+    bool empty;
+    if (gated_check(B, T, d, dtype, &empty) != MEMOROID_OK || empty) return 0;
+    GatedPlan p;
+    plan_gated(B, T, d, false, &p);
+    return p.total;
+}
+
+int memoroid_scan_gated(const void* x, const void* gates, const float* alpha, const uint8_t* start,
+                        const float* state_in, void* h, float* state_out, float* states, int64_t B, int64_t T,
+                        int64_t d, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    bool empty;
+    const int ok = gated_check(B, T, d, dtype, &empty);
+    if (ok != MEMOROID_OK || empty) return ok;
+    if (!ret_pointers_ok({x, gates}, {}, {h}, {}, (size_t)elem_bytes(dtype)) ||
+        !ret_pointers_ok({alpha, start}, {state_in, x, gates}, {h}, {state_out, states}, 1) ||
+        !floats_ok({alpha, state_in, state_out, states}))
+        return MEMOROID_EINVAL;
+    GatedPlan p;
+    plan_gated(B, T, d, false, &p);
+    if (!workspace || workspace_bytes < p.total) return MEMOROID_EWORKSPACE;
+    if (!aligned(workspace, 16)) return MEMOROID_EINVAL;
+    GatedFwdArgs a{};
+    a.x = x;
+    a.gates = gates;
+    a.alpha = alpha;
+    a.start = start;
+    a.state_in = state_in;
+    a.h = h;
+    a.state_out = state_out;
+    a.states = states;
+    a.B = B;
+    a.T = T;
+    a.d = d;
+    hipStream_t s = (hipStream_t)stream;
+    const int st = check_hip(ws_init_launch(nullptr, 0, workspace, kAlign, s));
+    if (st != MEMOROID_OK) return st;
+    return check_hip(gated_fwd_launch(dtype == MEMOROID_BF16, a, s));
+}
+
+size_t memoroid_scan_gated_bwd_workspace_bytes(int64_t B, int64_t T, int64_t d, int dtype) {
+    bool empty;
+    if (gated_check(B, T, d, dtype, &empty) != MEMOROID_OK || empty) return 0;
+    GatedPlan p;
+    plan_gated(B, T, d, true, &p);
+    return p.total;
+}
+
+int memoroid_scan_gated_bwd(const void* x, const void* gates, const float* alpha, const uint8_t* start,
+                            const float* states, const void* grad_h, const float* grad_state_out, void* grad_x,
+                            void* grad_gates, float* grad_alpha, float* grad_state_in, int64_t B, int64_t T, int64_t d,
+                            int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    bool empty;
+    const int ok = gated_check(B, T, d, dtype, &empty);
+    if (ok != MEMOROID_OK || empty) return ok;
+    if (!ret_pointers_ok({x, gates, grad_h}, {}, {grad_x, grad_gates}, {}, (size_t)elem_bytes(dtype)) ||
+        !ret_pointers_ok({alpha, start, states}, {grad_state_out, x, gates, grad_h}, {grad_x, grad_gates},
+                         {grad_alpha, grad_state_in}, 1) ||
+        !floats_ok({alpha, states, grad_state_out, grad_alpha, grad_state_in}))
+        return MEMOROID_EINVAL;
+    GatedPlan p;
+    plan_gated(B, T, d, true, &p);
+    if (!workspace || workspace_bytes < p.total) return MEMOROID_EWORKSPACE;
+    if (!aligned(workspace, 16)) return MEMOROID_EINVAL;
+    GatedBwdArgs a{};
+    a.x = x;
+    a.gates = gates;
+    a.alpha = alpha;
+    a.start = start;
+    a.states = states;
+    a.g = grad_h;
+    a.grad_state = grad_state_out;
+    a.dx = grad_x;
+    a.dgates = grad_gates;
+    a.grad_state_in = grad_state_in;
+    a.part = grad_alpha ? (float*)((char*)workspace + p.off_part) : nullptr;
+    a.part_rows = p.part_rows;
+    a.dalpha = grad_alpha;
+    a.B = B;
+    a.T = T;
+    a.d = d;
+    hipStream_t s = (hipStream_t)stream;
+    const int st = check_hip(ws_init_launch(nullptr, 0, workspace, kAlign, s));
+    if (st != MEMOROID_OK) return st;
+    return check_hip(gated_bwd_launch(dtype == MEMOROID_BF16, a, s));
+}
+
+int memoroid_gated_step(const void* x, const void* gates, const float* alpha, const uint8_t* start, float* state,
+                        void* h, int64_t B, int64_t d, int dtype, void* stream) {
+    bool empty;
+    int64_t n;
+    const int ok = gated_check(B > 1 ? 1 : B, 1, d, dtype, &empty);
+    if (ok != MEMOROID_OK || empty) return ok;
+    if (!mul_ok(B, d, &n) || n >= ((int64_t)1 << 31)) return MEMOROID_EUNSUPPORTED;
+    if (!ret_pointers_ok({x, gates}, {}, {h}, {}, (size_t)elem_bytes(dtype)) ||
+        !ret_pointers_ok({alpha}, {start, x, gates}, {h, state}, {}, 1) || !floats_ok({alpha, state}))
+        return MEMOROID_EINVAL;
+    GatedStepArgs a{};
+    a.x = x;
+    a.gates = gates;
+    a.alpha = alpha;
+    a.start = start;
+    a.state = state;
+    a.h = h;
+    a.B = B;
+    a.d = d;
+    return check_hip(gated_step_launch(dtype == MEMOROID_BF16, a, (hipStream_t)stream));
+}
+
+// ---------------------------------------------------- layer norm and dropout
+
+namespace {
+
+int rows_check(int64_t n, int64_t d, double p, int64_t site, const int64_t* rng, int dtype, bool* empty) {
+    *empty = false;
+    if (n < 0 || d < 0 || !(p >= 0.0 && p <= 1.0) || site < 0 || site > (int64_t)UINT32_MAX) return MEMOROID_EINVAL;
+    if (dtype != MEMOROID_F32 && dtype != MEMOROID_BF16) return MEMOROID_EUNSUPPORTED;
+    if (n == 0 || d == 0) {
+        *empty = true;
+        return MEMOROID_OK;
+    }
+    if (p > 0.0 && (!rng || !aligned(rng, 8))) return MEMOROID_EINVAL;
+    return n > INT32_MAX || d > INT32_MAX ? MEMOROID_EUNSUPPORTED : MEMOROID_OK;
+}
+DropArgs drop_args(double p, int64_t site, const int64_t* rng) {
+    DropArgs a{};
+    a.rng = rng;
+    a.limit = (uint64_t)llround(p * 4294967296.0);
+    // (p = 1 drops every element before its scale is of any account)
+    a.scale = p < 1.0 ? (float)(1.0 / (1.0 - p)) : 0.0f;
+    a.site = (uint32_t)site;
+    return a;
+}
+
+}  // namespace
+
+int memoroid_dropout(const void* x, const void* residual, const int64_t* rng, void* out, double p, int64_t site,
+                     int64_t n, int64_t d, int dtype, void* stream) {
+    bool empty;
+    const int ok = rows_check(n, d, p, site, rng, dtype, &empty);
+    if (ok != MEMOROID_OK || empty) return ok;
+    int64_t octets;
+    if (!mul_ok(n, (d + 7) / 8, &octets) || octets > INT32_MAX) return MEMOROID_EUNSUPPORTED;
+    if (!ret_pointers_ok({x}, {residual}, {out}, {}, (size_t)elem_bytes(dtype)) || out == (const void*)rng)
+        return MEMOROID_EINVAL;
+    DropoutArgs a{};
+    a.x = x;
+    a.residual = residual;
+    a.out = out;
+    a.drop = drop_args(p, site, rng);
+    a.n = n;
+    a.d = d;
+    return check_hip(dropout_launch(dtype == MEMOROID_BF16, a, (hipStream_t)stream));
+}
+
+int memoroid_layer_norm(const void* x, const void* residual, const float* weight, const float* bias,
+                        const int64_t* rng, void* y, void* s_out, float* stats, float eps, double p, int64_t site,
+                        int64_t n, int64_t d, int dtype, void* stream) {
+    bool empty;
+    if (!(eps >= 0.0f) || !std::isfinite(eps)) return MEMOROID_EINVAL;
+    const int ok = rows_check(n, d, p, site, rng, dtype, &empty);
+    if (ok != MEMOROID_OK || empty) return ok;
+    if (d > kNormMaxDim) return MEMOROID_EUNSUPPORTED;
+    if (!ret_pointers_ok({x}, {residual}, {y}, {s_out}, (size_t)elem_bytes(dtype)) ||
+        !ret_pointers_ok({x}, {residual, weight, bias, rng}, {y}, {s_out, stats}, 1) || !floats_ok({weight, bias, stats}))
+        return MEMOROID_EINVAL;
+    NormArgs a{};
+    a.x = x;
+    a.residual = residual;
+    a.w = weight;
+    a.b = bias;
+    a.y = y;
+    a.s = s_out;
+    a.stats = stats;
+    a.drop = drop_args(p, site, rng);
+    a.eps = eps;
+    a.n = n;
+    a.d = d;
+    return check_hip(norm_launch(dtype == MEMOROID_BF16, a, (hipStream_t)stream));
+}
+
+size_t memoroid_layer_norm_bwd_workspace_bytes(int64_t n, int64_t d) {
+    if (n <= 0 || d <= 0 || n > INT32_MAX || d > kNormMaxDim) return 0;
+    int64_t rows;
+    return align_up(kAlign + (size_t)norm_groups(n, d, &rows) * 2 * (size_t)d * 4);
+}
+
+int memoroid_layer_norm_bwd(const void* x, const void* residual, const float* weight, const int64_t* rng,
+                            const float* stats, const void* grad_y, const void* grad_s, void* grad_x,
+                            void* grad_residual, float* grad_weight, float* grad_bias, double p, int64_t site,
+                            int64_t n, int64_t d, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    bool empty;
+    const int ok = rows_check(n, d, p, site, rng, dtype, &empty);
+    if (ok != MEMOROID_OK || empty) return ok;
+    if (d > kNormMaxDim) return MEMOROID_EUNSUPPORTED;
+    if (!ret_pointers_ok({x, grad_y}, {residual, grad_s}, {grad_x}, {grad_residual}, (size_t)elem_bytes(dtype)) ||
+        !ret_pointers_ok({x, grad_y, stats}, {residual, grad_s, weight, rng}, {grad_x},
+                         {grad_residual, grad_weight, grad_bias}, 1) ||
+        !floats_ok({weight, stats, grad_weight, grad_bias}))
+        return MEMOROID_EINVAL;
+    NormBwdArgs a{};
+    a.groups = norm_groups(n, d, &a.rows);
+    hipStream_t s = (hipStream_t)stream;
+    if (grad_weight || grad_bias) {
+        if (!workspace || workspace_bytes < memoroid_layer_norm_bwd_workspace_bytes(n, d)) return MEMOROID_EWORKSPACE;
+        if (!aligned(workspace, 16)) return MEMOROID_EINVAL;
+        a.part = (float*)((char*)workspace + kAlign);
+        const int st = check_hip(ws_init_launch(nullptr, 0, workspace, kAlign, s));
+        if (st != MEMOROID_OK) return st;
+    }
+    a.x = x;
+    a.residual = residual;
+    a.w = weight;
+    a.stats = stats;
+    a.gy = grad_y;
+    a.gs = grad_s;
+    a.dx = grad_x;
+    a.dres = grad_residual;
+    a.dw = grad_weight;
+    a.db = grad_bias;
+    a.drop = drop_args(p, site, rng);
+    a.n = n;
+    a.d = d;
+    return check_hip(norm_bwd_launch(dtype == MEMOROID_BF16, a, s));
+}
+
 // ------------------------------------------- discounted return and GAE
 
 namespace {
@@ -1884,6 +2156,14 @@ size_t memoroid_workspace_bytes(memoroid_op op_in, int64_t B, int64_t T, int64_t
                 for (int64_t rot : {(int64_t)0, (int64_t)2})
                     take(memoroid_rotate_qk_bwd_workspace_bytes(T, d_or_H, dk, dv, rot, 0, dt));
             return best;
+        case MEMOROID_OP_GATED:
+            for (int dt : {MEMOROID_F32, MEMOROID_BF16}) take(memoroid_scan_gated_workspace_bytes(B, T, d_or_H, dt));
+            return best;
+        case MEMOROID_OP_GATED_BWD:
+            for (int dt : {MEMOROID_F32, MEMOROID_BF16}) take(memoroid_scan_gated_bwd_workspace_bytes(B, T, d_or_H, dt));
+            return best;
+        case MEMOROID_OP_LAYER_NORM_BWD:
+            return memoroid_layer_norm_bwd_workspace_bytes(T, d_or_H);
     }
     return 0;
 }

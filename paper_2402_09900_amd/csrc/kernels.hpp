@@ -436,6 +436,98 @@ struct RotateArgs {
 hipError_t rotate_launch(bool bf16, bool grad, int ch, const RotateArgs& a, hipStream_t s);
 hipError_t rotate_weights_launch(const RotateArgs& a, float* dwq, float* dwk, hipStream_t s);
 
+// -------------------------------------------------------- gated recurrence
+// (gated.hip).  The state before every kGateStateSteps-th step is kept for the gradient.
+constexpr int kGateStateSteps = 128;
+
+struct GatedFwdArgs {
+    const void* x;              // [B][T][d]
+    const void* gates;          // [B][T][2][d]
+    const float* alpha;         // [d]
+    const uint8_t* start;       // [B][T]
+    const float* state_in;      // [B][d], or NULL
+    void* h;                    // [B][T][d]
+    float* state_out;           // [B][d], or NULL
+    float* states;              // [B][ceil(T / kGateStateSteps)][d], or NULL
+    int64_t B, T, d;
+};
+struct GatedBwdArgs {
+    const void* x;
+    const void* gates;
+    const float* alpha;
+    const uint8_t* start;
+    const float* states;
+    const void* g;              // [B][T][d]
+    const float* grad_state;    // [B][d], or NULL
+    void* dx;
+    void* dgates;
+    float* grad_state_in;       // [B][d], or NULL
+    float* part;                // [part_rows][d] sums for dalpha, or NULL
+    float* dalpha;              // [d]
+    int64_t B, T, d, part_rows;
+};
+struct GatedStepArgs {
+    const void* x;              // [B][d]
+    const void* gates;          // [B][2][d]
+    const float* alpha;         // [d]
+    const uint8_t* start;       // [B], or NULL
+    float* state;               // [B][d], updated in place
+    void* h;                    // [B][d]
+    int64_t B, d;
+};
+hipError_t gated_fwd_launch(bool bf16, const GatedFwdArgs& a, hipStream_t s);
+hipError_t gated_bwd_launch(bool bf16, const GatedBwdArgs& a, hipStream_t s);
+hipError_t gated_step_launch(bool bf16, const GatedStepArgs& a, hipStream_t s);
+
+// ------------------------------------------------- layer norm and dropout
+// (norm.hip)
+constexpr int64_t kNormMaxDim = 16384;
+struct DropArgs {
+    const int64_t* rng;         // [2]: seed, step
+    uint64_t limit;             // elements whose number is below it go (2^32: all); 0: no dropout
+    float scale;                // 1 / (1 - p)
+    uint32_t site;
+};
+struct NormArgs {
+    const void* x;              // [n][d]
+    const void* residual;       // [n][d], or NULL
+    const float* w;             // [d], or NULL
+    const float* b;             // [d], or NULL
+    void* y;                    // [n][d]
+    void* s;                    // [n][d], or NULL
+    float* stats;               // [n][2]: mean, 1 / deviation; or NULL
+    DropArgs drop;
+    float eps;
+    int64_t n, d, rows;         // rows of a wavefront (set by the launch)
+};
+struct NormBwdArgs {
+    const void* x;
+    const void* residual;
+    const float* w;
+    const float* stats;
+    const void* gy;             // [n][d]
+    const void* gs;             // [n][d], or NULL
+    void* dx;                   // [n][d]
+    void* dres;                 // [n][d], or NULL: not asked for, or the same as dx
+    float* part;                // [groups][2][d] sums for dw and db, or NULL
+    float* dw;                  // [d], or NULL
+    float* db;                  // [d], or NULL
+    DropArgs drop;
+    int64_t n, d, rows, groups;
+};
+struct DropoutArgs {
+    const void* x;              // [n][d]
+    const void* residual;       // [n][d], or NULL
+    void* out;
+    DropArgs drop;
+    int64_t n, d;
+};
+// groups of rows with a row of sums each, and rows in a group
+int64_t norm_groups(int64_t n, int64_t d, int64_t* rows);
+hipError_t norm_launch(bool bf16, NormArgs a, hipStream_t s);
+hipError_t norm_bwd_launch(bool bf16, NormBwdArgs a, hipStream_t s);
+hipError_t dropout_launch(bool bf16, const DropoutArgs& a, hipStream_t s);
+
 // ------------------------------------------- discounted return and GAE
 // Steps per lane: 32 for the return (two streams in registers), 16 for the
 // advantage (four); a tile is 4 wavefronts of 64 lanes.

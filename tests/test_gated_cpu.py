@@ -1,0 +1,228 @@
+"""Layer norm, dropout and the gated recurrence on the CPU: the 64-bit reference against
+differences and known numbers, the refusals of the C and the torch layer, workspace
+sizes."""
+import ctypes
+
+import numpy as np
+import pytest
+
+import gated_ref as ref
+
+torch = pytest.importorskip("torch")
+from paper_2402_09900_amd import binding as mb  # noqa: E402
+
+P = [0x10000 * (i + 1) for i in range(16)]      # distinct, aligned, never followed
+BIG = 1 << 40
+
+
+def gated(**k):
+    a = dict(x=P[0], gates=P[1], alpha=P[2], start=P[3], state_in=P[4], h=P[5], state_out=P[6], states=P[7], B=2, T=100, d=30,
+             dtype=mb.F32, ws=P[8], wb=BIG, st=None)
+    a.update(k)
+    return mb.memoroid_scan_gated(*a.values())
+
+
+def gated_bwd(**k):
+    a = dict(x=P[0], gates=P[1], alpha=P[2], start=P[3], states=P[4], g=P[5], gs=P[6], gx=P[7], gg=P[8], ga=P[9], gsi=P[10],
+             B=2, T=100, d=30, dtype=mb.F32, ws=P[11], wb=BIG, st=None)
+    a.update(k)
+    return mb.memoroid_scan_gated_bwd(*a.values())
+
+
+def step(**k):
+    a = dict(x=P[0], gates=P[1], alpha=P[2], start=P[3], state=P[4], h=P[5], B=2, d=30, dtype=mb.F32, st=None)
+    a.update(k)
+    return mb.memoroid_gated_step(*a.values())
+
+
+def norm(**k):
+    a = dict(x=P[0], residual=P[1], w=P[2], b=P[3], rng=P[4], y=P[5], s=P[6], stats=P[7], eps=1e-5, p=0.1, site=0, n=10, d=30,
+             dtype=mb.F32, st=None)
+    a.update(k)
+    return mb.memoroid_layer_norm(*a.values())
+
+
+def norm_bwd(**k):
+    a = dict(x=P[0], residual=P[1], w=P[2], rng=P[3], stats=P[4], gy=P[5], gs=P[6], gx=P[7], gr=P[8], gw=P[9], gb=P[10], p=0.1,
+             site=0, n=10, d=30, dtype=mb.F32, ws=P[11], wb=BIG, st=None)
+    a.update(k)
+    return mb.memoroid_layer_norm_bwd(*a.values())
+
+
+def drop(**k):
+    a = dict(x=P[0], residual=P[1], rng=P[2], out=P[3], p=0.1, site=0, n=10, d=30, dtype=mb.F32, st=None)
+    a.update(k)
+    return mb.memoroid_dropout(*a.values())
+
+
+@pytest.mark.parametrize("call,outs,ins,optional", [
+    (gated, ["h", "state_out", "states"], ["x", "gates", "alpha", "start", "state_in"], ["state_in", "state_out", "states"]),
+    (gated_bwd, ["gx", "gg", "ga", "gsi"], ["x", "gates", "alpha", "start", "states", "g", "gs"], ["gs", "ga", "gsi"]),
+    (step, ["h", "state"], ["x", "gates", "alpha", "start"], ["start"]),
+    (norm, ["y", "s", "stats"], ["x", "residual", "w", "b", "rng"], ["residual", "w", "b", "s", "stats"]),
+    (norm_bwd, ["gx", "gr", "gw", "gb"], ["x", "residual", "w", "rng", "stats", "gy", "gs"],
+     ["residual", "w", "gs", "gr", "gw", "gb"]),
+    (drop, ["out"], ["x", "residual", "rng"], ["residual"])])
+def test_pointers(call, outs, ins, optional):
+    for name in outs + ins:
+        if name not in optional:
+            assert call(**{name: None}) == mb.EINVAL, name
+        if name != "start":
+            assert call(**{name: P[14] + 1}) == mb.EINVAL, name
+    for o in outs:
+        for other in outs + ins:
+            if other != o:
+                assert call(**{o: P[14], other: P[14]}) == mb.EINVAL, (o, other)
+
+
+@pytest.mark.parametrize("call", [gated, gated_bwd])
+def test_gated_refusals(call):
+    for name in ("B", "T", "d"):
+        assert call(**{name: -1}) == mb.EINVAL
+        assert call(**{name: 0, "ws": None}) == mb.OK            # nothing to do
+    assert call(dtype=mb.C64) == call(dtype=7) == mb.EUNSUPPORTED
+    assert call(d=(1 << 18) + 1) == mb.EUNSUPPORTED
+    assert call(T=1 << 30) == mb.EUNSUPPORTED
+    assert call(B=1 << 23, T=1, d=1) == mb.EUNSUPPORTED
+    assert call(B=(1 << 62), T=1 << 20, d=1 << 10) == mb.EUNSUPPORTED
+    assert call(ws=None) == call(wb=16) == mb.EWORKSPACE
+    assert call(ws=P[12] + 8) == mb.EINVAL
+
+
+def test_step_refusals():
+    assert step(B=-1) == step(d=-1) == mb.EINVAL
+    assert step(B=0) == step(d=0) == mb.OK
+    assert step(dtype=mb.C64) == step(d=(1 << 18) + 1) == step(B=1 << 31, d=1) == step(B=1 << 62, d=8) == mb.EUNSUPPORTED
+
+
+def test_norm_refusals():
+    for call in (norm, norm_bwd, drop):
+        assert call(n=-1) == call(d=-1) == call(p=-0.1) == call(p=1.1) == call(p=float("nan")) == mb.EINVAL
+        assert call(site=-1) == call(site=1 << 32) == mb.EINVAL
+        assert call(n=0) == call(d=0) == mb.OK
+        assert call(dtype=mb.C64) == call(n=1 << 31) == call(d=1 << 31) == mb.EUNSUPPORTED
+        assert call(rng=P[12] + 4) == mb.EINVAL
+    for eps in (-1.0, float("nan"), float("inf")):
+        assert norm(eps=eps) == mb.EINVAL
+    for call in (norm, norm_bwd):
+        assert call(d=16385) == mb.EUNSUPPORTED
+    assert norm_bwd(ws=None) == norm_bwd(wb=64) == mb.EWORKSPACE
+    assert norm_bwd(ws=P[12] + 8) == mb.EINVAL
+    assert drop(n=1 << 30, d=17) == mb.EUNSUPPORTED
+
+
+def test_workspace_sizes():
+    q = mb.memoroid_workspace_bytes
+    for dt in (mb.F32, mb.BF16):
+        for B, T, d in ((1, 1, 1), (3, 1000, 250), (8, 4096, 2048), (1, 65536, 33)):
+            assert 0 < mb.memoroid_scan_gated_workspace_bytes(B, T, d, dt) <= q(mb.OP_GATED, B, T, d, 0, 0, 0)
+            assert 0 < mb.memoroid_scan_gated_bwd_workspace_bytes(B, T, d, dt) <= q(mb.OP_GATED_BWD, B, T, d, 0, 0, 0)
+    assert mb.memoroid_layer_norm_bwd_workspace_bytes(1000, 256) == q(mb.OP_LAYER_NORM_BWD, 0, 1000, 256, 0, 0, 0) > 0
+    for f in (lambda: mb.memoroid_scan_gated_workspace_bytes(0, 5, 5, 0), lambda: mb.memoroid_scan_gated_workspace_bytes(1, 5, 5, 2),
+              lambda: mb.memoroid_scan_gated_bwd_workspace_bytes(-1, 5, 5, 0), lambda: q(mb.OP_GATED, 1, 1 << 30, 5, 0, 0, 0),
+              lambda: mb.memoroid_layer_norm_bwd_workspace_bytes(0, 5), lambda: mb.memoroid_layer_norm_bwd_workspace_bytes(5, 16385)):
+        assert f() == 0
+
+
+def test_torch_layer_refusals():
+    x, gates, alpha = torch.zeros(2, 5, 8), torch.zeros(2, 5, 2, 8), torch.zeros(8)
+    start, state = torch.zeros(2, 5, dtype=torch.uint8), torch.zeros(2, 8)
+    ok = dict(x=x, gates=gates, alpha=alpha, start=start)
+
+    def refuse(error, f, **k):
+        with pytest.raises(error):
+            f(**{**ok, **k})
+
+    refuse(ValueError, mb.scan_gated)                                # on the CPU
+    refuse(ValueError, mb.scan_gated, x=x[0])
+    refuse(ValueError, mb.scan_gated, gates=gates[:, :, 0])
+    refuse(ValueError, mb.scan_gated, gates=torch.zeros(2, 5, 3, 8))
+    refuse(TypeError, mb.scan_gated, gates=gates.bfloat16())
+    refuse(TypeError, mb.scan_gated, x=x.half(), gates=gates.half())
+    refuse(TypeError, mb.scan_gated, x=x.to(torch.complex64), gates=gates.to(torch.complex64))
+    refuse(TypeError, mb.scan_gated, alpha=alpha.double())
+    refuse(TypeError, mb.scan_gated, alpha=alpha[:4])
+    refuse(TypeError, mb.scan_gated, start=None)
+    refuse(TypeError, mb.scan_gated, start=start.bool())
+    refuse(TypeError, mb.scan_gated, state=state.double())
+    refuse(TypeError, mb.scan_gated, state=state[:1])
+    kept = torch.zeros(2, 1, 8)
+    for k in (dict(states=kept[:, :0]), dict(states=kept.double()), dict(grad_h=x[:1]), dict(grad_h=x.bfloat16()),
+              dict(grad_state=state[:1])):
+        refuse(TypeError, mb.scan_gated_bwd, **{**dict(states=kept, grad_h=x), **k})
+    with pytest.raises(TypeError):
+        mb.gated_step(x[:, 0], gates[:, 0], alpha, None)
+    with pytest.raises(TypeError):
+        mb.gated_step(x[:, 0], gates[:, 0], alpha, state, start)
+    with pytest.raises(RuntimeError):
+        mb.gated_step(x[:, 0].clone().requires_grad_(True), gates[:, 0], alpha, state)
+    rng = torch.zeros(2, dtype=torch.int64)
+    for f in (lambda **k: mb.norm_rows(x, **k), lambda **k: mb.drop_rows(x, **{**dict(p=0.5, rng=rng), **k})):
+        for k in (dict(p=0.5, rng=None), dict(p=-1.0), dict(p=2.0), dict(p=float("nan")), dict(site=-1), dict(site=1 << 32)):
+            with pytest.raises(ValueError):
+                f(**k)
+        for k in (dict(rng=rng[:1]), dict(rng=rng.int()), dict(residual=x[:1]), dict(residual=x.bfloat16())):
+            with pytest.raises(TypeError):
+                f(**k)
+    for k in (dict(weight=alpha[:3]), dict(weight=alpha.double()), dict(bias=alpha.bfloat16())):
+        with pytest.raises(TypeError):
+            mb.norm_rows(x, **k)
+    with pytest.raises(TypeError):
+        mb.norm_rows_bwd(x, torch.zeros(2, 5), x)
+    with pytest.raises(TypeError):
+        mb.norm_rows_bwd(x, torch.zeros(2, 5, 2), x[:1])
+    with pytest.raises(TypeError):
+        mb.norm_rows(x.half())
+
+
+# ---------------------------------------------------------------- reference
+
+def test_known_numbers():
+    """The published answers of Philox4x32-10 for a counter and key of zeros, of ones."""
+    assert ref.philox([0] * 4, [0] * 2) == [0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8]
+    assert ref.philox([0xFFFFFFFF] * 4, [0xFFFFFFFF] * 2) == [0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD]
+
+
+def test_reference_gradients():
+    """Against central differences in 64 bits: fourth order, steps of 1e-3."""
+    rng = np.random.default_rng(0)
+    B, T, d = 2, 9, 4
+    v = dict(x=rng.standard_normal((B, T, d)), gates=rng.standard_normal((B, T, 2, d)), alpha=rng.uniform(0.1, 1.0, d) * [1, -1, 1, -1],
+             state=rng.standard_normal((B, d)))
+    start = (rng.random((B, T)) < 0.3).astype(np.uint8)
+    start[0, 0] = 0
+    g, gs = rng.standard_normal((B, T, d)), rng.standard_normal((B, d))
+
+    def value(**k):
+        a = {**v, **k}
+        h, _, last, _ = ref.scan(a["x"], a["gates"], a["alpha"], start, a["state"])
+        return (h * g).sum() + (last * gs).sum()
+
+    got = ref.grads(v["x"], v["gates"], v["alpha"], start, g, v["state"], gs)
+    for name in v:
+        way = rng.standard_normal(v[name].shape)
+        f = [value(**{name: v[name] + s * 1e-3 * way}) for s in (-2, -1, 1, 2)]
+        want = (8 * (f[2] - f[1]) - (f[3] - f[0])) / 12e-3
+        assert abs((got[name][0] * way).sum() - want) <= 1e-8 * max(1, abs(want)), name
+
+
+def test_reference_norm_gradients():
+    rng = np.random.default_rng(1)
+    s, w, gy, gs = rng.standard_normal((3, 7)), rng.standard_normal(7), rng.standard_normal((3, 7)), rng.standard_normal((3, 7))
+    (ds, _), (dw, _), (db, _) = ref.norm_grads(s, w, 1e-5, gy, gs)
+    b = rng.standard_normal(7)
+
+    def value(s, w, b):
+        return (ref.norm(s, w, b, 1e-5)[0] * gy).sum() + (s * gs).sum()
+
+    for i, grad in ((0, ds), (1, dw), (2, db)):
+        a = [s, w, b]
+        way = rng.standard_normal(a[i].shape)
+        f = [value(*[x + t * 1e-3 * way if j == i else x for j, x in enumerate(a)]) for t in (-2, -1, 1, 2)]
+        assert abs((grad * way).sum() - (8 * (f[2] - f[1]) - (f[3] - f[0])) / 12e-3) <= 1e-7
+
+
+def test_ctypes_signature_of_p():
+    """p crosses as a double: the float nearest 0.1 would move the limit by 6."""
+    assert mb.lib().memoroid_dropout.argtypes[4] is ctypes.c_double
+    assert round(0.1 * 2.0 ** 32) != round(float(np.float32(0.1)) * 2.0 ** 32)
