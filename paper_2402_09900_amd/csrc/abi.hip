@@ -1501,16 +1501,52 @@ bool floats_ok(std::initializer_list<const void*> ps) {
 }
 
 struct GatedPlan {
-    size_t off_part = 0, total = 0;
+    int64_t nt = 1;
+    int32_t nfb = 1, nchains = 1;
+    size_t off_ctr = 0, off_agg = 0, off_incl = 0, off_part = 0, init = 0, total = 0;
     int64_t part_rows = 0;
 };
-void plan_gated(int64_t B, int64_t T, int64_t d, bool grad, GatedPlan* p) {
-    (void)T;
-    p->total = kAlign;
-    if (!grad) return;
-    p->off_part = kAlign;
-    p->part_rows = B;
-    p->total = align_up(p->off_part + (size_t)p->part_rows * (size_t)d * 4);
+// (the extents have passed gated_check)
+void plan_gated(int64_t B, int64_t T, int64_t d, int64_t tile_steps, bool grad, GatedPlan* p) {
+    p->nt = (T + tile_steps - 1) / tile_steps;
+    p->nfb = (int32_t)((d + kGateCols - 1) / kGateCols);
+    p->nchains = (int32_t)(B * p->nfb);
+    size_t off = kAlign;                                   // header
+    const size_t words = p->nt > 1 ? (size_t)p->nt * (size_t)p->nchains * kGateCols : 0;
+    p->off_ctr = off;
+    if (words) off = align_up(off + (size_t)p->nchains * kCtrStride * 4);
+    p->off_agg = off;
+    off = align_up(off + words * 8);
+    p->off_incl = off;
+    off = align_up(off + words * 4);
+    p->init = words ? off : 0;
+    p->off_part = off;
+    if (grad) {
+        p->part_rows = B;
+        off = align_up(off + (size_t)p->part_rows * (size_t)d * 4);
+    }
+    p->total = off;
+}
+GatedTiles gated_tiles(const GatedPlan& p, void* workspace, uint64_t sig) {
+    char* const ws = (char*)workspace;
+    GatedTiles t{};
+    t.nt = p.nt;
+    t.nfb = p.nfb;
+    t.nchains = p.nchains;
+    t.ctr = (uint32_t*)(ws + p.off_ctr);
+    t.agg = (uint64_t*)(ws + p.off_agg);
+    t.incl = (uint32_t*)(ws + p.off_incl);
+    t.hdr = (WsHeader*)ws;
+    t.sig = sig;
+    return t;
+}
+int64_t gated_fwd_tile(int dtype) { return 16 * gate_fwd_steps(dtype == MEMOROID_BF16); }
+// whether rows and addresses are whole vectors of four elements
+bool gated_full(int64_t d, int dtype, std::initializer_list<const void*> ps) {
+    if (d % 4 != 0) return false;
+    for (const void* x : ps)
+        if (!aligned(x, 4 * (size_t)elem_bytes(dtype))) return false;
+    return true;
 }
 
 // Argument checks that the gated entry points share; MEMOROID_OK and *empty when there
@@ -1536,7 +1572,7 @@ size_t memoroid_scan_gated_workspace_bytes(int64_t B, int64_t T, int64_t d, int 
     bool empty;
     if (gated_check(B, T, d, dtype, &empty) != MEMOROID_OK || empty) return 0;
     GatedPlan p;
-    plan_gated(B, T, d, false, &p);
+    plan_gated(B, T, d, gated_fwd_tile(dtype), false, &p);
     return p.total;
 }
 
@@ -1551,7 +1587,7 @@ int memoroid_scan_gated(const void* x, const void* gates, const float* alpha, co
         !floats_ok({alpha, state_in, state_out, states}))
         return MEMOROID_EINVAL;
     GatedPlan p;
-    plan_gated(B, T, d, false, &p);
+    plan_gated(B, T, d, gated_fwd_tile(dtype), false, &p);
     if (!workspace || workspace_bytes < p.total) return MEMOROID_EWORKSPACE;
     if (!aligned(workspace, 16)) return MEMOROID_EINVAL;
     GatedFwdArgs a{};
@@ -1566,17 +1602,17 @@ int memoroid_scan_gated(const void* x, const void* gates, const float* alpha, co
     a.B = B;
     a.T = T;
     a.d = d;
+    a.tiles = gated_tiles(p, workspace, layout_sig({kSigGated, B, T, d, dtype}));
     hipStream_t s = (hipStream_t)stream;
-    const int st = check_hip(ws_init_launch(nullptr, 0, workspace, kAlign, s));
-    if (st != MEMOROID_OK) return st;
-    return check_hip(gated_fwd_launch(dtype == MEMOROID_BF16, a, s));
+    if (p.init && ws_init_launch(nullptr, 0, workspace, p.init, s) != hipSuccess) return MEMOROID_EHIP;
+    return check_hip(gated_fwd_launch(dtype == MEMOROID_BF16, gated_full(d, dtype, {x, gates, h}), a, s));
 }
 
 size_t memoroid_scan_gated_bwd_workspace_bytes(int64_t B, int64_t T, int64_t d, int dtype) {
     bool empty;
     if (gated_check(B, T, d, dtype, &empty) != MEMOROID_OK || empty) return 0;
     GatedPlan p;
-    plan_gated(B, T, d, true, &p);
+    plan_gated(B, T, d, T, true, &p);
     return p.total;
 }
 
@@ -1593,7 +1629,7 @@ int memoroid_scan_gated_bwd(const void* x, const void* gates, const float* alpha
         !floats_ok({alpha, states, grad_state_out, grad_alpha, grad_state_in}))
         return MEMOROID_EINVAL;
     GatedPlan p;
-    plan_gated(B, T, d, true, &p);
+    plan_gated(B, T, d, T, true, &p);
     if (!workspace || workspace_bytes < p.total) return MEMOROID_EWORKSPACE;
     if (!aligned(workspace, 16)) return MEMOROID_EINVAL;
     GatedBwdArgs a{};

@@ -23,26 +23,6 @@ __device__ __forceinline__ void put(void* p, int64_t i, float v) {
     else ((float*)p)[i] = v;
 }
 
-// One thread per feature of a tape, step after step.
-template <bool BF16>
-__global__ __launch_bounds__(64) void gated_fwd_kernel(GatedFwdArgs p) {
-    const int64_t nfb = (p.d + 63) / 64, b = blockIdx.x / nfb, f = (blockIdx.x - b * nfb) * 64 + threadIdx.x;
-    if (f >= p.d) return;
-    const float rate = __builtin_fabsf(p.alpha[f]);
-    const int64_t ns = (p.T + kGateStateSteps - 1) / kGateStateSteps;
-    float h = p.state_in ? p.state_in[b * p.d + f] : 0.0f;
-    for (int64_t t = 0; t < p.T; ++t) {
-        if (p.states && t % kGateStateSteps == 0) p.states[(b * ns + t / kGateStateSteps) * p.d + f] = h;
-        const int64_t n = b * p.T + t;
-        const Gate<BF16, false> g(value<BF16>(p.gates, 2 * n * p.d + f),
-                                            value<BF16>(p.gates, (2 * n + 1) * p.d + f), rate);
-        const float v = g.m * g.si * value<BF16>(p.x, n * p.d + f);
-        h = p.start[n] ? v : g.decay.of(h, v);
-        put<BF16>(p.h, n * p.d + f, h);
-    }
-    if (p.state_out) p.state_out[b * p.d + f] = h;
-}
-
 template <bool BF16>
 __global__ __launch_bounds__(64) void gated_bwd_kernel(GatedBwdArgs p) {
     __shared__ float before[kGateStateSteps][64];
@@ -118,13 +98,6 @@ __global__ __launch_bounds__(256) void gated_step_kernel(GatedStepArgs p) {
 }
 
 }  // namespace
-
-hipError_t gated_fwd_launch(bool bf16, const GatedFwdArgs& a, hipStream_t s) {
-    const dim3 grid((unsigned)((a.d + 63) / 64 * a.B));
-    if (bf16) hipLaunchKernelGGL(gated_fwd_kernel<true>, grid, dim3(64), 0, s, a);
-    else hipLaunchKernelGGL(gated_fwd_kernel<false>, grid, dim3(64), 0, s, a);
-    return hipGetLastError();
-}
 
 hipError_t gated_bwd_launch(bool bf16, const GatedBwdArgs& a, hipStream_t s) {
     const dim3 grid((unsigned)((a.d + 63) / 64 * a.B));

@@ -50,26 +50,27 @@ __device__ __forceinline__ float loss_of(float u) {
     return p * u;
 }
 
-// A decay by exp(-u), u >= 0.  SLOW: the caller knows that no u is above kSlow.
+// A decay by exp(-u), u >= 0, in one float k: a slow one is minus what it takes away
+// (its sign bit set, for u = 0 too), a fast one what it leaves.  SLOW: the caller knows
+// that no u is above kSlow.
 template <bool SLOW>
 struct Decay {
-    float k;          // slow: minus what it takes away; else what it leaves
-    bool slow;
+    float k;
+    __device__ __forceinline__ Decay() {}
     __device__ __forceinline__ explicit Decay(float u) {
         k = -loss_of(u);
-        slow = true;
         if constexpr (!SLOW) {
             const float a = __builtin_amdgcn_exp2f(u * -kLog2e);
-            slow = u <= kSlow;
-            k = slow ? k : a;
+            k = u <= kSlow ? k : a;
         }
     }
-    __device__ __forceinline__ float left() const { return slow ? 1.0f + k : k; }          // a
-    __device__ __forceinline__ float taken() const { return slow ? -k : 1.0f - k; }        // w
+    __device__ __forceinline__ bool slow() const { return SLOW || (int)__float_as_uint(k) < 0; }
+    __device__ __forceinline__ float left() const { return slow() ? 1.0f + k : k; }          // a
+    __device__ __forceinline__ float taken() const { return slow() ? -k : 1.0f - k; }        // w
     // a v + add
     __device__ __forceinline__ float of(float v, float add) const {
         const float t = __builtin_fmaf(k, v, add);
-        return slow ? v + t : t;
+        return slow() ? v + t : t;
     }
 };
 
@@ -84,5 +85,137 @@ struct Gate {
         m = __builtin_amdgcn_sqrtf(w * (2.0f - w));
     }
 };
+
+// ------------------------------------------------------------------ tiles
+// A workgroup has kGateCols features of a tape (a chain) and 16 runs of L steps, one
+// behind the other: lane q of a run's 16 lanes the features 4 q .. 4 q + 3.
+constexpr int kGateRuns = 16;
+
+// Four features as they lie in memory.  FULL: rows and addresses are multiples of four
+// elements, and one access moves them.
+template <bool BF16>
+struct Four {
+    static constexpr int SIZE = BF16 ? 2 : 4, WORDS = BF16 ? 2 : 4;
+    uint32_t w[WORDS];
+    template <int AUX, bool FULL>
+    __device__ __forceinline__ void load(Rsrc r, uint32_t off, int left) {
+        if constexpr (FULL) {
+            WideAccess<4 * SIZE>::template bload<AUX>(w, r, off);
+        } else {
+            uint32_t v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int at = e < left ? (int)(off + e * SIZE) : (int)kOob;
+                if constexpr (BF16) v[e] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(r, at, 0, AUX);
+                else v[e] = __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, AUX);
+            }
+#pragma unroll
+            for (int e = 0; e < WORDS; ++e) w[e] = BF16 ? v[2 * e] | v[2 * e + 1] << 16 : v[e];
+        }
+    }
+    template <int AUX, bool FULL>
+    __device__ __forceinline__ void store(Rsrc r, uint32_t off, int left) const {
+        if constexpr (FULL) {
+            WideAccess<4 * SIZE>::template bstore<AUX>(r, off, w);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int at = e < left ? (int)(off + e * SIZE) : (int)kOob;
+                if constexpr (BF16)
+                    __builtin_amdgcn_raw_buffer_store_b16((unsigned short)(w[e / 2] >> (e & 1 ? 16 : 0)), r, at, 0, AUX);
+                else __builtin_amdgcn_raw_buffer_store_b32(w[e], r, at, 0, AUX);
+            }
+        }
+    }
+    __device__ __forceinline__ float get(int e) const {
+        if constexpr (BF16) return e & 1 ? bf16_hi(w[e / 2]) : bf16_lo(w[e / 2]);
+        else return __uint_as_float(w[e]);
+    }
+    __device__ __forceinline__ void set(const float (&v)[4]) {
+#pragma unroll
+        for (int e = 0; e < WORDS; ++e) w[e] = BF16 ? f32x2_to_bf16x2(v[2 * e], v[2 * e + 1]) : __float_as_uint(v[e]);
+    }
+};
+
+// The chain of a workgroup and its tile there: the n-th to start, so that all tiles
+// before it are running or done; one thread asks, `shared` hands it on.
+struct TileOf {
+    int64_t tile;
+    int chain;
+};
+__device__ __forceinline__ TileOf take_tile(const GatedTiles& t, uint32_t* shared) {
+    const uint32_t nch = (uint32_t)t.nchains;
+    TileOf r;
+    // every chain once per nchains workgroups, rotated so that none stays on one XCD
+    r.chain = (int)((blockIdx.x % nch + blockIdx.x / nch) % nch);
+    r.tile = 0;
+    if (t.nt > 1) {
+        if (threadIdx.x == 0)
+            *shared = claim_of(take_ticket(t.ctr + (size_t)r.chain * kCtrStride, (uint32_t)t.nt), (uint32_t)t.nt).pos;
+        barrier_lds();
+        r.tile = (int64_t)__builtin_amdgcn_readfirstlane(*shared);
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        if (t.nt == 1) t.hdr->timeout = kEmpty32;          // (else the fill before this kernel has written it)
+        t.hdr->sig = t.sig;
+    }
+    return r;
+}
+
+// Words that tiles hand on, per feature: AGG, a tile without a begin step, as its rates'
+// sum u and what it adds; INCL, the value after the tile.  Unpublished: all ones.
+__device__ __forceinline__ void put_agg(const GatedTiles& t, int64_t slot, int f, float u, float add) {
+    publish64(t.agg + slot * kGateCols + f, pack2(u, add));
+}
+__device__ __forceinline__ void put_incl(const GatedTiles& t, int64_t slot, int f, float v) {
+    publish32(t.incl + slot * kGateCols + f, __float_as_uint(canon(v)));
+}
+
+// The value that enters a tile, for the feature of this lane (`need` false: 0): from the
+// nearest tile before it that has published its own, the ones between applied one
+// after the other.  That is what each of them does for its own, so the result is the
+// same bit for bit whichever that tile was.
+__device__ __forceinline__ float look_back(const GatedTiles& t, int64_t tile, int chain, int f, bool need) {
+    constexpr int W = 8;
+    float v = 0.0f;
+    bool done = !need;
+    uint32_t polls = 0;
+    while (!__all(done)) {
+        if (!done) {
+            uint32_t in[W];
+            uint64_t ag[W];
+#pragma unroll
+            for (int k = 0; k < W; ++k) {
+                in[k] = kEmpty32;
+                ag[k] = kEmpty64;
+                if (k < tile) {
+                    const int64_t i = ((tile - 1 - k) * t.nchains + chain) * kGateCols + f;
+                    in[k] = peek32(t.incl + i);
+                    ag[k] = peek64(t.agg + i);
+                }
+            }
+            int at = W;
+#pragma unroll
+            for (int k = W - 1; k >= 0; --k) at = in[k] != kEmpty32 ? k : at;
+            bool ready = at < W;
+#pragma unroll
+            for (int k = 0; k < W - 1; ++k) ready = ready && (k >= at || ag[k] != kEmpty64);
+            if (ready) {
+#pragma unroll
+                for (int k = W - 1; k >= 0; --k) {
+                    const float next = Decay<false>(unpack_lo(ag[k])).of(v, unpack_hi(ag[k]));
+                    v = k == at ? __uint_as_float(in[k]) : k < at ? next : v;
+                }
+                done = true;
+            } else if (++polls > kMaxPolls) {
+                flag_timeout(&t.hdr->timeout);
+                done = true;
+            } else {
+                __builtin_amdgcn_s_sleep(1);
+            }
+        }
+    }
+    return v;
+}
 
 }  // namespace memoroid

@@ -439,6 +439,20 @@ hipError_t rotate_weights_launch(const RotateArgs& a, float* dwq, float* dwk, hi
 // -------------------------------------------------------- gated recurrence
 // (gated.hip).  The state before every kGateStateSteps-th step is kept for the gradient.
 constexpr int kGateStateSteps = 128;
+constexpr int kGateCols = 64;        // features of a chain
+// steps of a lane's run; a tile has 16 runs
+constexpr int gate_fwd_steps(bool bf16) { return bf16 ? 16 : 8; }
+
+// Tiles of the scans and the words they hand on (gated_common.hpp)
+struct GatedTiles {
+    int64_t nt;                 // tiles of a chain
+    int32_t nfb, nchains;       // chains of a tape, in all
+    uint32_t* ctr;              // [nchains], kCtrStride apart
+    uint64_t* agg;              // [nt][nchains][kGateCols]
+    uint32_t* incl;             // likewise
+    WsHeader* hdr;
+    uint64_t sig;
+};
 
 struct GatedFwdArgs {
     const void* x;              // [B][T][d]
@@ -450,6 +464,7 @@ struct GatedFwdArgs {
     float* state_out;           // [B][d], or NULL
     float* states;              // [B][ceil(T / kGateStateSteps)][d], or NULL
     int64_t B, T, d;
+    GatedTiles tiles;
 };
 struct GatedBwdArgs {
     const void* x;
@@ -475,7 +490,8 @@ struct GatedStepArgs {
     void* h;                    // [B][d]
     int64_t B, d;
 };
-hipError_t gated_fwd_launch(bool bf16, const GatedFwdArgs& a, hipStream_t s);
+// full: d and every address are multiples of four elements
+hipError_t gated_fwd_launch(bool bf16, bool full, const GatedFwdArgs& a, hipStream_t s);
 hipError_t gated_bwd_launch(bool bf16, const GatedBwdArgs& a, hipStream_t s);
 hipError_t gated_step_launch(bool bf16, const GatedStepArgs& a, hipStream_t s);
 
