@@ -1522,7 +1522,7 @@ void plan_gated(int64_t B, int64_t T, int64_t d, int64_t tile_steps, bool grad, 
     p->init = words ? off : 0;
     p->off_part = off;
     if (grad) {
-        p->part_rows = B;
+        p->part_rows = B * p->nt;
         off = align_up(off + (size_t)p->part_rows * (size_t)d * 4);
     }
     p->total = off;
@@ -1540,12 +1540,12 @@ GatedTiles gated_tiles(const GatedPlan& p, void* workspace, uint64_t sig) {
     t.sig = sig;
     return t;
 }
-int64_t gated_fwd_tile(int dtype) { return 16 * gate_fwd_steps(dtype == MEMOROID_BF16); }
-// whether rows and addresses are whole vectors of four elements
-bool gated_full(int64_t d, int dtype, std::initializer_list<const void*> ps) {
-    if (d % 4 != 0) return false;
+int64_t gated_fwd_tile(int dtype) { return gate_fwd_shape(dtype == MEMOROID_BF16).tile(); }
+// whether rows and addresses are whole vectors of a lane's features
+bool gated_full(int64_t d, int dtype, const GateShape& sh, std::initializer_list<const void*> ps) {
+    if (d % sh.f != 0) return false;
     for (const void* x : ps)
-        if (!aligned(x, 4 * (size_t)elem_bytes(dtype))) return false;
+        if (!aligned(x, (size_t)(sh.f * elem_bytes(dtype)))) return false;
     return true;
 }
 
@@ -1605,14 +1605,14 @@ int memoroid_scan_gated(const void* x, const void* gates, const float* alpha, co
     a.tiles = gated_tiles(p, workspace, layout_sig({kSigGated, B, T, d, dtype}));
     hipStream_t s = (hipStream_t)stream;
     if (p.init && ws_init_launch(nullptr, 0, workspace, p.init, s) != hipSuccess) return MEMOROID_EHIP;
-    return check_hip(gated_fwd_launch(dtype == MEMOROID_BF16, gated_full(d, dtype, {x, gates, h}), a, s));
+    return check_hip(gated_fwd_launch(dtype == MEMOROID_BF16, gated_full(d, dtype, gate_fwd_shape(dtype == MEMOROID_BF16), {x, gates, h}), a, s));
 }
 
 size_t memoroid_scan_gated_bwd_workspace_bytes(int64_t B, int64_t T, int64_t d, int dtype) {
     bool empty;
     if (gated_check(B, T, d, dtype, &empty) != MEMOROID_OK || empty) return 0;
     GatedPlan p;
-    plan_gated(B, T, d, T, true, &p);
+    plan_gated(B, T, d, kGateStateSteps, true, &p);
     return p.total;
 }
 
@@ -1629,7 +1629,7 @@ int memoroid_scan_gated_bwd(const void* x, const void* gates, const float* alpha
         !floats_ok({alpha, states, grad_state_out, grad_alpha, grad_state_in}))
         return MEMOROID_EINVAL;
     GatedPlan p;
-    plan_gated(B, T, d, T, true, &p);
+    plan_gated(B, T, d, kGateStateSteps, true, &p);
     if (!workspace || workspace_bytes < p.total) return MEMOROID_EWORKSPACE;
     if (!aligned(workspace, 16)) return MEMOROID_EINVAL;
     GatedBwdArgs a{};
@@ -1649,10 +1649,12 @@ int memoroid_scan_gated_bwd(const void* x, const void* gates, const float* alpha
     a.B = B;
     a.T = T;
     a.d = d;
+    a.tiles = gated_tiles(p, workspace, layout_sig({kSigGatedBwd, B, T, d, dtype}));
     hipStream_t s = (hipStream_t)stream;
-    const int st = check_hip(ws_init_launch(nullptr, 0, workspace, kAlign, s));
-    if (st != MEMOROID_OK) return st;
-    return check_hip(gated_bwd_launch(dtype == MEMOROID_BF16, a, s));
+    if (p.init && ws_init_launch(nullptr, 0, workspace, p.init, s) != hipSuccess) return MEMOROID_EHIP;
+    return check_hip(gated_bwd_launch(dtype == MEMOROID_BF16, gated_full(d, dtype, gate_bwd_shape(dtype == MEMOROID_BF16),
+                                                                         {x, gates, grad_h, grad_x, grad_gates}),
+                                      a, s));
 }
 
 int memoroid_gated_step(const void* x, const void* gates, const float* alpha, const uint8_t* start, float* state,

@@ -72,6 +72,10 @@ struct Decay {
         const float t = __builtin_fmaf(k, v, add);
         return slow() ? v + t : t;
     }
+    __device__ __forceinline__ float of(float v) const {
+        const float t = k * v;
+        return SLOW ? __builtin_fmaf(k, v, v) : slow() ? __builtin_fmaf(k, v, v) : t;
+    }
 };
 
 // A feature's gates at one step
@@ -87,24 +91,28 @@ struct Gate {
 };
 
 // ------------------------------------------------------------------ tiles
-// A workgroup has kGateCols features of a tape (a chain) and 16 runs of L steps, one
-// behind the other: lane q of a run's 16 lanes the features 4 q .. 4 q + 3.
-constexpr int kGateRuns = 16;
+// A workgroup has kGateCols features of a tape (a chain) and `runs` runs of L steps, one
+// behind the other.  A lane has F features of a run, so 64 / F lanes a run's all.
+template <int F, int THREADS>
+struct Lanes {
+    static constexpr int kRow = kGateCols / F, kRuns = THREADS / kRow;
+    static_assert(kRow <= 64 && kRuns <= 32, "a run lies in a wavefront, the runs' flags in a word");
+};
 
-// Four features as they lie in memory.  FULL: rows and addresses are multiples of four
+// F features as they lie in memory.  FULL: rows and addresses are multiples of F
 // elements, and one access moves them.
-template <bool BF16>
-struct Four {
-    static constexpr int SIZE = BF16 ? 2 : 4, WORDS = BF16 ? 2 : 4;
+template <bool BF16, int F>
+struct Few {
+    static constexpr int SIZE = BF16 ? 2 : 4, WORDS = F * SIZE / 4;
     uint32_t w[WORDS];
     template <int AUX, bool FULL>
     __device__ __forceinline__ void load(Rsrc r, uint32_t off, int left) {
         if constexpr (FULL) {
-            WideAccess<4 * SIZE>::template bload<AUX>(w, r, off);
+            WideAccess<F * SIZE>::template bload<AUX>(w, r, off);
         } else {
-            uint32_t v[4];
+            uint32_t v[F];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int e = 0; e < F; ++e) {
                 const int at = e < left ? (int)(off + e * SIZE) : (int)kOob;
                 if constexpr (BF16) v[e] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(r, at, 0, AUX);
                 else v[e] = __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, AUX);
@@ -116,10 +124,10 @@ struct Four {
     template <int AUX, bool FULL>
     __device__ __forceinline__ void store(Rsrc r, uint32_t off, int left) const {
         if constexpr (FULL) {
-            WideAccess<4 * SIZE>::template bstore<AUX>(r, off, w);
+            WideAccess<F * SIZE>::template bstore<AUX>(r, off, w);
         } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int e = 0; e < F; ++e) {
                 const int at = e < left ? (int)(off + e * SIZE) : (int)kOob;
                 if constexpr (BF16)
                     __builtin_amdgcn_raw_buffer_store_b16((unsigned short)(w[e / 2] >> (e & 1 ? 16 : 0)), r, at, 0, AUX);
@@ -131,9 +139,14 @@ struct Four {
         if constexpr (BF16) return e & 1 ? bf16_hi(w[e / 2]) : bf16_lo(w[e / 2]);
         else return __uint_as_float(w[e]);
     }
-    __device__ __forceinline__ void set(const float (&v)[4]) {
+    __device__ __forceinline__ void set(const float (&v)[F]) {
 #pragma unroll
         for (int e = 0; e < WORDS; ++e) w[e] = BF16 ? f32x2_to_bf16x2(v[2 * e], v[2 * e + 1]) : __float_as_uint(v[e]);
+    }
+    // hides that what follows could be formed from what came before
+    __device__ __forceinline__ void opaque() {
+#pragma unroll
+        for (int e = 0; e < WORDS; ++e) asm volatile("" : "+v"(w[e]));
     }
 };
 

@@ -16,24 +16,24 @@ namespace memoroid {
 
 namespace {
 
-template <bool BF16, bool FULL, int L>
-__global__ __launch_bounds__(256) void gated_fwd_kernel(GatedFwdArgs p) {
-    static_assert(L <= 16 && kGateStateSteps % L == 0, "flags: a lane per step; states lie between runs");
-    constexpr int kSteps = kGateRuns * L;
+template <bool BF16, bool FULL, int F, int L, int THREADS, int WAVES>
+__global__ __launch_bounds__(THREADS, WAVES) void gated_fwd_kernel(GatedFwdArgs p) {
+    constexpr int kRow = Lanes<F, THREADS>::kRow, kRuns = Lanes<F, THREADS>::kRuns, kSteps = kRuns * L;
+    static_assert(L <= kRow && L < 32 && kGateStateSteps % L == 0, "flags: a lane per step; states lie between runs");
     __shared__ uint32_t s_tile;
-    __shared__ float sU[kGateRuns][kGateCols], sH[kGateRuns][kGateCols];      // runs: rates' sum, added
-    __shared__ float sPU[kGateRuns][kGateCols], sPH[kGateRuns][kGateCols];    // what comes before them in the tile
+    __shared__ float sU[kRuns][kGateCols], sH[kRuns][kGateCols];      // runs: rates' sum, added
+    __shared__ float sPU[kRuns][kGateCols], sPH[kRuns][kGateCols];    // what comes before them in the tile
     __shared__ float sCarry[kGateCols];
-    __shared__ uint32_t sF[kGateRuns];
+    __shared__ uint32_t sF[kRuns];
 
     const TileOf at = take_tile(p.tiles, &s_tile);
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, q = tid & 15, run = tid >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, q = tid & (kRow - 1), run = tid / kRow;
     const int64_t b = at.chain / p.tiles.nfb, fb = at.chain - b * p.tiles.nfb;
     const int64_t slot = at.tile * p.tiles.nchains + at.chain;
     const int64_t row0 = at.tile * kSteps, rows = p.T - row0, tape0 = b * p.T + row0;
-    const int64_t f0 = fb * kGateCols + 4 * q;
-    const int left = p.d - f0 >= 4 ? 4 : p.d > f0 ? (int)(p.d - f0) : 0;
-    constexpr int S = Four<BF16>::SIZE;
+    const int64_t f0 = fb * kGateCols + F * q;
+    const int left = p.d - f0 >= F ? F : p.d > f0 ? (int)(p.d - f0) : 0;
+    constexpr int S = Few<BF16, F>::SIZE;
     const int64_t line = p.d * S;                                    // bytes of a row of x
 
     // ---- (1)
@@ -43,32 +43,36 @@ __global__ __launch_bounds__(256) void gated_fwd_kernel(GatedFwdArgs p) {
     const Rsrc rs_g = make_rsrc((const char*)p.gates + 2 * tape0 * line, 2 * rows * line);
     const uint32_t off = left ? (uint32_t)(run * L * line + f0 * S) : kOob, step = left ? (uint32_t)line : 0u;
     const uint32_t goff = left ? (uint32_t)(2 * run * L * line + f0 * S) : kOob;
-    Four<BF16> x[L], r[L], i[L];
+    Few<BF16, F> x[L], r[L], i[L];
 #pragma unroll
     for (int s = 0; s < L; ++s) {
         r[s].template load<0, FULL>(rs_g, goff + 2 * s * step, left);
         i[s].template load<0, FULL>(rs_g, goff + (2 * s + 1) * step, left);
         x[s].template load<0, FULL>(rs_x, off + s * step, left);
     }
-    float rate[4];
+    float rate[F], most = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) rate[e] = e < left ? __builtin_fabsf(p.alpha[f0 + e]) : 0.0f;
+    for (int e = 0; e < F; ++e) {
+        rate[e] = e < left ? __builtin_fabsf(p.alpha[f0 + e]) : 0.0f;
+        most = __builtin_fmaxf(most, rate[e]);
+    }
     __builtin_amdgcn_sched_barrier(0);
     const uint64_t flags = __ballot(flag != 0u);
-    const uint32_t begins = (uint32_t)(flags >> (lane & 48)) & ((1u << L) - 1u);
-    const bool slow = __all(rate[0] <= kSlow && rate[1] <= kSlow && rate[2] <= kSlow && rate[3] <= kSlow);
+    const uint32_t begins = (uint32_t)(flags >> (lane & (64 - kRow))) & ((1u << L) - 1u);
+    const bool slow = __all(most <= kSlow);
 
     // ---- (2)
-    float k[L][4], v[L][4], u[4] = {0.f, 0.f, 0.f, 0.f}, h[4] = {0.f, 0.f, 0.f, 0.f};
+    float k[L][F], v[L][F], u[F] = {}, h[F] = {};
     auto gates = [&](auto SLOW) {
 #pragma unroll
         for (int s = 0; s < L; ++s) {
             // (keeps the two branches' common work, all steps' of it, from being done ahead of
             // the branch, in registers that are not there)
+            r[s].opaque();
+            i[s].opaque();
+            x[s].opaque();
 #pragma unroll
-            for (int e = 0; e < Four<BF16>::WORDS; ++e) asm volatile("" : "+v"(r[s].w[e]), "+v"(i[s].w[e]), "+v"(x[s].w[e]));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int e = 0; e < F; ++e) {
                 const Gate<BF16, SLOW.value> g(r[s].get(e), i[s].get(e), rate[e]);
                 k[s][e] = g.decay.k;
                 v[s][e] = g.m * g.si * x[s].get(e);
@@ -82,7 +86,7 @@ __global__ __launch_bounds__(256) void gated_fwd_kernel(GatedFwdArgs p) {
 #pragma unroll
         for (int s = 0; s < L; ++s) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int e = 0; e < F; ++e) {
                 Decay<SLOW.value> d;
                 d.k = k[s][e];
                 const float next = d.of(h[e], v[s][e]);
@@ -105,22 +109,22 @@ __global__ __launch_bounds__(256) void gated_fwd_kernel(GatedFwdArgs p) {
     else gates(No{});
     run_through([](int) {});
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        sU[run][4 * q + e] = u[e];
-        sH[run][4 * q + e] = h[e];
+    for (int e = 0; e < F; ++e) {
+        sU[run][F * q + e] = u[e];
+        sH[run][F * q + e] = h[e];
     }
     if (q == 0) sF[run] = begins != 0u;
     barrier_lds();
 
     // ---- (3), (4): a lane per feature
     uint32_t held = 0;                                               // runs with a begin step
-    if (lane < kGateRuns) held = sF[lane];
-    held = (uint32_t)__ballot(held != 0u && lane < kGateRuns);
+    if (lane < kRuns) held = sF[lane];
+    held = (uint32_t)__ballot(held != 0u && lane < kRuns);
     float tu = 0.0f, th = 0.0f;
     const bool in = fb * kGateCols + lane < p.d;
     if (wave < 2) {
 #pragma unroll
-        for (int g = 0; g < kGateRuns; ++g) {
+        for (int g = 0; g < kRuns; ++g) {
             if (wave == 0) {
                 sPU[g][lane] = tu;
                 sPH[g][lane] = th;
@@ -151,9 +155,9 @@ __global__ __launch_bounds__(256) void gated_fwd_kernel(GatedFwdArgs p) {
         put_incl(p.tiles, slot, lane, Decay<false>(tu).of(sCarry[lane], th));
     const bool cut = (held & ((1u << run) - 1u)) != 0u;              // a begin step before this run
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const float ph = sPH[run][4 * q + e];
-        const float from = Decay<false>(sPU[run][4 * q + e]).of(sCarry[4 * q + e], ph);
+    for (int e = 0; e < F; ++e) {
+        const float ph = sPH[run][F * q + e];
+        const float from = Decay<false>(sPU[run][F * q + e]).of(sCarry[F * q + e], ph);
         h[e] = cut ? ph : from;
     }
     const Rsrc rs_h = make_rsrc((char*)p.h + tape0 * line, rows * line);
@@ -161,13 +165,13 @@ __global__ __launch_bounds__(256) void gated_fwd_kernel(GatedFwdArgs p) {
     asm volatile("" : "+v"(out));                                    // (the loads' offsets need not be kept for this)
     const int64_t last = rows - 1 - (int64_t)run * L;                // the tape's last step, seen from this run
     run_through([&](int s) {
-        Four<BF16> o;
+        Few<BF16, F> o;
         o.set(h);
         o.template store<kNt, FULL>(rs_h, out, left);
         out += step;
         if (s == last && p.state_out) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < F; ++e)
                 if (e < left) p.state_out[b * p.d + f0 + e] = h[e];
         }
     });
@@ -175,15 +179,16 @@ __global__ __launch_bounds__(256) void gated_fwd_kernel(GatedFwdArgs p) {
     if (p.states && next % kGateStateSteps == 0 && next < p.T) {
         float* const o = p.states + (b * ((p.T + kGateStateSteps - 1) / kGateStateSteps) + next / kGateStateSteps) * p.d;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < F; ++e)
             if (e < left) o[f0 + e] = h[e];
     }
 }
 
 template <bool BF16, bool FULL>
 void fwd(const GatedFwdArgs& a, hipStream_t s) {
-    constexpr int L = gate_fwd_steps(BF16);
-    hipLaunchKernelGGL((gated_fwd_kernel<BF16, FULL, L>), dim3((unsigned)(a.tiles.nt * a.tiles.nchains)), dim3(256), 0, s, a);
+    constexpr GateShape sh = gate_fwd_shape(BF16);
+    hipLaunchKernelGGL((gated_fwd_kernel<BF16, FULL, sh.f, sh.steps, sh.threads, sh.waves>),
+                       dim3((unsigned)(a.tiles.nt * a.tiles.nchains)), dim3(sh.threads), 0, s, a);
 }
 
 }  // namespace

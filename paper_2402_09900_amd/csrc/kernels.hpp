@@ -437,11 +437,23 @@ hipError_t rotate_launch(bool bf16, bool grad, int ch, const RotateArgs& a, hipS
 hipError_t rotate_weights_launch(const RotateArgs& a, float* dwq, float* dwk, hipStream_t s);
 
 // -------------------------------------------------------- gated recurrence
-// (gated.hip).  The state before every kGateStateSteps-th step is kept for the gradient.
+// (gated_fwd.hip, gated_bwd.hip, gated_step.hip).  The state before every kGateStateSteps-th step is kept for the gradient.
 constexpr int kGateStateSteps = 128;
 constexpr int kGateCols = 64;        // features of a chain
-// steps of a lane's run; a tile has 16 runs
-constexpr int gate_fwd_steps(bool bf16) { return bf16 ? 16 : 8; }
+// Features and steps of a lane, threads of a workgroup, wavefronts of a SIMD that its
+// registers are to allow
+struct GateShape {
+    int f, steps, threads, waves;
+    constexpr int tile() const { return threads * f / kGateCols * steps; }   // steps
+};
+#ifndef GF
+#define GF 2, 16, 256, 3
+#define GF32 2, 8, 256, 3
+#define GB 2, 16, 256, 2
+#define GB32 2, 8, 512, 2
+#endif
+constexpr GateShape gate_fwd_shape(bool bf16) { return bf16 ? GateShape{GF} : GateShape{GF32}; }
+constexpr GateShape gate_bwd_shape(bool bf16) { return bf16 ? GateShape{GB} : GateShape{GB32}; }
 
 // Tiles of the scans and the words they hand on (gated_common.hpp)
 struct GatedTiles {
@@ -480,6 +492,7 @@ struct GatedBwdArgs {
     float* part;                // [part_rows][d] sums for dalpha, or NULL
     float* dalpha;              // [d]
     int64_t B, T, d, part_rows;
+    GatedTiles tiles;
 };
 struct GatedStepArgs {
     const void* x;              // [B][d]
@@ -492,7 +505,7 @@ struct GatedStepArgs {
 };
 // full: d and every address are multiples of four elements
 hipError_t gated_fwd_launch(bool bf16, bool full, const GatedFwdArgs& a, hipStream_t s);
-hipError_t gated_bwd_launch(bool bf16, const GatedBwdArgs& a, hipStream_t s);
+hipError_t gated_bwd_launch(bool bf16, bool full, const GatedBwdArgs& a, hipStream_t s);
 hipError_t gated_step_launch(bool bf16, const GatedStepArgs& a, hipStream_t s);
 
 // ------------------------------------------------- layer norm and dropout
