@@ -535,7 +535,7 @@ int memoroid_rotate_qk_bwd(const void* q, const void* k, const int32_t* position
  *   state_out  optional out [B][d] fp32, the state after step T - 1 (not rounded to
  *              bf16); not written when T is 0.
  *   states     optional out [B][ceil(T / MEMOROID_GATED_STATE_STEPS)][d] fp32, the states
- *              before steps 0, 128, 256 ...: what the gradient starts from.
+ *              before steps 0, 64, 128 ...: what the gradient starts from.
  *   Gates may be infinite: r = -inf holds the state and lets nothing in (a = 1, b = 0),
  *   r = inf takes the whole rate.  A NaN (or an infinite x) stays in its feature's episode
  *   and in the steps from its own on.  States are fp32; b, a and their products are right
@@ -544,7 +544,7 @@ int memoroid_rotate_qk_bwd(const void* q, const void* k, const int32_t* position
  *   otherwise).  fp32 arrays 4-byte aligned.  state_out must
  *   not be state_in.  Workspace (self-initialising): memoroid_scan_gated_workspace_bytes.
  * ------------------------------------------------------------------------ */
-#define MEMOROID_GATED_STATE_STEPS 128
+#define MEMOROID_GATED_STATE_STEPS 64
 
 size_t memoroid_scan_gated_workspace_bytes(int64_t B, int64_t T, int64_t d, int dtype);
 

@@ -39,7 +39,7 @@ F32, BF16, C64 = 0, 1, 2
  OP_TBB_BEGIN_INDICES, OP_TBB_SAMPLE, OP_RETENTION, OP_RETENTION_BWD, OP_ROTATE_QK_BWD, OP_GATED, OP_GATED_BWD,
  OP_LAYER_NORM_BWD) = range(16)
 
-GATED_STATE_STEPS = 128             # MEMOROID_GATED_STATE_STEPS
+GATED_STATE_STEPS = 64             # MEMOROID_GATED_STATE_STEPS
 
 _lib = None
 
@@ -1119,7 +1119,7 @@ def scan_gated(x, gates, alpha, start, state=None, final_state: bool = False, ke
     float32 or bfloat16; alpha: float32 [d]; start: uint8 [B,T]; state: optional
     float32 [B,d], the state before step 0 (which begins an episode only if its flag
     says so).  Returns h [B,T,d], followed by the float32 state after the last step
-    when final_state is true and by the states [B,ceil(T/128),d] that scan_gated_bwd
+    when final_state is true and by the states [B,ceil(T/64),d] that scan_gated_bwd
     takes when keep_states is true."""
     torch = _torch()
     B, T, d, dt = _gated_args(x, gates, alpha, start, True)
@@ -1146,7 +1146,7 @@ def scan_gated_bwd(x, gates, alpha, start, states, grad_h, grad_state=None, need
     B, T, d, dt = _gated_args(x, gates, alpha, start, True)
     _gated_state(grad_state, "grad_state", B, d)
     if states.dtype != torch.float32 or states.shape != (B, -(-T // GATED_STATE_STEPS), d):
-        raise TypeError("states must be float32 [B,ceil(T/128),d]")
+        raise TypeError("states must be float32 [B,ceil(T/64),d]")
     if grad_h.dtype != x.dtype or grad_h.shape != x.shape:
         raise TypeError("grad_h must be [B,T,d] of x's dtype")
     dev = _check_cuda(x, gates, alpha, start, states, grad_h, grad_state)

@@ -1533,6 +1533,11 @@ GatedTiles gated_tiles(const GatedPlan& p, void* workspace, uint64_t sig) {
     t.nt = p.nt;
     t.nfb = p.nfb;
     t.nchains = p.nchains;
+    // With many chains few tiles of one are under way at once, and the value before a tile
+    // is soon near it; looking further costs more than it finds (T = 65536, d = 2048, 32
+    // chains, bf16: 233 us, 278 with one turn before all wavefronts look).  With few it
+    // pays (d = 512, no episode's begin: 182 -> 126 us; d = 256, fp32 326 -> 211).
+    t.near = p.nchains >= 16 ? kMaxPolls : 8;
     t.ctr = (uint32_t*)(ws + p.off_ctr);
     t.agg = (uint64_t*)(ws + p.off_agg);
     t.incl = (uint32_t*)(ws + p.off_incl);
@@ -1540,13 +1545,19 @@ GatedTiles gated_tiles(const GatedPlan& p, void* workspace, uint64_t sig) {
     t.sig = sig;
     return t;
 }
-int64_t gated_fwd_tile(int dtype) { return gate_fwd_shape(dtype == MEMOROID_BF16).tile(); }
+int64_t gated_tile(int dtype, bool grad) {
+    return (grad ? gate_bwd_shape(dtype == MEMOROID_BF16) : gate_fwd_shape(dtype == MEMOROID_BF16)).tile();
+}
 // whether rows and addresses are whole vectors of a lane's features
 bool gated_full(int64_t d, int dtype, const GateShape& sh, std::initializer_list<const void*> ps) {
     if (d % sh.f != 0) return false;
     for (const void* x : ps)
         if (!aligned(x, (size_t)(sh.f * elem_bytes(dtype)))) return false;
     return true;
+}
+
+int gated_policy(int64_t B, int64_t T, int64_t d, int dtype) {
+    return cache_policy(d * elem_bytes(dtype), (double)B * (double)T * (double)d * elem_bytes(dtype));
 }
 
 // Argument checks that the gated entry points share; MEMOROID_OK and *empty when there
@@ -1572,7 +1583,7 @@ size_t memoroid_scan_gated_workspace_bytes(int64_t B, int64_t T, int64_t d, int 
     bool empty;
     if (gated_check(B, T, d, dtype, &empty) != MEMOROID_OK || empty) return 0;
     GatedPlan p;
-    plan_gated(B, T, d, gated_fwd_tile(dtype), false, &p);
+    plan_gated(B, T, d, gated_tile(dtype, false), false, &p);
     return p.total;
 }
 
@@ -1587,7 +1598,7 @@ int memoroid_scan_gated(const void* x, const void* gates, const float* alpha, co
         !floats_ok({alpha, state_in, state_out, states}))
         return MEMOROID_EINVAL;
     GatedPlan p;
-    plan_gated(B, T, d, gated_fwd_tile(dtype), false, &p);
+    plan_gated(B, T, d, gated_tile(dtype, false), false, &p);
     if (!workspace || workspace_bytes < p.total) return MEMOROID_EWORKSPACE;
     if (!aligned(workspace, 16)) return MEMOROID_EINVAL;
     GatedFwdArgs a{};
@@ -1605,14 +1616,15 @@ int memoroid_scan_gated(const void* x, const void* gates, const float* alpha, co
     a.tiles = gated_tiles(p, workspace, layout_sig({kSigGated, B, T, d, dtype}));
     hipStream_t s = (hipStream_t)stream;
     if (p.init && ws_init_launch(nullptr, 0, workspace, p.init, s) != hipSuccess) return MEMOROID_EHIP;
-    return check_hip(gated_fwd_launch(dtype == MEMOROID_BF16, gated_full(d, dtype, gate_fwd_shape(dtype == MEMOROID_BF16), {x, gates, h}), a, s));
+    return check_hip(gated_fwd_launch(dtype == MEMOROID_BF16, gated_full(d, dtype, gate_fwd_shape(dtype == MEMOROID_BF16), {x, gates, h}),
+                                      gated_policy(B, T, d, dtype), a, s));
 }
 
 size_t memoroid_scan_gated_bwd_workspace_bytes(int64_t B, int64_t T, int64_t d, int dtype) {
     bool empty;
     if (gated_check(B, T, d, dtype, &empty) != MEMOROID_OK || empty) return 0;
     GatedPlan p;
-    plan_gated(B, T, d, kGateStateSteps, true, &p);
+    plan_gated(B, T, d, gated_tile(dtype, true), true, &p);
     return p.total;
 }
 
@@ -1629,7 +1641,7 @@ int memoroid_scan_gated_bwd(const void* x, const void* gates, const float* alpha
         !floats_ok({alpha, states, grad_state_out, grad_alpha, grad_state_in}))
         return MEMOROID_EINVAL;
     GatedPlan p;
-    plan_gated(B, T, d, kGateStateSteps, true, &p);
+    plan_gated(B, T, d, gated_tile(dtype, true), true, &p);
     if (!workspace || workspace_bytes < p.total) return MEMOROID_EWORKSPACE;
     if (!aligned(workspace, 16)) return MEMOROID_EINVAL;
     GatedBwdArgs a{};
@@ -1654,7 +1666,7 @@ int memoroid_scan_gated_bwd(const void* x, const void* gates, const float* alpha
     if (p.init && ws_init_launch(nullptr, 0, workspace, p.init, s) != hipSuccess) return MEMOROID_EHIP;
     return check_hip(gated_bwd_launch(dtype == MEMOROID_BF16, gated_full(d, dtype, gate_bwd_shape(dtype == MEMOROID_BF16),
                                                                          {x, gates, grad_h, grad_x, grad_gates}),
-                                      a, s));
+                                      gated_policy(B, T, d, dtype), a, s));
 }
 
 int memoroid_gated_step(const void* x, const void* gates, const float* alpha, const uint8_t* start, float* state,

@@ -5,7 +5,7 @@
 //     dx = lam m sig(i),   di = lam b (1 - sig(i)),
 //     du = lam a (sig(i) x a / m - h_before),   dr = du u (1 - sig(r)),
 //     dalpha = sign(alpha) sum du sig(r).
-// A tile is 128 steps: the forward call has kept the state before each, so h is run through
+// The forward call has kept the state before every tile (and more), so h is run through
 // again within a tile and only c goes from tile to tile, the last first.  Otherwise
 // as forward (gated_fwd.hip): the runs' effects on h and on c, put one behind the other
 // by a wavefront each; then h through each run; then, with the c that enters, back through
@@ -19,15 +19,19 @@ namespace memoroid {
 
 namespace {
 
-template <bool BF16, bool FULL, int F, int L, int THREADS, int WAVES>
+template <bool BF16, bool FULL, int POL, int F, int L, int THREADS, int WAVES>
 __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs p) {
+    constexpr int kLd = POL == kStreamAll ? kNt : 0, kSt = POL != kCached ? kNt : 0;
     constexpr int kRow = Lanes<F, THREADS>::kRow, kRuns = Lanes<F, THREADS>::kRuns, kSteps = kRuns * L;
-    static_assert(kSteps == kGateStateSteps, "a tile starts from a state that was kept");
+    static_assert(kSteps % kGateStateSteps == 0, "a tile starts from a state that was kept");
     static_assert(L <= kRow && L < 32, "flags: a lane per step");
     __shared__ uint32_t s_tile;
-    __shared__ float sU[kRuns][kGateCols], sH[kRuns][kGateCols], sC[kRuns][kGateCols];
-    __shared__ float sPU[kRuns][kGateCols], sPC[kRuns][kGateCols];    // what comes behind them in the tile
+    // per run: its rates' sum, its decay, what it adds to h and to c (then the state that enters
+    // it in the place of the one), the c that enters it
+    __shared__ float sU[kRuns][kGateCols], sK[kRuns][kGateCols], sH[kRuns][kGateCols], sC[kRuns][kGateCols];
+    __shared__ float sIn[kRuns][kGateCols];
     __shared__ float sCarry[kGateCols];
+    __shared__ LookBackLds sLook;
     __shared__ uint32_t sF[kRuns];
 
     const TileOf at = take_tile(p.tiles, &s_tile);
@@ -46,15 +50,29 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs 
     const Rsrc rs_x = make_rsrc((const char*)p.x + tape0 * line, rows * line);
     const Rsrc rs_h = make_rsrc((const char*)p.g + tape0 * line, rows * line);
     const Rsrc rs_g = make_rsrc((const char*)p.gates + 2 * tape0 * line, 2 * rows * line);
-    const uint32_t off = left ? (uint32_t)(run * L * line + f0 * S) : kOob, step = left ? (uint32_t)line : 0u;
+    const uint32_t off = left ? (uint32_t)(run * L * line + f0 * S) : kOob;
     const uint32_t goff = left ? (uint32_t)(2 * run * L * line + f0 * S) : kOob;
+    const uint32_t step = (uint32_t)line;
+    // (a whole tile's rows by scalar offsets, the last tile's by the lanes': gated_fwd.hip)
+    const bool whole = rows >= kSteps;
     Few<BF16, F> x[L], r[L], i[L], g[L];
+    if (whole) {
 #pragma unroll
-    for (int s = 0; s < L; ++s) {
-        r[s].template load<0, FULL>(rs_g, goff + 2 * s * step, left);
-        i[s].template load<0, FULL>(rs_g, goff + (2 * s + 1) * step, left);
-        x[s].template load<0, FULL>(rs_x, off + s * step, left);
-        g[s].template load<0, FULL>(rs_h, off + s * step, left);
+        for (int s = 0; s < L; ++s) {
+            r[s].template load<kLd, FULL>(rs_g, goff, 2 * s * step, left);
+            i[s].template load<kLd, FULL>(rs_g, goff, (2 * s + 1) * step, left);
+            x[s].template load<kLd, FULL>(rs_x, off, s * step, left);
+            g[s].template load<kLd, FULL>(rs_h, off, s * step, left);
+        }
+    } else {
+        const uint32_t by = left ? step : 0u;
+#pragma unroll
+        for (int s = 0; s < L; ++s) {
+            r[s].template load<kLd, FULL>(rs_g, goff + 2 * s * by, 0, left);
+            i[s].template load<kLd, FULL>(rs_g, goff + (2 * s + 1) * by, 0, left);
+            x[s].template load<kLd, FULL>(rs_x, off + s * by, 0, left);
+            g[s].template load<kLd, FULL>(rs_h, off + s * by, 0, left);
+        }
     }
     float rate[F], most = 0.0f;
 #pragma unroll
@@ -77,7 +95,10 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs 
     }
 
     // ---- the runs' effects on h, forwards, and on c, backwards
-    float k[L][F], sr[L][F], si[L][F], u[F] = {}, h[F] = {}, c[F] = {};
+    // Kept of a step, for the way back: the decay k, sig(r), and of what does not wait for h
+    // and c dx / lam, di / lam and sig(i) x a / m less the run's own h before the step
+    float k[L][F], sr[L][F], px[L][F], pi[L][F], z[L][F];
+    float u[F] = {}, h[F] = {}, c[F] = {};
     using Yes = std::true_type;
     using No = std::false_type;
     auto effects = [&](auto SLOW, auto BEGINS) {
@@ -89,14 +110,21 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs 
             g[s].opaque();
 #pragma unroll
             for (int e = 0; e < F; ++e) {
-                const Gate<BF16, SLOW.value> gate(r[s].get(e), i[s].get(e), rate[e]);
-                k[s][e] = gate.decay.k;
-                sr[s][e] = gate.sr;
-                si[s][e] = gate.si;
-                u[e] += gate.u;
-                const float v = gate.m * gate.si * x[s].get(e);
-                const float next = gate.decay.of(h[e], v);
-                h[e] = BEGINS.value && (begins >> s & 1u) ? v : next;
+                const float gr = sigmoid<BF16>(r[s].get(e)), gi = sigmoid<BF16>(i[s].get(e)), gu = rate[e] * gr;
+                const Decay<SLOW.value, BF16> d(gu);
+                const float w = d.taken(), m2 = w * (2.0f - w);
+                // (where nothing decays, m = 0 and 1 / m is to stay finite)
+                const float rm = __builtin_amdgcn_rsqf(__builtin_fmaxf(m2, 0x1p-100f)), m = m2 * rm;
+                const float xs = x[s].get(e) * gi, v = m * xs;
+                const bool begin = BEGINS.value && (begins >> s & 1u);
+                k[s][e] = d.k;
+                sr[s][e] = gr;
+                px[s][e] = m * gi;
+                pi[s][e] = v * (1.0f - gi);
+                z[s][e] = xs * rm * d.left() - (begin ? 0.0f : h[e]);
+                u[e] += gu;
+                const float next = d.of(h[e], v);
+                h[e] = begin ? v : next;
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -119,6 +147,7 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs 
 #pragma unroll
     for (int e = 0; e < F; ++e) {
         sU[run][F * q + e] = u[e];
+        sK[run][F * q + e] = Decay<false>(u[e]).k;
         sH[run][F * q + e] = h[e];
         sC[run][F * q + e] = c[e];
     }
@@ -129,115 +158,107 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs 
     uint32_t held = 0;                                               // runs with a begin step
     if (lane < kRuns) held = sF[lane];
     held = (uint32_t)__ballot(held != 0u && lane < kRuns);
-    float tu = 0.0f, tc = 0.0f;
     const bool in = fb * kGateCols + lane < p.d;
     const int64_t f = fb * kGateCols + lane;
-    if (wave < 2) {
+    float tc = 0.0f;                                                 // wavefront 1: the tile's
+    Decay<false> whole_tile;
+    whole_tile.k = 0.0f;
+    auto apply = [&](int n, float v, float add) {
+        Decay<false> d;
+        d.k = sK[n][lane];
+        const float next = d.of(v, add);
+        return held >> n & 1u ? add : next;
+    };
+    auto enter = [&](float v) {
+        sCarry[lane] = v;
 #pragma unroll
         for (int n = kRuns - 1; n >= 0; --n) {
-            if (wave == 0) {
-                sPU[n][lane] = tu;
-                sPC[n][lane] = tc;
-            }
-            const float nu = sU[n][lane], nc = sC[n][lane];
-            const float next = Decay<false>(nu).of(tc, nc);
-            tc = held >> n & 1u ? nc : next;
-            tu += nu;
+            sIn[n][lane] = v;
+            v = apply(n, v, sC[n][lane]);
         }
-        const float first = at.tile == 0 && p.grad_state && in ? p.grad_state[b * p.d + f] : 0.0f;
-        if (wave == 1) {
-            if (p.tiles.nt > 1 && in) {
-                if (held) put_incl(p.tiles, slot, lane, tc);
-                else if (at.tile == 0) put_incl(p.tiles, slot, lane, Decay<false>(tu).of(first, tc));
-                else put_agg(p.tiles, slot, lane, tu, tc);
+    };
+    if (wave == 0) {
+        float v = at.tile == 0 && p.grad_state && in ? p.grad_state[b * p.d + f] : 0.0f;
+        const bool there = at.tile == 0 || try_near(p.tiles, at.tile, at.chain, lane, in, v);
+        if (there) enter(v);
+        if (lane == 0) sLook.done = there;
+    } else if (wave == 1) {
+        if (p.tiles.nt > 1) {
+            float u = 0.0f;
+#pragma unroll
+            for (int n = kRuns - 1; n >= 0; --n) {
+                tc = apply(n, tc, sC[n][lane]);
+                u += sU[n][lane];
             }
-        } else {
-            sCarry[lane] = at.tile == 0 ? first : look_back(p.tiles, at.tile, at.chain, lane, in);
+            whole_tile = Decay<false>(u);
+            const float first = at.tile == 0 && p.grad_state && in ? p.grad_state[b * p.d + f] : 0.0f;
+            if (in) {
+                if (held) put_incl(p.tiles, slot, lane, tc);
+                else if (at.tile == 0) put_incl(p.tiles, slot, lane, whole_tile.of(first, tc));
+                else put_agg(p.tiles, slot, lane, whole_tile.k, tc);
+            }
         }
     } else if (wave == 2) {
-        // (in place: the state that enters a run for what the run does to one)
-        float now = in ? p.states[(b * p.tiles.nt + tile) * p.d + f] : 0.0f;
+        const int64_t ns = (p.T + kGateStateSteps - 1) / kGateStateSteps;
+        float v = in ? p.states[(b * ns + tile * (kSteps / kGateStateSteps)) * p.d + f] : 0.0f;
 #pragma unroll
         for (int n = 0; n < kRuns; ++n) {
-            const float nh = sH[n][lane];
-            sH[n][lane] = now;
-            const float next = Decay<false>(sU[n][lane]).of(now, nh);
-            now = held >> n & 1u ? nh : next;
+            const float add = sH[n][lane];
+            sH[n][lane] = v;
+            v = apply(n, v, add);
         }
     }
     barrier_lds();
+    if (!sLook.done) look_far<THREADS>(p.tiles, at.tile, at.chain, lane, in, sLook, enter);
 
-    // ---- h before every step; then back with c
+    // ---- the state that enters the run goes into z; then back with c
     if (wave == 1 && p.tiles.nt > 1 && at.tile > 0 && !held && in)
-        put_incl(p.tiles, slot, lane, Decay<false>(tu).of(sCarry[lane], tc));
-    const bool cut = held >> run >> 1 != 0u;                         // a begin step behind this run
+        put_incl(p.tiles, slot, lane, whole_tile.of(sCarry[lane], tc));
     float sum[F] = {};
 #pragma unroll
     for (int e = 0; e < F; ++e) {
         h[e] = sH[run][F * q + e];
-        const float pc = sPC[run][F * q + e];
-        const float from = Decay<false>(sPU[run][F * q + e]).of(sCarry[F * q + e], pc);
-        c[e] = cut ? pc : from;
+        c[e] = sIn[run][F * q + e];
     }
     const Rsrc rs_dx = make_rsrc((char*)p.dx + tape0 * line, rows * line);
     const Rsrc rs_dg = make_rsrc((char*)p.dgates + 2 * tape0 * line, 2 * rows * line);
-    uint32_t out = off, gout = goff;
-    asm volatile("" : "+v"(out), "+v"(gout));                        // (the loads' offsets need not be kept for this)
-    out += (L - 1) * step;
-    gout += 2 * (L - 1) * step;
     auto back = [&](auto SLOW, auto BEGINS) {
-        float before[L][F];
+        // (h: what is left of the entering state before each step)
 #pragma unroll
-        for (int s = 0; s < L; ++s) {
-            x[s].opaque();
-            g[s].opaque();
+        for (int s = 0; s < L; ++s)
 #pragma unroll
             for (int e = 0; e < F; ++e) {
-                const bool begin = BEGINS.value && (begins >> s & 1u);
                 Decay<SLOW.value> d;
                 d.k = k[s][e];
-                const float w = d.taken();
-                const float v = __builtin_amdgcn_sqrtf(w * (2.0f - w)) * si[s][e] * x[s].get(e);
-                const float next = d.of(h[e], v);
-                before[s][e] = begin ? 0.0f : h[e];
-                h[e] = begin ? v : next;
+                const bool begin = BEGINS.value && (begins >> s & 1u);
+                z[s][e] -= begin ? 0.0f : h[e];
+                h[e] = begin ? 0.0f : d.of(h[e]);
             }
-            __builtin_amdgcn_sched_barrier(0);
-        }
 #pragma unroll
         for (int s = L - 1; s >= 0; --s) {
-            // (what the loop above has formed of these is formed again rather than kept)
-            x[s].opaque();
-#pragma unroll
-            for (int e = 0; e < F; ++e) asm volatile("" : "+v"(k[s][e]), "+v"(si[s][e]), "+v"(sr[s][e]));
+            g[s].opaque();
             float dx[F], dr[F], di[F];
 #pragma unroll
             for (int e = 0; e < F; ++e) {
                 Decay<SLOW.value> d;
                 d.k = k[s][e];
-                const float w = d.taken(), a = d.left(), m2 = w * (2.0f - w);
-                // (where nothing decays, m = 0 and 1 / m is to stay finite)
-                const float rm = __builtin_amdgcn_rsqf(__builtin_fmaxf(m2, 0x1p-100f));
-                const float xs = x[s].get(e) * si[s][e], m = m2 * rm;
                 const float lam = g[s].get(e) + c[e];
-                const float du = lam * a * __builtin_fmaf(xs * a, rm, -before[s][e]);
-                const float ds = du * sr[s][e];
+                const float ds = lam * d.left() * z[s][e] * sr[s][e];
                 sum[e] += ds;
-                dx[e] = lam * m * si[s][e];
+                dx[e] = lam * px[s][e];
                 dr[e] = ds * rate[e] * (1.0f - sr[s][e]);
-                di[e] = lam * m * xs * (1.0f - si[s][e]);
+                di[e] = lam * pi[s][e];
                 const float next = d.of(lam);
                 c[e] = BEGINS.value && (begins >> s & 1u) ? 0.0f : next;
             }
             Few<BF16, F> o;
+            const uint32_t by = whole || !left ? 0u : step, sby = whole ? step : 0u;
             o.set(dx);
-            o.template store<kNt, FULL>(rs_dx, out, left);
+            o.template store<kSt, FULL>(rs_dx, off + s * by, s * sby, left);
             o.set(dr);
-            o.template store<kNt, FULL>(rs_dg, gout, left);
+            o.template store<kSt, FULL>(rs_dg, goff + 2 * s * by, 2 * s * sby, left);
             o.set(di);
-            o.template store<kNt, FULL>(rs_dg, gout + step, left);
-            out -= step;
-            gout -= 2 * step;
+            o.template store<kSt, FULL>(rs_dg, goff + (2 * s + 1) * by, (2 * s + 1) * sby, left);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -283,18 +304,25 @@ __global__ __launch_bounds__(1024) void gated_alpha_kernel(const float* part, co
     }
 }
 
-template <bool BF16, bool FULL>
-void bwd(const GatedBwdArgs& a, hipStream_t s) {
+template <bool BF16, bool FULL, int POL>
+void launch(const GatedBwdArgs& a, hipStream_t s) {
     constexpr GateShape sh = gate_bwd_shape(BF16);
-    hipLaunchKernelGGL((gated_bwd_kernel<BF16, FULL, sh.f, sh.steps, sh.threads, sh.waves>),
+    hipLaunchKernelGGL((gated_bwd_kernel<BF16, FULL, POL, sh.f, sh.steps, sh.threads, sh.waves>),
                        dim3((unsigned)(a.tiles.nt * a.tiles.nchains)), dim3(sh.threads), 0, s, a);
+}
+// (rows that lanes cannot take whole are not whole lines either)
+template <bool BF16>
+void with_policy(bool full, int policy, const GatedBwdArgs& a, hipStream_t s) {
+    if (!full) launch<BF16, false, kCached>(a, s);
+    else if (policy == kCached) launch<BF16, true, kCached>(a, s);
+    else if (policy == kStreamOut) launch<BF16, true, kStreamOut>(a, s);
+    else launch<BF16, true, kStreamAll>(a, s);
 }
 
 }  // namespace
 
-hipError_t gated_bwd_launch(bool bf16, bool full, const GatedBwdArgs& a, hipStream_t s) {
-    if (bf16) full ? bwd<true, true>(a, s) : bwd<true, false>(a, s);
-    else full ? bwd<false, true>(a, s) : bwd<false, false>(a, s);
+hipError_t gated_bwd_launch(bool bf16, bool full, int policy, const GatedBwdArgs& a, hipStream_t s) {
+    bf16 ? with_policy<true>(full, policy, a, s) : with_policy<false>(full, policy, a, s);
     if (!a.part) return hipGetLastError();
     hipLaunchKernelGGL(gated_alpha_kernel, dim3((unsigned)((a.d + 63) / 64)), dim3(1024), 0, s, a.part, a.alpha, a.dalpha,
                        a.part_rows, a.d);

@@ -38,27 +38,35 @@ __device__ __forceinline__ float sigmoid(float v) {
     return __builtin_amdgcn_rcpf(1.0f + exp_minus<FAST>(v));
 }
 
-// 1 - exp(-u) for 0 <= u <= 1/2, relative error 2^-23: a minimax fit of (1 - exp(-u)) / u
-// there with the constant 1, relative error 2^-27.
+// 1 - exp(-u) for 0 <= u <= 1/2: minimax fits of (1 - exp(-u)) / u there with the
+// constant 1.  Relative error with the roundings 2^-23; FAST: 2^-22.
+template <bool FAST>
 __device__ __forceinline__ float loss_of(float u) {
-    float p = -0x1.27c254p-10f;
-    p = __builtin_fmaf(p, u, 0x1.0c9214p-7f);
-    p = __builtin_fmaf(p, u, -0x1.550f3ep-5f);
-    p = __builtin_fmaf(p, u, 0x1.555374p-3f);
-    p = __builtin_fmaf(p, u, -0x1.fffff8p-2f);
-    p = __builtin_fmaf(p, u, 1.0f);
-    return p * u;
+    float p;
+    if constexpr (FAST) {
+        p = 0x1.bf3082p-8f;
+        p = __builtin_fmaf(p, u, -0x1.5058b2p-5f);
+        p = __builtin_fmaf(p, u, 0x1.5521aap-3f);
+        p = __builtin_fmaf(p, u, -0x1.fffebp-2f);
+    } else {
+        p = -0x1.27c254p-10f;
+        p = __builtin_fmaf(p, u, 0x1.0c9214p-7f);
+        p = __builtin_fmaf(p, u, -0x1.550f3ep-5f);
+        p = __builtin_fmaf(p, u, 0x1.555374p-3f);
+        p = __builtin_fmaf(p, u, -0x1.fffff8p-2f);
+    }
+    return __builtin_fmaf(p, u, 1.0f) * u;
 }
 
 // A decay by exp(-u), u >= 0, in one float k: a slow one is minus what it takes away
 // (its sign bit set, for u = 0 too), a fast one what it leaves.  SLOW: the caller knows
 // that no u is above kSlow.
-template <bool SLOW>
+template <bool SLOW, bool FAST = false>
 struct Decay {
     float k;
     __device__ __forceinline__ Decay() {}
     __device__ __forceinline__ explicit Decay(float u) {
-        k = -loss_of(u);
+        k = -loss_of<FAST>(u);
         if constexpr (!SLOW) {
             const float a = __builtin_amdgcn_exp2f(u * -kLog2e);
             k = u <= kSlow ? k : a;
@@ -82,7 +90,7 @@ struct Decay {
 template <bool FAST, bool SLOW>
 struct Gate {
     float sr, si, u, m;
-    Decay<SLOW> decay;
+    Decay<SLOW, FAST> decay;
     __device__ __forceinline__ Gate(float r, float i, float rate)
         : sr(sigmoid<FAST>(r)), si(sigmoid<FAST>(i)), u(rate * sr), decay(u) {
         const float w = decay.taken();
@@ -105,33 +113,54 @@ template <bool BF16, int F>
 struct Few {
     static constexpr int SIZE = BF16 ? 2 : 4, WORDS = F * SIZE / 4;
     uint32_t w[WORDS];
+    // soff: a scalar offset, which the range check does not cover
     template <int AUX, bool FULL>
-    __device__ __forceinline__ void load(Rsrc r, uint32_t off, int left) {
+    __device__ __forceinline__ void load(Rsrc r, uint32_t off, uint32_t soff, int left) {
         if constexpr (FULL) {
-            WideAccess<F * SIZE>::template bload<AUX>(w, r, off);
+            if constexpr (WORDS == 1) {
+                w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, (int)off, (int)soff, AUX);
+            } else if constexpr (WORDS == 2) {
+                const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(r, (int)off, (int)soff, AUX);
+                w[0] = v.x;
+                w[1] = v.y;
+            } else {
+                const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, (int)soff, AUX);
+                w[0] = v.x;
+                w[1] = v.y;
+                w[2] = v.z;
+                w[3] = v.w;
+            }
         } else {
             uint32_t v[F];
 #pragma unroll
             for (int e = 0; e < F; ++e) {
                 const int at = e < left ? (int)(off + e * SIZE) : (int)kOob;
-                if constexpr (BF16) v[e] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(r, at, 0, AUX);
-                else v[e] = __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, AUX);
+                if constexpr (BF16) v[e] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(r, at, (int)soff, AUX);
+                else v[e] = __builtin_amdgcn_raw_buffer_load_b32(r, at, (int)soff, AUX);
             }
 #pragma unroll
             for (int e = 0; e < WORDS; ++e) w[e] = BF16 ? v[2 * e] | v[2 * e + 1] << 16 : v[e];
         }
     }
     template <int AUX, bool FULL>
-    __device__ __forceinline__ void store(Rsrc r, uint32_t off, int left) const {
+    __device__ __forceinline__ void store(Rsrc r, uint32_t off, uint32_t soff, int left) const {
         if constexpr (FULL) {
-            WideAccess<F * SIZE>::template bstore<AUX>(r, off, w);
+            if constexpr (WORDS == 1) {
+                __builtin_amdgcn_raw_buffer_store_b32(w[0], r, (int)off, (int)soff, AUX);
+            } else if constexpr (WORDS == 2) {
+                const u32x2 v = {w[0], w[1]};
+                __builtin_amdgcn_raw_buffer_store_b64(v, r, (int)off, (int)soff, AUX);
+            } else {
+                const u32x4 v = {w[0], w[1], w[2], w[3]};
+                __builtin_amdgcn_raw_buffer_store_b128(v, r, (int)off, (int)soff, AUX);
+            }
         } else {
 #pragma unroll
             for (int e = 0; e < F; ++e) {
                 const int at = e < left ? (int)(off + e * SIZE) : (int)kOob;
                 if constexpr (BF16)
-                    __builtin_amdgcn_raw_buffer_store_b16((unsigned short)(w[e / 2] >> (e & 1 ? 16 : 0)), r, at, 0, AUX);
-                else __builtin_amdgcn_raw_buffer_store_b32(w[e], r, at, 0, AUX);
+                    __builtin_amdgcn_raw_buffer_store_b16((unsigned short)(w[e / 2] >> (e & 1 ? 16 : 0)), r, at, (int)soff, AUX);
+                else __builtin_amdgcn_raw_buffer_store_b32(w[e], r, at, (int)soff, AUX);
             }
         }
     }
@@ -175,60 +204,133 @@ __device__ __forceinline__ TileOf take_tile(const GatedTiles& t, uint32_t* share
     return r;
 }
 
-// Words that tiles hand on, per feature: AGG, a tile without a begin step, as its rates'
-// sum u and what it adds; INCL, the value after the tile.  Unpublished: all ones.
-__device__ __forceinline__ void put_agg(const GatedTiles& t, int64_t slot, int f, float u, float add) {
-    publish64(t.agg + slot * kGateCols + f, pack2(u, add));
+// Words that tiles hand on, per feature: AGG, a tile without a begin step, as its decay
+// and what it adds; INCL, the value after the tile.  Unpublished: all ones.
+__device__ __forceinline__ void put_agg(const GatedTiles& t, int64_t slot, int f, float k, float add) {
+    publish64(t.agg + slot * kGateCols + f, pack2(k, add));
 }
 __device__ __forceinline__ void put_incl(const GatedTiles& t, int64_t slot, int f, float v) {
     publish32(t.incl + slot * kGateCols + f, __float_as_uint(canon(v)));
 }
 
-// The value that enters a tile, for the feature of this lane (`need` false: 0): from the
-// nearest tile before it that has published its own, the ones between applied one
-// after the other.  That is what each of them does for its own, so the result is the
-// same bit for bit whichever that tile was.
-__device__ __forceinline__ float look_back(const GatedTiles& t, int64_t tile, int chain, int f, bool need) {
-    constexpr int W = 8;
-    float v = 0.0f;
+// The value that enters a tile, a lane per feature: that of the nearest tile before it
+// that has published its own, the ones between applied one after the other.  Each of them
+// does the same for its own, so the result is the same bit for bit whichever tile that
+// was.  First one wavefront tries: the word of the tile right before (which mostly is
+// there where chains are many), then once the four nearest tiles.  If that is not
+// enough, all wavefronts look at kNear tiles at a time, and the first puts what they
+// found together: where chains are few and long, that is what sets the pace.
+constexpr int kNear = 32;
+constexpr float kIsValue = 2.0f, kIsEmpty = 3.0f;                    // in the place of a decay's k, which is below 1
+struct LookBackLds {
+    float k[kNear][kGateCols], v[kNear][kGateCols];
+    uint32_t done;
+};
+
+__device__ __forceinline__ bool try_near(const GatedTiles& t, int64_t tile, int chain, int f, bool need, float& v) {
+    constexpr int W = 4;
+    const int64_t stride = (int64_t)t.nchains * kGateCols, from = ((tile - 1) * t.nchains + chain) * kGateCols + f;
+    v = 0.0f;
     bool done = !need;
-    uint32_t polls = 0;
-    while (!__all(done)) {
-        if (!done) {
-            uint32_t in[W];
-            uint64_t ag[W];
+    if (need) {
+        const uint32_t w = peek32(t.incl + from);
+        v = __uint_as_float(w);
+        done = w != kEmpty32;
+    }
+    for (uint32_t polls = 0; !__all(done); ++polls) {
+        if (polls == t.near) return false;
+        if (polls) __builtin_amdgcn_s_sleep(1);
+        uint32_t in[W];
+        uint64_t ag[W];
 #pragma unroll
-            for (int k = 0; k < W; ++k) {
+        for (int k = 0; k < W; ++k) {
+            in[k] = kEmpty32;
+            ag[k] = kEmpty64;
+            if (k < tile) {
+                in[k] = peek32(t.incl + (from - k * stride));
+                ag[k] = peek64(t.agg + (from - k * stride));
+            }
+        }
+        int at = W;
+#pragma unroll
+        for (int k = W - 1; k >= 0; --k) at = in[k] != kEmpty32 ? k : at;
+        bool ready = at < W && !done;
+#pragma unroll
+        for (int k = 0; k < W - 1; ++k) ready = ready && (k >= at || ag[k] != kEmpty64);
+#pragma unroll
+        for (int k = W - 1; k >= 0; --k) {
+            Decay<false> d;
+            d.k = unpack_lo(ag[k]);
+            const float next = d.of(v, unpack_hi(ag[k]));
+            v = !ready || k > at ? v : k == at ? __uint_as_float(in[k]) : next;
+        }
+        done = done || ready;
+    }
+    return true;
+}
+
+// All wavefronts of the workgroup; `use` is called by the first with the value
+template <int THREADS, class Use>
+__device__ __forceinline__ void look_far(const GatedTiles& t, int64_t tile, int chain, int f, bool need, LookBackLds& lds,
+                                         Use use) {
+    constexpr int kEach = kNear / (THREADS / 64);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int64_t stride = (int64_t)t.nchains * kGateCols, from = ((tile - 1) * t.nchains + chain) * kGateCols + f;
+    for (uint32_t polls = 0;; ++polls) {
+#pragma unroll
+        for (int n0 = 0; n0 < kEach; n0 += 4) {                      // (four at a time: few registers beside a tile's)
+            uint32_t in[4];
+            uint64_t ag[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int n = wave * kEach + n0 + k;
                 in[k] = kEmpty32;
                 ag[k] = kEmpty64;
-                if (k < tile) {
-                    const int64_t i = ((tile - 1 - k) * t.nchains + chain) * kGateCols + f;
-                    in[k] = peek32(t.incl + i);
-                    ag[k] = peek64(t.agg + i);
+                if (n < tile && need) {
+                    in[k] = peek32(t.incl + (from - n * stride));
+                    ag[k] = peek64(t.agg + (from - n * stride));
                 }
             }
-            int at = W;
 #pragma unroll
-            for (int k = W - 1; k >= 0; --k) at = in[k] != kEmpty32 ? k : at;
-            bool ready = at < W;
-#pragma unroll
-            for (int k = 0; k < W - 1; ++k) ready = ready && (k >= at || ag[k] != kEmpty64);
-            if (ready) {
-#pragma unroll
-                for (int k = W - 1; k >= 0; --k) {
-                    const float next = Decay<false>(unpack_lo(ag[k])).of(v, unpack_hi(ag[k]));
-                    v = k == at ? __uint_as_float(in[k]) : k < at ? next : v;
+            for (int k = 0; k < 4; ++k) {
+                const int n = wave * kEach + n0 + k;
+                const bool is = in[k] != kEmpty32;
+                lds.k[n][lane] = is ? kIsValue : ag[k] != kEmpty64 ? unpack_lo(ag[k]) : kIsEmpty;
+                lds.v[n][lane] = is ? __uint_as_float(in[k]) : unpack_hi(ag[k]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        barrier_lds();
+        if (wave == 0) {
+            int at = kNear;                                          // the nearest value
+            bool ready = !need;
+            for (int n = 0; n < kNear && !__all(ready || at < kNear); ++n) {
+                const float k = lds.k[n][lane];
+                if (at == kNear && k == kIsValue) at = n;
+                if (at == kNear && k == kIsEmpty) at = kNear + 1;    // not there yet
+            }
+            ready = ready || at < kNear;
+            const bool all = __all(ready);
+            const bool late = polls >= kMaxPolls;
+            if (all || late) {
+                float v = need && at < kNear ? lds.v[at][lane] : 0.0f;
+                for (int n = kNear - 2; n >= 0; --n) {
+                    if (!__any(need && n < at && at < kNear)) continue;
+                    Decay<false> d;
+                    d.k = lds.k[n][lane];
+                    const float next = d.of(v, lds.v[n][lane]);
+                    v = need && n < at && at < kNear ? next : v;
                 }
-                done = true;
-            } else if (++polls > kMaxPolls) {
-                flag_timeout(&t.hdr->timeout);
-                done = true;
+                if (!all) flag_timeout(&t.hdr->timeout);
+                use(v);
             } else {
                 __builtin_amdgcn_s_sleep(1);
             }
+            if (lane == 0) lds.done = all || late;
         }
+        barrier_lds();
+        if (lds.done) return;
     }
-    return v;
 }
 
 }  // namespace memoroid

@@ -16,15 +16,17 @@ namespace memoroid {
 
 namespace {
 
-template <bool BF16, bool FULL, int F, int L, int THREADS, int WAVES>
+template <bool BF16, bool FULL, int POL, int F, int L, int THREADS, int WAVES>
 __global__ __launch_bounds__(THREADS, WAVES) void gated_fwd_kernel(GatedFwdArgs p) {
+    constexpr int kLd = POL == kStreamAll ? kNt : 0, kSt = POL != kCached ? kNt : 0;
     constexpr int kRow = Lanes<F, THREADS>::kRow, kRuns = Lanes<F, THREADS>::kRuns, kSteps = kRuns * L;
     static_assert(L <= kRow && L < 32 && kGateStateSteps % L == 0, "flags: a lane per step; states lie between runs");
     __shared__ uint32_t s_tile;
-    __shared__ float sU[kRuns][kGateCols], sH[kRuns][kGateCols];      // runs: rates' sum, added
-    __shared__ float sPU[kRuns][kGateCols], sPH[kRuns][kGateCols];    // what comes before them in the tile
+    // per run: its rates' sum, its decay, what it adds, the state that enters it
+    __shared__ float sU[kRuns][kGateCols], sK[kRuns][kGateCols], sH[kRuns][kGateCols], sIn[kRuns][kGateCols];
     __shared__ float sCarry[kGateCols];
-    __shared__ uint32_t sF[kRuns];
+    __shared__ LookBackLds sLook;
+    __shared__ uint32_t sF[kRuns], sBegins;
 
     const TileOf at = take_tile(p.tiles, &s_tile);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, q = tid & (kRow - 1), run = tid / kRow;
@@ -41,14 +43,28 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_fwd_kernel(GatedFwdArgs 
     const uint32_t flag = q < L ? bload_u8(rs_st, (uint32_t)(run * L + q)) : 0u;
     const Rsrc rs_x = make_rsrc((const char*)p.x + tape0 * line, rows * line);
     const Rsrc rs_g = make_rsrc((const char*)p.gates + 2 * tape0 * line, 2 * rows * line);
-    const uint32_t off = left ? (uint32_t)(run * L * line + f0 * S) : kOob, step = left ? (uint32_t)line : 0u;
+    const uint32_t off = left ? (uint32_t)(run * L * line + f0 * S) : kOob;
     const uint32_t goff = left ? (uint32_t)(2 * run * L * line + f0 * S) : kOob;
+    const uint32_t step = (uint32_t)line;
+    // A whole tile's rows are reached by scalar offsets; those of the tape's last tile by
+    // the lanes', which the range check covers (lanes past d stay outside either way)
+    const bool whole = rows >= kSteps;
     Few<BF16, F> x[L], r[L], i[L];
+    if (whole) {
 #pragma unroll
-    for (int s = 0; s < L; ++s) {
-        r[s].template load<0, FULL>(rs_g, goff + 2 * s * step, left);
-        i[s].template load<0, FULL>(rs_g, goff + (2 * s + 1) * step, left);
-        x[s].template load<0, FULL>(rs_x, off + s * step, left);
+        for (int s = 0; s < L; ++s) {
+            r[s].template load<kLd, FULL>(rs_g, goff, 2 * s * step, left);
+            i[s].template load<kLd, FULL>(rs_g, goff, (2 * s + 1) * step, left);
+            x[s].template load<kLd, FULL>(rs_x, off, s * step, left);
+        }
+    } else {
+        const uint32_t by = left ? step : 0u;
+#pragma unroll
+        for (int s = 0; s < L; ++s) {
+            r[s].template load<kLd, FULL>(rs_g, goff + 2 * s * by, 0, left);
+            i[s].template load<kLd, FULL>(rs_g, goff + (2 * s + 1) * by, 0, left);
+            x[s].template load<kLd, FULL>(rs_x, off + s * by, 0, left);
+        }
     }
     float rate[F], most = 0.0f;
 #pragma unroll
@@ -111,70 +127,100 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_fwd_kernel(GatedFwdArgs 
 #pragma unroll
     for (int e = 0; e < F; ++e) {
         sU[run][F * q + e] = u[e];
+        sK[run][F * q + e] = Decay<false>(u[e]).k;
         sH[run][F * q + e] = h[e];
     }
     if (q == 0) sF[run] = begins != 0u;
+    if (tid == 0) sBegins = begins & 1u;
     barrier_lds();
 
     // ---- (3), (4): a lane per feature
     uint32_t held = 0;                                               // runs with a begin step
     if (lane < kRuns) held = sF[lane];
     held = (uint32_t)__ballot(held != 0u && lane < kRuns);
-    float tu = 0.0f, th = 0.0f;
     const bool in = fb * kGateCols + lane < p.d;
-    if (wave < 2) {
+    float th = 0.0f;                                                 // wavefront 1: the tile's
+    Decay<false> whole_tile;
+    whole_tile.k = 0.0f;
+    auto apply = [&](int n, float v) {
+        Decay<false> d;
+        d.k = sK[n][lane];
+        const float add = sH[n][lane], next = d.of(v, add);
+        return held >> n & 1u ? add : next;
+    };
+    const bool need = in && !sBegins;                                // a tile that begins an episode takes nothing
+    auto enter = [&](float v) {
+        sCarry[lane] = v;
 #pragma unroll
-        for (int g = 0; g < kRuns; ++g) {
-            if (wave == 0) {
-                sPU[g][lane] = tu;
-                sPH[g][lane] = th;
-            }
-            const float gu = sU[g][lane], gh = sH[g][lane];
-            const float next = Decay<false>(gu).of(th, gh);
-            th = held >> g & 1u ? gh : next;
-            tu += gu;
+        for (int n = 0; n < kRuns; ++n) {
+            sIn[n][lane] = v;
+            v = apply(n, v);
         }
+    };
+    if (wave == 0) {
+        float v = at.tile == 0 && p.state_in && in ? p.state_in[b * p.d + fb * kGateCols + lane] : 0.0f;
+        if (at.tile == 0 && p.states && in)
+            p.states[b * ((p.T + kGateStateSteps - 1) / kGateStateSteps) * p.d + fb * kGateCols + lane] = v;
+        const bool there = at.tile == 0 || try_near(p.tiles, at.tile, at.chain, lane, need, v);
+        if (there) enter(v);
+        if (lane == 0) sLook.done = there;
+    } else if (wave == 1 && p.tiles.nt > 1) {
+        float u = 0.0f;
+#pragma unroll
+        for (int n = 0; n < kRuns; ++n) {
+            th = apply(n, th);
+            u += sU[n][lane];
+        }
+        whole_tile = Decay<false>(u);
         const float first = at.tile == 0 && p.state_in && in ? p.state_in[b * p.d + fb * kGateCols + lane] : 0.0f;
-        if (wave == 1) {
-            if (p.tiles.nt > 1 && in) {
-                if (held) put_incl(p.tiles, slot, lane, th);
-                else if (at.tile == 0) put_incl(p.tiles, slot, lane, Decay<false>(tu).of(first, th));
-                else put_agg(p.tiles, slot, lane, tu, th);
-            }
-        } else {
-            const bool first_begins = flags & 1u;                    // (this wavefront's first lane: the tile's first step)
-            sCarry[lane] = at.tile == 0 ? first : look_back(p.tiles, at.tile, at.chain, lane, in && !first_begins);
-            if (at.tile == 0 && p.states && in)
-                p.states[b * ((p.T + kGateStateSteps - 1) / kGateStateSteps) * p.d + fb * kGateCols + lane] = first;
+        if (in) {
+            if (held) put_incl(p.tiles, slot, lane, th);
+            else if (at.tile == 0) put_incl(p.tiles, slot, lane, whole_tile.of(first, th));
+            else put_agg(p.tiles, slot, lane, whole_tile.k, th);
         }
     }
     barrier_lds();
+    if (!sLook.done) look_far<THREADS>(p.tiles, at.tile, at.chain, lane, need, sLook, enter);
 
     // ---- (5)
     if (wave == 1 && p.tiles.nt > 1 && at.tile > 0 && !held && in)
-        put_incl(p.tiles, slot, lane, Decay<false>(tu).of(sCarry[lane], th));
-    const bool cut = (held & ((1u << run) - 1u)) != 0u;              // a begin step before this run
+        put_incl(p.tiles, slot, lane, whole_tile.of(sCarry[lane], th));
 #pragma unroll
-    for (int e = 0; e < F; ++e) {
-        const float ph = sPH[run][F * q + e];
-        const float from = Decay<false>(sPU[run][F * q + e]).of(sCarry[F * q + e], ph);
-        h[e] = cut ? ph : from;
-    }
+    for (int e = 0; e < F; ++e) h[e] = sIn[run][F * q + e];
     const Rsrc rs_h = make_rsrc((char*)p.h + tape0 * line, rows * line);
-    uint32_t out = off;
-    asm volatile("" : "+v"(out));                                    // (the loads' offsets need not be kept for this)
+    float from[F];
+#pragma unroll
+    for (int e = 0; e < F; ++e) from[e] = h[e];
+    if (whole) {
+        run_through([&](int s) {
+            Few<BF16, F> o;
+            o.set(h);
+            o.template store<kSt, FULL>(rs_h, off, s * step, left);
+        });
+    } else {
+        const uint32_t by = left ? step : 0u;
+        through(No{}, Yes{}, [&](int s) {
+            Few<BF16, F> o;
+            o.set(h);
+            o.template store<kSt, FULL>(rs_h, off + s * by, 0, left);
+        });
+    }
     const int64_t last = rows - 1 - (int64_t)run * L;                // the tape's last step, seen from this run
-    run_through([&](int s) {
-        Few<BF16, F> o;
-        o.set(h);
-        o.template store<kNt, FULL>(rs_h, out, left);
-        out += step;
-        if (s == last && p.state_out) {
+    if (p.state_out && last >= 0 && last < L) {
+        float end[F];
+#pragma unroll
+        for (int e = 0; e < F; ++e) {
+            end[e] = h[e];
+            h[e] = from[e];
+        }
+        through(No{}, Yes{}, [&](int s) {
 #pragma unroll
             for (int e = 0; e < F; ++e)
-                if (e < left) p.state_out[b * p.d + f0 + e] = h[e];
-        }
-    });
+                if (s == last && e < left) p.state_out[b * p.d + f0 + e] = h[e];
+        });
+#pragma unroll
+        for (int e = 0; e < F; ++e) h[e] = end[e];
+    }
     const int64_t next = row0 + (int64_t)(run + 1) * L;              // the step behind this run
     if (p.states && next % kGateStateSteps == 0 && next < p.T) {
         float* const o = p.states + (b * ((p.T + kGateStateSteps - 1) / kGateStateSteps) + next / kGateStateSteps) * p.d;
@@ -184,18 +230,25 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_fwd_kernel(GatedFwdArgs 
     }
 }
 
-template <bool BF16, bool FULL>
-void fwd(const GatedFwdArgs& a, hipStream_t s) {
+template <bool BF16, bool FULL, int POL>
+void launch(const GatedFwdArgs& a, hipStream_t s) {
     constexpr GateShape sh = gate_fwd_shape(BF16);
-    hipLaunchKernelGGL((gated_fwd_kernel<BF16, FULL, sh.f, sh.steps, sh.threads, sh.waves>),
+    hipLaunchKernelGGL((gated_fwd_kernel<BF16, FULL, POL, sh.f, sh.steps, sh.threads, sh.waves>),
                        dim3((unsigned)(a.tiles.nt * a.tiles.nchains)), dim3(sh.threads), 0, s, a);
+}
+// (rows that lanes cannot take whole are not whole lines either)
+template <bool BF16>
+void with_policy(bool full, int policy, const GatedFwdArgs& a, hipStream_t s) {
+    if (!full) launch<BF16, false, kCached>(a, s);
+    else if (policy == kCached) launch<BF16, true, kCached>(a, s);
+    else if (policy == kStreamOut) launch<BF16, true, kStreamOut>(a, s);
+    else launch<BF16, true, kStreamAll>(a, s);
 }
 
 }  // namespace
 
-hipError_t gated_fwd_launch(bool bf16, bool full, const GatedFwdArgs& a, hipStream_t s) {
-    if (bf16) full ? fwd<true, true>(a, s) : fwd<true, false>(a, s);
-    else full ? fwd<false, true>(a, s) : fwd<false, false>(a, s);
+hipError_t gated_fwd_launch(bool bf16, bool full, int policy, const GatedFwdArgs& a, hipStream_t s) {
+    bf16 ? with_policy<true>(full, policy, a, s) : with_policy<false>(full, policy, a, s);
     return hipGetLastError();
 }
 

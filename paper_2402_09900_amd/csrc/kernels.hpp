@@ -438,7 +438,7 @@ hipError_t rotate_weights_launch(const RotateArgs& a, float* dwq, float* dwk, hi
 
 // -------------------------------------------------------- gated recurrence
 // (gated_fwd.hip, gated_bwd.hip, gated_step.hip).  The state before every kGateStateSteps-th step is kept for the gradient.
-constexpr int kGateStateSteps = 128;
+constexpr int kGateStateSteps = 64;
 constexpr int kGateCols = 64;        // features of a chain
 // Features and steps of a lane, threads of a workgroup, wavefronts of a SIMD that its
 // registers are to allow
@@ -446,19 +446,14 @@ struct GateShape {
     int f, steps, threads, waves;
     constexpr int tile() const { return threads * f / kGateCols * steps; }   // steps
 };
-#ifndef GF
-#define GF 2, 16, 256, 3
-#define GF32 2, 8, 256, 3
-#define GB 2, 16, 256, 2
-#define GB32 2, 8, 512, 2
-#endif
-constexpr GateShape gate_fwd_shape(bool bf16) { return bf16 ? GateShape{GF} : GateShape{GF32}; }
-constexpr GateShape gate_bwd_shape(bool bf16) { return bf16 ? GateShape{GB} : GateShape{GB32}; }
+constexpr GateShape gate_fwd_shape(bool bf16) { return bf16 ? GateShape{2, 16, 256, 4} : GateShape{2, 8, 256, 4}; }
+constexpr GateShape gate_bwd_shape(bool bf16) { return bf16 ? GateShape{2, 8, 256, 3} : GateShape{2, 8, 256, 2}; }
 
 // Tiles of the scans and the words they hand on (gated_common.hpp)
 struct GatedTiles {
     int64_t nt;                 // tiles of a chain
     int32_t nfb, nchains;       // chains of a tape, in all
+    uint32_t near;              // turns of the first wavefront alone (gated_common.hpp)
     uint32_t* ctr;              // [nchains], kCtrStride apart
     uint64_t* agg;              // [nt][nchains][kGateCols]
     uint32_t* incl;             // likewise
@@ -503,9 +498,9 @@ struct GatedStepArgs {
     void* h;                    // [B][d]
     int64_t B, d;
 };
-// full: d and every address are multiples of four elements
-hipError_t gated_fwd_launch(bool bf16, bool full, const GatedFwdArgs& a, hipStream_t s);
-hipError_t gated_bwd_launch(bool bf16, bool full, const GatedBwdArgs& a, hipStream_t s);
+// full: d and every address are multiples of a lane's features; policy: a CachePolicy
+hipError_t gated_fwd_launch(bool bf16, bool full, int policy, const GatedFwdArgs& a, hipStream_t s);
+hipError_t gated_bwd_launch(bool bf16, bool full, int policy, const GatedBwdArgs& a, hipStream_t s);
 hipError_t gated_step_launch(bool bf16, const GatedStepArgs& a, hipStream_t s);
 
 // ------------------------------------------------- layer norm and dropout
