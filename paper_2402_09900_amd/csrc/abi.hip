@@ -1765,8 +1765,11 @@ int memoroid_layer_norm(const void* x, const void* residual, const float* weight
 
 size_t memoroid_layer_norm_bwd_workspace_bytes(int64_t n, int64_t d) {
     if (n <= 0 || d <= 0 || n > INT32_MAX || d > kNormMaxDim) return 0;
-    int64_t rows;
-    return align_up(kAlign + (size_t)norm_groups(n, d, &rows) * 2 * (size_t)d * 4);
+    // (with a residual or without: the one size serves both)
+    int64_t rows, groups = norm_groups(n, d, false, &rows);
+    const int64_t with = norm_groups(n, d, true, &rows);
+    if (with > groups) groups = with;
+    return align_up(kAlign + (size_t)groups * 2 * (size_t)d * 4);
 }
 
 int memoroid_layer_norm_bwd(const void* x, const void* residual, const float* weight, const int64_t* rng,
@@ -1783,14 +1786,14 @@ int memoroid_layer_norm_bwd(const void* x, const void* residual, const float* we
         !floats_ok({weight, stats, grad_weight, grad_bias}))
         return MEMOROID_EINVAL;
     NormBwdArgs a{};
-    a.groups = norm_groups(n, d, &a.rows);
+    a.groups = norm_groups(n, d, residual != nullptr, &a.rows);
     hipStream_t s = (hipStream_t)stream;
     if (grad_weight || grad_bias) {
         if (!workspace || workspace_bytes < memoroid_layer_norm_bwd_workspace_bytes(n, d)) return MEMOROID_EWORKSPACE;
         if (!aligned(workspace, 16)) return MEMOROID_EINVAL;
         a.part = (float*)((char*)workspace + kAlign);
-        const int st = check_hip(ws_init_launch(nullptr, 0, workspace, kAlign, s));
-        if (st != MEMOROID_OK) return st;
+        a.hdr = (WsHeader*)workspace;
+        a.sig = layout_sig({kSigNormBwd, n, d});
     }
     a.x = x;
     a.residual = residual;

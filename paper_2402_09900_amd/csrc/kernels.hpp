@@ -538,6 +538,8 @@ struct NormBwdArgs {
     float* db;                  // [d], or NULL
     DropArgs drop;
     int64_t n, d, rows, groups;
+    WsHeader* hdr;              // header to prepare with sig, or NULL
+    uint64_t sig;
 };
 struct DropoutArgs {
     const void* x;              // [n][d]
@@ -547,9 +549,9 @@ struct DropoutArgs {
     int64_t n, d;
 };
 // groups of rows with a row of sums each, and rows in a group
-int64_t norm_groups(int64_t n, int64_t d, int64_t* rows);
+int64_t norm_groups(int64_t n, int64_t d, bool residual, int64_t* rows);
 hipError_t norm_launch(bool bf16, NormArgs a, hipStream_t s);
-hipError_t norm_bwd_launch(bool bf16, NormBwdArgs a, hipStream_t s);
+hipError_t norm_bwd_launch(bool bf16, const NormBwdArgs& a, hipStream_t s);
 hipError_t dropout_launch(bool bf16, const DropoutArgs& a, hipStream_t s);
 
 // ------------------------------------------- discounted return and GAE

@@ -10,8 +10,11 @@
 // s is summed up again from x and the residual for the gradient, in 32 bits: read
 // back from a bf16 s, xh would be off by 2^-9, and dw, a 32-bit result, with it.
 //
-// A lane has octets (eight elements in a row) 64 apart, CH of them; a row takes up to
-// a wavefront (the lanes of short rows hold several), four or sixteen.
+// A lane has octets (eight elements in a row), CH of them, and R rows at a time: loads of
+// all of them are under way together, and wavefronts that share a row meet once a sum for
+// R rows.  Rows of up to 512 elements lie in a wavefront's lanes (short ones side by side),
+// longer ones in 2 to 16 wavefronts, so that a lane keeps no more than 16 elements of the
+// weight and its sums in registers.
 #include <type_traits>
 
 #include "philox.hpp"
@@ -20,25 +23,58 @@ namespace memoroid {
 
 namespace {
 
-// Eight elements in memory order; `left` of them lie in the row.
-template <bool BF16>
+// 16 bytes at an address that is a multiple of 2 or 4
+typedef uint32_t Words2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t Words4 __attribute__((ext_vector_type(4), aligned(4)));
+
+// Eight elements in memory order.  EVEN: rows are whole octets.  Otherwise `left` of them
+// lie in the row, whose rows start at any element: accesses of up to 16 bytes at that
+// alignment, which the hardware takes.
+template <bool BF16, bool EVEN, int POL>
 struct Octet {
-    static constexpr int WORDS = BF16 ? 4 : 8;
+    static constexpr int WORDS = BF16 ? 4 : 8, SIZE = BF16 ? 2 : 4;
+    using Words = typename std::conditional<BF16, Words2, Words4>::type;
     uint32_t w[WORDS];
-    __device__ __forceinline__ void load(const void* p, int64_t i, int left) {
-        if (left >= 8) {
-            // (rows of odd widths start at any element: 16-byte accesses at that
-            // alignment, which the hardware takes)
-            __builtin_memcpy(w, (const char*)p + i * (BF16 ? 2 : 4), sizeof w);
+    // wide: the row has eight elements at least.  Its last octet is then loaded from where
+    // eight of them end the row, and settle() moves them down to the ones that are asked for:
+    // one access for every lane, and nobody waits for it before the values are due.
+    __device__ __forceinline__ void load(const void* p, int64_t i, int left, bool wide) {
+#pragma unroll
+        for (int e = 0; e < WORDS; ++e) w[e] = 0u;
+        if (left <= 0) return;
+        if (EVEN || wide) {
+            const char* const at = (const char*)p + (EVEN ? i : i - (8 - left)) * SIZE;
+#pragma unroll
+            for (int e = 0; e < WORDS; e += 4) {
+                const Words* const q = (const Words*)at + e / 4;
+                const Words v = POL == kStreamAll ? __builtin_nontemporal_load(q) : *q;
+                w[e] = v.x;
+                w[e + 1] = v.y;
+                w[e + 2] = v.z;
+                w[e + 3] = v.w;
+            }
         } else {
 #pragma unroll
-            for (int e = 0; e < WORDS; ++e) w[e] = 0u;
+            for (int e = 0; e < 7; ++e)
+                if (e < left) {
+                    if constexpr (BF16) w[e / 2] |= (uint32_t)((const uint16_t*)p)[i + e] << (e & 1 ? 16 : 0);
+                    else w[e] = ((const uint32_t*)p)[i + e];
+                }
+        }
+    }
+    __device__ __forceinline__ void settle(int left, bool wide) {
+        if (EVEN || left >= 8 || left <= 0 || !wide) return;
+        const int by = 8 - left;
+        if constexpr (BF16) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (e >= left) break;
-                if constexpr (BF16) w[e / 2] |= (uint32_t)((const uint16_t*)p)[i + e] << (e & 1 ? 16 : 0);
-                else w[e] = ((const uint32_t*)p)[i + e];
-            }
+            for (int e = 0; e < WORDS; ++e)
+                w[e] = by & 1 ? __builtin_amdgcn_alignbit(e + 1 < WORDS ? w[e + 1] : 0u, w[e], 16) : w[e];
+        }
+#pragma unroll
+        for (int m = BF16 ? 2 : 1; m < 8; m *= 2) {
+            const int words = m * SIZE / 4;
+#pragma unroll
+            for (int e = 0; e < WORDS; ++e) w[e] = by & m ? (e + words < WORDS ? w[e + words] : 0u) : w[e];
         }
     }
     __device__ __forceinline__ void values(float (&v)[8]) const {
@@ -57,72 +93,95 @@ struct Octet {
     }
     __device__ __forceinline__ void store(void* p, int64_t i, int left) const {
         if (left >= 8) {
-            __builtin_memcpy((char*)p + i * (BF16 ? 2 : 4), w, sizeof w);
-        } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (e >= left) break;
-                if constexpr (BF16) ((uint16_t*)p)[i + e] = (uint16_t)(w[e / 2] >> (e & 1 ? 16 : 0));
-                else ((uint32_t*)p)[i + e] = w[e];
+            for (int e = 0; e < WORDS; e += 4) {
+                Words* const q = (Words*)((char*)p + i * SIZE) + e / 4;
+                const Words v = {w[e], w[e + 1], w[e + 2], w[e + 3]};
+                if (POL != kCached && EVEN) __builtin_nontemporal_store(v, q);
+                else *q = v;
             }
+        } else if (!EVEN) {
+#pragma unroll
+            for (int e = 0; e < 7; ++e)
+                if (e < left) {
+                    if constexpr (BF16) ((uint16_t*)p)[i + e] = (uint16_t)(w[e / 2] >> (e & 1 ? 16 : 0));
+                    else ((uint32_t*)p)[i + e] = w[e];
+                }
         }
     }
 };
 
 __device__ __forceinline__ void load_floats(float (&v)[8], const float* p, int64_t i, int left, float other) {
+    if (p && left >= 8) {
+        __builtin_memcpy(v, p + i, sizeof v);
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = p && e < left ? p[i + e] : other;
-}
-
-// Sum over the lanes of a row: lanes of a wavefront (a power of two of them, `lanes`),
-// then WAVES wavefronts through LDS, in a fixed order.
-template <int WAVES>
-__device__ __forceinline__ float row_sum(float v, int lanes, float* lds) {
-    for (int m = 1; m < lanes; m <<= 1) v += lanes_xor(v, m);
-    if constexpr (WAVES > 1) {
-        const int wave = threadIdx.x >> 6;
-        if ((threadIdx.x & 63) == 0) lds[wave] = v;
-        barrier_lds();
-        v = 0.0f;
-#pragma unroll
-        for (int i = 0; i < WAVES; ++i) v += lds[i];
-        barrier_lds();
+        for (int e = 0; e < 8; ++e) v[e] = p && e < left ? p[i + e] : other;
     }
-    return v;
 }
 
-template <int WAVES>
-constexpr int block_of() { return WAVES == 1 ? 256 : 64 * WAVES; }
+// Sums over the lanes of a row, K of them at once: `lanes` lanes of a wavefront (a power
+// of two), then WAVES wavefronts through LDS, in a fixed order.  The two halves of `lds` take
+// turns, so that one barrier a call is enough: a half is written again only behind the
+// next call's.
+template <int WAVES, int K>
+__device__ __forceinline__ void row_sums(float (&v)[K], int lanes, float (*lds)[K][WAVES], int& turn) {
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        if (WAVES > 1 || m < lanes) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) v[k] += lanes_xor(v[k], m);
+        }
+    }
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) lds[turn][k][threadIdx.x >> 6] = v[k];
+        }
+        barrier_lds();
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            v[k] = lds[turn][k][0];
+#pragma unroll
+            for (int i = 1; i < WAVES; ++i) v[k] += lds[turn][k][i];
+        }
+        turn ^= 1;
+    }
+}
 
-// Where a thread's octets lie: octet `first` + 64 WAVES c of row `row` + at_once k
+constexpr int threads_of(int waves) { return waves == 1 ? 256 : 64 * waves; }
+
+// Where a thread's octets lie: octet first + 64 WAVES c of the rows row, row + at_once, ...
 struct Place {
     int lanes, first;
-    int64_t row, at_once;
+    int64_t row, at_once, end;          // the workgroup's rows are below `end`
 };
 template <int WAVES>
-__device__ __forceinline__ Place place_of(int64_t d, int64_t rows) {
+__device__ __forceinline__ Place place_of(int64_t n, int64_t d, int64_t rows) {
     Place p;
-    const int nv = (int)((d + 7) / 8);
+    const int nv = (int)((d + 7) / 8), lane = threadIdx.x & 63;
     if constexpr (WAVES == 1) {
         p.lanes = nv >= 64 ? 64 : nv <= 1 ? 1 : 1 << (32 - __builtin_clz(nv - 1));
-        const int lane = threadIdx.x & 63;
         p.first = lane & (p.lanes - 1);
-        p.at_once = 64 / p.lanes;
-        p.row = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * p.at_once * rows + lane / p.lanes;
+        p.at_once = 4 * (64 / p.lanes);
+        p.row = (threadIdx.x >> 6) * (64 / p.lanes) + lane / p.lanes;
     } else {
         p.lanes = 64;
         p.first = threadIdx.x;
         p.at_once = 1;
-        p.row = (int64_t)blockIdx.x * rows;
+        p.row = 0;
     }
+    const int64_t from = blockIdx.x * rows * p.at_once;
+    p.row += from;
+    p.end = from + rows * p.at_once < n ? from + rows * p.at_once : n;
     return p;
 }
 
-template <bool BF16, int WAVES, int CH>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_kernel(NormArgs p) {
-    __shared__ float lds[WAVES];
-    const Place at = place_of<WAVES>(p.d, p.rows);
-    const float inv = 1.0f / (float)p.d;
+template <bool BF16, bool EVEN, int POL, int WAVES, int CH, int R>
+__global__ __launch_bounds__(threads_of(WAVES)) void norm_kernel(NormArgs p) {
+    __shared__ float lds[2][R][WAVES];
+    int turn = 0;
+    const Place at = place_of<WAVES>(p.n, p.d, p.rows);
     DropKey key{};
     if (p.drop.limit) key = drop_key(p.drop);
     float w[CH][8], b[CH][8];
@@ -134,66 +193,115 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_kernel(Nor
         load_floats(w[c], p.w, col, left[c], 1.0f);
         load_floats(b[c], p.b, col, left[c], 0.0f);
     }
-    for (int64_t k = 0; k < p.rows; ++k) {
-        const int64_t row = at.row + at.at_once * k;
-        const bool in = row < p.n;             // (uniform where barriers follow: a row is the workgroup's)
-        if (WAVES > 1 && !in) return;
-        float s[CH][8], sum = 0.0f;
+    // (as many turns for every thread of the workgroup: barriers lie in them)
+    for (int64_t base = at.row - at.row % at.at_once; base < at.end; base += R * at.at_once) {
+        const int64_t row0 = base + at.row % at.at_once;
+        Octet<BF16, EVEN, POL> x[R][CH], res[R][CH];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int64_t col = 8 * ((int64_t)at.first + 64 * WAVES * c), i = row * p.d + col;
-            const int n = in ? left[c] : 0;
-            Octet<BF16> x;
-            x.load(p.x, i, n);
-            x.values(s[c]);
-            if (p.drop.limit) drop_octet(s[c], key, (uint32_t)(col / 8), (uint32_t)row);
-            if (p.residual) {
-                Octet<BF16> r;
-                float v[8];
-                r.load(p.residual, i, n);
-                r.values(v);
+        for (int r = 0; r < R; ++r) {
+            const int64_t row = row0 + r * at.at_once;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) s[c][e] += v[e];
+            for (int c = 0; c < CH; ++c) {
+                const int64_t i = row * p.d + 8 * ((int64_t)at.first + 64 * WAVES * c);
+                const int n = row < at.end ? left[c] : 0;
+                x[r][c].load(p.x, i, n, p.d >= 8);
+                if (p.residual) res[r][c].load(p.residual, i, n, p.d >= 8);
             }
-            if (p.s) {
-                Octet<BF16> o;
-                o.set(s[c]);
-                o.store(p.s, i, n);
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum += s[c][e];
         }
-        // (divided, not times 1 / d: a mean that a float holds comes out as it)
-        const float mean = row_sum<WAVES>(sum, at.lanes, lds) / (float)p.d;
-        sum = 0.0f;
+        float s[R][CH][8], sum[R];
 #pragma unroll
-        for (int c = 0; c < CH; ++c)
+        for (int r = 0; r < R; ++r) {
+            const int64_t row = row0 + r * at.at_once;
+            sum[r] = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                s[c][e] = e < left[c] ? s[c][e] - mean : 0.0f;
-                sum = __builtin_fmaf(s[c][e], s[c][e], sum);
+            for (int c = 0; c < CH; ++c) {
+                const int64_t col = 8 * ((int64_t)at.first + 64 * WAVES * c);
+                const int n = row < at.end ? left[c] : 0;
+                x[r][c].settle(n, p.d >= 8);
+                x[r][c].values(s[r][c]);
+                if (p.drop.limit) drop_octet(s[r][c], key, (uint32_t)(col / 8), (uint32_t)row);
+                if (p.residual) {
+                    float v[8];
+                    res[r][c].settle(n, p.d >= 8);
+                    res[r][c].values(v);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[r][c][e] += v[e];
+                }
+                if (p.s) {
+                    Octet<BF16, EVEN, POL> o;
+                    o.set(s[r][c]);
+                    o.store(p.s, row * p.d + col, n);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[r] += s[r][c][e];
             }
-        const float rstd = 1.0f / __builtin_sqrtf(row_sum<WAVES>(sum, at.lanes, lds) * inv + p.eps);
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int64_t i = row * p.d + 8 * ((int64_t)at.first + 64 * WAVES * c);
-            Octet<BF16> o;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s[c][e] = __builtin_fmaf(s[c][e] * rstd, w[c][e], b[c][e]);
-            o.set(s[c]);
-            o.store(p.y, i, in ? left[c] : 0);
         }
-        if (p.stats && in && at.first == 0) {
-            p.stats[2 * row] = mean;
-            p.stats[2 * row + 1] = rstd;
+        row_sums<WAVES, R>(sum, at.lanes, lds, turn);
+        float mean[R], rstd[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            // (divided, not times 1 / d: a mean that a float holds comes out as it)
+            mean[r] = sum[r] / (float)p.d;
+            sum[r] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    s[r][c][e] = e < left[c] ? s[r][c][e] - mean[r] : 0.0f;
+                    sum[r] = __builtin_fmaf(s[r][c][e], s[r][c][e], sum[r]);
+                }
+        }
+        row_sums<WAVES, R>(sum, at.lanes, lds, turn);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int64_t row = row0 + r * at.at_once;
+            rstd[r] = 1.0f / __builtin_sqrtf(sum[r] / (float)p.d + p.eps);
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                Octet<BF16, EVEN, POL> o;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[r][c][e] = __builtin_fmaf(s[r][c][e] * rstd[r], w[c][e], b[c][e]);
+                o.set(s[r][c]);
+                o.store(p.y, row * p.d + 8 * ((int64_t)at.first + 64 * WAVES * c), row < at.end ? left[c] : 0);
+            }
+            if (p.stats && row < at.end && at.first == 0) {
+                p.stats[2 * row] = mean[r];
+                p.stats[2 * row + 1] = rstd[r];
+            }
         }
     }
 }
 
-template <bool BF16, int WAVES, int CH>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_bwd_kernel(NormBwdArgs p) {
-    __shared__ float lds[WAVES];
-    const Place at = place_of<WAVES>(p.d, p.rows);
+// What the gradient reads of a lane's place in a row
+template <bool BF16, bool EVEN, int POL, int WAVES, int CH>
+struct RowIn {
+    Octet<BF16, EVEN, POL> x[CH], res[CH], gy[CH], gs[CH];
+    float mean, rstd;
+    __device__ __forceinline__ void load(const NormBwdArgs& p, const Place& at, int64_t row, const int (&left)[CH]) {
+        const bool in = row < at.end;
+        mean = in ? p.stats[2 * row] : 0.0f;
+        rstd = in ? p.stats[2 * row + 1] : 0.0f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int64_t i = row * p.d + 8 * ((int64_t)at.first + 64 * WAVES * c);
+            const int n = in ? left[c] : 0;
+            x[c].load(p.x, i, n, p.d >= 8);
+            if (p.residual) res[c].load(p.residual, i, n, p.d >= 8);
+            gy[c].load(p.gy, i, n, p.d >= 8);
+            if (p.gs) gs[c].load(p.gs, i, n, p.d >= 8);
+        }
+    }
+};
+
+template <bool BF16, bool EVEN, int POL, int WAVES, int CH>
+__global__ __launch_bounds__(threads_of(WAVES)) void norm_bwd_kernel(NormBwdArgs p) {
+    __shared__ float lds[2][2][WAVES];
+    int turn = 0;
+    if (p.hdr && blockIdx.x == 0 && threadIdx.x == 0) {
+        p.hdr->timeout = kEmpty32;
+        p.hdr->sig = p.sig;
+    }
+    const Place at = place_of<WAVES>(p.n, p.d, p.rows);
     const float inv = 1.0f / (float)p.d;
     DropKey key{};
     if (p.drop.limit) key = drop_key(p.drop);
@@ -207,73 +315,84 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_bwd_kernel
 #pragma unroll
         for (int e = 0; e < 8; ++e) dw[c][e] = db[c][e] = 0.0f;
     }
-    for (int64_t k = 0; k < p.rows; ++k) {
-        const int64_t row = at.row + at.at_once * k;
-        const bool in = row < p.n;
-        if (WAVES > 1 && !in) break;
-        const float mean = in ? p.stats[2 * row] : 0.0f, rstd = in ? p.stats[2 * row + 1] : 0.0f;
-        float xh[CH][8], gy[CH][8], c1 = 0.0f, c2 = 0.0f;
+    // (as many turns for every thread of the workgroup: barriers lie in them)
+    const int64_t mine = at.row % at.at_once;
+    for (int64_t base = at.row - mine; base < at.end; base += at.at_once) {
+        const int64_t row = base + mine;
+        RowIn<BF16, EVEN, POL, WAVES, CH> now;
+        now.load(p, at, row, left);
+        float xh[CH][8], gw[CH][8], sums[2] = {0.0f, 0.0f};
+        uint32_t stays[CH];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int64_t col = 8 * ((int64_t)at.first + 64 * WAVES * c), i = row * p.d + col;
-            const int n = in ? left[c] : 0;
-            Octet<BF16> x, g;
-            x.load(p.x, i, n);
-            g.load(p.gy, i, n);
-            x.values(xh[c]);
-            g.values(gy[c]);
-            if (p.drop.limit) drop_octet(xh[c], key, (uint32_t)(col / 8), (uint32_t)row);
+            const int64_t col = 8 * ((int64_t)at.first + 64 * WAVES * c);
+            const int n = row < at.end ? left[c] : 0;
+            now.x[c].settle(n, p.d >= 8);
+            now.gy[c].settle(n, p.d >= 8);
+            now.x[c].values(xh[c]);
+            now.gy[c].values(gw[c]);
+            if (p.drop.limit) {
+                stays[c] = 0u;
+                each_kept(key, (uint32_t)(col / 8), (uint32_t)row, [&](int e, bool on) {
+                    xh[c][e] = on ? xh[c][e] * key.scale : 0.0f;
+                    stays[c] |= on ? 1u << e : 0u;
+                });
+            }
             if (p.residual) {
-                Octet<BF16> r;
                 float v[8];
-                r.load(p.residual, i, n);
-                r.values(v);
+                now.res[c].settle(n, p.d >= 8);
+                now.res[c].values(v);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) xh[c][e] += v[e];
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                xh[c][e] = e < n ? (xh[c][e] - mean) * rstd : 0.0f;
-                dw[c][e] = __builtin_fmaf(gy[c][e], xh[c][e], dw[c][e]);
-                db[c][e] += gy[c][e];
-                gy[c][e] *= w[c][e];
-                c1 += gy[c][e];
-                c2 = __builtin_fmaf(gy[c][e], xh[c][e], c2);
+                const float g = gw[c][e], h = e < n ? (xh[c][e] - now.mean) * now.rstd : 0.0f;
+                xh[c][e] = h;
+                dw[c][e] = __builtin_fmaf(g, h, dw[c][e]);
+                db[c][e] += g;
+                gw[c][e] = g * w[c][e];
+                sums[0] += gw[c][e];
+                sums[1] = __builtin_fmaf(gw[c][e], h, sums[1]);
             }
         }
-        c1 = row_sum<WAVES>(c1, at.lanes, lds) * inv;
-        c2 = row_sum<WAVES>(c2, at.lanes, lds) * inv;
+        row_sums<WAVES, 2>(sums, at.lanes, lds, turn);
+        const float c1 = sums[0] * inv, c2 = sums[1] * inv;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int64_t col = 8 * ((int64_t)at.first + 64 * WAVES * c), i = row * p.d + col;
-            const int n = in ? left[c] : 0;
+            const int64_t i = row * p.d + 8 * ((int64_t)at.first + 64 * WAVES * c);
+            const int n = row < at.end ? left[c] : 0;
             float ds[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ds[e] = rstd * (gy[c][e] - c1 - xh[c][e] * c2);
+            for (int e = 0; e < 8; ++e) ds[e] = now.rstd * (gw[c][e] - c1 - xh[c][e] * c2);
             if (p.gs) {
-                Octet<BF16> g;
                 float v[8];
-                g.load(p.gs, i, n);
-                g.values(v);
+                now.gs[c].settle(n, p.d >= 8);
+                now.gs[c].values(v);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) ds[e] += v[e];
             }
-            Octet<BF16> o;
+            Octet<BF16, EVEN, POL> o;
             if (p.dres) {
                 o.set(ds);
                 o.store(p.dres, i, n);
             }
-            if (p.dx) {
-                if (p.drop.limit) drop_octet(ds, key, (uint32_t)(col / 8), (uint32_t)row);
-                o.set(ds);
-                o.store(p.dx, i, n);
+            if (p.drop.limit) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ds[e] = stays[c] >> e & 1u ? ds[e] * key.scale : 0.0f;
             }
+            o.set(ds);
+            o.store(p.dx, i, n);
         }
     }
     if (!p.part) return;
-    // the sums of a workgroup's wavefronts, then of the rows that one holds side by side
     if constexpr (WAVES == 1) {
-        for (int m = at.lanes; m < 64; m <<= 1) {
+        // the rows side by side in a wavefront, then the workgroup's four wavefronts
+        __shared__ float sum[3][2][CH * 512];
+        const int wave = threadIdx.x >> 6;
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            if (m < at.lanes) continue;
 #pragma unroll
             for (int c = 0; c < CH; ++c)
 #pragma unroll
@@ -282,55 +401,87 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_bwd_kernel
                     db[c][e] += lanes_xor(db[c][e], m);
                 }
         }
+        const bool mine = (int)(threadIdx.x & 63) < at.lanes;
+        if (wave > 0 && mine) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    sum[wave - 1][0][(c * 8 + e) * 64 + at.first] = dw[c][e];
+                    sum[wave - 1][1][(c * 8 + e) * 64 + at.first] = db[c][e];
+                }
+        }
+        barrier_lds();
+        if (wave > 0 || !mine) return;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int v = 0; v < 3; ++v) {
+                    dw[c][e] += sum[v][0][(c * 8 + e) * 64 + at.first];
+                    db[c][e] += sum[v][1][(c * 8 + e) * 64 + at.first];
+                }
     }
-    const int64_t group = WAVES == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
-    if (WAVES == 1 && (int)(threadIdx.x & 63) >= at.lanes) return;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int64_t col = 8 * ((int64_t)at.first + 64 * WAVES * c);
+        float* const o = p.part + 2 * (int64_t)blockIdx.x * p.d + col;
+        if (left[c] >= 8) {
+            __builtin_memcpy(o, dw[c], sizeof dw[c]);
+            __builtin_memcpy(o + p.d, db[c], sizeof db[c]);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < left[c]) {
-                p.part[(2 * group) * p.d + col + e] = dw[c][e];
-                p.part[(2 * group + 1) * p.d + col + e] = db[c][e];
-            }
+            for (int e = 0; e < 8; ++e)
+                if (e < left[c]) {
+                    o[e] = dw[c][e];
+                    o[p.d + e] = db[c][e];
+                }
+        }
     }
 }
 
-// dw (blockIdx.y 0) and db (1) from the groups' sums, in doubles: 64 columns, 16 rows at a time
+// dw (blockIdx.y 0) and db (1) from the groups' sums, in doubles: 32 columns, 32 rows at a
+// time
 __global__ __launch_bounds__(1024) void norm_weights_kernel(const float* part, float* dw, float* db, int64_t groups,
                                                             int64_t d) {
-    __shared__ double s[16][64];
+    __shared__ double s[32][32];
     float* const out = blockIdx.y ? db : dw;
     if (!out) return;
-    const int col = threadIdx.x & 63, row = threadIdx.x >> 6;
-    const int64_t f = (int64_t)blockIdx.x * 64 + col;
+    const int col = threadIdx.x & 31, row = threadIdx.x >> 5;
+    const int64_t f = (int64_t)blockIdx.x * 32 + col;
     double sum = 0.0;
-    if (f < d)
-        for (int64_t r = row; r < groups; r += 16) sum += (double)part[(2 * r + blockIdx.y) * d + f];
+    if (f < d) {
+#pragma unroll 8
+        for (int64_t r = row; r < groups; r += 32) sum += (double)part[(2 * r + blockIdx.y) * d + f];
+    }
     s[row][col] = sum;
     __syncthreads();
     if (row == 0 && f < d) {
-        for (int r = 1; r < 16; ++r) sum += s[r][col];
+        for (int r = 1; r < 32; ++r) sum += s[r][col];
         out[f] = (float)sum;
     }
 }
 
-template <bool BF16>
+template <bool BF16, bool EVEN, int POL>
 __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs p) {
-    const int64_t nv = (p.d + 7) / 8, idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint32_t nv = (uint32_t)((p.d + 7) / 8);
+    const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (idx >= p.n * nv) return;
-    const int64_t row = idx / nv, block = idx - row * nv, i = row * p.d + 8 * block;
-    const int left = p.d - 8 * block >= 8 ? 8 : (int)(p.d - 8 * block);
-    Octet<BF16> x;
+    // (idx and nv are below 2^31)
+    const uint32_t row = (uint32_t)idx / nv, block = (uint32_t)idx - row * nv;
+    const int64_t i = (int64_t)row * p.d + 8 * (int64_t)block;
+    const int left = p.d - 8 * (int64_t)block >= 8 ? 8 : (int)(p.d - 8 * (int64_t)block);
+    Octet<BF16, EVEN, POL> x, r;
     float v[8];
-    x.load(p.x, i, left);
+    x.load(p.x, i, left, p.d >= 8);
+    if (p.residual) r.load(p.residual, i, left, p.d >= 8);
+    x.settle(left, p.d >= 8);
     x.values(v);
-    if (p.drop.limit) drop_octet(v, drop_key(p.drop), (uint32_t)block, (uint32_t)row);
+    if (p.drop.limit) drop_octet(v, drop_key(p.drop), block, row);
     if (p.residual) {
-        Octet<BF16> r;
         float u[8];
-        r.load(p.residual, i, left);
+        r.settle(left, p.d >= 8);
         r.values(u);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += u[e];
@@ -339,82 +490,127 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs p) {
     x.store(p.out, i, left);
 }
 
-// wavefronts of a row and octets of a lane
+// Wavefronts of a row, octets of a lane, rows of a workgroup at once.  A lane with one
+// octet needs few registers, and workgroups of up to four wavefronts wait for one
+// another the least; the longest rows take two octets.  (32768 x 2048 bf16, residual and
+// dropout, with four octets a lane and a wavefront a row: 220 and 625 us.)
 struct Shape {
     int waves, ch;
-    int64_t at_once;    // rows of a workgroup at once
+    int64_t at_once;
 };
-Shape shape_of(int64_t d) {
+Shape shape_of(int64_t d, bool grad) {
     const int64_t nv = (d + 7) / 8;
     int64_t lanes = 1;
     while (lanes < nv && lanes < 64) lanes *= 2;
     if (nv <= 64) return {1, 1, 4 * (64 / lanes)};
-    if (nv <= 128) return {1, 2, 4};
-    if (nv <= 256) return {1, 4, 4};
-    if (nv <= 512) return {4, 2, 1};
-    if (nv <= 1024) return {4, 4, 1};
+    for (int waves = 2; waves <= (grad ? 16 : 8); waves *= 2)
+        if (nv <= 64 * waves) return {waves, 1, 1};
+    // (16 wavefronts of a row leave no room for another workgroup: 114 us where 8 take 97 at d = 8192)
+    if (!grad && nv <= 1024) return {8, 2, 1};
     return {16, 2, 1};
 }
 
-template <bool BF16, class F>
-hipError_t with_shape(const Shape& sh, F&& f) {
-    if (sh.waves == 1 && sh.ch == 1) f(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{});
-    else if (sh.waves == 1 && sh.ch == 2) f(std::integral_constant<int, 1>{}, std::integral_constant<int, 2>{});
-    else if (sh.waves == 1) f(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
-    else if (sh.waves == 4 && sh.ch == 2) f(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
-    else if (sh.waves == 4) f(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});
-    else f(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
-    return hipGetLastError();
+template <int W, int C>
+struct ShapeOf {
+    static constexpr int waves = W, ch = C;
+};
+template <class F>
+void with_shape(const Shape& sh, F&& f) {
+    if (sh.ch == 2) {
+        if (sh.waves == 8) f(ShapeOf<8, 2>{});
+        else f(ShapeOf<16, 2>{});
+    } else {
+        switch (sh.waves) {
+            case 1: f(ShapeOf<1, 1>{}); break;
+            case 2: f(ShapeOf<2, 1>{}); break;
+            case 4: f(ShapeOf<4, 1>{}); break;
+            case 8: f(ShapeOf<8, 1>{}); break;
+            default: f(ShapeOf<16, 1>{}); break;
+        }
+    }
 }
 
-int64_t rows_of(int64_t n, const Shape& sh, int64_t most) {
-    const int64_t steps = (n + sh.at_once - 1) / sh.at_once;   // workgroups with a row each
-    int64_t rows = steps / 1024;
-    if (rows > most) rows = most > steps / (1 << 20) ? most : steps / (1 << 20);   // (a grid has its limits)
+// The kinds of rows, and how they go through the caches (CachePolicy, kernels.hpp).  In
+// bf16 a lane's octet is one access and a wavefront's whole lines: outputs go past the
+// caches, inputs where the tensor is larger than they would be found in later (dropout with a
+// residual, 32768 x 2048: 69.2 -> 64.9 us, the norm 107 -> 97, its gradient 166 -> 162).  In fp32 an
+// octet is two accesses of every other 16 bytes, which that slows (71 -> 73, 110 -> 117 us); rows
+// that are not whole octets share lines, so their outputs stay in the caches.
+// With one tensor in and one out neither pays (dropout alone 46.4 -> 49.2 us).
+template <class F>
+void with_rows(bool bf16, bool few, int64_t n, int64_t d, F&& f) {
+    const bool even = d % 8 == 0, large = (double)n * (double)d * 2 > (double)kCachedTensorBytes;
+    using std::integral_constant;
+    if (!bf16) even ? f(std::false_type{}, std::true_type{}, integral_constant<int, kCached>{})
+                    : f(std::false_type{}, std::false_type{}, integral_constant<int, kCached>{});
+    else if (!even) f(std::true_type{}, std::false_type{}, integral_constant<int, kStreamAll>{});
+    else if (few) f(std::true_type{}, std::true_type{}, integral_constant<int, kCached>{});
+    else if (large) f(std::true_type{}, std::true_type{}, integral_constant<int, kStreamAll>{});
+    else f(std::true_type{}, std::true_type{}, integral_constant<int, kStreamOut>{});
+}
+
+// Rows that a lane sees one after the other, so that about `groups` workgroups of four
+// wavefronts, and never a few more, take all: at most 64, which is as many floats as a sum for the
+// weights adds before it goes on in doubles.
+int64_t rows_of(int64_t n, const Shape& sh, int64_t groups) {
+    const int64_t steps = (n + sh.at_once - 1) / sh.at_once;   // workgroups with a row a lane
+    if (sh.waves > 4) groups = groups * 4 / sh.waves;
+    int64_t rows = (steps + groups - 1) / groups;
+    if (rows > 64) rows = 64 > steps / (1 << 20) ? 64 : steps / (1 << 20);       // (a grid has its limits)
     return rows < 1 ? 1 : rows;
 }
+int64_t groups_of(int64_t n, const Shape& sh, int64_t rows) { return (n + sh.at_once * rows - 1) / (sh.at_once * rows); }
 
-template <bool BF16>
-hipError_t norm_launch_t(NormArgs a, hipStream_t s) {
-    const Shape sh = shape_of(a.d);
-    a.rows = rows_of(a.n, sh, 16);
-    const dim3 grid((unsigned)((a.n + sh.at_once * a.rows - 1) / (sh.at_once * a.rows)));
-    return with_shape<BF16>(sh, [&](auto waves, auto ch) {
-        hipLaunchKernelGGL((norm_kernel<BF16, waves.value, ch.value>), grid, dim3(block_of<waves.value>()), 0, s, a);
-    });
-}
-template <bool BF16>
-hipError_t norm_bwd_launch_t(NormBwdArgs a, hipStream_t s) {
-    const Shape sh = shape_of(a.d);
-    const dim3 grid((unsigned)((a.n + sh.at_once * a.rows - 1) / (sh.at_once * a.rows)));
-    const hipError_t e = with_shape<BF16>(sh, [&](auto waves, auto ch) {
-        hipLaunchKernelGGL((norm_bwd_kernel<BF16, waves.value, ch.value>), grid, dim3(block_of<waves.value>()), 0, s, a);
-    });
-    if (e != hipSuccess || !a.part) return e;
-    hipLaunchKernelGGL(norm_weights_kernel, dim3((unsigned)((a.d + 63) / 64), 2), dim3(1024), 0, s, a.part, a.dw, a.db,
-                       a.groups, a.d);
-    return hipGetLastError();
+// The gradient's rows: 1024 workgroups at most run at once, with a row's loads on the way.
+// With a residual (and two more tensors to read) half of them do, and leave half as
+// many sums (32768 x 2048 bf16: 178 -> 166 us; without a residual 92, and 104 with 512); wide rows, whose
+// wavefronts wait for one another, need all (d = 4096: 160 and 183 us).
+int64_t bwd_groups(const Shape& sh, int64_t d, bool residual) {
+    return sh.waves <= 4 && d % 8 == 0 && (residual || sh.waves == 1) ? 512 : 1024;
 }
 
 }  // namespace
 
-int64_t norm_groups(int64_t n, int64_t d, int64_t* rows) {
-    const Shape sh = shape_of(d);
-    *rows = rows_of(n, sh, 64);
-    const int64_t blocks = (n + sh.at_once * *rows - 1) / (sh.at_once * *rows);
-    return sh.waves == 1 ? 4 * blocks : blocks;
+int64_t norm_groups(int64_t n, int64_t d, bool residual, int64_t* rows) {
+    const Shape sh = shape_of(d, true);
+    *rows = rows_of(n, sh, bwd_groups(sh, d, residual));
+    return groups_of(n, sh, *rows);
 }
 
 hipError_t norm_launch(bool bf16, NormArgs a, hipStream_t s) {
-    return bf16 ? norm_launch_t<true>(a, s) : norm_launch_t<false>(a, s);
+    const Shape sh = shape_of(a.d, false);
+    // (many more workgroups than run at once: those that end make room; 2048 of them 115 us
+    // where 8192 take 97)
+    a.rows = rows_of(a.n, sh, 8192);
+    with_rows(bf16, !a.residual, a.n, a.d, [&](auto b, auto even, auto pol) {
+        with_shape(sh, [&](auto t) {
+            using T = decltype(t);
+            hipLaunchKernelGGL((norm_kernel<b.value, even.value, pol.value, T::waves, T::ch, T::ch == 1 ? 2 : 1>),
+                               dim3((unsigned)groups_of(a.n, sh, a.rows)), dim3(threads_of(T::waves)), 0, s, a);
+        });
+    });
+    return hipGetLastError();
 }
-hipError_t norm_bwd_launch(bool bf16, NormBwdArgs a, hipStream_t s) {
-    return bf16 ? norm_bwd_launch_t<true>(a, s) : norm_bwd_launch_t<false>(a, s);
+hipError_t norm_bwd_launch(bool bf16, const NormBwdArgs& a, hipStream_t s) {
+    const Shape sh = shape_of(a.d, true);
+    with_rows(bf16, false, a.n, a.d, [&](auto b, auto even, auto pol) {
+        with_shape(sh, [&](auto t) {
+            using T = decltype(t);
+            if constexpr (T::waves != 8 || T::ch == 1)
+                hipLaunchKernelGGL((norm_bwd_kernel<b.value, even.value, pol.value, T::waves, T::ch>), dim3((unsigned)a.groups),
+                                   dim3(threads_of(T::waves)), 0, s, a);
+        });
+    });
+    if (!a.part) return hipGetLastError();
+    hipLaunchKernelGGL(norm_weights_kernel, dim3((unsigned)((a.d + 31) / 32), 2), dim3(1024), 0, s, a.part, a.dw, a.db,
+                       a.groups, a.d);
+    return hipGetLastError();
 }
 hipError_t dropout_launch(bool bf16, const DropoutArgs& a, hipStream_t s) {
-    const dim3 grid((unsigned)((a.n * ((a.d + 7) / 8) + 255) / 256));
-    if (bf16) hipLaunchKernelGGL(dropout_kernel<true>, grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(dropout_kernel<false>, grid, dim3(256), 0, s, a);
+    with_rows(bf16, !a.residual, a.n, a.d, [&](auto b, auto even, auto pol) {
+        hipLaunchKernelGGL((dropout_kernel<b.value, even.value, pol.value>),
+                           dim3((unsigned)((a.n * ((a.d + 7) / 8) + 255) / 256)), dim3(256), 0, s, a);
+    });
     return hipGetLastError();
 }
 

@@ -49,8 +49,9 @@ __device__ __forceinline__ DropKey drop_key(const DropArgs& a) {
     return k;
 }
 
-// v[e] -> scale v[e] where element e of the octet (column / 8 = block) stays, else 0
-__device__ __forceinline__ void drop_octet(float (&v)[8], const DropKey& k, uint32_t block, uint32_t row) {
+// For each element e of the octet (column / 8 = block): stays(e, whether it stays)
+template <class F>
+__device__ __forceinline__ void each_kept(const DropKey& k, uint32_t block, uint32_t row, F stays) {
     uint32_t c[4] = {block, row, k.step, k.site};
     philox_block(c, k.k0, k.k1);
     bool tie = false;
@@ -71,9 +72,12 @@ __device__ __forceinline__ void drop_octet(float (&v)[8], const DropKey& k, uint
     for (int e = 0; e < 8; ++e) {
         const uint32_t u = e & 1 ? c[e >> 1] >> 16 : c[e >> 1] & 0xFFFFu;
         const uint32_t x = e & 1 ? l[e >> 1] >> 16 : l[e >> 1] & 0xFFFFu;
-        const bool stays = u > k.hi || (u == k.hi && x >= k.lo);
-        v[e] = stays ? v[e] * k.scale : 0.0f;
+        stays(e, u > k.hi || (u == k.hi && x >= k.lo));
     }
+}
+// v[e] -> scale v[e] where element e stays, else 0
+__device__ __forceinline__ void drop_octet(float (&v)[8], const DropKey& k, uint32_t block, uint32_t row) {
+    each_kept(k, block, row, [&](int e, bool stays) { v[e] = stays ? v[e] * k.scale : 0.0f; });
 }
 
 }  // namespace memoroid
