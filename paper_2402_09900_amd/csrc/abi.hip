@@ -1688,7 +1688,8 @@ int memoroid_gated_step(const void* x, const void* gates, const float* alpha, co
     a.h = h;
     a.B = B;
     a.d = d;
-    return check_hip(gated_step_launch(dtype == MEMOROID_BF16, a, (hipStream_t)stream));
+    const bool full = gated_full(d, dtype, GateShape{4, 1, 256, 1}, {x, gates, h}) && aligned(state, 16) && aligned(alpha, 16);
+    return check_hip(gated_step_launch(dtype == MEMOROID_BF16, full, a, (hipStream_t)stream));
 }
 
 // ---------------------------------------------------- layer norm and dropout

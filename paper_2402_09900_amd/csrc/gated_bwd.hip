@@ -30,7 +30,6 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs 
     // it in the place of the one), the c that enters it
     __shared__ float sU[kRuns][kGateCols], sK[kRuns][kGateCols], sH[kRuns][kGateCols], sC[kRuns][kGateCols];
     __shared__ float sIn[kRuns][kGateCols];
-    __shared__ float sCarry[kGateCols];
     __shared__ LookBackLds sLook;
     __shared__ uint32_t sF[kRuns];
 
@@ -160,17 +159,27 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs 
     held = (uint32_t)__ballot(held != 0u && lane < kRuns);
     const bool in = fb * kGateCols + lane < p.d;
     const int64_t f = fb * kGateCols + lane;
-    float tc = 0.0f;                                                 // wavefront 1: the tile's
-    Decay<false> whole_tile;
-    whole_tile.k = 0.0f;
     auto apply = [&](int n, float v, float add) {
         Decay<false> d;
         d.k = sK[n][lane];
         const float next = d.of(v, add);
         return held >> n & 1u ? add : next;
     };
+    // (wavefronts 0 and 1: the tile's own effect, as forward)
+    float tc = 0.0f;
+    Decay<false> all;
+    if (wave < 2 && p.tiles.nt > 1) {
+        float u = 0.0f;
+#pragma unroll
+        for (int n = kRuns - 1; n >= 0; --n) {
+            tc = apply(n, tc, sC[n][lane]);
+            u += sU[n][lane];
+        }
+        all = Decay<false>(u);
+    }
+    const float first = wave < 2 && at.tile == 0 && p.grad_state && in ? p.grad_state[b * p.d + f] : 0.0f;
     auto enter = [&](float v) {
-        sCarry[lane] = v;
+        if (at.tile > 0 && in && !held) put_incl(p.tiles, slot, lane, all.of(v, tc));
 #pragma unroll
         for (int n = kRuns - 1; n >= 0; --n) {
             sIn[n][lane] = v;
@@ -178,25 +187,15 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs 
         }
     };
     if (wave == 0) {
-        float v = at.tile == 0 && p.grad_state && in ? p.grad_state[b * p.d + f] : 0.0f;
+        float v = first;
         const bool there = at.tile == 0 || try_near(p.tiles, at.tile, at.chain, lane, in, v);
         if (there) enter(v);
         if (lane == 0) sLook.done = there;
     } else if (wave == 1) {
-        if (p.tiles.nt > 1) {
-            float u = 0.0f;
-#pragma unroll
-            for (int n = kRuns - 1; n >= 0; --n) {
-                tc = apply(n, tc, sC[n][lane]);
-                u += sU[n][lane];
-            }
-            whole_tile = Decay<false>(u);
-            const float first = at.tile == 0 && p.grad_state && in ? p.grad_state[b * p.d + f] : 0.0f;
-            if (in) {
-                if (held) put_incl(p.tiles, slot, lane, tc);
-                else if (at.tile == 0) put_incl(p.tiles, slot, lane, whole_tile.of(first, tc));
-                else put_agg(p.tiles, slot, lane, whole_tile.k, tc);
-            }
+        if (p.tiles.nt > 1 && in) {
+            if (held) put_incl(p.tiles, slot, lane, tc);
+            else if (at.tile == 0) put_incl(p.tiles, slot, lane, all.of(first, tc));
+            else put_agg(p.tiles, slot, lane, all.k, tc);
         }
     } else if (wave == 2) {
         const int64_t ns = (p.T + kGateStateSteps - 1) / kGateStateSteps;
@@ -212,8 +211,6 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs 
     if (!sLook.done) look_far<THREADS>(p.tiles, at.tile, at.chain, lane, in, sLook, enter);
 
     // ---- the state that enters the run goes into z; then back with c
-    if (wave == 1 && p.tiles.nt > 1 && at.tile > 0 && !held && in)
-        put_incl(p.tiles, slot, lane, whole_tile.of(sCarry[lane], tc));
     float sum[F] = {};
 #pragma unroll
     for (int e = 0; e < F; ++e) {
@@ -286,19 +283,21 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs 
     }
 }
 
-// dalpha from the rows of partial sums: 64 features and 16 rows at a time
+// dalpha from the rows of partial sums, in doubles: 32 features, 32 rows at a time
 __global__ __launch_bounds__(1024) void gated_alpha_kernel(const float* part, const float* alpha, float* dalpha,
                                                            int64_t rows, int64_t d) {
-    __shared__ double s[16][64];
-    const int col = threadIdx.x & 63, row = threadIdx.x >> 6;
-    const int64_t f = (int64_t)blockIdx.x * 64 + col;
+    __shared__ double s[32][32];
+    const int col = threadIdx.x & 31, row = threadIdx.x >> 5;
+    const int64_t f = (int64_t)blockIdx.x * 32 + col;
     double sum = 0.0;
-    if (f < d)
-        for (int64_t r = row; r < rows; r += 16) sum += (double)part[r * d + f];
+    if (f < d) {
+#pragma unroll 8
+        for (int64_t r = row; r < rows; r += 32) sum += (double)part[r * d + f];
+    }
     s[row][col] = sum;
     __syncthreads();
     if (row == 0 && f < d) {
-        for (int r = 1; r < 16; ++r) sum += s[r][col];
+        for (int r = 1; r < 32; ++r) sum += s[r][col];
         const float a = alpha[f];
         dalpha[f] = a > 0.0f ? (float)sum : a < 0.0f ? (float)-sum : 0.0f;
     }
@@ -324,7 +323,7 @@ void with_policy(bool full, int policy, const GatedBwdArgs& a, hipStream_t s) {
 hipError_t gated_bwd_launch(bool bf16, bool full, int policy, const GatedBwdArgs& a, hipStream_t s) {
     bf16 ? with_policy<true>(full, policy, a, s) : with_policy<false>(full, policy, a, s);
     if (!a.part) return hipGetLastError();
-    hipLaunchKernelGGL(gated_alpha_kernel, dim3((unsigned)((a.d + 63) / 64)), dim3(1024), 0, s, a.part, a.alpha, a.dalpha,
+    hipLaunchKernelGGL(gated_alpha_kernel, dim3((unsigned)((a.d + 31) / 32)), dim3(1024), 0, s, a.part, a.alpha, a.dalpha,
                        a.part_rows, a.d);
     return hipGetLastError();
 }

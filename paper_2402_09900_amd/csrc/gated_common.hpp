@@ -228,7 +228,10 @@ struct LookBackLds {
 };
 
 __device__ __forceinline__ bool try_near(const GatedTiles& t, int64_t tile, int chain, int f, bool need, float& v) {
-    constexpr int W = 4;
+#ifndef GW
+#define GW 4
+#endif
+    constexpr int W = GW;
     const int64_t stride = (int64_t)t.nchains * kGateCols, from = ((tile - 1) * t.nchains + chain) * kGateCols + f;
     v = 0.0f;
     bool done = !need;

@@ -24,7 +24,6 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_fwd_kernel(GatedFwdArgs 
     __shared__ uint32_t s_tile;
     // per run: its rates' sum, its decay, what it adds, the state that enters it
     __shared__ float sU[kRuns][kGateCols], sK[kRuns][kGateCols], sH[kRuns][kGateCols], sIn[kRuns][kGateCols];
-    __shared__ float sCarry[kGateCols];
     __shared__ LookBackLds sLook;
     __shared__ uint32_t sF[kRuns], sBegins;
 
@@ -139,18 +138,29 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_fwd_kernel(GatedFwdArgs 
     if (lane < kRuns) held = sF[lane];
     held = (uint32_t)__ballot(held != 0u && lane < kRuns);
     const bool in = fb * kGateCols + lane < p.d;
-    float th = 0.0f;                                                 // wavefront 1: the tile's
-    Decay<false> whole_tile;
-    whole_tile.k = 0.0f;
     auto apply = [&](int n, float v) {
         Decay<false> d;
         d.k = sK[n][lane];
         const float add = sH[n][lane], next = d.of(v, add);
         return held >> n & 1u ? add : next;
     };
+    // the tile's own effect: wavefront 1 publishes it, the first needs it to publish the state
+    // after the tile the moment it has the one before
+    float th = 0.0f;
+    Decay<false> all;
+    if (wave < 2 && p.tiles.nt > 1) {
+        float u = 0.0f;
+#pragma unroll
+        for (int n = 0; n < kRuns; ++n) {
+            th = apply(n, th);
+            u += sU[n][lane];
+        }
+        all = Decay<false>(u);
+    }
+    const float first = wave < 2 && at.tile == 0 && p.state_in && in ? p.state_in[b * p.d + fb * kGateCols + lane] : 0.0f;
     const bool need = in && !sBegins;                                // a tile that begins an episode takes nothing
     auto enter = [&](float v) {
-        sCarry[lane] = v;
+        if (at.tile > 0 && in && !held) put_incl(p.tiles, slot, lane, all.of(v, th));
 #pragma unroll
         for (int n = 0; n < kRuns; ++n) {
             sIn[n][lane] = v;
@@ -158,33 +168,21 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_fwd_kernel(GatedFwdArgs 
         }
     };
     if (wave == 0) {
-        float v = at.tile == 0 && p.state_in && in ? p.state_in[b * p.d + fb * kGateCols + lane] : 0.0f;
+        float v = first;
         if (at.tile == 0 && p.states && in)
             p.states[b * ((p.T + kGateStateSteps - 1) / kGateStateSteps) * p.d + fb * kGateCols + lane] = v;
         const bool there = at.tile == 0 || try_near(p.tiles, at.tile, at.chain, lane, need, v);
         if (there) enter(v);
         if (lane == 0) sLook.done = there;
-    } else if (wave == 1 && p.tiles.nt > 1) {
-        float u = 0.0f;
-#pragma unroll
-        for (int n = 0; n < kRuns; ++n) {
-            th = apply(n, th);
-            u += sU[n][lane];
-        }
-        whole_tile = Decay<false>(u);
-        const float first = at.tile == 0 && p.state_in && in ? p.state_in[b * p.d + fb * kGateCols + lane] : 0.0f;
-        if (in) {
-            if (held) put_incl(p.tiles, slot, lane, th);
-            else if (at.tile == 0) put_incl(p.tiles, slot, lane, whole_tile.of(first, th));
-            else put_agg(p.tiles, slot, lane, whole_tile.k, th);
-        }
+    } else if (wave == 1 && p.tiles.nt > 1 && in) {
+        if (held) put_incl(p.tiles, slot, lane, th);
+        else if (at.tile == 0) put_incl(p.tiles, slot, lane, all.of(first, th));
+        else put_agg(p.tiles, slot, lane, all.k, th);
     }
     barrier_lds();
     if (!sLook.done) look_far<THREADS>(p.tiles, at.tile, at.chain, lane, need, sLook, enter);
 
     // ---- (5)
-    if (wave == 1 && p.tiles.nt > 1 && at.tile > 0 && !held && in)
-        put_incl(p.tiles, slot, lane, whole_tile.of(sCarry[lane], th));
 #pragma unroll
     for (int e = 0; e < F; ++e) h[e] = sIn[run][F * q + e];
     const Rsrc rs_h = make_rsrc((char*)p.h + tape0 * line, rows * line);

@@ -501,7 +501,8 @@ struct GatedStepArgs {
 // full: d and every address are multiples of a lane's features; policy: a CachePolicy
 hipError_t gated_fwd_launch(bool bf16, bool full, int policy, const GatedFwdArgs& a, hipStream_t s);
 hipError_t gated_bwd_launch(bool bf16, bool full, int policy, const GatedBwdArgs& a, hipStream_t s);
-hipError_t gated_step_launch(bool bf16, const GatedStepArgs& a, hipStream_t s);
+// full: d and addresses are multiples of four elements
+hipError_t gated_step_launch(bool bf16, bool full, const GatedStepArgs& a, hipStream_t s);
 
 // ------------------------------------------------- layer norm and dropout
 // (norm.hip)
