@@ -1548,11 +1548,11 @@ GatedTiles gated_tiles(const GatedPlan& p, void* workspace, uint64_t sig) {
 int64_t gated_tile(int dtype, bool grad) {
     return (grad ? gate_bwd_shape(dtype == MEMOROID_BF16) : gate_fwd_shape(dtype == MEMOROID_BF16)).tile();
 }
-// whether rows and addresses are whole vectors of a lane's features
-bool gated_full(int64_t d, int dtype, const GateShape& sh, std::initializer_list<const void*> ps) {
-    if (d % sh.f != 0) return false;
+// whether rows and addresses are multiples of f elements
+bool gated_full(int64_t d, int dtype, int f, std::initializer_list<const void*> ps) {
+    if (d % f != 0) return false;
     for (const void* x : ps)
-        if (!aligned(x, (size_t)(sh.f * elem_bytes(dtype)))) return false;
+        if (!aligned(x, (size_t)(f * elem_bytes(dtype)))) return false;
     return true;
 }
 
@@ -1616,7 +1616,7 @@ int memoroid_scan_gated(const void* x, const void* gates, const float* alpha, co
     a.tiles = gated_tiles(p, workspace, layout_sig({kSigGated, B, T, d, dtype}));
     hipStream_t s = (hipStream_t)stream;
     if (p.init && ws_init_launch(nullptr, 0, workspace, p.init, s) != hipSuccess) return MEMOROID_EHIP;
-    return check_hip(gated_fwd_launch(dtype == MEMOROID_BF16, gated_full(d, dtype, gate_fwd_shape(dtype == MEMOROID_BF16), {x, gates, h}),
+    return check_hip(gated_fwd_launch(dtype == MEMOROID_BF16, gated_full(d, dtype, 2, {x, gates, h}),
                                       gated_policy(B, T, d, dtype), a, s));
 }
 
@@ -1664,8 +1664,7 @@ int memoroid_scan_gated_bwd(const void* x, const void* gates, const float* alpha
     a.tiles = gated_tiles(p, workspace, layout_sig({kSigGatedBwd, B, T, d, dtype}));
     hipStream_t s = (hipStream_t)stream;
     if (p.init && ws_init_launch(nullptr, 0, workspace, p.init, s) != hipSuccess) return MEMOROID_EHIP;
-    return check_hip(gated_bwd_launch(dtype == MEMOROID_BF16, gated_full(d, dtype, gate_bwd_shape(dtype == MEMOROID_BF16),
-                                                                         {x, gates, grad_h, grad_x, grad_gates}),
+    return check_hip(gated_bwd_launch(dtype == MEMOROID_BF16, gated_full(d, dtype, 2, {x, gates, grad_h, grad_x, grad_gates}),
                                       gated_policy(B, T, d, dtype), a, s));
 }
 
@@ -1688,7 +1687,7 @@ int memoroid_gated_step(const void* x, const void* gates, const float* alpha, co
     a.h = h;
     a.B = B;
     a.d = d;
-    const bool full = gated_full(d, dtype, GateShape{4, 1, 256, 1}, {x, gates, h}) && aligned(state, 16) && aligned(alpha, 16);
+    const bool full = gated_full(d, dtype, 4, {x, gates, h}) && aligned(state, 16) && aligned(alpha, 16);
     return check_hip(gated_step_launch(dtype == MEMOROID_BF16, full, a, (hipStream_t)stream));
 }
 

@@ -19,10 +19,10 @@ namespace memoroid {
 
 namespace {
 
-template <bool BF16, bool FULL, int POL, int F, int L, int THREADS, int WAVES>
+template <bool BF16, bool FULL, int POL, int L, int THREADS, int WAVES>
 __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs p) {
     constexpr int kLd = POL == kStreamAll ? kNt : 0, kSt = POL != kCached ? kNt : 0;
-    constexpr int kRow = Lanes<F, THREADS>::kRow, kRuns = Lanes<F, THREADS>::kRuns, kSteps = kRuns * L;
+    constexpr int F = 2, kRow = Lanes<F, THREADS>::kRow, kRuns = Lanes<F, THREADS>::kRuns, kSteps = kRuns * L;
     static_assert(kSteps % kGateStateSteps == 0, "a tile starts from a state that was kept");
     static_assert(L <= kRow && L < 32, "flags: a lane per step");
     __shared__ uint32_t s_tile;
@@ -41,36 +41,36 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs 
     const int64_t row0 = tile * kSteps, rows = p.T - row0, tape0 = b * p.T + row0;
     const int64_t f0 = fb * kGateCols + F * q;
     const int left = p.d - f0 >= F ? F : p.d > f0 ? (int)(p.d - f0) : 0;
-    constexpr int S = Few<BF16, F>::SIZE, W = Few<BF16, F>::WORDS;
+    constexpr int S = Few<BF16>::SIZE, W = Few<BF16>::WORDS;
     const int64_t line = p.d * S;
 
     const Rsrc rs_st = make_rsrc(p.start + tape0, rows);
     const uint32_t flag = q < L ? bload_u8(rs_st, (uint32_t)(run * L + q)) : 0u;
-    const Rsrc rs_x = make_rsrc((const char*)p.x + tape0 * line, rows * line);
-    const Rsrc rs_h = make_rsrc((const char*)p.g + tape0 * line, rows * line);
-    const Rsrc rs_g = make_rsrc((const char*)p.gates + 2 * tape0 * line, 2 * rows * line);
+    const Rows rs_x = rows_at((const char*)p.x + tape0 * line, rows * line);
+    const Rows rs_h = rows_at((const char*)p.g + tape0 * line, rows * line);
+    const Rows rs_g = rows_at((const char*)p.gates + 2 * tape0 * line, 2 * rows * line);
     const uint32_t off = left ? (uint32_t)(run * L * line + f0 * S) : kOob;
     const uint32_t goff = left ? (uint32_t)(2 * run * L * line + f0 * S) : kOob;
     const uint32_t step = (uint32_t)line;
     // (a whole tile's rows by scalar offsets, the last tile's by the lanes': gated_fwd.hip)
-    const bool whole = rows >= kSteps;
-    Few<BF16, F> x[L], r[L], i[L], g[L];
+    const bool whole = rows >= kSteps, wide = p.d > 1;
+    Few<BF16> x[L], r[L], i[L], g[L];
     if (whole) {
 #pragma unroll
         for (int s = 0; s < L; ++s) {
-            r[s].template load<kLd, FULL>(rs_g, goff, 2 * s * step, left);
-            i[s].template load<kLd, FULL>(rs_g, goff, (2 * s + 1) * step, left);
-            x[s].template load<kLd, FULL>(rs_x, off, s * step, left);
-            g[s].template load<kLd, FULL>(rs_h, off, s * step, left);
+            r[s].template load<kLd, FULL>(rs_g, goff, 2 * s * step, left, true, wide);
+            i[s].template load<kLd, FULL>(rs_g, goff, (2 * s + 1) * step, left, true, wide);
+            x[s].template load<kLd, FULL>(rs_x, off, s * step, left, true, wide);
+            g[s].template load<kLd, FULL>(rs_h, off, s * step, left, true, wide);
         }
     } else {
         const uint32_t by = left ? step : 0u;
 #pragma unroll
         for (int s = 0; s < L; ++s) {
-            r[s].template load<kLd, FULL>(rs_g, goff + 2 * s * by, 0, left);
-            i[s].template load<kLd, FULL>(rs_g, goff + (2 * s + 1) * by, 0, left);
-            x[s].template load<kLd, FULL>(rs_x, off + s * by, 0, left);
-            g[s].template load<kLd, FULL>(rs_h, off + s * by, 0, left);
+            r[s].template load<kLd, FULL>(rs_g, goff + 2 * s * by, 0, left, run * L + s < rows, wide);
+            i[s].template load<kLd, FULL>(rs_g, goff + (2 * s + 1) * by, 0, left, run * L + s < rows, wide);
+            x[s].template load<kLd, FULL>(rs_x, off + s * by, 0, left, run * L + s < rows, wide);
+            g[s].template load<kLd, FULL>(rs_h, off + s * by, 0, left, run * L + s < rows, wide);
         }
     }
     float rate[F], most = 0.0f;
@@ -107,6 +107,10 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs 
             i[s].opaque();
             x[s].opaque();
             g[s].opaque();
+            r[s].template settle<FULL>(left, wide);
+            i[s].template settle<FULL>(left, wide);
+            x[s].template settle<FULL>(left, wide);
+            g[s].template settle<FULL>(left, wide);
 #pragma unroll
             for (int e = 0; e < F; ++e) {
                 const float gr = sigmoid<BF16>(r[s].get(e)), gi = sigmoid<BF16>(i[s].get(e)), gu = rate[e] * gr;
@@ -217,8 +221,8 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs 
         h[e] = sH[run][F * q + e];
         c[e] = sIn[run][F * q + e];
     }
-    const Rsrc rs_dx = make_rsrc((char*)p.dx + tape0 * line, rows * line);
-    const Rsrc rs_dg = make_rsrc((char*)p.dgates + 2 * tape0 * line, 2 * rows * line);
+    const Rows rs_dx = rows_at((char*)p.dx + tape0 * line, rows * line);
+    const Rows rs_dg = rows_at((char*)p.dgates + 2 * tape0 * line, 2 * rows * line);
     auto back = [&](auto SLOW, auto BEGINS) {
         // (h: what is left of the entering state before each step)
 #pragma unroll
@@ -248,14 +252,15 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs 
                 const float next = d.of(lam);
                 c[e] = BEGINS.value && (begins >> s & 1u) ? 0.0f : next;
             }
-            Few<BF16, F> o;
+            Few<BF16> o;
             const uint32_t by = whole || !left ? 0u : step, sby = whole ? step : 0u;
+            const bool in_tape = whole || run * L + s < rows;
             o.set(dx);
-            o.template store<kSt, FULL>(rs_dx, off + s * by, s * sby, left);
+            o.template store<kSt, FULL>(rs_dx, off + s * by, s * sby, left, in_tape);
             o.set(dr);
-            o.template store<kSt, FULL>(rs_dg, goff + 2 * s * by, 2 * s * sby, left);
+            o.template store<kSt, FULL>(rs_dg, goff + 2 * s * by, 2 * s * sby, left, in_tape);
             o.set(di);
-            o.template store<kSt, FULL>(rs_dg, goff + (2 * s + 1) * by, (2 * s + 1) * sby, left);
+            o.template store<kSt, FULL>(rs_dg, goff + (2 * s + 1) * by, (2 * s + 1) * sby, left, in_tape);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -306,7 +311,7 @@ __global__ __launch_bounds__(1024) void gated_alpha_kernel(const float* part, co
 template <bool BF16, bool FULL, int POL>
 void launch(const GatedBwdArgs& a, hipStream_t s) {
     constexpr GateShape sh = gate_bwd_shape(BF16);
-    hipLaunchKernelGGL((gated_bwd_kernel<BF16, FULL, POL, sh.f, sh.steps, sh.threads, sh.waves>),
+    hipLaunchKernelGGL((gated_bwd_kernel<BF16, FULL, POL, sh.steps, sh.threads, sh.waves>),
                        dim3((unsigned)(a.tiles.nt * a.tiles.nchains)), dim3(sh.threads), 0, s, a);
 }
 // (rows that lanes cannot take whole are not whole lines either)

@@ -107,60 +107,72 @@ struct Lanes {
     static_assert(kRow <= 64 && kRuns <= 32, "a run lies in a wavefront, the runs' flags in a word");
 };
 
-// F features as they lie in memory.  FULL: rows and addresses are multiples of F
-// elements, and one access moves them.
-template <bool BF16, int F>
+// Rows of a tile in memory: the resource with the range check, and the bare address
+struct Rows {
+    Rsrc r;
+    char* p;
+};
+__device__ __forceinline__ Rows rows_at(const void* p, int64_t bytes) { return {make_rsrc(p, bytes), (char*)p}; }
+
+// 4 bytes at an address that is a multiple of 2
+typedef uint32_t Word2 __attribute__((aligned(2)));
+
+// Two features as they lie in memory.  FULL: rows and addresses are multiples of two
+// elements, accesses go through the resource.  Otherwise rows start at any element: in bf16
+// one access at that alignment, which the hardware takes; the last feature of an odd row comes
+// with the one before it and is moved down by settle(), when nobody waits for it any more.
+template <bool BF16>
 struct Few {
-    static constexpr int SIZE = BF16 ? 2 : 4, WORDS = F * SIZE / 4;
+    static constexpr int SIZE = BF16 ? 2 : 4, WORDS = BF16 ? 1 : 2;
     uint32_t w[WORDS];
-    // soff: a scalar offset, which the range check does not cover
+    // off, soff: bytes from the tile's first row, a lane's and a scalar part, the latter not
+    // covered by the range check; in: the row is one of the tape's; wide: rows of more than one
     template <int AUX, bool FULL>
-    __device__ __forceinline__ void load(Rsrc r, uint32_t off, uint32_t soff, int left) {
-        if constexpr (FULL) {
-            if constexpr (WORDS == 1) {
-                w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, (int)off, (int)soff, AUX);
-            } else if constexpr (WORDS == 2) {
-                const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(r, (int)off, (int)soff, AUX);
-                w[0] = v.x;
-                w[1] = v.y;
-            } else {
-                const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, (int)soff, AUX);
-                w[0] = v.x;
-                w[1] = v.y;
-                w[2] = v.z;
-                w[3] = v.w;
-            }
+    __device__ __forceinline__ void load(const Rows& m, uint32_t off, uint32_t soff, int left, bool in, bool wide) {
+        if constexpr (FULL && BF16) {
+            w[0] = __builtin_amdgcn_raw_buffer_load_b32(m.r, (int)off, (int)soff, AUX);
+        } else if constexpr (FULL) {
+            const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(m.r, (int)off, (int)soff, AUX);
+            w[0] = v.x;
+            w[1] = v.y;
         } else {
-            uint32_t v[F];
 #pragma unroll
-            for (int e = 0; e < F; ++e) {
-                const int at = e < left ? (int)(off + e * SIZE) : (int)kOob;
-                if constexpr (BF16) v[e] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(r, at, (int)soff, AUX);
-                else v[e] = __builtin_amdgcn_raw_buffer_load_b32(r, at, (int)soff, AUX);
+            for (int e = 0; e < WORDS; ++e) w[e] = 0u;
+            if (!in || left <= 0) return;
+            const char* const at = m.p + soff;
+            if constexpr (BF16) {
+                if (wide) w[0] = *(const Word2*)(at + (off - (left == 1 ? SIZE : 0)));
+                else w[0] = *(const uint16_t*)(at + off);
+            } else {
+                // (8 bytes in one access at a multiple of 4 are slower: 156 -> 183 us, 8 x 4096 x 1023)
+                w[0] = *(const uint32_t*)(at + off);
+                if (left > 1) w[1] = *(const uint32_t*)(at + (off + SIZE));
             }
-#pragma unroll
-            for (int e = 0; e < WORDS; ++e) w[e] = BF16 ? v[2 * e] | v[2 * e + 1] << 16 : v[e];
         }
     }
+    template <bool FULL>
+    __device__ __forceinline__ void settle(int left, bool wide) {
+        if constexpr (!FULL && BF16) w[0] = left == 1 && wide ? w[0] >> 16 : w[0];
+    }
     template <int AUX, bool FULL>
-    __device__ __forceinline__ void store(Rsrc r, uint32_t off, uint32_t soff, int left) const {
-        if constexpr (FULL) {
-            if constexpr (WORDS == 1) {
-                __builtin_amdgcn_raw_buffer_store_b32(w[0], r, (int)off, (int)soff, AUX);
-            } else if constexpr (WORDS == 2) {
-                const u32x2 v = {w[0], w[1]};
-                __builtin_amdgcn_raw_buffer_store_b64(v, r, (int)off, (int)soff, AUX);
-            } else {
-                const u32x4 v = {w[0], w[1], w[2], w[3]};
-                __builtin_amdgcn_raw_buffer_store_b128(v, r, (int)off, (int)soff, AUX);
-            }
+    __device__ __forceinline__ void store(const Rows& m, uint32_t off, uint32_t soff, int left, bool in) const {
+        if constexpr (FULL && BF16) {
+            __builtin_amdgcn_raw_buffer_store_b32(w[0], m.r, (int)off, (int)soff, AUX);
+        } else if constexpr (FULL) {
+            const u32x2 v = {w[0], w[1]};
+            __builtin_amdgcn_raw_buffer_store_b64(v, m.r, (int)off, (int)soff, AUX);
         } else {
-#pragma unroll
-            for (int e = 0; e < F; ++e) {
-                const int at = e < left ? (int)(off + e * SIZE) : (int)kOob;
-                if constexpr (BF16)
-                    __builtin_amdgcn_raw_buffer_store_b16((unsigned short)(w[e / 2] >> (e & 1 ? 16 : 0)), r, at, (int)soff, AUX);
-                else __builtin_amdgcn_raw_buffer_store_b32(w[e], r, at, (int)soff, AUX);
+            if (!in || left <= 0) return;
+            char* const at = m.p + soff;
+            if (left == 1) {
+                if constexpr (BF16) *(uint16_t*)(at + off) = (uint16_t)w[0];
+                else *(uint32_t*)(at + off) = w[0];
+            } else {
+                if constexpr (BF16) *(Word2*)(at + off) = w[0];
+                else {
+                    *(uint32_t*)(at + off) = w[0];
+                    *(uint32_t*)(at + (off + SIZE)) = w[1];
+                }
             }
         }
     }
@@ -168,7 +180,7 @@ struct Few {
         if constexpr (BF16) return e & 1 ? bf16_hi(w[e / 2]) : bf16_lo(w[e / 2]);
         else return __uint_as_float(w[e]);
     }
-    __device__ __forceinline__ void set(const float (&v)[F]) {
+    __device__ __forceinline__ void set(const float (&v)[2]) {
 #pragma unroll
         for (int e = 0; e < WORDS; ++e) w[e] = BF16 ? f32x2_to_bf16x2(v[2 * e], v[2 * e + 1]) : __float_as_uint(v[e]);
     }
@@ -186,10 +198,13 @@ struct TileOf {
     int chain;
 };
 __device__ __forceinline__ TileOf take_tile(const GatedTiles& t, uint32_t* shared) {
-    const uint32_t nch = (uint32_t)t.nchains;
+    // Every chain once per nchains workgroups.  Neighbouring chains run side by side on one
+    // accelerator die (workgroup g on die g mod kXcds), whose cache then serves the lines that
+    // both have a part of, and no chain stays on one die.
+    const uint32_t nch = (uint32_t)t.nchains, i = blockIdx.x % nch, turn = blockIdx.x / nch, each = nch / kXcds, rest = nch % kXcds;
+    const uint32_t die = rest ? i % kXcds : (i + turn) % kXcds;
     TileOf r;
-    // every chain once per nchains workgroups, rotated so that none stays on one XCD
-    r.chain = (int)((blockIdx.x % nch + blockIdx.x / nch) % nch);
+    r.chain = (int)(die * each + (die < rest ? die : rest) + i / kXcds);
     r.tile = 0;
     if (t.nt > 1) {
         if (threadIdx.x == 0)

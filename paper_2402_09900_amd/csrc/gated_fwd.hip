@@ -16,10 +16,10 @@ namespace memoroid {
 
 namespace {
 
-template <bool BF16, bool FULL, int POL, int F, int L, int THREADS, int WAVES>
+template <bool BF16, bool FULL, int POL, int L, int THREADS, int WAVES>
 __global__ __launch_bounds__(THREADS, WAVES) void gated_fwd_kernel(GatedFwdArgs p) {
     constexpr int kLd = POL == kStreamAll ? kNt : 0, kSt = POL != kCached ? kNt : 0;
-    constexpr int kRow = Lanes<F, THREADS>::kRow, kRuns = Lanes<F, THREADS>::kRuns, kSteps = kRuns * L;
+    constexpr int F = 2, kRow = Lanes<F, THREADS>::kRow, kRuns = Lanes<F, THREADS>::kRuns, kSteps = kRuns * L;
     static_assert(L <= kRow && L < 32 && kGateStateSteps % L == 0, "flags: a lane per step; states lie between runs");
     __shared__ uint32_t s_tile;
     // per run: its rates' sum, its decay, what it adds, the state that enters it
@@ -34,35 +34,35 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_fwd_kernel(GatedFwdArgs 
     const int64_t row0 = at.tile * kSteps, rows = p.T - row0, tape0 = b * p.T + row0;
     const int64_t f0 = fb * kGateCols + F * q;
     const int left = p.d - f0 >= F ? F : p.d > f0 ? (int)(p.d - f0) : 0;
-    constexpr int S = Few<BF16, F>::SIZE;
+    constexpr int S = Few<BF16>::SIZE;
     const int64_t line = p.d * S;                                    // bytes of a row of x
 
     // ---- (1)
     const Rsrc rs_st = make_rsrc(p.start + tape0, rows);
     const uint32_t flag = q < L ? bload_u8(rs_st, (uint32_t)(run * L + q)) : 0u;
-    const Rsrc rs_x = make_rsrc((const char*)p.x + tape0 * line, rows * line);
-    const Rsrc rs_g = make_rsrc((const char*)p.gates + 2 * tape0 * line, 2 * rows * line);
+    const Rows rs_x = rows_at((const char*)p.x + tape0 * line, rows * line);
+    const Rows rs_g = rows_at((const char*)p.gates + 2 * tape0 * line, 2 * rows * line);
     const uint32_t off = left ? (uint32_t)(run * L * line + f0 * S) : kOob;
     const uint32_t goff = left ? (uint32_t)(2 * run * L * line + f0 * S) : kOob;
     const uint32_t step = (uint32_t)line;
     // A whole tile's rows are reached by scalar offsets; those of the tape's last tile by
     // the lanes', which the range check covers (lanes past d stay outside either way)
-    const bool whole = rows >= kSteps;
-    Few<BF16, F> x[L], r[L], i[L];
+    const bool whole = rows >= kSteps, wide = p.d > 1;
+    Few<BF16> x[L], r[L], i[L];
     if (whole) {
 #pragma unroll
         for (int s = 0; s < L; ++s) {
-            r[s].template load<kLd, FULL>(rs_g, goff, 2 * s * step, left);
-            i[s].template load<kLd, FULL>(rs_g, goff, (2 * s + 1) * step, left);
-            x[s].template load<kLd, FULL>(rs_x, off, s * step, left);
+            r[s].template load<kLd, FULL>(rs_g, goff, 2 * s * step, left, true, wide);
+            i[s].template load<kLd, FULL>(rs_g, goff, (2 * s + 1) * step, left, true, wide);
+            x[s].template load<kLd, FULL>(rs_x, off, s * step, left, true, wide);
         }
     } else {
         const uint32_t by = left ? step : 0u;
 #pragma unroll
         for (int s = 0; s < L; ++s) {
-            r[s].template load<kLd, FULL>(rs_g, goff + 2 * s * by, 0, left);
-            i[s].template load<kLd, FULL>(rs_g, goff + (2 * s + 1) * by, 0, left);
-            x[s].template load<kLd, FULL>(rs_x, off + s * by, 0, left);
+            r[s].template load<kLd, FULL>(rs_g, goff + 2 * s * by, 0, left, run * L + s < rows, wide);
+            i[s].template load<kLd, FULL>(rs_g, goff + (2 * s + 1) * by, 0, left, run * L + s < rows, wide);
+            x[s].template load<kLd, FULL>(rs_x, off + s * by, 0, left, run * L + s < rows, wide);
         }
     }
     float rate[F], most = 0.0f;
@@ -86,6 +86,9 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_fwd_kernel(GatedFwdArgs 
             r[s].opaque();
             i[s].opaque();
             x[s].opaque();
+            r[s].template settle<FULL>(left, wide);
+            i[s].template settle<FULL>(left, wide);
+            x[s].template settle<FULL>(left, wide);
 #pragma unroll
             for (int e = 0; e < F; ++e) {
                 const Gate<BF16, SLOW.value> g(r[s].get(e), i[s].get(e), rate[e]);
@@ -185,22 +188,22 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_fwd_kernel(GatedFwdArgs 
     // ---- (5)
 #pragma unroll
     for (int e = 0; e < F; ++e) h[e] = sIn[run][F * q + e];
-    const Rsrc rs_h = make_rsrc((char*)p.h + tape0 * line, rows * line);
+    const Rows rs_h = rows_at((char*)p.h + tape0 * line, rows * line);
     float from[F];
 #pragma unroll
     for (int e = 0; e < F; ++e) from[e] = h[e];
     if (whole) {
         run_through([&](int s) {
-            Few<BF16, F> o;
+            Few<BF16> o;
             o.set(h);
-            o.template store<kSt, FULL>(rs_h, off, s * step, left);
+            o.template store<kSt, FULL>(rs_h, off, s * step, left, true);
         });
     } else {
         const uint32_t by = left ? step : 0u;
         through(No{}, Yes{}, [&](int s) {
-            Few<BF16, F> o;
+            Few<BF16> o;
             o.set(h);
-            o.template store<kSt, FULL>(rs_h, off + s * by, 0, left);
+            o.template store<kSt, FULL>(rs_h, off + s * by, 0, left, run * L + s < rows);
         });
     }
     const int64_t last = rows - 1 - (int64_t)run * L;                // the tape's last step, seen from this run
@@ -231,7 +234,7 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_fwd_kernel(GatedFwdArgs 
 template <bool BF16, bool FULL, int POL>
 void launch(const GatedFwdArgs& a, hipStream_t s) {
     constexpr GateShape sh = gate_fwd_shape(BF16);
-    hipLaunchKernelGGL((gated_fwd_kernel<BF16, FULL, POL, sh.f, sh.steps, sh.threads, sh.waves>),
+    hipLaunchKernelGGL((gated_fwd_kernel<BF16, FULL, POL, sh.steps, sh.threads, sh.waves>),
                        dim3((unsigned)(a.tiles.nt * a.tiles.nchains)), dim3(sh.threads), 0, s, a);
 }
 // (rows that lanes cannot take whole are not whole lines either)

@@ -440,14 +440,14 @@ hipError_t rotate_weights_launch(const RotateArgs& a, float* dwq, float* dwk, hi
 // (gated_fwd.hip, gated_bwd.hip, gated_step.hip).  The state before every kGateStateSteps-th step is kept for the gradient.
 constexpr int kGateStateSteps = 64;
 constexpr int kGateCols = 64;        // features of a chain
-// Features and steps of a lane, threads of a workgroup, wavefronts of a SIMD that its
+// Steps of a lane (of two features), threads of a workgroup, wavefronts of a SIMD that its
 // registers are to allow
 struct GateShape {
-    int f, steps, threads, waves;
-    constexpr int tile() const { return threads * f / kGateCols * steps; }   // steps
+    int steps, threads, waves;
+    constexpr int tile() const { return threads * 2 / kGateCols * steps; }   // steps
 };
-constexpr GateShape gate_fwd_shape(bool bf16) { return bf16 ? GateShape{2, 16, 256, 4} : GateShape{2, 8, 256, 4}; }
-constexpr GateShape gate_bwd_shape(bool bf16) { return bf16 ? GateShape{2, 8, 256, 3} : GateShape{2, 8, 256, 2}; }
+constexpr GateShape gate_fwd_shape(bool bf16) { return bf16 ? GateShape{16, 256, 4} : GateShape{8, 256, 4}; }
+constexpr GateShape gate_bwd_shape(bool bf16) { return bf16 ? GateShape{8, 256, 3} : GateShape{8, 256, 2}; }
 
 // Tiles of the scans and the words they hand on (gated_common.hpp)
 struct GatedTiles {
@@ -498,7 +498,7 @@ struct GatedStepArgs {
     void* h;                    // [B][d]
     int64_t B, d;
 };
-// full: d and every address are multiples of a lane's features; policy: a CachePolicy
+// full: d and every address are multiples of two elements; policy: a CachePolicy
 hipError_t gated_fwd_launch(bool bf16, bool full, int policy, const GatedFwdArgs& a, hipStream_t s);
 hipError_t gated_bwd_launch(bool bf16, bool full, int policy, const GatedBwdArgs& a, hipStream_t s);
 // full: d and addresses are multiples of four elements
