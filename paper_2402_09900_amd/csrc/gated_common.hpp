@@ -243,15 +243,13 @@ struct LookBackLds {
 };
 
 __device__ __forceinline__ bool try_near(const GatedTiles& t, int64_t tile, int chain, int f, bool need, float& v) {
-#ifndef GW
-#define GW 4
-#endif
-    constexpr int W = GW;
-    const int64_t stride = (int64_t)t.nchains * kGateCols, from = ((tile - 1) * t.nchains + chain) * kGateCols + f;
+    constexpr int W = 4;
+    // (the words' addresses: scalars, and the lane's 32 bits)
+    const int64_t stride = (int64_t)t.nchains * kGateCols, from = ((tile - 1) * t.nchains + chain) * kGateCols;
     v = 0.0f;
     bool done = !need;
     if (need) {
-        const uint32_t w = peek32(t.incl + from);
+        const uint32_t w = peek32(t.incl + from + f);
         v = __uint_as_float(w);
         done = w != kEmpty32;
     }
@@ -265,8 +263,8 @@ __device__ __forceinline__ bool try_near(const GatedTiles& t, int64_t tile, int 
             in[k] = kEmpty32;
             ag[k] = kEmpty64;
             if (k < tile) {
-                in[k] = peek32(t.incl + (from - k * stride));
-                ag[k] = peek64(t.agg + (from - k * stride));
+                in[k] = peek32(t.incl + (from - k * stride) + f);
+                ag[k] = peek64(t.agg + (from - k * stride) + f);
             }
         }
         int at = W;
@@ -292,8 +290,8 @@ template <int THREADS, class Use>
 __device__ __forceinline__ void look_far(const GatedTiles& t, int64_t tile, int chain, int f, bool need, LookBackLds& lds,
                                          Use use) {
     constexpr int kEach = kNear / (THREADS / 64);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t stride = (int64_t)t.nchains * kGateCols, from = ((tile - 1) * t.nchains + chain) * kGateCols + f;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int64_t stride = (int64_t)t.nchains * kGateCols, from = ((tile - 1) * t.nchains + chain) * kGateCols;
     for (uint32_t polls = 0;; ++polls) {
 #pragma unroll
         for (int n0 = 0; n0 < kEach; n0 += 4) {                      // (four at a time: few registers beside a tile's)
@@ -305,8 +303,8 @@ __device__ __forceinline__ void look_far(const GatedTiles& t, int64_t tile, int 
                 in[k] = kEmpty32;
                 ag[k] = kEmpty64;
                 if (n < tile && need) {
-                    in[k] = peek32(t.incl + (from - n * stride));
-                    ag[k] = peek64(t.agg + (from - n * stride));
+                    in[k] = peek32(t.incl + (from - n * stride) + f);
+                    ag[k] = peek64(t.agg + (from - n * stride) + f);
                 }
             }
 #pragma unroll
