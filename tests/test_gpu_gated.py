@@ -121,6 +121,52 @@ def test_rates(dtype, rates):
     check(dtype, 2, 600, 64, "some", True, 5, rates)
 
 
+def test_nothing_to_do():
+    """No tapes, no steps, no features: a carried state and its gradient pass through."""
+    announce("gated empty")
+    for B, T, d in ((0, 5, 8), (2, 0, 8), (2, 5, 0), (0, 0, 0)):
+        x, gates = torch.zeros(B, T, d, device=DEV, requires_grad=True), torch.zeros(B, T, 2, d, device=DEV, requires_grad=True)
+        alpha, start = torch.ones(d, device=DEV, requires_grad=True), torch.zeros(B, T, dtype=torch.uint8, device=DEV)
+        state = torch.randn(B, d, device=DEV).requires_grad_(True)
+        h, last = mb.gated_scan(x, gates, alpha, start, state, final_state=True)
+        assert h.shape == (B, T, d) and torch.equal(last, state)
+        up = torch.randn(B, d, device=DEV)
+        dx, dg, da, ds = torch.autograd.grad((h, last), (x, gates, alpha, state), (torch.zeros_like(h), up))
+        assert dx.shape == x.shape and dg.shape == gates.shape and not bool(da.any()) and torch.equal(ds, up)
+        if T == 0:
+            assert not bool(mb.gated_scan(x, gates, alpha, start, final_state=True)[1].any())
+    assert mb.gated_step(torch.zeros(0, 8, device=DEV), torch.zeros(0, 2, 8, device=DEV), torch.ones(8, device=DEV),
+                         torch.zeros(0, 8, device=DEV)).shape == (0, 8)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,T,d", [(1, 3, 1 << 18), (1, 70, (1 << 18) - 1), (6000, 70, 2), (1, 20000, 3)])
+def test_wide_and_many(dtype, B, T, d):
+    """The widest rows, many tapes, many tiles of one chain."""
+    check(dtype, B, T, d, seed=T)
+
+
+@pytest.mark.parametrize("need", [(0,), (1,), (2,), (3,), (0, 3)])
+def test_some_gradients(need):
+    """Whichever inputs want a gradient, it is the one that all of them get; outputs that
+    nothing hangs on count as zero."""
+    announce("gated need=%s" % (need,))
+    s = {k: v.to(DEV) for k, v in inputs("f32", 2, 300, 64, "some", seed=3).items()}
+    names = ("x", "gates", "alpha", "state")
+
+    def run(need, grad_h, grad_state):
+        leaves = [s[k].detach().requires_grad_(j in need) for j, k in enumerate(names)]
+        h, last = mb.gated_scan(*leaves[:3], s["start"], leaves[3], final_state=True)
+        outs, ups = zip(*[(o, g) for o, g in ((h, grad_h), (last, grad_state)) if g is not None])
+        return dict(zip(need, torch.autograd.grad(outs, [leaves[j] for j in need], ups)))
+
+    zh, zs = torch.zeros_like(s["grad_h"]), torch.zeros_like(s["grad_state"])
+    for gh, gs in ((s["grad_h"], s["grad_state"]), (s["grad_h"], None), (None, s["grad_state"])):
+        whole = run((0, 1, 2, 3), zh if gh is None else gh, zs if gs is None else gs)
+        for j, g in run(need, gh, gs).items():
+            assert torch.equal(g, whole[j])
+
+
 @pytest.mark.parametrize("T", [600, 1300])
 def test_one_begin_anywhere(T):
     """A begin step at each place of its own tape, around the edges of lanes and tiles."""

@@ -153,6 +153,32 @@ def test_equal_and_bad_rows():
     assert (~torch.isfinite(dx).all(-1)).nonzero().flatten().tolist() == [2, 4]
 
 
+def test_all_dropped():
+    """p = 1: the norm is that of the residual, x takes part in nothing and gets no gradient."""
+    announce("norm p=1")
+    for d in (64, 1500):
+        x = torch.full((9, d), float("nan"), device=DEV, requires_grad=True)
+        res, w = torch.randn(9, d, device=DEV).requires_grad_(True), torch.rand(d, device=DEV)
+        gy, gs = torch.randn(9, d, device=DEV), torch.randn(9, d, device=DEV)
+        y, s = mb.layer_norm(x, w, residual=res, p=1.0, rng=rng_tensor())
+        dx, dres = torch.autograd.grad((y, s), (x, res), (gy, gs))
+        assert torch.equal(s, res) and not bool(dx.any()) and torch.equal(y, mb.norm_rows(res.detach(), w))
+        zero = torch.zeros(9, d, device=DEV).requires_grad_(True)
+        y, s = mb.layer_norm(zero, w, residual=res, p=0.0)
+        assert torch.equal(dres, torch.autograd.grad((y, s), res, (gy, gs))[0])
+
+
+def test_overflow():
+    """Rows whose squared deviations are past fp32's range come out as the bias; large ones
+    below that do not."""
+    announce("norm overflow")
+    b = torch.randn(256, device=DEV)
+    z = torch.randn(4, 256, device=DEV)
+    y = mb.norm_rows(z * 2.0 ** 66, None, b)
+    assert torch.equal(y, b.expand_as(y))
+    assert torch.equal(mb.norm_rows(z * 2.0 ** 56, eps=0.0), mb.norm_rows(z, eps=0.0))
+
+
 def test_no_rows_and_no_columns():
     announce("norm empty")
     w = torch.ones(8, device=DEV)
