@@ -99,8 +99,9 @@ struct Gate {
 };
 
 // ------------------------------------------------------------------ tiles
-// A workgroup has kGateCols features of a tape (a chain) and `runs` runs of L steps, one
-// behind the other.  A lane has F features of a run, so 64 / F lanes a run's all.
+// A workgroup has kGateCols features of a tape (a chain) and kRuns runs of L steps, one
+// behind the other.  A lane has F features of a run, so kRow of them a run's all.  (F = 2:
+// 64 features of bf16 are one 128-byte line; with four a lane registers halve the steps.)
 template <int F, int THREADS>
 struct Lanes {
     static constexpr int kRow = kGateCols / F, kRuns = THREADS / kRow;

@@ -441,7 +441,10 @@ hipError_t rotate_weights_launch(const RotateArgs& a, float* dwq, float* dwk, hi
 constexpr int kGateStateSteps = 64;
 constexpr int kGateCols = 64;        // features of a chain
 // Steps of a lane (of two features), threads of a workgroup, wavefronts of a SIMD that its
-// registers are to allow
+// registers are to allow.  As many steps as registers leave room for with that many
+// wavefronts: a tile's fixed cost (ticket, barriers, look-back) spreads over them.  (8 x 4096 x
+// 2048 bf16, forward, 16 steps of 512 threads 134 us, of 256 threads 117; the gradient with 16
+// steps 238, with 8 212.  512 threads wait for one another's loads longer.)
 struct GateShape {
     int steps, threads, waves;
     constexpr int tile() const { return threads * 2 / kGateCols * steps; }   // steps

