@@ -625,7 +625,7 @@ int memoroid_dropout(const void* x, const void* residual, const int64_t* rng, vo
  *   eps >= 0, finite.  1 <= d <= 16384, n < 2^31 (MEMOROID_EUNSUPPORTED otherwise).  A row
  *   whose values are all equal has no deviation but the rounding of its mean; with eps = 0
  *   it may come out as NaN.  A NaN or Inf stays in its row.  A row whose squared deviations
- *   add up past fp32's range (elements of 2^60 and more) comes out as the bias, rstd 0.  No
+ *   add up past fp32's range (elements from 2^57 on can) comes out as the bias, rstd 0.  No
  *   workspace.
  * ------------------------------------------------------------------------ */
 int memoroid_layer_norm(const void* x, const void* residual, const float* weight, const float* bias,

@@ -13,7 +13,7 @@
 // kernel in doubles.
 //
 // Seven tensors are read or written once: 8 tapes of 4096 steps of 2048 bf16 features, 0.94
-// GB in 205 us, 4.6 TB/s, the VALU busy for 118 of them (64 instructions a value); fp32, 8 x
+// GB in 205 us, 4.6 TB/s, the VALU busy for 127 of them (66 instructions a value); fp32, 8 x
 // 4096 x 1024, 190 us.  A step's coefficients that do not wait for the carry (m sig(i), v (1 -
 // sig(i)), sig(i) x a / m) are formed before it comes: 264 -> 234 us beside forming all gates
 // twice.  The registers (five floats a step and feature) set the tile: 16 steps a lane leave room
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs 
                 k[s][e] = d.k;
                 sr[s][e] = gr;
                 px[s][e] = m * gi;
-                pi[s][e] = v * (1.0f - gi);
+                pi[s][e] = __builtin_fmaf(-v, gi, v);
                 z[s][e] = xs * rm * d.left() - (begin ? 0.0f : h[e]);
                 u[e] += gu;
                 const float next = d.of(h[e], v);
@@ -252,12 +252,11 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs 
                 Decay<SLOW.value> d;
                 d.k = k[s][e];
                 const float lam = g[s].get(e) + c[e];
-                const float ds = lam * d.left() * z[s][e] * sr[s][e];
+                const float next = d.of(lam), ds = next * z[s][e] * sr[s][e], du = ds * rate[e];
                 sum[e] += ds;
                 dx[e] = lam * px[s][e];
-                dr[e] = ds * rate[e] * (1.0f - sr[s][e]);
+                dr[e] = __builtin_fmaf(-du, sr[s][e], du);
                 di[e] = lam * pi[s][e];
-                const float next = d.of(lam);
                 c[e] = BEGINS.value && (begins >> s & 1u) ? 0.0f : next;
             }
             Few<BF16> o;

@@ -9,7 +9,7 @@
 //
 // Memory bounds it, with instruction issue close behind.  8 tapes of 4096 steps of 2048
 // bf16 features: 0.54 GB in 112 us, 4.8 TB/s (a copy of 2 GiB reaches 4.9, a pass that
-// reads as much as it writes 6.1), of which the VALU is busy for 72: 37 instructions a value, six
+// reads as much as it writes 6.1), of which the VALU is busy for 72: 35 instructions a value, six
 // of them transcendental in two issue slots, so gates are formed once and decays stay in
 // registers.  Without the look-back it takes 5 us less, without the gates' arithmetic another
 // 4, so what is left is the loads of a workgroup, which all go out at its start.  fp32, 8 x 4096 x
