@@ -16,7 +16,9 @@ runs in the library's HIP kernels:
   stream), as retention, rotation, the gated recurrence and layer norm always
   do, on a workspace of the call's own where none is passed.  ``diag_scan``,
   ``retention``, ``qk_rotate``, ``gated_scan``, ``layer_norm`` and ``dropout`` are
-  the differentiable forms (``torch.autograd.Function``).
+  the differentiable forms (``torch.autograd.Function``).  A backward pass that is
+  to be captured into a graph needs, as with torch's own operators, leaves that no
+  graph of autograd built outside the capture still holds.
 
 Loading fails loudly (``MemoroidError``) if the shared library is missing:
 there is no fallback implementation.
@@ -1089,17 +1091,23 @@ def _gated_args(x, gates, alpha, start, steps: bool):
     shape = x.shape
     if len(shape) != (3 if steps else 2):
         raise ValueError("x must be %s" % ("[B,T,d]" if steps else "[B,d]"))
-    B, T, d = shape if steps else (shape[0], 1, shape[1])
-    if gates.shape != shape[:-1] + (2, d):
+    if steps:
+        B, T, d = shape
+        lead = (B, T)
+    else:
+        B, d = shape
+        T, lead = 1, (B,)
+    dtype = x.dtype
+    if gates.shape != lead + (2, d):
         raise ValueError("gates must be %s" % ("[B,T,2,d]" if steps else "[B,2,d]"))
-    if gates.dtype != x.dtype:
+    if gates.dtype != dtype:
         raise TypeError("x and gates must share a dtype")
-    dt = _code_of(x.dtype)
+    dt = _code_of(dtype)
     if dt == C64:
         raise TypeError("the gated recurrence takes float32 or bfloat16")
     if alpha.dtype != _T.float32 or alpha.shape != (d,):
         raise TypeError("alpha must be float32 [d]")
-    if (start is None and steps) or (start is not None and (start.dtype != _T.uint8 or start.shape != shape[:-1])):
+    if (start is None and steps) or (start is not None and (start.dtype != _T.uint8 or start.shape != lead)):
         raise TypeError("start must be uint8 %s" % ("[B,T]" if steps else "[B]"))
     return B, T, d, dt
 
@@ -1124,8 +1132,8 @@ def scan_gated(x, gates, alpha, start, state=None, final_state: bool = False, ke
     _torch()
     got = _gated(_gated_tapes(x, gates, alpha, start, state), x, gates, alpha, start, state, final_state, keep_states,
                  workspace)
-    got = tuple(t for t in got if t is not None)
-    return got if len(got) > 1 else got[0]
+    got = [t for t in got if t is not None]
+    return tuple(got) if len(got) > 1 else got[0]
 
 
 def _gated_tapes(x, gates, alpha, start, state):
@@ -1213,13 +1221,14 @@ def gated_step(x, gates, alpha, state, start=None):
 
 def _rows_args(x, residual, p, rng, site, *grads):
     """Rows of a norm's or dropout's input and its checks."""
-    if x.dim() < 1:
+    shape, dtype = x.shape, x.dtype
+    if not shape:
         raise ValueError("x must be [...,d]")
-    dt = _code_of(x.dtype)
+    dt = _code_of(dtype)
     if dt == C64:
         raise TypeError("x must be float32 or bfloat16")
     for t in (residual,) + grads:
-        if t is not None and (t.dtype != x.dtype or t.shape != x.shape):
+        if t is not None and (t.dtype != dtype or t.shape != shape):
             raise TypeError("the residual and upstream gradients must be like x")
     if not 0.0 <= p <= 1.0:
         raise ValueError("p must be in [0, 1]")
@@ -1229,7 +1238,7 @@ def _rows_args(x, residual, p, rng, site, *grads):
         raise TypeError("rng must be int64 [2]")
     if not 0 <= site < 1 << 32:
         raise ValueError("site must be in [0, 2^32)")
-    d = x.shape[-1]
+    d = shape[-1]
     return (x.numel() // d if d else 0), d, dt
 
 
@@ -1268,8 +1277,8 @@ def norm_rows(x, weight=None, bias=None, eps: float = 1e-5, residual=None, p: fl
     [...,2], when keep_stats is true."""
     _torch()
     got = _norm(_norm_args(x, weight, bias, residual, p, rng, site), x, weight, bias, eps, residual, p, rng, site, keep_stats)
-    got = tuple(t for t in got if t is not None)
-    return got if len(got) > 1 else got[0]
+    got = [t for t in got if t is not None]
+    return tuple(got) if len(got) > 1 else got[0]
 
 
 def _norm_args(x, weight, bias, residual, p, rng, site):
