@@ -16,8 +16,8 @@ runs in the library's HIP kernels:
   stream), as retention, rotation, the gated recurrence and layer norm always
   do, on a workspace of the call's own where none is passed.  ``diag_scan``,
   ``retention``, ``qk_rotate``, ``gated_scan``, ``layer_norm`` and ``dropout`` are
-  the differentiable forms (``torch.autograd.Function``).  A backward pass that is
-  to be captured into a graph needs, as with torch's own operators, leaves that no
+  the differentiable forms (``torch.autograd.Function``; the last three nodes of
+  torch's engine in C++, csrc/autograd.cpp).  A backward pass that is to be captured into a graph needs, as with torch's own operators, leaves that no
   graph of autograd built outside the capture still holds.
 
 Loading fails loudly (``MemoroidError``) if the shared library is missing:
@@ -1129,25 +1129,9 @@ def scan_gated(x, gates, alpha, start, state=None, final_state: bool = False, ke
     says so).  Returns h [B,T,d], followed by the float32 state after the last step
     when final_state is true and by the states [B,ceil(T/64),d] that scan_gated_bwd
     takes when keep_states is true."""
-    _torch()
-    got = _gated(_gated_tapes(x, gates, alpha, start, state), x, gates, alpha, start, state, final_state, keep_states,
-                 workspace)
-    got = [t for t in got if t is not None]
-    return tuple(got) if len(got) > 1 else got[0]
-
-
-def _gated_tapes(x, gates, alpha, start, state):
-    """The checks of scan_gated: the sizes, dtype code and device that _gated and
-    _gated_bwd take."""
-    B, T, d, dt = _gated_args(x, gates, alpha, start, True)
-    _gated_state(state, "state", B, d)
-    return B, T, d, dt, _check_cuda(x, gates, alpha, start, state)
-
-
-def _gated(sizes, x, gates, alpha, start, state, final_state, keep_states, workspace=None):
-    """scan_gated of arguments that have been checked: (h, last or None, states or None)."""
-    B, T, d, dt, dev = sizes
-    h = _T.empty_like(x)
+    torch = _torch()
+    B, T, d, dt, dev = _gated_tapes(x, gates, alpha, start, state)
+    h = torch.empty_like(x)
     last = alpha.new_empty((B, d)) if final_state else None
     kept = alpha.new_empty((B, -(-T // GATED_STATE_STEPS), d)) if keep_states else None
     if T == 0 and final_state:                  # no step: the state stays
@@ -1155,7 +1139,15 @@ def _gated(sizes, x, gates, alpha, start, state, final_state, keep_states, works
     ws = _workspace(lib().memoroid_scan_gated_workspace_bytes(B, T, d, dt), dev, workspace)
     _launch("memoroid_scan_gated", dev, x.data_ptr(), gates.data_ptr(), alpha.data_ptr(), start.data_ptr(), _ptr(state),
             h.data_ptr(), _ptr(last), _ptr(kept), B, T, d, dt, ws.data_ptr(), ws.numel())
-    return h, last, kept
+    got = (h,) + ((last,) if final_state else ()) + ((kept,) if keep_states else ())
+    return got if len(got) > 1 else h
+
+
+def _gated_tapes(x, gates, alpha, start, state):
+    """Sizes, dtype code and device of a call over tapes, and its checks."""
+    B, T, d, dt = _gated_args(x, gates, alpha, start, True)
+    _gated_state(state, "state", B, d)
+    return B, T, d, dt, _check_cuda(x, gates, alpha, start, state)
 
 
 def scan_gated_bwd(x, gates, alpha, start, states, grad_h, grad_state=None, need_grad_alpha: bool = True,
@@ -1171,16 +1163,8 @@ def scan_gated_bwd(x, gates, alpha, start, states, grad_h, grad_state=None, need
     if grad_h.dtype != x.dtype or grad_h.shape != x.shape:
         raise TypeError("grad_h must be [B,T,d] of x's dtype")
     dev = _check_cuda(x, gates, alpha, start, states, grad_h, grad_state)
-    return _gated_bwd((B, T, d, dt, dev), x, gates, alpha, start, states, grad_h, grad_state, need_grad_alpha,
-                      need_grad_state, workspace)
-
-
-def _gated_bwd(sizes, x, gates, alpha, start, states, grad_h, grad_state, need_grad_alpha, need_grad_state,
-               workspace=None):
-    """scan_gated_bwd of arguments that have been checked."""
-    B, T, d, dt, dev = sizes
-    gx, gg = _T.empty_like(x), _T.empty_like(gates)
-    ga = _T.empty_like(alpha) if need_grad_alpha else None
+    gx, gg = torch.empty_like(x), torch.empty_like(gates)
+    ga = torch.empty_like(alpha) if need_grad_alpha else None
     gs = alpha.new_empty((B, d)) if need_grad_state else None
     if B == 0 or T == 0:                        # no step: the state stays, nothing decays
         if ga is not None:
@@ -1256,14 +1240,10 @@ def drop_rows(x, p: float, rng, site: int = 0, residual=None):
     include/memoroid.h), so that a program draws anew by raising the step -- in a
     captured graph too -- and gives each of a model's dropouts a site of its own.  The
     gradient of x is the same call on the upstream gradient, without the residual."""
-    _torch()
-    return _drop(_rows_args(x, residual, p, rng, site) + (_check_cuda(x, residual, rng),), x, p, rng, site, residual)
-
-
-def _drop(sizes, x, p, rng, site, residual):
-    """drop_rows of arguments that have been checked."""
-    n, d, dt, dev = sizes
-    out = _T.empty_like(x)
+    torch = _torch()
+    n, d, dt = _rows_args(x, residual, p, rng, site)
+    dev = _check_cuda(x, residual, rng)
+    out = torch.empty_like(x)
     _launch("memoroid_dropout", dev, x.data_ptr(), _ptr(residual), _ptr(rng), out.data_ptr(), p, site, n, d, dt)
     return out
 
@@ -1275,29 +1255,22 @@ def norm_rows(x, weight=None, bias=None, eps: float = 1e-5, residual=None, p: fl
     bfloat16, d up to 16384; weight, bias: float32 [d] or None.  Returns y, followed by s
     when there is a residual or dropout and by the rows' (mean, 1 / deviation), float32
     [...,2], when keep_stats is true."""
-    _torch()
-    got = _norm(_norm_args(x, weight, bias, residual, p, rng, site), x, weight, bias, eps, residual, p, rng, site, keep_stats)
-    got = [t for t in got if t is not None]
-    return tuple(got) if len(got) > 1 else got[0]
+    torch = _torch()
+    n, d, dt, dev = _norm_args(x, weight, bias, residual, p, rng, site)
+    y = torch.empty_like(x)
+    s = torch.empty_like(x) if residual is not None or p > 0 else None
+    stats = torch.empty(x.shape[:-1] + (2,), dtype=torch.float32, device=dev) if keep_stats else None
+    _launch("memoroid_layer_norm", dev, x.data_ptr(), _ptr(residual), _ptr(weight), _ptr(bias), _ptr(rng), y.data_ptr(),
+            _ptr(s), _ptr(stats), eps, p, site, n, d, dt)
+    got = (y,) + ((s,) if s is not None else ()) + ((stats,) if keep_stats else ())
+    return got if len(got) > 1 else y
 
 
 def _norm_args(x, weight, bias, residual, p, rng, site):
-    """The checks of norm_rows: the sizes, dtype code and device that _norm and
-    _norm_bwd take."""
+    """Sizes, dtype code and device of a norm of rows, and its checks."""
     n, d, dt = _rows_args(x, residual, p, rng, site)
     _weights_ok(d, weight, bias)
     return n, d, dt, _check_cuda(x, residual, weight, bias, rng)
-
-
-def _norm(sizes, x, weight, bias, eps, residual, p, rng, site, keep_stats):
-    """norm_rows of arguments that have been checked: (y, s or None, stats or None)."""
-    n, d, dt, dev = sizes
-    y = _T.empty_like(x)
-    s = _T.empty_like(x) if residual is not None or p > 0 else None
-    stats = _T.empty(x.shape[:-1] + (2,), dtype=_T.float32, device=dev) if keep_stats else None
-    _launch("memoroid_layer_norm", dev, x.data_ptr(), _ptr(residual), _ptr(weight), _ptr(bias), _ptr(rng), y.data_ptr(),
-            _ptr(s), _ptr(stats), eps, p, site, n, d, dt)
-    return y, s, stats
 
 
 def norm_rows_bwd(x, stats, grad_y, weight=None, residual=None, grad_s=None, p: float = 0.0, rng=None, site: int = 0,
@@ -1311,17 +1284,11 @@ def norm_rows_bwd(x, stats, grad_y, weight=None, residual=None, grad_s=None, p: 
     if stats.dtype != torch.float32 or stats.shape != x.shape[:-1] + (2,):
         raise TypeError("stats must be float32 [...,2]")
     dev = _check_cuda(x, residual, weight, rng, stats, grad_y, grad_s)
-    return _norm_bwd((n, d, dt, dev), x, stats, grad_y, weight, residual, grad_s, p, rng, site, need_grad_weights, workspace)
-
-
-def _norm_bwd(sizes, x, stats, grad_y, weight, residual, grad_s, p, rng, site, need_grad_weights, workspace=None):
-    """norm_rows_bwd of arguments that have been checked."""
-    n, d, dt, dev = sizes
-    gx = _T.empty_like(x)
-    gr = None if residual is None else _T.empty_like(x) if p > 0 else gx
+    gx = torch.empty_like(x)
+    gr = None if residual is None else torch.empty_like(x) if p > 0 else gx
     gw = gb = ws = None
     if need_grad_weights:
-        gw, gb = _T.empty(d, dtype=_T.float32, device=dev), _T.empty(d, dtype=_T.float32, device=dev)
+        gw, gb = (torch.empty(d, dtype=torch.float32, device=dev) for _ in range(2))
         if n == 0:                              # no rows: sums of nothing
             gw.zero_()
             gb.zero_()
@@ -1484,122 +1451,43 @@ def qk_rotate(q, k, positions, freq, wq=None, wk=None, eps: float = 1e-6, interl
     return _RotateQK.apply(q, k, positions, freq, wq, wk, eps, interleaved, amplitude)
 
 
-def _make_gated_autograd():
-    torch = _torch()
-
-    class GatedScan(torch.autograd.Function):
-        """Differentiable gated recurrence over tapes with resets and a carried state."""
-
-        @staticmethod
-        def forward(ctx, x, gates, alpha, start, state, final_state):
-            ctx.sizes = _gated_tapes(x, gates, alpha, start, state)
-            h, last, states = _gated(ctx.sizes, x, gates, alpha, start, state, final_state, True)
-            ctx.save_for_backward(x, gates, alpha, start, states)
-            ctx.set_materialize_grads(False)
-            return (h, last) if final_state else h
-
-        @staticmethod
-        @torch.autograd.function.once_differentiable
-        def backward(ctx, grad_h, grad_state=None):
-            x, gates, alpha, start, states = ctx.saved_tensors
-            grad_h = torch.zeros_like(x) if grad_h is None else grad_h.contiguous()
-            # (the engine has seen to it that gradients are like their outputs)
-            need = ctx.needs_input_grad
-            gx, gg, ga, gs = _gated_bwd(ctx.sizes, x, gates, alpha, start, states, grad_h,
-                                        None if grad_state is None else grad_state.contiguous(), need[2], need[4])
-            return gx, gg, ga, None, gs, None
-
-    return GatedScan
+_nodes = None               # the extension module with the nodes below (csrc/autograd.cpp)
 
 
-_GatedScan = None
+def _load_nodes():
+    """The nodes of torch's engine for the three forms below, loaded on first use."""
+    global _nodes
+    if _nodes is None:
+        _torch()
+        lib()
+        try:
+            from . import _autograd
+        except ImportError as e:
+            raise MemoroidError(EHIP, "loading _autograd.so (not built: run python -m paper_2402_09900_amd.build)") from e
+        _nodes = _autograd
+    return _nodes
 
 
 def gated_scan(x, gates, alpha, start, state=None, final_state: bool = False):
     """Autograd-aware scan_gated: gradients of x, gates, alpha and state."""
-    global _GatedScan
-    if _GatedScan is None:
-        _GatedScan = _make_gated_autograd()
-    return _GatedScan.apply(x, gates, alpha, start, state, final_state)
-
-
-def _make_norm_autograd():
-    torch = _torch()
-
-    class LayerNorm(torch.autograd.Function):
-        """Differentiable layer norm with dropout and a residual in its pass."""
-
-        @staticmethod
-        def forward(ctx, x, weight, bias, eps, residual, p, rng, site):
-            sizes = _norm_args(x, weight, bias, residual, p, rng, site)
-            y, s, stats = _norm(sizes, x, weight, bias, eps, residual, p, rng, site, True)
-            ctx.save_for_backward(x, weight, residual, rng if p > 0 else None, stats)
-            ctx.more = (sizes, p, site)
-            ctx.set_materialize_grads(False)
-            return y if s is None else (y, s)
-
-        @staticmethod
-        @torch.autograd.function.once_differentiable
-        def backward(ctx, grad_y, grad_s=None):
-            x, weight, residual, rng, stats = ctx.saved_tensors
-            sizes, p, site = ctx.more
-            need = ctx.needs_input_grad
-            grad_y = torch.zeros_like(x) if grad_y is None else grad_y.contiguous()
-            # (the engine has seen to it that gradients are like their outputs)
-            gx, gr, gw, gb = _norm_bwd(sizes, x, stats, grad_y, weight, residual,
-                                       None if grad_s is None else grad_s.contiguous(), p, rng, site, need[1] or need[2])
-            return gx, gw if need[1] else None, gb if need[2] else None, None, gr, None, None, None
-
-    return LayerNorm
-
-
-_LayerNorm = None
+    nodes = _nodes or _load_nodes()
+    _gated_tapes(x, gates, alpha, start, state)
+    return nodes.gated_scan(x, gates, alpha, start, state, bool(final_state))
 
 
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, p: float = 0.0, rng=None, site: int = 0):
     """Autograd-aware norm_rows: y, or (y, s) with a residual or dropout; gradients of
     x, weight, bias and the residual."""
-    global _LayerNorm
-    if _LayerNorm is None:
-        _LayerNorm = _make_norm_autograd()
-    return _LayerNorm.apply(x, weight, bias, eps, residual, p, rng, site)
-
-
-def _make_dropout_autograd():
-    torch = _torch()
-
-    class Dropout(torch.autograd.Function):
-        """Differentiable dropout into a residual."""
-
-        @staticmethod
-        def forward(ctx, x, p, rng, site, residual):
-            sizes = _rows_args(x, residual, p, rng, site) + (_check_cuda(x, residual, rng),)
-            ctx.save_for_backward(rng if p > 0 else None)
-            ctx.more = (sizes, p, site, residual is not None)
-            return _drop(sizes, x, p, rng, site, residual)
-
-        @staticmethod
-        @torch.autograd.function.once_differentiable
-        def backward(ctx, grad):
-            rng, = ctx.saved_tensors
-            sizes, p, site, added = ctx.more
-            gx = None
-            if ctx.needs_input_grad[0]:
-                # (the engine has seen to it that the gradient is like the output)
-                gx = _drop(sizes, grad.contiguous(), p, rng, site, None) if p > 0 else grad
-            return gx, None, None, None, grad if added else None
-
-    return Dropout
-
-
-_Dropout = None
+    nodes = _nodes or _load_nodes()
+    _norm_args(x, weight, bias, residual, p, rng, site)
+    return nodes.layer_norm(x, weight, bias, eps, residual, p, rng, site)
 
 
 def dropout(x, p: float, rng, site: int = 0, residual=None):
     """Autograd-aware drop_rows: gradients of x and the residual.  The backward pass
     forms the mask again from rng, which must not have changed since (it raises if it
     has): a program raises the step after the backward pass."""
-    global _Dropout
-    if _Dropout is None:
-        _Dropout = _make_dropout_autograd()
-    return _Dropout.apply(x, p, rng, site, residual)
+    nodes = _nodes or _load_nodes()
+    _rows_args(x, residual, p, rng, site)
+    _check_cuda(x, residual, rng)
+    return nodes.dropout(x, p, rng, site, residual)

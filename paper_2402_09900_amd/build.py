@@ -1,9 +1,10 @@
-"""Build libmemoroid.so (hand-written HIP for gfx950) in-tree with hipcc.
+"""Build libmemoroid.so (hand-written HIP for gfx950) in-tree with hipcc, and
+_autograd.so (nodes of torch's autograd engine, host code) with g++.
 
     python -m paper_2402_09900_amd.build
 
-The library is always rebuilt (a few tens of seconds); the result lands next
-to this file, where the binding loads it from.
+Both are always rebuilt (a few minutes); the results land next to this file,
+where the binding loads them from.
 """
 from __future__ import annotations
 
@@ -11,10 +12,12 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libmemoroid.so")
+NODES = os.path.join(HERE, "_autograd.so")
 ARCH = "gfx950"
 
 FLAGS = [
@@ -34,13 +37,47 @@ def sources():
     return sorted(glob.glob(os.path.join(HERE, "csrc", "*.hip")))
 
 
-def build(verbose: bool = False) -> str:
-    tmp = LIB + ".tmp%d" % os.getpid()
-    cmd = ["hipcc"] + FLAGS + ["-o", tmp] + sources()
+def _run(cmd, verbose):
     if verbose:
         print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
-    os.replace(tmp, LIB)
+    return subprocess.Popen(cmd)
+
+
+def _done(process):
+    if process.wait():
+        raise subprocess.CalledProcessError(process.returncode, process.args)
+
+
+def _nodes_commands(obj, tmp):
+    """The nodes' compile and link; they call the library, which is found beside them."""
+    from torch.utils import cpp_extension
+
+    includes = cpp_extension.include_paths("cuda") + [sysconfig.get_paths()["include"]]
+    return (["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", "-Wno-unknown-pragmas", "-D__HIP_PLATFORM_AMD__=1",
+             "-DUSE_ROCM=1", "-DTORCH_EXTENSION_NAME=_autograd", "-I", os.path.join(ROOT, "include")]
+            + [a for d in includes for a in ("-isystem", d)]
+            + ["-c", os.path.join(HERE, "csrc", "autograd.cpp"), "-o", obj],
+            ["g++", "-shared", obj, "-o", tmp, "-L", HERE, "-lmemoroid", "-Wl,-rpath,$ORIGIN"]
+            + [a for d in cpp_extension.library_paths("cuda") for a in ("-L", d)]
+            + ["-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch", "-ltorch_python"])
+
+
+def build(verbose: bool = False) -> str:
+    end = ".tmp%d" % os.getpid()
+    obj = os.path.join(HERE, "autograd%s.o" % end)
+    compile_nodes, link_nodes = _nodes_commands(obj, NODES + end)
+    nodes = _run(compile_nodes, verbose)
+    library = _run(["hipcc"] + FLAGS + ["-o", LIB + end] + sources(), verbose)
+    try:
+        _done(library)
+        os.replace(LIB + end, LIB)
+        _done(nodes)
+        _done(_run(link_nodes, verbose))
+        os.replace(NODES + end, NODES)
+    finally:
+        nodes.wait()
+        if os.path.exists(obj):
+            os.remove(obj)
     return LIB
 
 

@@ -223,3 +223,110 @@ def test_captured_training():
         torch.cuda.synchronize()
         for a, b in zip(got, want):
             assert far(a, b.double().cpu()) <= 1e-5, turn
+
+
+# ------------------------------------------------------------- autograd nodes
+
+def test_refused_by_the_library():
+    """What the library refuses is a MemoroidError with its status, as from the raw forms."""
+    announce("nodes refused")
+    x = torch.zeros(1, 16385, device=DEV, requires_grad=True)
+    for f in (lambda: mb.layer_norm(x), lambda: mb.norm_rows(x)):
+        with pytest.raises(mb.MemoroidError) as e:
+            f()
+        assert e.value.status == mb.EUNSUPPORTED and "memoroid_layer_norm failed" in str(e.value)
+    d = (1 << 18) + 1
+    with pytest.raises(mb.MemoroidError) as e:
+        mb.gated_scan(torch.zeros(1, 1, d, device=DEV), torch.zeros(1, 1, 2, d, device=DEV), torch.zeros(d, device=DEV),
+                      torch.zeros(1, 1, dtype=torch.uint8, device=DEV))
+    assert e.value.status == mb.EUNSUPPORTED
+    with pytest.raises(mb.MemoroidError):
+        mb.layer_norm(x[:, :8].detach(), eps=-1.0)
+
+
+@pytest.mark.parametrize("given", [(False, False), (True, False), (False, True), (True, True)])
+@pytest.mark.parametrize("residual", [False, True])
+def test_wanted_gradients_of_the_norm(given, residual):
+    """Any of the inputs given, any of those wanting a gradient: each the raw form's."""
+    announce("nodes norm %s %s" % (given, residual))
+    torch.manual_seed(0)
+    x, gy, gs, res = (torch.randn(7, 40, device=DEV) for _ in range(4))
+    w, b = (torch.randn(40, device=DEV) if g else None for g in given)
+    res = res if residual else None
+    rng = torch.tensor([SEED, 1], dtype=torch.int64, device=DEV)
+    *_, st = mb.norm_rows(x, w, b, residual=res, p=0.2, rng=rng, keep_stats=True)
+    raw = mb.norm_rows_bwd(x, st, gy, w, res, gs, 0.2, rng)
+    want = dict(zip("xrwb", raw))
+    names = [n for n, v in zip("xrwb", (x, res, w, b)) if v is not None]
+    for mask in range(1, 1 << len(names)):
+        leaves = {n: v.detach().requires_grad_(n in names and bool(mask >> names.index(n) & 1))
+                  for n, v in zip("xrwb", (x, res, w, b)) if v is not None}
+        y, s = mb.layer_norm(leaves["x"], leaves.get("w"), leaves.get("b"), residual=leaves.get("r"), p=0.2, rng=rng)
+        wanted = [n for n in names if leaves[n].requires_grad]
+        for n, g in zip(wanted, torch.autograd.grad((y, s), [leaves[n] for n in wanted], (gy, gs))):
+            assert g.dtype == torch.float32 and torch.equal(g, want[n]), (mask, n)
+
+
+def test_nodes_once_and_unchanged():
+    """No second derivative, also where only one output's gradient is in the graph; inputs
+    that changed after the forward pass are refused; under no_grad there is no node."""
+    announce("nodes once")
+    x = torch.randn(2, 9, 16, device=DEV).requires_grad_(True)
+    gates, alpha = torch.randn(2, 9, 2, 16, device=DEV), torch.rand(16, device=DEV)
+    start = torch.zeros(2, 9, dtype=torch.uint8, device=DEV)
+    rng = torch.tensor([SEED, 1], dtype=torch.int64, device=DEV)
+    forms = (lambda v: mb.gated_scan(v, gates, alpha, start), lambda v: mb.layer_norm(v), lambda v: mb.dropout(v, 0.3, rng))
+    for f in forms:
+        first, = torch.autograd.grad(f(x).square().sum(), x)
+        g, = torch.autograd.grad(f(x).square().sum(), x, create_graph=True)
+        assert torch.equal(g, first) and g.requires_grad
+        with pytest.raises(RuntimeError, match="twice"):
+            g.sum().backward()
+        with torch.no_grad():
+            y = f(x)
+        assert not y.requires_grad and torch.equal(y, f(x))
+    for f in forms[:2]:
+        v = x.detach().clone().requires_grad_(True)
+        u = v * 1.0
+        y = f(u)
+        with torch.no_grad():
+            u.add_(1.0)
+        with pytest.raises(RuntimeError, match="inplace"):
+            y.sum().backward()
+
+
+def test_nodes_on_threads_and_streams():
+    """Two threads, a stream each, train at once: the results of one alone."""
+    announce("nodes threads")
+    import threading
+
+    def work(seed, out, turns):
+        g = torch.Generator(device=DEV)
+        g.manual_seed(seed)
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            x, up = (torch.randn(2, 3000, 64, device=DEV, generator=g) for _ in range(2))
+            gates = torch.randn(2, 3000, 2, 64, device=DEV, generator=g)
+            alpha = torch.rand(64, device=DEV, generator=g).mul_(0.1).requires_grad_(True)
+            start = torch.zeros(2, 3000, dtype=torch.uint8, device=DEV)
+            rng = torch.tensor([seed, 1], dtype=torch.int64, device=DEV)
+            w = torch.ones(64, device=DEV, requires_grad=True)
+            x.requires_grad_(True)
+            for _ in range(turns):
+                y, s = mb.layer_norm(x, w, residual=up, p=0.1, rng=rng)
+                h = mb.dropout(mb.gated_scan(y, gates, alpha, start), 0.1, rng, 1, s)
+                got = torch.autograd.grad(h, (x, w, alpha), up)
+            out[seed] = [t.detach().clone() for t in (h, *got)]
+            stream.synchronize()
+
+    alone, both = {}, {}
+    for seed in (1, 2):
+        work(seed, alone, 1)
+    threads = [threading.Thread(target=work, args=(seed, both, 20)) for seed in (1, 2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(60)
+    assert sorted(both) == [1, 2]
+    for seed in (1, 2):
+        assert all(torch.equal(a, b) for a, b in zip(alone[seed], both[seed]))
