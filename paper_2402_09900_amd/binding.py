@@ -16,8 +16,9 @@ runs in the library's HIP kernels:
   stream), as retention, rotation, the gated recurrence and layer norm always
   do, on a workspace of the call's own where none is passed.  ``diag_scan``,
   ``retention``, ``qk_rotate``, ``gated_scan``, ``layer_norm`` and ``dropout`` are
-  the differentiable forms (``torch.autograd.Function``; the last three nodes of
-  torch's engine in C++, csrc/autograd.cpp).  A backward pass that is to be captured into a graph needs, as with torch's own operators, leaves that no
+  the differentiable forms (``torch.autograd.Function``, and nodes of torch's
+  engine in C++ where the layer is: the gated recurrence, layer norm and dropout,
+  csrc/torch_layer.cpp).  A backward pass that is to be captured into a graph needs, as with torch's own operators, leaves that no
   graph of autograd built outside the capture still holds.
 
 Loading fails loudly (``MemoroidError``) if the shared library is missing:
@@ -1086,35 +1087,22 @@ def rotate_qk_bwd(q, k, positions, freq, grad_q, grad_k, wq=None, wk=None, eps: 
     return gq, gk, gwq, gwk
 
 
-def _gated_args(x, gates, alpha, start, steps: bool):
-    """Sizes of a gated call (steps: tapes, else single steps) and its checks."""
-    shape = x.shape
-    if len(shape) != (3 if steps else 2):
-        raise ValueError("x must be %s" % ("[B,T,d]" if steps else "[B,d]"))
-    if steps:
-        B, T, d = shape
-        lead = (B, T)
-    else:
-        B, d = shape
-        T, lead = 1, (B,)
-    dtype = x.dtype
-    if gates.shape != lead + (2, d):
-        raise ValueError("gates must be %s" % ("[B,T,2,d]" if steps else "[B,2,d]"))
-    if gates.dtype != dtype:
-        raise TypeError("x and gates must share a dtype")
-    dt = _code_of(dtype)
-    if dt == C64:
-        raise TypeError("the gated recurrence takes float32 or bfloat16")
-    if alpha.dtype != _T.float32 or alpha.shape != (d,):
-        raise TypeError("alpha must be float32 [d]")
-    if (start is None and steps) or (start is not None and (start.dtype != _T.uint8 or start.shape != lead)):
-        raise TypeError("start must be uint8 %s" % ("[B,T]" if steps else "[B]"))
-    return B, T, d, dt
+_layer = None               # the extension module of the calls below (csrc/torch_layer.cpp)
 
 
-def _gated_state(state, name, B, d):
-    if state is not None and (state.dtype != _T.float32 or state.shape != (B, d)):
-        raise TypeError("%s must be float32 [B,d]" % name)
+def _torch_layer():
+    """The gated recurrence, layer norm and dropout on tensors: checks, outputs, calls of
+    the library and autograd nodes, in C++; loaded on first use."""
+    global _layer
+    if _layer is None:
+        _torch()
+        lib()
+        try:
+            from . import _torch_layer as layer
+        except ImportError as e:
+            raise MemoroidError(EHIP, "loading _torch_layer.so (not built: run python -m paper_2402_09900_amd.build)") from e
+        _layer = layer
+    return _layer
 
 
 def scan_gated(x, gates, alpha, start, state=None, final_state: bool = False, keep_states: bool = False, workspace=None):
@@ -1129,25 +1117,7 @@ def scan_gated(x, gates, alpha, start, state=None, final_state: bool = False, ke
     says so).  Returns h [B,T,d], followed by the float32 state after the last step
     when final_state is true and by the states [B,ceil(T/64),d] that scan_gated_bwd
     takes when keep_states is true."""
-    torch = _torch()
-    B, T, d, dt, dev = _gated_tapes(x, gates, alpha, start, state)
-    h = torch.empty_like(x)
-    last = alpha.new_empty((B, d)) if final_state else None
-    kept = alpha.new_empty((B, -(-T // GATED_STATE_STEPS), d)) if keep_states else None
-    if T == 0 and final_state:                  # no step: the state stays
-        last.zero_() if state is None else last.copy_(state)
-    ws = _workspace(lib().memoroid_scan_gated_workspace_bytes(B, T, d, dt), dev, workspace)
-    _launch("memoroid_scan_gated", dev, x.data_ptr(), gates.data_ptr(), alpha.data_ptr(), start.data_ptr(), _ptr(state),
-            h.data_ptr(), _ptr(last), _ptr(kept), B, T, d, dt, ws.data_ptr(), ws.numel())
-    got = (h,) + ((last,) if final_state else ()) + ((kept,) if keep_states else ())
-    return got if len(got) > 1 else h
-
-
-def _gated_tapes(x, gates, alpha, start, state):
-    """Sizes, dtype code and device of a call over tapes, and its checks."""
-    B, T, d, dt = _gated_args(x, gates, alpha, start, True)
-    _gated_state(state, "state", B, d)
-    return B, T, d, dt, _check_cuda(x, gates, alpha, start, state)
+    return (_layer or _torch_layer()).scan_gated(x, gates, alpha, start, state, final_state, keep_states, workspace)
 
 
 def scan_gated_bwd(x, gates, alpha, start, states, grad_h, grad_state=None, need_grad_alpha: bool = True,
@@ -1155,28 +1125,8 @@ def scan_gated_bwd(x, gates, alpha, start, states, grad_h, grad_state=None, need
     """Gradient of scan_gated: (dx, dgates, dalpha, dstate), from the states that
     scan_gated kept.  grad_state is the gradient of the state after the last step (None:
     zero); dalpha and dstate are None if not needed."""
-    torch = _torch()
-    B, T, d, dt = _gated_args(x, gates, alpha, start, True)
-    _gated_state(grad_state, "grad_state", B, d)
-    if states.dtype != torch.float32 or states.shape != (B, -(-T // GATED_STATE_STEPS), d):
-        raise TypeError("states must be float32 [B,ceil(T/64),d]")
-    if grad_h.dtype != x.dtype or grad_h.shape != x.shape:
-        raise TypeError("grad_h must be [B,T,d] of x's dtype")
-    dev = _check_cuda(x, gates, alpha, start, states, grad_h, grad_state)
-    gx, gg = torch.empty_like(x), torch.empty_like(gates)
-    ga = torch.empty_like(alpha) if need_grad_alpha else None
-    gs = alpha.new_empty((B, d)) if need_grad_state else None
-    if B == 0 or T == 0:                        # no step: the state stays, nothing decays
-        if ga is not None:
-            ga.zero_()
-        if gs is not None:
-            gs.zero_() if grad_state is None else gs.copy_(grad_state)
-        return gx, gg, ga, gs
-    ws = _workspace(lib().memoroid_scan_gated_bwd_workspace_bytes(B, T, d, dt), dev, workspace)
-    _launch("memoroid_scan_gated_bwd", dev, x.data_ptr(), gates.data_ptr(), alpha.data_ptr(), start.data_ptr(),
-            states.data_ptr(), grad_h.data_ptr(), _ptr(grad_state), gx.data_ptr(), gg.data_ptr(), _ptr(ga), _ptr(gs),
-            B, T, d, dt, ws.data_ptr(), ws.numel())
-    return gx, gg, ga, gs
+    return (_layer or _torch_layer()).scan_gated_bwd(x, gates, alpha, start, states, grad_h, grad_state, need_grad_alpha,
+                                                     need_grad_state, workspace)
 
 
 def gated_step(x, gates, alpha, state, start=None):
@@ -1186,50 +1136,7 @@ def gated_step(x, gates, alpha, state, start=None):
 
     The step has no gradient and refuses inputs that want one (outside
     torch.no_grad()): gated_scan() of tapes of one step with a carried state has."""
-    torch = _torch()
-    B, _, d, dt = _gated_args(x, gates, alpha, start, False)
-    if state is None:
-        raise TypeError("state must be float32 [B,d]")
-    _gated_state(state, "state", B, d)
-    if (x.requires_grad or gates.requires_grad or alpha.requires_grad or state.requires_grad) and \
-            torch.is_grad_enabled():
-        raise RuntimeError("gated_step has no gradient: call it under torch.no_grad(), or gated_scan() on tapes of one "
-                           "step")
-    dev = _check_cuda(x, gates, alpha, start, state)
-    h = torch.empty_like(x)
-    _launch("memoroid_gated_step", dev, x.data_ptr(), gates.data_ptr(), alpha.data_ptr(), _ptr(start), state.data_ptr(),
-            h.data_ptr(), B, d, dt)
-    torch.autograd.graph.increment_version(state)      # a graph that has saved it refuses its backward pass
-    return h
-
-
-def _rows_args(x, residual, p, rng, site, *grads):
-    """Rows of a norm's or dropout's input and its checks."""
-    shape, dtype = x.shape, x.dtype
-    if not shape:
-        raise ValueError("x must be [...,d]")
-    dt = _code_of(dtype)
-    if dt == C64:
-        raise TypeError("x must be float32 or bfloat16")
-    for t in (residual,) + grads:
-        if t is not None and (t.dtype != dtype or t.shape != shape):
-            raise TypeError("the residual and upstream gradients must be like x")
-    if not 0.0 <= p <= 1.0:
-        raise ValueError("p must be in [0, 1]")
-    if p > 0 and rng is None:
-        raise ValueError("dropout needs rng, int64 [2] on x's device: seed and step")
-    if rng is not None and (rng.dtype != _T.int64 or rng.shape != (2,)):
-        raise TypeError("rng must be int64 [2]")
-    if not 0 <= site < 1 << 32:
-        raise ValueError("site must be in [0, 2^32)")
-    d = shape[-1]
-    return (x.numel() // d if d else 0), d, dt
-
-
-def _weights_ok(d, *ws):
-    for w in ws:
-        if w is not None and (w.dtype != _T.float32 or w.shape != (d,)):
-            raise TypeError("weight and bias must be float32 [d]")
+    return (_layer or _torch_layer()).gated_step(x, gates, alpha, state, start)
 
 
 def drop_rows(x, p: float, rng, site: int = 0, residual=None):
@@ -1240,12 +1147,7 @@ def drop_rows(x, p: float, rng, site: int = 0, residual=None):
     include/memoroid.h), so that a program draws anew by raising the step -- in a
     captured graph too -- and gives each of a model's dropouts a site of its own.  The
     gradient of x is the same call on the upstream gradient, without the residual."""
-    torch = _torch()
-    n, d, dt = _rows_args(x, residual, p, rng, site)
-    dev = _check_cuda(x, residual, rng)
-    out = torch.empty_like(x)
-    _launch("memoroid_dropout", dev, x.data_ptr(), _ptr(residual), _ptr(rng), out.data_ptr(), p, site, n, d, dt)
-    return out
+    return (_layer or _torch_layer()).drop_rows(x, p, rng, site, residual)
 
 
 def norm_rows(x, weight=None, bias=None, eps: float = 1e-5, residual=None, p: float = 0.0, rng=None, site: int = 0,
@@ -1255,22 +1157,7 @@ def norm_rows(x, weight=None, bias=None, eps: float = 1e-5, residual=None, p: fl
     bfloat16, d up to 16384; weight, bias: float32 [d] or None.  Returns y, followed by s
     when there is a residual or dropout and by the rows' (mean, 1 / deviation), float32
     [...,2], when keep_stats is true."""
-    torch = _torch()
-    n, d, dt, dev = _norm_args(x, weight, bias, residual, p, rng, site)
-    y = torch.empty_like(x)
-    s = torch.empty_like(x) if residual is not None or p > 0 else None
-    stats = torch.empty(x.shape[:-1] + (2,), dtype=torch.float32, device=dev) if keep_stats else None
-    _launch("memoroid_layer_norm", dev, x.data_ptr(), _ptr(residual), _ptr(weight), _ptr(bias), _ptr(rng), y.data_ptr(),
-            _ptr(s), _ptr(stats), eps, p, site, n, d, dt)
-    got = (y,) + ((s,) if s is not None else ()) + ((stats,) if keep_stats else ())
-    return got if len(got) > 1 else y
-
-
-def _norm_args(x, weight, bias, residual, p, rng, site):
-    """Sizes, dtype code and device of a norm of rows, and its checks."""
-    n, d, dt = _rows_args(x, residual, p, rng, site)
-    _weights_ok(d, weight, bias)
-    return n, d, dt, _check_cuda(x, residual, weight, bias, rng)
+    return (_layer or _torch_layer()).norm_rows(x, weight, bias, eps, residual, p, rng, site, keep_stats)
 
 
 def norm_rows_bwd(x, stats, grad_y, weight=None, residual=None, grad_s=None, p: float = 0.0, rng=None, site: int = 0,
@@ -1278,25 +1165,8 @@ def norm_rows_bwd(x, stats, grad_y, weight=None, residual=None, grad_s=None, p: 
     """Gradient of norm_rows: (dx, dresidual, dweight, dbias), from the stats that it
     kept.  grad_s is the gradient of s (None: zero).  dresidual is None without a
     residual, and dx itself with p = 0; dweight and dbias are None if not needed."""
-    torch = _torch()
-    n, d, dt = _rows_args(x, residual, p, rng, site, grad_y, grad_s)
-    _weights_ok(d, weight)
-    if stats.dtype != torch.float32 or stats.shape != x.shape[:-1] + (2,):
-        raise TypeError("stats must be float32 [...,2]")
-    dev = _check_cuda(x, residual, weight, rng, stats, grad_y, grad_s)
-    gx = torch.empty_like(x)
-    gr = None if residual is None else torch.empty_like(x) if p > 0 else gx
-    gw = gb = ws = None
-    if need_grad_weights:
-        gw, gb = (torch.empty(d, dtype=torch.float32, device=dev) for _ in range(2))
-        if n == 0:                              # no rows: sums of nothing
-            gw.zero_()
-            gb.zero_()
-        ws = _workspace(lib().memoroid_layer_norm_bwd_workspace_bytes(n, d), dev, workspace)
-    _launch("memoroid_layer_norm_bwd", dev, x.data_ptr(), _ptr(residual), _ptr(weight), _ptr(rng), stats.data_ptr(),
-            grad_y.data_ptr(), _ptr(grad_s), gx.data_ptr(), gr.data_ptr() if gr is not None and p > 0 else None,
-            _ptr(gw), _ptr(gb), p, site, n, d, dt, _ptr(ws), 0 if ws is None else ws.numel())
-    return gx, gr, gw, gb
+    return (_layer or _torch_layer()).norm_rows_bwd(x, stats, grad_y, weight, residual, grad_s, p, rng, site,
+                                                    need_grad_weights, workspace)
 
 
 def workspace_status(workspace) -> int:
@@ -1451,43 +1321,19 @@ def qk_rotate(q, k, positions, freq, wq=None, wk=None, eps: float = 1e-6, interl
     return _RotateQK.apply(q, k, positions, freq, wq, wk, eps, interleaved, amplitude)
 
 
-_nodes = None               # the extension module with the nodes below (csrc/autograd.cpp)
-
-
-def _load_nodes():
-    """The nodes of torch's engine for the three forms below, loaded on first use."""
-    global _nodes
-    if _nodes is None:
-        _torch()
-        lib()
-        try:
-            from . import _autograd
-        except ImportError as e:
-            raise MemoroidError(EHIP, "loading _autograd.so (not built: run python -m paper_2402_09900_amd.build)") from e
-        _nodes = _autograd
-    return _nodes
-
-
 def gated_scan(x, gates, alpha, start, state=None, final_state: bool = False):
     """Autograd-aware scan_gated: gradients of x, gates, alpha and state."""
-    nodes = _nodes or _load_nodes()
-    _gated_tapes(x, gates, alpha, start, state)
-    return nodes.gated_scan(x, gates, alpha, start, state, bool(final_state))
+    return (_layer or _torch_layer()).gated_scan(x, gates, alpha, start, state, final_state)
 
 
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, p: float = 0.0, rng=None, site: int = 0):
     """Autograd-aware norm_rows: y, or (y, s) with a residual or dropout; gradients of
     x, weight, bias and the residual."""
-    nodes = _nodes or _load_nodes()
-    _norm_args(x, weight, bias, residual, p, rng, site)
-    return nodes.layer_norm(x, weight, bias, eps, residual, p, rng, site)
+    return (_layer or _torch_layer()).layer_norm(x, weight, bias, eps, residual, p, rng, site)
 
 
 def dropout(x, p: float, rng, site: int = 0, residual=None):
     """Autograd-aware drop_rows: gradients of x and the residual.  The backward pass
     forms the mask again from rng, which must not have changed since (it raises if it
     has): a program raises the step after the backward pass."""
-    nodes = _nodes or _load_nodes()
-    _rows_args(x, residual, p, rng, site)
-    _check_cuda(x, residual, rng)
-    return nodes.dropout(x, p, rng, site, residual)
+    return (_layer or _torch_layer()).dropout(x, p, rng, site, residual)

@@ -1,5 +1,5 @@
 """Build libmemoroid.so (hand-written HIP for gfx950) in-tree with hipcc, and
-_autograd.so (nodes of torch's autograd engine, host code) with g++.
+_torch_layer.so (calls on torch tensors and autograd nodes, host code) with g++.
 
     python -m paper_2402_09900_amd.build
 
@@ -17,7 +17,7 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libmemoroid.so")
-NODES = os.path.join(HERE, "_autograd.so")
+LAYER = os.path.join(HERE, "_torch_layer.so")
 ARCH = "gfx950"
 
 FLAGS = [
@@ -48,15 +48,15 @@ def _done(process):
         raise subprocess.CalledProcessError(process.returncode, process.args)
 
 
-def _nodes_commands(obj, tmp):
-    """The nodes' compile and link; they call the library, which is found beside them."""
+def _layer_commands(obj, tmp):
+    """The torch layer's compile and link; it calls the library, which is found beside it."""
     from torch.utils import cpp_extension
 
     includes = cpp_extension.include_paths("cuda") + [sysconfig.get_paths()["include"]]
     return (["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", "-Wno-unknown-pragmas", "-D__HIP_PLATFORM_AMD__=1",
-             "-DUSE_ROCM=1", "-DTORCH_EXTENSION_NAME=_autograd", "-I", os.path.join(ROOT, "include")]
+             "-DUSE_ROCM=1", "-DTORCH_EXTENSION_NAME=_torch_layer", "-I", os.path.join(ROOT, "include")]
             + [a for d in includes for a in ("-isystem", d)]
-            + ["-c", os.path.join(HERE, "csrc", "autograd.cpp"), "-o", obj],
+            + ["-c", os.path.join(HERE, "csrc", "torch_layer.cpp"), "-o", obj],
             ["g++", "-shared", obj, "-o", tmp, "-L", HERE, "-lmemoroid", "-Wl,-rpath,$ORIGIN"]
             + [a for d in cpp_extension.library_paths("cuda") for a in ("-L", d)]
             + ["-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch", "-ltorch_python"])
@@ -64,18 +64,18 @@ def _nodes_commands(obj, tmp):
 
 def build(verbose: bool = False) -> str:
     end = ".tmp%d" % os.getpid()
-    obj = os.path.join(HERE, "autograd%s.o" % end)
-    compile_nodes, link_nodes = _nodes_commands(obj, NODES + end)
-    nodes = _run(compile_nodes, verbose)
+    obj = os.path.join(HERE, "torch_layer%s.o" % end)
+    compile_layer, link_layer = _layer_commands(obj, LAYER + end)
+    layer = _run(compile_layer, verbose)
     library = _run(["hipcc"] + FLAGS + ["-o", LIB + end] + sources(), verbose)
     try:
         _done(library)
         os.replace(LIB + end, LIB)
-        _done(nodes)
-        _done(_run(link_nodes, verbose))
-        os.replace(NODES + end, NODES)
+        _done(layer)
+        _done(_run(link_layer, verbose))
+        os.replace(LAYER + end, LAYER)
     finally:
-        nodes.wait()
+        layer.wait()
         if os.path.exists(obj):
             os.remove(obj)
     return LIB

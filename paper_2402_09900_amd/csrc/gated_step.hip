@@ -7,7 +7,7 @@ namespace memoroid {
 namespace {
 
 // V features a lane (V 4: d is a multiple of 4 and addresses are of 4 elements).  Bound by
-// the launch where a state is small (16 rows of 256 in fp32: 2.4 us of kernel, 8.6 a call),
+// the launch where a state is small (16 rows of 256 in fp32: 2.4 us of kernel, 4.0 a call),
 // then by memory (512 rows of 2048 in bf16: 17 MB in 4.9 us).
 template <bool BF16, int V>
 __global__ __launch_bounds__(256) void gated_step_kernel(GatedStepArgs p) {
