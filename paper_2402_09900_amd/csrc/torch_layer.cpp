@@ -305,6 +305,12 @@ struct Dropout : Function<Dropout> {
 
 // ------------------------------------------------------------------ for Python
 
+// f() without the interpreter's lock, which other threads may want while it waits for a queue
+template <class F>
+auto unlocked(F&& f) {
+    const py::gil_scoped_release free;
+    return f();
+}
 // The tensors that are there: one by itself, else a tuple
 py::object result(std::initializer_list<Tensor> tensors) {
     py::list there;
@@ -323,7 +329,8 @@ py::object scan_gated(const Tensor& x, const Tensor& gates, const Tensor& alpha,
     check_tapes(x, gates, alpha, start);
     check_state(x, state, "state must be float32 [B,d]");
     check_places({&x, &gates, &alpha, &start, &state});
-    const Scanned got = gated_forward(x, gates, alpha, start, state, final_state, keep_states, given(callers));
+    const Scanned got =
+        unlocked([&] { return gated_forward(x, gates, alpha, start, state, final_state, keep_states, given(callers)); });
     return result({got.h, got.last, got.kept});
 }
 
@@ -336,7 +343,9 @@ py::object scan_gated_bwd(const Tensor& x, const Tensor& gates, const Tensor& al
     type_if(!is(states, at::kFloat, {x.size(0), kept_states(x.size(1)), x.size(2)}), "states must be float32 [B,ceil(T/64),d]");
     type_if(grad_h.scalar_type() != x.scalar_type() || grad_h.sizes() != x.sizes(), "grad_h must be [B,T,d] of x's dtype");
     check_places({&x, &gates, &alpha, &start, &states, &grad_h, &grad_state});
-    const variable_list g = gated_backward(x, gates, alpha, start, states, grad_h, grad_state, want_alpha, want_state, given(callers));
+    const variable_list g = unlocked([&] {
+        return gated_backward(x, gates, alpha, start, states, grad_h, grad_state, want_alpha, want_state, given(callers));
+    });
     return py::make_tuple(g[0], g[1], g[2], g[3]);
 }
 
@@ -350,6 +359,7 @@ Tensor gated_step(const Tensor& x, const Tensor& gates, const Tensor& alpha, con
         (x.requires_grad() || gates.requires_grad() || alpha.requires_grad() || state.requires_grad()))
         throw std::runtime_error("gated_step has no gradient: call it under torch.no_grad(), or gated_scan() on tapes of one step");
     check_places({&x, &gates, &alpha, &start, &state});
+    const py::gil_scoped_release free;
     Tensor h = at::empty_like(x);
     launch("memoroid_gated_step", memoroid_gated_step, x, ptr(x), ptr(gates), floats(alpha), (const uint8_t*)ptr(start),
            floats(state), ptr(h), x.size(0), x.size(1), dtype_of(x));
@@ -362,7 +372,7 @@ Tensor drop_rows(const Tensor& x, double p, const OptTensor& rng_, int64_t site,
     const Tensor rng = given(rng_), residual = given(residual_);
     check_rows(x, residual, p, rng, site);
     check_places({&x, &residual, &rng});
-    return drop(x, p, rng, site, residual);
+    return unlocked([&] { return drop(x, p, rng, site, residual); });
 }
 
 py::object norm_rows(const Tensor& x, const OptTensor& weight_, const OptTensor& bias_, double eps, const OptTensor& residual_,
@@ -371,7 +381,7 @@ py::object norm_rows(const Tensor& x, const OptTensor& weight_, const OptTensor&
     check_rows(x, residual, p, rng, site);
     check_weights(x, weight, bias);
     check_places({&x, &residual, &weight, &bias, &rng});
-    const Normed got = norm_forward(x, weight, bias, eps, residual, p, rng, site, keep_stats);
+    const Normed got = unlocked([&] { return norm_forward(x, weight, bias, eps, residual, p, rng, site, keep_stats); });
     return result({got.y, got.s, got.stats});
 }
 
@@ -386,8 +396,9 @@ py::object norm_rows_bwd(const Tensor& x, const Tensor& stats, const Tensor& gra
                 "upstream gradients must be like x");
     type_if(stats.scalar_type() != at::kFloat || stats.sizes() != at::IntArrayRef(stats_size(x)), "stats must be float32 [...,2]");
     check_places({&x, &residual, &weight, &rng, &stats, &grad_y, &grad_s});
-    const variable_list g = norm_backward(x, stats, grad_y, weight, residual, grad_s, p, rng, site, want_weights, want_weights,
-                                          given(callers));
+    const variable_list g = unlocked([&] {
+        return norm_backward(x, stats, grad_y, weight, residual, grad_s, p, rng, site, want_weights, want_weights, given(callers));
+    });
     return py::make_tuple(g[0], g[1], g[2], g[3]);
 }
 
@@ -397,7 +408,7 @@ py::object gated_scan(const Tensor& x, const Tensor& gates, const Tensor& alpha,
     check_tapes(x, gates, alpha, start);
     check_state(x, s, "state must be float32 [B,d]");
     check_places({&x, &gates, &alpha, &start, &s});
-    return result(GatedScan::apply(x, gates, alpha, start, state, final_state));
+    return result(unlocked([&] { return GatedScan::apply(x, gates, alpha, start, state, final_state); }));
 }
 
 py::object layer_norm(const Tensor& x, const OptTensor& weight, const OptTensor& bias, double eps, const OptTensor& residual,
@@ -406,14 +417,14 @@ py::object layer_norm(const Tensor& x, const OptTensor& weight, const OptTensor&
     check_rows(x, res, p, numbers, site);
     check_weights(x, w, b);
     check_places({&x, &res, &w, &b, &numbers});
-    return result(LayerNorm::apply(x, weight, bias, eps, residual, p, rng, site));
+    return result(unlocked([&] { return LayerNorm::apply(x, weight, bias, eps, residual, p, rng, site); }));
 }
 
 Tensor dropout(const Tensor& x, double p, const OptTensor& rng, int64_t site, const OptTensor& residual) {
     const Tensor numbers = given(rng), res = given(residual);
     check_rows(x, res, p, numbers, site);
     check_places({&x, &res, &numbers});
-    return Dropout::apply(x, p, rng, site, residual);
+    return unlocked([&] { return Dropout::apply(x, p, rng, site, residual); });
 }
 
 }  // namespace
