@@ -244,6 +244,38 @@ def test_refused_by_the_library():
         mb.layer_norm(x[:, :8].detach(), eps=-1.0)
 
 
+def test_workspaces():
+    """The caller's workspace, whatever it holds; one that is too small is not used, one with
+    gaps or on the host is refused."""
+    announce("nodes workspaces")
+    torch.manual_seed(1)
+    x, gates = torch.randn(2, 400, 40, device=DEV), torch.randn(2, 400, 2, 40, device=DEV)
+    alpha, start = torch.rand(40, device=DEV), torch.zeros(2, 400, dtype=torch.uint8, device=DEV)
+    h, kept = mb.scan_gated(x, gates, alpha, start, keep_states=True)
+    want = mb.scan_gated_bwd(x, gates, alpha, start, kept, h)
+    y, st = mb.norm_rows(x, alpha, keep_stats=True)
+    rows = mb.norm_rows_bwd(x, st, h, alpha)
+    for fill in (0, 255, 7):
+        ws = torch.full((1 << 20,), fill, dtype=torch.uint8, device=DEV)
+        assert torch.equal(mb.scan_gated(x, gates, alpha, start, workspace=ws), h)
+        assert mb.workspace_status(ws) == mb.OK
+        for a, b in zip(mb.scan_gated_bwd(x, gates, alpha, start, kept, h, workspace=ws), want):
+            assert torch.equal(a, b)
+        assert mb.workspace_status(ws) == mb.OK
+        for a, b in zip(mb.norm_rows_bwd(x, st, h, alpha, workspace=ws), rows):
+            assert (a is None and b is None) or torch.equal(a, b)
+    small = torch.full((300,), 9, dtype=torch.uint8, device=DEV)
+    assert torch.equal(mb.scan_gated(x, gates, alpha, start, workspace=small), h)
+    assert bool((small == 9).all())
+    for ws in (torch.zeros(1 << 20, dtype=torch.uint8), torch.zeros(1 << 21, dtype=torch.uint8, device=DEV)[::2]):
+        with pytest.raises(ValueError):
+            mb.scan_gated(x, gates, alpha, start, workspace=ws)
+        with pytest.raises(ValueError):
+            mb.scan_gated_bwd(x, gates, alpha, start, kept, h, workspace=ws)
+        with pytest.raises(ValueError):
+            mb.norm_rows_bwd(x, st, h, alpha, workspace=ws)
+
+
 @pytest.mark.parametrize("given", [(False, False), (True, False), (False, True), (True, True)])
 @pytest.mark.parametrize("residual", [False, True])
 def test_wanted_gradients_of_the_norm(given, residual):
