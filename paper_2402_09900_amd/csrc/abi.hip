@@ -1536,7 +1536,8 @@ GatedTiles gated_tiles(const GatedPlan& p, void* workspace, uint64_t sig) {
     // With many chains few tiles of one are under way at once, and the value before a tile
     // is soon near it; looking further costs more than it finds (T = 65536, d = 2048, 32
     // chains, bf16: 233 us, 278 with one turn before all wavefronts look).  With few it
-    // pays (d = 512, no episode's begin: 182 -> 126 us; d = 256, fp32 326 -> 211).
+    // pays (d = 512, no episode's begin: 182 -> 126 us; d = 256, fp32 326 -> 211, and 156 since
+    // what was found is read in blocks).
     t.near = p.nchains >= 16 ? kMaxPolls : 8;
     t.ctr = (uint32_t*)(ws + p.off_ctr);
     t.agg = (uint64_t*)(ws + p.off_agg);

@@ -220,7 +220,7 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs 
         }
     }
     barrier_lds();
-    if (!sLook.done) look_far<THREADS>(p.tiles, at.tile, at.chain, lane, in, sLook, enter);
+    if (!sLook.done) look_far<THREADS, BF16 ? 4 : 8>(p.tiles, at.tile, at.chain, lane, in, sLook, enter);
 
     // ---- the state that enters the run goes into z; then back with c
     float sum[F] = {};

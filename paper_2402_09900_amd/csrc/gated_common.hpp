@@ -235,7 +235,9 @@ __device__ __forceinline__ void put_incl(const GatedTiles& t, int64_t slot, int 
 // was.  First one wavefront tries: the word of the tile right before (which mostly is
 // there where chains are many), then once the four nearest tiles.  If that is not
 // enough, all wavefronts look at kNear tiles at a time, and the first puts what they
-// found together: where chains are few and long, that is what sets the pace.
+// found together: where chains are few and long, that is what sets the pace (one chain of
+// 1024 tiles, fp32, no episode's begin: 99 us, 28 without the look-back).  48 tiles take 101 there,
+// 64 93, but their LDS costs others more (8 x 4096 x 2048 bf16 117 -> 132 and 135 us).
 constexpr int kNear = 32;
 constexpr float kIsValue = 2.0f, kIsEmpty = 3.0f;                    // in the place of a decay's k, which is below 1
 struct LookBackLds {
@@ -286,8 +288,9 @@ __device__ __forceinline__ bool try_near(const GatedTiles& t, int64_t tile, int 
     return true;
 }
 
-// All wavefronts of the workgroup; `use` is called by the first with the value
-template <int THREADS, class Use>
+// All wavefronts of the workgroup; `use` is called by the first with the value.  WORDS: of a
+// batch whose latencies are one, as many as a tile's registers leave room for
+template <int THREADS, int WORDS, class Use>
 __device__ __forceinline__ void look_far(const GatedTiles& t, int64_t tile, int chain, int f, bool need, LookBackLds& lds,
                                          Use use) {
     constexpr int kEach = kNear / (THREADS / 64);
@@ -295,11 +298,11 @@ __device__ __forceinline__ void look_far(const GatedTiles& t, int64_t tile, int 
     const int64_t stride = (int64_t)t.nchains * kGateCols, from = ((tile - 1) * t.nchains + chain) * kGateCols;
     for (uint32_t polls = 0;; ++polls) {
 #pragma unroll
-        for (int n0 = 0; n0 < kEach; n0 += 4) {                      // (four at a time: few registers beside a tile's)
-            uint32_t in[4];
-            uint64_t ag[4];
+        for (int n0 = 0; n0 < kEach; n0 += WORDS) {
+            uint32_t in[WORDS];
+            uint64_t ag[WORDS];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < WORDS; ++k) {
                 const int n = wave * kEach + n0 + k;
                 in[k] = kEmpty32;
                 ag[k] = kEmpty64;
@@ -309,7 +312,7 @@ __device__ __forceinline__ void look_far(const GatedTiles& t, int64_t tile, int 
                 }
             }
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < WORDS; ++k) {
                 const int n = wave * kEach + n0 + k;
                 const bool is = in[k] != kEmpty32;
                 lds.k[n][lane] = is ? kIsValue : ag[k] != kEmpty64 ? unpack_lo(ag[k]) : kIsEmpty;
@@ -319,24 +322,41 @@ __device__ __forceinline__ void look_far(const GatedTiles& t, int64_t tile, int 
         }
         barrier_lds();
         if (wave == 0) {
+            // (a block at a time: read one by one they cost LDS's latency each)
+            constexpr int kBlock = WORDS;
             int at = kNear;                                          // the nearest value
             bool ready = !need;
-            for (int n = 0; n < kNear && !__all(ready || at < kNear); ++n) {
-                const float k = lds.k[n][lane];
-                if (at == kNear && k == kIsValue) at = n;
-                if (at == kNear && k == kIsEmpty) at = kNear + 1;    // not there yet
+            for (int n0 = 0; n0 < kNear && !__all(ready || at < kNear); n0 += kBlock) {
+                float k[kBlock];
+#pragma unroll
+                for (int j = 0; j < kBlock; ++j) k[j] = lds.k[n0 + j][lane];
+#pragma unroll
+                for (int j = 0; j < kBlock; ++j) {
+                    if (at == kNear && k[j] == kIsValue) at = n0 + j;
+                    if (at == kNear && k[j] == kIsEmpty) at = kNear + 1;    // not there yet
+                }
             }
             ready = ready || at < kNear;
             const bool all = __all(ready);
             const bool late = polls >= kMaxPolls;
             if (all || late) {
-                float v = need && at < kNear ? lds.v[at][lane] : 0.0f;
-                for (int n = kNear - 2; n >= 0; --n) {
-                    if (!__any(need && n < at && at < kNear)) continue;
-                    Decay<false> d;
-                    d.k = lds.k[n][lane];
-                    const float next = d.of(v, lds.v[n][lane]);
-                    v = need && n < at && at < kNear ? next : v;
+                const bool found = need && at < kNear;
+                float v = found ? lds.v[at][lane] : 0.0f;
+                for (int n0 = kNear - kBlock; n0 >= 0; n0 -= kBlock) {
+                    if (!__any(found && n0 < at)) continue;
+                    float k[kBlock], add[kBlock];
+#pragma unroll
+                    for (int j = 0; j < kBlock; ++j) {
+                        k[j] = lds.k[n0 + j][lane];
+                        add[j] = lds.v[n0 + j][lane];
+                    }
+#pragma unroll
+                    for (int j = kBlock - 1; j >= 0; --j) {
+                        Decay<false> d;
+                        d.k = k[j];
+                        const float next = d.of(v, add[j]);
+                        v = found && n0 + j < at ? next : v;
+                    }
                 }
                 if (!all) flag_timeout(&t.hdr->timeout);
                 use(v);

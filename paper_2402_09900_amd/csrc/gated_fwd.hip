@@ -190,7 +190,7 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_fwd_kernel(GatedFwdArgs 
         else put_agg(p.tiles, slot, lane, all.k, th);
     }
     barrier_lds();
-    if (!sLook.done) look_far<THREADS>(p.tiles, at.tile, at.chain, lane, need, sLook, enter);
+    if (!sLook.done) look_far<THREADS, BF16 ? 4 : 8>(p.tiles, at.tile, at.chain, lane, need, sLook, enter);
 
     // ---- (5)
 #pragma unroll
