@@ -2,6 +2,7 @@
 differences and known numbers, the refusals of the C and the torch layer, workspace
 sizes."""
 import ctypes
+import sys
 
 import numpy as np
 import pytest
@@ -173,6 +174,41 @@ def test_torch_layer_refusals():
         mb.norm_rows_bwd(x, torch.zeros(2, 5, 2), x[:1])
     with pytest.raises(TypeError):
         mb.norm_rows(x.half())
+
+
+def test_autograd_forms_refuse_alike():
+    x, gates, alpha = torch.zeros(2, 5, 8), torch.zeros(2, 5, 2, 8), torch.zeros(8)
+    start, state = torch.zeros(2, 5, dtype=torch.uint8), torch.zeros(2, 8)
+    ok = dict(x=x, gates=gates, alpha=alpha, start=start, state=state)
+    for error, k in ((ValueError, {}), (ValueError, dict(x=x[0])), (ValueError, dict(gates=gates[:1])),
+                     (TypeError, dict(gates=gates.bfloat16())), (TypeError, dict(x=x.half(), gates=gates.half())),
+                     (TypeError, dict(alpha=alpha.bfloat16())), (TypeError, dict(start=start.bool())),
+                     (TypeError, dict(start=None)), (TypeError, dict(state=state[:1])), (TypeError, dict(x=None)),
+                     (TypeError, dict(alpha=3.0))):
+        with pytest.raises(error):
+            mb.gated_scan(**{**ok, **k})
+    rng = torch.zeros(2, dtype=torch.int64)
+    for f in (lambda **k: mb.layer_norm(x, **k), lambda **k: mb.dropout(x, **{**dict(p=0.5, rng=rng), **k})):
+        for error, k in ((ValueError, {}), (ValueError, dict(p=0.5, rng=None)), (ValueError, dict(p=float("nan"))),
+                         (ValueError, dict(p=1.5)), (ValueError, dict(site=-1)), (ValueError, dict(site=1 << 32)),
+                         (TypeError, dict(site=1 << 64)), (TypeError, dict(p=None)), (TypeError, dict(rng=rng.int())),
+                         (TypeError, dict(residual=x.bfloat16())), (TypeError, dict(residual=x[:, :1]))):
+            with pytest.raises(error):
+                f(**k)
+    for k in (dict(weight=alpha[:3]), dict(bias=alpha.double())):
+        with pytest.raises(TypeError):
+            mb.layer_norm(x, **k)
+    with pytest.raises(ValueError):
+        mb.layer_norm(torch.tensor(1.0))
+
+
+def test_missing_layer(monkeypatch):
+    """Without the extension module the calls raise; there is nothing behind them."""
+    monkeypatch.setattr(mb, "_layer", None)
+    monkeypatch.setitem(sys.modules, "paper_2402_09900_amd._torch_layer", None)
+    monkeypatch.delattr(sys.modules["paper_2402_09900_amd"], "_torch_layer", raising=False)
+    with pytest.raises(mb.MemoroidError, match="not built"):
+        mb.dropout(torch.zeros(2, 8), 0.0, None)
 
 
 # ---------------------------------------------------------------- reference

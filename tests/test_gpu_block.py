@@ -276,6 +276,23 @@ def test_workspaces():
             mb.norm_rows_bwd(x, st, h, alpha, workspace=ws)
 
 
+def test_out_of_memory():
+    """No memory for an output is torch's error for it, and the call can be made again."""
+    announce("nodes out of memory")
+    x = torch.zeros(1 << 18, 1 << 10, device=DEV)
+    rng = torch.tensor([SEED, 1], dtype=torch.int64, device=DEV)
+    torch.cuda.empty_cache()
+    total = torch.cuda.get_device_properties(0).total_memory
+    torch.cuda.set_per_process_memory_fraction((torch.cuda.memory_reserved() + (1 << 28)) / total)
+    try:
+        for f in (lambda: mb.drop_rows(x, 0.5, rng), lambda: mb.dropout(x, 0.5, rng), lambda: mb.layer_norm(x)):
+            with pytest.raises(torch.OutOfMemoryError):
+                f()
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
+    assert torch.equal(mb.drop_rows(x, 0.5, rng), x)
+
+
 @pytest.mark.parametrize("given", [(False, False), (True, False), (False, True), (True, True)])
 @pytest.mark.parametrize("residual", [False, True])
 def test_wanted_gradients_of_the_norm(given, residual):
