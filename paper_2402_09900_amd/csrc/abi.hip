@@ -1546,8 +1546,8 @@ GatedTiles gated_tiles(const GatedPlan& p, void* workspace, uint64_t sig) {
     t.sig = sig;
     return t;
 }
-int64_t gated_tile(int dtype, bool grad) {
-    return (grad ? gate_bwd_shape(dtype == MEMOROID_BF16) : gate_fwd_shape(dtype == MEMOROID_BF16)).tile();
+int64_t gated_tile(int64_t T, int dtype, bool grad) {
+    return (grad ? gate_bwd_shape(dtype == MEMOROID_BF16, T) : gate_fwd_shape(dtype == MEMOROID_BF16, T)).tile();
 }
 // whether rows and addresses are multiples of f elements
 bool gated_full(int64_t d, int dtype, int f, std::initializer_list<const void*> ps) {
@@ -1584,7 +1584,7 @@ size_t memoroid_scan_gated_workspace_bytes(int64_t B, int64_t T, int64_t d, int 
     bool empty;
     if (gated_check(B, T, d, dtype, &empty) != MEMOROID_OK || empty) return 0;
     GatedPlan p;
-    plan_gated(B, T, d, gated_tile(dtype, false), false, &p);
+    plan_gated(B, T, d, gated_tile(T, dtype, false), false, &p);
     return p.total;
 }
 
@@ -1599,7 +1599,7 @@ int memoroid_scan_gated(const void* x, const void* gates, const float* alpha, co
         !floats_ok({alpha, state_in, state_out, states}))
         return MEMOROID_EINVAL;
     GatedPlan p;
-    plan_gated(B, T, d, gated_tile(dtype, false), false, &p);
+    plan_gated(B, T, d, gated_tile(T, dtype, false), false, &p);
     if (!workspace || workspace_bytes < p.total) return MEMOROID_EWORKSPACE;
     if (!aligned(workspace, 16)) return MEMOROID_EINVAL;
     GatedFwdArgs a{};
@@ -1625,7 +1625,7 @@ size_t memoroid_scan_gated_bwd_workspace_bytes(int64_t B, int64_t T, int64_t d, 
     bool empty;
     if (gated_check(B, T, d, dtype, &empty) != MEMOROID_OK || empty) return 0;
     GatedPlan p;
-    plan_gated(B, T, d, gated_tile(dtype, true), true, &p);
+    plan_gated(B, T, d, gated_tile(T, dtype, true), true, &p);
     return p.total;
 }
 
@@ -1642,7 +1642,7 @@ int memoroid_scan_gated_bwd(const void* x, const void* gates, const float* alpha
         !floats_ok({alpha, states, grad_state_out, grad_alpha, grad_state_in}))
         return MEMOROID_EINVAL;
     GatedPlan p;
-    plan_gated(B, T, d, gated_tile(dtype, true), true, &p);
+    plan_gated(B, T, d, gated_tile(T, dtype, true), true, &p);
     if (!workspace || workspace_bytes < p.total) return MEMOROID_EWORKSPACE;
     if (!aligned(workspace, 16)) return MEMOROID_EINVAL;
     GatedBwdArgs a{};

@@ -31,7 +31,6 @@ template <bool BF16, bool FULL, int POL, int L, int THREADS, int WAVES>
 __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs p) {
     constexpr int kLd = POL == kStreamAll ? kNt : 0, kSt = POL != kCached ? kNt : 0;
     constexpr int F = 2, kRow = Lanes<F, THREADS>::kRow, kRuns = Lanes<F, THREADS>::kRuns, kSteps = kRuns * L;
-    static_assert(kSteps % kGateStateSteps == 0, "a tile starts from a state that was kept");
     static_assert(L <= kRow && L < 32, "flags: a lane per step");
     __shared__ uint32_t s_tile;
     // per run: its rates' sum, its decay, what it adds to h and to c (then the state that enters
@@ -211,7 +210,7 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs 
         }
     } else if (wave == 2) {
         const int64_t ns = (p.T + kGateStateSteps - 1) / kGateStateSteps;
-        float v = in ? p.states[(b * ns + tile * (kSteps / kGateStateSteps)) * p.d + f] : 0.0f;
+        float v = in ? p.states[(b * ns + tile * kSteps / kGateStateSteps) * p.d + f] : 0.0f;
 #pragma unroll
         for (int n = 0; n < kRuns; ++n) {
             const float add = sH[n][lane];
@@ -315,11 +314,17 @@ __global__ __launch_bounds__(1024) void gated_alpha_kernel(const float* part, co
     }
 }
 
-template <bool BF16, bool FULL, int POL>
-void launch(const GatedBwdArgs& a, hipStream_t s) {
-    constexpr GateShape sh = gate_bwd_shape(BF16);
+template <bool BF16, bool FULL, int POL, int UPTO>
+void launch_for(const GatedBwdArgs& a, hipStream_t s) {
+    constexpr GateShape sh = gate_bwd_shape(BF16, UPTO);
+    static_assert(sh.tile() % kGateStateSteps == 0 || UPTO <= sh.tile(), "a tile starts from a state that was kept");
     hipLaunchKernelGGL((gated_bwd_kernel<BF16, FULL, POL, sh.steps, sh.threads, sh.waves>),
                        dim3((unsigned)(a.tiles.nt * a.tiles.nchains)), dim3(sh.threads), 0, s, a);
+}
+template <bool BF16, bool FULL, int POL>
+void launch(const GatedBwdArgs& a, hipStream_t s) {
+    if (a.T <= 32) launch_for<BF16, FULL, POL, 32>(a, s);
+    else launch_for<BF16, FULL, POL, 33>(a, s);
 }
 // (rows that lanes cannot take whole are not whole lines either)
 template <bool BF16>

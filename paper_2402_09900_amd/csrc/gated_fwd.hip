@@ -238,11 +238,17 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_fwd_kernel(GatedFwdArgs 
     }
 }
 
-template <bool BF16, bool FULL, int POL>
-void launch(const GatedFwdArgs& a, hipStream_t s) {
-    constexpr GateShape sh = gate_fwd_shape(BF16);
+template <bool BF16, bool FULL, int POL, int UPTO>
+void launch_for(const GatedFwdArgs& a, hipStream_t s) {
+    constexpr GateShape sh = gate_fwd_shape(BF16, UPTO);
     hipLaunchKernelGGL((gated_fwd_kernel<BF16, FULL, POL, sh.steps, sh.threads, sh.waves>),
                        dim3((unsigned)(a.tiles.nt * a.tiles.nchains)), dim3(sh.threads), 0, s, a);
+}
+template <bool BF16, bool FULL, int POL>
+void launch(const GatedFwdArgs& a, hipStream_t s) {
+    if (a.T <= 32) launch_for<BF16, FULL, POL, 32>(a, s);
+    else if (a.T <= 64) launch_for<BF16, FULL, POL, 64>(a, s);
+    else launch_for<BF16, FULL, POL, 65>(a, s);
 }
 // (rows that lanes cannot take whole are not whole lines either)
 template <bool BF16>

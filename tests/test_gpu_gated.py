@@ -146,6 +146,14 @@ def test_wide_and_many(dtype, B, T, d):
     check(dtype, B, T, d, seed=T)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,T,d", [(61, 4, 688), (5, 31, 70), (5, 32, 65), (5, 33, 64), (2, 63, 130), (9, 64, 129), (2, 66, 3)])
+def test_short_tapes(dtype, B, T, d):
+    """Tapes around the sizes where the tiles change."""
+    check(dtype, B, T, d, seed=T)
+    check(dtype, B, T, d, "none", seed=T + 1)
+
+
 @pytest.mark.parametrize("need", [(0,), (1,), (2,), (3,), (0, 3)])
 def test_some_gradients(need):
     """Whichever inputs want a gradient, it is the one that all of them get; outputs that
