@@ -1537,8 +1537,9 @@ GatedTiles gated_tiles(const GatedPlan& p, void* workspace, uint64_t sig) {
     // is soon near it; looking further costs more than it finds (T = 65536, d = 2048, 32
     // chains, bf16: 233 us, 278 with one turn before all wavefronts look).  With few it
     // pays (d = 512, no episode's begin: 182 -> 126 us; d = 256, fp32 326 -> 211, and 156 since
-    // what was found is read in blocks).
-    t.near = p.nchains >= 16 ? kMaxPolls : 8;
+    // what was found is read in blocks), after some turns where begins are frequent (T = 32768, d =
+    // 256, fp32, gradient: 70.1 us after three, 68.1 after 16; d = 512, bf16, no begin: 174 and 207).
+    t.near = p.nchains >= 16 ? kMaxPolls : 4;
     t.ctr = (uint32_t*)(ws + p.off_ctr);
     t.agg = (uint64_t*)(ws + p.off_agg);
     t.incl = (uint32_t*)(ws + p.off_incl);
