@@ -323,6 +323,14 @@ py::object result(const variable_list& got) {
     return got.size() == 1 ? py::cast(got[0]) : py::object(py::make_tuple(got[0], got[1]));
 }
 
+// Whether a call belongs in the engine's graph; outside it nothing is kept for a gradient
+bool in_graph(std::initializer_list<const Tensor*> inputs) {
+    if (!at::GradMode::is_enabled()) return false;
+    for (const Tensor* t : inputs)
+        if (t->defined() && t->requires_grad()) return true;
+    return false;
+}
+
 py::object scan_gated(const Tensor& x, const Tensor& gates, const Tensor& alpha, const Tensor& start, const OptTensor& state_,
                       bool final_state, bool keep_states, const OptTensor& callers) {
     const Tensor state = given(state_);
@@ -408,6 +416,10 @@ py::object gated_scan(const Tensor& x, const Tensor& gates, const Tensor& alpha,
     check_tapes(x, gates, alpha, start);
     check_state(x, s, "state must be float32 [B,d]");
     check_places({&x, &gates, &alpha, &start, &s});
+    if (!in_graph({&x, &gates, &alpha, &s})) {
+        const Scanned got = unlocked([&] { return gated_forward(x, gates, alpha, start, s, final_state, false, Tensor()); });
+        return result({got.h, got.last});
+    }
     return result(unlocked([&] { return GatedScan::apply(x, gates, alpha, start, state, final_state); }));
 }
 
@@ -417,6 +429,10 @@ py::object layer_norm(const Tensor& x, const OptTensor& weight, const OptTensor&
     check_rows(x, res, p, numbers, site);
     check_weights(x, w, b);
     check_places({&x, &res, &w, &b, &numbers});
+    if (!in_graph({&x, &res, &w, &b})) {
+        const Normed got = unlocked([&] { return norm_forward(x, w, b, eps, res, p, numbers, site, false); });
+        return result({got.y, got.s});
+    }
     return result(unlocked([&] { return LayerNorm::apply(x, weight, bias, eps, residual, p, rng, site); }));
 }
 
@@ -424,6 +440,7 @@ Tensor dropout(const Tensor& x, double p, const OptTensor& rng, int64_t site, co
     const Tensor numbers = given(rng), res = given(residual);
     check_rows(x, res, p, numbers, site);
     check_places({&x, &res, &numbers});
+    if (!in_graph({&x, &res})) return unlocked([&] { return drop(x, p, numbers, site, res); });
     return unlocked([&] { return Dropout::apply(x, p, rng, site, residual); });
 }
 
