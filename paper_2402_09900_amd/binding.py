@@ -18,8 +18,10 @@ runs in the library's HIP kernels:
   ``retention``, ``qk_rotate``, ``gated_scan``, ``layer_norm`` and ``dropout`` are
   the differentiable forms (``torch.autograd.Function``, and nodes of torch's
   engine in C++ where the layer is: the gated recurrence, layer norm and dropout,
-  csrc/torch_layer.cpp).  A backward pass that is to be captured into a graph needs, as with torch's own operators, leaves that no
-  graph of autograd built outside the capture still holds.
+  csrc/torch_layer.cpp).  None has a derivative in forward mode: inputs with tangents
+  are refused.  A backward pass that is to be captured into a graph needs, as with
+  torch's own operators, leaves that no graph of autograd built outside the capture
+  still holds.
 
 Loading fails loudly (``MemoroidError``) if the shared library is missing:
 there is no fallback implementation.

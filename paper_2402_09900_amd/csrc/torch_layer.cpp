@@ -323,6 +323,13 @@ py::object result(const variable_list& got) {
     return got.size() == 1 ? py::cast(got[0]) : py::object(py::make_tuple(got[0], got[1]));
 }
 
+// Forward mode has no derivative here, and a result without a tangent would count as one
+// whose tangent is zero: refused wherever forward mode is on, under no_grad too
+void refuse_tangents(std::initializer_list<const Tensor*> inputs) {
+    for (const Tensor* t : inputs)
+        if (t->defined() && t->_fw_grad(0).defined() && c10::AutogradState::get_tls_state().get_fw_grad_mode())
+            throw std::runtime_error("the gated recurrence, layer norm and dropout have no derivative in forward mode");
+}
 // Whether a call belongs in the engine's graph; outside it nothing is kept for a gradient
 bool in_graph(std::initializer_list<const Tensor*> inputs) {
     if (!at::GradMode::is_enabled()) return false;
@@ -363,6 +370,7 @@ Tensor gated_step(const Tensor& x, const Tensor& gates, const Tensor& alpha, con
     check_gates(x, gates, alpha);
     type_if(start.defined() && !is(start, at::kByte, {x.size(0)}), "start must be uint8 [B]");
     check_state(x, state, "state must be float32 [B,d]");
+    refuse_tangents({&x, &gates, &alpha, &state});
     if (at::GradMode::is_enabled() &&
         (x.requires_grad() || gates.requires_grad() || alpha.requires_grad() || state.requires_grad()))
         throw std::runtime_error("gated_step has no gradient: call it under torch.no_grad(), or gated_scan() on tapes of one step");
@@ -415,6 +423,7 @@ py::object gated_scan(const Tensor& x, const Tensor& gates, const Tensor& alpha,
     const Tensor s = given(state);
     check_tapes(x, gates, alpha, start);
     check_state(x, s, "state must be float32 [B,d]");
+    refuse_tangents({&x, &gates, &alpha, &s});
     check_places({&x, &gates, &alpha, &start, &s});
     if (!in_graph({&x, &gates, &alpha, &s})) {
         const Scanned got = unlocked([&] { return gated_forward(x, gates, alpha, start, s, final_state, false, Tensor()); });
@@ -428,6 +437,7 @@ py::object layer_norm(const Tensor& x, const OptTensor& weight, const OptTensor&
     const Tensor w = given(weight), b = given(bias), res = given(residual), numbers = given(rng);
     check_rows(x, res, p, numbers, site);
     check_weights(x, w, b);
+    refuse_tangents({&x, &res, &w, &b});
     check_places({&x, &res, &w, &b, &numbers});
     if (!in_graph({&x, &res, &w, &b})) {
         const Normed got = unlocked([&] { return norm_forward(x, w, b, eps, res, p, numbers, site, false); });
@@ -439,6 +449,7 @@ py::object layer_norm(const Tensor& x, const OptTensor& weight, const OptTensor&
 Tensor dropout(const Tensor& x, double p, const OptTensor& rng, int64_t site, const OptTensor& residual) {
     const Tensor numbers = given(rng), res = given(residual);
     check_rows(x, res, p, numbers, site);
+    refuse_tangents({&x, &res});
     check_places({&x, &res, &numbers});
     if (!in_graph({&x, &res})) return unlocked([&] { return drop(x, p, numbers, site, res); });
     return unlocked([&] { return Dropout::apply(x, p, rng, site, residual); });
