@@ -19,7 +19,9 @@ runs in the library's HIP kernels:
   the differentiable forms (``torch.autograd.Function``, and nodes of torch's
   engine in C++ where the layer is: the gated recurrence, layer norm and dropout,
   csrc/torch_layer.cpp).  None has a derivative in forward mode: inputs with tangents
-  are refused.  A backward pass that is to be captured into a graph needs, as with
+  are refused.  The C++ calls are not seen by what records torch's operators and refuse
+  to be traced (``torch.jit.trace``, ``make_fx``, fake tensors; graphs of the device
+  are another matter).  A backward pass that is to be captured into a graph needs, as with
   torch's own operators, leaves that no graph of autograd built outside the capture
   still holds.
 

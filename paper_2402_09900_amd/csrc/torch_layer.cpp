@@ -10,6 +10,8 @@
 #include <torch/extension.h>
 
 #include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
+#include <torch/csrc/jit/frontend/tracer.h>
 
 #include "memoroid.h"
 
@@ -36,13 +38,31 @@ bool is(const Tensor& t, at::ScalarType type, Shape shape) {
 }
 Tensor given(const OptTensor& t) { return t.has_value() ? *t : Tensor(); }
 
-// Device memory that kernels may index: of one device, without gaps
+// The library is no torch operator: what records operators (a trace, a graph of them, shapes
+// without memory) would see the results' new memory and not the call that fills it.  Modes
+// that only look on are no reason to refuse.
+void refuse_recording() {
+    using c10::impl::TorchDispatchModeKey;
+    using Modes = c10::impl::TorchDispatchModeTLS;
+    bool records = torch::jit::tracer::isTracing();
+    if (Modes::any_modes_set())
+        for (const auto key : {TorchDispatchModeKey::FAKE, TorchDispatchModeKey::PROXY, TorchDispatchModeKey::FUNCTIONAL})
+            records = records || Modes::get_mode(key).has_value();
+    if (records)
+        throw std::runtime_error("calls of the gated recurrence, layer norm and dropout cannot be traced or run without memory");
+}
+struct Unrecorded {
+    Unrecorded() { refuse_recording(); }
+};
+// Device memory that kernels may index: of one device, without gaps, there
 void check_places(std::initializer_list<const Tensor*> tensors) {
     const Tensor* first = nullptr;
     for (const Tensor* t : tensors) {
         if (!t->defined()) continue;
         value_if(!t->is_cuda(), "tensors must live on a CUDA (HIP) device");
         value_if(!t->is_contiguous(), "tensors must be contiguous");
+        // (a tensor of no memory of its own, as in functionalize: an optional one would count as not given)
+        value_if(t->numel() != 0 && !t->data_ptr(), "tensors must have memory");
         if (!first) first = t;
         value_if(t->device() != first->device(), "tensors must live on one device");
     }
@@ -248,6 +268,7 @@ struct GatedScan : Function<GatedScan> {
         return final_state ? variable_list{got.h, got.last} : variable_list{got.h};
     }
     static variable_list backward(AutogradContext* ctx, variable_list grads) {
+        refuse_recording();
         const variable_list s = ctx->get_saved_variables();
         const Tensor gh = grads[0].defined() ? grads[0].contiguous() : at::zeros_like(s[0]);
         // (inputs that are tensors are counted: x, gates, alpha, start, state)
@@ -270,6 +291,7 @@ struct LayerNorm : Function<LayerNorm> {
         return got.s.defined() ? variable_list{got.y, got.s} : variable_list{got.y};
     }
     static variable_list backward(AutogradContext* ctx, variable_list grads) {
+        refuse_recording();
         const variable_list s = ctx->get_saved_variables();
         const Tensor gy = grads[0].defined() ? grads[0].contiguous() : at::zeros_like(s[0]);
         // (inputs that are tensors are counted: x, weight and bias where they are given)
@@ -292,6 +314,7 @@ struct Dropout : Function<Dropout> {
         return drop(x, p, given(rng), site, given(residual));
     }
     static variable_list backward(AutogradContext* ctx, variable_list grads) {
+        refuse_recording();
         const double p = ctx->saved_data["p"].toDouble();
         const Tensor& g = grads[0];
         variable_list got(2);
@@ -458,15 +481,16 @@ Tensor dropout(const Tensor& x, double p, const OptTensor& rng, int64_t site, co
 }  // namespace
 
 PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
-    m.def("scan_gated", scan_gated);
-    m.def("scan_gated_bwd", scan_gated_bwd);
-    m.def("gated_step", gated_step);
-    m.def("drop_rows", drop_rows);
-    m.def("norm_rows", norm_rows);
-    m.def("norm_rows_bwd", norm_rows_bwd);
-    m.def("gated_scan", gated_scan);
-    m.def("layer_norm", layer_norm);
-    m.def("dropout", dropout);
+    const py::call_guard<Unrecorded> unrecorded;
+    m.def("scan_gated", scan_gated, unrecorded);
+    m.def("scan_gated_bwd", scan_gated_bwd, unrecorded);
+    m.def("gated_step", gated_step, unrecorded);
+    m.def("drop_rows", drop_rows, unrecorded);
+    m.def("norm_rows", norm_rows, unrecorded);
+    m.def("norm_rows_bwd", norm_rows_bwd, unrecorded);
+    m.def("gated_scan", gated_scan, unrecorded);
+    m.def("layer_norm", layer_norm, unrecorded);
+    m.def("dropout", dropout, unrecorded);
     py::register_local_exception_translator([](std::exception_ptr e) {
         try {
             if (e) std::rethrow_exception(e);

@@ -3,9 +3,10 @@ ways of calling: what it cannot answer it refuses, before it looks where tensors
 that the refusals are tested here on the CPU."""
 import pytest
 
+from conftest import announce
+
 torch = pytest.importorskip("torch")
 import torch.autograd.forward_ad as fwd  # noqa: E402
-
 from paper_2402_09900_amd import binding as mb  # noqa: E402
 
 X, GATES, ALPHA = torch.zeros(2, 5, 8), torch.zeros(2, 5, 2, 8), torch.zeros(8)
@@ -46,3 +47,120 @@ def test_functional_jvp_is_refused(name):
     f, inputs = DIFFERENTIABLE[name]
     with pytest.raises(RuntimeError, match="forward mode"):
         torch.func.jvp(lambda x: f(**{**inputs, "x": x}), (inputs["x"],), (torch.ones_like(inputs["x"]),))
+
+
+# ------------------------------------------------------------------ recording
+
+STATS, KEPT = torch.zeros(2, 5, 2), torch.zeros(2, 1, 8)
+RAW = {
+    "scan_gated": lambda x: mb.scan_gated(x, GATES, ALPHA, START),
+    "scan_gated_bwd": lambda x: mb.scan_gated_bwd(x, GATES, ALPHA, START, KEPT, x),
+    "norm_rows": lambda x: mb.norm_rows(x, ALPHA),
+    "norm_rows_bwd": lambda x: mb.norm_rows_bwd(x, STATS, x, ALPHA),
+    "drop_rows": lambda x: mb.drop_rows(x, 0.5, RNG),
+}
+
+
+def of_x(name):
+    f, inputs = DIFFERENTIABLE[name]
+    return lambda x: f(**{**inputs, "x": x})
+
+
+def input_of(name):
+    return ROW if name == "gated_step" else X
+
+
+FORMS = {**RAW, **{name: of_x(name) for name in DIFFERENTIABLE}}
+
+
+@pytest.mark.parametrize("name", FORMS)
+@pytest.mark.parametrize("grad", [False, True])
+def test_traces_are_refused(name, grad):
+    """A trace would hold the new memory of the results and not the call that fills it."""
+    x = input_of(name).clone().requires_grad_(grad and name != "gated_step")
+    with pytest.raises(RuntimeError, match="cannot be traced"):
+        torch.jit.trace(FORMS[name], (x,))
+    with pytest.raises(ValueError, match="CUDA"):                    # (and again afterwards as before)
+        FORMS[name](x)
+
+
+@pytest.mark.parametrize("name", FORMS)
+@pytest.mark.parametrize("mode", ["real", "fake", "symbolic"])
+def test_graphs_of_operators_are_refused(name, mode):
+    from torch.fx.experimental.proxy_tensor import make_fx
+
+    with pytest.raises(RuntimeError, match="cannot be traced"):
+        make_fx(FORMS[name], tracing_mode=mode)(input_of(name))
+
+
+@pytest.mark.parametrize("name", FORMS)
+def test_fake_tensors_are_refused(name):
+    from torch._subclasses.fake_tensor import FakeTensorMode
+
+    with FakeTensorMode(allow_non_fake_inputs=True) as mode:
+        x = mode.from_tensor(input_of(name))
+        with pytest.raises(RuntimeError, match="cannot be traced"):
+            FORMS[name](x)
+
+
+def test_other_modes_are_let_through():
+    """A dispatch mode that only looks on (a count of operations, checkpointing) does not
+    stand in the way."""
+    from torch.utils.flop_counter import FlopCounterMode
+
+    with FlopCounterMode(display=False), pytest.raises(ValueError, match="CUDA"):
+        mb.layer_norm(X)
+
+
+@pytest.mark.parametrize("name", FORMS)
+@pytest.mark.parametrize("through", [torch.func.vmap, lambda f: torch.func.grad(lambda x: f(x).sum()), torch.func.functionalize])
+def test_transforms_are_refused(name, through):
+    x = input_of(name)
+    if through is torch.func.vmap:
+        x = torch.stack([x, x])
+    with pytest.raises((RuntimeError, ValueError)):
+        through(FORMS[name])(x)
+
+
+@pytest.mark.gpu
+def test_graph_of_a_backward_pass_is_refused():
+    """A graph of operators that begins behind the forward call; afterwards the same pass
+    gives the gradient."""
+    from torch.fx.experimental.proxy_tensor import make_fx
+
+    announce("transforms: backward pass in a graph of operators")
+    dev = "cuda:0"
+    x = torch.randn(2, 5, 8, device=dev, requires_grad=True)
+    gates, alpha, start, rng = GATES.to(dev), ALPHA.to(dev) + 0.5, START.to(dev), RNG.to(dev)
+    for y in (mb.gated_scan(x, gates, alpha, start), mb.layer_norm(x), mb.dropout(x, 0.5, rng)):
+        def back(g, y=y):
+            return torch.autograd.grad(y, x, g, retain_graph=True)[0]
+
+        up = torch.randn_like(y)
+        want = back(up)
+        with pytest.raises(RuntimeError, match="cannot be traced"):
+            make_fx(lambda g: back(g))(up)
+        assert torch.equal(back(up), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("through", ["vmap", "grad", "functionalize"])
+def test_tensors_without_memory_are_refused(through):
+    """On the device, where nothing else is wrong with them, an optional input too: it would
+    count as not given."""
+    announce("transforms: no memory in %s" % through)
+    dev = "cuda:0"
+    x, row, alpha = X.to(dev), ROW.to(dev), ALPHA.to(dev)
+    gates, row_gates, start, state = GATES.to(dev), ROW_GATES.to(dev), START.to(dev), STATE.to(dev)
+    wrap = dict(vmap=lambda f: lambda t: torch.func.vmap(f)(torch.stack([t, t])),
+                grad=lambda f: torch.func.grad(lambda t: f(t).sum()), functionalize=torch.func.functionalize)[through]
+    calls = [(mb.layer_norm, x), (lambda r: mb.layer_norm(x, residual=r)[0], x), (lambda w: mb.layer_norm(x, w), alpha),
+             (lambda w: mb.layer_norm(x, None, w), alpha), (lambda r: mb.norm_rows(x, residual=r)[0], x),
+             (lambda t: mb.dropout(t, 0.0, None), x), (lambda r: mb.dropout(x, 0.0, None, residual=r), x),
+             (lambda r: mb.drop_rows(x, 0.0, None, residual=r), x), (lambda t: mb.gated_scan(t, gates, alpha, start), x),
+             (lambda s: mb.gated_scan(x, gates, alpha, start, s), state), (lambda s: mb.scan_gated(x, gates, alpha, start, s), state),
+             (lambda t: mb.gated_step(t, row_gates, alpha, state), row)]
+    for n, (f, t) in enumerate(calls):
+        with pytest.raises((RuntimeError, ValueError)):
+            wrap(f)(t)
+            assert False, "call %d went through" % n
