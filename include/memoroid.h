@@ -558,7 +558,8 @@ int memoroid_scan_gated(const void* x, const void* gates, const float* alpha, co
  *     lam_t = g_t + [t+1 < T and step t+1 is not a begin] a_{t+1} lam_{t+1} + [t == T-1] G,
  *     hp_t = h_{t-1}, 0 at a begin step,   m_t = sqrt(1 - a_t^2),
  *     dx_t = lam_t m_t sig(i_t),   di_t = lam_t b_t (1 - sig(i_t)),
- *     du_t = lam_t a_t (sig(i_t) x_t a_t / m_t - hp_t)   (no first term where m_t is 0),
+ *     du_t = lam_t a_t (sig(i_t) x_t a_t / m_t - hp_t)   (no first term where m_t is 0,
+ *                                                         as which one below 2^-63 counts),
  *     dr_t = du_t u_t (1 - sig(r_t)),   dalpha = sign(alpha) sum du_t sig(r_t)  (sign(0) = 0),
  *     dstate_in = [step 0 is not a begin] a_0 lam_0.
  *

@@ -123,8 +123,9 @@ __global__ __launch_bounds__(THREADS, WAVES) void gated_bwd_kernel(GatedBwdArgs 
                 const float gr = sigmoid<BF16>(r[s].get(e)), gi = sigmoid<BF16>(i[s].get(e)), gu = rate[e] * gr;
                 const Decay<SLOW.value, BF16> d(gu);
                 const float w = d.taken(), m2 = w * (2.0f - w);
-                // (where nothing decays, m = 0 and 1 / m is to stay finite)
-                const float rm = __builtin_amdgcn_rsqf(__builtin_fmaxf(m2, 0x1p-100f)), m = m2 * rm;
+                // (where nothing decays, m = 0: no 1 / m, and the term that has it none either; the
+                // root forward has no normal result there)
+                const float rm = m2 >= 0x1p-126f ? __builtin_amdgcn_rsqf(m2) : 0.0f, m = m2 * rm;
                 const float xs = x[s].get(e) * gi, v = m * xs;
                 const bool begin = BEGINS.value && (begins >> s & 1u);
                 k[s][e] = d.k;
