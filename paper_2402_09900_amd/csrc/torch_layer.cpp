@@ -11,6 +11,7 @@
 
 #include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/jit/frontend/tracer.h>
 
 #include "memoroid.h"
@@ -243,18 +244,24 @@ Tensor drop(const Tensor& x, double p, const Tensor& rng, int64_t site, const Te
 // ------------------------------------------------------------- autograd nodes
 // (gradients that arrive are like their outputs: the engine has seen to it)
 
-// Gradients here have none of their own: where the engine builds a graph of them, this
-// stands in it and refuses to be differentiated.
-struct Once : Function<Once> {
-    static Tensor forward(AutogradContext*, const Tensor& t) { return t.detach(); }
-    static variable_list backward(AutogradContext*, variable_list) {
-        throw std::runtime_error("trying to differentiate twice a function that has one derivative");
-    }
-};
-variable_list once(variable_list got) {
-    if (at::GradMode::is_enabled())
-        for (Tensor& t : got)
-            if (t.defined()) t = Once::apply(t.detach().requires_grad_());
+// Gradients here have none of their own.  Where the engine builds a graph of them, a node
+// that raises stands behind them, in front of all that they hang on: the inputs of the node
+// that has formed them, and the gradients that it was given.
+variable_list once(variable_list got, const variable_list& upstream) {
+    if (!at::GradMode::is_enabled()) return got;
+    torch::autograd::edge_list to;
+    for (const auto& e : torch::autograd::get_current_node()->next_edges())
+        if (e.is_valid()) to.push_back(e);
+    for (const Tensor& g : upstream)
+        if (g.defined() && g.requires_grad()) to.push_back(torch::autograd::impl::gradient_edge(g));
+    const auto node = std::make_shared<torch::autograd::Error>(
+        "trying to differentiate twice a function that has one derivative", std::move(to));
+    for (Tensor& t : got)
+        if (t.defined()) {
+            // (two gradients may be one tensor, which could stand behind one of them only)
+            t = t.detach();
+            torch::autograd::create_gradient_edge(t, node);
+        }
     return got;
 }
 
@@ -274,7 +281,7 @@ struct GatedScan : Function<GatedScan> {
         // (inputs that are tensors are counted: x, gates, alpha, start, state)
         const bool want_state = ctx->saved_data["state"].toBool() && ctx->needs_input_grad(4);
         const variable_list g = once(gated_backward(s[0], s[1], s[2], s[3], s[4], gh, grads.size() > 1 ? dense(grads[1]) : Tensor(),
-                                                    ctx->needs_input_grad(2), want_state, Tensor()));
+                                                    ctx->needs_input_grad(2), want_state, Tensor()), grads);
         return {g[0], g[1], g[2], Tensor(), g[3], Tensor()};
     }
 };
@@ -299,7 +306,7 @@ struct LayerNorm : Function<LayerNorm> {
         const variable_list g =
             once(norm_backward(s[0], s[4], gy, s[1], s[2], grads.size() > 1 ? dense(grads[1]) : Tensor(),
                                ctx->saved_data["p"].toDouble(), s[3], ctx->saved_data["site"].toInt(),
-                               weight && ctx->needs_input_grad(1), bias && ctx->needs_input_grad(weight ? 2 : 1), Tensor()));
+                               weight && ctx->needs_input_grad(1), bias && ctx->needs_input_grad(weight ? 2 : 1), Tensor()), grads);
         return {g[0], g[2], g[3], Tensor(), g[1], Tensor(), Tensor(), Tensor()};
     }
 };
@@ -317,12 +324,11 @@ struct Dropout : Function<Dropout> {
         refuse_recording();
         const double p = ctx->saved_data["p"].toDouble();
         const Tensor& g = grads[0];
-        variable_list got(2);
-        if (ctx->needs_input_grad(0))
-            got[0] = p > 0 ? drop(g.contiguous(), p, ctx->get_saved_variables()[0], ctx->saved_data["site"].toInt(), Tensor()) : g;
-        if (ctx->saved_data["residual"].toBool()) got[1] = g;
-        got = once(got);
-        return {got[0], Tensor(), Tensor(), Tensor(), got[1]};
+        Tensor gx;
+        if (p == 0) gx = g;
+        else if (ctx->needs_input_grad(0))
+            gx = once({drop(g.contiguous(), p, ctx->get_saved_variables()[0], ctx->saved_data["site"].toInt(), Tensor())}, grads)[0];
+        return {gx, Tensor(), Tensor(), Tensor(), ctx->saved_data["residual"].toBool() ? g : Tensor()};
     }
 };
 
