@@ -625,8 +625,10 @@ int memoroid_dropout(const void* x, const void* residual, const int64_t* rng, vo
  *   stats      optional out [n][2] fp32: mean and rstd, for the gradient.
  *   eps >= 0, finite.  1 <= d <= 16384, n < 2^31 (MEMOROID_EUNSUPPORTED otherwise).  A row
  *   whose values are all equal has no deviation but the rounding of its mean; with eps = 0
- *   it may come out as NaN.  A NaN or Inf stays in its row.  A row whose squared deviations
- *   add up past fp32's range (elements from 2^57 on can) comes out as the bias, rstd 0.  No
+ *   it may come out as NaN, as may one whose squared deviations are all below fp32's range
+ *   (deviations below 2^-63).  A NaN or Inf stays in its row.  A row whose squared deviations
+ *   add up past fp32's range (elements from 2^57 on can) comes out as the bias, rstd 0, as
+ *   long as each s and its deviation are finite, whatever their sum; else as NaN.  No
  *   workspace.
  * ------------------------------------------------------------------------ */
 int memoroid_layer_norm(const void* x, const void* residual, const float* weight, const float* bias,

@@ -184,6 +184,11 @@ __device__ __forceinline__ Place place_of(int64_t n, int64_t d, int64_t rows) {
     return p;
 }
 
+// A row's values are summed up as 2^-14 of them, which costs nothing and changes no digit: the sum
+// of as many as a row may have stays in the range that they are in
+constexpr float kSumScale = 0x1p-14f;
+static_assert((float)kNormMaxDim * kSumScale <= 1.0f, "the longest rows");
+
 template <bool BF16, bool EVEN, int POL, int WAVES, int CH, int R>
 __global__ __launch_bounds__(threads_of(WAVES)) void norm_kernel(NormArgs p) {
     __shared__ float lds[2][R][WAVES];
@@ -240,7 +245,7 @@ __global__ __launch_bounds__(threads_of(WAVES)) void norm_kernel(NormArgs p) {
                     o.store(p.s, row * p.d + col, n);
                 }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum[r] += s[r][c][e];
+                for (int e = 0; e < 8; ++e) sum[r] = __builtin_fmaf(s[r][c][e], kSumScale, sum[r]);
             }
         }
         row_sums<WAVES, R>(sum, at.lanes, lds, turn);
@@ -248,7 +253,7 @@ __global__ __launch_bounds__(threads_of(WAVES)) void norm_kernel(NormArgs p) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             // (divided, not times 1 / d: a mean that a float holds comes out as it)
-            mean[r] = sum[r] / (float)p.d;
+            mean[r] = sum[r] / (float)p.d * (1.0f / kSumScale);
             sum[r] = 0.0f;
 #pragma unroll
             for (int c = 0; c < CH; ++c)
