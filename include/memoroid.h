@@ -537,9 +537,13 @@ int memoroid_rotate_qk_bwd(const void* q, const void* k, const int32_t* position
  *   states     optional out [B][ceil(T / MEMOROID_GATED_STATE_STEPS)][d] fp32, the states
  *              before steps 0, 64, 128 ...: what the gradient starts from.
  *   Gates may be infinite: r = -inf holds the state and lets nothing in (a = 1, b = 0),
- *   r = inf takes the whole rate.  A NaN (or an infinite x) stays in its feature's episode
- *   and in the steps from its own on.  States are fp32; b, a and their products are right
- *   to a few 2^-24; h is rounded to bf16 once.  Results do not depend on timing.
+ *   r = inf takes the whole rate.  A NaN (or an infinite x or state) stays in its feature's
+ *   episode and in the steps from its own on, where an infinity may be a NaN (a decay is
+ *   applied as h - (1 - a) h).  States are fp32 and h is rounded to bf16 once.  Right to a
+ *   few 2^-24 of themselves are the sigmoids, b and, up to u = 1/2, 1 - a; a itself is off
+ *   by another u 2^-24 beyond, and with bf16 inputs the sigmoid of v by another |v| 2^-24,
+ *   which u, 1 - a and b take over (b by as much as both its gates).  m below 2^-63 may
+ *   count as 0.  Results do not depend on timing.
  *   d <= 2^18, T < 2^30 and B ceil(T / 64) ceil(d / 64) < 2^23 (MEMOROID_EUNSUPPORTED
  *   otherwise).  fp32 arrays 4-byte aligned.  state_out must
  *   not be state_in.  Workspace (self-initialising): memoroid_scan_gated_workspace_bytes.

@@ -8,7 +8,9 @@
 // itself, and applied as h_before - w h_before + b: a float a near 1 is off by up to
 // 2^-25, at every step the same way where a gate stands still, and a memory of 1 / w
 // steps with it by 2^-25 / w (3e-4 at w = 1e-4); m would lose the same digits to 1 - a^2.
-// A fast one is a itself: what little it leaves of a state has to be right, too.
+// A fast one is a itself, off by u 2^-24 of it (the exponent's product): what little it
+// leaves of a state has to be right, too.  (An infinite state turns into NaN under a slow
+// decay: inf - inf.)
 #pragma once
 
 #include "scan_common.hpp"
@@ -20,7 +22,8 @@ constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kLog2eLow = 1.92596299112661746e-08f;    // log2(e) less the float above
 constexpr float kSlow = 0.5f;                            // decays up to exp(-1/2) are slow
 
-// exp(-v).  FAST: one rounded product into the hardware's 2^y, off by |v| 2^-24; else
+// exp(-v).  FAST, for bf16 gates, whose own steps are 2^-9 of v and move the result by far
+// more: one rounded product into the hardware's 2^y, off by |v| 2^-24; else
 // by 2^-23 whatever v (the product's integer part taken out before it can cost the
 // fraction its digits).  v = NaN stays, +-inf give 0 and inf.
 template <bool FAST>
