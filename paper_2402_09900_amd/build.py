@@ -4,11 +4,12 @@ _torch_layer.so (calls on torch tensors and autograd nodes, host code) with g++.
     python -m paper_2402_09900_amd.build
 
 Both are always rebuilt (a few minutes); the results land next to this file,
-where the binding loads them from.
+where the binding loads them from.  Without torch the library alone is built.
 """
 from __future__ import annotations
 
 import glob
+import importlib.util
 import os
 import subprocess
 import sys
@@ -65,17 +66,23 @@ def _layer_commands(obj, tmp):
 def build(verbose: bool = False) -> str:
     end = ".tmp%d" % os.getpid()
     obj = os.path.join(HERE, "torch_layer%s.o" % end)
-    compile_layer, link_layer = _layer_commands(obj, LAYER + end)
-    layer = _run(compile_layer, verbose)
+    layer = None
+    if importlib.util.find_spec("torch") is not None:
+        compile_layer, link_layer = _layer_commands(obj, LAYER + end)
+        layer = _run(compile_layer, verbose)
+    else:
+        print("no torch here: building libmemoroid.so alone", flush=True)
     library = _run(["hipcc"] + FLAGS + ["-o", LIB + end] + sources(), verbose)
     try:
         _done(library)
         os.replace(LIB + end, LIB)
-        _done(layer)
-        _done(_run(link_layer, verbose))
-        os.replace(LAYER + end, LAYER)
+        if layer is not None:
+            _done(layer)
+            _done(_run(link_layer, verbose))
+            os.replace(LAYER + end, LAYER)
     finally:
-        layer.wait()
+        if layer is not None:
+            layer.wait()
         if os.path.exists(obj):
             os.remove(obj)
     return LIB
