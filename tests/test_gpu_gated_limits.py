@@ -147,3 +147,116 @@ def test_bad_states_stay_in_their_episode(bad, dtype, rates):
     assert not bool(ok[0, 7])
     ok[0, 7] = True
     assert bool(ok.all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,T,d", [(2, 131, 70), (3, 31, 2), (1, 60, 130), (2, 200, 256), (2, 64, 66)])
+def test_nothing_behind_even_rows(dtype, B, T, d):
+    """Rows of pairs at even addresses, whose last columns fill a chain partly or wholly:
+    guards around every output, and behind the workspaces."""
+    announce("gated guards of even rows %s B=%d T=%d d=%d" % (dtype, B, T, d))
+    s = inputs(dtype, B, T, d, "some", True, 6)
+    want = mb.scan_gated(*(s[k].to(DEV) for k in ("x", "gates", "alpha", "start", "state")), final_state=True, keep_states=True)
+    want += mb.scan_gated_bwd(*(s[k].to(DEV) for k in ("x", "gates", "alpha", "start")), want[2], s["grad_h"].to(DEV),
+                              s["grad_state"].to(DEV))
+
+    def shifted(t):
+        buf = torch.full((t.numel() + 132,), 7, dtype=t.dtype, device=DEV)
+        view = buf[66:66 + t.numel()].view(t.shape)
+        view.copy_(t)
+        return buf, view
+
+    p = {k: shifted(v)[1] for k, v in s.items()}
+    outs = [shifted(torch.zeros_like(t)) for t in want]
+    o = [v.data_ptr() for _, v in outs]
+    dt = mb.F32 if dtype == "f32" else mb.BF16
+    n = max(mb.memoroid_scan_gated_workspace_bytes(B, T, d, dt), mb.memoroid_scan_gated_bwd_workspace_bytes(B, T, d, dt))
+    ws = torch.randint(0, 256, (n + 512,), dtype=torch.uint8, device=DEV)
+    keep = ws[n:].clone()
+    st = torch.cuda.current_stream().cuda_stream
+    a = [p[k].data_ptr() for k in ("x", "gates", "alpha", "start", "state", "grad_h", "grad_state")]
+    assert mb.memoroid_scan_gated(*a[:5], o[0], o[1], o[2], B, T, d, dt, ws.data_ptr(), n, st) == mb.OK
+    assert mb.workspace_status(ws) == mb.OK
+    assert mb.memoroid_scan_gated_bwd(*a[:4], o[2], a[5], a[6], o[3], o[4], o[5], o[6], B, T, d, dt, ws.data_ptr(), n,
+                                      st) == mb.OK
+    assert mb.workspace_status(ws) == mb.OK
+    for (buf, view), w in zip(outs, want):
+        assert torch.equal(view, w)
+        assert bool((buf[:66] == 7).all()) and bool((buf[66 + w.numel():] == 7).all())
+    assert torch.equal(ws[n:], keep)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shift", [0, 1, 2, 4])
+@pytest.mark.parametrize("B,d", [(3, 70), (2, 256), (5, 33), (1, 1)])
+def test_step_at_any_address(dtype, shift, B, d):
+    """A step's operands at any element, guards around what it writes."""
+    announce("gated step guards %s shift=%d B=%d d=%d" % (dtype, shift, B, d))
+    s = inputs(dtype, B, 1, d, "dense", True, 3)
+    t = dict(x=s["x"][:, 0], gates=s["gates"][:, 0], alpha=s["alpha"], state=s["state"], start=s["start"][:, 0])
+    c = {k: v.contiguous().to(DEV) for k, v in t.items()}
+    state = c["state"].clone()
+    want = mb.gated_step(c["x"], c["gates"], c["alpha"], state, c["start"])
+    at = {}
+    for k, v in (*c.items(), ("h", torch.zeros_like(want))):
+        buf = torch.full((v.numel() + 64 + shift,), 7, dtype=v.dtype, device=DEV)
+        buf[32 + shift:32 + shift + v.numel()] = v.flatten()
+        at[k] = buf
+    p = {k: v.data_ptr() + (32 + shift) * v.element_size() for k, v in at.items()}
+    assert mb.memoroid_gated_step(p["x"], p["gates"], p["alpha"], p["start"], p["state"], p["h"], B, d,
+                                  mb.F32 if dtype == "f32" else mb.BF16, torch.cuda.current_stream().cuda_stream) == mb.OK
+    for k, w in (("h", want), ("state", state)):
+        buf = at[k]
+        assert torch.equal(buf[32 + shift:32 + shift + w.numel()].view(w.shape), w)
+        assert bool((buf[:32 + shift] == 7).all()) and bool((buf[32 + shift + w.numel():] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_runs_of_many_chains_are_equal(dtype):
+    """As many chains as one wavefront looks back for alone, and other work between the runs."""
+    announce("gated equal runs of many chains %s" % dtype)
+    s = inputs(dtype, 1, 16384, 1100, "none", True, 9)
+    c = {k: v.to(DEV) for k, v in s.items()}
+    first = None
+    for turn in range(8):
+        got = mb.scan_gated(c["x"], c["gates"], c["alpha"], c["start"], c["state"], final_state=True, keep_states=True)
+        got += mb.scan_gated_bwd(c["x"], c["gates"], c["alpha"], c["start"], got[2], c["grad_h"], c["grad_state"])
+        if first is None:
+            first = [t.clone() for t in got]
+        assert all(torch.equal(x, y) for x, y in zip(first, got)), turn
+        if turn % 2:
+            c["x"].float().exp().sum()
+
+
+def test_gradients_past_32_bits():
+    """More than 2^31 values: alpha's and the state's gradient are those of the last tape
+    alone.  A gradient that arrives in one tile of that tape alone, behind a begin step, leaves
+    one row of sums that is not zero, so alpha's is the same bit for bit."""
+    announce("gated gradients past 2^31 values")
+    B, T, d = 9, 65536, 4096
+    g = torch.Generator(device=DEV)
+    g.manual_seed(2)
+    bx, bg = torch.zeros(B, T, d, device=DEV, dtype=torch.bfloat16), torch.zeros(B, T, 2, d, device=DEV, dtype=torch.bfloat16)
+    bs, alpha = torch.zeros(B, T, device=DEV, dtype=torch.uint8), torch.rand(d, device=DEV, generator=g) * 0.1
+    bx[-1] = torch.randn(T, d, device=DEV, generator=g)
+    bg[-1] = torch.randn(T, 2, d, device=DEV, generator=g)
+    bs[-1, 1:] = (torch.rand(T - 1, device=DEV, generator=g) < 0.0001).to(torch.uint8)
+    up, state = torch.zeros(B, d, device=DEV), torch.zeros(B, d, device=DEV)
+    up[-1], state[-1] = torch.randn(d, device=DEV, generator=g), torch.randn(d, device=DEV, generator=g)
+    lone = [t[-1:].contiguous() for t in (bx, bg, bs, state, up)]
+    _, kept = mb.scan_gated(bx, bg, alpha, bs, state, keep_states=True)
+    _, lkept = mb.scan_gated(lone[0], lone[1], alpha, lone[2], lone[3], keep_states=True)
+    assert torch.equal(kept[-1], lkept[0])
+    got = mb.scan_gated_bwd(bx, bg, alpha, bs, kept, bx, up)
+    want = mb.scan_gated_bwd(lone[0], lone[1], alpha, lone[2], lkept, lone[0], lone[4])
+    assert torch.equal(got[3][-1], want[3][0]) and bool(want[3].any()) and not bool(got[3][:-1].any())
+    del got
+    bs[-1, T - 64] = 1
+    gh = torch.zeros_like(bx)
+    gh[-1, T - 64:] = bx[-1, T - 64:]
+    lone[2] = bs[-1:].contiguous()
+    _, kept = mb.scan_gated(bx, bg, alpha, bs, state, keep_states=True)
+    _, lkept = mb.scan_gated(lone[0], lone[1], alpha, lone[2], lone[3], keep_states=True)
+    got = mb.scan_gated_bwd(bx, bg, alpha, bs, kept, gh, up)[2]
+    want = mb.scan_gated_bwd(lone[0], lone[1], alpha, lone[2], lkept, gh[-1:].contiguous(), lone[4])[2]
+    assert torch.equal(got, want) and bool(want.all())

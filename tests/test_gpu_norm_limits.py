@@ -1,8 +1,9 @@
 """Layer norm where values come near the ends of fp32's range, and past 2^31 elements."""
 import pytest
 
-from conftest import announce
-from test_gpu_norm import DEV, DT
+import gated_ref as ref
+from conftest import announce, cond_err
+from test_gpu_norm import DEV, DT, E, np64
 
 torch = pytest.importorskip("torch")
 from paper_2402_09900_amd import binding as mb  # noqa: E402
@@ -36,3 +37,21 @@ def test_rows_whose_sum_is_past_the_range(dtype, d, size):
     gy, gs = torch.randn_like(x), torch.randn_like(x)
     dx, dres, dw, db = mb.norm_rows_bwd(x, st, gy, w, torch.zeros_like(x), gs)
     assert torch.equal(dx[1:4], gs[1:4]) and bool(torch.isfinite(dx).all()) and bool(torch.isfinite(dw).all())
+
+
+def test_weights_past_32_bits():
+    """More than 2^31 elements of which the last 64 rows are not zero: the gradients of weight
+    and bias against those rows' in 64 bits (144 E: test_gpu_norm.py)."""
+    announce("norm weights past 2^31 elements")
+    n, d, m = 1050000, 2048, 64
+    g = torch.Generator(device=DEV)
+    g.manual_seed(2)
+    x, gy = (torch.zeros(n, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    for t in (x, gy):
+        t[-m:] = torch.randn(m, d, device=DEV, generator=g).to(torch.bfloat16)
+    w = torch.rand(d, device=DEV, generator=g)
+    _, st = mb.norm_rows(x, w, keep_stats=True)
+    _, _, dw, db = mb.norm_rows_bwd(x, st, gy, w)
+    _, gw, gb = ref.norm_grads(np64(x[-m:]), np64(w), 1e-5, np64(gy[-m:]))
+    assert cond_err(np64(dw), *gw) <= 144 * E
+    assert cond_err(np64(db), *gb) <= 144 * E
