@@ -1534,11 +1534,12 @@ GatedTiles gated_tiles(const GatedPlan& p, void* workspace, uint64_t sig) {
     t.nfb = p.nfb;
     t.nchains = p.nchains;
     // With many chains few tiles of one are under way at once, and the value before a tile
-    // is soon near it; looking further costs more than it finds (T = 65536, d = 2048, 32
-    // chains, bf16: 233 us, 278 with one turn before all wavefronts look).  With few it
-    // pays (d = 512, no episode's begin: 182 -> 126 us; d = 256, fp32 326 -> 211, and 156 since
-    // what was found is read in blocks), after some turns where begins are frequent (T = 32768, d =
-    // 256, fp32, gradient: 70.1 us after three, 68.1 after 16; d = 512, bf16, no begin: 174 and 207).
+    // is soon near it; looking further costs more than it finds.  With few it pays, after some
+    // turns of the first wavefront alone where begins are frequent (T = 32768, d = 256, fp32,
+    // gradient: 70.1 us after three, 68.1 after 16).  All look after four turns / the first
+    // alone, T = 65536, bf16, us, forward and gradient without a begin, forward with one every
+    // 500 steps: 8 chains 97 / 132, 179 / 257, 71 / 68; 12 114 / 136, 238 / 267, 98 / 96; 16 141 /
+    // 153, 295 / 291, 122 / 119; 24 198 / 184, 385 / 358, 171 / 169; 32 233 / 227, 447 / 447, 219 / 217.
     t.near = p.nchains >= 16 ? kMaxPolls : 4;
     t.ctr = (uint32_t*)(ws + p.off_ctr);
     t.agg = (uint64_t*)(ws + p.off_agg);

@@ -533,7 +533,7 @@ struct NormArgs {
     float* stats;               // [n][2]: mean, 1 / deviation; or NULL
     DropArgs drop;
     float eps;
-    int64_t n, d, rows;         // rows of a wavefront (set by the launch)
+    int64_t n, d, rows;         // rows of a lane, one after the other (set by the launch)
 };
 struct NormBwdArgs {
     const void* x;

@@ -562,8 +562,10 @@ void with_rows(bool bf16, bool few, int64_t n, int64_t d, F&& f) {
 }
 
 // Rows that a lane sees one after the other, so that about `groups` workgroups of four
-// wavefronts, and never a few more, take all: at most 64, which is as many floats as a sum for the
-// weights adds before it goes on in doubles.
+// wavefronts, and never a few more, take all: at most 64 (more past 2^26 workgroups of one row a
+// lane).  A sum for the weights adds them as floats; where a workgroup has rows side by side,
+// the 64 / lanes in a wavefront and then the four wavefronts are floats too.  Over the
+// workgroups it goes on in doubles.
 int64_t rows_of(int64_t n, const Shape& sh, int64_t groups) {
     const int64_t steps = (n + sh.at_once - 1) / sh.at_once;   // workgroups with a row a lane
     if (sh.waves > 4) groups = groups * 4 / sh.waves;
@@ -574,11 +576,14 @@ int64_t rows_of(int64_t n, const Shape& sh, int64_t groups) {
 int64_t groups_of(int64_t n, const Shape& sh, int64_t rows) { return (n + sh.at_once * rows - 1) / (sh.at_once * rows); }
 
 // The gradient's rows: 1024 workgroups at most run at once, with a row's loads on the way.
-// With a residual (and two more tensors to read) half of them do, and leave half as
-// many sums (32768 x 2048 bf16: 178 -> 166 us; without a residual 92, and 104 with 512); wide rows, whose
-// wavefronts wait for one another, need all (d = 4096: 160 and 183 us).
+// With a residual (and two more tensors to read) half of them do, and leave half as many
+// sums.  In us with 512 and 1024, bf16 (fp32): with a residual 262144 x 256 123 and 134 (268 and
+// 274), 32768 x 2048 124 and 136 (268 and 277); without 94 and 82 (159 and 165), 101 and 86 (160
+// and 168).  Rows that are no whole octets, whose last ones straddle lines, and wide ones,
+// whose wavefronts wait for one another, need all of them: with a residual 262144 x 250 187 and
+// 150 (302 and 274), 32768 x 2047 198 and 156 (306 and 281), 16384 x 4096 139 and 128 (270 and 271).
 int64_t bwd_groups(const Shape& sh, int64_t d, bool residual) {
-    return sh.waves <= 4 && d % 8 == 0 && (residual || sh.waves == 1) ? 512 : 1024;
+    return residual && sh.waves <= 4 && d % 8 == 0 ? 512 : 1024;
 }
 
 }  // namespace
