@@ -249,8 +249,10 @@ Tensor drop(const Tensor& x, double p, const Tensor& rng, int64_t site, const Te
 // that has formed them, and the gradients that it was given.
 variable_list once(variable_list got, const variable_list& upstream) {
     if (!at::GradMode::is_enabled()) return got;
+    const auto by = torch::autograd::get_current_node();
+    if (!by) throw std::runtime_error("a graph of gradients needs torch's engine to call the backward pass");
     torch::autograd::edge_list to;
-    for (const auto& e : torch::autograd::get_current_node()->next_edges())
+    for (const auto& e : by->next_edges())
         if (e.is_valid()) to.push_back(e);
     for (const Tensor& g : upstream)
         if (g.defined() && g.requires_grad()) to.push_back(torch::autograd::impl::gradient_edge(g));
