@@ -13,7 +13,7 @@
 // kernel in doubles.
 //
 // Seven tensors are read or written once: 8 tapes of 4096 steps of 2048 bf16 features, 0.94
-// GB in 205 us, 4.6 TB/s, the VALU busy for 127 of them (66 instructions a value); fp32, 8 x
+// GB in 205 us, 4.6 TB/s, the VALU busy for 130 of them (67 instructions a value); fp32, 8 x
 // 4096 x 1024, 190 us.  A step's coefficients that do not wait for the carry (m sig(i), v (1 -
 // sig(i)), sig(i) x a / m) are formed before it comes: 264 -> 234 us beside forming all gates
 // twice.  The registers (five floats a step and feature) set the tile: 16 steps a lane leave room

@@ -184,8 +184,8 @@ __device__ __forceinline__ Place place_of(int64_t n, int64_t d, int64_t rows) {
     return p;
 }
 
-// A row's values are summed up as 2^-14 of them, which costs nothing and changes no digit: the sum
-// of as many as a row may have stays in the range that they are in
+// A row's values are summed up as 2^-14 of them, which costs no instruction and, above 2^-112,
+// changes no digit: the sum of as many as a row may have stays in the range that they are in
 constexpr float kSumScale = 0x1p-14f;
 static_assert((float)kNormMaxDim * kSumScale <= 1.0f, "the longest rows");
 
