@@ -164,3 +164,56 @@ def test_tensors_without_memory_are_refused(through):
         with pytest.raises((RuntimeError, ValueError)):
             wrap(f)(t)
             assert False, "call %d went through" % n
+
+
+@pytest.mark.gpu
+def test_onlookers_see_the_same_results():
+    """Dispatch modes that only look on, a level of forward mode that no input belongs to,
+    and both kinds of checkpointing: the results and gradients of a plain call."""
+    from torch.utils._python_dispatch import TorchDispatchMode
+    from torch.utils.checkpoint import CheckpointPolicy, checkpoint, create_selective_checkpoint_contexts
+    from torch.utils.flop_counter import FlopCounterMode
+
+    class Looks(TorchDispatchMode):
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            return func(*args, **(kwargs or {}))
+
+    announce("transforms: onlookers")
+    dev = "cuda:0"
+    torch.manual_seed(0)
+    x, res = (torch.randn(2, 300, 8, device=dev) for _ in range(2))
+    gates, alpha = torch.randn(2, 300, 2, 8, device=dev), torch.rand(8, device=dev)
+    start, rng = torch.zeros(2, 300, dtype=torch.uint8, device=dev), RNG.to(dev)
+    up = torch.randn_like(x)
+    leaves = [t.requires_grad_(True) for t in (x, res, gates, alpha)]
+
+    def block(x, res, gates, alpha):
+        y, s = mb.layer_norm(x, alpha, residual=res, p=0.1, rng=rng)
+        return mb.dropout(mb.gated_scan(y, gates, alpha, start), 0.2, rng, 1, s)
+
+    def both(f=block):
+        y = f(*leaves)
+        y.backward(up)
+        got = (y.detach(), *[t.grad for t in leaves])
+        for t in leaves:
+            t.grad = None
+        return got
+
+    want = both()
+
+    def policy(ctx, op, *args, **kwargs):
+        return CheckpointPolicy.MUST_SAVE
+
+    def same(got):
+        return all(torch.equal(a, b) for a, b in zip(got, want))
+
+    with FlopCounterMode(display=False):
+        assert same(both())
+    with Looks():
+        assert same(both())
+    with fwd.dual_level():
+        assert same(both())
+    assert same(both(lambda *a: checkpoint(block, *a, use_reentrant=False)))
+    assert same(both(lambda *a: checkpoint(block, *a, use_reentrant=True)))
+    assert same(both(lambda *a: checkpoint(block, *a, use_reentrant=False,
+                                           context_fn=lambda: create_selective_checkpoint_contexts(policy))))
